@@ -28,8 +28,9 @@
  *   - Tensor pointers must be 16-byte aligned (they are read and written with vector accesses);
  *     a misaligned pointer is rejected with FOCUS_ERR_SHAPE.
  *   - Results are deterministic: every floating-point reduction has a fixed order and no kernel of
- *     the scale-learning step uses atomics. The only atomics in the library are integer additions
- *     to focus_kl_top's radix-select histogram in LDS, whose counts do not depend on their order.
+ *     the scale-learning step uses atomics. The only atomics in the library are integer additions in
+ *     LDS, to focus_kl_top's radix-select histogram and to focus_token_logprobs' counts of alternatives,
+ *     whose results do not depend on their order.
  */
 #ifndef FOCUS_H
 #define FOCUS_H
@@ -109,7 +110,13 @@ typedef enum {
     FOCUS_CALL_RECON_GEMM_DX = 7,
     FOCUS_CALL_FAKEQUANT_ACT_BWD = 8,
     FOCUS_CALL_KL_TOP = 9,
-    FOCUS_CALL_FAKEQUANT_WEIGHTS = 10
+    FOCUS_CALL_FAKEQUANT_WEIGHTS = 10,
+    FOCUS_CALL_NORM_FWD = 11,       /* M = tokens, K = features */
+    FOCUS_CALL_NORM_BWD = 12,       /* M = tokens, K = features */
+    FOCUS_CALL_ATTENTION_FWD = 13,  /* sized by focus_attention_workspace_size */
+    FOCUS_CALL_ATTENTION_BWD = 14,  /* sized by focus_attention_workspace_size */
+    FOCUS_CALL_TOKEN_LOGPROBS = 15, /* M = tokens, N = vocabulary, K = alternatives (`top`) */
+    FOCUS_CALL_TOKEN_LOGPROBS_BWD = 16
 } focus_call;
 
 /* Workspace bytes a call needs for the given sizes (M = tokens, N = rows / out features,
@@ -364,11 +371,124 @@ typedef struct {
 focus_status focus_adamw_step(const focus_adamw_config *cfg, int64_t t, int64_t n, float *param, const float *grad,
                               float *exp_avg, float *exp_avg_sq, void *ws, size_t ws_bytes, focus_stream stream);
 
+/* ---- operators around the linears of a decoder block -------------------------------------------
+ * The end-to-end objective (Sec. 4.1) runs through whole decoder blocks: the norms and the attention between the
+ * quantised linears, and the log probabilities that a calibrated model is scored by. These calls take and give
+ * unquantised tensors; the conventions at the top hold for them too. */
+
+typedef enum { FOCUS_NORM_LAYER = 0, FOCUS_NORM_RMS = 1 } focus_norm_kind;
+
+/* Layer norm or RMS norm of T tokens of C features, with an optional residual sum in front of it:
+ *   H = X + residual, rounded to dtype (without a residual: H = X, and H_out must be NULL)
+ *   layer: mean = (1/C) sum H, rstd = 1 / sqrt((1/C) sum (H - mean)^2 + eps); RMS: the same with mean = 0
+ *   Y = (H - mean) rstd weight + bias
+ *   X, residual_opt, H_out, Y [T][C] (dtype); weight, bias_opt [C] (w_dtype, either type); sums in fp32.
+ *   mean_opt (layer only), rstd_opt [T] fp32: what the backward needs; NULL where it is not wanted.
+ *   H_out may alias X or residual_opt, Y may alias X.
+ * 0 <= T < 2^31, 0 <= C <= 2^24 (FOCUS_ERR_SHAPE); eps >= 0 and finite, kind as above, mean_opt NULL for RMS
+ * (FOCUS_ERR_CONFIG). ws: focus_workspace_size(FOCUS_CALL_NORM_FWD, NULL, T, 0, C) bytes. */
+focus_status focus_norm_fwd(int kind, float eps, const void *X, const void *residual_opt, int dtype, int64_t T, int64_t C,
+                            const void *weight, const void *bias_opt, int w_dtype, void *H_out, void *Y, float *mean_opt,
+                            float *rstd_opt, void *ws, size_t ws_bytes, focus_stream stream);
+
+/* Its backward pass. With xh = (H - mean) rstd and g = dY weight:
+ *   dX = rstd (g - mean_c(g) - xh mean_c(g xh)) + dH_opt      (RMS: without mean_c(g))
+ *   dweight = sum over tokens of dY xh,  dbias = sum over tokens of dY      (fp32, overwritten)
+ *   H [T][C] is the norm's input: H_out of the forward, or X where it had no residual. dH_opt [T][C] is the gradient that
+ *   reaches H past the norm (the residual stream's), or NULL. dX is the gradient of X and of the residual alike.
+ *   mean (layer only; NULL for RMS) and rstd [T] as the forward wrote them. dY, H, dH_opt, dX in dtype; dX may alias dY or
+ *   dH_opt. dbias_opt may be NULL. With T == 0 dweight and dbias are zeros.
+ * The sums over tokens have a fixed order. ws: focus_workspace_size(FOCUS_CALL_NORM_BWD, NULL, T, 0, C) bytes. */
+focus_status focus_norm_bwd(int kind, const void *dY, const void *H, int dtype, int64_t T, int64_t C, const void *weight,
+                            int w_dtype, const float *mean, const float *rstd, const void *dH_opt, void *dX, float *dweight,
+                            float *dbias_opt, void *ws, size_t ws_bytes, focus_stream stream);
+
+/* Shapes of an attention call.
+ *   heads_q, heads_kv : query heads and key-value heads; heads_q is a multiple of heads_kv, and query head h reads key-value
+ *               head h / (heads_q / heads_kv).
+ *   head_dim  : features per head, a multiple of 8 up to 128.
+ *   causal    : 1 -> a query sees the keys up to its own place, the sequence's last query standing at its last key (with
+ *               as many keys as queries the usual mask; with more keys the queries are their end); 0 -> it sees all.
+ *   scale     : factor of the scores, finite (1 / sqrt(head_dim) as a rule).
+ *   *_stride  : elements between consecutive tokens of q, k, v and of the gradients; 0 -> contiguous, heads x head_dim.
+ *               A token's heads are contiguous. At least heads x head_dim and 16 bytes' multiple, so that slices of one fused
+ *               q-k-v product can be passed as they lie. */
+typedef struct {
+    int32_t heads_q;
+    int32_t heads_kv;
+    int32_t head_dim;
+    int32_t causal;
+    float scale;
+    int32_t reserved; /* 0 */
+    int64_t q_stride, k_stride, v_stride;
+    int64_t dq_stride, dk_stride, dv_stride;
+} focus_attention_config;
+
+/* Workspace bytes of focus_attention_fwd (call = FOCUS_CALL_ATTENTION_FWD) and focus_attention_bwd
+ * (FOCUS_CALL_ATTENTION_BWD). Host-only; 0 for invalid arguments. */
+size_t focus_attention_workspace_size(int call, const focus_attention_config *cfg, int64_t Tq, int64_t Tk, int64_t n_seq);
+
+/* Attention over whole prompts, several sequences packed one after the other without padding:
+ *   S = scale q k^T (hidden keys at -inf), P = softmax(S), O = P v, lse = log sum exp S, per sequence and head.
+ *   q [Tq][heads_q][head_dim], k, v [Tk][heads_kv][head_dim], O [Tq][heads_q][head_dim] contiguous (dtype);
+ *   lse_opt [heads_q][Tq] fp32 (the backward needs it).
+ *   cu_q, cu_k : DEVICE arrays of n_seq + 1 int32, sequence s holding queries cu_q[s] .. cu_q[s + 1] - 1 and keys
+ *               cu_k[s] .. cu_k[s + 1] - 1; they may be one array. Both NULL: one sequence of everything (n_seq == 1).
+ *               They rise and lie in [0, Tq] and [0, Tk]; a pair that does not raises the domain flag and its sequence is
+ *               treated as empty. Rows of no sequence are neither read nor written.
+ *   A query that sees no key (none there, or causal with fewer keys than queries) has O = 0 and lse = -inf.
+ *   Nothing outside a query's own sequence reaches its output, NaN and infinities included. A hidden key of its own
+ *   sequence does not either, as long as its v is finite.
+ *   bf16: products on the bf16 matrix instructions with fp32 sums, probabilities rounded to bf16 for the second product;
+ *   fp32: fp32 products throughout. Tq, Tk <= 2^30, n_seq <= 2^24, heads_q <= 65535.
+ *   Tensor pointers 16-byte aligned, lse and cu_* element-aligned. */
+focus_status focus_attention_fwd(const focus_attention_config *cfg, const void *q, const void *k, const void *v, int dtype,
+                                 int64_t Tq, int64_t Tk, const int32_t *cu_q, const int32_t *cu_k, int64_t n_seq, void *O,
+                                 float *lse_opt, void *ws, size_t ws_bytes, focus_stream stream);
+
+/* Its backward pass: from dO [Tq][heads_q][head_dim] and the forward's O and lse,
+ *   dv = P^T dO, dP = dO v^T, dS = P (dP - rowsum(dO O)), dq = scale dS k, dk = scale dS^T q,
+ * dk and dv summed over the query heads that share a key-value head. P is formed again from lse; bf16: P and dS are
+ * rounded to bf16 for the products. dq, dk, dv in dtype, with cfg's gradient strides; keys that no query sees get zeros.
+ * No atomics: every sum has a fixed order. */
+focus_status focus_attention_bwd(const focus_attention_config *cfg, const void *dO, const void *q, const void *k,
+                                 const void *v, const void *O, const float *lse, int dtype, int64_t Tq, int64_t Tk,
+                                 const int32_t *cu_q, const int32_t *cu_k, int64_t n_seq, void *dq, void *dk, void *dv,
+                                 void *ws, size_t ws_bytes, focus_stream stream);
+
+#define FOCUS_MAX_TOP 64
+
+/* Log probabilities of given tokens under rows of logits Z [T][V] (dtype; element-aligned rows of any V), with the
+ * entropy and the largest alternatives of each row:
+ *   lse[t] = log sum_i exp Z[t][i]                                        (fp32 [T])
+ *   logp_opt[t] = Z[t][target[t]] - lse[t]; 0 where target[t] < 0 (a token left out)
+ *   entropy_opt[t] = -sum_i p_i log p_i, p = softmax(Z[t])
+ *   top_logp, top_index [T][top]: log probability and index of the `top` largest logits, largest first, equal logits by
+ *     rising index; with V < top the rest is -inf and -1. Both NULL with top == 0.
+ *   target_opt [T] int64 (NULL: none, logp_opt must be NULL too).
+ * A logit of -inf is a masked token of probability 0; a row of nothing else has lse = logp = -inf and entropy 0.
+ * A NaN or +inf logit, and a target >= V (taken as left out), raise the domain flag; the row's results are then unspecified.
+ * T < 2^31, 1 <= V < 2^31, 0 <= top <= FOCUS_MAX_TOP (FOCUS_ERR_CONFIG). T == 0 is a no-op.
+ * ws: focus_workspace_size(FOCUS_CALL_TOKEN_LOGPROBS, NULL, T, V, top) bytes. */
+focus_status focus_token_logprobs(const void *Z, int dtype, int64_t T, int64_t V, const int64_t *target_opt, int32_t top,
+                                  float *logp_opt, float *entropy_opt, float *lse, float *top_logp, int32_t *top_index,
+                                  void *ws, size_t ws_bytes, focus_stream stream);
+
+/* Its gradient: with g = d_logp[t] (0 where target[t] < 0) and h = d_entropy[t],
+ *   dZ[t][i] = g ([i == target[t]] - p_i) - h p_i (log p_i + entropy[t]),   p_i = exp(Z[t][i] - lse[t])
+ * (the mean cross entropy of the T tokens is d_logp = -1/T). lse and entropy as the forward wrote them. d_logp_opt needs
+ * target_opt, d_entropy_opt needs entropy_opt; one of the two is given at least (FOCUS_ERR_NULL). dZ [T][V] (dtype) may
+ * alias Z. ws: focus_workspace_size(FOCUS_CALL_TOKEN_LOGPROBS_BWD, NULL, T, V, 0) bytes. */
+focus_status focus_token_logprobs_bwd(const void *Z, int dtype, int64_t T, int64_t V, const int64_t *target_opt,
+                                      const float *lse, const float *entropy_opt, const float *d_logp_opt,
+                                      const float *d_entropy_opt, void *dZ, void *ws, size_t ws_bytes, focus_stream stream);
+
 /* Synchronises `stream`, reads and clears the workspace's sticky domain flag. Returns
  * FOCUS_ERR_DOMAIN if any call on this workspace met a NaN scale or a coefficient c that is
  * <= 0 or not finite, a log2-domain AdamW step met a parameter that is not positive and
- * finite, or focus_kl_top met a logit that is not finite, since the last check (outputs of such blocks are unspecified), FOCUS_OK
- * otherwise, FOCUS_ERR_HIP on a runtime error. */
+ * finite, focus_kl_top met a logit that is not finite, focus_attention_* met sequence ends that do not rise, or
+ * focus_token_logprobs met a NaN or +inf logit or a target past the vocabulary, since the last check (outputs of such
+ * blocks are unspecified), FOCUS_OK otherwise, FOCUS_ERR_HIP on a runtime error. */
 focus_status focus_check_flags(void *ws, focus_stream stream);
 
 /* Static description of a status code. */

@@ -123,6 +123,57 @@ size_t noalloc_fwd_scratch_bytes(int64_t M, int64_t N, bool have_col_sq) {
     return kWsHeader + (mtiles * (size_t)N + (have_col_sq ? 0 : (size_t)N)) * sizeof(double);
 }
 
+// ---- operators around the linears ---------------------------------------------------------------
+focus_status check_norm_shape(int64_t T, int64_t C) {
+    return T < 0 || C < 0 || T > kMaxDim || C > (int64_t(1) << 24) ? FOCUS_ERR_SHAPE : FOCUS_OK;
+}
+
+focus_status check_logits(int64_t T, int64_t V) {
+    return T < 0 || V < 1 || T > kMaxDim || V > kMaxDim || (T > 0 && V > kMaxElems / T) ? FOCUS_ERR_SHAPE : FOCUS_OK;
+}
+
+bool aligned_to(std::initializer_list<const void *> ps, uintptr_t bytes) {
+    for (const void *p : ps)
+        if (reinterpret_cast<uintptr_t>(p) % bytes) return false;
+    return true;
+}
+
+bool logits_aligned(const void *Z, int dtype) { return aligned_to({Z}, dtype == FOCUS_BF16 ? 2 : 4); }
+
+// checks the shapes of an attention call and fills them in (the pointers stay unset)
+focus_status attention_args(const focus_attention_config *cfg, int64_t Tq, int64_t Tk, int64_t n_seq, AttnArgs &a) {
+    if (!cfg) return FOCUS_ERR_NULL;
+    if (cfg->causal != 0 && cfg->causal != 1) return FOCUS_ERR_CONFIG;
+    if (!std::isfinite(cfg->scale) || cfg->reserved != 0) return FOCUS_ERR_CONFIG;
+    const int64_t hq = cfg->heads_q, hkv = cfg->heads_kv, d = cfg->head_dim;
+    if (hq < 1 || hkv < 1 || hq > 65535 || hq % hkv != 0 || d < 8 || d > 128 || d % 8 != 0) return FOCUS_ERR_SHAPE;
+    constexpr int64_t kMaxTokens = int64_t(1) << 30;
+    if (Tq < 0 || Tk < 0 || n_seq < 0 || Tq > kMaxTokens || Tk > kMaxTokens || n_seq > (int64_t(1) << 24)) return FOCUS_ERR_SHAPE;
+    a = AttnArgs{};
+    const int64_t rq = hq * d, rk = hkv * d;
+    const int64_t given[6] = {cfg->q_stride, cfg->k_stride, cfg->v_stride, cfg->dq_stride, cfg->dk_stride, cfg->dv_stride};
+    int64_t *const out[6] = {&a.q_stride, &a.k_stride, &a.v_stride, &a.dq_stride, &a.dk_stride, &a.dv_stride};
+    for (int i = 0; i < 6; i++) {
+        const int64_t row = i % 3 == 0 ? rq : rk;
+        if (given[i] != 0 && (given[i] < row || given[i] > (int64_t(1) << 24))) return FOCUS_ERR_SHAPE;
+        *out[i] = given[i] ? given[i] : row;
+    }
+    a.Tq = Tq, a.Tk = Tk, a.n_seq = (int)n_seq;
+    a.Hq = (int)hq, a.Hkv = (int)hkv, a.D = (int)d, a.causal = cfg->causal, a.scale = cfg->scale;
+    return FOCUS_OK;
+}
+
+// 16-byte rows
+bool strides_ok(const AttnArgs &a, int dtype) {
+    const int64_t e = dtype == FOCUS_BF16 ? 8 : 4;
+    return (a.q_stride | a.k_stride | a.v_stride | a.dq_stride | a.dk_stride | a.dv_stride) % e == 0;
+}
+
+focus_status check_ends(const int32_t *cu_q, const int32_t *cu_k, int64_t n_seq) {
+    if (!cu_q != !cu_k || (!cu_q && n_seq != 1)) return FOCUS_ERR_NULL;
+    return aligned_to({cu_q, cu_k}, 4) ? FOCUS_OK : FOCUS_ERR_SHAPE;
+}
+
 }  // namespace
 
 // One copy per GPU, held until the process ends, shared by every call on that GPU (calls that
@@ -168,6 +219,15 @@ size_t focus_workspace_size(int call, const focus_qconfig *q, int64_t M, int64_t
         if (M < 0 || M > kMaxDim) return 0;
         return kWsHeader + round256((size_t)M * sizeof(double)) + sizeof(double);
     }
+    if (call == FOCUS_CALL_NORM_FWD || call == FOCUS_CALL_NORM_BWD) {  // the operators around the linears: q may be NULL
+        if (check_norm_shape(M, K) != FOCUS_OK) return 0;
+        return call == FOCUS_CALL_NORM_FWD ? kWsHeader : norm_bwd_ws(M, K);
+    }
+    if (call == FOCUS_CALL_TOKEN_LOGPROBS) {
+        if (check_logits(M, N) != FOCUS_OK || K < 0 || K > FOCUS_MAX_TOP) return 0;
+        return logprobs_ws(M, N, (int)K);
+    }
+    if (call == FOCUS_CALL_TOKEN_LOGPROBS_BWD) return check_logits(M, N) == FOCUS_OK ? kWsHeader : 0;
     if (check_q(q) != FOCUS_OK) return 0;
     const int B = block_of(q->format);
     switch (call) {
@@ -443,6 +503,119 @@ focus_status focus_adamw_step(const focus_adamw_config *cfg, int64_t t, int64_t 
     if (n == 0) return FOCUS_OK;
     return hip_status(launch_adamw(cfg->lr, cfg->beta1, cfg->beta2, cfg->eps, cfg->weight_decay, cfg->log2_domain,
                                    t, n, param, grad, exp_avg, exp_avg_sq, flag_of(ws), (hipStream_t)stream));
+}
+
+focus_status focus_norm_fwd(int kind, float eps, const void *X, const void *residual_opt, int dtype, int64_t T, int64_t C,
+                            const void *weight, const void *bias_opt, int w_dtype, void *H_out, void *Y, float *mean_opt,
+                            float *rstd_opt, void *ws, size_t ws_bytes, focus_stream stream) {
+    if (kind != FOCUS_NORM_LAYER && kind != FOCUS_NORM_RMS) return FOCUS_ERR_CONFIG;
+    if (!std::isfinite(eps) || eps < 0.f || (kind == FOCUS_NORM_RMS && mean_opt)) return FOCUS_ERR_CONFIG;
+    if (!dtype_ok(dtype) || !dtype_ok(w_dtype)) return FOCUS_ERR_DTYPE;
+    FOCUS_TRY(check_norm_shape(T, C));
+    if (T > 0 && C > 0 && (!X || !weight || !Y || (residual_opt && !H_out))) return FOCUS_ERR_NULL;
+    if (!residual_opt && H_out) return FOCUS_ERR_CONFIG;
+    if (!all_aligned({X, residual_opt, weight, bias_opt, H_out, Y, mean_opt, rstd_opt})) return FOCUS_ERR_SHAPE;
+    FOCUS_TRY(check_ws(ws, ws_bytes, kWsHeader));
+    if (T == 0 || C == 0) return FOCUS_OK;
+    return hip_status(launch_norm_fwd(kind == FOCUS_NORM_LAYER, eps, dtype, X, residual_opt, T, C, weight, bias_opt, w_dtype,
+                                      H_out, Y, mean_opt, rstd_opt, (hipStream_t)stream));
+}
+
+focus_status focus_norm_bwd(int kind, const void *dY, const void *H, int dtype, int64_t T, int64_t C, const void *weight,
+                            int w_dtype, const float *mean, const float *rstd, const void *dH_opt, void *dX, float *dweight,
+                            float *dbias_opt, void *ws, size_t ws_bytes, focus_stream stream) {
+    if (kind != FOCUS_NORM_LAYER && kind != FOCUS_NORM_RMS) return FOCUS_ERR_CONFIG;
+    if (kind == FOCUS_NORM_RMS && mean) return FOCUS_ERR_CONFIG;
+    if (!dtype_ok(dtype) || !dtype_ok(w_dtype)) return FOCUS_ERR_DTYPE;
+    FOCUS_TRY(check_norm_shape(T, C));
+    if (C > 0 && !dweight) return FOCUS_ERR_NULL;
+    if (T > 0 && C > 0 && (!dY || !H || !weight || !rstd || !dX || (kind == FOCUS_NORM_LAYER && !mean))) return FOCUS_ERR_NULL;
+    if (!all_aligned({dY, H, weight, mean, rstd, dH_opt, dX, dweight, dbias_opt})) return FOCUS_ERR_SHAPE;
+    FOCUS_TRY(check_ws(ws, ws_bytes, norm_bwd_ws(T, C)));
+    if (C == 0) return FOCUS_OK;
+    const hipStream_t st = (hipStream_t)stream;
+    if (T == 0) {  // empty sums
+        const hipError_t e = launch_zero_fill(dweight, (size_t)C * sizeof(float), st);
+        if (e != hipSuccess || !dbias_opt) return hip_status(e);
+        return hip_status(launch_zero_fill(dbias_opt, (size_t)C * sizeof(float), st));
+    }
+    return hip_status(launch_norm_bwd(kind == FOCUS_NORM_LAYER, dtype, dY, H, T, C, weight, w_dtype, mean, rstd, dH_opt, dX,
+                                      dweight, dbias_opt, ws, st));
+}
+
+size_t focus_attention_workspace_size(int call, const focus_attention_config *cfg, int64_t Tq, int64_t Tk, int64_t n_seq) {
+    AttnArgs a;
+    if (attention_args(cfg, Tq, Tk, n_seq, a) != FOCUS_OK) return 0;
+    if (call == FOCUS_CALL_ATTENTION_FWD) return attn_fwd_ws(Tq, Tk, a.Hq, a.Hkv, a.D, n_seq);
+    if (call == FOCUS_CALL_ATTENTION_BWD) return attn_bwd_ws(Tq, Tk, a.Hq, a.Hkv, a.D, n_seq);
+    return 0;
+}
+
+focus_status focus_attention_fwd(const focus_attention_config *cfg, const void *q, const void *k, const void *v, int dtype,
+                                 int64_t Tq, int64_t Tk, const int32_t *cu_q, const int32_t *cu_k, int64_t n_seq, void *O,
+                                 float *lse_opt, void *ws, size_t ws_bytes, focus_stream stream) {
+    AttnArgs a;
+    FOCUS_TRY(attention_args(cfg, Tq, Tk, n_seq, a));
+    if (!dtype_ok(dtype)) return FOCUS_ERR_DTYPE;
+    if ((Tq > 0 && (!q || !O)) || (Tk > 0 && (!k || !v))) return FOCUS_ERR_NULL;
+    FOCUS_TRY(check_ends(cu_q, cu_k, n_seq));
+    if (!all_aligned({q, k, v, O}) || !strides_ok(a, dtype) || (reinterpret_cast<uintptr_t>(lse_opt) & 3u))
+        return FOCUS_ERR_SHAPE;
+    FOCUS_TRY(check_ws(ws, ws_bytes, attn_fwd_ws(Tq, Tk, a.Hq, a.Hkv, a.D, n_seq)));
+    if (Tq == 0 || n_seq == 0) return FOCUS_OK;
+    a.q = q, a.k = k, a.v = v, a.O = O, a.lse = lse_opt, a.cu_q = cu_q, a.cu_k = cu_k, a.flag = flag_of(ws);
+    return hip_status(launch_attn_fwd(dtype, a, ws, (hipStream_t)stream));
+}
+
+focus_status focus_attention_bwd(const focus_attention_config *cfg, const void *dO, const void *q, const void *k,
+                                 const void *v, const void *O, const float *lse, int dtype, int64_t Tq, int64_t Tk,
+                                 const int32_t *cu_q, const int32_t *cu_k, int64_t n_seq, void *dq, void *dk, void *dv,
+                                 void *ws, size_t ws_bytes, focus_stream stream) {
+    AttnArgs a;
+    FOCUS_TRY(attention_args(cfg, Tq, Tk, n_seq, a));
+    if (!dtype_ok(dtype)) return FOCUS_ERR_DTYPE;
+    if ((Tq > 0 && (!q || !O || !dO || !lse || !dq)) || (Tk > 0 && (!k || !v || !dk || !dv))) return FOCUS_ERR_NULL;
+    FOCUS_TRY(check_ends(cu_q, cu_k, n_seq));
+    if (!all_aligned({q, k, v, O, dO, dq, dk, dv}) || !strides_ok(a, dtype) || (reinterpret_cast<uintptr_t>(lse) & 3u))
+        return FOCUS_ERR_SHAPE;
+    FOCUS_TRY(check_ws(ws, ws_bytes, attn_bwd_ws(Tq, Tk, a.Hq, a.Hkv, a.D, n_seq)));
+    if ((Tq == 0 && Tk == 0) || n_seq == 0) return FOCUS_OK;
+    a.q = q, a.k = k, a.v = v, a.O = const_cast<void *>(O), a.dO = dO, a.lse = const_cast<float *>(lse);
+    a.dq = dq, a.dk = dk, a.dv = dv, a.cu_q = cu_q, a.cu_k = cu_k, a.flag = flag_of(ws);
+    return hip_status(launch_attn_bwd(dtype, a, ws, (hipStream_t)stream));
+}
+
+focus_status focus_token_logprobs(const void *Z, int dtype, int64_t T, int64_t V, const int64_t *target_opt, int32_t top,
+                                  float *logp_opt, float *entropy_opt, float *lse, float *top_logp, int32_t *top_index,
+                                  void *ws, size_t ws_bytes, focus_stream stream) {
+    if (!dtype_ok(dtype)) return FOCUS_ERR_DTYPE;
+    if (top < 0 || top > FOCUS_MAX_TOP) return FOCUS_ERR_CONFIG;
+    FOCUS_TRY(check_logits(T, V));
+    if (T > 0 && (!Z || !lse || (top > 0 && (!top_logp || !top_index)) || (logp_opt && !target_opt))) return FOCUS_ERR_NULL;
+    if (!logits_aligned(Z, dtype) || !aligned_to({logp_opt, entropy_opt, lse, top_logp, top_index}, 4) ||
+        !aligned_to({target_opt}, 8))
+        return FOCUS_ERR_SHAPE;
+    FOCUS_TRY(check_ws(ws, ws_bytes, logprobs_ws(T, V, top)));
+    if (T == 0) return FOCUS_OK;
+    return hip_status(launch_logprobs(dtype, Z, T, V, target_opt, top, logp_opt, entropy_opt, lse, top_logp, top_index,
+                                      flag_of(ws), ws, (hipStream_t)stream));
+}
+
+focus_status focus_token_logprobs_bwd(const void *Z, int dtype, int64_t T, int64_t V, const int64_t *target_opt,
+                                      const float *lse, const float *entropy_opt, const float *d_logp_opt,
+                                      const float *d_entropy_opt, void *dZ, void *ws, size_t ws_bytes, focus_stream stream) {
+    if (!dtype_ok(dtype)) return FOCUS_ERR_DTYPE;
+    FOCUS_TRY(check_logits(T, V));
+    if (T > 0 && (!Z || !lse || !dZ || (!d_logp_opt && !d_entropy_opt) || (d_logp_opt && !target_opt) ||
+                  (d_entropy_opt && !entropy_opt)))
+        return FOCUS_ERR_NULL;
+    if (!logits_aligned(Z, dtype) || !logits_aligned(dZ, dtype) ||
+        !aligned_to({lse, entropy_opt, d_logp_opt, d_entropy_opt}, 4) || !aligned_to({target_opt}, 8))
+        return FOCUS_ERR_SHAPE;
+    FOCUS_TRY(check_ws(ws, ws_bytes, kWsHeader));
+    if (T == 0) return FOCUS_OK;
+    return hip_status(launch_logprobs_bwd(dtype, Z, T, V, target_opt, lse, entropy_opt, d_logp_opt, d_entropy_opt, dZ,
+                                          (hipStream_t)stream));
 }
 
 focus_status focus_check_flags(void *ws, focus_stream stream) {

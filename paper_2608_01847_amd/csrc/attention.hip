@@ -1,0 +1,338 @@
+// Attention over whole prompts on the fp32 matrix instructions (v_mfma_f32_32x32x2_f32), forward and backward.
+//
+//   S = scale q k^T (causal: keys past the query's own place hidden, the last query at the last key),
+//   P = softmax(S), O = P v, lse = log sum exp S
+//   dv = P^T dO, dP = dO v^T, dS = P (dP - rowsum(dO O)) scale, dq = dS k, dk = dS^T q
+//
+// A workgroup takes 32 queries (forward, dq) or 32 keys (dk, dv) of one head; its four waves take alternate tiles of 32
+// of the other side, each with its own running maximum and sum, and are joined through LDS in a fixed order. The
+// scores are formed transposed (keys down the accumulator's rows, one query per lane), so that the softmax runs within
+// a lane and its partner, and a register of probabilities is at once the B operand of the next product: register r
+// holds the keys acc_row(r) (lanes 0-31) and acc_row(r) + 4 (lanes 32-63), the two that one instruction contracts.
+// Operands come straight from global memory: one instruction takes 64 cycles for 512 bytes of operands.
+#include "attn_common.h"
+
+namespace focus {
+
+namespace {
+
+constexpr int kWaves = 4;
+constexpr int kThreads = 64 * kWaves;
+constexpr int kTile = 32;
+
+__device__ __forceinline__ void load4(const float *p, float (&v)[4]) {
+    const float4 w = *reinterpret_cast<const float4 *>(p);
+    v[0] = w.x, v[1] = w.y, v[2] = w.z, v[3] = w.w;
+}
+__device__ __forceinline__ void load4(const uint16_t *p, float (&v)[4]) {
+    const uint2 w = *reinterpret_cast<const uint2 *>(p);
+    unpack_bf16(w.x, v[0], v[1]);
+    unpack_bf16(w.y, v[2], v[3]);
+}
+__device__ __forceinline__ void store4(float *p, const float (&v)[4]) {
+    *reinterpret_cast<float4 *>(p) = make_float4(v[0], v[1], v[2], v[3]);
+}
+__device__ __forceinline__ void store4(uint16_t *p, const float (&v)[4]) {
+    *reinterpret_cast<uint2 *>(p) = make_uint2(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]));
+}
+
+// One row's part of a lane: features 8 j + 4 (lane / 32) .. + 3 for every j (zeros where the row or a feature does
+// not exist).
+template <typename T, int DT>
+__device__ __forceinline__ void load_row(const T *row, bool ok, int D, int half, float (&v)[4 * DT][4]) {
+#pragma unroll
+    for (int j = 0; j < 4 * DT; j++) {
+        const int d = 8 * j + 4 * half;
+        if (ok && d < D) load4(row + d, v[j]);
+        else v[j][0] = v[j][1] = v[j][2] = v[j][3] = 0.0f;
+    }
+}
+
+// 32 x 32 products of 32 rows at `row` (this lane's) with the 32 rows held in b
+template <typename T, int DT>
+__device__ __forceinline__ f32x16_t row_products(const T *row, bool ok, int D, int half, const float (&b)[4 * DT][4]) {
+    f32x16_t acc = {};
+#pragma unroll
+    for (int j = 0; j < 4 * DT; j++) {
+        float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+        const int d = 8 * j + 4 * half;
+        if (ok && d < D) load4(row + d, v);
+#pragma unroll
+        for (int e = 0; e < 4; e++) acc = __builtin_amdgcn_mfma_f32_32x32x2f32(v[e], b[j][e], acc, 0, 0, 0);
+    }
+    return acc;
+}
+
+// out^T[d][column] += sum over 32 rows of X[row][d] w[row][column], w in accumulator layout; row r0 + i exists for
+// i < n
+template <typename T, int DT>
+__device__ __forceinline__ void add_products(f32x16_t (&out)[DT], const T *X, int64_t stride, int n, int D, int lane,
+                                             const float (&w)[16]) {
+    const int half = lane >> 5, col = lane & 31;
+#pragma unroll
+    for (int r = 0; r < 16; r++) {
+        const int row = acc_row(r) + 4 * half;
+#pragma unroll
+        for (int t = 0; t < DT; t++) {
+            const int d = 32 * t + col;
+            const float x = row < n && d < D ? load_one(X + row * stride + d) : 0.0f;
+            out[t] = __builtin_amdgcn_mfma_f32_32x32x2f32(x, w[r], out[t], 0, 0, 0);
+        }
+    }
+}
+
+// Adds the four waves' accumulators in wave 0: (0 + 2) + (1 + 3).
+template <int DT>
+__device__ __forceinline__ void join(f32x16_t (&acc)[DT], float *lds, int wave, int lane) {
+#pragma unroll
+    for (int step = 2; step >= 1; step >>= 1) {
+        __syncthreads();
+        if (wave >= step && wave < 2 * step) {
+#pragma unroll
+            for (int t = 0; t < DT; t++)
+#pragma unroll
+                for (int r = 0; r < 16; r++) lds[(((wave - step) * DT + t) * 16 + r) * 64 + lane] = acc[t][r];
+        }
+        __syncthreads();
+        if (wave < step) {
+#pragma unroll
+            for (int t = 0; t < DT; t++)
+#pragma unroll
+                for (int r = 0; r < 16; r++) acc[t][r] += lds[((wave * DT + t) * 16 + r) * 64 + lane];
+        }
+    }
+}
+
+// out^T of one lane's column to its row, times `f`
+template <typename T, int DT>
+__device__ __forceinline__ void store_column(T *row, int D, int half, const f32x16_t (&acc)[DT], float f) {
+#pragma unroll
+    for (int t = 0; t < DT; t++)
+#pragma unroll
+        for (int g = 0; g < 4; g++) {
+            const int d = 32 * t + 8 * g + 4 * half;
+            if (d < D) {
+                const float v[4] = {acc[t][4 * g] * f, acc[t][4 * g + 1] * f, acc[t][4 * g + 2] * f, acc[t][4 * g + 3] * f};
+                store4(row + d, v);
+            }
+        }
+}
+
+template <typename T, int DT>
+__global__ void __launch_bounds__(kThreads) attn_fwd_kernel(AttnArgs a) {
+    __shared__ float lds[2 * DT * 16 * 64];
+    __shared__ float stat[2][kWaves][32];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5, col = lane & 31;
+    int tile;
+    const int s = slot_sequence(a.cu_q, a.n_seq, kTile, (int)blockIdx.x, tile);
+    SeqRange r;
+    seq_range(a, s, r);
+    check_ends<kThreads>(a);
+    if (!tile_in(tile, kTile, r.lq)) return;
+    const int h = blockIdx.y, hk = h / (a.Hq / a.Hkv), D = a.D;
+    const int q = tile * kTile + col, shift = r.lk - r.lq;
+    const bool q_ok = q < r.lq;
+    const T *K = static_cast<const T *>(a.k) + r.k0 * a.k_stride + (int64_t)hk * D;
+    const T *V = static_cast<const T *>(a.v) + r.k0 * a.v_stride + (int64_t)hk * D;
+    float qv[4 * DT][4];
+    load_row<T, DT>(static_cast<const T *>(a.q) + (r.q0 + q) * a.q_stride + (int64_t)h * D, q_ok, D, half, qv);
+    const float c = a.scale * kLog2e;
+    const int q_end = tile * kTile + kTile < r.lq ? tile * kTile + kTile : r.lq;
+    const int k_end = a.causal ? (q_end + shift < r.lk ? q_end + shift : r.lk) : r.lk;
+    const int seen = a.causal ? (q + shift < r.lk ? q + shift : r.lk - 1) : r.lk - 1;  // last key of this lane's query
+    f32x16_t o[DT] = {};
+    float m = -__builtin_inff(), l = 0.0f;
+    for (int k0 = wave * kTile; k0 < k_end; k0 += kWaves * kTile) {
+        const bool k_ok = k0 + col < r.lk;
+        const f32x16_t acc = row_products<T, DT>(K + (k0 + col) * a.k_stride, k_ok, D, half, qv);
+        float p[16], top = -__builtin_inff();
+#pragma unroll
+        for (int i = 0; i < 16; i++) {
+            p[i] = k0 + acc_row(i) + 4 * half <= seen ? acc[i] * c : -__builtin_inff();
+            top = fmaxf(top, p[i]);
+        }
+        top = fmaxf(fmaxf(top, __shfl_xor(top, 32, 64)), m);
+        const float base = top == -__builtin_inff() ? 0.0f : top;
+        const float alpha = exp2_raw(m - base);
+        float sum = 0.0f;
+#pragma unroll
+        for (int i = 0; i < 16; i++) {
+            p[i] = exp2_raw(p[i] - base);
+            sum += p[i];
+        }
+        m = top;
+        l = l * alpha + sum;
+#pragma unroll
+        for (int t = 0; t < DT; t++)
+#pragma unroll
+            for (int i = 0; i < 16; i++) o[t][i] *= alpha;
+        add_products<T, DT>(o, V + k0 * a.v_stride, a.v_stride, r.lk - k0, D, lane, p);
+    }
+    l += __shfl_xor(l, 32, 64);
+    if (half == 0) {
+        stat[0][wave][col] = m;
+        stat[1][wave][col] = l;
+    }
+    __syncthreads();
+    float top = -__builtin_inff(), total = 0.0f;
+#pragma unroll
+    for (int w = 0; w < kWaves; w++) top = fmaxf(top, stat[0][w][col]);
+    const float base = top == -__builtin_inff() ? 0.0f : top;
+#pragma unroll
+    for (int w = 0; w < kWaves; w++) total += stat[1][w][col] * exp2_raw(stat[0][w][col] - base);
+    const float mine = exp2_raw(m - base);
+#pragma unroll
+    for (int t = 0; t < DT; t++)
+#pragma unroll
+        for (int i = 0; i < 16; i++) o[t][i] *= mine;
+    join<DT>(o, lds, wave, lane);
+    if (wave != 0 || !q_ok) return;
+    const float inv = total > 0.0f ? 1.0f / total : (total == 0.0f ? 0.0f : total);
+    store_column<T, DT>(static_cast<T *>(a.O) + ((r.q0 + q) * a.Hq + h) * D, D, half, o, inv);
+    if (a.lse && half == 0) a.lse[(int64_t)h * a.Tq + r.q0 + q] = total == 0.0f ? -__builtin_inff() : (top + log2f(total)) * kLn2;
+}
+
+// dq of 32 queries, and delta = rowsum(dO O) for the keys' pass
+template <typename T, int DT>
+__global__ void __launch_bounds__(kThreads, 1) attn_bwd_q_kernel(AttnArgs a) {
+    __shared__ float lds[2 * DT * 16 * 64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5, col = lane & 31;
+    int tile;
+    const int s = slot_sequence(a.cu_q, a.n_seq, kTile, (int)blockIdx.x, tile);
+    SeqRange r;
+    seq_range(a, s, r);
+    check_ends<kThreads>(a);
+    if (!tile_in(tile, kTile, r.lq)) return;
+    const int h = blockIdx.y, hk = h / (a.Hq / a.Hkv), D = a.D;
+    const int q = tile * kTile + col, shift = r.lk - r.lq;
+    const bool q_ok = q < r.lq;
+    const T *K = static_cast<const T *>(a.k) + r.k0 * a.k_stride + (int64_t)hk * D;
+    const T *V = static_cast<const T *>(a.v) + r.k0 * a.v_stride + (int64_t)hk * D;
+    float qv[4 * DT][4], gv[4 * DT][4];
+    const int64_t oq = ((r.q0 + q) * a.Hq + h) * D;
+    float delta = 0.0f;
+    load_row<T, DT>(static_cast<const T *>(a.O) + oq, q_ok, D, half, qv);
+    load_row<T, DT>(static_cast<const T *>(a.dO) + oq, q_ok, D, half, gv);
+#pragma unroll
+    for (int j = 0; j < 4 * DT; j++)
+#pragma unroll
+        for (int e = 0; e < 4; e++) delta = __builtin_fmaf(qv[j][e], gv[j][e], delta);
+    delta += __shfl_xor(delta, 32, 64);
+    if (wave == 0 && half == 0 && q_ok) a.delta[(int64_t)h * a.Tq + r.q0 + q] = delta;
+    load_row<T, DT>(static_cast<const T *>(a.q) + (r.q0 + q) * a.q_stride + (int64_t)h * D, q_ok, D, half, qv);
+    const float c = a.scale * kLog2e;
+    const float lse2 = q_ok ? a.lse[(int64_t)h * a.Tq + r.q0 + q] * kLog2e : 0.0f;
+    const int q_end = tile * kTile + kTile < r.lq ? tile * kTile + kTile : r.lq;
+    const int k_end = a.causal ? (q_end + shift < r.lk ? q_end + shift : r.lk) : r.lk;
+    const int seen = a.causal ? (q + shift < r.lk ? q + shift : r.lk - 1) : r.lk - 1;
+    f32x16_t dq[DT] = {};
+    for (int k0 = wave * kTile; k0 < k_end; k0 += kWaves * kTile) {
+        const bool k_ok = k0 + col < r.lk;
+        const f32x16_t sc = row_products<T, DT>(K + (k0 + col) * a.k_stride, k_ok, D, half, qv);
+        const f32x16_t dp = row_products<T, DT>(V + (k0 + col) * a.v_stride, k_ok, D, half, gv);
+        float ds[16];
+#pragma unroll
+        for (int i = 0; i < 16; i++)
+            ds[i] = k0 + acc_row(i) + 4 * half <= seen ? exp2_raw(__builtin_fmaf(sc[i], c, -lse2)) * (dp[i] - delta) : 0.0f;
+        add_products<T, DT>(dq, K + k0 * a.k_stride, a.k_stride, r.lk - k0, D, lane, ds);
+    }
+    join<DT>(dq, lds, wave, lane);
+    if (wave != 0 || !q_ok) return;
+    store_column<T, DT>(static_cast<T *>(a.dq) + (r.q0 + q) * a.dq_stride + (int64_t)h * D, D, half, dq, a.scale);
+}
+
+// dk and dv of 32 keys of one key-value head, summed over the query heads that share it
+template <typename T, int DT>
+__global__ void __launch_bounds__(kThreads, 1) attn_bwd_kv_kernel(AttnArgs a) {
+    __shared__ float lds[2 * DT * 16 * 64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5, col = lane & 31;
+    int tile;
+    const int s = slot_sequence(a.cu_k, a.n_seq, kTile, (int)blockIdx.x, tile);
+    SeqRange r;
+    seq_range(a, s, r);
+    check_ends<kThreads>(a);
+    if (!tile_in(tile, kTile, r.lk)) return;
+    const int hk = blockIdx.y, group = a.Hq / a.Hkv, D = a.D;
+    const int k = tile * kTile + col, shift = r.lk - r.lq;
+    const bool k_ok = k < r.lk;
+    float kv[4 * DT][4], vv[4 * DT][4];
+    load_row<T, DT>(static_cast<const T *>(a.k) + (r.k0 + k) * a.k_stride + (int64_t)hk * D, k_ok, D, half, kv);
+    load_row<T, DT>(static_cast<const T *>(a.v) + (r.k0 + k) * a.v_stride + (int64_t)hk * D, k_ok, D, half, vv);
+    const float c = a.scale * kLog2e;
+    // first query that sees this tile's first key, and this lane's key
+    const int q_first = a.causal && tile * kTile - shift > 0 ? (tile * kTile - shift) / kTile * kTile : 0;
+    const int q_sees = a.causal ? k - shift : 0;
+    const int q_tiles = r.lq > q_first ? (r.lq - q_first + kTile - 1) / kTile : 0;
+    f32x16_t dk[DT] = {}, dv[DT] = {};
+    for (int it = wave; it < q_tiles * group; it += kWaves) {
+        const int h = hk * group + it / q_tiles, q0 = q_first + it % q_tiles * kTile;
+        const T *Q = static_cast<const T *>(a.q) + (r.q0 + q0) * a.q_stride + (int64_t)h * D;
+        const T *G = static_cast<const T *>(a.dO) + ((r.q0 + q0) * a.Hq + h) * D;
+        const int64_t g_stride = (int64_t)a.Hq * D, at = (int64_t)h * a.Tq + r.q0 + q0;
+        const int n = r.lq - q0;
+        const f32x16_t sc = row_products<T, DT>(Q + col * a.q_stride, col < n, D, half, kv);
+        const f32x16_t dp = row_products<T, DT>(G + col * g_stride, col < n, D, half, vv);
+        float p[16], ds[16];
+#pragma unroll
+        for (int i = 0; i < 16; i++) {
+            const int row = acc_row(i) + 4 * half;
+            const bool ok = k_ok && row < n && q0 + row >= q_sees;
+            p[i] = ok ? exp2_raw(__builtin_fmaf(sc[i], c, -a.lse[at + (row < n ? row : 0)] * kLog2e)) : 0.0f;
+            ds[i] = ok ? p[i] * (dp[i] - a.delta[at + (row < n ? row : 0)]) : 0.0f;
+        }
+        add_products<T, DT>(dv, G, g_stride, n, D, lane, p);
+        add_products<T, DT>(dk, Q, a.q_stride, n, D, lane, ds);
+    }
+    join<DT>(dk, lds, wave, lane);
+    join<DT>(dv, lds, wave, lane);
+    if (wave != 0 || !k_ok) return;
+    store_column<T, DT>(static_cast<T *>(a.dk) + (r.k0 + k) * a.dk_stride + (int64_t)hk * D, D, half, dk, a.scale);
+    store_column<T, DT>(static_cast<T *>(a.dv) + (r.k0 + k) * a.dv_stride + (int64_t)hk * D, D, half, dv, 1.0f);
+}
+
+int64_t slots(int64_t T, int64_t n_seq, int rows) { return T / rows + n_seq; }
+
+template <typename F>
+void pick_dt(int D, F &&f) {
+    if (D <= 32) f(std::integral_constant<int, 1>{});
+    else if (D <= 64) f(std::integral_constant<int, 2>{});
+    else if (D <= 96) f(std::integral_constant<int, 3>{});
+    else f(std::integral_constant<int, 4>{});
+}
+
+template <typename T>
+hipError_t fwd(const AttnArgs &a, hipStream_t st) {
+    const dim3 grid((unsigned)slots(a.Tq, a.n_seq, kTile), (unsigned)a.Hq);
+    pick_dt(a.D, [&](auto dt) { attn_fwd_kernel<T, decltype(dt)::value><<<grid, kThreads, 0, st>>>(a); });
+    return hipGetLastError();
+}
+
+template <typename T>
+hipError_t bwd(const AttnArgs &a, hipStream_t st) {
+    const dim3 gq((unsigned)slots(a.Tq, a.n_seq, kTile), (unsigned)a.Hq), gk((unsigned)slots(a.Tk, a.n_seq, kTile), (unsigned)a.Hkv);
+    pick_dt(a.D, [&](auto dt) {
+        constexpr int DT = decltype(dt)::value;
+        if (a.Tq > 0) attn_bwd_q_kernel<T, DT><<<gq, kThreads, 0, st>>>(a);
+        if (a.Tk > 0) attn_bwd_kv_kernel<T, DT><<<gk, kThreads, 0, st>>>(a);
+    });
+    return hipGetLastError();
+}
+
+}  // namespace
+
+size_t attn_fwd_ws(int64_t, int64_t, int, int, int, int64_t) { return kWsHeader; }
+
+size_t attn_bwd_ws(int64_t Tq, int64_t, int Hq, int, int, int64_t) {
+    return kWsHeader + (size_t)Tq * (size_t)Hq * sizeof(float);
+}
+
+hipError_t launch_attn_fwd(int dtype, const AttnArgs &a, void *, hipStream_t st) {
+    return dtype == kBF16 ? fwd<uint16_t>(a, st) : fwd<float>(a, st);
+}
+
+hipError_t launch_attn_bwd(int dtype, AttnArgs a, void *ws, hipStream_t st) {
+    a.delta = reinterpret_cast<float *>(static_cast<char *>(ws) + kWsHeader);
+    return dtype == kBF16 ? bwd<uint16_t>(a, st) : bwd<float>(a, st);
+}
+
+}  // namespace focus

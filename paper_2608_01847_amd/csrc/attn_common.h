@@ -1,0 +1,76 @@
+// Pieces shared by the attention kernels: which tile of which sequence a workgroup takes, and the masks.
+#pragma once
+
+#include "internal.h"
+#include "ops_device.h"
+
+namespace focus {
+
+constexpr float kLog2e = 1.44269504088896341f;
+constexpr float kLn2 = 0.693147180559945309f;
+
+// One sequence's rows of the packed queries and keys.
+struct SeqRange {
+    int64_t q0, k0;  // first rows
+    int lq, lk;
+};
+
+__device__ __forceinline__ void seq_range(const AttnArgs &a, int s, SeqRange &r) {
+    if (!a.cu_q) {
+        r.q0 = r.k0 = 0;
+        r.lq = (int)a.Tq;
+        r.lk = (int)a.Tk;
+        return;
+    }
+    // ends that do not rise or that pass the tensors raise the domain flag and leave an empty sequence
+    const int64_t qa = a.cu_q[s], qb = a.cu_q[s + 1], ka = a.cu_k[s], kb = a.cu_k[s + 1];
+    const bool ok = qa >= 0 && qa <= qb && qb <= a.Tq && ka >= 0 && ka <= kb && kb <= a.Tk;
+    if (!ok) *a.flag = 1u;
+    r.q0 = ok ? qa : 0;
+    r.k0 = ok ? ka : 0;
+    r.lq = ok ? (int)(qb - qa) : 0;
+    r.lk = ok ? (int)(kb - ka) : 0;
+}
+
+// Tiles of `rows` rows over packed sequences with ends cu[0..n]: sequence i's tiles take the slots from
+// cu[i] / rows + i on, which leaves room for ceil(length / rows) of them whatever the lengths are, so the number of
+// slots, T / rows + n, needs no look at the lengths on the host. Returns the sequence, `tile` its tile, which may
+// lie past its end or, in slots before the first sequence, be -1: nothing to do (tile_rows below).
+__device__ __forceinline__ int slot_sequence(const int32_t *cu, int n, int rows, int slot, int &tile) {
+    if (!cu) {
+        tile = slot;
+        return 0;
+    }
+    int lo = 0, len = n;  // the answer is in [lo, lo + len)
+    while (len > 64) {    // a scalar bisection down to one wave's width
+        const int half = len / 2;
+        if (cu[lo + half] / rows + lo + half <= slot) {
+            lo += half;
+            len -= half;
+        } else {
+            len = half;
+        }
+    }
+    const int lane = threadIdx.x & 63;
+    const int start = lane < len ? cu[lo + lane] / rows + lo + lane : 0x7FFFFFFF;
+    const unsigned long long below = __ballot(start <= slot);
+    const int s = __builtin_amdgcn_readfirstlane(lo + (below ? 63 - __builtin_clzll(below) : 0));
+    tile = below ? slot - __builtin_amdgcn_readfirstlane(cu[s] / rows + s) : -1;
+    return s;
+}
+
+// Whether a tile of `rows` rows has any of a sequence's n
+__device__ __forceinline__ bool tile_in(int tile, int rows, int n) { return tile >= 0 && (int64_t)tile * rows < n; }
+
+// Every pair of ends, by the first workgroup of a launch (the others meet only those of their own tiles)
+template <int THREADS>
+__device__ __forceinline__ void check_ends(const AttnArgs &a) {
+    if (!a.cu_q || blockIdx.x != 0 || blockIdx.y != 0) return;
+    SeqRange r;
+    for (int s = threadIdx.x; s < a.n_seq; s += THREADS) seq_range(a, s, r);
+}
+
+// row of register r in the 32 x 32 accumulator of a lane: 8 (r / 4) + 4 (lane / 32) + r % 4
+__device__ __forceinline__ constexpr int acc_row(int r) { return (r & 3) + 8 * (r >> 2); }
+
+}  // namespace focus

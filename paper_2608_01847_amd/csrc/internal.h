@@ -107,4 +107,41 @@ hipError_t launch_adamw(float lr, float beta1, float beta2, float eps, float wei
                         int64_t t, int64_t n, float *param, const float *grad, float *exp_avg, float *exp_avg_sq,
                         uint32_t *flag, hipStream_t st);
 
+// ---- operators around the linears ---------------------------------------------------------------
+size_t norm_bwd_ws(int64_t T, int64_t C);
+hipError_t launch_norm_fwd(int layer, float eps, int dtype, const void *X, const void *R, int64_t T, int64_t C, const void *w,
+                           const void *b, int w_dtype, void *H, void *Y, float *mean, float *rstd, hipStream_t st);
+hipError_t launch_norm_bwd(int layer, int dtype, const void *dY, const void *H, int64_t T, int64_t C, const void *w,
+                           int w_dtype, const float *mean, const float *rstd, const void *dR, void *dX, float *dw, float *db,
+                           void *ws, hipStream_t st);
+
+// An attention call: elements between the tokens of a tensor, lengths as the ends of the sequences (NULL: one sequence
+// of all tokens).
+struct AttnArgs {
+    const void *q, *k, *v;
+    void *O;
+    float *lse;  // [Hq][Tq]
+    const void *dO;
+    void *dq, *dk, *dv;
+    float *delta;  // [Hq][Tq], workspace of the backward
+    const int32_t *cu_q, *cu_k;
+    uint32_t *flag;
+    int64_t q_stride, k_stride, v_stride, dq_stride, dk_stride, dv_stride;
+    int64_t Tq, Tk;
+    int n_seq, Hq, Hkv, D, causal;
+    float scale;
+};
+size_t attn_fwd_ws(int64_t Tq, int64_t Tk, int Hq, int Hkv, int D, int64_t n_seq);
+size_t attn_bwd_ws(int64_t Tq, int64_t Tk, int Hq, int Hkv, int D, int64_t n_seq);
+hipError_t launch_attn_fwd(int dtype, const AttnArgs &a, void *ws, hipStream_t st);
+hipError_t launch_attn_bwd(int dtype, AttnArgs a, void *ws, hipStream_t st);
+
+constexpr int kMaxTop = 64;  // alternatives per row of logits
+size_t logprobs_ws(int64_t T, int64_t V, int top);
+hipError_t launch_logprobs(int dtype, const void *Z, int64_t T, int64_t V, const int64_t *target, int top, float *logp,
+                           float *entropy, float *lse, float *top_logp, int32_t *top_index, uint32_t *flag, void *ws,
+                           hipStream_t st);
+hipError_t launch_logprobs_bwd(int dtype, const void *Z, int64_t T, int64_t V, const int64_t *target, const float *lse,
+                               const float *entropy, const float *d_logp, const float *d_entropy, void *dZ, hipStream_t st);
+
 }  // namespace focus

@@ -18,7 +18,11 @@ F32, BF16 = 0, 1
 CALL_SCALES_INIT, CALL_FAKEQUANT_FWD, CALL_FAKEQUANT_BWD = 0, 1, 2
 CALL_RECON_GEMM_FWD, CALL_RECON_GEMM_BWD, CALL_EXPORT_PACKED, CALL_ADAMW = 3, 4, 5, 6
 CALL_RECON_GEMM_DX, CALL_FAKEQUANT_ACT_BWD, CALL_KL_TOP, CALL_FAKEQUANT_WEIGHTS = 7, 8, 9, 10
+CALL_NORM_FWD, CALL_NORM_BWD, CALL_ATTENTION_FWD, CALL_ATTENTION_BWD = 11, 12, 13, 14
+CALL_TOKEN_LOGPROBS, CALL_TOKEN_LOGPROBS_BWD = 15, 16
 MAX_WEIGHT_LAYERS = 16
+NORM_LAYER, NORM_RMS = 0, 1
+MAX_TOP = 64
 
 OK, ERR_NULL, ERR_SHAPE, ERR_DTYPE, ERR_CONFIG, ERR_WORKSPACE, ERR_DOMAIN, ERR_HIP, ERR_SCRATCH = range(9)
 
@@ -26,7 +30,9 @@ EXPORTED = ("focus_workspace_size", "focus_scales_init", "focus_fakequant_fwd", 
             "focus_recon_gemm_fwd", "focus_recon_gemm_fwd_mxfp4", "focus_recon_gemm_fwd_mxfp4_noalloc",
             "focus_recon_gemm_bwd",
             "focus_recon_gemm_bwd_mxfp4", "focus_export_packed", "focus_fakequant_weights", "focus_recon_gemm_dx",
-            "focus_fakequant_act_bwd", "focus_kl_top", "focus_adamw_step", "focus_check_flags", "focus_status_string")
+            "focus_fakequant_act_bwd", "focus_kl_top", "focus_adamw_step", "focus_norm_fwd", "focus_norm_bwd",
+            "focus_attention_workspace_size", "focus_attention_fwd", "focus_attention_bwd", "focus_token_logprobs",
+            "focus_token_logprobs_bwd", "focus_check_flags", "focus_status_string")
 
 
 class QConfig(ctypes.Structure):
@@ -44,6 +50,13 @@ class WeightLayer(ctypes.Structure):
 class AdamWConfig(ctypes.Structure):
     _fields_ = [("lr", ctypes.c_float), ("beta1", ctypes.c_float), ("beta2", ctypes.c_float),
                 ("eps", ctypes.c_float), ("weight_decay", ctypes.c_float), ("log2_domain", ctypes.c_int32)]
+
+
+class AttentionConfig(ctypes.Structure):
+    _fields_ = [("heads_q", ctypes.c_int32), ("heads_kv", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+                ("causal", ctypes.c_int32), ("scale", ctypes.c_float), ("reserved", ctypes.c_int32),
+                ("q_stride", ctypes.c_int64), ("k_stride", ctypes.c_int64), ("v_stride", ctypes.c_int64),
+                ("dq_stride", ctypes.c_int64), ("dk_stride", ctypes.c_int64), ("dv_stride", ctypes.c_int64)]
 
 
 class FocusError(RuntimeError):
@@ -80,6 +93,15 @@ def lib() -> ctypes.CDLL:
         L.focus_fakequant_act_bwd.argtypes = [q, p, i32, i64, i64, p, i32, p, p, sz, p]
         L.focus_kl_top.argtypes = [p, p, i32, i64, i64, i32, p, p, p, sz, p]
         L.focus_adamw_step.argtypes = [ctypes.POINTER(AdamWConfig), i64, i64, p, p, p, p, p, sz, p]
+        f32, attn = ctypes.c_float, ctypes.POINTER(AttentionConfig)
+        L.focus_norm_fwd.argtypes = [i32, f32, p, p, i32, i64, i64, p, p, i32, p, p, p, p, p, sz, p]
+        L.focus_norm_bwd.argtypes = [i32, p, p, i32, i64, i64, p, i32, p, p, p, p, p, p, p, sz, p]
+        L.focus_attention_workspace_size.argtypes = [i32, attn, i64, i64, i64]
+        L.focus_attention_workspace_size.restype = sz
+        L.focus_attention_fwd.argtypes = [attn, p, p, p, i32, i64, i64, p, p, i64, p, p, p, sz, p]
+        L.focus_attention_bwd.argtypes = [attn, p, p, p, p, p, p, i32, i64, i64, p, p, i64, p, p, p, p, sz, p]
+        L.focus_token_logprobs.argtypes = [p, i32, i64, i64, p, i32, p, p, p, p, p, p, sz, p]
+        L.focus_token_logprobs_bwd.argtypes = [p, i32, i64, i64, p, p, p, p, p, p, p, sz, p]
         L.focus_check_flags.argtypes = [p, p]
         L.focus_status_string.argtypes = [i32]
         L.focus_status_string.restype = ctypes.c_char_p
@@ -87,7 +109,8 @@ def lib() -> ctypes.CDLL:
                      "focus_recon_gemm_fwd_mxfp4", "focus_recon_gemm_fwd_mxfp4_noalloc", "focus_recon_gemm_bwd",
                      "focus_recon_gemm_bwd_mxfp4",
                      "focus_export_packed", "focus_fakequant_weights", "focus_adamw_step", "focus_check_flags", "focus_recon_gemm_dx", "focus_fakequant_act_bwd",
-                     "focus_kl_top"):
+                     "focus_kl_top", "focus_norm_fwd", "focus_norm_bwd", "focus_attention_fwd", "focus_attention_bwd",
+                     "focus_token_logprobs", "focus_token_logprobs_bwd"):
             getattr(L, name).restype = ctypes.c_int
         _LIB = L
     return _LIB
@@ -419,6 +442,213 @@ def adamw_step(param: torch.Tensor, grad: torch.Tensor, exp_avg: torch.Tensor, e
         ws = workspace(256, param.device)
     _check(lib().focus_adamw_step(ctypes.byref(cfg), t, param.numel(), _ptr(param), _ptr(grad), _ptr(exp_avg),
                                   _ptr(exp_avg_sq), _ptr(ws), ws.numel(), _stream()), "focus_adamw_step")
+
+
+def norm_workspace_size(T: int, C: int) -> int:
+    """Workspace bytes of norm_fwd and norm_bwd on T tokens of C features."""
+    return int(lib().focus_workspace_size(CALL_NORM_BWD, None, T, 0, C))
+
+
+def _sized(ws: torch.Tensor | None, need: int, device) -> torch.Tensor:
+    """ws if it does, else a workspace of `need` bytes of which only the header is cleared."""
+    if need == 0:
+        need = 256  # the call itself reports what is wrong with its arguments
+    if ws is None or ws.numel() < need:
+        ws = torch.empty(need, dtype=torch.uint8, device=device)
+        ws[:256].zero_()
+    return ws
+
+
+def norm_fwd(X: torch.Tensor, weight: torch.Tensor, bias=None, residual=None, kind: int = NORM_LAYER, eps: float = 1e-5,
+             want_stats: bool = True, ws=None, out=None, h_out=None):
+    """Layer norm (NORM_LAYER) or RMS norm (NORM_RMS) over the last dimension of X [T][C], with an optional residual sum
+    H = X + residual in front of it -> (Y, H or None, mean [T] or None, rstd [T] or None). `out` / `h_out`: preallocated
+    Y / H. The statistics are fp32 (mean: layer norm only; neither without want_stats)."""
+    T, C = X.shape
+    for t in (residual, out, h_out):
+        if t is not None and (t.shape != X.shape or t.dtype != X.dtype):
+            raise ValueError("norm_fwd: residual, out and h_out have X's shape and dtype")
+    if weight.shape != (C,) or (bias is not None and (bias.shape != (C,) or bias.dtype != weight.dtype)):
+        raise ValueError("norm_fwd: weight and bias are [C] of one dtype")
+    if h_out is not None and residual is None:
+        raise ValueError("norm_fwd: h_out without a residual")
+    Y = out if out is not None else torch.empty_like(X)
+    H = (h_out if h_out is not None else torch.empty_like(X)) if residual is not None else None
+    mean = rstd = None
+    if want_stats:
+        rstd = torch.empty(T, dtype=torch.float32, device=X.device)
+        mean = torch.empty(T, dtype=torch.float32, device=X.device) if kind == NORM_LAYER else None
+    ws = _sized(ws, 256, X.device)
+    _check(lib().focus_norm_fwd(kind, eps, _ptr(X), _ptr(residual), _dt(X), T, C, _ptr(weight), _ptr(bias), _dt(weight),
+                                _ptr(H), _ptr(Y), _ptr(mean), _ptr(rstd), _ptr(ws), ws.numel(), _stream()),
+           "focus_norm_fwd")
+    return Y, H, mean, rstd
+
+
+def norm_bwd(dY: torch.Tensor, H: torch.Tensor, weight: torch.Tensor, mean, rstd: torch.Tensor, d_residual=None,
+             kind: int = NORM_LAYER, want_bias: bool = False, ws=None, out=None, dw_out=None, db_out=None):
+    """Backward of norm_fwd on its input H (the residual sum, or X where there was none) -> (dX, dweight [C] fp32,
+    dbias [C] fp32 or None). d_residual: the gradient that reaches H past the norm; dX is the gradient of X and of the
+    residual alike. dX may be dY's or d_residual's own tensor (`out`)."""
+    T, C = H.shape
+    for t in (dY, d_residual, out):
+        if t is not None and (t.shape != H.shape or t.dtype != H.dtype):
+            raise ValueError("norm_bwd: dY, d_residual and out have H's shape and dtype")
+    for t, n in ((weight, C), (mean, T), (rstd, T), (dw_out, C), (db_out, C)):
+        if t is not None and t.shape != (n,):
+            raise ValueError("norm_bwd: weight and its gradients are [C], mean and rstd [T]")
+    for t in (mean, rstd, dw_out, db_out):
+        if t is not None and t.dtype != torch.float32:
+            raise TypeError("norm_bwd: statistics and parameter gradients are float32")
+    dX = out if out is not None else torch.empty_like(H)
+    dw = dw_out if dw_out is not None else torch.empty(C, dtype=torch.float32, device=H.device)
+    db = db_out
+    if db is None and want_bias:
+        db = torch.empty(C, dtype=torch.float32, device=H.device)
+    ws = _sized(ws, norm_workspace_size(T, C), H.device)
+    _check(lib().focus_norm_bwd(kind, _ptr(dY), _ptr(H), _dt(H), T, C, _ptr(weight), _dt(weight), _ptr(mean), _ptr(rstd),
+                                _ptr(d_residual), _ptr(dX), _ptr(dw), _ptr(db), _ptr(ws), ws.numel(), _stream()),
+           "focus_norm_bwd")
+    return dX, dw, db
+
+
+def _heads(t: torch.Tensor, name: str) -> tuple:
+    """(pointer, elements between tokens) of [tokens][heads][head_dim] whose tokens may lie apart (a slice of a fused
+    product); a token's heads are contiguous."""
+    if t.dim() != 3:
+        raise ValueError(f"{name}: [tokens][heads][head_dim] expected")
+    n, h, d = t.shape
+    if n and ((d > 1 and t.stride(2) != 1) or (h > 1 and t.stride(1) != d)):
+        raise ValueError(f"{name}: a token's heads must be contiguous")
+    stride = t.stride(0) if n > 1 else h * d
+    return t.data_ptr(), stride
+
+
+def _attention_config(q, k, causal, scale, strides=(0,) * 6) -> AttentionConfig:
+    d = q.shape[2]
+    return AttentionConfig(q.shape[1], k.shape[1], d, int(causal), d ** -0.5 if scale is None else scale, 0, *strides)
+
+
+def _ends(cu: torch.Tensor | None, name: str):
+    if cu is None:
+        return None, 1
+    if cu.dtype != torch.int32 or cu.dim() != 1 or cu.numel() < 1:
+        raise ValueError(f"{name}: a tensor of n_seq + 1 int32 ends expected")
+    return _ptr(cu), cu.numel() - 1
+
+
+def _attention_inputs(q, k, v, cu_q, cu_k):
+    if k.shape != v.shape or q.shape[2] != k.shape[2] or not (q.dtype == k.dtype == v.dtype):
+        raise ValueError("attention: q [Tq][Hq][D], k and v [Tk][Hkv][D] of one dtype expected")
+    if cu_k is None:
+        cu_k = cu_q
+    pq, n = _ends(cu_q, "cu_q")
+    pk, nk = _ends(cu_k, "cu_k")
+    if n != nk or (cu_q is None) != (cu_k is None):
+        raise ValueError("attention: cu_q and cu_k name the same sequences")
+    return pq, pk, n
+
+
+def attention_workspace_size(q: torch.Tensor, k: torch.Tensor, n_seq: int = 1) -> int:
+    """Workspace bytes of attention_fwd and attention_bwd on tensors of these shapes, packed into n_seq sequences."""
+    c = _attention_config(q, k, 0, 1.0)
+    size = lib().focus_attention_workspace_size
+    return max(int(size(call, ctypes.byref(c), q.shape[0], k.shape[0], n_seq))
+               for call in (CALL_ATTENTION_FWD, CALL_ATTENTION_BWD))
+
+
+def attention_fwd(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_q=None, cu_k=None, causal: bool = True,
+                  scale: float | None = None, want_lse: bool = True, ws=None, out=None, lse=None):
+    """Attention of q [Tq][Hq][D] over k, v [Tk][Hkv][D], sequences packed one after the other with ends cu_q, cu_k
+    (int32 [n_seq + 1] on the device; cu_k defaults to cu_q, both None: one sequence) -> (O [Tq][Hq][D], lse [Hq][Tq]
+    fp32 or None). q, k and v may be slices of one fused product (tokens apart). scale defaults to D ** -0.5."""
+    pq, pk, n = _attention_inputs(q, k, v, cu_q, cu_k)
+    (aq, sq), (ak, sk), (av, sv) = _heads(q, "q"), _heads(k, "k"), _heads(v, "v")
+    cfg = _attention_config(q, k, causal, scale, (sq, sk, sv, 0, 0, 0))
+    O = out if out is not None else torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    if O.shape != q.shape or O.dtype != q.dtype:
+        raise ValueError("attention_fwd: out has q's shape and dtype")
+    if lse is None and want_lse:
+        lse = torch.empty(q.shape[1], q.shape[0], dtype=torch.float32, device=q.device)
+    if lse is not None and (lse.shape != (q.shape[1], q.shape[0]) or lse.dtype != torch.float32):
+        raise ValueError("attention_fwd: lse is float32 [Hq][Tq]")
+    ws = _sized(ws, int(lib().focus_attention_workspace_size(CALL_ATTENTION_FWD, ctypes.byref(cfg), q.shape[0], k.shape[0],
+                                                             n)), q.device)
+    _check(lib().focus_attention_fwd(ctypes.byref(cfg), aq, ak, av, _dt(q), q.shape[0], k.shape[0], pq, pk, n, _ptr(O),
+                                     _ptr(lse), _ptr(ws), ws.numel(), _stream()), "focus_attention_fwd")
+    return O, lse
+
+
+def attention_bwd(dO: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, O: torch.Tensor, lse: torch.Tensor,
+                  cu_q=None, cu_k=None, causal: bool = True, scale: float | None = None, ws=None, out=None):
+    """Backward of attention_fwd from its outputs O and lse -> (dq, dk, dv) in q's dtype. `out`: preallocated (dq, dk, dv),
+    which may be slices of one fused gradient."""
+    pq, pk, n = _attention_inputs(q, k, v, cu_q, cu_k)
+    if dO.shape != q.shape or O.shape != q.shape or lse.shape != (q.shape[1], q.shape[0]):
+        raise ValueError("attention_bwd: dO and O have q's shape, lse is [Hq][Tq]")
+    if dO.dtype != q.dtype or O.dtype != q.dtype or lse.dtype != torch.float32:
+        raise TypeError("attention_bwd: dO and O have q's dtype, lse is float32")
+    if out is None:
+        out = tuple(torch.empty(t.shape, dtype=t.dtype, device=t.device) for t in (q, k, v))
+    dq, dk, dv = out
+    for g, t in ((dq, q), (dk, k), (dv, v)):
+        if g.shape != t.shape or g.dtype != t.dtype:
+            raise ValueError("attention_bwd: the gradients have the shapes and dtype of q, k, v")
+    ptrs = [_heads(t, name) for t, name in ((q, "q"), (k, "k"), (v, "v"), (dq, "dq"), (dk, "dk"), (dv, "dv"))]
+    cfg = _attention_config(q, k, causal, scale, tuple(s for _, s in ptrs))
+    ws = _sized(ws, int(lib().focus_attention_workspace_size(CALL_ATTENTION_BWD, ctypes.byref(cfg), q.shape[0], k.shape[0],
+                                                             n)), q.device)
+    (aq, ak, av, adq, adk, adv) = (a for a, _ in ptrs)
+    _check(lib().focus_attention_bwd(ctypes.byref(cfg), _ptr(dO), aq, ak, av, _ptr(O), _ptr(lse), _dt(q), q.shape[0],
+                                     k.shape[0], pq, pk, n, adq, adk, adv, _ptr(ws), ws.numel(), _stream()),
+           "focus_attention_bwd")
+    return dq, dk, dv
+
+
+def token_logprobs_workspace_size(T: int, V: int, top: int = 0) -> int:
+    """Workspace bytes of token_logprobs (and token_logprobs_bwd) on T rows of V logits."""
+    return int(lib().focus_workspace_size(CALL_TOKEN_LOGPROBS, None, T, V, top))
+
+
+def _targets(target, T: int):
+    if target is not None and (target.shape != (T,) or target.dtype != torch.int64):
+        raise ValueError("targets are int64 [T]")
+    return _ptr(target)
+
+
+def token_logprobs(Z: torch.Tensor, target=None, top: int = 0, ws=None):
+    """Log probabilities under logits Z [T][V] -> (logp [T] of the tokens `target` (int64; below zero: left out, 0) or
+    None, entropy [T], lse [T], top_logp [T][top] or None, top_index [T][top] int32 or None), fp32."""
+    T, V = Z.shape
+    f32 = dict(dtype=torch.float32, device=Z.device)
+    pt = _targets(target, T)
+    logp = torch.empty(T, **f32) if target is not None else None
+    entropy, lse = torch.empty(T, **f32), torch.empty(T, **f32)
+    top_logp = top_index = None
+    if top:
+        top_logp = torch.empty(T, max(0, top), **f32)
+        top_index = torch.empty(T, max(0, top), dtype=torch.int32, device=Z.device)
+    ws = _sized(ws, token_logprobs_workspace_size(T, V, top), Z.device)
+    _check(lib().focus_token_logprobs(_ptr(Z), _dt(Z), T, V, pt, top, _ptr(logp), _ptr(entropy), _ptr(lse), _ptr(top_logp),
+                                      _ptr(top_index), _ptr(ws), ws.numel(), _stream()), "focus_token_logprobs")
+    return logp, entropy, lse, top_logp, top_index
+
+
+def token_logprobs_bwd(Z: torch.Tensor, target, lse: torch.Tensor, entropy=None, d_logp=None, d_entropy=None, ws=None,
+                       out=None) -> torch.Tensor:
+    """Gradient of token_logprobs' logp and entropy -> dZ [T][V] in Z's dtype (`out` may be Z itself)."""
+    T, V = Z.shape
+    for t in (lse, entropy, d_logp, d_entropy):
+        if t is not None and (t.shape != (T,) or t.dtype != torch.float32):
+            raise ValueError("token_logprobs_bwd: lse, entropy and their gradients are float32 [T]")
+    dZ = out if out is not None else torch.empty_like(Z)
+    if dZ.shape != Z.shape or dZ.dtype != Z.dtype:
+        raise ValueError("token_logprobs_bwd: out has Z's shape and dtype")
+    ws = _sized(ws, 256, Z.device)
+    _check(lib().focus_token_logprobs_bwd(_ptr(Z), _dt(Z), T, V, _targets(target, T), _ptr(lse), _ptr(entropy), _ptr(d_logp),
+                                          _ptr(d_entropy), _ptr(dZ), _ptr(ws), ws.numel(), _stream()),
+           "focus_token_logprobs_bwd")
+    return dZ
 
 
 def check_flags(ws: torch.Tensor) -> int:
