@@ -124,7 +124,7 @@ __global__ void __launch_bounds__(kThreads) attn_fwd_kernel(AttnArgs a) {
     __shared__ float stat[2][kWaves][32];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5, col = lane & 31;
     int tile;
-    const int s = slot_sequence(a.cu_q, a.n_seq, kTile, (int)blockIdx.x, tile);
+    const int s = slot_sequence(a.cu_q, a.n_seq, kTile, (int)blockIdx.x, 1, tile);
     SeqRange r;
     seq_range(a, s, r);
     check_ends<kThreads>(a);
@@ -198,7 +198,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_bwd_q_kernel(AttnArgs a) {
     __shared__ float lds[2 * DT * 16 * 64];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5, col = lane & 31;
     int tile;
-    const int s = slot_sequence(a.cu_q, a.n_seq, kTile, (int)blockIdx.x, tile);
+    const int s = slot_sequence(a.cu_q, a.n_seq, kTile, (int)blockIdx.x, 1, tile);
     SeqRange r;
     seq_range(a, s, r);
     check_ends<kThreads>(a);
@@ -247,7 +247,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_bwd_kv_kernel(AttnArgs a) {
     __shared__ float lds[2 * DT * 16 * 64];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5, col = lane & 31;
     int tile;
-    const int s = slot_sequence(a.cu_k, a.n_seq, kTile, (int)blockIdx.x, tile);
+    const int s = slot_sequence(a.cu_k, a.n_seq, kTile, (int)blockIdx.x, 1, tile);
     SeqRange r;
     seq_range(a, s, r);
     check_ends<kThreads>(a);
@@ -327,7 +327,7 @@ size_t attn_bwd_ws(int64_t Tq, int64_t, int Hq, int, int, int64_t) {
 }
 
 hipError_t launch_attn_fwd(int dtype, const AttnArgs &a, void *, hipStream_t st) {
-    return dtype == kBF16 ? fwd<uint16_t>(a, st) : fwd<float>(a, st);
+    return dtype == kBF16 ? launch_attn_fwd_bf16(a, st) : fwd<float>(a, st);
 }
 
 hipError_t launch_attn_bwd(int dtype, AttnArgs a, void *ws, hipStream_t st) {

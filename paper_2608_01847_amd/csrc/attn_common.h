@@ -32,19 +32,20 @@ __device__ __forceinline__ void seq_range(const AttnArgs &a, int s, SeqRange &r)
     r.lk = ok ? (int)(kb - ka) : 0;
 }
 
-// Tiles of `rows` rows over packed sequences with ends cu[0..n]: sequence i's tiles take the slots from
-// cu[i] / rows + i on, which leaves room for ceil(length / rows) of them whatever the lengths are, so the number of
-// slots, T / rows + n, needs no look at the lengths on the host. Returns the sequence, `tile` its tile, which may
+// Tiles of `rows` rows over packed sequences with ends cu[0..n], `each` rows per token: sequence i's tiles take the
+// slots from cu[i] each / rows + i on, which leaves room for ceil(length / rows) of them whatever the lengths are, so the number of
+// slots, T each / rows + n, needs no look at the lengths on the host. Returns the sequence, `tile` its tile, which may
 // lie past its end or, in slots before the first sequence, be -1: nothing to do (tile_rows below).
-__device__ __forceinline__ int slot_sequence(const int32_t *cu, int n, int rows, int slot, int &tile) {
+__device__ __forceinline__ int slot_sequence(const int32_t *cu, int n, int rows, int slot, int each, int &tile) {
     if (!cu) {
         tile = slot;
         return 0;
     }
+    auto start_of = [&](int i) { return (int)((int64_t)cu[i] * each / rows) + i; };
     int lo = 0, len = n;  // the answer is in [lo, lo + len)
     while (len > 64) {    // a scalar bisection down to one wave's width
         const int half = len / 2;
-        if (cu[lo + half] / rows + lo + half <= slot) {
+        if (start_of(lo + half) <= slot) {
             lo += half;
             len -= half;
         } else {
@@ -52,15 +53,15 @@ __device__ __forceinline__ int slot_sequence(const int32_t *cu, int n, int rows,
         }
     }
     const int lane = threadIdx.x & 63;
-    const int start = lane < len ? cu[lo + lane] / rows + lo + lane : 0x7FFFFFFF;
+    const int start = lane < len ? start_of(lo + lane) : 0x7FFFFFFF;
     const unsigned long long below = __ballot(start <= slot);
     const int s = __builtin_amdgcn_readfirstlane(lo + (below ? 63 - __builtin_clzll(below) : 0));
-    tile = below ? slot - __builtin_amdgcn_readfirstlane(cu[s] / rows + s) : -1;
+    tile = below ? slot - __builtin_amdgcn_readfirstlane(start_of(s)) : -1;
     return s;
 }
 
 // Whether a tile of `rows` rows has any of a sequence's n
-__device__ __forceinline__ bool tile_in(int tile, int rows, int n) { return tile >= 0 && (int64_t)tile * rows < n; }
+__device__ __forceinline__ bool tile_in(int tile, int rows, int64_t n) { return tile >= 0 && (int64_t)tile * rows < n; }
 
 // Every pair of ends, by the first workgroup of a launch (the others meet only those of their own tiles)
 template <int THREADS>
@@ -72,5 +73,7 @@ __device__ __forceinline__ void check_ends(const AttnArgs &a) {
 
 // row of register r in the 32 x 32 accumulator of a lane: 8 (r / 4) + 4 (lane / 32) + r % 4
 __device__ __forceinline__ constexpr int acc_row(int r) { return (r & 3) + 8 * (r >> 2); }
+
+hipError_t launch_attn_fwd_bf16(const AttnArgs &a, hipStream_t st);
 
 }  // namespace focus

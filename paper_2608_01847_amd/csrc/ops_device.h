@@ -12,12 +12,14 @@ __device__ __forceinline__ float load_one(const float *p) { return *p; }
 __device__ __forceinline__ void store_one(uint16_t *p, float v) { *p = (uint16_t)f32_to_bf16_bits(v); }
 __device__ __forceinline__ void store_one(float *p, float v) { *p = v; }
 
-// Two fp32 values rounded to bf16 (to nearest, ties to even), the first in the low half. One instruction; written
-// out because the toolchain in use miscompiles the two-element vector conversion for gfx950.
+// Two fp32 values rounded to bf16 (to nearest, ties to even), the first in the low half: one v_cvt_pk_bf16_f32, left to
+// the compiler, which knows what may not directly precede it (the instruction after an exponential may not read it)
 __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
-    uint32_t r;
-    asm("v_cvt_pk_bf16_f32 %0, %1, %2" : "=v"(r) : "v"(lo), "v"(hi));
-    return r;
+    typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
+    bf16x2_t v;
+    v[0] = (__bf16)lo;
+    v[1] = (__bf16)hi;
+    return __builtin_bit_cast(uint32_t, v);
 }
 
 __device__ __forceinline__ void zero8(float (&v)[8]) {
