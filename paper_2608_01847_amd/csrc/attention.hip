@@ -332,7 +332,7 @@ hipError_t launch_attn_fwd(int dtype, const AttnArgs &a, void *, hipStream_t st)
 
 hipError_t launch_attn_bwd(int dtype, AttnArgs a, void *ws, hipStream_t st) {
     a.delta = reinterpret_cast<float *>(static_cast<char *>(ws) + kWsHeader);
-    return dtype == kBF16 ? bwd<uint16_t>(a, st) : bwd<float>(a, st);
+    return dtype == kBF16 ? launch_attn_bwd_bf16(a, st) : bwd<float>(a, st);
 }
 
 }  // namespace focus

@@ -128,15 +128,6 @@ __device__ __forceinline__ bf16x8_t pack8(const f32x16_t &p, int s) {
     return __builtin_bit_cast(bf16x8_t, w);
 }
 
-// A wave's 32 query rows: this lane's row, and the key ranges that the wave sees
-struct Rows {
-    bool ok;
-    int q, g;       // this lane's query and head of the group
-    int seen;       // last key that it sees
-    int all_seen;   // last key that every row of the wave sees
-    int any_seen;   // last key that some row sees (-1: none)
-};
-
 template <int DT>
 __device__ __forceinline__ void load_row(const uint16_t *row, bool ok, int D, int half, bf16x8_t (&v)[2 * DT]) {
 #pragma unroll
@@ -167,6 +158,39 @@ __device__ __forceinline__ void store_row(uint16_t *row, bool ok, int D, int hal
         }
 }
 
+// What a wave's lane does in the kernels whose columns are query rows: its row, and the keys that it, its wave and its
+// workgroup see.
+struct RowTile {
+    int64_t rows;   // of the sequence and key-value head
+    bool ok;
+    int q, h;       // this lane's query (in its sequence) and head
+    int seen;       // last key that it sees
+    int all_seen;   // last key that every row of the wave sees
+    int any_seen;   // last key that some row of the wave sees (-1: none)
+    int nk;         // tiles of 64 keys that the workgroup goes through
+    __device__ __forceinline__ void init(const AttnArgs &a, const SeqRange &r, int tile, int hk, int wave, int col) {
+        constexpr int kRows = 32 * kWaves;
+        const int group = a.Hq / a.Hkv, shift = r.lk - r.lq;
+        rows = (int64_t)r.lq * group;
+        const int64_t first = (int64_t)tile * kRows;
+        const int64_t last = first + kRows < rows ? first + kRows - 1 : rows - 1;
+        auto sees = [&](int64_t row) {
+            const int k = a.causal ? (int)(row / group) + shift : r.lk - 1;
+            return k < r.lk ? k : r.lk - 1;
+        };
+        const int k_end = sees(last) + 1;
+        nk = k_end > 0 ? (k_end + kKeys - 1) / kKeys : 0;
+        const int64_t w_first = first + 32 * wave, w_last = w_first + 31 < last ? w_first + 31 : last;
+        any_seen = w_first <= last ? sees(w_last) : -1;
+        all_seen = sees(w_first);
+        const int64_t row = w_first + col;
+        ok = row <= last;
+        q = (int)(row / group);
+        h = hk * group + (int)(row - (int64_t)q * group);
+        seen = ok ? sees(row) : r.lk - 1;
+    }
+};
+
 template <int DT>
 __global__ void __launch_bounds__(kThreads, 2) attn_fwd_bf16_kernel(AttnArgs a) {
     using G = Tile<DT>;
@@ -180,21 +204,10 @@ __global__ void __launch_bounds__(kThreads, 2) attn_fwd_bf16_kernel(AttnArgs a) 
     seq_range(a, s, r);
     check_ends<kThreads>(a);
     if (!tile_in(tile, kRows, (int64_t)r.lq * group)) return;
-    const int shift = r.lk - r.lq;
-    const int64_t rows = (int64_t)r.lq * group, first = (int64_t)tile * kRows;
-    const int64_t last = first + kRows < rows ? first + kRows - 1 : rows - 1;
-    auto sees = [&](int64_t row) {
-        const int k = a.causal ? (int)(row / group) + shift : r.lk - 1;
-        return k < r.lk ? k : r.lk - 1;
-    };
-    const int k_end = sees(last) + 1;
-    const int nk = k_end > 0 ? (k_end + kKeys - 1) / kKeys : 0;
-    const int64_t w_first = first + 32 * wave, w_last = w_first + 31 < last ? w_first + 31 : last;
-    const int any_seen = w_first <= last ? sees(w_last) : -1, all_seen = sees(w_first);
-    const int64_t row = w_first + col;
-    const bool ok = row <= last;
-    const int q = (int)(row / group), h = hk * group + (int)(row - (int64_t)q * group);
-    const int seen = ok ? sees(row) : r.lk - 1;
+    RowTile w;
+    w.init(a, r, tile, hk, wave, col);
+    const int nk = w.nk, seen = w.seen, all_seen = w.all_seen, any_seen = w.any_seen, q = w.q, h = w.h;
+    const bool ok = w.ok;
 
     bf16x8_t qv[2 * DT];
     load_row<DT>(static_cast<const uint16_t *>(a.q) + (r.q0 + q) * a.q_stride + (int64_t)h * D, ok, D, half, qv);
@@ -293,6 +306,222 @@ __global__ void __launch_bounds__(kThreads, 2) attn_fwd_bf16_kernel(AttnArgs a) 
     if (a.lse && ok && half == 0) a.lse[(int64_t)h * a.Tq + r.q0 + q] = l == 0.0f ? kNone : (m + log2f(l)) * kLn2;
 }
 
+// dq of 128 query rows, and delta = rowsum(dO O) for the keys' pass. Both score-shaped products are transposed as in the
+// forward, so dS is the B operand of dq^T = k^T dS^T as it stands.
+template <int DT>
+__global__ void __launch_bounds__(kThreads, 2) attn_bwd_q_bf16_kernel(AttnArgs a) {
+    using G = Tile<DT>;
+    __shared__ __attribute__((aligned(16))) char smem[4 * G::kBytes];  // K, K, V, V
+    constexpr int kRows = 32 * kWaves;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5, col = lane & 31;
+    const int hk = blockIdx.x % a.Hkv, group = a.Hq / a.Hkv, D = a.D;
+    int tile;
+    const int s = slot_sequence(a.cu_q, a.n_seq, kRows, (int)(gridDim.x / a.Hkv - 1 - blockIdx.x / a.Hkv), group, tile);
+    SeqRange r;
+    seq_range(a, s, r);
+    check_ends<kThreads>(a);
+    if (!tile_in(tile, kRows, (int64_t)r.lq * group)) return;
+    RowTile w;
+    w.init(a, r, tile, hk, wave, col);
+
+    bf16x8_t qv[2 * DT], gv[2 * DT];
+    const int64_t at = ((r.q0 + w.q) * a.Hq + w.h) * D, stat = (int64_t)w.h * a.Tq + r.q0 + w.q;
+    load_row<DT>(static_cast<const uint16_t *>(a.O) + at, w.ok, D, half, qv);
+    load_row<DT>(static_cast<const uint16_t *>(a.dO) + at, w.ok, D, half, gv);
+    float delta = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 2 * DT; i++)
+#pragma unroll
+        for (int e = 0; e < 8; e++) delta = __builtin_fmaf((float)qv[i][e], (float)gv[i][e], delta);
+    delta = sum_halves(delta);
+    if (w.ok && half == 0) a.delta[stat] = delta;
+    load_row<DT>(static_cast<const uint16_t *>(a.q) + (r.q0 + w.q) * a.q_stride + (int64_t)w.h * D, w.ok, D, half, qv);
+    const float c = a.scale * kLog2e;
+    const float lse2 = w.ok ? a.lse[stat] * kLog2e : 0.0f;
+
+    const uint16_t *K = static_cast<const uint16_t *>(a.k) + r.k0 * a.k_stride + (int64_t)hk * D;
+    const uint16_t *V = static_cast<const uint16_t *>(a.v) + r.k0 * a.v_stride + (int64_t)hk * D;
+    Stager<DT> ks, vs;
+    ks.init(a.k_stride, D);
+    vs.init(a.v_stride, D);
+    Frags<DT> f;
+    f.init(lane);
+    const uint32_t base = Stager<DT>::lds_addr(smem);
+    f32x16_t dq[DT] = {};
+    if (w.nk > 0) {
+        ks.load(K, a.k_stride, 0, r.lk, D);
+        vs.load(V, a.v_stride, 0, r.lk, D);
+        ks.store(smem);
+        vs.store(smem + 2 * G::kBytes);
+    }
+    __syncthreads();
+    for (int j = 0; j < w.nk; j++) {
+        const int st = j & 1, k0 = j * kKeys;
+        const uint32_t kt = base + st * G::kBytes, vt = base + (2 + st) * G::kBytes;
+        const bool more = j + 1 < w.nk, active = k0 <= w.any_seen;
+        if (more) ks.load(K, a.k_stride, k0 + kKeys, r.lk, D);
+        auto block = [&](int b) {
+            f32x16_t sc = {}, dp = {};
+#pragma unroll
+            for (int i = 0; i < 2 * DT; i++) {
+                sc = mfma(f.straight(kt, b, i), qv[i], sc);
+                dp = mfma(f.straight(vt, b, i), gv[i], dp);
+            }
+#pragma unroll
+            for (int i = 0; i < 16; i++) sc[i] = exp2_raw(__builtin_fmaf(sc[i], c, -lse2)) * (dp[i] - delta);
+            if (k0 + 32 * b + 31 > w.all_seen) {
+#pragma unroll
+                for (int i = 0; i < 16; i++)
+                    if (k0 + 32 * b + acc_row(i) + 4 * half > w.seen) sc[i] = 0.0f;
+            }
+#pragma unroll
+            for (int i = 0; i < 2; i++) {
+                const bf16x8_t ds = pack8(sc, i);
+#pragma unroll
+                for (int t = 0; t < DT; t++) dq[t] = mfma(f.transposed(kt, 2 * b + i, t), ds, dq[t]);
+            }
+        };
+        if (active) block(0);
+        if (more) {
+            ks.store(smem + (st ^ 1) * G::kBytes);
+            vs.load(V, a.v_stride, k0 + kKeys, r.lk, D);
+        }
+        if (active) block(1);
+        if (more) vs.store(smem + (2 + (st ^ 1)) * G::kBytes);
+        __syncthreads();
+    }
+    store_row<DT>(static_cast<uint16_t *>(a.dq) + (r.q0 + w.q) * a.dq_stride + (int64_t)w.h * D, w.ok, D, half, dq, a.scale);
+}
+
+// dk and dv of 128 keys of one key-value head, 32 per wave, over the queries of every head that shares it, head by head.
+// Here a lane's column is a key and the queries run down the accumulators (S = q k^T as it is written): P and dS are the
+// B operands of dv^T = dO^T P and dk^T = q^T dS. Queries and their gradients go through LDS in tiles of 64 with their lse
+// and delta; a query that does not exist, or sees nothing, has lse = +inf there and so probability 0.
+template <int DT>
+__global__ void __launch_bounds__(kThreads, 1) attn_bwd_kv_bf16_kernel(AttnArgs a) {
+    using G = Tile<DT>;
+    __shared__ __attribute__((aligned(16))) char smem[4 * G::kBytes];  // q, q, dO, dO
+    __shared__ __attribute__((aligned(16))) float stats[2][2][kKeys];  // [stage][lse log2 e, delta]
+    constexpr int kRows = 32 * kWaves;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5, col = lane & 31;
+    const int hk = blockIdx.x % a.Hkv, group = a.Hq / a.Hkv, D = a.D;
+    int tile;
+    const int s = slot_sequence(a.cu_k, a.n_seq, kRows, (int)(blockIdx.x / a.Hkv), 1, tile);
+    SeqRange r;
+    seq_range(a, s, r);
+    check_ends<kThreads>(a);
+    if (!tile_in(tile, kRows, r.lk)) return;
+    const int shift = r.lk - r.lq, w_first = tile * kRows + 32 * wave, k = w_first + col;
+    const bool ok = k < r.lk;
+    // the first query that sees a key: of the workgroup's tile (where the loop starts), of the wave's first and last
+    // key, of this lane's
+    auto seen_from = [&](int key) { return a.causal && key > shift ? key - shift : 0; };
+    const int q_first = seen_from(tile * kRows) / kKeys * kKeys;
+    const int any_from = seen_from(w_first), all_from = seen_from(w_first + 31), from = seen_from(k);
+    const int per_head = r.lq > q_first ? (r.lq - q_first + kKeys - 1) / kKeys : 0;
+    const int items = per_head * group;
+
+    bf16x8_t kv[2 * DT], vv[2 * DT];
+    load_row<DT>(static_cast<const uint16_t *>(a.k) + (r.k0 + k) * a.k_stride + (int64_t)hk * D, ok, D, half, kv);
+    load_row<DT>(static_cast<const uint16_t *>(a.v) + (r.k0 + k) * a.v_stride + (int64_t)hk * D, ok, D, half, vv);
+    const float c = a.scale * kLog2e;
+    const int64_t g_stride = (int64_t)a.Hq * D;
+    const uint16_t *Q = static_cast<const uint16_t *>(a.q) + r.q0 * a.q_stride + (int64_t)hk * group * D;
+    const uint16_t *dO = static_cast<const uint16_t *>(a.dO) + r.q0 * g_stride + (int64_t)hk * group * D;
+    const int64_t stat = (int64_t)hk * group * a.Tq + r.q0;
+    Stager<DT> qs, gs;
+    qs.init(a.q_stride, D);
+    gs.init(g_stride, D);
+    Frags<DT> f;
+    f.init(lane);
+    const uint32_t base = Stager<DT>::lds_addr(smem);
+    float sv = 0.0f;
+    auto load_stats = [&](int head, int q0) {
+        if (threadIdx.x < 2 * kKeys) {
+            const int row = q0 + (threadIdx.x & (kKeys - 1)), which = threadIdx.x / kKeys;
+            const int64_t at = stat + (int64_t)head * a.Tq + row;
+            sv = which == 0 ? __builtin_inff() : 0.0f;
+            if (row < r.lq) sv = which == 0 ? a.lse[at] * kLog2e : a.delta[at];
+            if (which == 0 && sv == kNone) sv = __builtin_inff();
+        }
+    };
+    auto store_stats = [&](int stage) {
+        if (threadIdx.x < 2 * kKeys) (&stats[stage][0][0])[threadIdx.x] = sv;
+    };
+    f32x16_t dk[DT] = {}, dv[DT] = {};
+    if (items > 0) {
+        qs.load(Q, a.q_stride, q_first, r.lq, D);
+        gs.load(dO, g_stride, q_first, r.lq, D);
+        load_stats(0, q_first);
+        qs.store(smem);
+        gs.store(smem + 2 * G::kBytes);
+        store_stats(0);
+    }
+    __syncthreads();
+    int head = 0, q0 = q_first;
+    for (int it = 0; it < items; it++) {
+        const int st = it & 1;
+        const uint32_t qt = base + st * G::kBytes, gt = base + (2 + st) * G::kBytes;
+        const bool more = it + 1 < items, active = q0 + kKeys > any_from;
+        int next_head = head, next_q0 = q0 + kKeys;
+        if (next_q0 >= r.lq) {
+            next_head++;
+            next_q0 = q_first;
+        }
+        if (more) {
+            qs.load(Q + (int64_t)next_head * D, a.q_stride, next_q0, r.lq, D);
+            gs.load(dO + (int64_t)next_head * D, g_stride, next_q0, r.lq, D);
+            load_stats(next_head, next_q0);
+        }
+        if (active) {
+#pragma unroll
+            for (int b = 0; b < 2; b++) {
+                f32x16_t sc = {}, dp = {};
+#pragma unroll
+                for (int i = 0; i < 2 * DT; i++) sc = mfma(f.straight(qt, b, i), kv[i], sc);
+#pragma unroll
+                for (int i = 0; i < 2 * DT; i++) dp = mfma(f.straight(gt, b, i), vv[i], dp);
+#pragma unroll
+                for (int g = 0; g < 4; g++) {
+                    const f32x4_any_t ls = *reinterpret_cast<const f32x4_any_t *>(&stats[st][0][32 * b + 8 * g + 4 * half]);
+                    const f32x4_any_t de = *reinterpret_cast<const f32x4_any_t *>(&stats[st][1][32 * b + 8 * g + 4 * half]);
+#pragma unroll
+                    for (int e = 0; e < 4; e++) {
+                        sc[4 * g + e] = exp2_raw(__builtin_fmaf(sc[4 * g + e], c, -ls[e]));
+                        dp[4 * g + e] -= de[e];
+                    }
+                }
+                if (q0 + 32 * b < all_from) {
+#pragma unroll
+                    for (int i = 0; i < 16; i++)
+                        if (q0 + 32 * b + acc_row(i) + 4 * half < from) sc[i] = dp[i] = 0.0f;
+                }
+#pragma unroll
+                for (int i = 0; i < 16; i++) dp[i] *= sc[i];
+#pragma unroll
+                for (int i = 0; i < 2; i++) {
+                    const bf16x8_t p = pack8(sc, i), ds = pack8(dp, i);
+#pragma unroll
+                    for (int t = 0; t < DT; t++) {
+                        dv[t] = mfma(f.transposed(gt, 2 * b + i, t), p, dv[t]);
+                        dk[t] = mfma(f.transposed(qt, 2 * b + i, t), ds, dk[t]);
+                    }
+                }
+            }
+        }
+        if (more) {
+            qs.store(smem + (st ^ 1) * G::kBytes);
+            gs.store(smem + (2 + (st ^ 1)) * G::kBytes);
+            store_stats(st ^ 1);
+        }
+        head = next_head;
+        q0 = next_q0;
+        __syncthreads();
+    }
+    store_row<DT>(static_cast<uint16_t *>(a.dk) + (r.k0 + k) * a.dk_stride + (int64_t)hk * D, ok, D, half, dk, a.scale);
+    store_row<DT>(static_cast<uint16_t *>(a.dv) + (r.k0 + k) * a.dv_stride + (int64_t)hk * D, ok, D, half, dv, 1.0f);
+}
+
 template <typename F>
 void pick_dt(int D, F &&f) {
     if (D <= 64) f(std::integral_constant<int, 2>{});
@@ -305,6 +534,17 @@ void pick_dt(int D, F &&f) {
 hipError_t launch_attn_fwd_bf16(const AttnArgs &a, hipStream_t st) {
     const int64_t slots = a.Tq * (a.Hq / a.Hkv) / (32 * kWaves) + a.n_seq;
     pick_dt(a.D, [&](auto dt) { attn_fwd_bf16_kernel<decltype(dt)::value><<<(unsigned)(slots * a.Hkv), kThreads, 0, st>>>(a); });
+    return hipGetLastError();
+}
+
+hipError_t launch_attn_bwd_bf16(const AttnArgs &a, hipStream_t st) {
+    constexpr int kRows = 32 * kWaves;
+    const int64_t q_slots = a.Tq * (a.Hq / a.Hkv) / kRows + a.n_seq, k_slots = a.Tk / kRows + a.n_seq;
+    pick_dt(a.D, [&](auto dt) {
+        constexpr int DT = decltype(dt)::value;
+        if (a.Tq > 0) attn_bwd_q_bf16_kernel<DT><<<(unsigned)(q_slots * a.Hkv), kThreads, 0, st>>>(a);
+        if (a.Tk > 0) attn_bwd_kv_bf16_kernel<DT><<<(unsigned)(k_slots * a.Hkv), kThreads, 0, st>>>(a);
+    });
     return hipGetLastError();
 }
 

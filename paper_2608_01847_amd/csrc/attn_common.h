@@ -75,5 +75,6 @@ __device__ __forceinline__ void check_ends(const AttnArgs &a) {
 __device__ __forceinline__ constexpr int acc_row(int r) { return (r & 3) + 8 * (r >> 2); }
 
 hipError_t launch_attn_fwd_bf16(const AttnArgs &a, hipStream_t st);
+hipError_t launch_attn_bwd_bf16(const AttnArgs &a, hipStream_t st);
 
 }  // namespace focus
