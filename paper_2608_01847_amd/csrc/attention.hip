@@ -320,14 +320,18 @@ hipError_t bwd(const AttnArgs &a, hipStream_t st) {
 
 }  // namespace
 
-size_t attn_fwd_ws(int64_t, int64_t, int, int, int, int64_t) { return kWsHeader; }
+size_t attn_fwd_ws(int64_t Tq, int64_t Tk, int Hq, int Hkv, int D, int64_t n_seq) {
+    const int splits = attn_splits_bf16(Tq, Tk, Hq, Hkv, n_seq);
+    if (splits == 1) return kWsHeader;
+    return kWsHeader + attn_part_stats(splits, Tq * Hq) + (size_t)splits * (size_t)(Tq * Hq) * (size_t)D * sizeof(float);
+}
 
 size_t attn_bwd_ws(int64_t Tq, int64_t, int Hq, int, int, int64_t) {
     return kWsHeader + (size_t)Tq * (size_t)Hq * sizeof(float);
 }
 
-hipError_t launch_attn_fwd(int dtype, const AttnArgs &a, void *, hipStream_t st) {
-    return dtype == kBF16 ? launch_attn_fwd_bf16(a, st) : fwd<float>(a, st);
+hipError_t launch_attn_fwd(int dtype, const AttnArgs &a, void *ws, hipStream_t st) {
+    return dtype == kBF16 ? launch_attn_fwd_bf16(a, ws, st) : fwd<float>(a, st);
 }
 
 hipError_t launch_attn_bwd(int dtype, AttnArgs a, void *ws, hipStream_t st) {

@@ -191,8 +191,10 @@ struct RowTile {
     }
 };
 
-template <int DT>
-__global__ void __launch_bounds__(kThreads, 2) attn_fwd_bf16_kernel(AttnArgs a) {
+// SPLIT: the tiles of keys are dealt to gridDim.y workgroups, each leaving its unnormalised output, reference and sum in
+// fp32 for attn_join_kernel.
+template <int DT, bool SPLIT>
+__global__ void __launch_bounds__(kThreads, 2) attn_fwd_bf16_kernel(AttnArgs a, AttnParts parts) {
     using G = Tile<DT>;
     __shared__ __attribute__((aligned(16))) char smem[4 * G::kBytes];  // K, K, V, V
     constexpr int kRows = 32 * kWaves;
@@ -206,7 +208,9 @@ __global__ void __launch_bounds__(kThreads, 2) attn_fwd_bf16_kernel(AttnArgs a) 
     if (!tile_in(tile, kRows, (int64_t)r.lq * group)) return;
     RowTile w;
     w.init(a, r, tile, hk, wave, col);
-    const int nk = w.nk, seen = w.seen, all_seen = w.all_seen, any_seen = w.any_seen, q = w.q, h = w.h;
+    const int per = SPLIT ? (w.nk + (int)gridDim.y - 1) / (int)gridDim.y : w.nk;
+    const int j0 = SPLIT ? (int)blockIdx.y * per : 0, nk = SPLIT && j0 + per < w.nk ? j0 + per : w.nk;  // tiles j0 .. nk - 1
+    const int seen = w.seen, all_seen = w.all_seen, any_seen = w.any_seen, q = w.q, h = w.h;
     const bool ok = w.ok;
 
     bf16x8_t qv[2 * DT];
@@ -229,15 +233,15 @@ __global__ void __launch_bounds__(kThreads, 2) attn_fwd_bf16_kernel(AttnArgs a) 
 
     f32x16_t o[DT] = {};
     float m = kNone, l = 0.0f;
-    if (nk > 0) {
-        ks.load(K, a.k_stride, 0, r.lk, D);
-        vs.load(V, a.v_stride, 0, r.lk, D);
+    if (j0 < nk) {
+        ks.load(K, a.k_stride, j0 * kKeys, r.lk, D);
+        vs.load(V, a.v_stride, j0 * kKeys, r.lk, D);
         ks.store(smem);
         vs.store(smem + 2 * G::kBytes);
     }
     __syncthreads();
-    for (int j = 0; j < nk; j++) {
-        const int st = j & 1, k0 = j * kKeys;
+    for (int j = j0; j < nk; j++) {
+        const int st = (j - j0) & 1, k0 = j * kKeys;
         const uint32_t kt = base + st * G::kBytes, vt = base + (2 + st) * G::kBytes;
         const bool more = j + 1 < nk, active = k0 <= any_seen;
         if (more) ks.load(K, a.k_stride, k0 + kKeys, r.lk, D);
@@ -300,10 +304,74 @@ __global__ void __launch_bounds__(kThreads, 2) attn_fwd_bf16_kernel(AttnArgs a) 
         __syncthreads();
     }
     l = sum_halves(l);
+    if constexpr (SPLIT) {
+        const int64_t at = ((int64_t)blockIdx.y * a.Hq + h) * a.Tq + r.q0 + q;
+        if (ok && half == 0) {
+            parts.m[at] = m;
+            parts.l[at] = l;
+        }
+        if (l == 0.0f) return;  // the join does not look at this part's output
+#pragma unroll
+        for (int t = 0; t < DT; t++)
+#pragma unroll
+            for (int g = 0; g < 4; g++) {
+                const int d = 32 * t + 8 * g + 4 * half;
+                if (ok && d < D)
+                    *reinterpret_cast<float4 *>(parts.o + at * D + d) =
+                        make_float4(o[t][4 * g], o[t][4 * g + 1], o[t][4 * g + 2], o[t][4 * g + 3]);
+            }
+        return;
+    }
     // no key seen: zeros and -inf; a NaN among the scores stays one
     const float inv = l == 0.0f ? 0.0f : 1.0f / l;
     store_row<DT>(static_cast<uint16_t *>(a.O) + ((r.q0 + q) * a.Hq + h) * D, ok, D, half, o, inv);
     if (a.lse && ok && half == 0) a.lse[(int64_t)h * a.Tq + r.q0 + q] = l == 0.0f ? kNone : (m + log2f(l)) * kLn2;
+}
+
+// Joins the parts of a split forward, a workgroup per row, two features per lane: each wave adds a run of the parts in
+// order, eight loads under way, and the waves' sums are added in order.
+__global__ void __launch_bounds__(kThreads) attn_join_kernel(AttnArgs a, AttnParts parts, int splits) {
+    __shared__ float2 lds[kWaves][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int64_t rows = (int64_t)a.Hq * a.Tq, row = blockIdx.x;
+    const int h = (int)(row / a.Tq);
+    const int64_t q = row - (int64_t)h * a.Tq;
+    if (a.cu_q && (q < a.cu_q[0] || q >= a.cu_q[a.n_seq])) return;  // a row of no sequence
+    const float m = lane < splits ? parts.m[lane * rows + row] : kNone, l = lane < splits ? parts.l[lane * rows + row] : 0.0f;
+    const float top = wave_max(m);
+    const float w = top == kNone ? 1.0f : exp2_raw(m - top);
+    const float total = wave_sum(l * w);
+    const int per = (splits + kWaves - 1) / kWaves, s1 = (wave + 1) * per < splits ? (wave + 1) * per : splits;
+    float x = 0.0f, y = 0.0f;
+    for (int s0 = wave * per; s0 < s1; s0 += 8) {
+        float2 v[8];
+#pragma unroll
+        for (int i = 0; i < 8; i++) {
+            const int s = s0 + i < s1 ? s0 + i : s0;
+            v[i] = {0.0f, 0.0f};
+            // a part that saw no key has left no output
+            if (s0 + i < s1 && __shfl(l, s, 64) != 0.0f && 2 * lane < a.D)
+                v[i] = *reinterpret_cast<const float2 *>(parts.o + (s * rows + row) * a.D + 2 * lane);
+        }
+#pragma unroll
+        for (int i = 0; i < 8; i++) {
+            const float ws = __shfl(w, s0 + i < s1 ? s0 + i : s0, 64);
+            x = __builtin_fmaf(v[i].x, ws, x);
+            y = __builtin_fmaf(v[i].y, ws, y);
+        }
+    }
+    lds[wave][lane] = {x, y};
+    __syncthreads();
+    if (wave != 0) return;
+#pragma unroll
+    for (int i = 1; i < kWaves; i++) {
+        x += lds[i][lane].x;
+        y += lds[i][lane].y;
+    }
+    const float inv = total == 0.0f ? 0.0f : 1.0f / total;
+    if (2 * lane < a.D)
+        *reinterpret_cast<uint32_t *>(static_cast<uint16_t *>(a.O) + (q * a.Hq + h) * a.D + 2 * lane) = pack_bf16(x * inv, y * inv);
+    if (a.lse && lane == 0) a.lse[row] = total == 0.0f ? kNone : (top + log2f(total)) * kLn2;
 }
 
 // dq of 128 query rows, and delta = rowsum(dO O) for the keys' pass. Both score-shaped products are transposed as in the
@@ -531,9 +599,32 @@ void pick_dt(int D, F &&f) {
 
 }  // namespace
 
-hipError_t launch_attn_fwd_bf16(const AttnArgs &a, hipStream_t st) {
+// Parts that a forward's keys are split into: where the row tiles leave workgroups idle (two per CU), as many as fill them
+// with 128 keys each at least (by the mean length; lengths are not known on the host), up to a wave's lanes.
+int attn_splits_bf16(int64_t Tq, int64_t Tk, int Hq, int Hkv, int64_t n_seq) {
+    if (n_seq < 1) return 1;
+    const int64_t wgs = (Tq * (Hq / Hkv) / (32 * kWaves) + n_seq) * Hkv;
+    const int64_t most = std::min<int64_t>(64, Tk / n_seq / (2 * kKeys));
+    return (int)std::max<int64_t>(1, std::min(most, 2 * kMfmaConcurrentWgs / wgs));
+}
+
+hipError_t launch_attn_fwd_bf16(const AttnArgs &a, void *ws, hipStream_t st) {
     const int64_t slots = a.Tq * (a.Hq / a.Hkv) / (32 * kWaves) + a.n_seq;
-    pick_dt(a.D, [&](auto dt) { attn_fwd_bf16_kernel<decltype(dt)::value><<<(unsigned)(slots * a.Hkv), kThreads, 0, st>>>(a); });
+    const int splits = attn_splits_bf16(a.Tq, a.Tk, a.Hq, a.Hkv, a.n_seq);
+    const int64_t rows = a.Tq * a.Hq;
+    AttnParts p{};
+    p.m = reinterpret_cast<float *>(static_cast<char *>(ws) + kWsHeader);
+    p.l = p.m + splits * rows;
+    p.o = reinterpret_cast<float *>(static_cast<char *>(ws) + kWsHeader + attn_part_stats(splits, rows));
+    const dim3 grid((unsigned)(slots * a.Hkv), (unsigned)splits);
+    pick_dt(a.D, [&](auto dt) {
+        constexpr int DT = decltype(dt)::value;
+        if (splits > 1) attn_fwd_bf16_kernel<DT, true><<<grid, kThreads, 0, st>>>(a, p);
+        else attn_fwd_bf16_kernel<DT, false><<<grid, kThreads, 0, st>>>(a, p);
+    });
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess || splits == 1) return e;
+    attn_join_kernel<<<(unsigned)rows, kThreads, 0, st>>>(a, p, splits);
     return hipGetLastError();
 }
 

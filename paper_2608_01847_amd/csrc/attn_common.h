@@ -74,7 +74,14 @@ __device__ __forceinline__ void check_ends(const AttnArgs &a) {
 // row of register r in the 32 x 32 accumulator of a lane: 8 (r / 4) + 4 (lane / 32) + r % 4
 __device__ __forceinline__ constexpr int acc_row(int r) { return (r & 3) + 8 * (r >> 2); }
 
-hipError_t launch_attn_fwd_bf16(const AttnArgs &a, hipStream_t st);
+// Partial results of a forward whose keys are split: [splits][Hq][Tq] (x D)
+struct AttnParts {
+    float *m, *l, *o;
+};
+// bytes of m and l, rounded to keep o aligned
+inline size_t attn_part_stats(int splits, int64_t rows) { return ((size_t)splits * (size_t)rows * 8 + 255) / 256 * 256; }
+int attn_splits_bf16(int64_t Tq, int64_t Tk, int Hq, int Hkv, int64_t n_seq);
+hipError_t launch_attn_fwd_bf16(const AttnArgs &a, void *ws, hipStream_t st);
 hipError_t launch_attn_bwd_bf16(const AttnArgs &a, hipStream_t st);
 
 }  // namespace focus

@@ -9,10 +9,10 @@
 // sums of terms of one sign, in place of the difference of lse and sum p z. The difference z - m is taken first, so that
 // the largest logit's d is exactly 0 and logits near the type's lowest value stay finite.
 //
-// The alternatives: logits are ordered by (value, lower index first), as 64-bit keys. A key `tau` that at least `top` keys of
-// the row reach is kept; the few elements that reach it are collected in LDS and ranked at the end (the step that sees
-// more of them than there is room first raises tau). Counts do not depend on the order of the LDS additions, nor does
-// the ranking, keys being distinct.
+// The alternatives: logits are ordered by (value, lower index first), as 64-bit keys. Of the threads' largest logits,
+// which the pass has anyway, follows a value that at least `top` logits of the row reach; the few threads that have such
+// logits have theirs read a second time (from the caches), by all threads, and those that reach it are ranked in LDS. The LDS
+// additions count and hand out places; no result depends on their order, keys being distinct.
 #include "internal.h"
 #include "ops_device.h"
 
@@ -25,7 +25,6 @@ constexpr int kWavesL = kThreads / 64;
 constexpr int kVecs = 4;                        // vectors of 8 logits per thread and step
 constexpr int kStep = kThreads * kVecs * 8;     // logits per step
 constexpr int kRoom = 1024;                     // collected keys
-constexpr int kFull = 512;                      // keys from which the list is cut to `top` after a step
 constexpr int kMaxSplits = 64;
 constexpr int kRowsUnsplit = 512;               // rows from which a row is one workgroup's
 constexpr int64_t kSplitLogits = 4096;          // logits of a part, at least
@@ -44,11 +43,6 @@ __device__ __forceinline__ float value_of(uint32_t o) {
 __device__ __forceinline__ uint64_t key_of(float v, uint32_t index) {
     return ((uint64_t)order_of(v) << 32) | (0xFFFFFFFFu - index);
 }
-__device__ __forceinline__ uint64_t shfl_key(uint64_t k, int mask) {
-    const uint32_t lo = __shfl_xor((uint32_t)k, mask, 64), hi = __shfl_xor((uint32_t)(k >> 32), mask, 64);
-    return ((uint64_t)hi << 32) | lo;
-}
-
 struct Stat {
     float m, s, w;  // the largest logit; s, w relative to it (m = -inf: nothing seen)
 };
@@ -78,139 +72,137 @@ __device__ __forceinline__ Stat wave_merge(Stat v) {
 struct TopLds {
     uint64_t list[kRoom];
     uint64_t cut[kMaxTop];
-    uint64_t group[64];
-    uint64_t wave_best[kWavesL];
-    int count[3];
-    int pos;
+    uint32_t group[64];
+    int hist[256];
+    int flagged[kThreads];
+    int n_flagged, pos;
 };
 
-// The running list of the largest keys of a workgroup's elements. Every member is called by all threads.
-struct TopList {
-    TopLds &l;
-    int top, n = 0, turn = 0;
-    uint64_t tau = 0;  // at least `top` of the keys seen so far reach it (0: all do)
-
-    __device__ __forceinline__ TopList(TopLds &lds, int k) : l(lds), top(k) {
-        if (threadIdx.x == 0) {
-            l.count[0] = l.count[1] = l.count[2] = 0;
-            l.pos = 0;
-        }
-        __syncthreads();
+// Ranks the `top` largest keys of a workgroup's elements, called by all threads: on return l.list holds them, largest
+// first; returns their number (fewer than `top` where there are fewer elements). Thread t's elements are the vectors of eight
+// t, t + kThreads, .. (nvec of them); load(i, k) gives the keys of vector i (0 for elements that do not exist), `best` is the
+// largest order_of among the thread's own (0: none).
+template <typename Load>
+__device__ __forceinline__ int select_top(TopLds &l, int top, uint32_t best, int nvec, Load &&load) {
+    // tau: the top-th of the largest values of 64 groups of threads, which `top` elements reach at least
+    uint32_t group = best;
+#pragma unroll
+    for (int x = 1; x < kThreads / 64; x <<= 1) {
+        const uint32_t o = __shfl_xor(group, x, 64);
+        group = o > group ? o : group;
     }
-
-    // sum of c over the workgroup
-    __device__ __forceinline__ int total(int c) {
-        if (c) atomicAdd(&l.count[turn], c);
-        const int next = turn == 2 ? 0 : turn + 1;
-        if (threadIdx.x == 0) l.count[next] = 0;  // last read before the previous call's barrier
+    if (threadIdx.x % (kThreads / 64) == 0) l.group[threadIdx.x / (kThreads / 64)] = group;
+    if (threadIdx.x == 0) l.n_flagged = l.pos = 0;
+    __syncthreads();
+    const int me = threadIdx.x & 63;
+    const uint32_t g = l.group[me];
+    int rank = 0;
+#pragma unroll 16
+    for (int j = 0; j < 64; j++) {
+        const uint32_t o = __builtin_amdgcn_readlane(g, j);
+        rank += o > g || (o == g && j < me) ? 1 : 0;
+    }
+    const uint32_t kth = __shfl(g, __builtin_ctzll(__ballot(rank == top - 1)), 64);
+    uint64_t tau = (uint64_t)kth << 32;
+    // the few threads that have any, whose vectors are then shared out among all
+    if (best != 0 && best >= kth) l.flagged[atomicAdd(&l.n_flagged, 1)] = threadIdx.x;
+    __syncthreads();
+    const int flagged = l.n_flagged, items = flagged * nvec;
+    auto scan = [&](auto &&f) {
+        for (int i = threadIdx.x; i < items; i += kThreads) {
+            uint64_t k[8];
+            const int j = i / flagged;
+            load(j * kThreads + l.flagged[i - j * flagged], k);
+#pragma unroll
+            for (int e = 0; e < 8; e++)
+                if (k[e] != 0) f(k[e]);
+        }
+    };
+    auto collect = [&]() {
+        scan([&](uint64_t k) {
+            if (k >= tau) {
+                const int at = atomicAdd(&l.pos, 1);
+                if (at < kRoom) l.list[at] = k;
+            }
+        });
         __syncthreads();
-        const int r = l.count[turn];
-        turn = next;
+        const int r = l.pos;
+        __syncthreads();  // before it is cleared
         return r;
-    }
-
-    // Keeps the `top` largest of the list, in order.
-    __device__ __forceinline__ void cut() {
-        __syncthreads();
-        for (int i = threadIdx.x; i < n; i += kThreads) {
-            const uint64_t k = l.list[i];
-            int rank = 0;
-            for (int j = 0; j < n; j++) rank += l.list[j] > k ? 1 : 0;
-            if (rank < top) l.cut[rank] = k;
-        }
-        __syncthreads();
-        const int kept = n < top ? n : top;
-        for (int i = threadIdx.x; i < kept; i += kThreads) l.list[i] = l.cut[i];
-        if (threadIdx.x == 0) l.pos = kept;
-        __syncthreads();
-        n = kept;
-        if (kept == top && l.list[top - 1] > tau) tau = l.list[top - 1];
-    }
-
-    // Takes in a thread's E elements; key(e) is an element's key, 0 for none, best(): the largest order_of among them
-    template <int E, typename Key>
-    __device__ __forceinline__ void add(uint32_t best, Key &&key) {
-        auto reach = [&]() {
-            int c = 0;
-            if (best >= (uint32_t)(tau >> 32)) {
-#pragma unroll
-                for (int e = 0; e < E; e++) {
-                    const uint64_t k = key(e);
-                    c += k >= tau && k != 0 ? 1 : 0;
-                }
-            }
-            return c;
-        };
-        int c = reach(), sum = total(c);
-        if (sum == 0) return;
-        if (n + sum > kRoom && n > top) {
-            cut();
-            c = reach();
-            sum = total(c);
-        }
-        if (n + sum > kRoom) {
-            // Raise tau: of the largest keys of 64 groups of threads, the top-th is reached by `top` keys at least.
-            uint64_t mine = 0;
-#pragma unroll
-            for (int e = 0; e < E; e++) {
-                const uint64_t k = key(e);
-                mine = k > mine ? k : mine;
-            }
-#pragma unroll
-            for (int x = 1; x < kThreads / 64; x <<= 1) {
-                const uint64_t o = shfl_key(mine, x);
-                mine = o > mine ? o : mine;
-            }
-            if (threadIdx.x % (kThreads / 64) == 0) l.group[threadIdx.x / (kThreads / 64)] = mine;
+    };
+    int n = collect();
+    if (n > kRoom) {
+        // Equal values, or few threads that hold most of the largest: tau rises byte by byte to what `top` keys reach, until
+        // the list holds those that do. Keys are distinct, so the last byte ends it.
+        uint64_t prefix = 0;
+        int need = top, shift = 56;  // the need-th largest of the keys that begin with prefix is wanted
+        for (;; shift -= 8) {
+            for (int i = threadIdx.x; i < 256; i += kThreads) l.hist[i] = 0;
+            if (threadIdx.x == 0) l.pos = 0;
             __syncthreads();
-            uint64_t g = l.group[threadIdx.x & 63];
-            int rank = 0;
-            for (int j = 0; j < 64; j++) rank += l.group[j] > g || (l.group[j] == g && j < (int)(threadIdx.x & 63)) ? 1 : 0;
-            const unsigned long long who = __ballot(rank == top - 1);
-            const uint64_t kth = l.group[__builtin_ctzll(who)];
-            if (kth > tau) tau = kth;
-            c = reach();
-            sum = total(c);
+            scan([&](uint64_t k) {
+                if (shift == 56 || (k >> (shift + 8)) == (prefix >> (shift + 8))) atomicAdd(&l.hist[(int)(k >> shift) & 255], 1);
+            });
+            __syncthreads();
+            int bin = 255, above = 0;
+            for (; bin > 0 && above + l.hist[bin] < need; bin--) above += l.hist[bin];
+            const int reach = top - need + above + l.hist[bin];
+            prefix |= (uint64_t)bin << shift;
+            need -= above;
+            __syncthreads();  // before the histogram is cleared again
+            if (reach <= kRoom || shift == 0) break;
         }
-        if (n + sum <= kRoom) {
-            if (c) {
-                int at = atomicAdd(&l.pos, c);
-#pragma unroll
-                for (int e = 0; e < E; e++) {
-                    const uint64_t k = key(e);
-                    if (k >= tau && k != 0) l.list[at++] = k;
-                }
-            }
-            n += sum;
-        } else {
-            // Few threads hold most of the largest keys: take them one by one.
-            uint64_t below = ~(uint64_t)0;
-            for (int i = 0; i < top; i++) {
-                uint64_t mine = 0;
-#pragma unroll
-                for (int e = 0; e < E; e++) {
-                    const uint64_t k = key(e);
-                    mine = k < below && k > mine ? k : mine;
-                }
-#pragma unroll
-                for (int x = 1; x < 64; x <<= 1) {
-                    const uint64_t o = shfl_key(mine, x);
-                    mine = o > mine ? o : mine;
-                }
-                if ((threadIdx.x & 63) == 0) l.wave_best[threadIdx.x >> 6] = mine;
-                __syncthreads();
-                uint64_t b = 0;
-                for (int w = 0; w < kWavesL; w++) b = l.wave_best[w] > b ? l.wave_best[w] : b;
-                __syncthreads();
-                if (b == 0) break;
-                if (threadIdx.x == 0) l.list[n] = b;
-                n++;
-                below = b;
-            }
-            if (threadIdx.x == 0) l.pos = n;
-        }
-        if (n > kFull) cut();
+        tau = prefix;
+        n = collect();
+        n = n < kRoom ? n : kRoom;
     }
+    // ranks among what is left
+    for (int i = threadIdx.x; i < n; i += kThreads) {
+        const uint64_t k = l.list[i];
+        int r = 0;
+#pragma unroll 4
+        for (int j = 0; j < n; j++) r += l.list[j] > k ? 1 : 0;
+        if (r < top) l.cut[r] = k;
+    }
+    __syncthreads();
+    const int kept = n < top ? n : top;
+    if ((int)threadIdx.x < kept) l.list[threadIdx.x] = l.cut[threadIdx.x];
+    __syncthreads();
+    return kept;
+}
+
+// Eight consecutive logits as they lie in memory, missing ones -inf
+template <typename T>
+struct Logits8;
+template <>
+struct Logits8<uint16_t> {
+    u32x4_any_t w;
+    __device__ __forceinline__ void load(const uint16_t *p, int64_t left) {
+        if (left >= 8) {
+            w = *reinterpret_cast<const u32x4_any_t *>(p);
+        } else {
+#pragma unroll
+            for (int e = 0; e < 4; e++)
+                w[e] = (2 * e < left ? p[2 * e] : 0xFF80u) | (uint32_t)(2 * e + 1 < left ? p[2 * e + 1] : 0xFF80u) << 16;
+        }
+    }
+    __device__ __forceinline__ float operator[](int e) const {
+        return __uint_as_float((e & 1) ? w[e >> 1] & 0xFFFF0000u : w[e >> 1] << 16);
+    }
+};
+template <>
+struct Logits8<float> {
+    f32x4_any_t w[2];
+    __device__ __forceinline__ void load(const float *p, int64_t left) {
+        if (left >= 8) {
+            w[0] = reinterpret_cast<const f32x4_any_t *>(p)[0];
+            w[1] = reinterpret_cast<const f32x4_any_t *>(p)[1];
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; e++) w[e >> 2][e & 3] = e < left ? p[e] : -__builtin_inff();
+        }
+    }
+    __device__ __forceinline__ float operator[](int e) const { return w[e >> 2][e & 3]; }
 };
 
 struct LogprobArgs {
@@ -253,23 +245,21 @@ __global__ void __launch_bounds__(kThreads) logprobs_kernel(LogprobArgs a) {
     const int split = (int)(blockIdx.x % (unsigned)a.splits);
     const int64_t v0 = split * a.per, v1 = v0 + a.per < a.V ? v0 + a.per : a.V;
     const T *z = static_cast<const T *>(a.Z) + row * a.V;
-    TopList list(lds_top, TOP ? a.top : 1);
+    const int64_t target = a.target && a.splits == 1 ? a.target[row] : -1;  // under way while the row streams
+    const float zt = target >= 0 && target < a.V ? load_one(z + target) : 0.0f;
     Stat t = {-__builtin_inff(), 0.0f, 0.0f};
     for (int64_t c0 = v0; c0 < v1; c0 += kStep) {
-        float v[kVecs][8];
+        Logits8<T> v[kVecs];
         float top = -__builtin_inff();
 #pragma unroll
         for (int j = 0; j < kVecs; j++) {
             const int64_t c = c0 + (j * kThreads + (int)threadIdx.x) * 8;
-            const int64_t left = v1 - c;
-            const int n = left >= 8 ? 8 : left > 0 ? (int)left : 0;
-            if (n > 0) load8_n(z + c, n, v[j]);
-#pragma unroll
-            for (int e = 0; e < 8; e++) {
-                v[j][e] = e < n ? v[j][e] : -__builtin_inff();
-                top = fmaxf(top, v[j][e]);
-            }
+            v[j].load(z + c, v1 - c);
         }
+#pragma unroll
+        for (int j = 0; j < kVecs; j++)
+#pragma unroll
+            for (int e = 0; e < 8; e++) top = fmaxf(top, v[j][e]);
         const float m = fmaxf(t.m, top), base = m == -__builtin_inff() ? 0.0f : m;
         float s = 0.0f, w = 0.0f;
 #pragma unroll
@@ -291,29 +281,30 @@ __global__ void __launch_bounds__(kThreads) logprobs_kernel(LogprobArgs a) {
                 }
         }
         t = merge(t, Stat{m, s, w});
-        if constexpr (TOP) {
-            list.add<kVecs * 8>(order_of(top), [&](int e) {
-                const int64_t c = c0 + ((e >> 3) * kThreads + (int)threadIdx.x) * 8 + (e & 7);
-                return c < v1 ? key_of(v[e >> 3][e & 7], (uint32_t)c) : (uint64_t)0;
-            });
-        }
     }
+    const uint32_t best = v0 + (int64_t)threadIdx.x * 8 < v1 ? order_of(t.m) : 0u;  // of this thread's own logits
     t = wave_merge(t);
     if ((threadIdx.x & 63) == 0) lds_stat[threadIdx.x >> 6] = t;
     __syncthreads();
     t = lds_stat[0];
 #pragma unroll
     for (int i = 1; i < kWavesL; i++) t = merge(t, lds_stat[i]);
-    if constexpr (TOP) list.cut();
+    int kept = 0;
+    if constexpr (TOP)
+        kept = select_top(lds_top, a.top, best, (int)((v1 - v0 + kThreads * 8 - 1) / (kThreads * 8)), [&](int i, uint64_t (&k)[8]) {
+            const int64_t c = v0 + (int64_t)i * 8;
+            Logits8<T> x;
+            x.load(z + c, v1 - c);
+#pragma unroll
+            for (int e = 0; e < 8; e++) k[e] = c + e < v1 ? key_of(x[e], (uint32_t)(c + e)) : (uint64_t)0;
+        });
     if (a.splits == 1) {
-        const int64_t target = a.target ? a.target[row] : -1;
-        const float zt = target >= 0 && target < a.V ? load_one(z + target) : 0.0f;
-        finish_row(a, row, t, lds_top.list, TOP ? list.n : 0, zt, target);
+        finish_row(a, row, t, lds_top.list, kept, zt, target);
     } else {
         if (threadIdx.x == 0) a.part[blockIdx.x] = t;
         if constexpr (TOP)
             for (int i = threadIdx.x; i < a.top; i += kThreads)
-                a.keys[(int64_t)blockIdx.x * a.top + i] = i < list.n ? lds_top.list[i] : 0;
+                a.keys[(int64_t)blockIdx.x * a.top + i] = i < kept ? lds_top.list[i] : 0;
     }
 }
 
@@ -322,27 +313,27 @@ template <typename T, bool TOP>
 __global__ void __launch_bounds__(kThreads) logprobs_join_kernel(LogprobArgs a) {
     __shared__ TopLds lds_top;
     const int64_t row = blockIdx.x;
-    TopList list(lds_top, TOP ? a.top : 1);
+    int kept = 0;
     Stat t = {-__builtin_inff(), 0.0f, 0.0f};
     if ((int)(threadIdx.x & 63) < a.splits) t = a.part[row * a.splits + (threadIdx.x & 63)];
     t = wave_merge(t);
     if constexpr (TOP) {
-        constexpr int E = kMaxSplits * kMaxTop / kThreads;
-        uint64_t k[E];
-        uint64_t best = 0;
+        static_assert(kMaxSplits * kMaxTop == 8 * kThreads, "eight keys per thread hold every part's");
         const int n = a.splits * a.top;
+        auto load = [&](int i, uint64_t (&k)[8]) {
 #pragma unroll
-        for (int e = 0; e < E; e++) {
-            const int i = e * kThreads + (int)threadIdx.x;
-            k[e] = i < n ? a.keys[row * n + i] : 0;
-            best = k[e] > best ? k[e] : best;
-        }
-        list.add<E>((uint32_t)(best >> 32), [&](int e) { return k[e]; });
-        list.cut();
+            for (int e = 0; e < 8; e++) k[e] = e * kThreads + i < n ? a.keys[row * n + e * kThreads + i] : 0;
+        };
+        uint64_t k[8];
+        uint32_t best = 0;
+        load(threadIdx.x, k);
+#pragma unroll
+        for (int e = 0; e < 8; e++) best = (uint32_t)(k[e] >> 32) > best ? (uint32_t)(k[e] >> 32) : best;
+        kept = select_top(lds_top, a.top, best, 1, load);
     }
     const int64_t target = a.target ? a.target[row] : -1;
     const float zt = target >= 0 && target < a.V ? load_one(static_cast<const T *>(a.Z) + row * a.V + target) : 0.0f;
-    finish_row(a, row, t, lds_top.list, TOP ? list.n : 0, zt, target);
+    finish_row(a, row, t, lds_top.list, kept, zt, target);
 }
 
 constexpr int kBwdThreads = 256;
