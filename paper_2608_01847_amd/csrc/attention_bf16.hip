@@ -8,8 +8,8 @@
 // tile contracts, for lanes 0-31 (32-63), keys 16 t + {0-3, 8-11} (+ 4), the order in which the accumulator holds them;
 // the transposing LDS reads of V follow the same order.
 //
-// Keys and values go through LDS in tiles of 64, two stages each, loaded into registers half a tile's work before they are
-// written. Range-checked buffer loads read rows past a sequence and features past head_dim as zeros.
+// Keys and values go through LDS in tiles of 64, two stages each, by direct-to-LDS loads a tile ahead, whose range check reads
+// rows past a sequence and features past head_dim as zeros.
 #include "attn_common.h"
 
 namespace focus {
@@ -28,59 +28,89 @@ constexpr int kThreads = 64 * kWaves;
 constexpr int kKeys = 64;   // rows of a staged tile
 constexpr float kNone = -__builtin_inff();
 
-// Geometry of a staged tile of 64 rows: DT x 32 features, a row of 128 (DT <= 2) or 256 bytes. 16-byte chunk c of row r
+// Geometry of a staged tile of ROWS rows: DT x 32 features, a row of 128 (DT <= 2) or 256 bytes. 16-byte chunk c of row r
 // lies at chunk c ^ key(r): 8 consecutive rows of one chunk (a fragment read), and 4 rows of two neighbouring chunks (half a
 // transposing read), then lie in different banks.
-template <int DT>
+template <int DT, int ROWS = kKeys>
 struct Tile {
     static constexpr int kChunks = DT <= 2 ? 8 : 16;
     static constexpr int kPitch = kChunks * 16;
-    static constexpr int kBytes = kKeys * kPitch;
-    static constexpr int kLoads = kKeys * kChunks / kThreads;  // 16-byte loads per thread
-    static constexpr int kRowStep = kThreads / kChunks;        // rows between a thread's loads
-    __device__ static __forceinline__ uint32_t key(uint32_t r) {
+    static constexpr int kBytes = ROWS * kPitch;
+    static constexpr int kLoads = ROWS * kChunks / kThreads;  // 16-byte loads per thread
+    // linear in the bits of r (exclusive or), and of its low four alone
+    __host__ __device__ static constexpr uint32_t key(uint32_t r) {
         if constexpr (kChunks == 16) return ((r & 7u) << 1) | ((r >> 3) & 1u);
         return (((r >> 1) & 3u) << 1) | ((r >> 3) & 1u);
     }
 };
 
-// A thread's part of the tiles of one operand
-template <int DT>
-struct Stager {
-    using G = Tile<DT>;
-    uint32_t off[G::kLoads];  // byte offsets in a tile of the tensor, bit 31 set past head_dim
-    uint32_t lds;
-    u32x4_t v[G::kLoads];
-    __device__ __forceinline__ void init(int64_t stride, int D) {
-        const uint32_t c = threadIdx.x % G::kChunks, r = threadIdx.x / G::kChunks;
-        const uint32_t past = (int)c * 8 < D ? 0u : 0x80000000u;
-#pragma unroll
-        for (int i = 0; i < G::kLoads; i++) off[i] = ((r + i * G::kRowStep) * (uint32_t)(stride * 2) + c * 16u) | past;
-        lds = r * G::kPitch + ((c ^ G::key(r)) << 4);
+__device__ __forceinline__ uint32_t lds_addr(const char *p) {
+    return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) char *)p;
+}
+
+__device__ __forceinline__ uint32_t scalar(uint32_t x) { return __builtin_amdgcn_readfirstlane(x); }
+
+// Direct-to-LDS loads of one operand's tiles: lane L of a wave's instruction i writes 16 bytes at 16 L from the
+// instruction's place, 1 KB of whole rows, and so reads the chunk of its row that belongs there.
+//
+// The instructions are written out: to the compiler's builtin every LDS read may alias the loads under way, and it would
+// wait for all of them before the first fragment of the tile at hand. They have no result in registers, and `landed` waits
+// for them before the barrier that hands the tile over. A scalar register that holds part of the descriptor may have been
+// written by a vector instruction just before, and M0 by a scalar one: the waits the hardware asks for stand in the block.
+template <int DT, int ROWS = kKeys>
+struct Dma {
+    using G = Tile<DT, ROWS>;
+    static constexpr uint32_t kRowsEach = 1024 / G::kPitch;
+    uint32_t row, chunk;  // byte offsets of this lane's row and chunk of the first load
+    __device__ __forceinline__ void init(int64_t stride, int wave, int lane) {
+        const uint32_t r = (uint32_t)wave * (G::kLoads * kRowsEach) + (uint32_t)lane / G::kChunks;
+        row = r * (uint32_t)(stride * 2);
+        chunk = (((uint32_t)lane % G::kChunks) ^ G::key(r)) << 4;
     }
-    // rows `row` .. of a sequence of n rows that starts at base
-    __device__ __forceinline__ void load(const uint16_t *base, int64_t stride, int row, int n, int D) {
-        const int left = n - row < kKeys ? n - row : kKeys;
-        const __amdgpu_buffer_rsrc_t rs = make_rsrc(base + row * stride, left > 0 ? ((left - 1) * stride + D) * 2 : 0);
-#pragma unroll
-        for (int i = 0; i < G::kLoads; i++) v[i] = __builtin_amdgcn_raw_buffer_load_b128(rs, (int)off[i], 0, 0);
+    // (the key's linearity needs rows that differ by whole kRowsEach to differ in bits that a lane's row does not use)
+    static_assert(G::kLoads * kRowsEach >= 8 && (kRowsEach & (kRowsEach - 1)) == 0, "rows of a wave's loads");
+    // offset of load i: past head_dim with bit 31 set (read as zeros)
+    __device__ __forceinline__ uint32_t off(uint32_t i, int64_t stride, int D) const {
+        const uint32_t c = chunk ^ (G::key(i * kRowsEach) << 4);
+        return (row + i * kRowsEach * (uint32_t)(stride * 2) + c) | ((int)c < 2 * D ? 0u : 0x80000000u);
     }
-    __device__ __forceinline__ void store(char *tile) const {
-#pragma unroll
-        for (int i = 0; i < G::kLoads; i++)
-            *(lds_u32x4 *)(uintptr_t)(lds_addr(tile) + lds + i * (G::kRowStep * G::kPitch)) = v[i];
-    }
-    __device__ static __forceinline__ uint32_t lds_addr(const char *p) {
-        return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) char *)p;
+    // rows `row` .. of a sequence of n rows that starts at base, into the tile at LDS address `tile`
+    __device__ __forceinline__ void load(const uint16_t *base, int64_t stride, int row, int n, int D, uint32_t tile, int wave) const {
+        const int left = n - row < ROWS ? n - row : ROWS;
+        const uint64_t p = (uint64_t)(base + row * stride);
+        const u32x4_t rs = {scalar((uint32_t)p), scalar((uint32_t)(p >> 32) & 0xFFFFu),
+                            scalar(left > 0 ? (uint32_t)(((left - 1) * stride + D) * 2) : 0u), (uint32_t)kRsrcWord3};
+        const uint32_t at = scalar(tile + (uint32_t)wave * (G::kLoads * 1024u));
+        if constexpr (G::kLoads == 4) {
+            asm volatile(
+                "s_nop 4\n\ts_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %5, 0 offen lds\n\t"
+                "s_add_u32 m0, %0, 0x400\n\ts_nop 0\n\tbuffer_load_dwordx4 %2, %5, 0 offen lds\n\t"
+                "s_add_u32 m0, %0, 0x800\n\ts_nop 0\n\tbuffer_load_dwordx4 %3, %5, 0 offen lds\n\t"
+                "s_add_u32 m0, %0, 0xc00\n\ts_nop 0\n\tbuffer_load_dwordx4 %4, %5, 0 offen lds"
+                :
+                : "s"(at), "v"(off(0, stride, D)), "v"(off(1, stride, D)), "v"(off(2, stride, D)), "v"(off(3, stride, D)), "s"(rs)
+                : "memory", "scc");
+        } else {
+            static_assert(G::kLoads == 2, "two or four loads per wave");
+            asm volatile(
+                "s_nop 4\n\ts_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %3, 0 offen lds\n\t"
+                "s_add_u32 m0, %0, 0x400\n\ts_nop 0\n\tbuffer_load_dwordx4 %2, %3, 0 offen lds"
+                :
+                : "s"(at), "v"(off(0, stride, D)), "v"(off(1, stride, D)), "s"(rs)
+                : "memory", "scc");
+        }
     }
 };
+
+// Every load of this wave has landed and every LDS read of it is done; then the same holds for the workgroup.
+__device__ __forceinline__ void landed() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 
 // A lane's LDS offsets of the fragments of a tile
 template <int DT>
 struct Frags {
     using G = Tile<DT>;
-    uint32_t row;       // straight reads: row lane % 32, chunk lane / 32; chunk 2 s + that of step s at ^ 32 s
-    uint32_t tr[2][DT];  // transposing reads: rows 8 e + 4 (lane / 32) .. + 3, features 32 t + 16 (lane / 16 % 2) .. + 15
+    uint32_t row;    // straight reads: row lane % 32, chunk lane / 32; chunk 2 s + that of step s at ^ 32 s
+    uint32_t tr[2];  // transposing reads: rows 8 e + 4 (lane / 32) .. + 3, features 16 (lane / 16 % 2) .. + 15; 32 t more at ^ 64 t
     __device__ __forceinline__ void init(int lane) {
         const uint32_t r = lane & 31, h = lane >> 5;
         row = r * G::kPitch + ((h ^ G::key(r)) << 4);
@@ -88,11 +118,12 @@ struct Frags {
 #pragma unroll
         for (uint32_t e = 0; e < 2; e++) {
             const uint32_t tr_row = 8 * e + 4 * h + j / 4;
-#pragma unroll
-            for (uint32_t t = 0; t < DT; t++)
-                tr[e][t] = tr_row * G::kPitch + (((4 * t + 2 * g + (j % 4) / 2) ^ G::key(tr_row)) << 4) + 8 * (j % 2);
+            tr[e] = tr_row * G::kPitch + (((2 * g + (j % 4) / 2) ^ G::key(tr_row)) << 4) + 8 * (j % 2);
         }
     }
+    // Keeps the compiler from holding every step's address in a register of its own over a loop: one operation forms
+    // each, and the registers are short.
+    __device__ __forceinline__ void hold() { asm volatile("" : "+v"(row), "+v"(tr[0]), "+v"(tr[1])); }
     // A operand: 32 rows from row 32 b on, features 16 s .. 16 s + 15
     __device__ __forceinline__ bf16x8_t straight(uint32_t tile, int b, int s) const {
         return *(lds_bf16x8 *)(uintptr_t)((row ^ (uint32_t)(32 * s)) + tile + b * 32 * G::kPitch);
@@ -100,8 +131,8 @@ struct Frags {
     // A operand: features 32 t .. 32 t + 31, the 16 rows from 16 s on in accumulator order
     __device__ __forceinline__ bf16x8_t transposed(uint32_t tile, int s, int t) const {
         const i16x4_t v[2] = {
-            __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4 *)(uintptr_t)(tr[0][t] + tile + s * 16 * G::kPitch)),
-            __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4 *)(uintptr_t)(tr[1][t] + tile + s * 16 * G::kPitch))};
+            __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4 *)(uintptr_t)((tr[0] ^ (uint32_t)(64 * t)) + tile + s * 16 * G::kPitch)),
+            __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4 *)(uintptr_t)((tr[1] ^ (uint32_t)(64 * t)) + tile + s * 16 * G::kPitch))};
         return __builtin_bit_cast(bf16x8_t, v);
     }
 };
@@ -224,27 +255,28 @@ __global__ void __launch_bounds__(kThreads, 2) attn_fwd_bf16_kernel(AttnArgs a, 
 
     const uint16_t *K = static_cast<const uint16_t *>(a.k) + r.k0 * a.k_stride + (int64_t)hk * D;
     const uint16_t *V = static_cast<const uint16_t *>(a.v) + r.k0 * a.v_stride + (int64_t)hk * D;
-    Stager<DT> ks, vs;
-    ks.init(a.k_stride, D);
-    vs.init(a.v_stride, D);
+    Dma<DT> ks, vs;
+    ks.init(a.k_stride, wave, lane);
+    vs.init(a.v_stride, wave, lane);
     Frags<DT> f;
     f.init(lane);
-    const uint32_t base = Stager<DT>::lds_addr(smem);
+    const uint32_t base = lds_addr(smem);
 
     f32x16_t o[DT] = {};
     float m = kNone, l = 0.0f;
     if (j0 < nk) {
-        ks.load(K, a.k_stride, j0 * kKeys, r.lk, D);
-        vs.load(V, a.v_stride, j0 * kKeys, r.lk, D);
-        ks.store(smem);
-        vs.store(smem + 2 * G::kBytes);
+        ks.load(K, a.k_stride, j0 * kKeys, r.lk, D, base, wave);
+        vs.load(V, a.v_stride, j0 * kKeys, r.lk, D, base + 2 * G::kBytes, wave);
     }
-    __syncthreads();
+    landed();
     for (int j = j0; j < nk; j++) {
         const int st = (j - j0) & 1, k0 = j * kKeys;
         const uint32_t kt = base + st * G::kBytes, vt = base + (2 + st) * G::kBytes;
         const bool more = j + 1 < nk, active = k0 <= any_seen;
-        if (more) ks.load(K, a.k_stride, k0 + kKeys, r.lk, D);
+        if (more) {
+            ks.load(K, a.k_stride, k0 + kKeys, r.lk, D, base + (st ^ 1) * G::kBytes, wave);
+            vs.load(V, a.v_stride, k0 + kKeys, r.lk, D, base + (2 + (st ^ 1)) * G::kBytes, wave);
+        }
         bf16x8_t p[4];
         if (active) {
             f32x16_t sc[2] = {};
@@ -290,18 +322,13 @@ __global__ void __launch_bounds__(kThreads, 2) attn_fwd_bf16_kernel(AttnArgs a, 
 #pragma unroll
             for (int i = 0; i < 4; i++) p[i] = pack8(sc[i >> 1], i & 1);
         }
-        if (more) {
-            ks.store(smem + (st ^ 1) * G::kBytes);
-            vs.load(V, a.v_stride, k0 + kKeys, r.lk, D);
-        }
         if (active) {
 #pragma unroll
             for (int i = 0; i < 4; i++)
 #pragma unroll
                 for (int t = 0; t < DT; t++) o[t] = mfma(f.transposed(vt, i, t), p[i], o[t]);
         }
-        if (more) vs.store(smem + (2 + (st ^ 1)) * G::kBytes);
-        __syncthreads();
+        landed();
     }
     l = sum_halves(l);
     if constexpr (SPLIT) {
@@ -409,25 +436,26 @@ __global__ void __launch_bounds__(kThreads, 2) attn_bwd_q_bf16_kernel(AttnArgs a
 
     const uint16_t *K = static_cast<const uint16_t *>(a.k) + r.k0 * a.k_stride + (int64_t)hk * D;
     const uint16_t *V = static_cast<const uint16_t *>(a.v) + r.k0 * a.v_stride + (int64_t)hk * D;
-    Stager<DT> ks, vs;
-    ks.init(a.k_stride, D);
-    vs.init(a.v_stride, D);
+    Dma<DT> ks, vs;
+    ks.init(a.k_stride, wave, lane);
+    vs.init(a.v_stride, wave, lane);
     Frags<DT> f;
     f.init(lane);
-    const uint32_t base = Stager<DT>::lds_addr(smem);
+    const uint32_t base = lds_addr(smem);
     f32x16_t dq[DT] = {};
     if (w.nk > 0) {
-        ks.load(K, a.k_stride, 0, r.lk, D);
-        vs.load(V, a.v_stride, 0, r.lk, D);
-        ks.store(smem);
-        vs.store(smem + 2 * G::kBytes);
+        ks.load(K, a.k_stride, 0, r.lk, D, base, wave);
+        vs.load(V, a.v_stride, 0, r.lk, D, base + 2 * G::kBytes, wave);
     }
-    __syncthreads();
+    landed();
     for (int j = 0; j < w.nk; j++) {
         const int st = j & 1, k0 = j * kKeys;
         const uint32_t kt = base + st * G::kBytes, vt = base + (2 + st) * G::kBytes;
         const bool more = j + 1 < w.nk, active = k0 <= w.any_seen;
-        if (more) ks.load(K, a.k_stride, k0 + kKeys, r.lk, D);
+        if (more) {
+            ks.load(K, a.k_stride, k0 + kKeys, r.lk, D, base + (st ^ 1) * G::kBytes, wave);
+            vs.load(V, a.v_stride, k0 + kKeys, r.lk, D, base + (2 + (st ^ 1)) * G::kBytes, wave);
+        }
         auto block = [&](int b) {
             f32x16_t sc = {}, dp = {};
 #pragma unroll
@@ -449,28 +477,30 @@ __global__ void __launch_bounds__(kThreads, 2) attn_bwd_q_bf16_kernel(AttnArgs a
                 for (int t = 0; t < DT; t++) dq[t] = mfma(f.transposed(kt, 2 * b + i, t), ds, dq[t]);
             }
         };
-        if (active) block(0);
-        if (more) {
-            ks.store(smem + (st ^ 1) * G::kBytes);
-            vs.load(V, a.v_stride, k0 + kKeys, r.lk, D);
+        if (active) {
+            block(0);
+            block(1);
         }
-        if (active) block(1);
-        if (more) vs.store(smem + (2 + (st ^ 1)) * G::kBytes);
-        __syncthreads();
+        landed();
     }
     store_row<DT>(static_cast<uint16_t *>(a.dq) + (r.q0 + w.q) * a.dq_stride + (int64_t)w.h * D, w.ok, D, half, dq, a.scale);
 }
 
 // dk and dv of 128 keys of one key-value head, 32 per wave, over the queries of every head that shares it, head by head.
 // Here a lane's column is a key and the queries run down the accumulators (S = q k^T as it is written): P and dS are the
-// B operands of dv^T = dO^T P and dk^T = q^T dS. Queries and their gradients go through LDS in tiles of 64 with their lse
-// and delta; a query that does not exist, or sees nothing, has lse = +inf there and so probability 0.
+// B operands of dv^T = dO^T P and dk^T = q^T dS. Queries and their gradients go through LDS in tiles with their lse and delta;
+// a query that does not exist, or sees nothing, has lse = +inf there and so probability 0.
+// Two waves per SIMD, whose 256 registers hold the sums (64 per gradient and 128 features) and k: from 65 features on, v is read
+// from LDS each time and the tiles have 32 queries rather than 64.
 template <int DT>
-__global__ void __launch_bounds__(kThreads, 1) attn_bwd_kv_bf16_kernel(AttnArgs a) {
-    using G = Tile<DT>;
-    __shared__ __attribute__((aligned(16))) char smem[4 * G::kBytes];  // q, q, dO, dO
-    __shared__ __attribute__((aligned(16))) float stats[2][2][kKeys];  // [stage][lse log2 e, delta]
+__global__ void __launch_bounds__(kThreads, 2) attn_bwd_kv_bf16_kernel(AttnArgs a) {
+    constexpr bool kWide = DT > 2;
+    constexpr int kQ = kWide ? 32 : 64;  // queries of a tile
+    using G = Tile<DT, kQ>;
+    using GV = Tile<DT>;  // half of the workgroup's 128 keys
     constexpr int kRows = 32 * kWaves;
+    __shared__ __attribute__((aligned(16))) char smem[4 * G::kBytes + (kWide ? 2 * GV::kBytes : 0)];  // q, q, dO, dO, v
+    __shared__ __attribute__((aligned(16))) float stats[2][2][kQ];  // [stage][lse log2 e, delta]
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5, col = lane & 31;
     const int hk = blockIdx.x % a.Hkv, group = a.Hq / a.Hkv, D = a.D;
     int tile;
@@ -484,29 +514,27 @@ __global__ void __launch_bounds__(kThreads, 1) attn_bwd_kv_bf16_kernel(AttnArgs 
     // the first query that sees a key: of the workgroup's tile (where the loop starts), of the wave's first and last
     // key, of this lane's
     auto seen_from = [&](int key) { return a.causal && key > shift ? key - shift : 0; };
-    const int q_first = seen_from(tile * kRows) / kKeys * kKeys;
+    const int q_first = seen_from(tile * kRows) / kQ * kQ;
     const int any_from = seen_from(w_first), all_from = seen_from(w_first + 31), from = seen_from(k);
-    const int per_head = r.lq > q_first ? (r.lq - q_first + kKeys - 1) / kKeys : 0;
+    const int per_head = r.lq > q_first ? (r.lq - q_first + kQ - 1) / kQ : 0;
     const int items = per_head * group;
 
-    bf16x8_t kv[2 * DT], vv[2 * DT];
-    load_row<DT>(static_cast<const uint16_t *>(a.k) + (r.k0 + k) * a.k_stride + (int64_t)hk * D, ok, D, half, kv);
-    load_row<DT>(static_cast<const uint16_t *>(a.v) + (r.k0 + k) * a.v_stride + (int64_t)hk * D, ok, D, half, vv);
     const float c = a.scale * kLog2e;
     const int64_t g_stride = (int64_t)a.Hq * D;
     const uint16_t *Q = static_cast<const uint16_t *>(a.q) + r.q0 * a.q_stride + (int64_t)hk * group * D;
     const uint16_t *dO = static_cast<const uint16_t *>(a.dO) + r.q0 * g_stride + (int64_t)hk * group * D;
+    const uint16_t *V = static_cast<const uint16_t *>(a.v) + r.k0 * a.v_stride + (int64_t)hk * D;
     const int64_t stat = (int64_t)hk * group * a.Tq + r.q0;
-    Stager<DT> qs, gs;
-    qs.init(a.q_stride, D);
-    gs.init(g_stride, D);
+    Dma<DT, kQ> qs, gs;
+    qs.init(a.q_stride, wave, lane);
+    gs.init(g_stride, wave, lane);
     Frags<DT> f;
     f.init(lane);
-    const uint32_t base = Stager<DT>::lds_addr(smem);
+    const uint32_t base = lds_addr(smem), vt = base + 4 * G::kBytes;
     float sv = 0.0f;
     auto load_stats = [&](int head, int q0) {
-        if (threadIdx.x < 2 * kKeys) {
-            const int row = q0 + (threadIdx.x & (kKeys - 1)), which = threadIdx.x / kKeys;
+        if (threadIdx.x < 2 * kQ) {
+            const int row = q0 + (threadIdx.x & (kQ - 1)), which = threadIdx.x / kQ;
             const int64_t at = stat + (int64_t)head * a.Tq + row;
             sv = which == 0 ? __builtin_inff() : 0.0f;
             if (row < r.lq) sv = which == 0 ? a.lse[at] * kLog2e : a.delta[at];
@@ -514,41 +542,52 @@ __global__ void __launch_bounds__(kThreads, 1) attn_bwd_kv_bf16_kernel(AttnArgs 
         }
     };
     auto store_stats = [&](int stage) {
-        if (threadIdx.x < 2 * kKeys) (&stats[stage][0][0])[threadIdx.x] = sv;
+        if (threadIdx.x < 2 * kQ) (&stats[stage][0][0])[threadIdx.x] = sv;
     };
+    bf16x8_t kv[2 * DT], vv[kWide ? 1 : 2 * DT];
+    load_row<DT>(static_cast<const uint16_t *>(a.k) + (r.k0 + k) * a.k_stride + (int64_t)hk * D, ok, D, half, kv);
+    if constexpr (!kWide) load_row<DT>(V + k * a.v_stride, ok, D, half, vv);
     f32x16_t dk[DT] = {}, dv[DT] = {};
     if (items > 0) {
-        qs.load(Q, a.q_stride, q_first, r.lq, D);
-        gs.load(dO, g_stride, q_first, r.lq, D);
         load_stats(0, q_first);
-        qs.store(smem);
-        gs.store(smem + 2 * G::kBytes);
+        qs.load(Q, a.q_stride, q_first, r.lq, D, base, wave);
+        gs.load(dO, g_stride, q_first, r.lq, D, base + 2 * G::kBytes, wave);
+        if constexpr (kWide) {
+            Dma<DT> vs;
+            vs.init(a.v_stride, wave, lane);
+            vs.load(V, a.v_stride, tile * kRows, r.lk, D, vt, wave);
+            vs.load(V, a.v_stride, tile * kRows + kKeys, r.lk, D, vt + GV::kBytes, wave);
+        }
         store_stats(0);
     }
-    __syncthreads();
+    landed();
     int head = 0, q0 = q_first;
     for (int it = 0; it < items; it++) {
         const int st = it & 1;
         const uint32_t qt = base + st * G::kBytes, gt = base + (2 + st) * G::kBytes;
-        const bool more = it + 1 < items, active = q0 + kKeys > any_from;
-        int next_head = head, next_q0 = q0 + kKeys;
+        const bool more = it + 1 < items, active = q0 + kQ > any_from;
+        int next_head = head, next_q0 = q0 + kQ;
         if (next_q0 >= r.lq) {
             next_head++;
             next_q0 = q_first;
         }
         if (more) {
-            qs.load(Q + (int64_t)next_head * D, a.q_stride, next_q0, r.lq, D);
-            gs.load(dO + (int64_t)next_head * D, g_stride, next_q0, r.lq, D);
             load_stats(next_head, next_q0);
+            qs.load(Q + (int64_t)next_head * D, a.q_stride, next_q0, r.lq, D, base + (st ^ 1) * G::kBytes, wave);
+            gs.load(dO + (int64_t)next_head * D, g_stride, next_q0, r.lq, D, base + (2 + (st ^ 1)) * G::kBytes, wave);
         }
         if (active) {
 #pragma unroll
-            for (int b = 0; b < 2; b++) {
+            for (int b = 0; b < kQ / 32; b++) {
+                f.hold();
                 f32x16_t sc = {}, dp = {};
 #pragma unroll
                 for (int i = 0; i < 2 * DT; i++) sc = mfma(f.straight(qt, b, i), kv[i], sc);
 #pragma unroll
-                for (int i = 0; i < 2 * DT; i++) dp = mfma(f.straight(gt, b, i), vv[i], dp);
+                for (int i = 0; i < 2 * DT; i++) {
+                    if constexpr (kWide) dp = mfma(f.straight(gt, b, i), f.straight(vt, wave, i), dp);
+                    else dp = mfma(f.straight(gt, b, i), vv[i], dp);
+                }
 #pragma unroll
                 for (int g = 0; g < 4; g++) {
                     const f32x4_any_t ls = *reinterpret_cast<const f32x4_any_t *>(&stats[st][0][32 * b + 8 * g + 4 * half]);
@@ -577,14 +616,10 @@ __global__ void __launch_bounds__(kThreads, 1) attn_bwd_kv_bf16_kernel(AttnArgs 
                 }
             }
         }
-        if (more) {
-            qs.store(smem + (st ^ 1) * G::kBytes);
-            gs.store(smem + (2 + (st ^ 1)) * G::kBytes);
-            store_stats(st ^ 1);
-        }
+        if (more) store_stats(st ^ 1);
         head = next_head;
         q0 = next_q0;
-        __syncthreads();
+        landed();
     }
     store_row<DT>(static_cast<uint16_t *>(a.dk) + (r.k0 + k) * a.dk_stride + (int64_t)hk * D, ok, D, half, dk, a.scale);
     store_row<DT>(static_cast<uint16_t *>(a.dv) + (r.k0 + k) * a.dv_stride + (int64_t)hk * D, ok, D, half, dv, 1.0f);

@@ -63,8 +63,9 @@ __device__ __forceinline__ void load8_n(const float *p, int n, float (&v)[8]) {
     }
 }
 
+template <bool TAIL = true>
 __device__ __forceinline__ void store8_n(uint16_t *p, int n, const float (&v)[8]) {
-    if (n >= 8) {
+    if (!TAIL || n >= 8) {
         u32x4_any_t w;
 #pragma unroll
         for (int e = 0; e < 4; e++) w[e] = pack_bf16(v[2 * e], v[2 * e + 1]);
@@ -76,8 +77,9 @@ __device__ __forceinline__ void store8_n(uint16_t *p, int n, const float (&v)[8]
     }
 }
 
+template <bool TAIL = true>
 __device__ __forceinline__ void store8_n(float *p, int n, const float (&v)[8]) {
-    if (n >= 8) {
+    if (!TAIL || n >= 8) {
         reinterpret_cast<f32x4_any_t *>(p)[0] = f32x4_any_t{v[0], v[1], v[2], v[3]};
         reinterpret_cast<f32x4_any_t *>(p)[1] = f32x4_any_t{v[4], v[5], v[6], v[7]};
     } else {
@@ -86,6 +88,50 @@ __device__ __forceinline__ void store8_n(float *p, int n, const float (&v)[8]) {
             if (e < n) p[e] = v[e];
     }
 }
+
+// Eight consecutive elements as they lie in memory (bf16: four registers), the missing ones zeros
+template <typename T>
+struct Raw8;
+template <>
+struct Raw8<uint16_t> {
+    u32x4_any_t w;
+    __device__ __forceinline__ void load(const uint16_t *p, int n) {
+        if (n >= 8) {
+            w = *reinterpret_cast<const u32x4_any_t *>(p);
+        } else {
+#pragma unroll
+            for (int e = 0; e < 4; e++) w[e] = (2 * e < n ? p[2 * e] : 0u) | (uint32_t)(2 * e + 1 < n ? p[2 * e + 1] : 0u) << 16;
+        }
+    }
+    __device__ __forceinline__ float operator[](int e) const {
+        return __uint_as_float((e & 1) ? w[e >> 1] & 0xFFFF0000u : w[e >> 1] << 16);
+    }
+    // the eight from element c on of a row of n (a multiple of 8) behind rs, zeros past its end: no branch
+    __device__ __forceinline__ void load_row(__amdgpu_buffer_rsrc_t rs, int c) {
+        w = __builtin_amdgcn_raw_buffer_load_b128(rs, c * 2, 0, 0);
+    }
+    // keeps the compiler from holding the unpacked values over this point in place of the packed ones
+    __device__ __forceinline__ void keep_packed() { asm volatile("" : "+v"(w)); }
+};
+template <>
+struct Raw8<float> {
+    f32x4_any_t w[2];
+    __device__ __forceinline__ void load(const float *p, int n) {
+        if (n >= 8) {
+            w[0] = reinterpret_cast<const f32x4_any_t *>(p)[0];
+            w[1] = reinterpret_cast<const f32x4_any_t *>(p)[1];
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; e++) w[e >> 2][e & 3] = e < n ? p[e] : 0.0f;
+        }
+    }
+    __device__ __forceinline__ void load_row(__amdgpu_buffer_rsrc_t rs, int c) {
+        w[0] = __builtin_bit_cast(f32x4_any_t, __builtin_amdgcn_raw_buffer_load_b128(rs, c * 4, 0, 0));
+        w[1] = __builtin_bit_cast(f32x4_any_t, __builtin_amdgcn_raw_buffer_load_b128(rs, c * 4 + 16, 0, 0));
+    }
+    __device__ __forceinline__ float operator[](int e) const { return w[e >> 2][e & 3]; }
+    __device__ __forceinline__ void keep_packed() {}
+};
 
 // 8 consecutive parameters from element c on, of either type
 __device__ __forceinline__ void load8_param(const void *base, int dtype, int c, int n, float (&v)[8]) {
