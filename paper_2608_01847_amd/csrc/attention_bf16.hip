@@ -151,6 +151,21 @@ __device__ __forceinline__ float sum_halves(float x) {
     return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
 
+// N groups of matrix instructions, each on up to four fragments that are read from LDS while the group before runs: two
+// sets of registers in turn. Left to itself the compiler reads each fragment just before its use, into the same few
+// registers, and every pair of instructions waits out the LDS latency.
+template <int N, typename Load, typename Run>
+__device__ __forceinline__ void pipelined(Load &&load, Run &&run) {
+    bf16x8_t x[2][4];
+    load(std::integral_constant<int, 0>{}, x[0]);
+    static_for<N>([&](auto g) {
+        if constexpr (g + 1 < N) load(std::integral_constant<int, g + 1>{}, x[(g + 1) & 1]);
+        __builtin_amdgcn_sched_barrier(0);
+        run(g, x[g & 1]);
+        __builtin_amdgcn_sched_barrier(0);
+    });
+}
+
 // 8 accumulator registers from 8 s on as a B operand
 __device__ __forceinline__ bf16x8_t pack8(const f32x16_t &p, int s) {
     uint32_t w[4];
@@ -277,56 +292,68 @@ __global__ void __launch_bounds__(kThreads, 2) attn_fwd_bf16_kernel(AttnArgs a, 
             ks.load(K, a.k_stride, k0 + kKeys, r.lk, D, base + (st ^ 1) * G::kBytes, wave);
             vs.load(V, a.v_stride, k0 + kKeys, r.lk, D, base + (2 + (st ^ 1)) * G::kBytes, wave);
         }
-        bf16x8_t p[4];
         if (active) {
             f32x16_t sc[2] = {};
+            bf16x8_t p[4];
+            // DT groups of scores (two steps of 16 features, both halves of the tile), then four of the output
+            pipelined<DT + 4>(
+                [&](auto g, bf16x8_t (&x)[4]) {
+                    if constexpr (g < DT) {
 #pragma unroll
-            for (int i = 0; i < 2 * DT; i++)
+                        for (int i = 0; i < 4; i++) x[i] = f.straight(kt, i & 1, 2 * g + (i >> 1));
+                    } else {
 #pragma unroll
-                for (int b = 0; b < 2; b++) sc[b] = mfma(f.straight(kt, b, i), qv[i], sc[b]);
-            if (k0 + kKeys - 1 > all_seen) {
+                        for (int t = 0; t < DT; t++) x[t] = f.transposed(vt, g - DT, t);
+                    }
+                },
+                [&](auto g, bf16x8_t (&x)[4]) {
+                    if constexpr (g < DT) {
 #pragma unroll
-                for (int b = 0; b < 2; b++)
+                        for (int i = 0; i < 4; i++) sc[i & 1] = mfma(x[i], qv[2 * g + (i >> 1)], sc[i & 1]);
+                    } else {
 #pragma unroll
-                    for (int i = 0; i < 16; i++)
-                        if (k0 + 32 * b + acc_row(i) + 4 * half > seen) sc[b][i] = kNone;
-            }
-            float top = sc[0][0];
+                        for (int t = 0; t < DT; t++) o[t] = mfma(x[t], p[g - DT], o[t]);
+                    }
+                    if constexpr (g == DT - 1) {
+                        if (k0 + kKeys - 1 > all_seen) {
 #pragma unroll
-            for (int b = 0; b < 2; b++)
+                            for (int b = 0; b < 2; b++)
 #pragma unroll
-                for (int i = 0; i < 16; i++) top = fmaxf(top, sc[b][i]);
-            top = max_halves(top) * c;
-            // The reference that the exponents are taken from follows the maximum only where it is passed by more than
-            // 8: probabilities stay below 2^8, and most tiles need no rescaling.
-            if (__any(top > m + 8.0f)) {
-                const float now = fmaxf(m, top);
-                const float alpha = now == kNone ? 1.0f : exp2_raw(m - now);
-                m = now;
-                l *= alpha;
+                                for (int i = 0; i < 16; i++)
+                                    if (k0 + 32 * b + acc_row(i) + 4 * half > seen) sc[b][i] = kNone;
+                        }
+                        float top = sc[0][0];
 #pragma unroll
-                for (int t = 0; t < DT; t++)
+                        for (int b = 0; b < 2; b++)
 #pragma unroll
-                    for (int i = 0; i < 16; i++) o[t][i] *= alpha;
-            }
-            const float from = m == kNone ? 0.0f : m;
-            float sum = 0.0f;
+                            for (int i = 0; i < 16; i++) top = fmaxf(top, sc[b][i]);
+                        top = max_halves(top) * c;
+                        // The reference that the exponents are taken from follows the maximum only where it is passed by
+                        // more than 8: probabilities stay below 2^8, and most tiles need no rescaling.
+                        if (__any(top > m + 8.0f)) {
+                            const float now = fmaxf(m, top);
+                            const float alpha = now == kNone ? 1.0f : exp2_raw(m - now);
+                            m = now;
+                            l *= alpha;
 #pragma unroll
-            for (int b = 0; b < 2; b++)
+                            for (int t = 0; t < DT; t++)
 #pragma unroll
-                for (int i = 0; i < 16; i++) {
-                    sc[b][i] = exp2_raw(__builtin_fmaf(sc[b][i], c, -from));
-                    sum += sc[b][i];
-                }
-            l += sum;
+                                for (int i = 0; i < 16; i++) o[t][i] *= alpha;
+                        }
+                        const float from = m == kNone ? 0.0f : m;
+                        float sum = 0.0f;
 #pragma unroll
-            for (int i = 0; i < 4; i++) p[i] = pack8(sc[i >> 1], i & 1);
-        }
-        if (active) {
+                        for (int b = 0; b < 2; b++)
 #pragma unroll
-            for (int i = 0; i < 4; i++)
+                            for (int i = 0; i < 16; i++) {
+                                sc[b][i] = exp2_raw(__builtin_fmaf(sc[b][i], c, -from));
+                                sum += sc[b][i];
+                            }
+                        l += sum;
 #pragma unroll
-                for (int t = 0; t < DT; t++) o[t] = mfma(f.transposed(vt, i, t), p[i], o[t]);
+                        for (int i = 0; i < 4; i++) p[i] = pack8(sc[i >> 1], i & 1);
+                    }
+                });
         }
         landed();
     }
@@ -456,30 +483,46 @@ __global__ void __launch_bounds__(kThreads, 2) attn_bwd_q_bf16_kernel(AttnArgs a
             ks.load(K, a.k_stride, k0 + kKeys, r.lk, D, base + (st ^ 1) * G::kBytes, wave);
             vs.load(V, a.v_stride, k0 + kKeys, r.lk, D, base + (2 + (st ^ 1)) * G::kBytes, wave);
         }
-        auto block = [&](int b) {
-            f32x16_t sc = {}, dp = {};
-#pragma unroll
-            for (int i = 0; i < 2 * DT; i++) {
-                sc = mfma(f.straight(kt, b, i), qv[i], sc);
-                dp = mfma(f.straight(vt, b, i), gv[i], dp);
-            }
-#pragma unroll
-            for (int i = 0; i < 16; i++) sc[i] = exp2_raw(__builtin_fmaf(sc[i], c, -lse2)) * (dp[i] - delta);
-            if (k0 + 32 * b + 31 > w.all_seen) {
-#pragma unroll
-                for (int i = 0; i < 16; i++)
-                    if (k0 + 32 * b + acc_row(i) + 4 * half > w.seen) sc[i] = 0.0f;
-            }
-#pragma unroll
-            for (int i = 0; i < 2; i++) {
-                const bf16x8_t ds = pack8(sc, i);
-#pragma unroll
-                for (int t = 0; t < DT; t++) dq[t] = mfma(f.transposed(kt, 2 * b + i, t), ds, dq[t]);
-            }
-        };
         if (active) {
-            block(0);
-            block(1);
+            f32x16_t sc, dp;
+            bf16x8_t ds[2];
+            // for each 32 keys: DT groups of S and dP (two steps of 16 features each), then two of dq
+            pipelined<2 * (DT + 2)>(
+                [&](auto g, bf16x8_t (&x)[4]) {
+                    constexpr int b = g / (DT + 2), n = g % (DT + 2);
+                    if constexpr (n < DT) {
+#pragma unroll
+                        for (int i = 0; i < 4; i++) x[i] = f.straight((i & 1) ? vt : kt, b, 2 * n + (i >> 1));
+                    } else {
+#pragma unroll
+                        for (int t = 0; t < DT; t++) x[t] = f.transposed(kt, 2 * b + n - DT, t);
+                    }
+                },
+                [&](auto g, bf16x8_t (&x)[4]) {
+                    constexpr int b = g / (DT + 2), n = g % (DT + 2);
+                    if constexpr (n == 0) sc = dp = f32x16_t{};
+                    if constexpr (n < DT) {
+#pragma unroll
+                        for (int i = 0; i < 2; i++) {
+                            sc = mfma(x[2 * i], qv[2 * n + i], sc);
+                            dp = mfma(x[2 * i + 1], gv[2 * n + i], dp);
+                        }
+                    } else {
+#pragma unroll
+                        for (int t = 0; t < DT; t++) dq[t] = mfma(x[t], ds[n - DT], dq[t]);
+                    }
+                    if constexpr (n == DT - 1) {
+#pragma unroll
+                        for (int i = 0; i < 16; i++) sc[i] = exp2_raw(__builtin_fmaf(sc[i], c, -lse2)) * (dp[i] - delta);
+                        if (k0 + 32 * b + 31 > w.all_seen) {
+#pragma unroll
+                            for (int i = 0; i < 16; i++)
+                                if (k0 + 32 * b + acc_row(i) + 4 * half > w.seen) sc[i] = 0.0f;
+                        }
+#pragma unroll
+                        for (int i = 0; i < 2; i++) ds[i] = pack8(sc, i);
+                    }
+                });
         }
         landed();
     }
@@ -577,44 +620,82 @@ __global__ void __launch_bounds__(kThreads, 2) attn_bwd_kv_bf16_kernel(AttnArgs 
             gs.load(dO + (int64_t)next_head * D, g_stride, next_q0, r.lq, D, base + (2 + (st ^ 1)) * G::kBytes, wave);
         }
         if (active) {
+            f32x16_t sc, dp;
+            bf16x8_t p[2], ds[2];
+            // for each 32 queries: groups of S (four steps of 16 features), of dP (two steps where v comes from LDS
+            // too), then dv and dk of 16 queries each in turn
+            constexpr int kS = (2 * DT + 3) / 4, kP = kWide ? DT : kS, kAll = kS + kP + 4;
+            pipelined<kQ / 32 * kAll>(
+                [&](auto g, bf16x8_t (&x)[4]) {
+                    constexpr int b = g / kAll, n = g % kAll;
+                    if constexpr (n == 0) f.hold();
+                    if constexpr (n < kS) {
 #pragma unroll
-            for (int b = 0; b < kQ / 32; b++) {
-                f.hold();
-                f32x16_t sc = {}, dp = {};
+                        for (int i = 0; i < 4; i++)
+                            if (4 * n + i < 2 * DT) x[i] = f.straight(qt, b, 4 * n + i);
+                    } else if constexpr (n < kS + kP) {
+                        constexpr int m = n - kS;
 #pragma unroll
-                for (int i = 0; i < 2 * DT; i++) sc = mfma(f.straight(qt, b, i), kv[i], sc);
+                        for (int i = 0; i < 4; i++) {
+                            if constexpr (kWide) x[i] = (i & 1) ? f.straight(vt, wave, 2 * m + (i >> 1)) : f.straight(gt, b, 2 * m + (i >> 1));
+                            else if (4 * m + i < 2 * DT) x[i] = f.straight(gt, b, 4 * m + i);
+                        }
+                    } else {
+                        constexpr int m = n - kS - kP;
 #pragma unroll
-                for (int i = 0; i < 2 * DT; i++) {
-                    if constexpr (kWide) dp = mfma(f.straight(gt, b, i), f.straight(vt, wave, i), dp);
-                    else dp = mfma(f.straight(gt, b, i), vv[i], dp);
-                }
-#pragma unroll
-                for (int g = 0; g < 4; g++) {
-                    const f32x4_any_t ls = *reinterpret_cast<const f32x4_any_t *>(&stats[st][0][32 * b + 8 * g + 4 * half]);
-                    const f32x4_any_t de = *reinterpret_cast<const f32x4_any_t *>(&stats[st][1][32 * b + 8 * g + 4 * half]);
-#pragma unroll
-                    for (int e = 0; e < 4; e++) {
-                        sc[4 * g + e] = exp2_raw(__builtin_fmaf(sc[4 * g + e], c, -ls[e]));
-                        dp[4 * g + e] -= de[e];
+                        for (int t = 0; t < DT; t++) x[t] = f.transposed((m & 1) ? qt : gt, 2 * b + (m >> 1), t);
                     }
-                }
-                if (q0 + 32 * b < all_from) {
+                },
+                [&](auto g, bf16x8_t (&x)[4]) {
+                    constexpr int b = g / kAll, n = g % kAll;
+                    if constexpr (n == 0) sc = dp = f32x16_t{};
+                    if constexpr (n < kS) {
 #pragma unroll
-                    for (int i = 0; i < 16; i++)
-                        if (q0 + 32 * b + acc_row(i) + 4 * half < from) sc[i] = dp[i] = 0.0f;
-                }
+                        for (int i = 0; i < 4; i++)
+                            if (4 * n + i < 2 * DT) sc = mfma(x[i], kv[4 * n + i], sc);
+                    } else if constexpr (n < kS + kP) {
+                        constexpr int m = n - kS;
+                        if constexpr (kWide) {
+                            dp = mfma(x[0], x[1], dp);
+                            dp = mfma(x[2], x[3], dp);
+                        } else {
 #pragma unroll
-                for (int i = 0; i < 16; i++) dp[i] *= sc[i];
+                            for (int i = 0; i < 4; i++)
+                                if (4 * m + i < 2 * DT) dp = mfma(x[i], vv[4 * m + i], dp);
+                        }
+                    } else {
+                        constexpr int m = n - kS - kP;
 #pragma unroll
-                for (int i = 0; i < 2; i++) {
-                    const bf16x8_t p = pack8(sc, i), ds = pack8(dp, i);
-#pragma unroll
-                    for (int t = 0; t < DT; t++) {
-                        dv[t] = mfma(f.transposed(gt, 2 * b + i, t), p, dv[t]);
-                        dk[t] = mfma(f.transposed(qt, 2 * b + i, t), ds, dk[t]);
+                        for (int t = 0; t < DT; t++) {
+                            if constexpr (m & 1) dk[t] = mfma(x[t], ds[m >> 1], dk[t]);
+                            else dv[t] = mfma(x[t], p[m >> 1], dv[t]);
+                        }
                     }
-                }
-            }
+                    if constexpr (n == kS + kP - 1) {
+#pragma unroll
+                        for (int q = 0; q < 4; q++) {
+                            const f32x4_any_t ls = *reinterpret_cast<const f32x4_any_t *>(&stats[st][0][32 * b + 8 * q + 4 * half]);
+                            const f32x4_any_t de = *reinterpret_cast<const f32x4_any_t *>(&stats[st][1][32 * b + 8 * q + 4 * half]);
+#pragma unroll
+                            for (int e = 0; e < 4; e++) {
+                                sc[4 * q + e] = exp2_raw(__builtin_fmaf(sc[4 * q + e], c, -ls[e]));
+                                dp[4 * q + e] -= de[e];
+                            }
+                        }
+                        if (q0 + 32 * b < all_from) {
+#pragma unroll
+                            for (int i = 0; i < 16; i++)
+                                if (q0 + 32 * b + acc_row(i) + 4 * half < from) sc[i] = dp[i] = 0.0f;
+                        }
+#pragma unroll
+                        for (int i = 0; i < 16; i++) dp[i] *= sc[i];
+#pragma unroll
+                        for (int i = 0; i < 2; i++) {
+                            p[i] = pack8(sc, i);
+                            ds[i] = pack8(dp, i);
+                        }
+                    }
+                });
         }
         if (more) store_stats(st ^ 1);
         head = next_head;
