@@ -69,14 +69,18 @@ struct Dma {
     }
     // (the key's linearity needs rows that differ by whole kRowsEach to differ in bits that a lane's row does not use)
     static_assert(G::kLoads * kRowsEach >= 8 && (kRowsEach & (kRowsEach - 1)) == 0, "rows of a wave's loads");
-    // offset of load i: past head_dim with bit 31 set (read as zeros)
-    __device__ __forceinline__ uint32_t off(uint32_t i, int64_t stride, int D) const {
+    // offset of load i: past head_dim, and for the `lead` rows of the tile that lie before the base, with bit 31 set (read
+    // as zeros)
+    __device__ __forceinline__ uint32_t off(uint32_t i, int64_t stride, int D, int lead) const {
         const uint32_t c = chunk ^ (G::key(i * kRowsEach) << 4);
-        return (row + i * kRowsEach * (uint32_t)(stride * 2) + c) | ((int)c < 2 * D ? 0u : 0x80000000u);
+        return (row + i * kRowsEach * (uint32_t)(stride * 2) - (uint32_t)lead * (uint32_t)(stride * 2) + c) |
+               ((int)c < 2 * D ? 0u : 0x80000000u);
     }
-    // rows `row` .. of a sequence of n rows that starts at base, into the tile at LDS address `tile`
-    __device__ __forceinline__ void load(const uint16_t *base, int64_t stride, int row, int n, int D, uint32_t tile, int wave) const {
-        const int left = n - row < ROWS ? n - row : ROWS;
+    // rows `row` .. of a sequence of n rows that starts at base, into the tile at LDS address `tile`, behind `lead` rows of
+    // zeros
+    __device__ __forceinline__ void load(const uint16_t *base, int64_t stride, int row, int n, int D, uint32_t tile, int wave,
+                                         int lead = 0) const {
+        const int left = n - row < ROWS - lead ? n - row : ROWS - lead;
         const uint64_t p = (uint64_t)(base + row * stride);
         const u32x4_t rs = {scalar((uint32_t)p), scalar((uint32_t)(p >> 32) & 0xFFFFu),
                             scalar(left > 0 ? (uint32_t)(((left - 1) * stride + D) * 2) : 0u), (uint32_t)kRsrcWord3};
@@ -88,7 +92,7 @@ struct Dma {
                 "s_add_u32 m0, %0, 0x800\n\ts_nop 0\n\tbuffer_load_dwordx4 %3, %5, 0 offen lds\n\t"
                 "s_add_u32 m0, %0, 0xc00\n\ts_nop 0\n\tbuffer_load_dwordx4 %4, %5, 0 offen lds"
                 :
-                : "s"(at), "v"(off(0, stride, D)), "v"(off(1, stride, D)), "v"(off(2, stride, D)), "v"(off(3, stride, D)), "s"(rs)
+                : "s"(at), "v"(off(0, stride, D, lead)), "v"(off(1, stride, D, lead)), "v"(off(2, stride, D, lead)), "v"(off(3, stride, D, lead)), "s"(rs)
                 : "memory", "scc");
         } else {
             static_assert(G::kLoads == 2, "two or four loads per wave");
@@ -96,7 +100,7 @@ struct Dma {
                 "s_nop 4\n\ts_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %3, 0 offen lds\n\t"
                 "s_add_u32 m0, %0, 0x400\n\ts_nop 0\n\tbuffer_load_dwordx4 %2, %3, 0 offen lds"
                 :
-                : "s"(at), "v"(off(0, stride, D)), "v"(off(1, stride, D)), "s"(rs)
+                : "s"(at), "v"(off(0, stride, D, lead)), "v"(off(1, stride, D, lead)), "s"(rs)
                 : "memory", "scc");
         }
     }
@@ -133,6 +137,39 @@ struct Frags {
         const i16x4_t v[2] = {
             __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4 *)(uintptr_t)((tr[0] ^ (uint32_t)(64 * t)) + tile + s * 16 * G::kPitch)),
             __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4 *)(uintptr_t)((tr[1] ^ (uint32_t)(64 * t)) + tile + s * 16 * G::kPitch))};
+        return __builtin_bit_cast(bf16x8_t, v);
+    }
+};
+
+// The same with every address in a register of its own, for tiles at compile-time offsets: no operation per read.
+template <int DT>
+struct Addresses {
+    using G = Tile<DT>;
+    uint32_t row[2 * DT], tr[2][DT];
+    __device__ __forceinline__ void init(int lane, uint32_t base) {
+        Frags<DT> f;
+        f.init(lane);
+#pragma unroll
+        for (int s = 0; s < 2 * DT; s++) row[s] = (f.row ^ (uint32_t)(32 * s)) + base;
+#pragma unroll
+        for (int t = 0; t < DT; t++)
+#pragma unroll
+            for (int e = 0; e < 2; e++) tr[e][t] = (f.tr[e] ^ (uint32_t)(64 * t)) + base;
+        // from here on they are what they are, not something to be formed again
+#pragma unroll
+        for (int s = 0; s < 2 * DT; s++) asm volatile("" : "+v"(row[s]));
+#pragma unroll
+        for (int t = 0; t < DT; t++) asm volatile("" : "+v"(tr[0][t]), "+v"(tr[1][t]));
+    }
+    template <uint32_t TILE>
+    __device__ __forceinline__ bf16x8_t straight(int b, int s) const {
+        return *(lds_bf16x8 *)(uintptr_t)(row[s] + (TILE + b * 32 * G::kPitch));
+    }
+    template <uint32_t TILE>
+    __device__ __forceinline__ bf16x8_t transposed(int s, int t) const {
+        const i16x4_t v[2] = {
+            __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4 *)(uintptr_t)(tr[0][t] + (TILE + s * 16 * G::kPitch))),
+            __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4 *)(uintptr_t)(tr[1][t] + (TILE + s * 16 * G::kPitch)))};
         return __builtin_bit_cast(bf16x8_t, v);
     }
 };
@@ -273,89 +310,132 @@ __global__ void __launch_bounds__(kThreads, 2) attn_fwd_bf16_kernel(AttnArgs a, 
     Dma<DT> ks, vs;
     ks.init(a.k_stride, wave, lane);
     vs.init(a.v_stride, wave, lane);
-    Frags<DT> f;
-    f.init(lane);
     const uint32_t base = lds_addr(smem);
+    Addresses<DT> f;
+    f.init(lane, base);
 
     f32x16_t o[DT] = {};
     float m = kNone, l = 0.0f;
-    if (j0 < nk) {
-        ks.load(K, a.k_stride, j0 * kKeys, r.lk, D, base, wave);
-        vs.load(V, a.v_stride, j0 * kKeys, r.lk, D, base + 2 * G::kBytes, wave);
-    }
+    // The scores of 32 keys are formed a step ahead: the exponentials of a step, as much work as its products, go between
+    // the matrix instructions that form the next step's scores and the first half of this one's output, and the next step's
+    // maximum between those of the second half.
+    f32x16_t sa, sb;  // steps of the first and the second half of a tile
+    float top;
+    constexpr int kS = (2 * DT + 3) / 4;  // groups of four 16-feature steps
+    auto load_keys = [&](auto stage, int b, auto g, bf16x8_t (&x)[4]) {
+        constexpr uint32_t kTile = decltype(stage)::value * G::kBytes;
+#pragma unroll
+        for (int i = 0; i < 4; i++)
+            if (4 * g + i < 2 * DT) x[i] = f.template straight<kTile>(b, 4 * g + i);
+    };
+    auto hide = [&](f32x16_t &x, int k0) {  // keys that a row does not see, in the steps where there are any
+        if (k0 + 31 > all_seen) {
+#pragma unroll
+            for (int i = 0; i < 16; i++)
+                if (k0 + acc_row(i) + 4 * half > seen) x[i] = kNone;
+        }
+    };
+    // Tile j of the values is 32 rows behind tile j of the keys: what an iteration reads of either is then one tile.
+    constexpr std::integral_constant<int, 0> s0{};
+    constexpr std::integral_constant<int, 1> s1{};
+    auto fetch = [&](int j, uint32_t stage) {
+        if (j < nk) ks.load(K, a.k_stride, j * kKeys, r.lk, D, base + stage * G::kBytes, wave);
+        if (j <= nk) vs.load(V, a.v_stride, j > 0 ? j * kKeys - 32 : 0, r.lk, D, base + (2 + stage) * G::kBytes, wave, j > 0 ? 0 : 32);
+    };
+    if (j0 < nk) fetch(j0, 0u);
     landed();
-    for (int j = j0; j < nk; j++) {
-        const int st = (j - j0) & 1, k0 = j * kKeys;
-        const uint32_t kt = base + st * G::kBytes, vt = base + (2 + st) * G::kBytes;
-        const bool more = j + 1 < nk, active = k0 <= any_seen;
-        if (more) {
-            ks.load(K, a.k_stride, k0 + kKeys, r.lk, D, base + (st ^ 1) * G::kBytes, wave);
-            vs.load(V, a.v_stride, k0 + kKeys, r.lk, D, base + (2 + (st ^ 1)) * G::kBytes, wave);
+    const int last = any_seen < 0 ? -1 : any_seen / 32 < 2 * nk ? any_seen / 32 : 2 * nk - 1;  // this wave's last step
+    if (2 * j0 <= last) {
+        sa = f32x16_t{};
+        pipelined<kS>([&](auto g, bf16x8_t (&x)[4]) { load_keys(s0, 0, g, x); },
+                      [&](auto g, bf16x8_t (&x)[4]) {
+#pragma unroll
+                          for (int i = 0; i < 4; i++)
+                              if (4 * g + i < 2 * DT) sa = mfma(x[i], qv[4 * g + i], sa);
+                      });
+        hide(sa, j0 * kKeys);
+        top = sa[0];
+#pragma unroll
+        for (int i = 1; i < 16; i++) top = fmaxf(top, sa[i]);
+    }
+    // Step u of 32 keys with scores sc, its values the rows 32 b .. 32 b + 31 of the staged ones; the next step's scores into
+    // sn from the keys 32 b .. (after the last step: whatever the stage holds, which nothing reads).
+    auto step = [&](int u, auto stage, auto b, f32x16_t &sc, f32x16_t &sn) {
+        constexpr uint32_t kValues = (2 + decltype(stage)::value) * G::kBytes;
+        bf16x8_t p[2];
+        float sum[2] = {0.0f, 0.0f};
+        top = max_halves(top) * c;
+        // The reference that the exponents are taken from follows the maximum only where it is passed by more than 8:
+        // probabilities stay below 2^8, and most steps need no rescaling.
+        if (__any(top > m + 8.0f)) {
+            const float now = fmaxf(m, top);
+            const float alpha = now == kNone ? 1.0f : exp2_raw(m - now);
+            m = now;
+            l *= alpha;
+#pragma unroll
+            for (int t = 0; t < DT; t++)
+#pragma unroll
+                for (int i = 0; i < 16; i++) o[t][i] *= alpha;
         }
-        if (active) {
-            f32x16_t sc[2] = {};
-            bf16x8_t p[4];
-            // DT groups of scores (two steps of 16 features, both halves of the tile), then four of the output
-            pipelined<DT + 4>(
-                [&](auto g, bf16x8_t (&x)[4]) {
-                    if constexpr (g < DT) {
+        const float from = m == kNone ? 0.0f : m;
+        // part n of `of` of the eight exponentials of half h of the accumulator; packed when they are complete
+        auto exponentials = [&](int h, int n, int of) {
 #pragma unroll
-                        for (int i = 0; i < 4; i++) x[i] = f.straight(kt, i & 1, 2 * g + (i >> 1));
-                    } else {
+            for (int e = 8 * n / of; e < 8 * (n + 1) / of; e++) {
+                const float x = exp2_raw(__builtin_fmaf(sc[8 * h + e], c, -from));
+                sc[8 * h + e] = x;
+                sum[e & 1] += x;
+            }
+            if (n == of - 1) p[h] = pack8(sc, h);
+        };
+        sn = f32x16_t{};
+        pipelined<kS + 2>(
+            [&](auto g, bf16x8_t (&x)[4]) {
+                if constexpr (g < kS) {
+                    load_keys(stage, b, g, x);
+                } else {
 #pragma unroll
-                        for (int t = 0; t < DT; t++) x[t] = f.transposed(vt, g - DT, t);
-                    }
-                },
-                [&](auto g, bf16x8_t (&x)[4]) {
-                    if constexpr (g < DT) {
-#pragma unroll
-                        for (int i = 0; i < 4; i++) sc[i & 1] = mfma(x[i], qv[2 * g + (i >> 1)], sc[i & 1]);
-                    } else {
-#pragma unroll
-                        for (int t = 0; t < DT; t++) o[t] = mfma(x[t], p[g - DT], o[t]);
-                    }
-                    if constexpr (g == DT - 1) {
-                        if (k0 + kKeys - 1 > all_seen) {
-#pragma unroll
-                            for (int b = 0; b < 2; b++)
-#pragma unroll
-                                for (int i = 0; i < 16; i++)
-                                    if (k0 + 32 * b + acc_row(i) + 4 * half > seen) sc[b][i] = kNone;
+                    for (int t = 0; t < DT; t++) x[t] = f.template transposed<kValues>(2 * b + g - kS, t);
+                }
+            },
+            [&](auto g, bf16x8_t (&x)[4]) {
+                if constexpr (g < kS) {
+                    static_for<4>([&](auto i) {
+                        if constexpr (4 * g + i < 2 * DT) {
+                            sn = mfma(x[i], qv[4 * g + i], sn);
+                            exponentials(0, 4 * g + i, 2 * DT);
+                            __builtin_amdgcn_sched_barrier(0);
                         }
-                        float top = sc[0][0];
+                    });
+                    if constexpr (g == kS - 1) hide(sn, 32 * u + 32);
+                } else if constexpr (g == kS) {
+                    static_for<DT>([&](auto t) {
+                        o[t] = mfma(x[t], p[0], o[t]);
+                        exponentials(1, t, DT);
+                        __builtin_amdgcn_sched_barrier(0);
+                    });
+                } else {
+                    top = sn[0];
 #pragma unroll
-                        for (int b = 0; b < 2; b++)
+                    for (int t = 0; t < DT; t++) o[t] = mfma(x[t], p[1], o[t]);
 #pragma unroll
-                            for (int i = 0; i < 16; i++) top = fmaxf(top, sc[b][i]);
-                        top = max_halves(top) * c;
-                        // The reference that the exponents are taken from follows the maximum only where it is passed by
-                        // more than 8: probabilities stay below 2^8, and most tiles need no rescaling.
-                        if (__any(top > m + 8.0f)) {
-                            const float now = fmaxf(m, top);
-                            const float alpha = now == kNone ? 1.0f : exp2_raw(m - now);
-                            m = now;
-                            l *= alpha;
-#pragma unroll
-                            for (int t = 0; t < DT; t++)
-#pragma unroll
-                                for (int i = 0; i < 16; i++) o[t][i] *= alpha;
-                        }
-                        const float from = m == kNone ? 0.0f : m;
-                        float sum = 0.0f;
-#pragma unroll
-                        for (int b = 0; b < 2; b++)
-#pragma unroll
-                            for (int i = 0; i < 16; i++) {
-                                sc[b][i] = exp2_raw(__builtin_fmaf(sc[b][i], c, -from));
-                                sum += sc[b][i];
-                            }
-                        l += sum;
-#pragma unroll
-                        for (int i = 0; i < 4; i++) p[i] = pack8(sc[i >> 1], i & 1);
-                    }
-                });
-        }
+                    for (int i = 1; i < 16; i++) top = fmaxf(top, sn[i]);
+                }
+            });
+        l += sum[0] + sum[1];
+    };
+    // iteration j: the second half of tile j - 1 and the first of tile j
+    auto iteration = [&](int j, auto stage) {
+        fetch(j + 1, decltype(stage)::value ^ 1u);
+        if (j > j0 && 2 * j - 1 <= last) step(2 * j - 1, stage, s0, sb, sa);
+        if (2 * j <= last) step(2 * j, stage, s1, sa, sb);
         landed();
+    };
+    if (j0 < nk) {
+        for (int j = j0; j <= nk; j += 2) {
+            iteration(j, s0);
+            if (j < nk) iteration(j + 1, s1);
+        }
     }
     l = sum_halves(l);
     if constexpr (SPLIT) {
