@@ -29,8 +29,9 @@ constexpr int kKeys = 64;   // rows of a staged tile
 constexpr float kNone = -__builtin_inff();
 
 // Geometry of a staged tile of ROWS rows: DT x 32 features, a row of 128 (DT <= 2) or 256 bytes. 16-byte chunk c of row r
-// lies at chunk c ^ key(r): 8 consecutive rows of one chunk (a fragment read), and 4 rows of two neighbouring chunks (half a
-// transposing read), then lie in different banks.
+// lies at chunk c ^ key(r): 16 consecutive rows of one chunk (a fragment read) then fill the 256 bytes of a pass over the
+// banks, and so do 4 rows of four neighbouring chunks (half a transposing read; keys that put two of the rows in one
+// 64-byte quarter made those reads take twice as long).
 template <int DT, int ROWS = kKeys>
 struct Tile {
     static constexpr int kChunks = DT <= 2 ? 8 : 16;
@@ -39,8 +40,7 @@ struct Tile {
     static constexpr int kLoads = ROWS * kChunks / kThreads;  // 16-byte loads per thread
     // linear in the bits of r (exclusive or), and of its low four alone
     __host__ __device__ static constexpr uint32_t key(uint32_t r) {
-        if constexpr (kChunks == 16) return ((r & 7u) << 1) | ((r >> 3) & 1u);
-        return (((r >> 1) & 3u) << 1) | ((r >> 3) & 1u);
+        return kChunks == 16 ? (r & 3u) << 2 | ((r >> 2) & 3u) : (r & 2u) << 1 | ((r >> 2) & 3u);
     }
 };
 
@@ -659,13 +659,13 @@ __global__ void __launch_bounds__(kThreads, 2) attn_bwd_kv_bf16_kernel(AttnArgs 
         if (threadIdx.x < 2 * kQ) {
             const int row = q0 + (threadIdx.x & (kQ - 1)), which = threadIdx.x / kQ;
             const int64_t at = stat + (int64_t)head * a.Tq + row;
-            sv = which == 0 ? __builtin_inff() : 0.0f;
-            if (row < r.lq) sv = which == 0 ? a.lse[at] * kLog2e : a.delta[at];
-            if (which == 0 && sv == kNone) sv = __builtin_inff();
+            sv = which == 0 ? kNone : 0.0f;
+            if (row < r.lq) sv = which == 0 ? a.lse[at] : a.delta[at];  // not looked at before the tile's work is done
         }
     };
     auto store_stats = [&](int stage) {
-        if (threadIdx.x < 2 * kQ) (&stats[stage][0][0])[threadIdx.x] = sv;
+        if (threadIdx.x < 2 * kQ)
+            (&stats[stage][0][0])[threadIdx.x] = threadIdx.x >= kQ ? sv : sv == kNone ? __builtin_inff() : sv * kLog2e;
     };
     bf16x8_t kv[2 * DT], vv[kWide ? 1 : 2 * DT];
     load_row<DT>(static_cast<const uint16_t *>(a.k) + (r.k0 + k) * a.k_stride + (int64_t)hk * D, ok, D, half, kv);
