@@ -609,7 +609,10 @@ __global__ void __launch_bounds__(kThreads, 2) attn_bwd_q_bf16_kernel(AttnArgs a
     store_row<DT>(static_cast<uint16_t *>(a.dq) + (r.q0 + w.q) * a.dq_stride + (int64_t)w.h * D, w.ok, D, half, dq, a.scale);
 }
 
-// dk and dv of 128 keys of one key-value head, 32 per wave, over the queries of every head that shares it, head by head.
+// dk and dv of 128 keys of one key-value head, 32 per wave, over the queries of every head that shares it: tiles of queries
+// from the last to the first that sees a key, the heads of each in turn, so that the workgroups of a sequence, which end at
+// different queries, run through the same tiles at the same time and find them in L2 (from the first on, head by head, they
+// were spread over the sequence, and the backward of 32 x 2,048 tokens took BEFORE ms in place of AFTER).
 // Here a lane's column is a key and the queries run down the accumulators (S = q k^T as it is written): P and dS are the
 // B operands of dv^T = dO^T P and dk^T = q^T dS. Queries and their gradients go through LDS in tiles with their lse and delta;
 // a query that does not exist, or sees nothing, has lse = +inf there and so probability 0.
@@ -640,7 +643,7 @@ __global__ void __launch_bounds__(kThreads, 2) attn_bwd_kv_bf16_kernel(AttnArgs 
     const int q_first = seen_from(tile * kRows) / kQ * kQ;
     const int any_from = seen_from(w_first), all_from = seen_from(w_first + 31), from = seen_from(k);
     const int per_head = r.lq > q_first ? (r.lq - q_first + kQ - 1) / kQ : 0;
-    const int items = per_head * group;
+    const int items = per_head * group, q_last = q_first + (per_head - 1) * kQ;
 
     const float c = a.scale * kLog2e;
     const int64_t g_stride = (int64_t)a.Hq * D;
@@ -654,48 +657,56 @@ __global__ void __launch_bounds__(kThreads, 2) attn_bwd_kv_bf16_kernel(AttnArgs 
     Frags<DT> f;
     f.init(lane);
     const uint32_t base = lds_addr(smem), vt = base + 4 * G::kBytes;
-    float sv = 0.0f;
+    // lse and delta of a tile's queries: loaded by every wave, without a branch (the values of two paths would be joined, and
+    // so waited for, at once), looked at and written by the first when the tile's work is done
+    constexpr int kStats = 2 * kQ / 64;
+    float sv[kStats];
     auto load_stats = [&](int head, int q0) {
-        if (threadIdx.x < 2 * kQ) {
-            const int row = q0 + (threadIdx.x & (kQ - 1)), which = threadIdx.x / kQ;
-            const int64_t at = stat + (int64_t)head * a.Tq + row;
-            sv = which == 0 ? kNone : 0.0f;
-            if (row < r.lq) sv = which == 0 ? a.lse[at] : a.delta[at];  // not looked at before the tile's work is done
+#pragma unroll
+        for (int i = 0; i < kStats; i++) {
+            const int v = lane + 64 * i, row = q0 + v % kQ;
+            const float *from_stat = (v < kQ ? a.lse : a.delta) + stat + (int64_t)head * a.Tq;
+            sv[i] = from_stat[row < r.lq ? row : r.lq - 1];
         }
     };
-    auto store_stats = [&](int stage) {
-        if (threadIdx.x < 2 * kQ)
-            (&stats[stage][0][0])[threadIdx.x] = threadIdx.x >= kQ ? sv : sv == kNone ? __builtin_inff() : sv * kLog2e;
+    auto store_stats = [&](int stage, int q0) {
+        if (wave != 0) return;
+#pragma unroll
+        for (int i = 0; i < kStats; i++) {
+            const int v = lane + 64 * i;
+            const bool in = q0 + v % kQ < r.lq;
+            (&stats[stage][0][0])[v] = v >= kQ ? (in ? sv[i] : 0.0f) : in && sv[i] != kNone ? sv[i] * kLog2e : __builtin_inff();
+        }
     };
     bf16x8_t kv[2 * DT], vv[kWide ? 1 : 2 * DT];
     load_row<DT>(static_cast<const uint16_t *>(a.k) + (r.k0 + k) * a.k_stride + (int64_t)hk * D, ok, D, half, kv);
     if constexpr (!kWide) load_row<DT>(V + k * a.v_stride, ok, D, half, vv);
     f32x16_t dk[DT] = {}, dv[DT] = {};
     if (items > 0) {
-        load_stats(0, q_first);
-        qs.load(Q, a.q_stride, q_first, r.lq, D, base, wave);
-        gs.load(dO, g_stride, q_first, r.lq, D, base + 2 * G::kBytes, wave);
+        load_stats(0, q_last);
+        qs.load(Q, a.q_stride, q_last, r.lq, D, base, wave);
+        gs.load(dO, g_stride, q_last, r.lq, D, base + 2 * G::kBytes, wave);
         if constexpr (kWide) {
             Dma<DT> vs;
             vs.init(a.v_stride, wave, lane);
             vs.load(V, a.v_stride, tile * kRows, r.lk, D, vt, wave);
             vs.load(V, a.v_stride, tile * kRows + kKeys, r.lk, D, vt + GV::kBytes, wave);
         }
-        store_stats(0);
+        store_stats(0, q_last);
     }
     landed();
-    int head = 0, q0 = q_first;
+    int head = 0, q0 = q_last;
     for (int it = 0; it < items; it++) {
         const int st = it & 1;
         const uint32_t qt = base + st * G::kBytes, gt = base + (2 + st) * G::kBytes;
         const bool more = it + 1 < items, active = q0 + kQ > any_from;
-        int next_head = head, next_q0 = q0 + kQ;
-        if (next_q0 >= r.lq) {
-            next_head++;
-            next_q0 = q_first;
+        int next_head = head + 1, next_q0 = q0;
+        if (next_head == group) {
+            next_head = 0;
+            next_q0 -= kQ;
         }
+        load_stats(more ? next_head : head, more ? next_q0 : q0);
         if (more) {
-            load_stats(next_head, next_q0);
             qs.load(Q + (int64_t)next_head * D, a.q_stride, next_q0, r.lq, D, base + (st ^ 1) * G::kBytes, wave);
             gs.load(dO + (int64_t)next_head * D, g_stride, next_q0, r.lq, D, base + (2 + (st ^ 1)) * G::kBytes, wave);
         }
@@ -777,7 +788,7 @@ __global__ void __launch_bounds__(kThreads, 2) attn_bwd_kv_bf16_kernel(AttnArgs 
                     }
                 });
         }
-        if (more) store_stats(st ^ 1);
+        if (more) store_stats(st ^ 1, next_q0);
         head = next_head;
         q0 = next_q0;
         landed();
