@@ -188,17 +188,19 @@ __device__ __forceinline__ float sum_halves(float x) {
     return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
 
-// N groups of matrix instructions, each on up to four fragments that are read from LDS while the group before runs: two
-// sets of registers in turn. Left to itself the compiler reads each fragment just before its use, into the same few
-// registers, and every pair of instructions waits out the LDS latency.
-template <int N, typename Load, typename Run>
+// N groups of matrix instructions, each on up to F fragments that are read from LDS while the groups before run: R sets of
+// registers in turn, R - 1 groups ahead. Left to itself the compiler reads each fragment just before its use, into the same
+// few registers, and every pair of instructions waits out the LDS latency.
+template <int N, int F = 4, int R = 2, typename Load, typename Run>
 __device__ __forceinline__ void pipelined(Load &&load, Run &&run) {
-    bf16x8_t x[2][4];
-    load(std::integral_constant<int, 0>{}, x[0]);
+    bf16x8_t x[R][F];
+    static_for<R - 1>([&](auto g) {
+        if constexpr (g < N) load(g, x[g]);
+    });
     static_for<N>([&](auto g) {
-        if constexpr (g + 1 < N) load(std::integral_constant<int, g + 1>{}, x[(g + 1) & 1]);
+        if constexpr (g + R - 1 < N) load(std::integral_constant<int, g + R - 1>{}, x[(g + R - 1) % R]);
         __builtin_amdgcn_sched_barrier(0);
-        run(g, x[g & 1]);
+        run(g, x[g % R]);
         __builtin_amdgcn_sched_barrier(0);
     });
 }
@@ -713,56 +715,56 @@ __global__ void __launch_bounds__(kThreads, 2) attn_bwd_kv_bf16_kernel(AttnArgs 
         if (active) {
             f32x16_t sc, dp;
             bf16x8_t p[2], ds[2];
-            // for each 32 queries: groups of S (four steps of 16 features), of dP (two steps where v comes from LDS
-            // too), then dv and dk of 16 queries each in turn
-            constexpr int kS = (2 * DT + 3) / 4, kP = kWide ? DT : kS, kAll = kS + kP + 4;
-            pipelined<kQ / 32 * kAll>(
-                [&](auto g, bf16x8_t (&x)[4]) {
+            // for each 32 queries: groups of S (two steps of 16 features), of dP (one step where v comes from LDS too),
+            // then dv and dk of 16 queries each in turn (two blocks of 32 features at a time)
+            constexpr int kP = kWide ? 2 * DT : DT, kT = (DT + 1) / 2, kAll = DT + kP + 4 * kT;
+            pipelined<kQ / 32 * kAll, 2, 3>(
+                [&](auto g, bf16x8_t (&x)[2]) {
                     constexpr int b = g / kAll, n = g % kAll;
                     if constexpr (n == 0) f.hold();
-                    if constexpr (n < kS) {
+                    if constexpr (n < DT) {
 #pragma unroll
-                        for (int i = 0; i < 4; i++)
-                            if (4 * n + i < 2 * DT) x[i] = f.straight(qt, b, 4 * n + i);
-                    } else if constexpr (n < kS + kP) {
-                        constexpr int m = n - kS;
-#pragma unroll
-                        for (int i = 0; i < 4; i++) {
-                            if constexpr (kWide) x[i] = (i & 1) ? f.straight(vt, wave, 2 * m + (i >> 1)) : f.straight(gt, b, 2 * m + (i >> 1));
-                            else if (4 * m + i < 2 * DT) x[i] = f.straight(gt, b, 4 * m + i);
-                        }
-                    } else {
-                        constexpr int m = n - kS - kP;
-#pragma unroll
-                        for (int t = 0; t < DT; t++) x[t] = f.transposed((m & 1) ? qt : gt, 2 * b + (m >> 1), t);
-                    }
-                },
-                [&](auto g, bf16x8_t (&x)[4]) {
-                    constexpr int b = g / kAll, n = g % kAll;
-                    if constexpr (n == 0) sc = dp = f32x16_t{};
-                    if constexpr (n < kS) {
-#pragma unroll
-                        for (int i = 0; i < 4; i++)
-                            if (4 * n + i < 2 * DT) sc = mfma(x[i], kv[4 * n + i], sc);
-                    } else if constexpr (n < kS + kP) {
-                        constexpr int m = n - kS;
+                        for (int i = 0; i < 2; i++) x[i] = f.straight(qt, b, 2 * n + i);
+                    } else if constexpr (n < DT + kP) {
+                        constexpr int m = n - DT;
                         if constexpr (kWide) {
-                            dp = mfma(x[0], x[1], dp);
-                            dp = mfma(x[2], x[3], dp);
+                            x[0] = f.straight(gt, b, m);
+                            x[1] = f.straight(vt, wave, m);
                         } else {
 #pragma unroll
-                            for (int i = 0; i < 4; i++)
-                                if (4 * m + i < 2 * DT) dp = mfma(x[i], vv[4 * m + i], dp);
+                            for (int i = 0; i < 2; i++) x[i] = f.straight(gt, b, 2 * m + i);
                         }
                     } else {
-                        constexpr int m = n - kS - kP;
+                        constexpr int m = (n - DT - kP) / kT, t0 = 2 * ((n - DT - kP) % kT);
 #pragma unroll
-                        for (int t = 0; t < DT; t++) {
-                            if constexpr (m & 1) dk[t] = mfma(x[t], ds[m >> 1], dk[t]);
-                            else dv[t] = mfma(x[t], p[m >> 1], dv[t]);
+                        for (int i = 0; i < 2; i++)
+                            if (t0 + i < DT) x[i] = f.transposed((m & 1) ? qt : gt, 2 * b + (m >> 1), t0 + i);
+                    }
+                },
+                [&](auto g, bf16x8_t (&x)[2]) {
+                    constexpr int b = g / kAll, n = g % kAll;
+                    if constexpr (n == 0) sc = dp = f32x16_t{};
+                    if constexpr (n < DT) {
+#pragma unroll
+                        for (int i = 0; i < 2; i++) sc = mfma(x[i], kv[2 * n + i], sc);
+                    } else if constexpr (n < DT + kP) {
+                        constexpr int m = n - DT;
+                        if constexpr (kWide) {
+                            dp = mfma(x[0], x[1], dp);
+                        } else {
+#pragma unroll
+                            for (int i = 0; i < 2; i++) dp = mfma(x[i], vv[2 * m + i], dp);
+                        }
+                    } else {
+                        constexpr int m = (n - DT - kP) / kT, t0 = 2 * ((n - DT - kP) % kT);
+#pragma unroll
+                        for (int i = 0; i < 2; i++) {
+                            if (t0 + i >= DT) continue;
+                            if constexpr (m & 1) dk[t0 + i] = mfma(x[i], ds[m >> 1], dk[t0 + i]);
+                            else dv[t0 + i] = mfma(x[i], p[m >> 1], dv[t0 + i]);
                         }
                     }
-                    if constexpr (n == kS + kP - 1) {
+                    if constexpr (n == DT + kP - 1) {
 #pragma unroll
                         for (int q = 0; q < 4; q++) {
                             const f32x4_any_t ls = *reinterpret_cast<const f32x4_any_t *>(&stats[st][0][32 * b + 8 * q + 4 * half]);
