@@ -19,6 +19,7 @@ namespace {
 typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
 typedef short i16x4_t __attribute__((ext_vector_type(4)));
 typedef unsigned int u32x4_t __attribute__((ext_vector_type(4)));
+typedef float f32x4_t __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) i16x4_t lds_i16x4;
 typedef __attribute__((address_space(3))) bf16x8_t lds_bf16x8;
 typedef __attribute__((address_space(3))) u32x4_t lds_u32x4;
@@ -568,34 +569,47 @@ __global__ void __launch_bounds__(kThreads, 2) attn_bwd_q_bf16_kernel(AttnArgs a
         if (active) {
             f32x16_t sc, dp;
             bf16x8_t ds[2];
-            // for each 32 keys: DT groups of S and dP (two steps of 16 features each), then two of dq
-            pipelined<2 * (DT + 2)>(
+            // for each 32 keys: groups of S, then of dP (four steps of 16 features each) with the exponentials between their
+            // instructions, then two of dq
+            constexpr int kS = (2 * DT + 3) / 4, kAll = 2 * kS + 2;
+            pipelined<2 * kAll>(
                 [&](auto g, bf16x8_t (&x)[4]) {
-                    constexpr int b = g / (DT + 2), n = g % (DT + 2);
-                    if constexpr (n < DT) {
+                    constexpr int b = g / kAll, n = g % kAll;
+                    if constexpr (n < 2 * kS) {
 #pragma unroll
-                        for (int i = 0; i < 4; i++) x[i] = f.straight((i & 1) ? vt : kt, b, 2 * n + (i >> 1));
+                        for (int i = 0; i < 4; i++)
+                            if (4 * (n % kS) + i < 2 * DT) x[i] = f.straight(n < kS ? kt : vt, b, 4 * (n % kS) + i);
                     } else {
 #pragma unroll
-                        for (int t = 0; t < DT; t++) x[t] = f.transposed(kt, 2 * b + n - DT, t);
+                        for (int t = 0; t < DT; t++) x[t] = f.transposed(kt, 2 * b + n - 2 * kS, t);
                     }
                 },
                 [&](auto g, bf16x8_t (&x)[4]) {
-                    constexpr int b = g / (DT + 2), n = g % (DT + 2);
-                    if constexpr (n == 0) sc = dp = f32x16_t{};
-                    if constexpr (n < DT) {
+                    constexpr int b = g / kAll, n = g % kAll;
+                    if constexpr (n == 0) sc = f32x16_t{};
+                    if constexpr (n == kS) dp = f32x16_t{};
+                    if constexpr (n < kS) {
 #pragma unroll
-                        for (int i = 0; i < 2; i++) {
-                            sc = mfma(x[2 * i], qv[2 * n + i], sc);
-                            dp = mfma(x[2 * i + 1], gv[2 * n + i], dp);
-                        }
+                        for (int i = 0; i < 4; i++)
+                            if (4 * n + i < 2 * DT) sc = mfma(x[i], qv[4 * n + i], sc);
+                    } else if constexpr (n < 2 * kS) {
+                        static_for<4>([&](auto i) {
+                            constexpr int step = 4 * (n - kS) + i;
+                            if constexpr (step < 2 * DT) {
+                                dp = mfma(x[i], gv[step], dp);
+#pragma unroll
+                                for (int e = 16 * step / (2 * DT); e < 16 * (step + 1) / (2 * DT); e++)
+                                    sc[e] = exp2_raw(__builtin_fmaf(sc[e], c, -lse2));
+                                __builtin_amdgcn_sched_barrier(0);
+                            }
+                        });
                     } else {
 #pragma unroll
-                        for (int t = 0; t < DT; t++) dq[t] = mfma(x[t], ds[n - DT], dq[t]);
+                        for (int t = 0; t < DT; t++) dq[t] = mfma(x[t], ds[n - 2 * kS], dq[t]);
                     }
-                    if constexpr (n == DT - 1) {
+                    if constexpr (n == 2 * kS - 1) {
 #pragma unroll
-                        for (int i = 0; i < 16; i++) sc[i] = exp2_raw(__builtin_fmaf(sc[i], c, -lse2)) * (dp[i] - delta);
+                        for (int i = 0; i < 16; i++) sc[i] *= dp[i] - delta;
                         if (k0 + 32 * b + 31 > w.all_seen) {
 #pragma unroll
                             for (int i = 0; i < 16; i++)
@@ -616,8 +630,8 @@ __global__ void __launch_bounds__(kThreads, 2) attn_bwd_q_bf16_kernel(AttnArgs a
 // different queries, run through the same tiles at the same time and find them in L2 (from the first on, head by head, they
 // were spread over the sequence, and the backward of 32 x 2,048 tokens took BEFORE ms in place of AFTER).
 // Here a lane's column is a key and the queries run down the accumulators (S = q k^T as it is written): P and dS are the
-// B operands of dv^T = dO^T P and dk^T = q^T dS. Queries and their gradients go through LDS in tiles with their lse and delta;
-// a query that does not exist, or sees nothing, has lse = +inf there and so probability 0.
+// B operands of dv^T = dO^T P and dk^T = q^T dS. Queries and their gradients go through LDS in tiles with their lse and delta,
+// from which the accumulators start; a query that does not exist, or sees nothing, has probability 0.
 // Two waves per SIMD, whose 256 registers hold the sums (64 per gradient and 128 features) and k: from 65 features on, v is read
 // from LDS each time and the tiles have 32 queries rather than 64.
 template <int DT>
@@ -628,7 +642,7 @@ __global__ void __launch_bounds__(kThreads, 2) attn_bwd_kv_bf16_kernel(AttnArgs 
     using GV = Tile<DT>;  // half of the workgroup's 128 keys
     constexpr int kRows = 32 * kWaves;
     __shared__ __attribute__((aligned(16))) char smem[4 * G::kBytes + (kWide ? 2 * GV::kBytes : 0)];  // q, q, dO, dO, v
-    __shared__ __attribute__((aligned(16))) float stats[2][2][kQ];  // [stage][lse log2 e, delta]
+    __shared__ __attribute__((aligned(16))) float stats[2][2][kQ];  // [stage][-lse / scale, -delta]
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5, col = lane & 31;
     const int hk = blockIdx.x % a.Hkv, group = a.Hq / a.Hkv, D = a.D;
     int tile;
@@ -647,7 +661,10 @@ __global__ void __launch_bounds__(kThreads, 2) attn_bwd_kv_bf16_kernel(AttnArgs 
     const int per_head = r.lq > q_first ? (r.lq - q_first + kQ - 1) / kQ : 0;
     const int items = per_head * group, q_last = q_first + (per_head - 1) * kQ;
 
-    const float c = a.scale * kLog2e;
+    // The accumulators of S and dP start from -lse / scale and -delta: exp2(c S') is the probability and P dP' is dS. A
+    // scale too small to divide by does as well as the smallest that is not.
+    const float scale = __builtin_fabsf(a.scale) < 1e-20f ? 1e-20f : a.scale, c = scale * kLog2e;
+    const float nothing = __builtin_copysignf(3e38f, -scale);  // of a query that does not exist or sees nothing: c times it is far below -126
     const int64_t g_stride = (int64_t)a.Hq * D;
     const uint16_t *Q = static_cast<const uint16_t *>(a.q) + r.q0 * a.q_stride + (int64_t)hk * group * D;
     const uint16_t *dO = static_cast<const uint16_t *>(a.dO) + r.q0 * g_stride + (int64_t)hk * group * D;
@@ -677,7 +694,7 @@ __global__ void __launch_bounds__(kThreads, 2) attn_bwd_kv_bf16_kernel(AttnArgs 
         for (int i = 0; i < kStats; i++) {
             const int v = lane + 64 * i;
             const bool in = q0 + v % kQ < r.lq;
-            (&stats[stage][0][0])[v] = v >= kQ ? (in ? sv[i] : 0.0f) : in && sv[i] != kNone ? sv[i] * kLog2e : __builtin_inff();
+            (&stats[stage][0][0])[v] = v >= kQ ? (in ? -sv[i] : 0.0f) : in && sv[i] != kNone ? -sv[i] / scale : nothing;
         }
     };
     bf16x8_t kv[2 * DT], vv[kWide ? 1 : 2 * DT];
@@ -716,7 +733,7 @@ __global__ void __launch_bounds__(kThreads, 2) attn_bwd_kv_bf16_kernel(AttnArgs 
             f32x16_t sc, dp;
             bf16x8_t p[2], ds[2];
             // for each 32 queries: groups of S (two steps of 16 features), of dP (one step where v comes from LDS too),
-            // then dv and dk of 16 queries each in turn (two blocks of 32 features at a time)
+            // then dv and dk of 16 queries each (two blocks of 32 features at a time)
             constexpr int kP = kWide ? 2 * DT : DT, kT = (DT + 1) / 2, kAll = DT + kP + 4 * kT;
             pipelined<kQ / 32 * kAll, 2, 3>(
                 [&](auto g, bf16x8_t (&x)[2]) {
@@ -738,16 +755,27 @@ __global__ void __launch_bounds__(kThreads, 2) attn_bwd_kv_bf16_kernel(AttnArgs 
                         constexpr int m = (n - DT - kP) / kT, t0 = 2 * ((n - DT - kP) % kT);
 #pragma unroll
                         for (int i = 0; i < 2; i++)
-                            if (t0 + i < DT) x[i] = f.transposed((m & 1) ? qt : gt, 2 * b + (m >> 1), t0 + i);
+                            if (t0 + i < DT) x[i] = f.transposed(m >= 2 ? qt : gt, 2 * b + (m & 1), t0 + i);
                     }
                 },
                 [&](auto g, bf16x8_t (&x)[2]) {
                     constexpr int b = g / kAll, n = g % kAll;
-                    if constexpr (n == 0) sc = dp = f32x16_t{};
+                    // an accumulator's start from its rows' statistics
+                    auto start = [&](f32x16_t &acc, int which) {
+#pragma unroll
+                        for (int q = 0; q < 4; q++) {
+                            const f32x4_t v = *reinterpret_cast<const f32x4_t *>(&stats[st][which][32 * b + 8 * q + 4 * half]);
+#pragma unroll
+                            for (int e = 0; e < 4; e++) acc[4 * q + e] = v[e];
+                        }
+                    };
+                    if constexpr (n == 0) start(sc, 0);
+                    if constexpr (n == DT - 1) start(dp, 1);
                     if constexpr (n < DT) {
 #pragma unroll
                         for (int i = 0; i < 2; i++) sc = mfma(x[i], kv[2 * n + i], sc);
                     } else if constexpr (n < DT + kP) {
+                        // the probabilities, 16 / kP after each group
                         constexpr int m = n - DT;
                         if constexpr (kWide) {
                             dp = mfma(x[0], x[1], dp);
@@ -755,38 +783,31 @@ __global__ void __launch_bounds__(kThreads, 2) attn_bwd_kv_bf16_kernel(AttnArgs 
 #pragma unroll
                             for (int i = 0; i < 2; i++) dp = mfma(x[i], vv[2 * m + i], dp);
                         }
+#pragma unroll
+                        for (int e = 16 * m / kP; e < 16 * (m + 1) / kP; e++) sc[e] = exp2_raw(sc[e] * c);
                     } else {
+                        // dS between the instructions of dv, 8 at a time
                         constexpr int m = (n - DT - kP) / kT, t0 = 2 * ((n - DT - kP) % kT);
 #pragma unroll
                         for (int i = 0; i < 2; i++) {
                             if (t0 + i >= DT) continue;
-                            if constexpr (m & 1) dk[t0 + i] = mfma(x[i], ds[m >> 1], dk[t0 + i]);
-                            else dv[t0 + i] = mfma(x[i], p[m >> 1], dv[t0 + i]);
+                            if constexpr (m >= 2) dk[t0 + i] = mfma(x[i], ds[m & 1], dk[t0 + i]);
+                            else dv[t0 + i] = mfma(x[i], p[m & 1], dv[t0 + i]);
+                        }
+                        if constexpr (m < 2 && t0 == 0) {
+#pragma unroll
+                            for (int e = 8 * m; e < 8 * m + 8; e++) dp[e] *= sc[e];
+                            ds[m & 1] = pack8(dp, m & 1);
                         }
                     }
                     if constexpr (n == DT + kP - 1) {
-#pragma unroll
-                        for (int q = 0; q < 4; q++) {
-                            const f32x4_any_t ls = *reinterpret_cast<const f32x4_any_t *>(&stats[st][0][32 * b + 8 * q + 4 * half]);
-                            const f32x4_any_t de = *reinterpret_cast<const f32x4_any_t *>(&stats[st][1][32 * b + 8 * q + 4 * half]);
-#pragma unroll
-                            for (int e = 0; e < 4; e++) {
-                                sc[4 * q + e] = exp2_raw(__builtin_fmaf(sc[4 * q + e], c, -ls[e]));
-                                dp[4 * q + e] -= de[e];
-                            }
-                        }
                         if (q0 + 32 * b < all_from) {
 #pragma unroll
                             for (int i = 0; i < 16; i++)
                                 if (q0 + 32 * b + acc_row(i) + 4 * half < from) sc[i] = dp[i] = 0.0f;
                         }
 #pragma unroll
-                        for (int i = 0; i < 16; i++) dp[i] *= sc[i];
-#pragma unroll
-                        for (int i = 0; i < 2; i++) {
-                            p[i] = pack8(sc, i);
-                            ds[i] = pack8(dp, i);
-                        }
+                        for (int i = 0; i < 2; i++) p[i] = pack8(sc, i);
                     }
                 });
         }
