@@ -116,46 +116,49 @@ struct Frags {
     using G = Tile<DT>;
     uint32_t row;    // straight reads: row lane % 32, chunk lane / 32; chunk 2 s + that of step s at ^ 32 s
     uint32_t tr[2];  // transposing reads: rows 8 e + 4 (lane / 32) .. + 3, features 16 (lane / 16 % 2) .. + 15; 32 t more at ^ 64 t
-    __device__ __forceinline__ void init(int lane) {
+    // `base`: LDS address of the tiles, a multiple of 256
+    __device__ __forceinline__ void init(int lane, uint32_t base) {
         const uint32_t r = lane & 31, h = lane >> 5;
-        row = r * G::kPitch + ((h ^ G::key(r)) << 4);
+        row = base + r * G::kPitch + ((h ^ G::key(r)) << 4);
         const uint32_t j = lane & 15, g = (lane >> 4) & 1;
 #pragma unroll
         for (uint32_t e = 0; e < 2; e++) {
             const uint32_t tr_row = 8 * e + 4 * h + j / 4;
-            tr[e] = tr_row * G::kPitch + (((2 * g + (j % 4) / 2) ^ G::key(tr_row)) << 4) + 8 * (j % 2);
+            tr[e] = base + tr_row * G::kPitch + (((2 * g + (j % 4) / 2) ^ G::key(tr_row)) << 4) + 8 * (j % 2);
         }
     }
     // Keeps the compiler from holding every step's address in a register of its own over a loop: one operation forms
     // each, and the registers are short.
     __device__ __forceinline__ void hold() { asm volatile("" : "+v"(row), "+v"(tr[0]), "+v"(tr[1])); }
-    // A operand: 32 rows from row 32 b on, features 16 s .. 16 s + 15
-    __device__ __forceinline__ bf16x8_t straight(uint32_t tile, int b, int s) const {
-        return *(lds_bf16x8 *)(uintptr_t)((row ^ (uint32_t)(32 * s)) + tile + b * 32 * G::kPitch);
+    // A operand: 32 rows from row 32 b of the tile at byte TILE on, features 16 s .. 16 s + 15
+    template <uint32_t TILE>
+    __device__ __forceinline__ bf16x8_t straight(int b, int s) const {
+        return *(lds_bf16x8 *)(uintptr_t)((row ^ (uint32_t)(32 * s)) + (TILE + b * 32 * G::kPitch));
     }
     // A operand: features 32 t .. 32 t + 31, the 16 rows from 16 s on in accumulator order
-    __device__ __forceinline__ bf16x8_t transposed(uint32_t tile, int s, int t) const {
+    template <uint32_t TILE>
+    __device__ __forceinline__ bf16x8_t transposed(int s, int t) const {
         const i16x4_t v[2] = {
-            __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4 *)(uintptr_t)((tr[0] ^ (uint32_t)(64 * t)) + tile + s * 16 * G::kPitch)),
-            __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4 *)(uintptr_t)((tr[1] ^ (uint32_t)(64 * t)) + tile + s * 16 * G::kPitch))};
+            __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4 *)(uintptr_t)((tr[0] ^ (uint32_t)(64 * t)) + (TILE + s * 16 * G::kPitch))),
+            __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4 *)(uintptr_t)((tr[1] ^ (uint32_t)(64 * t)) + (TILE + s * 16 * G::kPitch)))};
         return __builtin_bit_cast(bf16x8_t, v);
     }
 };
 
-// The same with every address in a register of its own, for tiles at compile-time offsets: no operation per read.
+// The same with every address in a register of its own: no operation per read.
 template <int DT>
 struct Addresses {
     using G = Tile<DT>;
     uint32_t row[2 * DT], tr[2][DT];
     __device__ __forceinline__ void init(int lane, uint32_t base) {
         Frags<DT> f;
-        f.init(lane);
+        f.init(lane, base);
 #pragma unroll
-        for (int s = 0; s < 2 * DT; s++) row[s] = (f.row ^ (uint32_t)(32 * s)) + base;
+        for (int s = 0; s < 2 * DT; s++) row[s] = f.row ^ (uint32_t)(32 * s);
 #pragma unroll
         for (int t = 0; t < DT; t++)
 #pragma unroll
-            for (int e = 0; e < 2; e++) tr[e][t] = (f.tr[e] ^ (uint32_t)(64 * t)) + base;
+            for (int e = 0; e < 2; e++) tr[e][t] = f.tr[e] ^ (uint32_t)(64 * t);
         // from here on they are what they are, not something to be formed again
 #pragma unroll
         for (int s = 0; s < 2 * DT; s++) asm volatile("" : "+v"(row[s]));
@@ -204,6 +207,13 @@ __device__ __forceinline__ void pipelined(Load &&load, Run &&run) {
         run(g, x[g % R]);
         __builtin_amdgcn_sched_barrier(0);
     });
+}
+
+// The lane's number formed again where it is needed, for kernels that have no register to keep it in
+__device__ __forceinline__ int lane_again() {
+    int t = threadIdx.x;
+    asm volatile("" : "+v"(t));
+    return t & 63;
 }
 
 // 8 accumulator registers from 8 s on as a B operand
@@ -282,7 +292,7 @@ struct RowTile {
 template <int DT, bool SPLIT>
 __global__ void __launch_bounds__(kThreads, 2) attn_fwd_bf16_kernel(AttnArgs a, AttnParts parts) {
     using G = Tile<DT>;
-    __shared__ __attribute__((aligned(16))) char smem[4 * G::kBytes];  // K, K, V, V
+    __shared__ __attribute__((aligned(1024))) char smem[4 * G::kBytes];  // K, K, V, V
     constexpr int kRows = 32 * kWaves;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5, col = lane & 31;
     const int hk = blockIdx.x % a.Hkv, group = a.Hq / a.Hkv, D = a.D;
@@ -516,7 +526,7 @@ __global__ void __launch_bounds__(kThreads) attn_join_kernel(AttnArgs a, AttnPar
 template <int DT>
 __global__ void __launch_bounds__(kThreads, 2) attn_bwd_q_bf16_kernel(AttnArgs a) {
     using G = Tile<DT>;
-    __shared__ __attribute__((aligned(16))) char smem[4 * G::kBytes];  // K, K, V, V
+    __shared__ __attribute__((aligned(1024))) char smem[4 * G::kBytes];  // K, K, V, V
     constexpr int kRows = 32 * kWaves;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5, col = lane & 31;
     const int hk = blockIdx.x % a.Hkv, group = a.Hq / a.Hkv, D = a.D;
@@ -549,18 +559,19 @@ __global__ void __launch_bounds__(kThreads, 2) attn_bwd_q_bf16_kernel(AttnArgs a
     Dma<DT> ks, vs;
     ks.init(a.k_stride, wave, lane);
     vs.init(a.v_stride, wave, lane);
-    Frags<DT> f;
-    f.init(lane);
     const uint32_t base = lds_addr(smem);
+    Addresses<DT> f;
+    f.init(lane, base);
     f32x16_t dq[DT] = {};
     if (w.nk > 0) {
         ks.load(K, a.k_stride, 0, r.lk, D, base, wave);
         vs.load(V, a.v_stride, 0, r.lk, D, base + 2 * G::kBytes, wave);
     }
     landed();
-    for (int j = 0; j < w.nk; j++) {
-        const int st = j & 1, k0 = j * kKeys;
-        const uint32_t kt = base + st * G::kBytes, vt = base + (2 + st) * G::kBytes;
+    auto iteration = [&](int j, auto stage) {
+        constexpr int st = decltype(stage)::value;
+        constexpr uint32_t kt = st * G::kBytes, vt = (2 + st) * G::kBytes;
+        const int k0 = j * kKeys;
         const bool more = j + 1 < w.nk, active = k0 <= w.any_seen;
         if (more) {
             ks.load(K, a.k_stride, k0 + kKeys, r.lk, D, base + (st ^ 1) * G::kBytes, wave);
@@ -578,10 +589,10 @@ __global__ void __launch_bounds__(kThreads, 2) attn_bwd_q_bf16_kernel(AttnArgs a
                     if constexpr (n < 2 * kS) {
 #pragma unroll
                         for (int i = 0; i < 4; i++)
-                            if (4 * (n % kS) + i < 2 * DT) x[i] = f.straight(n < kS ? kt : vt, b, 4 * (n % kS) + i);
+                            if (4 * (n % kS) + i < 2 * DT) x[i] = f.template straight<n < kS ? kt : vt>(b, 4 * (n % kS) + i);
                     } else {
 #pragma unroll
-                        for (int t = 0; t < DT; t++) x[t] = f.transposed(kt, 2 * b + n - 2 * kS, t);
+                        for (int t = 0; t < DT; t++) x[t] = f.template transposed<kt>(2 * b + n - 2 * kS, t);
                     }
                 },
                 [&](auto g, bf16x8_t (&x)[4]) {
@@ -621,6 +632,10 @@ __global__ void __launch_bounds__(kThreads, 2) attn_bwd_q_bf16_kernel(AttnArgs a
                 });
         }
         landed();
+    };
+    for (int j = 0; j < w.nk; j += 2) {
+        iteration(j, std::integral_constant<int, 0>{});
+        if (j + 1 < w.nk) iteration(j + 1, std::integral_constant<int, 1>{});
     }
     store_row<DT>(static_cast<uint16_t *>(a.dq) + (r.q0 + w.q) * a.dq_stride + (int64_t)w.h * D, w.ok, D, half, dq, a.scale);
 }
@@ -641,7 +656,7 @@ __global__ void __launch_bounds__(kThreads, 2) attn_bwd_kv_bf16_kernel(AttnArgs 
     using G = Tile<DT, kQ>;
     using GV = Tile<DT>;  // half of the workgroup's 128 keys
     constexpr int kRows = 32 * kWaves;
-    __shared__ __attribute__((aligned(16))) char smem[4 * G::kBytes + (kWide ? 2 * GV::kBytes : 0)];  // q, q, dO, dO, v
+    __shared__ __attribute__((aligned(1024))) char smem[4 * G::kBytes + (kWide ? 2 * GV::kBytes : 0)];  // q, q, dO, dO, v
     __shared__ __attribute__((aligned(16))) float stats[2][2][kQ];  // [stage][-lse / scale, -delta]
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5, col = lane & 31;
     const int hk = blockIdx.x % a.Hkv, group = a.Hq / a.Hkv, D = a.D;
@@ -657,7 +672,7 @@ __global__ void __launch_bounds__(kThreads, 2) attn_bwd_kv_bf16_kernel(AttnArgs 
     // key, of this lane's
     auto seen_from = [&](int key) { return a.causal && key > shift ? key - shift : 0; };
     const int q_first = seen_from(tile * kRows) / kQ * kQ;
-    const int any_from = seen_from(w_first), all_from = seen_from(w_first + 31), from = seen_from(k);
+    const int any_from = seen_from(w_first), all_from = seen_from(w_first + 31);
     const int per_head = r.lq > q_first ? (r.lq - q_first + kQ - 1) / kQ : 0;
     const int items = per_head * group, q_last = q_first + (per_head - 1) * kQ;
 
@@ -673,9 +688,10 @@ __global__ void __launch_bounds__(kThreads, 2) attn_bwd_kv_bf16_kernel(AttnArgs 
     Dma<DT, kQ> qs, gs;
     qs.init(a.q_stride, wave, lane);
     gs.init(g_stride, wave, lane);
+    const uint32_t base = lds_addr(smem);
+    constexpr uint32_t kV = 4 * G::kBytes;
     Frags<DT> f;
-    f.init(lane);
-    const uint32_t base = lds_addr(smem), vt = base + 4 * G::kBytes;
+    f.init(lane, base);
     // lse and delta of a tile's queries: loaded by every wave, without a branch (the values of two paths would be joined, and
     // so waited for, at once), looked at and written by the first when the tile's work is done
     constexpr int kStats = 2 * kQ / 64;
@@ -708,16 +724,16 @@ __global__ void __launch_bounds__(kThreads, 2) attn_bwd_kv_bf16_kernel(AttnArgs 
         if constexpr (kWide) {
             Dma<DT> vs;
             vs.init(a.v_stride, wave, lane);
-            vs.load(V, a.v_stride, tile * kRows, r.lk, D, vt, wave);
-            vs.load(V, a.v_stride, tile * kRows + kKeys, r.lk, D, vt + GV::kBytes, wave);
+            vs.load(V, a.v_stride, tile * kRows, r.lk, D, base + kV, wave);
+            vs.load(V, a.v_stride, tile * kRows + kKeys, r.lk, D, base + kV + GV::kBytes, wave);
         }
         store_stats(0, q_last);
     }
     landed();
     int head = 0, q0 = q_last;
-    for (int it = 0; it < items; it++) {
-        const int st = it & 1;
-        const uint32_t qt = base + st * G::kBytes, gt = base + (2 + st) * G::kBytes;
+    auto iteration = [&](int it, auto stage) {
+        constexpr int st = decltype(stage)::value;
+        constexpr uint32_t qt = st * G::kBytes, gt = (2 + st) * G::kBytes;
         const bool more = it + 1 < items, active = q0 + kQ > any_from;
         int next_head = head + 1, next_q0 = q0;
         if (next_head == group) {
@@ -741,27 +757,28 @@ __global__ void __launch_bounds__(kThreads, 2) attn_bwd_kv_bf16_kernel(AttnArgs 
                     if constexpr (n == 0) f.hold();
                     if constexpr (n < DT) {
 #pragma unroll
-                        for (int i = 0; i < 2; i++) x[i] = f.straight(qt, b, 2 * n + i);
+                        for (int i = 0; i < 2; i++) x[i] = f.template straight<qt>(b, 2 * n + i);
                     } else if constexpr (n < DT + kP) {
                         constexpr int m = n - DT;
                         if constexpr (kWide) {
-                            x[0] = f.straight(gt, b, m);
-                            x[1] = f.straight(vt, wave, m);
+                            x[0] = f.template straight<gt>(b, m);
+                            x[1] = f.template straight<kV>(wave, m);
                         } else {
 #pragma unroll
-                            for (int i = 0; i < 2; i++) x[i] = f.straight(gt, b, 2 * m + i);
+                            for (int i = 0; i < 2; i++) x[i] = f.template straight<gt>(b, 2 * m + i);
                         }
                     } else {
                         constexpr int m = (n - DT - kP) / kT, t0 = 2 * ((n - DT - kP) % kT);
 #pragma unroll
                         for (int i = 0; i < 2; i++)
-                            if (t0 + i < DT) x[i] = f.transposed(m >= 2 ? qt : gt, 2 * b + (m & 1), t0 + i);
+                            if (t0 + i < DT) x[i] = f.template transposed<m >= 2 ? qt : gt>(2 * b + (m & 1), t0 + i);
                     }
                 },
                 [&](auto g, bf16x8_t (&x)[2]) {
                     constexpr int b = g / kAll, n = g % kAll;
                     // an accumulator's start from its rows' statistics
                     auto start = [&](f32x16_t &acc, int which) {
+                        const int half = lane_again() >> 5;
 #pragma unroll
                         for (int q = 0; q < 4; q++) {
                             const f32x4_t v = *reinterpret_cast<const f32x4_t *>(&stats[st][which][32 * b + 8 * q + 4 * half]);
@@ -802,6 +819,7 @@ __global__ void __launch_bounds__(kThreads, 2) attn_bwd_kv_bf16_kernel(AttnArgs 
                     }
                     if constexpr (n == DT + kP - 1) {
                         if (q0 + 32 * b < all_from) {
+                            const int l = lane_again(), from = seen_from(w_first + (l & 31)), half = l >> 5;
 #pragma unroll
                             for (int i = 0; i < 16; i++)
                                 if (q0 + 32 * b + acc_row(i) + 4 * half < from) sc[i] = dp[i] = 0.0f;
@@ -815,6 +833,10 @@ __global__ void __launch_bounds__(kThreads, 2) attn_bwd_kv_bf16_kernel(AttnArgs 
         head = next_head;
         q0 = next_q0;
         landed();
+    };
+    for (int it = 0; it < items; it += 2) {
+        iteration(it, std::integral_constant<int, 0>{});
+        if (it + 1 < items) iteration(it + 1, std::integral_constant<int, 1>{});
     }
     store_row<DT>(static_cast<uint16_t *>(a.dk) + (r.k0 + k) * a.dk_stride + (int64_t)hk * D, ok, D, half, dk, a.scale);
     store_row<DT>(static_cast<uint16_t *>(a.dv) + (r.k0 + k) * a.dv_stride + (int64_t)hk * D, ok, D, half, dv, 1.0f);
