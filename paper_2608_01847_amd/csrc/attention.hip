@@ -36,15 +36,19 @@ __device__ __forceinline__ void store4(uint16_t *p, const float (&v)[4]) {
     *reinterpret_cast<uint2 *>(p) = make_uint2(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]));
 }
 
-// One row's part of a lane: features 8 j + 4 (lane / 32) .. + 3 for every j (zeros where the row or a feature does
-// not exist).
+// Loads are not branched around: what does not exist is loaded from a place that does and replaced by zeros, so that all of
+// a tile's loads are under way together (`row` is a row that exists in every function here).
+
+// One row's part of a lane: features 8 j + 4 (lane / 32) .. + 3 for every j (zeros where !ok or past D).
 template <typename T, int DT>
 __device__ __forceinline__ void load_row(const T *row, bool ok, int D, int half, float (&v)[4 * DT][4]) {
 #pragma unroll
     for (int j = 0; j < 4 * DT; j++) {
         const int d = 8 * j + 4 * half;
-        if (ok && d < D) load4(row + d, v[j]);
-        else v[j][0] = v[j][1] = v[j][2] = v[j][3] = 0.0f;
+        const bool in = ok && d < D;
+        load4(row + (in ? d : 0), v[j]);
+#pragma unroll
+        for (int e = 0; e < 4; e++) v[j][e] = in ? v[j][e] : 0.0f;
     }
 }
 
@@ -52,14 +56,12 @@ __device__ __forceinline__ void load_row(const T *row, bool ok, int D, int half,
 template <typename T, int DT>
 __device__ __forceinline__ f32x16_t row_products(const T *row, bool ok, int D, int half, const float (&b)[4 * DT][4]) {
     f32x16_t acc = {};
+    float v[4 * DT][4];
+    load_row<T, DT>(row, ok, D, half, v);
 #pragma unroll
-    for (int j = 0; j < 4 * DT; j++) {
-        float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-        const int d = 8 * j + 4 * half;
-        if (ok && d < D) load4(row + d, v);
+    for (int j = 0; j < 4 * DT; j++)
 #pragma unroll
-        for (int e = 0; e < 4; e++) acc = __builtin_amdgcn_mfma_f32_32x32x2f32(v[e], b[j][e], acc, 0, 0, 0);
-    }
+        for (int e = 0; e < 4; e++) acc = __builtin_amdgcn_mfma_f32_32x32x2f32(v[j][e], b[j][e], acc, 0, 0, 0);
     return acc;
 }
 
@@ -69,16 +71,22 @@ template <typename T, int DT>
 __device__ __forceinline__ void add_products(f32x16_t (&out)[DT], const T *X, int64_t stride, int n, int D, int lane,
                                              const float (&w)[16]) {
     const int half = lane >> 5, col = lane & 31;
+    float x[16][DT];
 #pragma unroll
     for (int r = 0; r < 16; r++) {
         const int row = acc_row(r) + 4 * half;
 #pragma unroll
         for (int t = 0; t < DT; t++) {
             const int d = 32 * t + col;
-            const float x = row < n && d < D ? load_one(X + row * stride + d) : 0.0f;
-            out[t] = __builtin_amdgcn_mfma_f32_32x32x2f32(x, w[r], out[t], 0, 0, 0);
+            const bool in = row < n && d < D;
+            x[r][t] = load_one(X + (row < n ? row : 0) * stride + (d < D ? d : 0));
+            x[r][t] = in ? x[r][t] : 0.0f;
         }
     }
+#pragma unroll
+    for (int r = 0; r < 16; r++)
+#pragma unroll
+        for (int t = 0; t < DT; t++) out[t] = __builtin_amdgcn_mfma_f32_32x32x2f32(x[r][t], w[r], out[t], 0, 0, 0);
 }
 
 // Adds the four waves' accumulators in wave 0: (0 + 2) + (1 + 3).
@@ -135,7 +143,7 @@ __global__ void __launch_bounds__(kThreads) attn_fwd_kernel(AttnArgs a) {
     const T *K = static_cast<const T *>(a.k) + r.k0 * a.k_stride + (int64_t)hk * D;
     const T *V = static_cast<const T *>(a.v) + r.k0 * a.v_stride + (int64_t)hk * D;
     float qv[4 * DT][4];
-    load_row<T, DT>(static_cast<const T *>(a.q) + (r.q0 + q) * a.q_stride + (int64_t)h * D, q_ok, D, half, qv);
+    load_row<T, DT>(static_cast<const T *>(a.q) + (r.q0 + (q_ok ? q : 0)) * a.q_stride + (int64_t)h * D, q_ok, D, half, qv);
     const float c = a.scale * kLog2e;
     const int q_end = tile * kTile + kTile < r.lq ? tile * kTile + kTile : r.lq;
     const int k_end = a.causal ? (q_end + shift < r.lk ? q_end + shift : r.lk) : r.lk;
@@ -144,7 +152,7 @@ __global__ void __launch_bounds__(kThreads) attn_fwd_kernel(AttnArgs a) {
     float m = -__builtin_inff(), l = 0.0f;
     for (int k0 = wave * kTile; k0 < k_end; k0 += kWaves * kTile) {
         const bool k_ok = k0 + col < r.lk;
-        const f32x16_t acc = row_products<T, DT>(K + (k0 + col) * a.k_stride, k_ok, D, half, qv);
+        const f32x16_t acc = row_products<T, DT>(K + (k_ok ? k0 + col : 0) * a.k_stride, k_ok, D, half, qv);
         float p[16], top = -__builtin_inff();
 #pragma unroll
         for (int i = 0; i < 16; i++) {
@@ -209,7 +217,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_bwd_q_kernel(AttnArgs a) {
     const T *K = static_cast<const T *>(a.k) + r.k0 * a.k_stride + (int64_t)hk * D;
     const T *V = static_cast<const T *>(a.v) + r.k0 * a.v_stride + (int64_t)hk * D;
     float qv[4 * DT][4], gv[4 * DT][4];
-    const int64_t oq = ((r.q0 + q) * a.Hq + h) * D;
+    const int64_t oq = ((r.q0 + (q_ok ? q : 0)) * a.Hq + h) * D;
     float delta = 0.0f;
     load_row<T, DT>(static_cast<const T *>(a.O) + oq, q_ok, D, half, qv);
     load_row<T, DT>(static_cast<const T *>(a.dO) + oq, q_ok, D, half, gv);
@@ -219,7 +227,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_bwd_q_kernel(AttnArgs a) {
         for (int e = 0; e < 4; e++) delta = __builtin_fmaf(qv[j][e], gv[j][e], delta);
     delta += __shfl_xor(delta, 32, 64);
     if (wave == 0 && half == 0 && q_ok) a.delta[(int64_t)h * a.Tq + r.q0 + q] = delta;
-    load_row<T, DT>(static_cast<const T *>(a.q) + (r.q0 + q) * a.q_stride + (int64_t)h * D, q_ok, D, half, qv);
+    load_row<T, DT>(static_cast<const T *>(a.q) + (r.q0 + (q_ok ? q : 0)) * a.q_stride + (int64_t)h * D, q_ok, D, half, qv);
     const float c = a.scale * kLog2e;
     const float lse2 = q_ok ? a.lse[(int64_t)h * a.Tq + r.q0 + q] * kLog2e : 0.0f;
     const int q_end = tile * kTile + kTile < r.lq ? tile * kTile + kTile : r.lq;
@@ -228,8 +236,8 @@ __global__ void __launch_bounds__(kThreads, 1) attn_bwd_q_kernel(AttnArgs a) {
     f32x16_t dq[DT] = {};
     for (int k0 = wave * kTile; k0 < k_end; k0 += kWaves * kTile) {
         const bool k_ok = k0 + col < r.lk;
-        const f32x16_t sc = row_products<T, DT>(K + (k0 + col) * a.k_stride, k_ok, D, half, qv);
-        const f32x16_t dp = row_products<T, DT>(V + (k0 + col) * a.v_stride, k_ok, D, half, gv);
+        const f32x16_t sc = row_products<T, DT>(K + (k_ok ? k0 + col : 0) * a.k_stride, k_ok, D, half, qv);
+        const f32x16_t dp = row_products<T, DT>(V + (k_ok ? k0 + col : 0) * a.v_stride, k_ok, D, half, gv);
         float ds[16];
 #pragma unroll
         for (int i = 0; i < 16; i++)
@@ -256,8 +264,8 @@ __global__ void __launch_bounds__(kThreads, 1) attn_bwd_kv_kernel(AttnArgs a) {
     const int k = tile * kTile + col, shift = r.lk - r.lq;
     const bool k_ok = k < r.lk;
     float kv[4 * DT][4], vv[4 * DT][4];
-    load_row<T, DT>(static_cast<const T *>(a.k) + (r.k0 + k) * a.k_stride + (int64_t)hk * D, k_ok, D, half, kv);
-    load_row<T, DT>(static_cast<const T *>(a.v) + (r.k0 + k) * a.v_stride + (int64_t)hk * D, k_ok, D, half, vv);
+    load_row<T, DT>(static_cast<const T *>(a.k) + (r.k0 + (k_ok ? k : 0)) * a.k_stride + (int64_t)hk * D, k_ok, D, half, kv);
+    load_row<T, DT>(static_cast<const T *>(a.v) + (r.k0 + (k_ok ? k : 0)) * a.v_stride + (int64_t)hk * D, k_ok, D, half, vv);
     const float c = a.scale * kLog2e;
     // first query that sees this tile's first key, and this lane's key
     const int q_first = a.causal && tile * kTile - shift > 0 ? (tile * kTile - shift) / kTile * kTile : 0;
@@ -270,8 +278,8 @@ __global__ void __launch_bounds__(kThreads, 1) attn_bwd_kv_kernel(AttnArgs a) {
         const T *G = static_cast<const T *>(a.dO) + ((r.q0 + q0) * a.Hq + h) * D;
         const int64_t g_stride = (int64_t)a.Hq * D, at = (int64_t)h * a.Tq + r.q0 + q0;
         const int n = r.lq - q0;
-        const f32x16_t sc = row_products<T, DT>(Q + col * a.q_stride, col < n, D, half, kv);
-        const f32x16_t dp = row_products<T, DT>(G + col * g_stride, col < n, D, half, vv);
+        const f32x16_t sc = row_products<T, DT>(Q + (col < n ? col : 0) * a.q_stride, col < n, D, half, kv);
+        const f32x16_t dp = row_products<T, DT>(G + (col < n ? col : 0) * g_stride, col < n, D, half, vv);
         float p[16], ds[16];
 #pragma unroll
         for (int i = 0; i < 16; i++) {
@@ -326,8 +334,13 @@ size_t attn_fwd_ws(int64_t Tq, int64_t Tk, int Hq, int Hkv, int D, int64_t n_seq
     return kWsHeader + attn_part_stats(splits, Tq * Hq) + (size_t)splits * (size_t)(Tq * Hq) * (size_t)D * sizeof(float);
 }
 
-size_t attn_bwd_ws(int64_t Tq, int64_t, int Hq, int, int, int64_t) {
-    return kWsHeader + (size_t)Tq * (size_t)Hq * sizeof(float);
+static size_t delta_bytes(int64_t Tq, int Hq) { return ((size_t)Tq * (size_t)Hq * sizeof(float) + 255) / 256 * 256; }
+
+size_t attn_bwd_ws(int64_t Tq, int64_t Tk, int Hq, int Hkv, int D, int64_t n_seq) {
+    const AttnBwdPlan p = plan_attn_bwd_bf16(Tq, Tk, Hq, Hkv, n_seq);
+    const size_t dq = p.q_splits > 1 ? (size_t)p.q_splits * (size_t)Tq * (size_t)Hq : 0;
+    const size_t dkv = p.k_splits > 1 ? (size_t)p.k_splits * (size_t)Tk * (size_t)Hkv * 2 : 0;
+    return kWsHeader + delta_bytes(Tq, Hq) + (dq + dkv) * (size_t)D * sizeof(float);
 }
 
 hipError_t launch_attn_fwd(int dtype, const AttnArgs &a, void *ws, hipStream_t st) {
@@ -336,7 +349,8 @@ hipError_t launch_attn_fwd(int dtype, const AttnArgs &a, void *ws, hipStream_t s
 
 hipError_t launch_attn_bwd(int dtype, AttnArgs a, void *ws, hipStream_t st) {
     a.delta = reinterpret_cast<float *>(static_cast<char *>(ws) + kWsHeader);
-    return dtype == kBF16 ? launch_attn_bwd_bf16(a, st) : bwd<float>(a, st);
+    if (dtype != kBF16) return bwd<float>(a, st);
+    return launch_attn_bwd_bf16(a, reinterpret_cast<float *>(static_cast<char *>(ws) + kWsHeader + delta_bytes(a.Tq, a.Hq)), st);
 }
 
 }  // namespace focus

@@ -27,6 +27,8 @@ typedef __attribute__((address_space(3))) u32x4_t lds_u32x4;
 constexpr int kWaves = 4;
 constexpr int kThreads = 64 * kWaves;
 constexpr int kKeys = 64;   // rows of a staged tile
+constexpr int64_t kBwdWgs = 2048;  // workgroups that a backward launch is split for
+constexpr int64_t kBwdSplits = 16;
 constexpr float kNone = -__builtin_inff();
 
 // Geometry of a staged tile of ROWS rows: DT x 32 features, a row of 128 (DT <= 2) or 256 bytes. 16-byte chunk c of row r
@@ -254,6 +256,18 @@ __device__ __forceinline__ void store_row(uint16_t *row, bool ok, int D, int hal
         }
 }
 
+// The same unscaled and in fp32, into a part of a split sum
+template <int DT>
+__device__ __forceinline__ void store_part(float *row, bool ok, int D, int half, const f32x16_t (&acc)[DT]) {
+#pragma unroll
+    for (int t = 0; t < DT; t++)
+#pragma unroll
+        for (int g = 0; g < 4; g++) {
+            const int d = 32 * t + 8 * g + 4 * half;
+            if (ok && d < D) *reinterpret_cast<f32x4_t *>(row + d) = f32x4_t{acc[t][4 * g], acc[t][4 * g + 1], acc[t][4 * g + 2], acc[t][4 * g + 3]};
+        }
+}
+
 // What a wave's lane does in the kernels whose columns are query rows: its row, and the keys that it, its wave and its
 // workgroup see.
 struct RowTile {
@@ -458,15 +472,7 @@ __global__ void __launch_bounds__(kThreads, 2) attn_fwd_bf16_kernel(AttnArgs a, 
             parts.l[at] = l;
         }
         if (l == 0.0f) return;  // the join does not look at this part's output
-#pragma unroll
-        for (int t = 0; t < DT; t++)
-#pragma unroll
-            for (int g = 0; g < 4; g++) {
-                const int d = 32 * t + 8 * g + 4 * half;
-                if (ok && d < D)
-                    *reinterpret_cast<float4 *>(parts.o + at * D + d) =
-                        make_float4(o[t][4 * g], o[t][4 * g + 1], o[t][4 * g + 2], o[t][4 * g + 3]);
-            }
+        store_part<DT>(parts.o + at * D, ok, D, half, o);
         return;
     }
     // no key seen: zeros and -inf; a NaN among the scores stays one
@@ -523,8 +529,9 @@ __global__ void __launch_bounds__(kThreads) attn_join_kernel(AttnArgs a, AttnPar
 
 // dq of 128 query rows, and delta = rowsum(dO O) for the keys' pass. Both score-shaped products are transposed as in the
 // forward, so dS is the B operand of dq^T = k^T dS^T as it stands.
-template <int DT>
-__global__ void __launch_bounds__(kThreads, 2) attn_bwd_q_bf16_kernel(AttnArgs a) {
+// SPLIT: the tiles of keys are dealt to gridDim.y workgroups, whose sums attn_grad_join_kernel adds.
+template <int DT, bool SPLIT>
+__global__ void __launch_bounds__(kThreads, 2) attn_bwd_q_bf16_kernel(AttnArgs a, AttnGradParts parts) {
     using G = Tile<DT>;
     __shared__ __attribute__((aligned(1024))) char smem[4 * G::kBytes];  // K, K, V, V
     constexpr int kRows = 32 * kWaves;
@@ -549,7 +556,7 @@ __global__ void __launch_bounds__(kThreads, 2) attn_bwd_q_bf16_kernel(AttnArgs a
 #pragma unroll
         for (int e = 0; e < 8; e++) delta = __builtin_fmaf((float)qv[i][e], (float)gv[i][e], delta);
     delta = sum_halves(delta);
-    if (w.ok && half == 0) a.delta[stat] = delta;
+    if (w.ok && half == 0 && blockIdx.y == 0) a.delta[stat] = delta;
     load_row<DT>(static_cast<const uint16_t *>(a.q) + (r.q0 + w.q) * a.q_stride + (int64_t)w.h * D, w.ok, D, half, qv);
     const float c = a.scale * kLog2e;
     const float lse2 = w.ok ? a.lse[stat] * kLog2e : 0.0f;
@@ -563,16 +570,18 @@ __global__ void __launch_bounds__(kThreads, 2) attn_bwd_q_bf16_kernel(AttnArgs a
     Addresses<DT> f;
     f.init(lane, base);
     f32x16_t dq[DT] = {};
-    if (w.nk > 0) {
-        ks.load(K, a.k_stride, 0, r.lk, D, base, wave);
-        vs.load(V, a.v_stride, 0, r.lk, D, base + 2 * G::kBytes, wave);
+    const int per = SPLIT ? (w.nk + (int)gridDim.y - 1) / (int)gridDim.y : w.nk;
+    const int j0 = SPLIT ? (int)blockIdx.y * per : 0, nk = SPLIT && j0 + per < w.nk ? j0 + per : w.nk;  // tiles j0 .. nk - 1
+    if (j0 < nk) {
+        ks.load(K, a.k_stride, j0 * kKeys, r.lk, D, base, wave);
+        vs.load(V, a.v_stride, j0 * kKeys, r.lk, D, base + 2 * G::kBytes, wave);
     }
     landed();
     auto iteration = [&](int j, auto stage) {
         constexpr int st = decltype(stage)::value;
         constexpr uint32_t kt = st * G::kBytes, vt = (2 + st) * G::kBytes;
         const int k0 = j * kKeys;
-        const bool more = j + 1 < w.nk, active = k0 <= w.any_seen;
+        const bool more = j + 1 < nk, active = k0 <= w.any_seen;
         if (more) {
             ks.load(K, a.k_stride, k0 + kKeys, r.lk, D, base + (st ^ 1) * G::kBytes, wave);
             vs.load(V, a.v_stride, k0 + kKeys, r.lk, D, base + (2 + (st ^ 1)) * G::kBytes, wave);
@@ -633,9 +642,13 @@ __global__ void __launch_bounds__(kThreads, 2) attn_bwd_q_bf16_kernel(AttnArgs a
         }
         landed();
     };
-    for (int j = 0; j < w.nk; j += 2) {
+    for (int j = j0; j < nk; j += 2) {
         iteration(j, std::integral_constant<int, 0>{});
-        if (j + 1 < w.nk) iteration(j + 1, std::integral_constant<int, 1>{});
+        if (j + 1 < nk) iteration(j + 1, std::integral_constant<int, 1>{});
+    }
+    if constexpr (SPLIT) {
+        store_part<DT>(parts.dq + (((int64_t)blockIdx.y * a.Tq + r.q0 + w.q) * a.Hq + w.h) * D, w.ok, D, half, dq);
+        return;
     }
     store_row<DT>(static_cast<uint16_t *>(a.dq) + (r.q0 + w.q) * a.dq_stride + (int64_t)w.h * D, w.ok, D, half, dq, a.scale);
 }
@@ -649,8 +662,9 @@ __global__ void __launch_bounds__(kThreads, 2) attn_bwd_q_bf16_kernel(AttnArgs a
 // from which the accumulators start; a query that does not exist, or sees nothing, has probability 0.
 // Two waves per SIMD, whose 256 registers hold the sums (64 per gradient and 128 features) and k: from 65 features on, v is read
 // from LDS each time and the tiles have 32 queries rather than 64.
-template <int DT>
-__global__ void __launch_bounds__(kThreads, 2) attn_bwd_kv_bf16_kernel(AttnArgs a) {
+// SPLIT: the tiles of queries, all heads together, are dealt to gridDim.y workgroups, whose sums attn_grad_join_kernel adds.
+template <int DT, bool SPLIT>
+__global__ void __launch_bounds__(kThreads, 2) attn_bwd_kv_bf16_kernel(AttnArgs a, AttnGradParts parts) {
     constexpr bool kWide = DT > 2;
     constexpr int kQ = kWide ? 32 : 64;  // queries of a tile
     using G = Tile<DT, kQ>;
@@ -674,7 +688,10 @@ __global__ void __launch_bounds__(kThreads, 2) attn_bwd_kv_bf16_kernel(AttnArgs 
     const int q_first = seen_from(tile * kRows) / kQ * kQ;
     const int any_from = seen_from(w_first), all_from = seen_from(w_first + 31);
     const int per_head = r.lq > q_first ? (r.lq - q_first + kQ - 1) / kQ : 0;
-    const int items = per_head * group, q_last = q_first + (per_head - 1) * kQ;
+    const int all_items = per_head * group;
+    const int per = SPLIT ? (all_items + (int)gridDim.y - 1) / (int)gridDim.y : all_items, i0 = SPLIT ? (int)blockIdx.y * per : 0;
+    const int items = i0 + per < all_items ? per : all_items - i0;  // this workgroup's, none or fewer possibly
+    const int head0 = i0 % group, q_start = q_first + (per_head - 1 - i0 / group) * kQ;
 
     // The accumulators of S and dP start from -lse / scale and -delta: exp2(c S') is the probability and P dP' is dS. A
     // scale too small to divide by does as well as the smallest that is not.
@@ -718,19 +735,19 @@ __global__ void __launch_bounds__(kThreads, 2) attn_bwd_kv_bf16_kernel(AttnArgs 
     if constexpr (!kWide) load_row<DT>(V + k * a.v_stride, ok, D, half, vv);
     f32x16_t dk[DT] = {}, dv[DT] = {};
     if (items > 0) {
-        load_stats(0, q_last);
-        qs.load(Q, a.q_stride, q_last, r.lq, D, base, wave);
-        gs.load(dO, g_stride, q_last, r.lq, D, base + 2 * G::kBytes, wave);
+        load_stats(head0, q_start);
+        qs.load(Q + (int64_t)head0 * D, a.q_stride, q_start, r.lq, D, base, wave);
+        gs.load(dO + (int64_t)head0 * D, g_stride, q_start, r.lq, D, base + 2 * G::kBytes, wave);
         if constexpr (kWide) {
             Dma<DT> vs;
             vs.init(a.v_stride, wave, lane);
             vs.load(V, a.v_stride, tile * kRows, r.lk, D, base + kV, wave);
             vs.load(V, a.v_stride, tile * kRows + kKeys, r.lk, D, base + kV + GV::kBytes, wave);
         }
-        store_stats(0, q_last);
+        store_stats(0, q_start);
     }
     landed();
-    int head = 0, q0 = q_last;
+    int head = head0, q0 = q_start;
     auto iteration = [&](int it, auto stage) {
         constexpr int st = decltype(stage)::value;
         constexpr uint32_t qt = st * G::kBytes, gt = (2 + st) * G::kBytes;
@@ -838,8 +855,39 @@ __global__ void __launch_bounds__(kThreads, 2) attn_bwd_kv_bf16_kernel(AttnArgs 
         iteration(it, std::integral_constant<int, 0>{});
         if (it + 1 < items) iteration(it + 1, std::integral_constant<int, 1>{});
     }
+    if constexpr (SPLIT) {
+        const int64_t at = (((int64_t)blockIdx.y * a.Tk + r.k0 + k) * a.Hkv + hk) * D;
+        store_part<DT>(parts.dk + at, ok, D, half, dk);
+        store_part<DT>(parts.dv + at, ok, D, half, dv);
+        return;
+    }
     store_row<DT>(static_cast<uint16_t *>(a.dk) + (r.k0 + k) * a.dk_stride + (int64_t)hk * D, ok, D, half, dk, a.scale);
     store_row<DT>(static_cast<uint16_t *>(a.dv) + (r.k0 + k) * a.dv_stride + (int64_t)hk * D, ok, D, half, dv, 1.0f);
+}
+
+// Adds the parts of a gradient [tokens][heads][D] in order, four features per thread, and rounds the sum times `scale`.
+// cu: ends of the sequences, whose tokens alone have parts
+__global__ void __launch_bounds__(256) attn_grad_join_kernel(const float *part, int splits, int64_t tokens, int heads, int D,
+                                                             const int32_t *cu, int n_seq, uint16_t *out, int64_t stride,
+                                                             float scale) {
+    const int64_t row = (int64_t)heads * D, all = tokens * row;
+    const int64_t at = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4;
+    if (at >= all) return;
+    const int64_t token = at / row;
+    if (cu && (token < cu[0] || token >= cu[n_seq])) return;
+    f32x4_t sum = {};
+    for (int s0 = 0; s0 < splits; s0 += 4) {
+        f32x4_t v[4];
+#pragma unroll
+        for (int i = 0; i < 4; i++)
+            v[i] = s0 + i < splits ? *reinterpret_cast<const f32x4_t *>(part + (s0 + i) * all + at) : f32x4_t{};
+#pragma unroll
+        for (int i = 0; i < 4; i++)
+#pragma unroll
+            for (int e = 0; e < 4; e++) sum[e] += v[i][e];
+    }
+    *reinterpret_cast<uint2 *>(out + token * stride + (at - token * row)) =
+        make_uint2(pack_bf16(sum[0] * scale, sum[1] * scale), pack_bf16(sum[2] * scale, sum[3] * scale));
 }
 
 template <typename F>
@@ -880,14 +928,46 @@ hipError_t launch_attn_fwd_bf16(const AttnArgs &a, void *ws, hipStream_t st) {
     return hipGetLastError();
 }
 
-hipError_t launch_attn_bwd_bf16(const AttnArgs &a, hipStream_t st) {
+// Parts of a backward's sums. One workgroup's run through all queries (keys) of a long sequence is the whole call's
+// time where there are few of them, so they are split until there are kBwdWgs, each with 8 tiles at least by the mean length.
+AttnBwdPlan plan_attn_bwd_bf16(int64_t Tq, int64_t Tk, int Hq, int Hkv, int64_t n_seq) {
+    constexpr int64_t kRows = 32 * kWaves;
+    if (n_seq < 1) return {1, 1};
+    const int64_t q_wgs = (Tq * (Hq / Hkv) / kRows + n_seq) * Hkv, k_wgs = (Tk / kRows + n_seq) * Hkv;
+    const int64_t q_most = Tk / n_seq / kKeys / 8, k_most = Tq / n_seq * (Hq / Hkv) / 32 / 8;
+    auto pick = [](int64_t wgs, int64_t most) {
+        return (int)std::max<int64_t>(1, std::min<int64_t>({kBwdWgs / wgs, most, kBwdSplits}));
+    };
+    return {pick(q_wgs, q_most), pick(k_wgs, k_most)};
+}
+
+hipError_t launch_attn_bwd_bf16(const AttnArgs &a, float *parts, hipStream_t st) {
     constexpr int kRows = 32 * kWaves;
     const int64_t q_slots = a.Tq * (a.Hq / a.Hkv) / kRows + a.n_seq, k_slots = a.Tk / kRows + a.n_seq;
+    const AttnBwdPlan p = plan_attn_bwd_bf16(a.Tq, a.Tk, a.Hq, a.Hkv, a.n_seq);
+    const int64_t dq_size = a.Tq * a.Hq * a.D, dk_size = a.Tk * a.Hkv * a.D;
+    AttnGradParts g{};
+    g.dq = parts;
+    g.dk = parts + (p.q_splits > 1 ? p.q_splits * dq_size : 0);
+    g.dv = g.dk + p.k_splits * dk_size;
+    const dim3 q_grid((unsigned)(q_slots * a.Hkv), (unsigned)p.q_splits), k_grid((unsigned)(k_slots * a.Hkv), (unsigned)p.k_splits);
     pick_dt(a.D, [&](auto dt) {
         constexpr int DT = decltype(dt)::value;
-        if (a.Tq > 0) attn_bwd_q_bf16_kernel<DT><<<(unsigned)(q_slots * a.Hkv), kThreads, 0, st>>>(a);
-        if (a.Tk > 0) attn_bwd_kv_bf16_kernel<DT><<<(unsigned)(k_slots * a.Hkv), kThreads, 0, st>>>(a);
+        if (a.Tq > 0 && p.q_splits > 1) attn_bwd_q_bf16_kernel<DT, true><<<q_grid, kThreads, 0, st>>>(a, g);
+        else if (a.Tq > 0) attn_bwd_q_bf16_kernel<DT, false><<<q_grid, kThreads, 0, st>>>(a, g);
+        if (a.Tk > 0 && p.k_splits > 1) attn_bwd_kv_bf16_kernel<DT, true><<<k_grid, kThreads, 0, st>>>(a, g);
+        else if (a.Tk > 0) attn_bwd_kv_bf16_kernel<DT, false><<<k_grid, kThreads, 0, st>>>(a, g);
     });
+    auto add = [&](const float *part, int splits, int64_t tokens, int heads, const int32_t *cu, void *out, int64_t stride, float scale) {
+        const int64_t threads = tokens * heads * a.D / 4;
+        attn_grad_join_kernel<<<(unsigned)((threads + 255) / 256), 256, 0, st>>>(part, splits, tokens, heads, a.D, cu, a.n_seq,
+                                                                                static_cast<uint16_t *>(out), stride, scale);
+    };
+    if (a.Tq > 0 && p.q_splits > 1) add(g.dq, p.q_splits, a.Tq, a.Hq, a.cu_q, a.dq, a.dq_stride, a.scale);
+    if (a.Tk > 0 && p.k_splits > 1) {
+        add(g.dk, p.k_splits, a.Tk, a.Hkv, a.cu_k, a.dk, a.dk_stride, a.scale);
+        add(g.dv, p.k_splits, a.Tk, a.Hkv, a.cu_k, a.dv, a.dv_stride, 1.0f);
+    }
     return hipGetLastError();
 }
 

@@ -78,10 +78,18 @@ __device__ __forceinline__ constexpr int acc_row(int r) { return (r & 3) + 8 * (
 struct AttnParts {
     float *m, *l, *o;
 };
+// Gradients of a backward whose sums are split, fp32: dq [splits][Tq][Hq][D], dk and dv [splits][Tk][Hkv][D]
+struct AttnGradParts {
+    float *dq, *dk, *dv;
+};
+struct AttnBwdPlan {
+    int q_splits, k_splits;
+};
+AttnBwdPlan plan_attn_bwd_bf16(int64_t Tq, int64_t Tk, int Hq, int Hkv, int64_t n_seq);
 // bytes of m and l, rounded to keep o aligned
 inline size_t attn_part_stats(int splits, int64_t rows) { return ((size_t)splits * (size_t)rows * 8 + 255) / 256 * 256; }
 int attn_splits_bf16(int64_t Tq, int64_t Tk, int Hq, int Hkv, int64_t n_seq);
 hipError_t launch_attn_fwd_bf16(const AttnArgs &a, void *ws, hipStream_t st);
-hipError_t launch_attn_bwd_bf16(const AttnArgs &a, hipStream_t st);
+hipError_t launch_attn_bwd_bf16(const AttnArgs &a, float *parts, hipStream_t st);
 
 }  // namespace focus
