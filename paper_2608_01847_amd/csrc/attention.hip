@@ -1,4 +1,5 @@
-// Attention over whole prompts on the fp32 matrix instructions (v_mfma_f32_32x32x2_f32), forward and backward.
+// Attention over whole prompts in fp32 (v_mfma_f32_32x32x2_f32), forward and backward, and the choice between it and the
+// bf16 kernels.
 //
 //   S = scale q k^T (causal: keys past the query's own place hidden, the last query at the last key),
 //   P = softmax(S), O = P v, lse = log sum exp S
@@ -24,24 +25,16 @@ __device__ __forceinline__ void load4(const float *p, float (&v)[4]) {
     const float4 w = *reinterpret_cast<const float4 *>(p);
     v[0] = w.x, v[1] = w.y, v[2] = w.z, v[3] = w.w;
 }
-__device__ __forceinline__ void load4(const uint16_t *p, float (&v)[4]) {
-    const uint2 w = *reinterpret_cast<const uint2 *>(p);
-    unpack_bf16(w.x, v[0], v[1]);
-    unpack_bf16(w.y, v[2], v[3]);
-}
 __device__ __forceinline__ void store4(float *p, const float (&v)[4]) {
     *reinterpret_cast<float4 *>(p) = make_float4(v[0], v[1], v[2], v[3]);
-}
-__device__ __forceinline__ void store4(uint16_t *p, const float (&v)[4]) {
-    *reinterpret_cast<uint2 *>(p) = make_uint2(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]));
 }
 
 // Loads are not branched around: what does not exist is loaded from a place that does and replaced by zeros, so that all of
 // a tile's loads are under way together (`row` is a row that exists in every function here).
 
 // One row's part of a lane: features 8 j + 4 (lane / 32) .. + 3 for every j (zeros where !ok or past D).
-template <typename T, int DT>
-__device__ __forceinline__ void load_row(const T *row, bool ok, int D, int half, float (&v)[4 * DT][4]) {
+template <int DT>
+__device__ __forceinline__ void load_row(const float *row, bool ok, int D, int half, float (&v)[4 * DT][4]) {
 #pragma unroll
     for (int j = 0; j < 4 * DT; j++) {
         const int d = 8 * j + 4 * half;
@@ -52,42 +45,44 @@ __device__ __forceinline__ void load_row(const T *row, bool ok, int D, int half,
     }
 }
 
-// 32 x 32 products of 32 rows at `row` (this lane's) with the 32 rows held in b
-template <typename T, int DT>
-__device__ __forceinline__ f32x16_t row_products(const T *row, bool ok, int D, int half, const float (&b)[4 * DT][4]) {
+// 32 x 32 products of the 32 rows in a (rows of the result) with those in b (columns)
+template <int DT>
+__device__ __forceinline__ f32x16_t row_products(const float (&a)[4 * DT][4], const float (&b)[4 * DT][4]) {
     f32x16_t acc = {};
-    float v[4 * DT][4];
-    load_row<T, DT>(row, ok, D, half, v);
 #pragma unroll
     for (int j = 0; j < 4 * DT; j++)
 #pragma unroll
-        for (int e = 0; e < 4; e++) acc = __builtin_amdgcn_mfma_f32_32x32x2f32(v[j][e], b[j][e], acc, 0, 0, 0);
+        for (int e = 0; e < 4; e++) acc = __builtin_amdgcn_mfma_f32_32x32x2f32(a[j][e], b[j][e], acc, 0, 0, 0);
     return acc;
 }
 
-// out^T[d][column] += sum over 32 rows of X[row][d] w[row][column], w in accumulator layout; row r0 + i exists for
-// i < n
-template <typename T, int DT>
-__device__ __forceinline__ void add_products(f32x16_t (&out)[DT], const T *X, int64_t stride, int n, int D, int lane,
-                                             const float (&w)[16]) {
+// A lane's features d = 32 t + lane % 32 of the 32 rows of an accumulator's registers; row i exists for i < n
+template <int DT>
+__device__ __forceinline__ void load_columns(const float *X, int64_t stride, int n, int D, int lane, float (&x)[16][DT]) {
     const int half = lane >> 5, col = lane & 31;
-    float x[16][DT];
 #pragma unroll
     for (int r = 0; r < 16; r++) {
         const int row = acc_row(r) + 4 * half;
 #pragma unroll
         for (int t = 0; t < DT; t++) {
             const int d = 32 * t + col;
-            const bool in = row < n && d < D;
-            x[r][t] = load_one(X + (row < n ? row : 0) * stride + (d < D ? d : 0));
-            x[r][t] = in ? x[r][t] : 0.0f;
+            x[r][t] = X[(row < n ? row : 0) * stride + (d < D ? d : 0)];
+            x[r][t] = row < n && d < D ? x[r][t] : 0.0f;
         }
     }
+}
+
+// out^T[d][column] += sum over 32 rows of x[row][d] w[row][column], w in accumulator layout
+template <int DT>
+__device__ __forceinline__ void add_products(f32x16_t (&out)[DT], const float (&x)[16][DT], const float (&w)[16]) {
 #pragma unroll
     for (int r = 0; r < 16; r++)
 #pragma unroll
         for (int t = 0; t < DT; t++) out[t] = __builtin_amdgcn_mfma_f32_32x32x2f32(x[r][t], w[r], out[t], 0, 0, 0);
 }
+
+// Everything loaded for a tile is under way before the first product, which the compiler would otherwise put off load by load
+__device__ __forceinline__ void loads_first() { __builtin_amdgcn_sched_barrier(0); }
 
 // Adds the four waves' accumulators in wave 0: (0 + 2) + (1 + 3).
 template <int DT>
@@ -112,8 +107,8 @@ __device__ __forceinline__ void join(f32x16_t (&acc)[DT], float *lds, int wave, 
 }
 
 // out^T of one lane's column to its row, times `f`
-template <typename T, int DT>
-__device__ __forceinline__ void store_column(T *row, int D, int half, const f32x16_t (&acc)[DT], float f) {
+template <int DT>
+__device__ __forceinline__ void store_column(float *row, int D, int half, const f32x16_t (&acc)[DT], float f) {
 #pragma unroll
     for (int t = 0; t < DT; t++)
 #pragma unroll
@@ -126,8 +121,8 @@ __device__ __forceinline__ void store_column(T *row, int D, int half, const f32x
         }
 }
 
-template <typename T, int DT>
-__global__ void __launch_bounds__(kThreads) attn_fwd_kernel(AttnArgs a) {
+template <int DT>
+__global__ void __launch_bounds__(kThreads, 1) attn_fwd_kernel(AttnArgs a) {
     __shared__ float lds[2 * DT * 16 * 64];
     __shared__ float stat[2][kWaves][32];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5, col = lane & 31;
@@ -140,10 +135,10 @@ __global__ void __launch_bounds__(kThreads) attn_fwd_kernel(AttnArgs a) {
     const int h = blockIdx.y, hk = h / (a.Hq / a.Hkv), D = a.D;
     const int q = tile * kTile + col, shift = r.lk - r.lq;
     const bool q_ok = q < r.lq;
-    const T *K = static_cast<const T *>(a.k) + r.k0 * a.k_stride + (int64_t)hk * D;
-    const T *V = static_cast<const T *>(a.v) + r.k0 * a.v_stride + (int64_t)hk * D;
+    const float *K = static_cast<const float *>(a.k) + r.k0 * a.k_stride + (int64_t)hk * D;
+    const float *V = static_cast<const float *>(a.v) + r.k0 * a.v_stride + (int64_t)hk * D;
     float qv[4 * DT][4];
-    load_row<T, DT>(static_cast<const T *>(a.q) + (r.q0 + (q_ok ? q : 0)) * a.q_stride + (int64_t)h * D, q_ok, D, half, qv);
+    load_row<DT>(static_cast<const float *>(a.q) + (r.q0 + (q_ok ? q : 0)) * a.q_stride + (int64_t)h * D, q_ok, D, half, qv);
     const float c = a.scale * kLog2e;
     const int q_end = tile * kTile + kTile < r.lq ? tile * kTile + kTile : r.lq;
     const int k_end = a.causal ? (q_end + shift < r.lk ? q_end + shift : r.lk) : r.lk;
@@ -152,7 +147,11 @@ __global__ void __launch_bounds__(kThreads) attn_fwd_kernel(AttnArgs a) {
     float m = -__builtin_inff(), l = 0.0f;
     for (int k0 = wave * kTile; k0 < k_end; k0 += kWaves * kTile) {
         const bool k_ok = k0 + col < r.lk;
-        const f32x16_t acc = row_products<T, DT>(K + (k_ok ? k0 + col : 0) * a.k_stride, k_ok, D, half, qv);
+        float kv[4 * DT][4], vx[16][DT];
+        load_row<DT>(K + (k_ok ? k0 + col : 0) * a.k_stride, k_ok, D, half, kv);
+        load_columns<DT>(V + k0 * a.v_stride, a.v_stride, r.lk - k0, D, lane, vx);
+        loads_first();
+        const f32x16_t acc = row_products<DT>(kv, qv);
         float p[16], top = -__builtin_inff();
 #pragma unroll
         for (int i = 0; i < 16; i++) {
@@ -174,7 +173,7 @@ __global__ void __launch_bounds__(kThreads) attn_fwd_kernel(AttnArgs a) {
         for (int t = 0; t < DT; t++)
 #pragma unroll
             for (int i = 0; i < 16; i++) o[t][i] *= alpha;
-        add_products<T, DT>(o, V + k0 * a.v_stride, a.v_stride, r.lk - k0, D, lane, p);
+        add_products<DT>(o, vx, p);
     }
     l += __shfl_xor(l, 32, 64);
     if (half == 0) {
@@ -196,12 +195,12 @@ __global__ void __launch_bounds__(kThreads) attn_fwd_kernel(AttnArgs a) {
     join<DT>(o, lds, wave, lane);
     if (wave != 0 || !q_ok) return;
     const float inv = total > 0.0f ? 1.0f / total : (total == 0.0f ? 0.0f : total);
-    store_column<T, DT>(static_cast<T *>(a.O) + ((r.q0 + q) * a.Hq + h) * D, D, half, o, inv);
+    store_column<DT>(static_cast<float *>(a.O) + ((r.q0 + q) * a.Hq + h) * D, D, half, o, inv);
     if (a.lse && half == 0) a.lse[(int64_t)h * a.Tq + r.q0 + q] = total == 0.0f ? -__builtin_inff() : (top + log2f(total)) * kLn2;
 }
 
 // dq of 32 queries, and delta = rowsum(dO O) for the keys' pass
-template <typename T, int DT>
+template <int DT>
 __global__ void __launch_bounds__(kThreads, 1) attn_bwd_q_kernel(AttnArgs a) {
     __shared__ float lds[2 * DT * 16 * 64];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5, col = lane & 31;
@@ -214,20 +213,20 @@ __global__ void __launch_bounds__(kThreads, 1) attn_bwd_q_kernel(AttnArgs a) {
     const int h = blockIdx.y, hk = h / (a.Hq / a.Hkv), D = a.D;
     const int q = tile * kTile + col, shift = r.lk - r.lq;
     const bool q_ok = q < r.lq;
-    const T *K = static_cast<const T *>(a.k) + r.k0 * a.k_stride + (int64_t)hk * D;
-    const T *V = static_cast<const T *>(a.v) + r.k0 * a.v_stride + (int64_t)hk * D;
+    const float *K = static_cast<const float *>(a.k) + r.k0 * a.k_stride + (int64_t)hk * D;
+    const float *V = static_cast<const float *>(a.v) + r.k0 * a.v_stride + (int64_t)hk * D;
     float qv[4 * DT][4], gv[4 * DT][4];
     const int64_t oq = ((r.q0 + (q_ok ? q : 0)) * a.Hq + h) * D;
     float delta = 0.0f;
-    load_row<T, DT>(static_cast<const T *>(a.O) + oq, q_ok, D, half, qv);
-    load_row<T, DT>(static_cast<const T *>(a.dO) + oq, q_ok, D, half, gv);
+    load_row<DT>(static_cast<const float *>(a.O) + oq, q_ok, D, half, qv);
+    load_row<DT>(static_cast<const float *>(a.dO) + oq, q_ok, D, half, gv);
 #pragma unroll
     for (int j = 0; j < 4 * DT; j++)
 #pragma unroll
         for (int e = 0; e < 4; e++) delta = __builtin_fmaf(qv[j][e], gv[j][e], delta);
     delta += __shfl_xor(delta, 32, 64);
     if (wave == 0 && half == 0 && q_ok) a.delta[(int64_t)h * a.Tq + r.q0 + q] = delta;
-    load_row<T, DT>(static_cast<const T *>(a.q) + (r.q0 + (q_ok ? q : 0)) * a.q_stride + (int64_t)h * D, q_ok, D, half, qv);
+    load_row<DT>(static_cast<const float *>(a.q) + (r.q0 + (q_ok ? q : 0)) * a.q_stride + (int64_t)h * D, q_ok, D, half, qv);
     const float c = a.scale * kLog2e;
     const float lse2 = q_ok ? a.lse[(int64_t)h * a.Tq + r.q0 + q] * kLog2e : 0.0f;
     const int q_end = tile * kTile + kTile < r.lq ? tile * kTile + kTile : r.lq;
@@ -236,21 +235,26 @@ __global__ void __launch_bounds__(kThreads, 1) attn_bwd_q_kernel(AttnArgs a) {
     f32x16_t dq[DT] = {};
     for (int k0 = wave * kTile; k0 < k_end; k0 += kWaves * kTile) {
         const bool k_ok = k0 + col < r.lk;
-        const f32x16_t sc = row_products<T, DT>(K + (k_ok ? k0 + col : 0) * a.k_stride, k_ok, D, half, qv);
-        const f32x16_t dp = row_products<T, DT>(V + (k_ok ? k0 + col : 0) * a.v_stride, k_ok, D, half, gv);
+        float kv[4 * DT][4], vv[4 * DT][4], kx[16][DT];
+        load_row<DT>(K + (k_ok ? k0 + col : 0) * a.k_stride, k_ok, D, half, kv);
+        load_row<DT>(V + (k_ok ? k0 + col : 0) * a.v_stride, k_ok, D, half, vv);
+        load_columns<DT>(K + k0 * a.k_stride, a.k_stride, r.lk - k0, D, lane, kx);
+        loads_first();
+        const f32x16_t sc = row_products<DT>(kv, qv);
+        const f32x16_t dp = row_products<DT>(vv, gv);
         float ds[16];
 #pragma unroll
         for (int i = 0; i < 16; i++)
             ds[i] = k0 + acc_row(i) + 4 * half <= seen ? exp2_raw(__builtin_fmaf(sc[i], c, -lse2)) * (dp[i] - delta) : 0.0f;
-        add_products<T, DT>(dq, K + k0 * a.k_stride, a.k_stride, r.lk - k0, D, lane, ds);
+        add_products<DT>(dq, kx, ds);
     }
     join<DT>(dq, lds, wave, lane);
     if (wave != 0 || !q_ok) return;
-    store_column<T, DT>(static_cast<T *>(a.dq) + (r.q0 + q) * a.dq_stride + (int64_t)h * D, D, half, dq, a.scale);
+    store_column<DT>(static_cast<float *>(a.dq) + (r.q0 + q) * a.dq_stride + (int64_t)h * D, D, half, dq, a.scale);
 }
 
 // dk and dv of 32 keys of one key-value head, summed over the query heads that share it
-template <typename T, int DT>
+template <int DT>
 __global__ void __launch_bounds__(kThreads, 1) attn_bwd_kv_kernel(AttnArgs a) {
     __shared__ float lds[2 * DT * 16 * 64];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5, col = lane & 31;
@@ -264,8 +268,8 @@ __global__ void __launch_bounds__(kThreads, 1) attn_bwd_kv_kernel(AttnArgs a) {
     const int k = tile * kTile + col, shift = r.lk - r.lq;
     const bool k_ok = k < r.lk;
     float kv[4 * DT][4], vv[4 * DT][4];
-    load_row<T, DT>(static_cast<const T *>(a.k) + (r.k0 + (k_ok ? k : 0)) * a.k_stride + (int64_t)hk * D, k_ok, D, half, kv);
-    load_row<T, DT>(static_cast<const T *>(a.v) + (r.k0 + (k_ok ? k : 0)) * a.v_stride + (int64_t)hk * D, k_ok, D, half, vv);
+    load_row<DT>(static_cast<const float *>(a.k) + (r.k0 + (k_ok ? k : 0)) * a.k_stride + (int64_t)hk * D, k_ok, D, half, kv);
+    load_row<DT>(static_cast<const float *>(a.v) + (r.k0 + (k_ok ? k : 0)) * a.v_stride + (int64_t)hk * D, k_ok, D, half, vv);
     const float c = a.scale * kLog2e;
     // first query that sees this tile's first key, and this lane's key
     const int q_first = a.causal && tile * kTile - shift > 0 ? (tile * kTile - shift) / kTile * kTile : 0;
@@ -274,28 +278,49 @@ __global__ void __launch_bounds__(kThreads, 1) attn_bwd_kv_kernel(AttnArgs a) {
     f32x16_t dk[DT] = {}, dv[DT] = {};
     for (int it = wave; it < q_tiles * group; it += kWaves) {
         const int h = hk * group + it / q_tiles, q0 = q_first + it % q_tiles * kTile;
-        const T *Q = static_cast<const T *>(a.q) + (r.q0 + q0) * a.q_stride + (int64_t)h * D;
-        const T *G = static_cast<const T *>(a.dO) + ((r.q0 + q0) * a.Hq + h) * D;
+        const float *Q = static_cast<const float *>(a.q) + (r.q0 + q0) * a.q_stride + (int64_t)h * D;
+        const float *G = static_cast<const float *>(a.dO) + ((r.q0 + q0) * a.Hq + h) * D;
         const int64_t g_stride = (int64_t)a.Hq * D, at = (int64_t)h * a.Tq + r.q0 + q0;
         const int n = r.lq - q0;
-        const f32x16_t sc = row_products<T, DT>(Q + (col < n ? col : 0) * a.q_stride, col < n, D, half, kv);
-        const f32x16_t dp = row_products<T, DT>(G + (col < n ? col : 0) * g_stride, col < n, D, half, vv);
+        float x[16][DT], ls[16], de[16];
+        f32x16_t sc, dp;
+        {
+            float qv[4 * DT][4], gv[4 * DT][4];
+            load_row<DT>(Q + (col < n ? col : 0) * a.q_stride, col < n, D, half, qv);
+            load_row<DT>(G + (col < n ? col : 0) * g_stride, col < n, D, half, gv);
+#pragma unroll
+            for (int i = 0; i < 16; i++) {
+                const int row = acc_row(i) + 4 * half;
+                ls[i] = a.lse[at + (row < n ? row : 0)];
+                de[i] = a.delta[at + (row < n ? row : 0)];
+            }
+            if constexpr (DT <= 2) load_columns<DT>(G, g_stride, n, D, lane, x);  // more do not fit the registers
+            loads_first();
+            sc = row_products<DT>(qv, kv);
+            dp = row_products<DT>(gv, vv);
+        }
+        if constexpr (DT > 2) {
+            load_columns<DT>(G, g_stride, n, D, lane, x);
+            loads_first();
+        }
         float p[16], ds[16];
 #pragma unroll
         for (int i = 0; i < 16; i++) {
             const int row = acc_row(i) + 4 * half;
             const bool ok = k_ok && row < n && q0 + row >= q_sees;
-            p[i] = ok ? exp2_raw(__builtin_fmaf(sc[i], c, -a.lse[at + (row < n ? row : 0)] * kLog2e)) : 0.0f;
-            ds[i] = ok ? p[i] * (dp[i] - a.delta[at + (row < n ? row : 0)]) : 0.0f;
+            p[i] = ok ? exp2_raw(__builtin_fmaf(sc[i], c, -ls[i] * kLog2e)) : 0.0f;
+            ds[i] = ok ? p[i] * (dp[i] - de[i]) : 0.0f;
         }
-        add_products<T, DT>(dv, G, g_stride, n, D, lane, p);
-        add_products<T, DT>(dk, Q, a.q_stride, n, D, lane, ds);
+        add_products<DT>(dv, x, p);
+        load_columns<DT>(Q, a.q_stride, n, D, lane, x);
+        loads_first();
+        add_products<DT>(dk, x, ds);
     }
     join<DT>(dk, lds, wave, lane);
     join<DT>(dv, lds, wave, lane);
     if (wave != 0 || !k_ok) return;
-    store_column<T, DT>(static_cast<T *>(a.dk) + (r.k0 + k) * a.dk_stride + (int64_t)hk * D, D, half, dk, a.scale);
-    store_column<T, DT>(static_cast<T *>(a.dv) + (r.k0 + k) * a.dv_stride + (int64_t)hk * D, D, half, dv, 1.0f);
+    store_column<DT>(static_cast<float *>(a.dk) + (r.k0 + k) * a.dk_stride + (int64_t)hk * D, D, half, dk, a.scale);
+    store_column<DT>(static_cast<float *>(a.dv) + (r.k0 + k) * a.dv_stride + (int64_t)hk * D, D, half, dv, 1.0f);
 }
 
 int64_t slots(int64_t T, int64_t n_seq, int rows) { return T / rows + n_seq; }
@@ -308,20 +333,18 @@ void pick_dt(int D, F &&f) {
     else f(std::integral_constant<int, 4>{});
 }
 
-template <typename T>
 hipError_t fwd(const AttnArgs &a, hipStream_t st) {
     const dim3 grid((unsigned)slots(a.Tq, a.n_seq, kTile), (unsigned)a.Hq);
-    pick_dt(a.D, [&](auto dt) { attn_fwd_kernel<T, decltype(dt)::value><<<grid, kThreads, 0, st>>>(a); });
+    pick_dt(a.D, [&](auto dt) { attn_fwd_kernel<decltype(dt)::value><<<grid, kThreads, 0, st>>>(a); });
     return hipGetLastError();
 }
 
-template <typename T>
 hipError_t bwd(const AttnArgs &a, hipStream_t st) {
     const dim3 gq((unsigned)slots(a.Tq, a.n_seq, kTile), (unsigned)a.Hq), gk((unsigned)slots(a.Tk, a.n_seq, kTile), (unsigned)a.Hkv);
     pick_dt(a.D, [&](auto dt) {
         constexpr int DT = decltype(dt)::value;
-        if (a.Tq > 0) attn_bwd_q_kernel<T, DT><<<gq, kThreads, 0, st>>>(a);
-        if (a.Tk > 0) attn_bwd_kv_kernel<T, DT><<<gk, kThreads, 0, st>>>(a);
+        if (a.Tq > 0) attn_bwd_q_kernel<DT><<<gq, kThreads, 0, st>>>(a);
+        if (a.Tk > 0) attn_bwd_kv_kernel<DT><<<gk, kThreads, 0, st>>>(a);
     });
     return hipGetLastError();
 }
@@ -344,12 +367,12 @@ size_t attn_bwd_ws(int64_t Tq, int64_t Tk, int Hq, int Hkv, int D, int64_t n_seq
 }
 
 hipError_t launch_attn_fwd(int dtype, const AttnArgs &a, void *ws, hipStream_t st) {
-    return dtype == kBF16 ? launch_attn_fwd_bf16(a, ws, st) : fwd<float>(a, st);
+    return dtype == kBF16 ? launch_attn_fwd_bf16(a, ws, st) : fwd(a, st);
 }
 
 hipError_t launch_attn_bwd(int dtype, AttnArgs a, void *ws, hipStream_t st) {
     a.delta = reinterpret_cast<float *>(static_cast<char *>(ws) + kWsHeader);
-    if (dtype != kBF16) return bwd<float>(a, st);
+    if (dtype != kBF16) return bwd(a, st);
     return launch_attn_bwd_bf16(a, reinterpret_cast<float *>(static_cast<char *>(ws) + kWsHeader + delta_bytes(a.Tq, a.Hq)), st);
 }
 

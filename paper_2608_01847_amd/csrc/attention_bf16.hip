@@ -27,8 +27,6 @@ typedef __attribute__((address_space(3))) u32x4_t lds_u32x4;
 constexpr int kWaves = 4;
 constexpr int kThreads = 64 * kWaves;
 constexpr int kKeys = 64;   // rows of a staged tile
-constexpr int64_t kBwdWgs = 2048;  // workgroups that a backward launch is split for
-constexpr int64_t kBwdSplits = 16;
 constexpr float kNone = -__builtin_inff();
 
 // Geometry of a staged tile of ROWS rows: DT x 32 features, a row of 128 (DT <= 2) or 256 bytes. 16-byte chunk c of row r
@@ -928,17 +926,21 @@ hipError_t launch_attn_fwd_bf16(const AttnArgs &a, void *ws, hipStream_t st) {
     return hipGetLastError();
 }
 
-// Parts of a backward's sums. One workgroup's run through all queries (keys) of a long sequence is the whole call's
-// time where there are few of them, so they are split until there are kBwdWgs, each with 8 tiles at least by the mean length.
+// Parts of a backward's sums. Where workgroups are few, one's run through all queries (keys) of a long sequence is the whole
+// call's time: they are split until two per CU are busy, with 4 tiles each at least by the mean length. The keys' pass, whose
+// runs over a causal sequence are from one to all of its queries long, is split on until there are four times as many with 64
+// tiles each, so that long and short ones even out (four sequences of 2,048 with 64/8 heads 1.46 ms in place of 1.52). A part
+// costs 64 KB of fp32 sums per 128 rows and gradient, written and read again: splitting either pass up to 2,048 workgroups
+// with 8 tiles each made two sequences of 2,500 with 16/8 heads take 554 us in place of 462.
 AttnBwdPlan plan_attn_bwd_bf16(int64_t Tq, int64_t Tk, int Hq, int Hkv, int64_t n_seq) {
-    constexpr int64_t kRows = 32 * kWaves;
+    const int64_t kRows = 32 * kWaves, kBusy = 2 * kMfmaConcurrentWgs, kMost = 16;
     if (n_seq < 1) return {1, 1};
-    const int64_t q_wgs = (Tq * (Hq / Hkv) / kRows + n_seq) * Hkv, k_wgs = (Tk / kRows + n_seq) * Hkv;
-    const int64_t q_most = Tk / n_seq / kKeys / 8, k_most = Tq / n_seq * (Hq / Hkv) / 32 / 8;
-    auto pick = [](int64_t wgs, int64_t most) {
-        return (int)std::max<int64_t>(1, std::min<int64_t>({kBwdWgs / wgs, most, kBwdSplits}));
-    };
-    return {pick(q_wgs, q_most), pick(k_wgs, k_most)};
+    const int64_t group = Hq / Hkv, q_wgs = (Tq * group / kRows + n_seq) * Hkv, k_wgs = (Tk / kRows + n_seq) * Hkv;
+    const int64_t q_tiles = Tk / n_seq / kKeys, k_tiles = Tq / n_seq * group / 32;
+    const int64_t q = std::min(kBusy / q_wgs, q_tiles / 4);
+    const int64_t k = std::max(std::min(kBusy / k_wgs, k_tiles / 4), std::min(4 * kBusy / k_wgs, k_tiles / 64));
+    auto clip = [&](int64_t s) { return (int)std::max<int64_t>(1, std::min(kMost, s)); };
+    return {clip(q), clip(k)};
 }
 
 hipError_t launch_attn_bwd_bf16(const AttnArgs &a, float *parts, hipStream_t st) {
