@@ -590,6 +590,11 @@ __global__ void __launch_bounds__(kThreads, 2) attn_bwd_q_bf16_kernel(AttnArgs a
             // for each 32 keys: groups of S, then of dP (four steps of 16 features each) with the exponentials between their
             // instructions, then two of dq
             constexpr int kS = (2 * DT + 3) / 4, kAll = 2 * kS + 2;
+            auto dscore = [&](int h) {  // half h of dS = P (dP - delta)
+#pragma unroll
+                for (int i = 8 * h; i < 8 * h + 8; i++) sc[i] *= dp[i];
+                ds[h] = pack8(sc, h);
+            };
             pipelined<2 * kAll>(
                 [&](auto g, bf16x8_t (&x)[4]) {
                     constexpr int b = g / kAll, n = g % kAll;
@@ -605,11 +610,14 @@ __global__ void __launch_bounds__(kThreads, 2) attn_bwd_q_bf16_kernel(AttnArgs a
                 [&](auto g, bf16x8_t (&x)[4]) {
                     constexpr int b = g / kAll, n = g % kAll;
                     if constexpr (n == 0) sc = f32x16_t{};
-                    if constexpr (n == kS) dp = f32x16_t{};
                     if constexpr (n < kS) {
 #pragma unroll
                         for (int i = 0; i < 4; i++)
                             if (4 * n + i < 2 * DT) sc = mfma(x[i], qv[4 * n + i], sc);
+                        if constexpr (n == kS - 1) {  // dP - delta
+#pragma unroll
+                            for (int i = 0; i < 16; i++) dp[i] = -delta;
+                        }
                     } else if constexpr (n < 2 * kS) {
                         static_for<4>([&](auto i) {
                             constexpr int step = 4 * (n - kS) + i;
@@ -622,19 +630,19 @@ __global__ void __launch_bounds__(kThreads, 2) attn_bwd_q_bf16_kernel(AttnArgs a
                             }
                         });
                     } else {
-#pragma unroll
-                        for (int t = 0; t < DT; t++) dq[t] = mfma(x[t], ds[n - 2 * kS], dq[t]);
+                        static_for<DT>([&](auto t) {
+                            dq[t] = mfma(x[t], ds[n - 2 * kS], dq[t]);
+                            if constexpr (n == 2 * kS && t == 0) dscore(1);  // the second half behind the first's products
+                            __builtin_amdgcn_sched_barrier(0);
+                        });
                     }
                     if constexpr (n == 2 * kS - 1) {
-#pragma unroll
-                        for (int i = 0; i < 16; i++) sc[i] *= dp[i] - delta;
                         if (k0 + 32 * b + 31 > w.all_seen) {
 #pragma unroll
                             for (int i = 0; i < 16; i++)
-                                if (k0 + 32 * b + acc_row(i) + 4 * half > w.seen) sc[i] = 0.0f;
+                                if (k0 + 32 * b + acc_row(i) + 4 * half > w.seen) sc[i] = dp[i] = 0.0f;
                         }
-#pragma unroll
-                        for (int i = 0; i < 2; i++) ds[i] = pack8(sc, i);
+                        dscore(0);
                     }
                 });
         }
