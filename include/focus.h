@@ -425,7 +425,8 @@ typedef struct {
 } focus_attention_config;
 
 /* Workspace bytes of focus_attention_fwd (call = FOCUS_CALL_ATTENTION_FWD) and focus_attention_bwd
- * (FOCUS_CALL_ATTENTION_BWD). Host-only; 0 for invalid arguments. */
+ * (FOCUS_CALL_ATTENTION_BWD). They do not grow with the shape alone: fewer queries may be split into more parts, so ask
+ * for every shape that is called, and take the largest. Host-only; 0 for invalid arguments. */
 size_t focus_attention_workspace_size(int call, const focus_attention_config *cfg, int64_t Tq, int64_t Tk, int64_t n_seq);
 
 /* Attention over whole prompts, several sequences packed one after the other without padding:
@@ -434,13 +435,14 @@ size_t focus_attention_workspace_size(int call, const focus_attention_config *cf
  *   lse_opt [heads_q][Tq] fp32 (the backward needs it).
  *   cu_q, cu_k : DEVICE arrays of n_seq + 1 int32, sequence s holding queries cu_q[s] .. cu_q[s + 1] - 1 and keys
  *               cu_k[s] .. cu_k[s + 1] - 1; they may be one array. Both NULL: one sequence of everything (n_seq == 1).
- *               They rise and lie in [0, Tq] and [0, Tk]; a pair that does not raises the domain flag and its sequence is
- *               treated as empty. Rows of no sequence are neither read nor written.
+ *               They rise and lie in [0, Tq] and [0, Tk]; a pair that does not raises the domain flag, its sequence is
+ *               treated as empty and its rows' results are unspecified. Rows of no sequence are neither read nor written.
  *   A query that sees no key (none there, or causal with fewer keys than queries) has O = 0 and lse = -inf.
  *   Nothing outside a query's own sequence reaches its output, NaN and infinities included. A hidden key of its own
  *   sequence does not either, as long as its v is finite.
  *   bf16: products on the bf16 matrix instructions with fp32 sums, probabilities rounded to bf16 for the second product;
- *   fp32: fp32 products throughout. Tq, Tk <= 2^30, n_seq <= 2^24, heads_q <= 65535.
+ *   fp32: fp32 products throughout. heads_q <= 65535, Tq / 32 + n_seq, Tk / 32 + n_seq,
+ *   Tq heads_q / 128 + n_seq heads_kv and Tk heads_kv / 128 + n_seq heads_kv below 2^24 (FOCUS_ERR_SHAPE).
  *   Tensor pointers 16-byte aligned, lse and cu_* element-aligned. */
 focus_status focus_attention_fwd(const focus_attention_config *cfg, const void *q, const void *k, const void *v, int dtype,
                                  int64_t Tq, int64_t Tk, const int32_t *cu_q, const int32_t *cu_k, int64_t n_seq, void *O,
@@ -450,7 +452,10 @@ focus_status focus_attention_fwd(const focus_attention_config *cfg, const void *
  *   dv = P^T dO, dP = dO v^T, dS = P (dP - rowsum(dO O)), dq = scale dS k, dk = scale dS^T q,
  * dk and dv summed over the query heads that share a key-value head. P is formed again from lse; bf16: P and dS are
  * rounded to bf16 for the products. dq, dk, dv in dtype, with cfg's gradient strides; keys that no query sees get zeros.
- * No atomics: every sum has a fixed order. */
+ * A hidden pair of a sequence has probability 0, whose products with a NaN or infinity of the pair's q, k, v or dO are NaN:
+ * these have to be finite. Nothing reaches one sequence from another.
+ * bf16 gradients: rounding dS, and O as the forward rounded it in rowsum(dO O), each add about as much error as rounding the
+ * result does (2^-9 of it). No atomics: every sum has a fixed order. */
 focus_status focus_attention_bwd(const focus_attention_config *cfg, const void *dO, const void *q, const void *k,
                                  const void *v, const void *O, const float *lse, int dtype, int64_t Tq, int64_t Tk,
                                  const int32_t *cu_q, const int32_t *cu_k, int64_t n_seq, void *dq, void *dk, void *dv,

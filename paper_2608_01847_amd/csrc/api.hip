@@ -158,6 +158,11 @@ focus_status attention_args(const focus_attention_config *cfg, int64_t Tq, int64
         if (given[i] != 0 && (given[i] < row || given[i] > (int64_t(1) << 24))) return FOCUS_ERR_SHAPE;
         *out[i] = given[i] ? given[i] : row;
     }
+    // a launch's work-items in x (256 per workgroup: 32 tokens in fp32, 128 rows of a key-value head in bf16) stay below 2^32
+    constexpr int64_t kMaxWgs = (int64_t(1) << 24) - 1;
+    const int64_t most = std::max(Tq, Tk);
+    if (most / 32 + n_seq > kMaxWgs || (Tq * (hq / hkv) / 128 + n_seq) * hkv > kMaxWgs || (Tk / 128 + n_seq) * hkv > kMaxWgs)
+        return FOCUS_ERR_SHAPE;
     a.Tq = Tq, a.Tk = Tk, a.n_seq = (int)n_seq;
     a.Hq = (int)hq, a.Hkv = (int)hkv, a.D = (int)d, a.causal = cfg->causal, a.scale = cfg->scale;
     return FOCUS_OK;

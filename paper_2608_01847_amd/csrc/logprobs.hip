@@ -412,17 +412,36 @@ hipError_t launch_logprobs(int dtype, const void *Z, int64_t T, int64_t V, const
     const int splits = plan_splits(T, V);
     const int64_t per = ((V + splits - 1) / splits + 7) / 8 * 8;
     char *base = static_cast<char *>(ws) + kWsHeader;
-    LogprobArgs a{Z, target, logp, entropy, lse, top_logp, top_index, flag, reinterpret_cast<Stat *>(base),
-                  reinterpret_cast<uint64_t *>(base + kMaxParts * 16), T, V, per, top, splits};
-    return dtype == kBF16 ? fwd<uint16_t>(a, st) : fwd<float>(a, st);
+    // a launch's work-items (512 per row where rows are not split) must stay below 2^32
+    constexpr int64_t kRows = (int64_t(1) << 23) - 1;
+    for (int64_t r = 0; r < T; r += kRows) {
+        LogprobArgs a{static_cast<const char *>(Z) + (size_t)(r * V) * (dtype == kBF16 ? 2 : 4),
+                      target ? target + r : nullptr,
+                      logp ? logp + r : nullptr,
+                      entropy ? entropy + r : nullptr,
+                      lse + r,
+                      top_logp + r * top,
+                      top_index + r * top,
+                      flag,
+                      reinterpret_cast<Stat *>(base),
+                      reinterpret_cast<uint64_t *>(base + kMaxParts * 16),
+                      std::min(kRows, T - r),
+                      V,
+                      per,
+                      top,
+                      splits};
+        const hipError_t e = dtype == kBF16 ? fwd<uint16_t>(a, st) : fwd<float>(a, st);
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
 }
 
 hipError_t launch_logprobs_bwd(int dtype, const void *Z, int64_t T, int64_t V, const int64_t *target, const float *lse,
                                const float *entropy, const float *d_logp, const float *d_entropy, void *dZ, hipStream_t st) {
     const int64_t chunks = (V + kBwdChunk - 1) / kBwdChunk;
     LogprobBwdArgs a{Z, target, lse, entropy, d_logp, d_entropy, dZ, V, (unsigned)chunks};
-    // one launch for as many rows as a grid holds
-    const int64_t rows = std::max<int64_t>(1, ((int64_t(1) << 31) - 1) / chunks);
+    // one launch for as many rows as a grid holds: its work-items (256 per chunk) must stay below 2^32
+    const int64_t rows = std::max<int64_t>(1, ((int64_t(1) << 24) - 1) / chunks);
     const size_t esz = dtype == kBF16 ? 2 : 4;
     for (int64_t r = 0; r < T; r += rows) {
         const int64_t n = std::min(rows, T - r);

@@ -440,8 +440,17 @@ size_t norm_bwd_ws(int64_t T, int64_t C) {
 
 hipError_t launch_norm_fwd(int layer, float eps, int dtype, const void *X, const void *R, int64_t T, int64_t C, const void *w,
                            const void *b, int w_dtype, void *H, void *Y, float *mean, float *rstd, hipStream_t st) {
-    NormFwdArgs a{X, R, w, b, H, Y, mean, rstd, T, (int)C, w_dtype, layer, eps};
-    return dtype == kBF16 ? norm_fwd<uint16_t>(a, st) : norm_fwd<float>(a, st);
+    const size_t row = (size_t)C * (dtype == kBF16 ? 2 : 4);
+    auto at = [&](const void *p, int64_t r) { return p ? static_cast<const char *>(p) + (size_t)r * row : nullptr; };
+    // a launch's work-items (256 per row at most) must stay below 2^32
+    constexpr int64_t kRows = (int64_t(1) << 24) - 1;
+    for (int64_t r = 0; r < T; r += kRows) {
+        NormFwdArgs a{at(X, r), at(R, r), w, b, const_cast<char *>(at(H, r)), const_cast<char *>(at(Y, r)),
+                      mean ? mean + r : nullptr, rstd ? rstd + r : nullptr, std::min(kRows, T - r), (int)C, w_dtype, layer, eps};
+        const hipError_t e = dtype == kBF16 ? norm_fwd<uint16_t>(a, st) : norm_fwd<float>(a, st);
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
 }
 
 hipError_t launch_norm_bwd(int layer, int dtype, const void *dY, const void *H, int64_t T, int64_t C, const void *w,

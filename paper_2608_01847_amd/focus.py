@@ -459,6 +459,13 @@ def _sized(ws: torch.Tensor | None, need: int, device) -> torch.Tensor:
     return ws
 
 
+def _one_gpu(where: str, first: torch.Tensor, *rest) -> None:
+    """All tensors (None: not given) lie on one GPU: a host address would reach a kernel otherwise."""
+    d = first.get_device()
+    if d < 0 or any(t is not None and t.get_device() != d for t in rest):
+        raise ValueError(f"{where}: tensors of one GPU expected")
+
+
 def norm_fwd(X: torch.Tensor, weight: torch.Tensor, bias=None, residual=None, kind: int = NORM_LAYER, eps: float = 1e-5,
              want_stats: bool = True, ws=None, out=None, h_out=None):
     """Layer norm (NORM_LAYER) or RMS norm (NORM_RMS) over the last dimension of X [T][C], with an optional residual sum
@@ -472,6 +479,7 @@ def norm_fwd(X: torch.Tensor, weight: torch.Tensor, bias=None, residual=None, ki
         raise ValueError("norm_fwd: weight and bias are [C] of one dtype")
     if h_out is not None and residual is None:
         raise ValueError("norm_fwd: h_out without a residual")
+    _one_gpu("norm_fwd", X, weight, bias, residual, ws, out, h_out)
     Y = out if out is not None else torch.empty_like(X)
     H = (h_out if h_out is not None else torch.empty_like(X)) if residual is not None else None
     mean = rstd = None
@@ -500,6 +508,7 @@ def norm_bwd(dY: torch.Tensor, H: torch.Tensor, weight: torch.Tensor, mean, rstd
     for t in (mean, rstd, dw_out, db_out):
         if t is not None and t.dtype != torch.float32:
             raise TypeError("norm_bwd: statistics and parameter gradients are float32")
+    _one_gpu("norm_bwd", H, dY, weight, mean, rstd, d_residual, ws, out, dw_out, db_out)
     dX = out if out is not None else torch.empty_like(H)
     dw = dw_out if dw_out is not None else torch.empty(C, dtype=torch.float32, device=H.device)
     db = db_out
@@ -521,6 +530,8 @@ def _heads(t: torch.Tensor, name: str) -> tuple:
     if n and ((d > 1 and t.stride(2) != 1) or (h > 1 and t.stride(1) != d)):
         raise ValueError(f"{name}: a token's heads must be contiguous")
     stride = t.stride(0) if n > 1 else h * d
+    if stride < h * d:
+        raise ValueError(f"{name}: tokens overlap")
     return t.data_ptr(), stride
 
 
@@ -572,6 +583,7 @@ def attention_fwd(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_q=None, 
         lse = torch.empty(q.shape[1], q.shape[0], dtype=torch.float32, device=q.device)
     if lse is not None and (lse.shape != (q.shape[1], q.shape[0]) or lse.dtype != torch.float32):
         raise ValueError("attention_fwd: lse is float32 [Hq][Tq]")
+    _one_gpu("attention_fwd", q, k, v, cu_q, cu_k, ws, out, lse)
     ws = _sized(ws, int(lib().focus_attention_workspace_size(CALL_ATTENTION_FWD, ctypes.byref(cfg), q.shape[0], k.shape[0],
                                                              n)), q.device)
     _check(lib().focus_attention_fwd(ctypes.byref(cfg), aq, ak, av, _dt(q), q.shape[0], k.shape[0], pq, pk, n, _ptr(O),
@@ -594,6 +606,7 @@ def attention_bwd(dO: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v: torch.T
     for g, t in ((dq, q), (dk, k), (dv, v)):
         if g.shape != t.shape or g.dtype != t.dtype:
             raise ValueError("attention_bwd: the gradients have the shapes and dtype of q, k, v")
+    _one_gpu("attention_bwd", q, k, v, dO, O, lse, cu_q, cu_k, ws, dq, dk, dv)
     ptrs = [_heads(t, name) for t, name in ((q, "q"), (k, "k"), (v, "v"), (dq, "dq"), (dk, "dk"), (dv, "dv"))]
     cfg = _attention_config(q, k, causal, scale, tuple(s for _, s in ptrs))
     ws = _sized(ws, int(lib().focus_attention_workspace_size(CALL_ATTENTION_BWD, ctypes.byref(cfg), q.shape[0], k.shape[0],
@@ -622,6 +635,7 @@ def token_logprobs(Z: torch.Tensor, target=None, top: int = 0, ws=None):
     T, V = Z.shape
     f32 = dict(dtype=torch.float32, device=Z.device)
     pt = _targets(target, T)
+    _one_gpu("token_logprobs", Z, target, ws)
     logp = torch.empty(T, **f32) if target is not None else None
     entropy, lse = torch.empty(T, **f32), torch.empty(T, **f32)
     top_logp = top_index = None
@@ -644,6 +658,7 @@ def token_logprobs_bwd(Z: torch.Tensor, target, lse: torch.Tensor, entropy=None,
     dZ = out if out is not None else torch.empty_like(Z)
     if dZ.shape != Z.shape or dZ.dtype != Z.dtype:
         raise ValueError("token_logprobs_bwd: out has Z's shape and dtype")
+    _one_gpu("token_logprobs_bwd", Z, target, lse, entropy, d_logp, d_entropy, ws, out)
     ws = _sized(ws, 256, Z.device)
     _check(lib().focus_token_logprobs_bwd(_ptr(Z), _dt(Z), T, V, _targets(target, T), _ptr(lse), _ptr(entropy), _ptr(d_logp),
                                           _ptr(d_entropy), _ptr(dZ), _ptr(ws), ws.numel(), _stream()),

@@ -365,3 +365,17 @@ def test_refusals(F):
         F.attention_fwd(q.transpose(0, 1), k, k)
     with pytest.raises(ValueError):
         F.attention_fwd(q, k, k, lse=torch.empty(8, 4).cuda())
+
+
+def test_refuses_what_would_reach_a_kernel_wrongly(F):
+    """Tensors of the host, and tokens that share their memory (a broadcast tensor)."""
+    q = torch.zeros(4, 2, 64, dtype=torch.bfloat16, device="cuda")
+    cu = torch.tensor([0, 4], dtype=torch.int32)
+    wide = q[:1].expand(4, 2, 64)
+    O, lse = F.attention_fwd(q, q, q)
+    for call in (lambda: F.attention_fwd(q, q.cpu(), q), lambda: F.attention_fwd(q, q, q, cu),
+                 lambda: F.attention_fwd(q.cpu(), q, q), lambda: F.attention_fwd(q, wide, wide),
+                 lambda: F.attention_bwd(q, q, q, q, O, lse.cpu()), lambda: F.attention_bwd(q, wide, q, q, O, lse),
+                 lambda: F.attention_bwd(q, q, q, q, O, lse, out=(q, wide, q))):
+        with pytest.raises(ValueError):
+            call()

@@ -200,3 +200,23 @@ def test_refusals(F):
         with pytest.raises(F.FocusError) as e:
             call()
         assert e.value.status == F.ERR_CONFIG
+
+
+def test_more_rows_than_one_launch_holds(F):
+    """The rows past 2^24 - 1 against a call of their own."""
+    T, C, tail = (1 << 24) + 1000, 16, 1500
+    X = torch.randn(T, C, device="cuda", generator=torch.Generator("cuda").manual_seed(3)).bfloat16()
+    w = torch.linspace(0.5, 1.5, C, device="cuda")
+    Y, H, mean, rstd = F.norm_fwd(X, w, residual=X, kind=F.NORM_LAYER)
+    y, h, m, r = F.norm_fwd(X[-tail:].contiguous(), w, residual=X[-tail:].contiguous(), kind=F.NORM_LAYER)
+    for all_rows, some in ((Y, y), (H, h), (mean, m), (rstd, r)):
+        assert torch.equal(all_rows[-tail:], some)
+
+
+def test_refuses_tensors_of_the_host(F):
+    X, w = torch.zeros(3, 16, device="cuda"), torch.ones(16, device="cuda")
+    Y, H, mean, rstd = F.norm_fwd(X, w)
+    for call in (lambda: F.norm_fwd(X.cpu(), w), lambda: F.norm_fwd(X, w.cpu()), lambda: F.norm_fwd(X, w, residual=X.cpu()),
+                 lambda: F.norm_bwd(X, X, w, mean, rstd.cpu()), lambda: F.norm_bwd(X.cpu(), X, w, mean, rstd)):
+        with pytest.raises(ValueError):
+            call()

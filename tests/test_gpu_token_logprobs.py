@@ -241,3 +241,26 @@ def test_refusals(F):
     with pytest.raises(TypeError):
         F.token_logprobs(Z.half(), t)
     assert F.token_logprobs(torch.empty(0, 100).cuda(), None)[1].shape == (0,)
+
+
+def test_more_rows_than_one_launch_holds(F):
+    """The rows past 2^23 - 1 (forward) and 2^24 - 1 (gradient) against calls of their own."""
+    T, V, tail = (1 << 24) + 1000, 5, 1500
+    Z = torch.randn(T, V, device="cuda", generator=torch.Generator("cuda").manual_seed(4)).bfloat16()
+    target = (torch.arange(T, device="cuda") * 7) % (V + 1) - 1
+    some, mine = Z[-tail:].contiguous(), target[-tail:].contiguous()
+    got, ref = F.token_logprobs(Z, target, 2), F.token_logprobs(some, mine, 2)
+    for a, b in zip(got, ref):
+        assert torch.equal(a[-tail:], b)
+    g = torch.linspace(-1, 1, T, device="cuda")
+    dZ = F.token_logprobs_bwd(Z, target, got[2], got[1], g, g)
+    assert torch.equal(dZ[-tail:], F.token_logprobs_bwd(some, mine, ref[2], ref[1], g[-tail:].contiguous(), g[-tail:].contiguous()))
+
+
+def test_refuses_tensors_of_the_host(F):
+    Z, t = torch.zeros(3, 16, device="cuda"), torch.zeros(3, dtype=torch.int64, device="cuda")
+    logp, entropy, lse, _, _ = F.token_logprobs(Z, t)
+    for call in (lambda: F.token_logprobs(Z.cpu(), t), lambda: F.token_logprobs(Z, t.cpu()),
+                 lambda: F.token_logprobs_bwd(Z, t, lse.cpu(), d_logp=lse), lambda: F.token_logprobs_bwd(Z, t, lse, d_logp=lse.cpu())):
+        with pytest.raises(ValueError):
+            call()

@@ -136,3 +136,14 @@ def test_workspace_sizes(L):
     assert F.token_logprobs_workspace_size(8, 1000, 65) == 0 and F.token_logprobs_workspace_size(8, 0, 1) == 0
     assert F.token_logprobs_workspace_size(1, 1000, 5) == F.token_logprobs_workspace_size(100000, 1000, 5)
     assert L.focus_workspace_size(F.CALL_TOKEN_LOGPROBS_BWD, q, 8, 1000, 0) == 256
+
+
+def test_attention_sizes_of_a_launch(L, cpu_only):
+    """Work-items of a launch stay below 2^32: sizes past that are refused, sizes just below are not."""
+    size = lambda Hq, Hkv, Tq, Tk, n: L.focus_attention_workspace_size(
+        focus.CALL_ATTENTION_FWD, ctypes.byref(focus.AttentionConfig(Hq, Hkv, 8, 1, 0.1, 0, *(0,) * 6)), Tq, Tk, n)
+    assert size(1, 1, 1 << 29, 1, 1) == 0 and size(1, 1, 1, 1 << 29, 1) == 0 and size(1, 1, (1 << 29) - 64, 1, 1) > 0
+    assert size(64, 8, 1 << 25, 1, 1) == 0 and size(64, 8, (1 << 25) - 256, 1, 1) > 0
+    assert size(64, 64, 1, 1 << 25, 1) == 0
+    assert size(8, 8, 1, 1, 1 << 21) == 0 and size(8, 8, 1, 1, (1 << 21) - 1) > 0
+    assert attn(L, "fwd", Hq=8, Hkv=8, cu_q=B, cu_k=B, n=1 << 21) == focus.ERR_SHAPE
