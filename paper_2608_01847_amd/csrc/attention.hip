@@ -126,10 +126,8 @@ __global__ void __launch_bounds__(kThreads, 1) attn_fwd_kernel(AttnArgs a) {
     __shared__ float lds[2 * DT * 16 * 64];
     __shared__ float stat[2][kWaves][32];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5, col = lane & 31;
-    int tile;
-    const int s = slot_sequence(a.cu_q, a.n_seq, kTile, (int)blockIdx.x, 1, tile);
     SeqRange r;
-    seq_range(a, s, r);
+    const int tile = slot_range<false>(a, kTile, (int)blockIdx.x, 1, r);
     check_ends<kThreads>(a);
     if (!tile_in(tile, kTile, r.lq)) return;
     const int h = blockIdx.y, hk = h / (a.Hq / a.Hkv), D = a.D;
@@ -204,10 +202,8 @@ template <int DT>
 __global__ void __launch_bounds__(kThreads, 1) attn_bwd_q_kernel(AttnArgs a) {
     __shared__ float lds[2 * DT * 16 * 64];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5, col = lane & 31;
-    int tile;
-    const int s = slot_sequence(a.cu_q, a.n_seq, kTile, (int)blockIdx.x, 1, tile);
     SeqRange r;
-    seq_range(a, s, r);
+    const int tile = slot_range<false>(a, kTile, (int)blockIdx.x, 1, r);
     check_ends<kThreads>(a);
     if (!tile_in(tile, kTile, r.lq)) return;
     const int h = blockIdx.y, hk = h / (a.Hq / a.Hkv), D = a.D;
@@ -258,10 +254,8 @@ template <int DT>
 __global__ void __launch_bounds__(kThreads, 1) attn_bwd_kv_kernel(AttnArgs a) {
     __shared__ float lds[2 * DT * 16 * 64];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5, col = lane & 31;
-    int tile;
-    const int s = slot_sequence(a.cu_k, a.n_seq, kTile, (int)blockIdx.x, 1, tile);
     SeqRange r;
-    seq_range(a, s, r);
+    const int tile = slot_range<true>(a, kTile, (int)blockIdx.x, 1, r);
     check_ends<kThreads>(a);
     if (!tile_in(tile, kTile, r.lk)) return;
     const int hk = blockIdx.y, group = a.Hq / a.Hkv, D = a.D;

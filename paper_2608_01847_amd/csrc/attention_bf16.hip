@@ -269,7 +269,6 @@ __device__ __forceinline__ void store_part(float *row, bool ok, int D, int half,
 // What a wave's lane does in the kernels whose columns are query rows: its row, and the keys that it, its wave and its
 // workgroup see.
 struct RowTile {
-    int64_t rows;   // of the sequence and key-value head
     bool ok;
     int q, h;       // this lane's query (in its sequence) and head
     int seen;       // last key that it sees
@@ -277,25 +276,26 @@ struct RowTile {
     int any_seen;   // last key that some row of the wave sees (-1: none)
     int nk;         // tiles of 64 keys that the workgroup goes through
     __device__ __forceinline__ void init(const AttnArgs &a, const SeqRange &r, int tile, int hk, int wave, int col) {
-        constexpr int kRows = 32 * kWaves;
-        const int group = a.Hq / a.Hkv, shift = r.lk - r.lq;
-        rows = (int64_t)r.lq * group;
-        const int64_t first = (int64_t)tile * kRows;
-        const int64_t last = first + kRows < rows ? first + kRows - 1 : rows - 1;
-        auto sees = [&](int64_t row) {
-            const int k = a.causal ? (int)(row / group) + shift : r.lk - 1;
+        constexpr uint32_t kRows = 32 * kWaves;
+        const uint32_t group = (uint32_t)(a.Hq / a.Hkv);
+        const int shift = r.lk - r.lq;
+        // rows of a key-value head are below 2^31 (checked on the host)
+        const uint32_t rows = (uint32_t)r.lq * group, first = (uint32_t)tile * kRows;
+        const uint32_t last = first + kRows < rows ? first + kRows - 1 : rows - 1;
+        auto sees = [&](uint32_t query) {
+            const int k = a.causal ? (int)query + shift : r.lk - 1;
             return k < r.lk ? k : r.lk - 1;
         };
-        const int k_end = sees(last) + 1;
+        const int k_end = sees(last / group) + 1;
         nk = k_end > 0 ? (k_end + kKeys - 1) / kKeys : 0;
-        const int64_t w_first = first + 32 * wave, w_last = w_first + 31 < last ? w_first + 31 : last;
-        any_seen = w_first <= last ? sees(w_last) : -1;
-        all_seen = sees(w_first);
-        const int64_t row = w_first + col;
+        const uint32_t w_first = first + 32 * (uint32_t)wave, w_last = w_first + 31 < last ? w_first + 31 : last;
+        any_seen = w_first <= last ? sees(w_last / group) : -1;
+        all_seen = sees(w_first / group);
+        const uint32_t row = w_first + (uint32_t)col;
         ok = row <= last;
         q = (int)(row / group);
-        h = hk * group + (int)(row - (int64_t)q * group);
-        seen = ok ? sees(row) : r.lk - 1;
+        h = hk * (int)group + (int)(row - (uint32_t)q * group);
+        seen = ok ? sees((uint32_t)q) : r.lk - 1;
     }
 };
 
@@ -308,10 +308,8 @@ __global__ void __launch_bounds__(kThreads, 2) attn_fwd_bf16_kernel(AttnArgs a, 
     constexpr int kRows = 32 * kWaves;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5, col = lane & 31;
     const int hk = blockIdx.x % a.Hkv, group = a.Hq / a.Hkv, D = a.D;
-    int tile;
-    const int s = slot_sequence(a.cu_q, a.n_seq, kRows, (int)(gridDim.x / a.Hkv - 1 - blockIdx.x / a.Hkv), group, tile);
     SeqRange r;
-    seq_range(a, s, r);
+    const int tile = slot_range<false>(a, kRows, (int)(gridDim.x / a.Hkv - 1 - blockIdx.x / a.Hkv), group, r);
     check_ends<kThreads>(a);
     if (!tile_in(tile, kRows, (int64_t)r.lq * group)) return;
     RowTile w;
@@ -535,10 +533,8 @@ __global__ void __launch_bounds__(kThreads, 2) attn_bwd_q_bf16_kernel(AttnArgs a
     constexpr int kRows = 32 * kWaves;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5, col = lane & 31;
     const int hk = blockIdx.x % a.Hkv, group = a.Hq / a.Hkv, D = a.D;
-    int tile;
-    const int s = slot_sequence(a.cu_q, a.n_seq, kRows, (int)(gridDim.x / a.Hkv - 1 - blockIdx.x / a.Hkv), group, tile);
     SeqRange r;
-    seq_range(a, s, r);
+    const int tile = slot_range<false>(a, kRows, (int)(gridDim.x / a.Hkv - 1 - blockIdx.x / a.Hkv), group, r);
     check_ends<kThreads>(a);
     if (!tile_in(tile, kRows, (int64_t)r.lq * group)) return;
     RowTile w;
@@ -680,10 +676,8 @@ __global__ void __launch_bounds__(kThreads, 2) attn_bwd_kv_bf16_kernel(AttnArgs 
     __shared__ __attribute__((aligned(16))) float stats[2][2][kQ];  // [stage][-lse / scale, -delta]
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5, col = lane & 31;
     const int hk = blockIdx.x % a.Hkv, group = a.Hq / a.Hkv, D = a.D;
-    int tile;
-    const int s = slot_sequence(a.cu_k, a.n_seq, kRows, (int)(blockIdx.x / a.Hkv), 1, tile);
     SeqRange r;
-    seq_range(a, s, r);
+    const int tile = slot_range<true>(a, kRows, (int)(blockIdx.x / a.Hkv), 1, r);
     check_ends<kThreads>(a);
     if (!tile_in(tile, kRows, r.lk)) return;
     const int shift = r.lk - r.lq, w_first = tile * kRows + 32 * wave, k = w_first + col;

@@ -15,49 +15,50 @@ struct SeqRange {
     int lq, lk;
 };
 
-__device__ __forceinline__ void seq_range(const AttnArgs &a, int s, SeqRange &r) {
-    if (!a.cu_q) {
-        r.q0 = r.k0 = 0;
-        r.lq = (int)a.Tq;
-        r.lk = (int)a.Tk;
-        return;
-    }
-    // ends that do not rise or that pass the tensors raise the domain flag and leave an empty sequence
-    const int64_t qa = a.cu_q[s], qb = a.cu_q[s + 1], ka = a.cu_k[s], kb = a.cu_k[s + 1];
+// ends that do not rise or that pass the tensors raise the domain flag and leave an empty sequence
+__device__ __forceinline__ void set_range(const AttnArgs &a, int qa, int qb, int ka, int kb, SeqRange &r) {
     const bool ok = qa >= 0 && qa <= qb && qb <= a.Tq && ka >= 0 && ka <= kb && kb <= a.Tk;
     if (!ok) *a.flag = 1u;
     r.q0 = ok ? qa : 0;
     r.k0 = ok ? ka : 0;
-    r.lq = ok ? (int)(qb - qa) : 0;
-    r.lk = ok ? (int)(kb - ka) : 0;
+    r.lq = ok ? qb - qa : 0;
+    r.lk = ok ? kb - ka : 0;
 }
 
-// Tiles of `rows` rows over packed sequences with ends cu[0..n], `each` rows per token: sequence i's tiles take the
-// slots from cu[i] each / rows + i on, which leaves room for ceil(length / rows) of them whatever the lengths are, so the number of
-// slots, T each / rows + n, needs no look at the lengths on the host. Returns the sequence, `tile` its tile, which may
-// lie past its end or, in slots before the first sequence, be -1: nothing to do (tile_rows below).
-__device__ __forceinline__ int slot_sequence(const int32_t *cu, int n, int rows, int slot, int each, int &tile) {
-    if (!cu) {
-        tile = slot;
-        return 0;
+// Tiles of `rows` rows over packed sequences with ends cu[0..n] (the keys' where KEYS), `each` rows per token: sequence i's
+// tiles take the slots from cu[i] each / rows + i on, which leaves room for ceil(length / rows) of them whatever the lengths
+// are, so the number of slots, T each / rows + n, needs no look at the lengths on the host. Gives the slot's sequence in r and
+// returns its tile, which may lie past the sequence's end or, in slots before the first sequence, be -1: nothing to do (tile_in
+// below). Every lane loads one sequence's four ends at once: after the bisection that many sequences need, one trip to memory.
+template <bool KEYS>
+__device__ __forceinline__ int slot_range(const AttnArgs &a, int rows, int slot, int each, SeqRange &r) {
+    if (!a.cu_q) {
+        r.q0 = r.k0 = 0;
+        r.lq = (int)a.Tq;
+        r.lk = (int)a.Tk;
+        return slot;
     }
-    auto start_of = [&](int i) { return (int)((int64_t)cu[i] * each / rows) + i; };
-    int lo = 0, len = n;  // the answer is in [lo, lo + len)
-    while (len > 64) {    // a scalar bisection down to one wave's width
+    const int32_t *cu = KEYS ? a.cu_k : a.cu_q;
+    // (T each is below 2^31; ends that lie outside give a place of no meaning, and their sequence is empty)
+    auto start_of = [&](int end, int i) { return (int)((uint32_t)end * (uint32_t)each / (uint32_t)rows) + i; };
+    int lo = 0, len = a.n_seq;  // the answer is in [lo, lo + len)
+    while (len > 64) {          // a scalar bisection down to one wave's width
         const int half = len / 2;
-        if (start_of(lo + half) <= slot) {
+        if (start_of(cu[lo + half], lo + half) <= slot) {
             lo += half;
             len -= half;
         } else {
             len = half;
         }
     }
-    const int lane = threadIdx.x & 63;
-    const int start = lane < len ? start_of(lo + lane) : 0x7FFFFFFF;
-    const unsigned long long below = __ballot(start <= slot);
-    const int s = __builtin_amdgcn_readfirstlane(lo + (below ? 63 - __builtin_clzll(below) : 0));
-    tile = below ? slot - __builtin_amdgcn_readfirstlane(start_of(s)) : -1;
-    return s;
+    const int lane = threadIdx.x & 63, i = lo + (lane < len ? lane : len - 1);
+    const int qa = a.cu_q[i], qb = a.cu_q[i + 1], ka = a.cu_k[i], kb = a.cu_k[i + 1];
+    const int start = start_of(KEYS ? ka : qa, i);
+    const unsigned long long below = __ballot(lane < len && start <= slot);
+    const int at = __builtin_amdgcn_readfirstlane(below ? 63 - __builtin_clzll(below) : 0);
+    auto of = [&](int v) { return __builtin_amdgcn_readlane(v, at); };
+    set_range(a, of(qa), of(qb), of(ka), of(kb), r);
+    return below ? slot - of(start) : -1;
 }
 
 // Whether a tile of `rows` rows has any of a sequence's n
@@ -68,7 +69,7 @@ template <int THREADS>
 __device__ __forceinline__ void check_ends(const AttnArgs &a) {
     if (!a.cu_q || blockIdx.x != 0 || blockIdx.y != 0) return;
     SeqRange r;
-    for (int s = threadIdx.x; s < a.n_seq; s += THREADS) seq_range(a, s, r);
+    for (int s = threadIdx.x; s < a.n_seq; s += THREADS) set_range(a, a.cu_q[s], a.cu_q[s + 1], a.cu_k[s], a.cu_k[s + 1], r);
 }
 
 // row of register r in the 32 x 32 accumulator of a lane: 8 (r / 4) + 4 (lane / 32) + r % 4
