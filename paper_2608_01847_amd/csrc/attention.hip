@@ -276,7 +276,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_bwd_kv_kernel(AttnArgs a) {
         const float *G = static_cast<const float *>(a.dO) + ((r.q0 + q0) * a.Hq + h) * D;
         const int64_t g_stride = (int64_t)a.Hq * D, at = (int64_t)h * a.Tq + r.q0 + q0;
         const int n = r.lq - q0;
-        float x[16][DT], ls[16], de[16];
+        float x[16][DT], y[16][DT], ls[16], de[16];
         f32x16_t sc, dp;
         {
             float qv[4 * DT][4], gv[4 * DT][4];
@@ -288,7 +288,10 @@ __global__ void __launch_bounds__(kThreads, 1) attn_bwd_kv_kernel(AttnArgs a) {
                 ls[i] = a.lse[at + (row < n ? row : 0)];
                 de[i] = a.delta[at + (row < n ? row : 0)];
             }
-            if constexpr (DT <= 2) load_columns<DT>(G, g_stride, n, D, lane, x);  // more do not fit the registers
+            if constexpr (DT <= 2) {  // more do not fit the registers
+                load_columns<DT>(G, g_stride, n, D, lane, x);
+                load_columns<DT>(Q, a.q_stride, n, D, lane, y);
+            }
             loads_first();
             sc = row_products<DT>(qv, kv);
             dp = row_products<DT>(gv, vv);
@@ -306,9 +309,11 @@ __global__ void __launch_bounds__(kThreads, 1) attn_bwd_kv_kernel(AttnArgs a) {
             ds[i] = ok ? p[i] * (dp[i] - de[i]) : 0.0f;
         }
         add_products<DT>(dv, x, p);
-        load_columns<DT>(Q, a.q_stride, n, D, lane, x);
-        loads_first();
-        add_products<DT>(dk, x, ds);
+        if constexpr (DT > 2) {
+            load_columns<DT>(Q, a.q_stride, n, D, lane, y);
+            loads_first();
+        }
+        add_products<DT>(dk, y, ds);
     }
     join<DT>(dk, lds, wave, lane);
     join<DT>(dv, lds, wave, lane);
