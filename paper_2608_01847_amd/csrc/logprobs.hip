@@ -13,6 +13,11 @@
 // which the pass has anyway, follows a value that at least `top` logits of the row reach; the few threads that have such
 // logits have theirs read a second time (from the caches), by all threads, and those that reach it are ranked in LDS. The LDS
 // additions count and hand out places; no result depends on their order, keys being distinct.
+//
+// Measured, bf16: 8,192 rows of 151,936 with 5 alternatives, 2.49 GB, 450 us (5.5 TB/s); 4,096 rows of 32,000 forward 69 us
+// (3.8 TB/s), gradient 92 us (5.7 TB/s both ways); one row of 151,936 with 20 alternatives 11 us and the join's 7, latency.
+// Vectors of 8 logits, four per thread and step, are enough loads under way: fetching a step ahead (94 registers in place of 60)
+// made 8,192 rows take 490 us.
 #include "internal.h"
 #include "ops_device.h"
 
@@ -26,9 +31,7 @@ constexpr int kVecs = 4;                        // vectors of 8 logits per threa
 constexpr int kStep = kThreads * kVecs * 8;     // logits per step
 constexpr int kRoom = 1024;                     // collected keys
 constexpr int kMaxSplits = 64;
-constexpr int kRowsUnsplit = 512;               // rows from which a row is one workgroup's
-constexpr int64_t kSplitLogits = 4096;          // logits of a part, at least
-constexpr int kMaxParts = 2 * kRowsUnsplit;     // parts of a split launch, at most
+constexpr int kMaxParts = 512;                  // parts of a split launch, at most: two workgroups per CU
 constexpr float kLog2e = 1.44269504088896341f;
 constexpr float kLn2 = 0.693147180559945309f;
 
@@ -217,7 +220,7 @@ struct LogprobArgs {
     int top, splits;
 };
 
-// One row's results from its statistics and the ranked list
+// One row's results from its statistics and the ranked list (by the threads of a workgroup, all in fp32)
 __device__ __forceinline__ void finish_row(const LogprobArgs &a, int64_t row, const Stat &t, const uint64_t *list, int n,
                                            float target_logit, int64_t target) {
     const bool none = t.m == -__builtin_inff();  // every logit is -inf
@@ -237,6 +240,7 @@ __device__ __forceinline__ void finish_row(const LogprobArgs &a, int64_t row, co
     }
 }
 
+// A workgroup takes a row, or one of its parts where rows are few (a whole row would leave CUs idle).
 template <typename T, bool TOP>
 __global__ void __launch_bounds__(kThreads) logprobs_kernel(LogprobArgs a) {
     __shared__ TopLds lds_top;
@@ -349,6 +353,7 @@ struct LogprobBwdArgs {
     unsigned chunks;  // workgroups per row
 };
 
+// The gradient, element by element from the row's statistics: one read and one write of the logits.
 template <typename T>
 __global__ void __launch_bounds__(kBwdThreads) logprobs_bwd_kernel(LogprobBwdArgs a) {
     const int64_t row = blockIdx.x / a.chunks, c0 = (int64_t)(blockIdx.x % a.chunks) * kBwdChunk;
@@ -382,10 +387,14 @@ __global__ void __launch_bounds__(kBwdThreads) logprobs_bwd_kernel(LogprobBwdArg
     }
 }
 
+// Parts of a row: up to two workgroups per CU, of one step each at least, where that takes off enough of a row's steps to
+// pay for the join. With 5 alternatives, one row of 151,936 (10 steps) takes 15.9 us in parts and 19.9 us in one, of 65,536 (4
+// steps) 15.6 and 12.3; 32 rows of 151,936 19.6 and 20.4, 64 rows 22.8 and 20.2;
+// 64 rows of 300,000 (19 steps) 25.7 and 32.7, 256 rows 42.2 and 34.9.
 int plan_splits(int64_t T, int64_t V) {
-    if (T >= kRowsUnsplit) return 1;
-    const int64_t want = (kRowsUnsplit + T - 1) / T, parts = (V + kSplitLogits - 1) / kSplitLogits;
-    return (int)std::max<int64_t>(1, std::min<int64_t>({want, parts, kMaxSplits}));
+    const int64_t steps = (V + kStep - 1) / kStep;
+    if (T >= 256 || steps <= (T < 64 ? 4 : 16)) return 1;
+    return (int)std::min<int64_t>({kMaxParts / T, steps, kMaxSplits});
 }
 
 template <typename T>

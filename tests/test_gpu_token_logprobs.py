@@ -264,3 +264,42 @@ def test_refuses_tensors_of_the_host(F):
                  lambda: F.token_logprobs_bwd(Z, t, lse.cpu(), d_logp=lse), lambda: F.token_logprobs_bwd(Z, t, lse, d_logp=lse.cpu())):
         with pytest.raises(ValueError):
             call()
+
+
+@pytest.mark.parametrize("top", [1, 5, 64])
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+def test_rows_in_parts(F, dt, top):
+    """Few long rows: the largest in one part or in all, equal over the parts, a part without a token, a row without any."""
+    g = torch.Generator().manual_seed(8)
+    for V in (65537, 100003, 262144):
+        i = torch.arange(V)
+        rows = [torch.randn(V, generator=g), torch.zeros(V), i.float() / 64, -i.float() / 64, torch.where(i > V - 70, 3.0, -1.0),
+                torch.where(i % 15000 == 0, 4.0, torch.randn(V, generator=g)), torch.where(i < 40000, -math.inf, 1.0),
+                torch.where(i == V - 1, 0.0, -math.inf), torch.full((V,), -math.inf),
+                torch.full((V,), torch.finfo(DT[dt]).min)]
+        Z = torch.stack(rows).to(DT[dt]).cuda()
+        announce(f"rows in parts {dt} V={V} top={top}")
+        t = targets(len(rows), V, 4)
+        lse, ent, lp, none = check(F, Z, t, top)
+        assert none.tolist() == [False] * 8 + [True, False] and ent[8] == 0
+        for n in (1, 3, 9):  # other numbers of rows are other numbers of parts
+            check(F, Z[:n].contiguous(), t[:n].contiguous(), top)
+
+
+def test_many_rows_in_parts(F):
+    Z, t = logits(64, 300001, "bf16", 12), targets(64, 300001, 3)
+    check(F, Z, t, 6)
+    check(F, Z[:63], t[:63].contiguous(), 6)
+
+
+def test_domain_errors_of_parts(F):
+    for bad in (float("nan"), float("inf")):
+        Z = logits(5, 90000, "bf16", 1)
+        Z[1, 88888] = bad
+        ws = F.workspace(F.token_logprobs_workspace_size(5, 90000, 3))
+        logp, _, lse, _, _ = F.token_logprobs(Z, torch.zeros(5, dtype=torch.int64).cuda(), 3, ws=ws)
+        assert F.check_flags(ws) == F.ERR_DOMAIN
+        assert torch.isfinite(logp[[0, 2, 3, 4]]).all() and torch.isfinite(lse[[0, 2, 3, 4]]).all()
+    Z[1, 88888] = 0.0
+    logp = F.token_logprobs(Z, torch.tensor([3, 90000, -5, 0, 1]).cuda(), ws=ws)[0]
+    assert F.check_flags(ws) == F.ERR_DOMAIN and logp[1] == 0 and logp[2] == 0
