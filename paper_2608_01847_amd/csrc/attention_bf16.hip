@@ -313,15 +313,16 @@ __global__ void __launch_bounds__(kThreads, 2) attn_fwd_bf16_kernel(AttnArgs a, 
     __shared__ __attribute__((aligned(1024))) char smem[4 * G::kBytes];  // K, K, V, V
     constexpr int kRows = 32 * kWaves;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5, col = lane & 31;
-    const int hk = blockIdx.x % a.Hkv, group = a.Hq / a.Hkv, D = a.D;
+    const Place at_work = place<SPLIT>(a.Hkv);
+    const int hk = at_work.hk, part = at_work.part, group = a.Hq / a.Hkv, D = a.D;
     SeqRange r;
-    const int tile = slot_range<false>(a, kRows, (int)(gridDim.x / a.Hkv - 1 - blockIdx.x / a.Hkv), group, r);
+    const int tile = slot_range<false>(a, kRows, at_work.slot, group, r);
     check_ends<kThreads>(a);
     if (!tile_in(tile, kRows, (int64_t)r.lq * group)) return;
     RowTile w;
     w.init(a, r, tile, hk, wave, col);
     const int per = SPLIT ? (w.nk + (int)gridDim.y - 1) / (int)gridDim.y : w.nk;
-    const int j0 = SPLIT ? (int)blockIdx.y * per : 0, nk = SPLIT && j0 + per < w.nk ? j0 + per : w.nk;  // tiles j0 .. nk - 1
+    const int j0 = SPLIT ? part * per : 0, nk = SPLIT && j0 + per < w.nk ? j0 + per : w.nk;  // tiles j0 .. nk - 1
     const int seen = w.seen, all_seen = w.all_seen, any_seen = w.any_seen, q = w.q, h = w.h;
     const bool ok = w.ok;
 
@@ -468,7 +469,7 @@ __global__ void __launch_bounds__(kThreads, 2) attn_fwd_bf16_kernel(AttnArgs a, 
     }
     l = sum_halves(l);
     if constexpr (SPLIT) {
-        const int64_t at = ((int64_t)blockIdx.y * a.Hq + h) * a.Tq + r.q0 + q;
+        const int64_t at = ((int64_t)part * a.Hq + h) * a.Tq + r.q0 + q;
         if (ok && half == 0) {
             parts.m[at] = m;
             parts.l[at] = l;
@@ -543,9 +544,10 @@ __global__ void __launch_bounds__(kThreads, 2) attn_bwd_q_bf16_kernel(AttnArgs a
     __shared__ __attribute__((aligned(1024))) char smem[4 * G::kBytes];  // K, K, V, V
     constexpr int kRows = 32 * kWaves;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5, col = lane & 31;
-    const int hk = blockIdx.x % a.Hkv, group = a.Hq / a.Hkv, D = a.D;
+    const Place at_work = place<SPLIT>(a.Hkv);
+    const int hk = at_work.hk, part = at_work.part, group = a.Hq / a.Hkv, D = a.D;
     SeqRange r;
-    const int tile = slot_range<false>(a, kRows, (int)(gridDim.x / a.Hkv - 1 - blockIdx.x / a.Hkv), group, r);
+    const int tile = slot_range<false>(a, kRows, at_work.slot, group, r);
     check_ends<kThreads>(a);
     if (!tile_in(tile, kRows, (int64_t)r.lq * group)) return;
     RowTile w;
@@ -561,7 +563,7 @@ __global__ void __launch_bounds__(kThreads, 2) attn_bwd_q_bf16_kernel(AttnArgs a
 #pragma unroll
         for (int e = 0; e < 8; e++) delta = __builtin_fmaf((float)qv[i][e], (float)gv[i][e], delta);
     delta = sum_halves(delta);
-    if (w.ok && half == 0 && blockIdx.y == 0) a.delta[stat] = delta;
+    if (w.ok && half == 0 && part == 0) a.delta[stat] = delta;
     load_row<DT>(static_cast<const uint16_t *>(a.q) + (r.q0 + w.q) * a.q_stride + (int64_t)w.h * D, w.ok, D, half, qv);
     const float c = a.scale * kLog2e;
     const float lse2 = w.ok ? a.lse[stat] * kLog2e : 0.0f;
@@ -576,7 +578,7 @@ __global__ void __launch_bounds__(kThreads, 2) attn_bwd_q_bf16_kernel(AttnArgs a
     f.init(lane, base);
     f32x16_t dq[DT] = {};
     const int per = SPLIT ? (w.nk + (int)gridDim.y - 1) / (int)gridDim.y : w.nk;
-    const int j0 = SPLIT ? (int)blockIdx.y * per : 0, nk = SPLIT && j0 + per < w.nk ? j0 + per : w.nk;  // tiles j0 .. nk - 1
+    const int j0 = SPLIT ? part * per : 0, nk = SPLIT && j0 + per < w.nk ? j0 + per : w.nk;  // tiles j0 .. nk - 1
     if (j0 < nk) {
         ks.load(K, a.k_stride, j0 * kKeys, r.lk, D, base, wave);
         vs.load(V, a.v_stride, j0 * kKeys, r.lk, D, base + 2 * G::kBytes, wave);
@@ -660,7 +662,7 @@ __global__ void __launch_bounds__(kThreads, 2) attn_bwd_q_bf16_kernel(AttnArgs a
         if (j + 1 < nk) iteration(j + 1, std::integral_constant<int, 1>{});
     }
     if constexpr (SPLIT) {
-        store_part<DT>(parts.dq + (((int64_t)blockIdx.y * a.Tq + r.q0 + w.q) * a.Hq + w.h) * D, w.ok, D, half, dq);
+        store_part<DT>(parts.dq + (((int64_t)part * a.Tq + r.q0 + w.q) * a.Hq + w.h) * D, w.ok, D, half, dq);
         return;
     }
     store_row<DT>(static_cast<uint16_t *>(a.dq) + (r.q0 + w.q) * a.dq_stride + (int64_t)w.h * D, w.ok, D, half, dq, a.scale);
@@ -688,9 +690,10 @@ __global__ void __launch_bounds__(kThreads, 2) attn_bwd_kv_bf16_kernel(AttnArgs 
     __shared__ __attribute__((aligned(1024))) char smem[4 * G::kBytes + (kWide ? 2 * GV::kBytes : 0)];  // q, q, dO, dO, v
     __shared__ __attribute__((aligned(16))) float stats[2][2][kQ];  // [stage][-lse / scale, -delta]
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5, col = lane & 31;
-    const int hk = blockIdx.x % a.Hkv, group = a.Hq / a.Hkv, D = a.D;
+    const Place at_work = place<SPLIT>(a.Hkv);
+    const int hk = at_work.hk, part = at_work.part, group = a.Hq / a.Hkv, D = a.D;
     SeqRange r;
-    const int tile = slot_range<true>(a, kRows, (int)(blockIdx.x / a.Hkv), 1, r);
+    const int tile = slot_range<true>(a, kRows, at_work.slot, 1, r);
     check_ends<kThreads>(a);
     if (!tile_in(tile, kRows, r.lk)) return;
     const int shift = r.lk - r.lq, w_first = tile * kRows + 32 * wave, k = w_first + col;
@@ -702,7 +705,7 @@ __global__ void __launch_bounds__(kThreads, 2) attn_bwd_kv_bf16_kernel(AttnArgs 
     const int any_from = seen_from(w_first), all_from = seen_from(w_first + 31);
     const int per_head = r.lq > q_first ? (r.lq - q_first + kQ - 1) / kQ : 0;
     const int all_items = per_head * group;
-    const int per = SPLIT ? (all_items + (int)gridDim.y - 1) / (int)gridDim.y : all_items, i0 = SPLIT ? (int)blockIdx.y * per : 0;
+    const int per = SPLIT ? (all_items + (int)gridDim.y - 1) / (int)gridDim.y : all_items, i0 = SPLIT ? part * per : 0;
     const int items = i0 + per < all_items ? per : all_items - i0;  // this workgroup's, none or fewer possibly
     const int head0 = i0 % group, q_start = q_first + (per_head - 1 - i0 / group) * kQ;
 
@@ -869,7 +872,7 @@ __global__ void __launch_bounds__(kThreads, 2) attn_bwd_kv_bf16_kernel(AttnArgs 
         if (it + 1 < items) iteration(it + 1, std::integral_constant<int, 1>{});
     }
     if constexpr (SPLIT) {
-        const int64_t at = (((int64_t)blockIdx.y * a.Tk + r.k0 + k) * a.Hkv + hk) * D;
+        const int64_t at = (((int64_t)part * a.Tk + r.k0 + k) * a.Hkv + hk) * D;
         store_part<DT>(parts.dk + at, ok, D, half, dk);
         store_part<DT>(parts.dv + at, ok, D, half, dv);
         return;

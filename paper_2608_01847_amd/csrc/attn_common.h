@@ -15,9 +15,13 @@ struct SeqRange {
     int lq, lk;
 };
 
+__device__ __forceinline__ bool ends_ok(const AttnArgs &a, int qa, int qb, int ka, int kb) {
+    return qa >= 0 && qa <= qb && qb <= a.Tq && ka >= 0 && ka <= kb && kb <= a.Tk;
+}
+
 // ends that do not rise or that pass the tensors raise the domain flag and leave an empty sequence
 __device__ __forceinline__ void set_range(const AttnArgs &a, int qa, int qb, int ka, int kb, SeqRange &r) {
-    const bool ok = qa >= 0 && qa <= qb && qb <= a.Tq && ka >= 0 && ka <= kb && kb <= a.Tk;
+    const bool ok = ends_ok(a, qa, qb, ka, kb);
     if (!ok) *a.flag = 1u;
     r.q0 = ok ? qa : 0;
     r.k0 = ok ? ka : 0;
@@ -26,24 +30,32 @@ __device__ __forceinline__ void set_range(const AttnArgs &a, int qa, int qb, int
 }
 
 // Tiles of `rows` rows over packed sequences with ends cu[0..n] (the keys' where KEYS), `each` rows per token: sequence i's
-// tiles take the slots from cu[i] each / rows + i on, which leaves room for ceil(length / rows) of them whatever the lengths
+// tiles have the slots from cu[i] each / rows + i on, which leaves room for ceil(length / rows) of them whatever the lengths
 // are, so the number of slots, T each / rows + n, needs no look at the lengths on the host. Gives the slot's sequence in r and
-// returns its tile, which may lie past the sequence's end or, in slots before the first sequence, be -1: nothing to do (tile_in
-// below). Every lane loads one sequence's four ends at once: after the bisection that many sequences need, one trip to memory.
+// returns its tile, which may lie past the sequence's end or be negative: nothing to do (tile_in below).
+//
+// Under a causal mask a tile's work grows with the rows before it (KEYS: behind it). The slots of kOrdered sequences, one after
+// the other, are then given out from the longest tiles to the shortest, over those sequences together: workgroups start in
+// the order of the slots, and what starts last should end soonest. ORDERED
+//
+// Every lane loads one sequence's four ends at once: after the bisection that many sequences need, one trip to memory.
+constexpr int kOrdered = 8;
+
 template <bool KEYS>
 __device__ __forceinline__ int slot_range(const AttnArgs &a, int rows, int slot, int each, SeqRange &r) {
+    // (T each is below 2^31; ends that lie outside give a place of no meaning, and their sequence is empty)
+    auto tiles_of = [&](int tokens) { return (int)(((uint32_t)tokens * (uint32_t)each + (uint32_t)rows - 1) / (uint32_t)rows); };
     if (!a.cu_q) {
         r.q0 = r.k0 = 0;
         r.lq = (int)a.Tq;
         r.lk = (int)a.Tk;
-        return slot;
+        return KEYS || !a.causal ? slot : tiles_of(r.lq) - 1 - slot;
     }
     const int32_t *cu = KEYS ? a.cu_k : a.cu_q;
-    // (T each is below 2^31; ends that lie outside give a place of no meaning, and their sequence is empty)
     auto start_of = [&](int end, int i) { return (int)((uint32_t)end * (uint32_t)each / (uint32_t)rows) + i; };
     int lo = 0, len = a.n_seq;  // the answer is in [lo, lo + len)
-    while (len > 64) {          // a scalar bisection down to one wave's width
-        const int half = len / 2;
+    while (len > 64) {          // a scalar bisection down to one wave's width, by whole runs of kOrdered
+        const int half = len / 2 / kOrdered * kOrdered;
         if (start_of(cu[lo + half], lo + half) <= slot) {
             lo += half;
             len -= half;
@@ -55,10 +67,53 @@ __device__ __forceinline__ int slot_range(const AttnArgs &a, int rows, int slot,
     const int qa = a.cu_q[i], qb = a.cu_q[i + 1], ka = a.cu_k[i], kb = a.cu_k[i + 1];
     const int start = start_of(KEYS ? ka : qa, i);
     const unsigned long long below = __ballot(lane < len && start <= slot);
-    const int at = __builtin_amdgcn_readfirstlane(below ? 63 - __builtin_clzll(below) : 0);
-    auto of = [&](int v) { return __builtin_amdgcn_readlane(v, at); };
+    int at = __builtin_amdgcn_readfirstlane(below ? 63 - __builtin_clzll(below) : 0);
+    int tile = below ? slot - __builtin_amdgcn_readlane(start, at) : -1;
+    if (a.causal && below) {
+        const int first = at / kOrdered * kOrdered, p = slot - __builtin_amdgcn_readlane(start, first);
+        const int own = lane < len && ends_ok(a, qa, qb, ka, kb) ? tiles_of(KEYS ? kb - ka : qb - qa) : 0;
+        int tiles[kOrdered], most = 0;
+#pragma unroll
+        for (int j = 0; j < kOrdered; j++) {
+            tiles[j] = __builtin_amdgcn_readlane(own, first + j);
+            most = tiles[j] > most ? tiles[j] : most;
+        }
+        auto longer = [&](int v) {  // tiles of more than v units of work
+            int n = 0;
+#pragma unroll
+            for (int j = 0; j < kOrdered; j++) n += tiles[j] > v ? tiles[j] - v : 0;
+            return n;
+        };
+        int v = 0, high = most;  // this slot's work: the least v that no more than p tiles pass
+        while (v < high) {
+            const int mid = (v + high) / 2;
+            if (longer(mid) <= p) high = mid;
+            else v = mid + 1;
+        }
+        int left = p - longer(v);  // tiles of the same work before this one
+        tile = -1;
+#pragma unroll
+        for (int j = 0; j < kOrdered; j++) {
+            if (tiles[j] >= v && left-- == 0 && v > 0) {
+                at = first + j;
+                tile = KEYS ? tiles[j] - v : v - 1;
+            }
+        }
+    }
+    auto of = [&](int x) { return __builtin_amdgcn_readlane(x, at); };
     set_range(a, of(qa), of(qb), of(ka), of(kb), r);
-    return below ? slot - of(start) : -1;
+    return tile;
+}
+
+// The key-value head, the slot and the part of a split sum that a workgroup takes: heads in turn (consecutive workgroups go to
+// different XCDs, so that an XCD's L2 sees few heads), a slot's parts one after the other.
+struct Place {
+    int hk, slot, part;
+};
+template <bool SPLIT>
+__device__ __forceinline__ Place place(int Hkv) {
+    const uint32_t flat = SPLIT ? blockIdx.y * gridDim.x + blockIdx.x : blockIdx.x, rest = flat / (uint32_t)Hkv;
+    return {(int)(flat - rest * (uint32_t)Hkv), (int)(SPLIT ? rest / gridDim.y : rest), (int)(SPLIT ? rest % gridDim.y : 0u)};
 }
 
 // Whether a tile of `rows` rows has any of a sequence's n
