@@ -302,9 +302,9 @@ struct RowTile {
 // Forward of 128 query rows. Bound: two products of 4 D flops a visible pair on the matrix instructions, and an exponential
 // per pair, a quarter-rate instruction: 256 of about 500 vector cycles beside 512 of the matrix unit for a wave's 32 x 32 pairs
 // and 128 features. Two waves per SIMD (210 registers, 64 KB of LDS twice) overlap the two. Measured with 32/8 heads of 128,
-// causal: 16,384 tokens 2.09 ms, 1.05 PFLOP/s (a bf16 product of 8,192^3 reaches 1.38); 32 x 2,048 tokens 1.31-1.40 ms, 0.79-0.84, the
-// matrix units busy half of the cycles, no LDS bank conflicts; a workgroup's start and end, about 7 of its 41 us there, are
-// hidden only by the other one on its CU.
+// causal: 16,384 tokens 2.09 ms, 1.05 PFLOP/s (a bf16 product of 8,192^3 reaches 1.38), matrix units busy 53% of the cycles; 32 x
+// 2,048 tokens 1.31-1.40 ms, 0.79-0.84, busy 42%: a workgroup's start and end, about 7 of its 41 us there, are hidden only
+// by the other one on its CU. No LDS bank conflicts.
 // SPLIT: the tiles of keys are dealt to gridDim.y workgroups, each leaving its unnormalised output, reference and sum in
 // fp32 for attn_join_kernel. One query of 32/8 heads over 8,192 keys: 10 us and the join's 5, of 33 MB at 3.2 TB/s; latency.
 template <int DT, bool SPLIT>
@@ -533,7 +533,7 @@ __global__ void __launch_bounds__(kThreads) attn_join_kernel(AttnArgs a, AttnPar
 // dq of 128 query rows, and delta = rowsum(dO O) for the keys' pass. Both score-shaped products are transposed as in the
 // forward, so dS is the B operand of dq^T = k^T dS^T as it stands.
 // Bound: three products of 2 D flops a visible pair and an exponential. 32 x 2,048 tokens, 32/8 heads of 128, causal: 1.72 ms,
-// 0.96 PFLOP/s, matrix units busy 48%. Two waves per SIMD, 256 registers.
+// 0.96 PFLOP/s, matrix units busy 51%. Two waves per SIMD, 256 registers.
 // dS is rounded to bf16 for its product (an error of 0.0017 of the gradient's size on normal inputs, as much as rounding the
 // result), and delta comes from the O that the forward rounded (0.0014): carrying dS in two halves, or delta from fp32
 // products formed again, would add a quarter to the matrix work.
@@ -675,8 +675,8 @@ __global__ void __launch_bounds__(kThreads, 2) attn_bwd_q_bf16_kernel(AttnArgs a
 // Here a lane's column is a key and the queries run down the accumulators (S = q k^T as it is written): P and dS are the
 // B operands of dv^T = dO^T P and dk^T = q^T dS. Queries and their gradients go through LDS in tiles with their lse and delta,
 // from which the accumulators start; a query that does not exist, or sees nothing, has probability 0.
-// Bound: four products of 2 D flops a visible pair and an exponential. 32 x 2,048 tokens, 32/8 heads of 128, causal: 2.2 ms,
-// 1.0 PFLOP/s, matrix units busy 53%, no bank conflicts. P and dS are rounded to bf16 as in the other kernels.
+// Bound: four products of 2 D flops a visible pair and an exponential. 32 x 2,048 tokens, 32/8 heads of 128, causal: 2.1 ms,
+// 1.05 PFLOP/s, matrix units busy 56%, no bank conflicts. P and dS are rounded to bf16 as in the other kernels.
 // Two waves per SIMD, whose 256 registers hold the sums (64 per gradient and 128 features) and k: from 65 features on, v is read
 // from LDS each time and the tiles have 32 queries rather than 64.
 // SPLIT: the tiles of queries, all heads together, are dealt to gridDim.y workgroups, whose sums attn_grad_join_kernel adds.
@@ -949,7 +949,8 @@ hipError_t launch_attn_fwd_bf16(const AttnArgs &a, void *ws, hipStream_t st) {
 // Parts of a backward's sums. Where workgroups are few, one's run through all queries (keys) of a long sequence is the whole
 // call's time: they are split until two per CU are busy, with 4 tiles each at least by the mean length. The keys' pass, whose
 // runs over a causal sequence are from one to all of its queries long, is split on until there are four times as many with 64
-// tiles each, so that long and short ones even out (four sequences of 2,048 with 64/8 heads 1.46 ms in place of 1.52). A part
+// tiles each, so that long and short ones even out (backward of four sequences of 2,048 with 64/8 heads 1.03 ms, 1.08 without
+// these parts and 1.11 with twice as many; of one of 8,192 3.4, 4.1 and 3.4). A part
 // costs 64 KB of fp32 sums per 128 rows and gradient, written and read again: splitting either pass up to 2,048 workgroups
 // with 8 tiles each made two sequences of 2,500 with 16/8 heads take 554 us in place of 462.
 AttnBwdPlan plan_attn_bwd_bf16(int64_t Tq, int64_t Tk, int Hq, int Hkv, int64_t n_seq) {

@@ -15,7 +15,7 @@
 // additions count and hand out places; no result depends on their order, keys being distinct.
 //
 // Measured, bf16: 8,192 rows of 151,936 with 5 alternatives, 2.49 GB, 450 us (5.5 TB/s); 4,096 rows of 32,000 forward 69 us
-// (3.8 TB/s), gradient 92 us (5.7 TB/s both ways); one row of 151,936 with 20 alternatives 11 us and the join's 7, latency.
+// (3.8 TB/s), gradient 92 us (5.7 TB/s both ways); one row of 151,936 with 20 alternatives 11 us and the join's 8, latency.
 // Vectors of 8 logits, four per thread and step, are enough loads under way: fetching a step ahead (94 registers in place of 60)
 // made 8,192 rows take 490 us.
 #include "internal.h"
