@@ -435,8 +435,8 @@ size_t focus_attention_workspace_size(int call, const focus_attention_config *cf
  *   lse_opt [heads_q][Tq] fp32 (the backward needs it).
  *   cu_q, cu_k : DEVICE arrays of n_seq + 1 int32, sequence s holding queries cu_q[s] .. cu_q[s + 1] - 1 and keys
  *               cu_k[s] .. cu_k[s + 1] - 1; they may be one array. Both NULL: one sequence of everything (n_seq == 1).
- *               They rise and lie in [0, Tq] and [0, Tk]; a pair that does not raises the domain flag, its sequence is
- *               treated as empty and its rows' results are unspecified. Rows of no sequence are neither read nor written.
+ *               They rise and lie in [0, Tq] and [0, Tk]; a pair that does not raises the domain flag and leaves the
+ *               call's results unspecified (nothing outside the tensors is touched). Rows of no sequence are neither read nor written.
  *   A query that sees no key (none there, or causal with fewer keys than queries) has O = 0 and lse = -inf.
  *   Nothing outside a query's own sequence reaches its output, NaN and infinities included. A hidden key of its own
  *   sequence does not either, as long as its v is finite.

@@ -379,3 +379,16 @@ def test_refuses_what_would_reach_a_kernel_wrongly(F):
                  lambda: F.attention_bwd(q, q, q, q, O, lse, out=(q, wide, q))):
         with pytest.raises(ValueError):
             call()
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("n", [9, 64, 75, 140])
+def test_many_sequences_of_different_lengths(F, n, dt):
+    """Every tile is taken once, whatever the lengths of the sequences whose tiles are given out together."""
+    g = torch.Generator().manual_seed(n)
+    lk = [int(x) for x in torch.randint(0, 60, (n,), generator=g)]
+    for i in range(0, n, 13):
+        lk[i] = 200 + 5 * i
+    lq = [x if i % 3 else x // 2 for i, x in enumerate(lk)]
+    run_case(F, lk, lk, 2, 1, 32, dt, True, seed=n)
+    run_case(F, lq, lk, 4, 2, 16, dt, True, seed=n + 1)
