@@ -1,0 +1,94 @@
+"""GPU tests of the attention kernels whose sums are split into parts, at every width of head that has kernels of its own.
+
+Reference and bounds are those of test_gpu_attention. The workspace is full of NaN past its header, so that a part which a
+kernel does not write, or one that it reads without need, shows in the result.
+"""
+import pytest
+import torch
+
+from gpu_common import require_gpu
+from test_gpu_attention import run_case
+
+pytestmark = pytest.mark.gpu
+
+HEADER = 256
+
+
+class DirtyWorkspaces:
+    """The binding with workspaces of 0xFF bytes (NaN in fp32) behind a cleared header."""
+
+    def __init__(self, F):
+        self.F = F
+
+    def __getattr__(self, name):
+        return getattr(self.F, name)
+
+    def workspace(self, nbytes, device="cuda"):
+        ws = self.F.workspace(nbytes, device)
+        ws[HEADER:] = 0xFF
+        return ws
+
+
+@pytest.fixture(scope="module")
+def F():
+    return DirtyWorkspaces(require_gpu())
+
+
+def sizes(F, lq, lk, Hq, Hkv, D):
+    """Workspace bytes of the forward and the backward that the parts take."""
+    import ctypes
+    cfg = F.AttentionConfig(Hq, Hkv, D, 1, 1.0, 0, *(0,) * 6)
+    size = lambda call: F.lib().focus_attention_workspace_size(call, ctypes.byref(cfg), sum(lq), sum(lk), len(lq))
+    delta = -(-sum(lq) * Hq * 4 // 256) * 256
+    return size(F.CALL_ATTENTION_FWD) - HEADER, size(F.CALL_ATTENTION_BWD) - HEADER - delta
+
+
+@pytest.mark.parametrize("D", [8, 64, 72, 80, 96, 104, 128])
+@pytest.mark.parametrize("causal", [True, False])
+def test_two_sequences_in_parts(F, D, causal):
+    lengths = [700, 301]
+    fwd, bwd = sizes(F, lengths, lengths, 4, 1, D)
+    dq, dkv = 1001 * 4 * D * 4, 2 * 1001 * D * 4
+    assert fwd > 0 and bwd >= 2 * dq + 2 * dkv  # the forward, dq, and dk with dv, in two parts at least
+    run_case(F, lengths, lengths, 4, 1, D, "bf16", causal, seed=D)
+
+
+@pytest.mark.parametrize("D", [64, 80, 128])
+@pytest.mark.parametrize("causal", [True, False])
+def test_few_queries_in_parts(F, D, causal):
+    """Some parts hold no key that a query sees."""
+    for lq, lk in (([3], [2000]), ([1, 1], [40, 1900]), ([0, 5], [600, 700])):
+        assert sizes(F, lq, lk, 4, 2, D)[0] > 0
+        run_case(F, lq, lk, 4, 2, D, "bf16", causal, seed=D)
+
+
+@pytest.mark.parametrize("D", [40, 96, 128])
+def test_no_parts(F, D):
+    lengths = [70, 1, 0, 129]
+    run_case(F, lengths, lengths, 4, 2, D, "bf16", True, seed=D)
+    run_case(F, lengths, lengths, 4, 2, D, "f32", True, seed=D)
+
+
+@pytest.mark.parametrize("scale", [0.02, 0.0, -0.1])
+@pytest.mark.parametrize("D", [64, 96, 128])
+def test_scales_of_both_signs(F, D, scale):
+    """Also where v is read from LDS (from 65 features on) and the rows' statistics are divided by the scale."""
+    for lengths in ([50], [900]):  # in one part, in several
+        run_case(F, lengths, lengths, 2, 1, D, "bf16", True, seed=D, scale=scale)
+    run_case(F, [50], [50], 2, 1, D, "f32", True, seed=D, scale=scale)
+
+
+def test_parts_of_sequences_with_rows_before_and_behind(F):
+    """Rows of no sequence have no parts: the join neither reads nor writes them."""
+    T, cu = 900, torch.tensor([130, 500, 770], dtype=torch.int32).cuda()
+    g = torch.Generator().manual_seed(5)
+    q, k, v, dO = (torch.randn(T, 2, 80, generator=g).bfloat16().cuda() for _ in range(4))
+    ws = F.workspace(F.attention_workspace_size(q, k, 2))
+    assert sizes(F, [T - 1, 1], [T - 1, 1], 2, 2, 80)[1] > 0
+    O, lse = torch.full_like(q, 7.0), torch.full((2, T), 7.0).cuda()
+    F.attention_fwd(q, k, v, cu, ws=ws, out=O, lse=lse)
+    out = tuple(torch.full_like(q, 7.0) for _ in range(3))
+    F.attention_bwd(dO, q, k, v, O, lse, cu, ws=ws, out=out)
+    for x in (O, lse.t(), *out):
+        assert (x[:130] == 7.0).all() and (x[770:] == 7.0).all() and torch.isfinite(x[130:770]).all()
+    assert F.check_flags(ws) == F.OK
