@@ -450,11 +450,10 @@ def norm_workspace_size(T: int, C: int) -> int:
 
 
 def _sized(ws: torch.Tensor | None, need: int, device) -> torch.Tensor:
-    """ws if it does, else a workspace of `need` bytes of which only the header is cleared."""
-    if need == 0:
-        need = 256  # the call itself reports what is wrong with its arguments
-    if ws is None or ws.numel() < need:
-        ws = torch.empty(need, dtype=torch.uint8, device=device)
+    """ws, or where none is given one of `need` bytes of which only the header is cleared. A given workspace is never replaced:
+    its header is where the caller looks for the domain flag, and the call refuses one that is too small."""
+    if ws is None:
+        ws = torch.empty(max(need, 256), dtype=torch.uint8, device=device)  # need is 0 for arguments that the call refuses
         ws[:256].zero_()
     return ws
 
@@ -561,7 +560,8 @@ def _attention_inputs(q, k, v, cu_q, cu_k):
 
 
 def attention_workspace_size(q: torch.Tensor, k: torch.Tensor, n_seq: int = 1) -> int:
-    """Workspace bytes of attention_fwd and attention_bwd on tensors of these shapes, packed into n_seq sequences."""
+    """Workspace bytes of attention_fwd and attention_bwd on tensors of these shapes, packed into n_seq sequences. Fewer queries
+    may need more (their keys are split): take the largest over the shapes that are called."""
     c = _attention_config(q, k, 0, 1.0)
     size = lib().focus_attention_workspace_size
     return max(int(size(call, ctypes.byref(c), q.shape[0], k.shape[0], n_seq))
