@@ -113,10 +113,12 @@ typedef enum {
     FOCUS_CALL_FAKEQUANT_WEIGHTS = 10,
     FOCUS_CALL_NORM_FWD = 11,       /* M = tokens, K = features */
     FOCUS_CALL_NORM_BWD = 12,       /* M = tokens, K = features */
-    FOCUS_CALL_ATTENTION_FWD = 13,  /* sized by focus_attention_workspace_size */
-    FOCUS_CALL_ATTENTION_BWD = 14,  /* sized by focus_attention_workspace_size */
+    FOCUS_CALL_ATTENTION_FWD = 13,  /* sized by focus_attention_workspace_size: bf16, which does for fp32 too */
+    FOCUS_CALL_ATTENTION_BWD = 14,
     FOCUS_CALL_TOKEN_LOGPROBS = 15, /* M = tokens, N = vocabulary, K = alternatives (`top`) */
-    FOCUS_CALL_TOKEN_LOGPROBS_BWD = 16
+    FOCUS_CALL_TOKEN_LOGPROBS_BWD = 16,
+    FOCUS_CALL_ATTENTION_FWD_F32 = 17,  /* sized by focus_attention_workspace_size: fp32, no more than bf16 */
+    FOCUS_CALL_ATTENTION_BWD_F32 = 18
 } focus_call;
 
 /* Workspace bytes a call needs for the given sizes (M = tokens, N = rows / out features,
@@ -424,9 +426,11 @@ typedef struct {
     int64_t dq_stride, dk_stride, dv_stride;
 } focus_attention_config;
 
-/* Workspace bytes of focus_attention_fwd (call = FOCUS_CALL_ATTENTION_FWD) and focus_attention_bwd
- * (FOCUS_CALL_ATTENTION_BWD). They do not grow with the shape alone: fewer queries may be split into more parts, so ask
- * for every shape that is called, and take the largest. Host-only; 0 for invalid arguments. */
+/* Workspace bytes of focus_attention_fwd (call = FOCUS_CALL_ATTENTION_FWD, on fp32 tensors FOCUS_CALL_ATTENTION_FWD_F32) and
+ * focus_attention_bwd (FOCUS_CALL_ATTENTION_BWD, FOCUS_CALL_ATTENTION_BWD_F32). In bf16 they do not grow with the shape alone:
+ * fewer queries may be split into more parts, so ask for every shape that is called, and take the largest. fp32 sums are not
+ * split: the forward needs the 256 bytes of the header, the backward 4 bytes more per query and head. Host-only; 0 for
+ * invalid arguments. */
 size_t focus_attention_workspace_size(int call, const focus_attention_config *cfg, int64_t Tq, int64_t Tk, int64_t n_seq);
 
 /* Attention over whole prompts, several sequences packed one after the other without padding:

@@ -551,8 +551,12 @@ focus_status focus_norm_bwd(int kind, const void *dY, const void *H, int dtype, 
 size_t focus_attention_workspace_size(int call, const focus_attention_config *cfg, int64_t Tq, int64_t Tk, int64_t n_seq) {
     AttnArgs a;
     if (attention_args(cfg, Tq, Tk, n_seq, a) != FOCUS_OK) return 0;
-    if (call == FOCUS_CALL_ATTENTION_FWD) return attn_fwd_ws(Tq, Tk, a.Hq, a.Hkv, a.D, n_seq);
-    if (call == FOCUS_CALL_ATTENTION_BWD) return attn_bwd_ws(Tq, Tk, a.Hq, a.Hkv, a.D, n_seq);
+    switch (call) {
+        case FOCUS_CALL_ATTENTION_FWD: return attn_fwd_ws(FOCUS_BF16, Tq, Tk, a.Hq, a.Hkv, a.D, n_seq);
+        case FOCUS_CALL_ATTENTION_BWD: return attn_bwd_ws(FOCUS_BF16, Tq, Tk, a.Hq, a.Hkv, a.D, n_seq);
+        case FOCUS_CALL_ATTENTION_FWD_F32: return attn_fwd_ws(FOCUS_F32, Tq, Tk, a.Hq, a.Hkv, a.D, n_seq);
+        case FOCUS_CALL_ATTENTION_BWD_F32: return attn_bwd_ws(FOCUS_F32, Tq, Tk, a.Hq, a.Hkv, a.D, n_seq);
+    }
     return 0;
 }
 
@@ -566,7 +570,7 @@ focus_status focus_attention_fwd(const focus_attention_config *cfg, const void *
     FOCUS_TRY(check_ends(cu_q, cu_k, n_seq));
     if (!all_aligned({q, k, v, O}) || !strides_ok(a, dtype) || (reinterpret_cast<uintptr_t>(lse_opt) & 3u))
         return FOCUS_ERR_SHAPE;
-    FOCUS_TRY(check_ws(ws, ws_bytes, attn_fwd_ws(Tq, Tk, a.Hq, a.Hkv, a.D, n_seq)));
+    FOCUS_TRY(check_ws(ws, ws_bytes, attn_fwd_ws(dtype, Tq, Tk, a.Hq, a.Hkv, a.D, n_seq)));
     if (Tq == 0 || n_seq == 0) return FOCUS_OK;
     a.q = q, a.k = k, a.v = v, a.O = O, a.lse = lse_opt, a.cu_q = cu_q, a.cu_k = cu_k, a.flag = flag_of(ws);
     return hip_status(launch_attn_fwd(dtype, a, ws, (hipStream_t)stream));
@@ -583,7 +587,7 @@ focus_status focus_attention_bwd(const focus_attention_config *cfg, const void *
     FOCUS_TRY(check_ends(cu_q, cu_k, n_seq));
     if (!all_aligned({q, k, v, O, dO, dq, dk, dv}) || !strides_ok(a, dtype) || (reinterpret_cast<uintptr_t>(lse) & 3u))
         return FOCUS_ERR_SHAPE;
-    FOCUS_TRY(check_ws(ws, ws_bytes, attn_bwd_ws(Tq, Tk, a.Hq, a.Hkv, a.D, n_seq)));
+    FOCUS_TRY(check_ws(ws, ws_bytes, attn_bwd_ws(dtype, Tq, Tk, a.Hq, a.Hkv, a.D, n_seq)));
     if ((Tq == 0 && Tk == 0) || n_seq == 0) return FOCUS_OK;
     a.q = q, a.k = k, a.v = v, a.O = const_cast<void *>(O), a.dO = dO, a.lse = const_cast<float *>(lse);
     a.dq = dq, a.dk = dk, a.dv = dv, a.cu_q = cu_q, a.cu_k = cu_k, a.flag = flag_of(ws);

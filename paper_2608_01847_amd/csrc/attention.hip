@@ -353,16 +353,16 @@ hipError_t bwd(const AttnArgs &a, hipStream_t st) {
 
 }  // namespace
 
-size_t attn_fwd_ws(int64_t Tq, int64_t Tk, int Hq, int Hkv, int D, int64_t n_seq) {
-    const int splits = attn_splits_bf16(Tq, Tk, Hq, Hkv, n_seq);
+size_t attn_fwd_ws(int dtype, int64_t Tq, int64_t Tk, int Hq, int Hkv, int D, int64_t n_seq) {
+    const int splits = dtype == kBF16 ? attn_splits_bf16(Tq, Tk, Hq, Hkv, n_seq) : 1;  // the fp32 kernels have no parts
     if (splits == 1) return kWsHeader;
     return kWsHeader + attn_part_stats(splits, Tq * Hq) + (size_t)splits * (size_t)(Tq * Hq) * (size_t)D * sizeof(float);
 }
 
 static size_t delta_bytes(int64_t Tq, int Hq) { return ((size_t)Tq * (size_t)Hq * sizeof(float) + 255) / 256 * 256; }
 
-size_t attn_bwd_ws(int64_t Tq, int64_t Tk, int Hq, int Hkv, int D, int64_t n_seq) {
-    const AttnBwdPlan p = plan_attn_bwd_bf16(Tq, Tk, Hq, Hkv, n_seq);
+size_t attn_bwd_ws(int dtype, int64_t Tq, int64_t Tk, int Hq, int Hkv, int D, int64_t n_seq) {
+    const AttnBwdPlan p = dtype == kBF16 ? plan_attn_bwd_bf16(Tq, Tk, Hq, Hkv, n_seq) : AttnBwdPlan{1, 1};
     const size_t dq = p.q_splits > 1 ? (size_t)p.q_splits * (size_t)Tq * (size_t)Hq : 0;
     const size_t dkv = p.k_splits > 1 ? (size_t)p.k_splits * (size_t)Tk * (size_t)Hkv * 2 : 0;
     return kWsHeader + delta_bytes(Tq, Hq) + (dq + dkv) * (size_t)D * sizeof(float);

@@ -131,8 +131,8 @@ struct AttnArgs {
     int n_seq, Hq, Hkv, D, causal;
     float scale;
 };
-size_t attn_fwd_ws(int64_t Tq, int64_t Tk, int Hq, int Hkv, int D, int64_t n_seq);
-size_t attn_bwd_ws(int64_t Tq, int64_t Tk, int Hq, int Hkv, int D, int64_t n_seq);
+size_t attn_fwd_ws(int dtype, int64_t Tq, int64_t Tk, int Hq, int Hkv, int D, int64_t n_seq);
+size_t attn_bwd_ws(int dtype, int64_t Tq, int64_t Tk, int Hq, int Hkv, int D, int64_t n_seq);
 hipError_t launch_attn_fwd(int dtype, const AttnArgs &a, void *ws, hipStream_t st);
 hipError_t launch_attn_bwd(int dtype, AttnArgs a, void *ws, hipStream_t st);
 

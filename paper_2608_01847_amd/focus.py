@@ -19,7 +19,7 @@ CALL_SCALES_INIT, CALL_FAKEQUANT_FWD, CALL_FAKEQUANT_BWD = 0, 1, 2
 CALL_RECON_GEMM_FWD, CALL_RECON_GEMM_BWD, CALL_EXPORT_PACKED, CALL_ADAMW = 3, 4, 5, 6
 CALL_RECON_GEMM_DX, CALL_FAKEQUANT_ACT_BWD, CALL_KL_TOP, CALL_FAKEQUANT_WEIGHTS = 7, 8, 9, 10
 CALL_NORM_FWD, CALL_NORM_BWD, CALL_ATTENTION_FWD, CALL_ATTENTION_BWD = 11, 12, 13, 14
-CALL_TOKEN_LOGPROBS, CALL_TOKEN_LOGPROBS_BWD = 15, 16
+CALL_TOKEN_LOGPROBS, CALL_TOKEN_LOGPROBS_BWD, CALL_ATTENTION_FWD_F32, CALL_ATTENTION_BWD_F32 = 15, 16, 17, 18
 MAX_WEIGHT_LAYERS = 16
 NORM_LAYER, NORM_RMS = 0, 1
 MAX_TOP = 64
@@ -560,12 +560,16 @@ def _attention_inputs(q, k, v, cu_q, cu_k):
 
 
 def attention_workspace_size(q: torch.Tensor, k: torch.Tensor, n_seq: int = 1) -> int:
-    """Workspace bytes of attention_fwd and attention_bwd on tensors of these shapes, packed into n_seq sequences. Fewer queries
-    may need more (their keys are split): take the largest over the shapes that are called."""
+    """Workspace bytes of attention_fwd and attention_bwd on tensors of these shapes and dtype, packed into n_seq sequences. Fewer
+    bf16 queries may need more (their keys are split): take the largest over the shapes that are called."""
     c = _attention_config(q, k, 0, 1.0)
-    size = lib().focus_attention_workspace_size
-    return max(int(size(call, ctypes.byref(c), q.shape[0], k.shape[0], n_seq))
-               for call in (CALL_ATTENTION_FWD, CALL_ATTENTION_BWD))
+    return max(_attention_ws_bytes(call, c, q, k, n_seq) for call in (CALL_ATTENTION_FWD, CALL_ATTENTION_BWD))
+
+
+def _attention_ws_bytes(call: int, cfg: AttentionConfig, q: torch.Tensor, k: torch.Tensor, n_seq: int) -> int:
+    if _dt(q) == F32:
+        call = {CALL_ATTENTION_FWD: CALL_ATTENTION_FWD_F32, CALL_ATTENTION_BWD: CALL_ATTENTION_BWD_F32}[call]
+    return int(lib().focus_attention_workspace_size(call, ctypes.byref(cfg), q.shape[0], k.shape[0], n_seq))
 
 
 def attention_fwd(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_q=None, cu_k=None, causal: bool = True,
@@ -584,8 +588,7 @@ def attention_fwd(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_q=None, 
     if lse is not None and (lse.shape != (q.shape[1], q.shape[0]) or lse.dtype != torch.float32):
         raise ValueError("attention_fwd: lse is float32 [Hq][Tq]")
     _one_gpu("attention_fwd", q, k, v, cu_q, cu_k, ws, out, lse)
-    ws = _sized(ws, int(lib().focus_attention_workspace_size(CALL_ATTENTION_FWD, ctypes.byref(cfg), q.shape[0], k.shape[0],
-                                                             n)), q.device)
+    ws = _sized(ws, _attention_ws_bytes(CALL_ATTENTION_FWD, cfg, q, k, n), q.device)
     _check(lib().focus_attention_fwd(ctypes.byref(cfg), aq, ak, av, _dt(q), q.shape[0], k.shape[0], pq, pk, n, _ptr(O),
                                      _ptr(lse), _ptr(ws), ws.numel(), _stream()), "focus_attention_fwd")
     return O, lse
@@ -609,8 +612,7 @@ def attention_bwd(dO: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v: torch.T
     _one_gpu("attention_bwd", q, k, v, dO, O, lse, cu_q, cu_k, ws, dq, dk, dv)
     ptrs = [_heads(t, name) for t, name in ((q, "q"), (k, "k"), (v, "v"), (dq, "dq"), (dk, "dk"), (dv, "dv"))]
     cfg = _attention_config(q, k, causal, scale, tuple(s for _, s in ptrs))
-    ws = _sized(ws, int(lib().focus_attention_workspace_size(CALL_ATTENTION_BWD, ctypes.byref(cfg), q.shape[0], k.shape[0],
-                                                             n)), q.device)
+    ws = _sized(ws, _attention_ws_bytes(CALL_ATTENTION_BWD, cfg, q, k, n), q.device)
     (aq, ak, av, adq, adk, adv) = (a for a, _ in ptrs)
     _check(lib().focus_attention_bwd(ctypes.byref(cfg), _ptr(dO), aq, ak, av, _ptr(O), _ptr(lse), _dt(q), q.shape[0],
                                      k.shape[0], pq, pk, n, adq, adk, adv, _ptr(ws), ws.numel(), _stream()),

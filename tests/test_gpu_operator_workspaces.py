@@ -40,3 +40,20 @@ def test_the_flag_is_raised_in_the_given_workspace(F):
     ws = F.workspace(F.attention_workspace_size(few, many))
     call(ws)
     assert F.check_flags(ws) == F.ERR_DOMAIN
+
+
+def test_fp32_attention_in_its_own_workspace(F):
+    """What the size function gives does, on shapes whose bf16 sums are split, and memory behind it is not touched."""
+    for Tq, Tk in ((1, 3000), (600, 600)):
+        q, dO = (torch.randn(Tq, 4, 64).cuda() for _ in range(2))
+        k, v = (torch.randn(Tk, 2, 64).cuda() for _ in range(2))
+        need = F.attention_workspace_size(q, k)
+        assert need < F.attention_workspace_size(q.bfloat16(), k.bfloat16())
+        room = F.workspace(need + 4096)
+        room[need:] = 0xA5
+        O, lse = F.attention_fwd(q, k, v, ws=room[:256])
+        got = F.attention_bwd(dO, q, k, v, O, lse, ws=room[:need])
+        want = F.attention_bwd(dO, q, k, v, O, lse)
+        assert all(torch.equal(a, b) for a, b in zip(got, want)) and (room[need:] == 0xA5).all()
+        with pytest.raises(F.FocusError):
+            F.attention_bwd(dO, q, k, v, O, lse, ws=room[:need - 1])

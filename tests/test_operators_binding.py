@@ -1,4 +1,5 @@
 """Host-side checks of the binding of norms, attention and token log probabilities."""
+import pytest
 import torch
 
 from paper_2608_01847_amd import focus
@@ -11,3 +12,14 @@ def test_a_given_workspace_is_never_replaced():
     own = focus._sized(None, 1000, "cpu")
     assert own.numel() == 1000 and not own[:256].any()
     assert focus._sized(None, 0, "cpu").numel() == 256
+
+
+def test_fp32_attention_asks_for_what_it_uses():
+    """The fp32 kernels have no parts: the header, and in the backward a number per query and head."""
+    if not focus.LIBRARY.exists():
+        pytest.skip("libfocus.so is not built")
+    for Tq, Tk, n, Hq, Hkv in ((8192, 8192, 4, 64, 8), (16384, 16384, 1, 2, 1), (1, 8192, 1, 32, 8), (0, 5, 1, 4, 2)):
+        q, k = (torch.empty(T, H, 128, device="meta") for T, H in ((Tq, Hq), (Tk, Hkv)))
+        delta = -(-Tq * Hq * 4 // 256) * 256
+        assert focus.attention_workspace_size(q, k, n) == 256 + delta
+        assert focus.attention_workspace_size(q.bfloat16(), k.bfloat16(), n) >= 256 + delta
