@@ -459,10 +459,13 @@ def _sized(ws: torch.Tensor | None, need: int, device) -> torch.Tensor:
 
 
 def _one_gpu(where: str, first: torch.Tensor, *rest) -> None:
-    """All tensors (None: not given) lie on one GPU: a host address would reach a kernel otherwise."""
+    """All tensors (None: not given) lie on one GPU, the current one: a host address would reach a kernel otherwise, or a
+    kernel run on another GPU's stream, in no order with the work on the tensors."""
     d = first.get_device()
     if d < 0 or any(t is not None and t.get_device() != d for t in rest):
         raise ValueError(f"{where}: tensors of one GPU expected")
+    if d != torch.cuda.current_device():
+        raise ValueError(f"{where}: tensors of GPU {d} while GPU {torch.cuda.current_device()} is the current one")
 
 
 def norm_fwd(X: torch.Tensor, weight: torch.Tensor, bias=None, residual=None, kind: int = NORM_LAYER, eps: float = 1e-5,

@@ -23,3 +23,20 @@ def test_fp32_attention_asks_for_what_it_uses():
         delta = -(-Tq * Hq * 4 // 256) * 256
         assert focus.attention_workspace_size(q, k, n) == 256 + delta
         assert focus.attention_workspace_size(q.bfloat16(), k.bfloat16(), n) >= 256 + delta
+
+
+def test_tensors_of_a_gpu_that_is_not_the_current_one(monkeypatch):
+    """The call's stream is the current GPU's: work on another's tensors would run there, in no order with theirs."""
+    class On:
+        def __init__(self, device):
+            self.device_index = device
+
+        def get_device(self):
+            return self.device_index
+
+    for current in (0, 1):
+        monkeypatch.setattr(torch.cuda, "current_device", lambda: current)
+        focus._one_gpu("call", On(current), On(current), None)
+        for tensors in ((On(1 - current), On(1 - current)), (On(current), On(1 - current)), (On(1 - current), None), (On(-1),)):
+            with pytest.raises(ValueError):
+                focus._one_gpu("call", *tensors)
