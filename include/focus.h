@@ -470,7 +470,8 @@ focus_status focus_attention_bwd(const focus_attention_config *cfg, const void *
 /* Log probabilities of given tokens under rows of logits Z [T][V] (dtype; element-aligned rows of any V), with the
  * entropy and the largest alternatives of each row:
  *   lse[t] = log sum_i exp Z[t][i]                                        (fp32 [T])
- *   logp_opt[t] = Z[t][target[t]] - lse[t]; 0 where target[t] < 0 (a token left out)
+ *   logp_opt[t] = Z[t][target[t]] - lse[t]; 0 where target[t] < 0 (a token left out). It and top_logp are taken from the
+ *     row's largest logit rather than from lse, whose digits are few where the logits are large against their differences
  *   entropy_opt[t] = -sum_i p_i log p_i, p = softmax(Z[t])
  *   top_logp, top_index [T][top]: log probability and index of the `top` largest logits, largest first, equal logits by
  *     rising index; with V < top the rest is -inf and -1. Both NULL with top == 0.

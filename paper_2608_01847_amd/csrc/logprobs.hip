@@ -224,11 +224,13 @@ struct LogprobArgs {
 __device__ __forceinline__ void finish_row(const LogprobArgs &a, int64_t row, const Stat &t, const uint64_t *list, int n,
                                            float target_logit, int64_t target) {
     const bool none = t.m == -__builtin_inff();  // every logit is -inf
-    const float lse = none ? -__builtin_inff() : __builtin_fmaf(log2f(t.s), kLn2, t.m);
+    // A log probability is the logit's distance from the largest less log s: taken from lse it would have lse's digits only,
+    // and a row of the type's lowest value probability 1 for every token.
+    const float log_s = kLn2 * log2f(t.s), lse = none ? -__builtin_inff() : t.m + log_s;
     if (threadIdx.x == 0) {
         a.lse[row] = lse;
         if (a.entropy) a.entropy[row] = none ? 0.0f : kLn2 * (log2f(t.s) - t.w / t.s);
-        if (a.logp) a.logp[row] = target < 0 || target >= a.V ? 0.0f : none ? -__builtin_inff() : target_logit - lse;
+        if (a.logp) a.logp[row] = target < 0 || target >= a.V ? 0.0f : none ? -__builtin_inff() : target_logit - t.m - log_s;
         if (t.s != t.s || target >= a.V) *a.flag = 1u;  // a NaN or +inf among the logits, or no such token
     }
     for (int i = threadIdx.x; i < a.top; i += kThreads) {
@@ -236,7 +238,7 @@ __device__ __forceinline__ void finish_row(const LogprobArgs &a, int64_t row, co
         const uint64_t k = in ? list[i] : 0;
         const float v = value_of((uint32_t)(k >> 32));
         a.top_index[row * a.top + i] = in ? (int32_t)(0xFFFFFFFFu - (uint32_t)k) : -1;
-        a.top_logp[row * a.top + i] = !in || none ? -__builtin_inff() : v - lse;
+        a.top_logp[row * a.top + i] = !in || none ? -__builtin_inff() : v - t.m - log_s;
     }
 }
 
