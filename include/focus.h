@@ -487,8 +487,10 @@ focus_status focus_token_logprobs(const void *Z, int dtype, int64_t T, int64_t V
 /* Its gradient: with g = d_logp[t] (0 where target[t] < 0) and h = d_entropy[t],
  *   dZ[t][i] = g ([i == target[t]] - p_i) - h p_i (log p_i + entropy[t]),   p_i = exp(Z[t][i] - lse[t])
  * (the mean cross entropy of the T tokens is d_logp = -1/T). lse and entropy as the forward wrote them. d_logp_opt needs
- * target_opt, d_entropy_opt needs entropy_opt; one of the two is given at least (FOCUS_ERR_NULL). dZ [T][V] (dtype) may
- * alias Z. ws: focus_workspace_size(FOCUS_CALL_TOKEN_LOGPROBS_BWD, NULL, T, V, 0) bytes. */
+ * target_opt, d_entropy_opt needs entropy_opt; one of the two is given at least (FOCUS_ERR_NULL). p_i carries the rounding of
+ * lse, 2^-24 |lse| of it; a row with |lse| above 65,536 (or NaN), where that is more than bf16's own, and a gradient other
+ * than 0 raises the domain flag, and its dZ is unspecified: subtract a number near the row's largest logit beforehand. dZ [T][V]
+ * (dtype) may alias Z. ws: focus_workspace_size(FOCUS_CALL_TOKEN_LOGPROBS_BWD, NULL, T, V, 0) bytes. */
 focus_status focus_token_logprobs_bwd(const void *Z, int dtype, int64_t T, int64_t V, const int64_t *target_opt,
                                       const float *lse, const float *entropy_opt, const float *d_logp_opt,
                                       const float *d_entropy_opt, void *dZ, void *ws, size_t ws_bytes, focus_stream stream);
@@ -497,7 +499,8 @@ focus_status focus_token_logprobs_bwd(const void *Z, int dtype, int64_t T, int64
  * FOCUS_ERR_DOMAIN if any call on this workspace met a NaN scale or a coefficient c that is
  * <= 0 or not finite, a log2-domain AdamW step met a parameter that is not positive and
  * finite, focus_kl_top met a logit that is not finite, focus_attention_* met sequence ends that do not rise, or
- * focus_token_logprobs met a NaN or +inf logit or a target past the vocabulary, since the last check (outputs of such
+ * focus_token_logprobs met a NaN or +inf logit or a target past the vocabulary, or focus_token_logprobs_bwd an lse without digits
+ * for its probabilities, since the last check (outputs of such
  * blocks are unspecified), FOCUS_OK otherwise, FOCUS_ERR_HIP on a runtime error. */
 focus_status focus_check_flags(void *ws, focus_stream stream);
 

@@ -624,7 +624,7 @@ focus_status focus_token_logprobs_bwd(const void *Z, int dtype, int64_t T, int64
     FOCUS_TRY(check_ws(ws, ws_bytes, kWsHeader));
     if (T == 0) return FOCUS_OK;
     return hip_status(launch_logprobs_bwd(dtype, Z, T, V, target_opt, lse, entropy_opt, d_logp_opt, d_entropy_opt, dZ,
-                                          (hipStream_t)stream));
+                                          flag_of(ws), (hipStream_t)stream));
 }
 
 focus_status focus_check_flags(void *ws, focus_stream stream) {

@@ -142,6 +142,7 @@ hipError_t launch_logprobs(int dtype, const void *Z, int64_t T, int64_t V, const
                            float *entropy, float *lse, float *top_logp, int32_t *top_index, uint32_t *flag, void *ws,
                            hipStream_t st);
 hipError_t launch_logprobs_bwd(int dtype, const void *Z, int64_t T, int64_t V, const int64_t *target, const float *lse,
-                               const float *entropy, const float *d_logp, const float *d_entropy, void *dZ, hipStream_t st);
+                               const float *entropy, const float *d_logp, const float *d_entropy, void *dZ, uint32_t *flag,
+                               hipStream_t st);
 
 }  // namespace focus

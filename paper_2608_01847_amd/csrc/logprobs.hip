@@ -351,9 +351,13 @@ struct LogprobBwdArgs {
     const int64_t *target;
     const float *lse, *entropy, *d_logp, *d_entropy;
     void *dZ;
+    uint32_t *flag;
     int64_t V;
     unsigned chunks;  // workgroups per row
 };
+
+// From here on the rounding of lse, 2^-24 of it, is more of a probability than rounding it to bf16 is (2^-9)
+constexpr float kMostLse = 65536.0f;
 
 // The gradient, element by element from the row's statistics: one read and one write of the logits.
 template <typename T>
@@ -368,6 +372,7 @@ __global__ void __launch_bounds__(kBwdThreads) logprobs_bwd_kernel(LogprobBwdArg
     const float g = used && a.d_logp && !none ? a.d_logp[row] : 0.0f, h = a.d_entropy && !none ? a.d_entropy[row] : 0.0f;
     const float entropy = h != 0.0f ? a.entropy[row] : 0.0f;
     const float base = none ? 0.0f : lse;
+    if ((g != 0.0f || h != 0.0f) && !(__builtin_fabsf(lse) <= kMostLse) && c0 == 0 && threadIdx.x == 0) *a.flag = 1u;
     float v[kBwdVecs][8];
 #pragma unroll
     for (int j = 0; j < kBwdVecs; j++) {
@@ -448,9 +453,10 @@ hipError_t launch_logprobs(int dtype, const void *Z, int64_t T, int64_t V, const
 }
 
 hipError_t launch_logprobs_bwd(int dtype, const void *Z, int64_t T, int64_t V, const int64_t *target, const float *lse,
-                               const float *entropy, const float *d_logp, const float *d_entropy, void *dZ, hipStream_t st) {
+                               const float *entropy, const float *d_logp, const float *d_entropy, void *dZ, uint32_t *flag,
+                               hipStream_t st) {
     const int64_t chunks = (V + kBwdChunk - 1) / kBwdChunk;
-    LogprobBwdArgs a{Z, target, lse, entropy, d_logp, d_entropy, dZ, V, (unsigned)chunks};
+    LogprobBwdArgs a{Z, target, lse, entropy, d_logp, d_entropy, dZ, flag, V, (unsigned)chunks};
     // one launch for as many rows as a grid holds: its work-items (256 per chunk) must stay below 2^32
     const int64_t rows = std::max<int64_t>(1, ((int64_t(1) << 24) - 1) / chunks);
     const size_t esz = dtype == kBF16 ? 2 : 4;

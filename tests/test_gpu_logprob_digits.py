@@ -47,3 +47,27 @@ def test_rows_of_the_lowest_value(F, T, dt):
     for x in (-logp, ent, -top_logp):
         assert ((x - math.log(V)).abs() <= 1e-4).all()
     assert top_index.tolist() == [[0, 1, 2]] * T
+
+
+def test_gradients_that_lse_has_no_digits_for(F):
+    """Raise the domain flag; rows without a gradient of their own, masked whole or not, do not."""
+    Z = torch.randn(6, 700).cuda()
+    Z[1] += 7e4
+    Z[2] -= 1e7
+    Z[3] = torch.finfo(torch.float32).min
+    Z[4] += 6e4
+    Z[5] = -math.inf
+    t = torch.zeros(6, dtype=torch.int64).cuda()
+    ws = F.workspace(F.token_logprobs_workspace_size(6, 700))
+    _, ent, lse, _, _ = F.token_logprobs(Z, t, ws=ws)
+    assert F.check_flags(ws) == F.OK
+    for row, far in ((0, False), (1, True), (2, True), (3, True), (4, False), (5, False)):
+        for g, h in ((1.0, None), (None, 1.0), (0.0, 1.0), (0.0, 0.0)):
+            d = [None if x is None else torch.zeros(6).cuda().index_fill_(0, torch.tensor([row]).cuda(), x) for x in (g, h)]
+            dZ = F.token_logprobs_bwd(Z, t, lse, ent, *d, ws=ws)
+            assert F.check_flags(ws) == (F.ERR_DOMAIN if far and (g or h) else F.OK), (row, g, h)
+            keep = [i for i in range(6) if i != row]
+            assert (dZ[keep] == 0).all()
+    left_out = torch.full((6,), -1).cuda()
+    F.token_logprobs_bwd(Z, left_out, lse, ent, torch.ones(6).cuda(), ws=ws)
+    assert F.check_flags(ws) == F.OK
