@@ -268,15 +268,26 @@ __global__ void __launch_bounds__(kThreads) logprobs_kernel(LogprobArgs a) {
             for (int e = 0; e < 8; e++) top = fmaxf(top, v[j][e]);
         const float m = fmaxf(t.m, top), base = m == -__builtin_inff() ? 0.0f : m;
         float s = 0.0f, w = 0.0f;
+        auto add = [&](float d) {
+            const float x = exp2_raw(d);
+            s += x;
+            w = __builtin_fmaf(x, d, w);
+        };
+        if (c0 + kStep <= v1) {
 #pragma unroll
-        for (int j = 0; j < kVecs; j++)
+            for (int j = 0; j < kVecs; j++)
 #pragma unroll
-            for (int e = 0; e < 8; e++) {
-                const float d = (v[j][e] - base) * kLog2e, x = exp2_raw(d);
-                s += x;
-                w = __builtin_fmaf(x, d, w);
+                for (int e = 0; e < 8; e++) add((v[j][e] - base) * kLog2e);
+        } else {  // the last step: no exponentials of vectors that do not exist, terms of 0 for what one of them lacks
+#pragma unroll
+            for (int j = 0; j < kVecs; j++) {
+                const int64_t left = v1 - c0 - (j * kThreads + (int)threadIdx.x) * 8;
+                if (left <= 0) break;
+#pragma unroll
+                for (int e = 0; e < 8; e++) add(e < left ? (v[j][e] - base) * kLog2e : -200.0f);
             }
-        if (w != w) {  // a -inf among them (0 times -inf), or a NaN, which s keeps
+        }
+        if (w != w) {  // a masked logit, -inf, among them (0 times -inf), or a NaN, which s keeps
             w = 0.0f;
 #pragma unroll
             for (int j = 0; j < kVecs; j++)
@@ -394,8 +405,8 @@ __global__ void __launch_bounds__(kBwdThreads) logprobs_bwd_kernel(LogprobBwdArg
     }
 }
 
-// Parts of a row: up to two workgroups per CU, of one step each at least, where that takes off enough of a row's steps to
-// pay for the join. With 5 alternatives, one row of 151,936 (10 steps) takes 15.9 us in parts and 19.9 us in one, of 65,536 (4
+// Parts of a row: up to two workgroups per CU, and no more than the row has steps (so that a part is a step or little less at
+// least), where that takes off enough of a row's steps to pay for the join. With 5 alternatives, one row of 151,936 (10 steps) takes 15.9 us in parts and 19.9 us in one, of 65,536 (4
 // steps) 15.6 and 12.3; 32 rows of 151,936 19.6 and 20.4, 64 rows 22.8 and 20.2;
 // 64 rows of 300,000 (19 steps) 25.7 and 32.7, 256 rows 42.2 and 34.9.
 int plan_splits(int64_t T, int64_t V) {
