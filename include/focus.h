@@ -447,7 +447,8 @@ size_t focus_attention_workspace_size(int call, const focus_attention_config *cf
  *   bf16: products on the bf16 matrix instructions with fp32 sums, probabilities rounded to bf16 for the second product;
  *   fp32: fp32 products throughout. heads_q <= 65535, Tq / 32 + n_seq, Tk / 32 + n_seq,
  *   Tq heads_q / 128 + n_seq heads_kv and Tk heads_kv / 128 + n_seq heads_kv below 2^24 (FOCUS_ERR_SHAPE).
- *   Tensor pointers 16-byte aligned, lse and cu_* element-aligned. */
+ *   Tensor pointers 16-byte aligned, lse and cu_* element-aligned. O may be q itself (of one stride); apart from that it shares
+ *   no memory with q, k and v (FOCUS_ERR_SHAPE). */
 focus_status focus_attention_fwd(const focus_attention_config *cfg, const void *q, const void *k, const void *v, int dtype,
                                  int64_t Tq, int64_t Tk, const int32_t *cu_q, const int32_t *cu_k, int64_t n_seq, void *O,
                                  float *lse_opt, void *ws, size_t ws_bytes, focus_stream stream);
@@ -459,7 +460,9 @@ focus_status focus_attention_fwd(const focus_attention_config *cfg, const void *
  * A hidden pair of a sequence has probability 0, whose products with a NaN or infinity of the pair's q, k, v or dO are NaN:
  * these have to be finite. Nothing reaches one sequence from another.
  * bf16 gradients: rounding dS, and O as the forward rounded it in rowsum(dO O), each add about as much error as rounding the
- * result does (2^-9 of it). No atomics: every sum has a fixed order. */
+ * result does (2^-9 of it). No atomics: every sum has a fixed order.
+ * dq, dk and dv share no memory with each other or with any of the inputs (FOCUS_ERR_SHAPE); slices of one fused tensor, whose
+ * rows interleave at one stride, do not. */
 focus_status focus_attention_bwd(const focus_attention_config *cfg, const void *dO, const void *q, const void *k,
                                  const void *v, const void *O, const float *lse, int dtype, int64_t Tq, int64_t Tk,
                                  const int32_t *cu_q, const int32_t *cu_k, int64_t n_seq, void *dq, void *dk, void *dv,

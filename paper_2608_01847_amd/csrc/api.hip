@@ -174,6 +174,37 @@ bool strides_ok(const AttnArgs &a, int dtype) {
     return (a.q_stride | a.k_stride | a.v_stride | a.dq_stride | a.dk_stride | a.dv_stride) % e == 0;
 }
 
+// The tokens of an attention tensor in memory: `n` rows of `width` bytes, `stride` apart
+struct Rows {
+    const void *base;
+    int64_t n, stride, width;
+};
+
+// Whether two of them share memory. Slices of one fused tensor, whose rows interleave at one stride, need not; rows that
+// interleave at different strides are taken to.
+bool overlap(Rows a, Rows b) {
+    if (a.n == 0 || b.n == 0) return false;
+    const int64_t off = (int64_t)((intptr_t)a.base - (intptr_t)b.base);  // of a's row 0 from b's
+    if (off >= (b.n - 1) * b.stride + b.width || -off >= (a.n - 1) * a.stride + a.width) return false;
+    if (a.n == 1) a.stride = b.stride;
+    if (b.n == 1) b.stride = a.stride;
+    if (a.stride != b.stride) return true;
+    // rows i of a and j of b share memory where -a.width < off + (i - j) stride < b.width: the largest i - j below that bound
+    const int64_t most = b.width - 1 - off, up = most >= 0 ? most / a.stride : -((-most + a.stride - 1) / a.stride);
+    const int64_t diff = std::min(up, a.n - 1);
+    return diff >= -(b.n - 1) && off + diff * a.stride > -a.width;
+}
+
+struct AttnRows {
+    Rows q, k, v, O, dO, dq, dk, dv;
+    AttnRows(const AttnArgs &a, int dtype) {
+        const int64_t e = dtype == FOCUS_BF16 ? 2 : 4, wq = (int64_t)a.Hq * a.D * e, wk = (int64_t)a.Hkv * a.D * e;
+        q = {a.q, a.Tq, a.q_stride * e, wq}, O = {a.O, a.Tq, wq, wq}, dO = {a.dO, a.Tq, wq, wq}, dq = {a.dq, a.Tq, a.dq_stride * e, wq};
+        k = {a.k, a.Tk, a.k_stride * e, wk}, v = {a.v, a.Tk, a.v_stride * e, wk};
+        dk = {a.dk, a.Tk, a.dk_stride * e, wk}, dv = {a.dv, a.Tk, a.dv_stride * e, wk};
+    }
+};
+
 focus_status check_ends(const int32_t *cu_q, const int32_t *cu_k, int64_t n_seq) {
     if (!cu_q != !cu_k || (!cu_q && n_seq != 1)) return FOCUS_ERR_NULL;
     return aligned_to({cu_q, cu_k}, 4) ? FOCUS_OK : FOCUS_ERR_SHAPE;
@@ -573,6 +604,9 @@ focus_status focus_attention_fwd(const focus_attention_config *cfg, const void *
     FOCUS_TRY(check_ws(ws, ws_bytes, attn_fwd_ws(dtype, Tq, Tk, a.Hq, a.Hkv, a.D, n_seq)));
     if (Tq == 0 || n_seq == 0) return FOCUS_OK;
     a.q = q, a.k = k, a.v = v, a.O = O, a.lse = lse_opt, a.cu_q = cu_q, a.cu_k = cu_k, a.flag = flag_of(ws);
+    const AttnRows r(a, dtype);
+    const bool in_place = O == q && r.q.stride == r.O.stride;  // a row's queries are read before its output is written
+    if (overlap(r.O, r.k) || overlap(r.O, r.v) || (!in_place && overlap(r.O, r.q))) return FOCUS_ERR_SHAPE;
     return hip_status(launch_attn_fwd(dtype, a, ws, (hipStream_t)stream));
 }
 
@@ -591,6 +625,12 @@ focus_status focus_attention_bwd(const focus_attention_config *cfg, const void *
     if ((Tq == 0 && Tk == 0) || n_seq == 0) return FOCUS_OK;
     a.q = q, a.k = k, a.v = v, a.O = const_cast<void *>(O), a.dO = dO, a.lse = const_cast<float *>(lse);
     a.dq = dq, a.dk = dk, a.dv = dv, a.cu_q = cu_q, a.cu_k = cu_k, a.flag = flag_of(ws);
+    // the keys' pass reads what the queries' pass, before it, and its own other workgroups would have written over
+    const AttnRows r(a, dtype);
+    for (const Rows &out : {r.dq, r.dk, r.dv})
+        for (const Rows &in : {r.q, r.k, r.v, r.O, r.dO})
+            if (overlap(out, in)) return FOCUS_ERR_SHAPE;
+    if (overlap(r.dq, r.dk) || overlap(r.dq, r.dv) || overlap(r.dk, r.dv)) return FOCUS_ERR_SHAPE;
     return hip_status(launch_attn_bwd(dtype, a, ws, (hipStream_t)stream));
 }
 

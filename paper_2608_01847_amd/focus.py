@@ -579,7 +579,7 @@ def attention_fwd(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_q=None, 
                   scale: float | None = None, want_lse: bool = True, ws=None, out=None, lse=None):
     """Attention of q [Tq][Hq][D] over k, v [Tk][Hkv][D], sequences packed one after the other with ends cu_q, cu_k
     (int32 [n_seq + 1] on the device; cu_k defaults to cu_q, both None: one sequence) -> (O [Tq][Hq][D], lse [Hq][Tq]
-    fp32 or None). q, k and v may be slices of one fused product (tokens apart). scale defaults to D ** -0.5."""
+    fp32 or None). q, k and v may be slices of one fused product (tokens apart); `out` may be q. scale defaults to D ** -0.5."""
     pq, pk, n = _attention_inputs(q, k, v, cu_q, cu_k)
     (aq, sq), (ak, sk), (av, sv) = _heads(q, "q"), _heads(k, "k"), _heads(v, "v")
     cfg = _attention_config(q, k, causal, scale, (sq, sk, sv, 0, 0, 0))
@@ -600,7 +600,7 @@ def attention_fwd(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_q=None, 
 def attention_bwd(dO: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, O: torch.Tensor, lse: torch.Tensor,
                   cu_q=None, cu_k=None, causal: bool = True, scale: float | None = None, ws=None, out=None):
     """Backward of attention_fwd from its outputs O and lse -> (dq, dk, dv) in q's dtype. `out`: preallocated (dq, dk, dv),
-    which may be slices of one fused gradient."""
+    which may be slices of one fused gradient and share no memory with each other or with an input."""
     pq, pk, n = _attention_inputs(q, k, v, cu_q, cu_k)
     if dO.shape != q.shape or O.shape != q.shape or lse.shape != (q.shape[1], q.shape[0]):
         raise ValueError("attention_bwd: dO and O have q's shape, lse is [Hq][Tq]")

@@ -92,3 +92,32 @@ def test_parts_of_sequences_with_rows_before_and_behind(F):
     for x in (O, lse.t(), *out):
         assert (x[:130] == 7.0).all() and (x[770:] == 7.0).all() and torch.isfinite(x[130:770]).all()
     assert F.check_flags(ws) == F.OK
+
+
+@pytest.mark.parametrize("dt", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("Tq,Tk", [(70, 70), (513, 513), (3, 2000)])
+def test_output_in_the_queries_place(F, Tq, Tk, dt):
+    g = torch.Generator().manual_seed(Tq)
+    q, k, v = (torch.randn(T, H, 128, generator=g).to(dt).cuda() for T, H in ((Tq, 6), (Tk, 2), (Tk, 2)))
+    O, lse = F.attention_fwd(q, k, v)
+    x = q.clone()
+    O2, lse2 = F.attention_fwd(x, k, v, out=x)
+    assert O2.data_ptr() == x.data_ptr() and torch.equal(O, O2) and torch.equal(lse, lse2)
+
+
+def test_outputs_over_other_inputs_are_refused(F):
+    q, k, v, dO = (torch.randn(64, 2, 64).cuda() for _ in range(4))
+    O, lse = F.attention_fwd(q, k, v)
+    fresh = lambda: [torch.empty_like(q) for _ in range(3)]
+    calls = [lambda: F.attention_fwd(q, k, v, out=k), lambda: F.attention_fwd(q, k, v, out=v)]
+    for i in range(3):
+        for t in (q, k, v, dO, O):
+            out = fresh()
+            out[i] = t
+            calls.append(lambda out=tuple(out): F.attention_bwd(dO, q, k, v, O, lse, out=out))
+    g = fresh()
+    calls.append(lambda: F.attention_bwd(dO, q, k, v, O, lse, out=(g[0], g[1], g[1])))
+    for call in calls:
+        with pytest.raises(F.FocusError) as e:
+            call()
+        assert e.value.status == F.ERR_SHAPE
