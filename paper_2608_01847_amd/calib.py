@@ -290,8 +290,8 @@ class DecoderStack:
     LEARNING_RATES = {F.MXFP4: (1e-3, 2e-3), F.NVFP4: (5e-3, 1e-3)}
 
     def __init__(self, fmt: int, variant: str, hidden: int = 2560, heads: tuple = (32, 8), head_dim: int = 128,
-                 vocab: int = 32000, lengths: tuple = (2048, 1024, 700, 324), k: int = 1000, hyper: Hyper | None = None,
-                 device="cuda"):
+                 vocab: int = 32000, lengths: tuple = (2048, 1024, 700, 324), k: int = 1000, x_kind: str = "lowrank",
+                 hyper: Hyper | None = None, device="cuda"):
         from .synth import Linear, Workload
         hq, hkv = heads
         self.heads, self.D, self.T = heads, head_dim, sum(lengths)
@@ -299,7 +299,7 @@ class DecoderStack:
         self.w = Workload(name=f"decoder{hidden}x{vocab}", fmt=fmt, sub_block=8, M=self.T,
                           linears=(Linear("qkv", rows, hidden, "x"), Linear("o", hidden, hq * head_dim, "o"),
                                    Linear("head", vocab, hidden, "b")),
-                          inputs={"x": hidden, "o": hq * head_dim, "b": hidden}, x_kind="lowrank", x_outlier_p=0.01, x_outlier_f=30.0)
+                          inputs={"x": hidden, "o": hq * head_dim, "b": hidden}, x_kind=x_kind, x_outlier_p=0.01, x_outlier_f=30.0)
         self.variant, self.k, self.device = variant, k, device
         self.sb, self.learn_s, self.learn_c, self.use_c = variant_setup(self.w, variant)
         self.hyper = hyper or Hyper(*self.LEARNING_RATES[fmt])
@@ -423,22 +423,27 @@ def main() -> None:
     ap.add_argument("--eval-tokens", type=int, default=None)
     ap.add_argument("--variants", default=",".join(VARIANTS))
     ap.add_argument("--x-kind", default=None, choices=("normal", "student_t3", "lowrank"),
-                    help="activation distribution (default: the workload's)")
+                    help="activation distribution (default: the workload's, lowrank for the stacks)")
     ap.add_argument("--kl-top-stack", action="store_true",
                     help="train the synthetic two-linear stack end to end on KL-Top instead")
     ap.add_argument("--decoder-stack", action="store_true",
                     help="train one attention layer and the output layer of a decoder end to end on KL-Top instead")
     ap.add_argument("--vocab", type=int, default=32000)
     a = ap.parse_args()
+    if a.decoder_stack and (a.kl_top_stack or a.tokens is not None or a.eval_tokens is not None):
+        ap.error("--decoder-stack is a loop of its own, on sequences of its own lengths")
+    if a.decoder_stack and len(synth.WORKLOADS[a.workload].linears) < 7:
+        ap.error(f"--decoder-stack: {a.workload} has no attention heads")
     if not torch.cuda.is_available():
         raise SystemExit("the calibration epoch runs on the GPU")
     w = synth.WORKLOADS[a.workload]
     if a.decoder_stack:
         hidden = w.inputs[w.linears[0].source]
         heads = (w.linears[0].N // 128, w.linears[1].N // 128)
-        out = {"stack": f"hidden {hidden}, {heads[0]}/{heads[1]} heads of 128 -> vocab {a.vocab}", "steps": a.steps, "results": {}}
+        out = {"stack": f"hidden {hidden}, {heads[0]}/{heads[1]} heads of 128 -> vocab {a.vocab}",
+               "x_kind": a.x_kind or "lowrank", "steps": a.steps, "results": {}}
         for v in a.variants.split(","):
-            r = decoder_epoch(w.fmt, v, a.steps, hidden=hidden, heads=heads, vocab=a.vocab)
+            r = decoder_epoch(w.fmt, v, a.steps, hidden=hidden, heads=heads, vocab=a.vocab, x_kind=a.x_kind or "lowrank")
             out["results"][v] = {"eval_before": r["eval_before"], "eval_after": r["eval_after"], "seconds": round(r["seconds"], 3),
                                  "train_first_last": r["train_curve"][:1] + r["train_curve"][-1:]}
         print(json.dumps(out))
