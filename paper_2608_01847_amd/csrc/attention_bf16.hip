@@ -916,14 +916,25 @@ void pick_dt(int D, F &&f) {
 
 }  // namespace
 
-// Parts that a forward's keys are split into: where the row tiles leave workgroups idle (two per CU), as many as fill them
-// with 128 keys each at least (by the mean length; lengths are not known on the host), up to a wave's lanes. One query of
-// 32/8 heads over 8,192 keys takes 18.6 us split in 64, and 161 us in one part.
+// Parts that a forward's keys are split into: where the row tiles leave workgroups idle (two per CU), up to as many as fill
+// them with 128 keys each at least (by the mean length; lengths are not known on the host) and a wave's lanes. Of these the
+// number that gains most, none where none does: a tile of keys that a workgroup does not go through saves 1.15 us, and the parts
+// cost 5 us and per row 1.2 ns and 0.15 for each of them (written, read and joined, a workgroup per row). In one part and in
+// the parts taken here, us, heads of 128: one query of 32/8 heads on 8,192 keys 158 and 17 (64 parts), on 300 keys 15 and (in
+// two) 17; causal prompts: 2,048 with 2/1 heads 42 and 26, 4,096 with 2/1 78 and 39, but 512 with 32/8 16 and (in three) 42, 1,024
+// with 8/8 25 and (in seven) 33, four of 507 with 4/4 16 and (in three) 26. Lengths that differ widely lose by the mean: 2,000,
+// 10, 10, 10 with 4/4 heads 42 and (in three) 35.
 int attn_splits_bf16(int64_t Tq, int64_t Tk, int Hq, int Hkv, int64_t n_seq) {
     if (n_seq < 1) return 1;
-    const int64_t wgs = (Tq * (Hq / Hkv) / (32 * kWaves) + n_seq) * Hkv;
-    const int64_t most = std::min<int64_t>(64, Tk / n_seq / (2 * kKeys));
-    return (int)std::max<int64_t>(1, std::min(most, 2 * kMfmaConcurrentWgs / wgs));
+    const int64_t wgs = (Tq * (Hq / Hkv) / (32 * kWaves) + n_seq) * Hkv, rows = Tq * Hq;
+    const int64_t keys = Tk / n_seq, tiles = (keys + kKeys - 1) / kKeys;
+    const int64_t most = std::min({int64_t(64), keys / (2 * kKeys), 2 * kMfmaConcurrentWgs / wgs});
+    int64_t best = 1, gain = 0;  // ns
+    for (int64_t s = 2; s <= most; s++) {
+        const int64_t g = (tiles - (tiles + s - 1) / s) * 1150 - 5000 - rows * (24 + 3 * s) / 20;
+        if (g > gain) gain = g, best = s;
+    }
+    return (int)best;
 }
 
 hipError_t launch_attn_fwd_bf16(const AttnArgs &a, void *ws, hipStream_t st) {

@@ -46,11 +46,12 @@ def sizes(F, lq, lk, Hq, Hkv, D):
 @pytest.mark.parametrize("D", [8, 64, 72, 80, 96, 104, 128])
 @pytest.mark.parametrize("causal", [True, False])
 def test_two_sequences_in_parts(F, D, causal):
-    lengths = [700, 301]
-    fwd, bwd = sizes(F, lengths, lengths, 4, 1, D)
-    dq, dkv = 1001 * 4 * D * 4, 2 * 1001 * D * 4
-    assert fwd > 0 and bwd >= 2 * dq + 2 * dkv  # the forward, dq, and dk with dv, in two parts at least
-    run_case(F, lengths, lengths, 4, 1, D, "bf16", causal, seed=D)
+    for lengths, Hq in (([700, 301], 4), ([2200, 301], 2)):
+        T = sum(lengths)
+        fwd, bwd = sizes(F, lengths, lengths, Hq, 1, D)
+        dq, dkv = T * Hq * D * 4, 2 * T * D * 4
+        assert bwd >= 2 * dq + 2 * dkv and (fwd > 0 or Hq == 4)  # dq, dk with dv, the second one's forward: in two parts at least
+        run_case(F, lengths, lengths, Hq, 1, D, "bf16", causal, seed=D)
 
 
 @pytest.mark.parametrize("D", [64, 80, 128])
