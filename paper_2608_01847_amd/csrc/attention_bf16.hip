@@ -960,10 +960,16 @@ hipError_t launch_attn_fwd_bf16(const AttnArgs &a, void *ws, hipStream_t st) {
 // Parts of a backward's sums. Where workgroups are few, one's run through all queries (keys) of a long sequence is the whole
 // call's time: they are split until two per CU are busy, with 4 tiles each at least by the mean length. The keys' pass, whose
 // runs over a causal sequence are from one to all of its queries long, is split on until there are four times as many with 64
-// tiles each, so that long and short ones even out (backward of four sequences of 2,048 with 64/8 heads 1.03 ms, 1.08 without
-// these parts and 1.11 with twice as many; of one of 8,192 3.4, 4.1 and 3.4). A part
-// costs 64 KB of fp32 sums per 128 rows and gradient, written and read again: splitting either pass up to 2,048 workgroups
-// with 8 tiles each made two sequences of 2,500 with 16/8 heads take 554 us in place of 462.
+// tiles each, so that long and short ones even out (backward of four sequences of 2,048 with 64/8 heads 1.06 ms, 1.13 without
+// these parts and 1.15 with twice as many; of one of 8,192 3.70, 4.36 and 3.65). A part
+// costs 64 KB of fp32 sums per 128 rows and gradient, written and read again: splitting both passes up to 2,048 workgroups
+// with 8 tiles each made two sequences of 2,500 with 16/8 heads take 356 us in place of 239.
+//
+// The keys' parts also have to save more than their two joins cost: 8 us, and per key and head 0.2 ns and 0.25 for each part, at
+// 1 us for a tile of 32 queries that a workgroup does not go through. In one part and in those, us, heads of 128: 64 queries of
+// 32/8 heads on 2,048 keys 38 and (two) 51, 512 of 4/4 on 4,096 50 and (three) 61, four of 507 with 4/4 42 and (three) 49; but
+// 256 with 32/8 54 and (eight) 40, 1,024 with 8/8 66 and (seven) 59, 4,096 with 2/1 307 and (fifteen) 85. Lengths that differ
+// widely lose by the mean here too: 2,000, 10, 10, 10 with 4/4 heads 121 and (three) 97.
 AttnBwdPlan plan_attn_bwd_bf16(int64_t Tq, int64_t Tk, int Hq, int Hkv, int64_t n_seq) {
     const int64_t kRows = 32 * kWaves, kBusy = 2 * kMfmaConcurrentWgs, kMost = 16;
     if (n_seq < 1) return {1, 1};
@@ -972,7 +978,9 @@ AttnBwdPlan plan_attn_bwd_bf16(int64_t Tq, int64_t Tk, int Hq, int Hkv, int64_t 
     const int64_t q = std::min(kBusy / q_wgs, q_tiles / 4);
     const int64_t k = std::max(std::min(kBusy / k_wgs, k_tiles / 4), std::min(4 * kBusy / k_wgs, k_tiles / 64));
     auto clip = [&](int64_t s) { return (int)std::max<int64_t>(1, std::min(kMost, s)); };
-    return {clip(q), clip(k)};
+    const int64_t parts = clip(k), saved = k_tiles - (k_tiles + parts - 1) / parts;
+    const bool pays = saved * 1000 > 8000 + Tk * Hkv * (4 + 5 * parts) / 20;  // ns
+    return {clip(q), pays ? (int)parts : 1};
 }
 
 hipError_t launch_attn_bwd_bf16(const AttnArgs &a, float *parts, hipStream_t st) {

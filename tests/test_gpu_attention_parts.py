@@ -81,17 +81,18 @@ def test_scales_of_both_signs(F, D, scale):
 
 def test_parts_of_sequences_with_rows_before_and_behind(F):
     """Rows of no sequence have no parts: the join neither reads nor writes them."""
-    T, cu = 900, torch.tensor([130, 500, 770], dtype=torch.int32).cuda()
+    T, a, b = 2400, 130, 2270
+    cu = torch.tensor([a, 1300, b], dtype=torch.int32).cuda()
     g = torch.Generator().manual_seed(5)
-    q, k, v, dO = (torch.randn(T, 2, 80, generator=g).bfloat16().cuda() for _ in range(4))
+    q, k, v, dO = (torch.randn(T, H, 80, generator=g).bfloat16().cuda() for H in (2, 1, 1, 2))
     ws = F.workspace(F.attention_workspace_size(q, k, 2))
-    assert sizes(F, [T - 1, 1], [T - 1, 1], 2, 2, 80)[1] > 0
+    assert all(n > 0 for n in sizes(F, [T - 1, 1], [T - 1, 1], 2, 1, 80))
     O, lse = torch.full_like(q, 7.0), torch.full((2, T), 7.0).cuda()
     F.attention_fwd(q, k, v, cu, ws=ws, out=O, lse=lse)
-    out = tuple(torch.full_like(q, 7.0) for _ in range(3))
+    out = tuple(torch.full_like(t, 7.0) for t in (q, k, v))
     F.attention_bwd(dO, q, k, v, O, lse, cu, ws=ws, out=out)
     for x in (O, lse.t(), *out):
-        assert (x[:130] == 7.0).all() and (x[770:] == 7.0).all() and torch.isfinite(x[130:770]).all()
+        assert (x[:a] == 7.0).all() and (x[b:] == 7.0).all() and torch.isfinite(x[a:b]).all()
     assert F.check_flags(ws) == F.OK
 
 
