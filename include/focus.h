@@ -459,8 +459,9 @@ focus_status focus_attention_fwd(const focus_attention_config *cfg, const void *
  * rounded to bf16 for the products. dq, dk, dv in dtype, with cfg's gradient strides; keys that no query sees get zeros.
  * A hidden pair of a sequence has probability 0, whose products with a NaN or infinity of the pair's q, k, v or dO are NaN:
  * these have to be finite. Nothing reaches one sequence from another.
- * bf16 gradients: rounding dS, and O as the forward rounded it in rowsum(dO O), each add about as much error as rounding the
- * result does (2^-9 of it). No atomics: every sum has a fixed order.
+ * bf16 gradients: the rounding of P and dS adds about as much error to dv and dk as rounding the result does (2^-9 of it); dq has dS
+ * in 16 bits. rowsum(dO O) is corrected for the rounding that the forward gave O, in dq for rows of up to 256 keys (over more, what is
+ * left of it is averaged: some tenths of the result's rounding). No atomics: every sum has a fixed order.
  * dq, dk and dv share no memory with each other or with any of the inputs (FOCUS_ERR_SHAPE); slices of one fused tensor, whose
  * rows interleave at one stride, do not. */
 focus_status focus_attention_bwd(const focus_attention_config *cfg, const void *dO, const void *q, const void *k,

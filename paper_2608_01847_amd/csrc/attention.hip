@@ -365,7 +365,7 @@ size_t attn_bwd_ws(int dtype, int64_t Tq, int64_t Tk, int Hq, int Hkv, int D, in
     const AttnBwdPlan p = dtype == kBF16 ? plan_attn_bwd_bf16(Tq, Tk, Hq, Hkv, n_seq) : AttnBwdPlan{1, 1};
     const size_t dq = p.q_splits > 1 ? (size_t)p.q_splits * (size_t)Tq * (size_t)Hq : 0;
     const size_t dkv = p.k_splits > 1 ? (size_t)p.k_splits * (size_t)Tk * (size_t)Hkv * 2 : 0;
-    return kWsHeader + delta_bytes(Tq, Hq) + (dq + dkv) * (size_t)D * sizeof(float);
+    return kWsHeader + delta_bytes(Tq, Hq) + ((size_t)attn_rest_floats(p.q_splits, Tq * Hq) + (dq + dkv) * (size_t)D) * sizeof(float);
 }
 
 hipError_t launch_attn_fwd(int dtype, const AttnArgs &a, void *ws, hipStream_t st) {

@@ -27,6 +27,7 @@ typedef __attribute__((address_space(3))) u32x4_t lds_u32x4;
 constexpr int kWaves = 4;
 constexpr int kThreads = 64 * kWaves;
 constexpr int kKeys = 64;   // rows of a staged tile
+constexpr int kFewTiles = 4;  // of keys, at most: row tiles that the queries' backward goes through twice
 constexpr float kNone = -__builtin_inff();
 
 // Geometry of a staged tile of ROWS rows: DT x 32 features, a row of 128 (DT <= 2) or 256 bytes. 16-byte chunk c of row r
@@ -221,6 +222,15 @@ __device__ __forceinline__ bf16x8_t pack8(const f32x16_t &p, int s) {
     uint32_t w[4];
 #pragma unroll
     for (int e = 0; e < 4; e++) w[e] = pack_bf16(p[8 * s + 2 * e], p[8 * s + 2 * e + 1]);
+    return __builtin_bit_cast(bf16x8_t, w);
+}
+
+// What rounding those 8 to `high` left, rounded likewise: high + low has 16 bits
+__device__ __forceinline__ bf16x8_t pack8_rest(const f32x16_t &p, int s, bf16x8_t high) {
+    uint32_t w[4];
+#pragma unroll
+    for (int e = 0; e < 4; e++)
+        w[e] = pack_bf16(p[8 * s + 2 * e] - (float)high[2 * e], p[8 * s + 2 * e + 1] - (float)high[2 * e + 1]);
     return __builtin_bit_cast(bf16x8_t, w);
 }
 
@@ -534,9 +544,11 @@ __global__ void __launch_bounds__(kThreads) attn_join_kernel(AttnArgs a, AttnPar
 // forward, so dS is the B operand of dq^T = k^T dS^T as it stands.
 // Bound: three products of 2 D flops a visible pair and an exponential. 32 x 2,048 tokens, 32/8 heads of 128, causal: 1.72 ms,
 // 0.96 PFLOP/s, matrix units busy 51%. Two waves per SIMD, 256 registers.
-// dS is rounded to bf16 for its product (an error of 0.0017 of the gradient's size on normal inputs, as much as rounding the
-// result), and delta comes from the O that the forward rounded (0.0014): carrying dS in two halves, or delta from fp32
-// products formed again, would add a quarter to the matrix work.
+// dS goes into its product in two parts, rounded to bf16 and what that left, so that 16 of its bits count. delta from the O that the
+// forward rounded is off by that rounding, which all of a row's dS share: their sum over the row's keys, 0 from the exact delta,
+// is what it is off by, and is added to it for the keys' pass. dq has it averaged over the row's keys; row tiles of few keys, whose dq
+// it would spoil most, are gone through twice, the first time for the sum alone. Error of dq against 64 bits, in that of rounding
+// it (rounded dS and this delta in brackets): 64 tokens 1.00 (1.71), 300 1.19 (1.58), 2,048 1.06 (1.54).
 // SPLIT: the tiles of keys are dealt to gridDim.y workgroups, whose sums attn_grad_join_kernel adds.
 template <int DT, bool SPLIT>
 __global__ void __launch_bounds__(kThreads, 2) attn_bwd_q_bf16_kernel(AttnArgs a, AttnGradParts parts) {
@@ -563,7 +575,6 @@ __global__ void __launch_bounds__(kThreads, 2) attn_bwd_q_bf16_kernel(AttnArgs a
 #pragma unroll
         for (int e = 0; e < 8; e++) delta = __builtin_fmaf((float)qv[i][e], (float)gv[i][e], delta);
     delta = sum_halves(delta);
-    if (w.ok && half == 0 && part == 0) a.delta[stat] = delta;
     load_row<DT>(static_cast<const uint16_t *>(a.q) + (r.q0 + w.q) * a.q_stride + (int64_t)w.h * D, w.ok, D, half, qv);
     const float c = a.scale * kLog2e;
     const float lse2 = w.ok ? a.lse[stat] * kLog2e : 0.0f;
@@ -574,19 +585,18 @@ __global__ void __launch_bounds__(kThreads, 2) attn_bwd_q_bf16_kernel(AttnArgs a
     ks.init(a.k_stride, wave, lane);
     vs.init(a.v_stride, wave, lane);
     const uint32_t base = lds_addr(smem);
-    Addresses<DT> f;
+    Frags<DT> f;
     f.init(lane, base);
     f32x16_t dq[DT] = {};
-    const int per = SPLIT ? (w.nk + (int)gridDim.y - 1) / (int)gridDim.y : w.nk;
+    const bool twice = w.nk <= kFewTiles;  // all of them in the first part then, which has the row's whole sum
+    const int per = SPLIT && !twice ? (w.nk + (int)gridDim.y - 1) / (int)gridDim.y : w.nk;
     const int j0 = SPLIT ? part * per : 0, nk = SPLIT && j0 + per < w.nk ? j0 + per : w.nk;  // tiles j0 .. nk - 1
-    if (j0 < nk) {
-        ks.load(K, a.k_stride, j0 * kKeys, r.lk, D, base, wave);
-        vs.load(V, a.v_stride, j0 * kKeys, r.lk, D, base + 2 * G::kBytes, wave);
-    }
-    landed();
-    auto iteration = [&](int j, auto stage) {
+    float rest;  // sum of dS over this lane's half of the row
+    auto iteration = [&](int j, auto stage, auto sum_only) {
         constexpr int st = decltype(stage)::value;
+        constexpr bool SUM = decltype(sum_only)::value;
         constexpr uint32_t kt = st * G::kBytes, vt = (2 + st) * G::kBytes;
+        f.hold();
         const int k0 = j * kKeys;
         const bool more = j + 1 < nk, active = k0 <= w.any_seen;
         if (more) {
@@ -595,14 +605,18 @@ __global__ void __launch_bounds__(kThreads, 2) attn_bwd_q_bf16_kernel(AttnArgs a
         }
         if (active) {
             f32x16_t sc, dp;
-            bf16x8_t ds[2];
+            bf16x8_t ds[2], low[2];
             // for each 32 keys: groups of S, then of dP (four steps of 16 features each) with the exponentials between their
             // instructions, then two of dq
-            constexpr int kS = (2 * DT + 3) / 4, kAll = 2 * kS + 2;
+            constexpr int kS = (2 * DT + 3) / 4, kAll = 2 * kS + (SUM ? 0 : 2);
             auto dscore = [&](int h) {  // half h of dS = P (dP - delta)
 #pragma unroll
-                for (int i = 8 * h; i < 8 * h + 8; i++) sc[i] *= dp[i];
-                ds[h] = pack8(sc, h);
+                for (int i = 8 * h; i < 8 * h + 8; i++) {
+                    sc[i] *= dp[i];
+                    rest += sc[i];
+                }
+                asm volatile("" : "+v"(rest));  // summed here: put off, the sum would hold its terms' registers
+                if constexpr (!SUM) ds[h] = pack8(sc, h);
             };
             pipelined<2 * kAll>(
                 [&](auto g, bf16x8_t (&x)[4]) {
@@ -639,9 +653,15 @@ __global__ void __launch_bounds__(kThreads, 2) attn_bwd_q_bf16_kernel(AttnArgs a
                             }
                         });
                     } else {
+                        constexpr int m = n - 2 * kS;
                         static_for<DT>([&](auto t) {
-                            dq[t] = mfma(x[t], ds[n - 2 * kS], dq[t]);
-                            if constexpr (n == 2 * kS && t == 0) dscore(1);  // the second half behind the first's products
+                            dq[t] = mfma(x[t], ds[m], dq[t]);
+                            if constexpr (t == 0) low[m] = pack8_rest(sc, m, ds[m]);
+                            __builtin_amdgcn_sched_barrier(0);
+                        });
+                        static_for<DT>([&](auto t) {
+                            dq[t] = mfma(x[t], low[m], dq[t]);
+                            if constexpr (m == 0 && t == 0) dscore(1);
                             __builtin_amdgcn_sched_barrier(0);
                         });
                     }
@@ -652,14 +672,31 @@ __global__ void __launch_bounds__(kThreads, 2) attn_bwd_q_bf16_kernel(AttnArgs a
                                 if (k0 + 32 * b + acc_row(i) + 4 * half > w.seen) sc[i] = dp[i] = 0.0f;
                         }
                         dscore(0);
+                        if constexpr (SUM) dscore(1);
                     }
                 });
         }
         landed();
     };
-    for (int j = j0; j < nk; j += 2) {
-        iteration(j, std::integral_constant<int, 0>{});
-        if (j + 1 < nk) iteration(j + 1, std::integral_constant<int, 1>{});
+    auto through = [&](auto sum_only) {
+        rest = 0.0f;
+        if (j0 < nk) {
+            ks.load(K, a.k_stride, j0 * kKeys, r.lk, D, base, wave);
+            vs.load(V, a.v_stride, j0 * kKeys, r.lk, D, base + 2 * G::kBytes, wave);
+        }
+        landed();
+        for (int j = j0; j < nk; j += 2) {
+            iteration(j, std::integral_constant<int, 0>{}, sum_only);
+            if (j + 1 < nk) iteration(j + 1, std::integral_constant<int, 1>{}, sum_only);
+        }
+        rest = sum_halves(rest);
+        if (!SPLIT || twice) delta += rest;
+    };
+    if (twice) through(std::true_type{});
+    through(std::false_type{});
+    if (w.ok && half == 0) {
+        if (part == 0) a.delta[stat] = delta;
+        if (SPLIT) parts.rest[(int64_t)part * a.Hq * a.Tq + stat] = twice ? 0.0f : rest;
     }
     if constexpr (SPLIT) {
         store_part<DT>(parts.dq + (((int64_t)part * a.Tq + r.q0 + w.q) * a.Hq + w.h) * D, w.ok, D, half, dq);
@@ -881,17 +918,24 @@ __global__ void __launch_bounds__(kThreads, 2) attn_bwd_kv_bf16_kernel(AttnArgs 
     store_row<DT>(static_cast<uint16_t *>(a.dv) + (r.k0 + k) * a.dv_stride + (int64_t)hk * D, ok, D, half, dv, 1.0f);
 }
 
-// Adds the parts of a gradient [tokens][heads][D] in order, four features per thread, and rounds the sum times `scale`.
-// HBM-bound: two parts of 8,192 tokens with 8 heads of 128, 84 MB, 21 us (4.0 TB/s).
+// Adds the parts of a gradient [tokens][heads][D] in order, four features per thread, and rounds the sum times `scale`;
+// dq's (`rest` given) also the parts of the rows' sums of dS, to delta.
+// HBM-bound: three parts of 8,192 tokens with 8 heads of 128, 117 MB, 21 us (5.6 TB/s).
 // cu: ends of the sequences, whose tokens alone have parts
 __global__ void __launch_bounds__(256) attn_grad_join_kernel(const float *part, int splits, int64_t tokens, int heads, int D,
                                                              const int32_t *cu, int n_seq, uint16_t *out, int64_t stride,
-                                                             float scale) {
+                                                             float scale, const float *rest, float *delta) {
     const int64_t row = (int64_t)heads * D, all = tokens * row;
     const int64_t at = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4;
     if (at >= all) return;
     const int64_t token = at / row;
     if (cu && (token < cu[0] || token >= cu[n_seq])) return;
+    if (rest && at % D == 0) {
+        const int64_t stat = (at - token * row) / D * tokens + token;
+        float d = delta[stat];
+        for (int s = 0; s < splits; s++) d += rest[s * heads * tokens + stat];
+        delta[stat] = d;
+    }
     f32x4_t sum = {};
     for (int s0 = 0; s0 < splits; s0 += 4) {
         f32x4_t v[4];
@@ -989,26 +1033,28 @@ hipError_t launch_attn_bwd_bf16(const AttnArgs &a, float *parts, hipStream_t st)
     const AttnBwdPlan p = plan_attn_bwd_bf16(a.Tq, a.Tk, a.Hq, a.Hkv, a.n_seq);
     const int64_t dq_size = a.Tq * a.Hq * a.D, dk_size = a.Tk * a.Hkv * a.D;
     AttnGradParts g{};
-    g.dq = parts;
-    g.dk = parts + (p.q_splits > 1 ? p.q_splits * dq_size : 0);
+    g.rest = parts;
+    g.dq = parts + attn_rest_floats(p.q_splits, a.Tq * a.Hq);
+    g.dk = g.dq + (p.q_splits > 1 ? p.q_splits * dq_size : 0);
     g.dv = g.dk + p.k_splits * dk_size;
     const dim3 q_grid((unsigned)(q_slots * a.Hkv), (unsigned)p.q_splits), k_grid((unsigned)(k_slots * a.Hkv), (unsigned)p.k_splits);
+    auto add = [&](const float *part, int splits, int64_t tokens, int heads, const int32_t *cu, void *out, int64_t stride, float scale,
+                   const float *rest) {
+        const int64_t threads = tokens * heads * a.D / 4;
+        attn_grad_join_kernel<<<(unsigned)((threads + 255) / 256), 256, 0, st>>>(part, splits, tokens, heads, a.D, cu, a.n_seq,
+                                                                                static_cast<uint16_t *>(out), stride, scale, rest, a.delta);
+    };
     pick_dt(a.D, [&](auto dt) {
         constexpr int DT = decltype(dt)::value;
         if (a.Tq > 0 && p.q_splits > 1) attn_bwd_q_bf16_kernel<DT, true><<<q_grid, kThreads, 0, st>>>(a, g);
         else if (a.Tq > 0) attn_bwd_q_bf16_kernel<DT, false><<<q_grid, kThreads, 0, st>>>(a, g);
+        if (a.Tq > 0 && p.q_splits > 1) add(g.dq, p.q_splits, a.Tq, a.Hq, a.cu_q, a.dq, a.dq_stride, a.scale, g.rest);  // and delta
         if (a.Tk > 0 && p.k_splits > 1) attn_bwd_kv_bf16_kernel<DT, true><<<k_grid, kThreads, 0, st>>>(a, g);
         else if (a.Tk > 0) attn_bwd_kv_bf16_kernel<DT, false><<<k_grid, kThreads, 0, st>>>(a, g);
     });
-    auto add = [&](const float *part, int splits, int64_t tokens, int heads, const int32_t *cu, void *out, int64_t stride, float scale) {
-        const int64_t threads = tokens * heads * a.D / 4;
-        attn_grad_join_kernel<<<(unsigned)((threads + 255) / 256), 256, 0, st>>>(part, splits, tokens, heads, a.D, cu, a.n_seq,
-                                                                                static_cast<uint16_t *>(out), stride, scale);
-    };
-    if (a.Tq > 0 && p.q_splits > 1) add(g.dq, p.q_splits, a.Tq, a.Hq, a.cu_q, a.dq, a.dq_stride, a.scale);
     if (a.Tk > 0 && p.k_splits > 1) {
-        add(g.dk, p.k_splits, a.Tk, a.Hkv, a.cu_k, a.dk, a.dk_stride, a.scale);
-        add(g.dv, p.k_splits, a.Tk, a.Hkv, a.cu_k, a.dv, a.dv_stride, 1.0f);
+        add(g.dk, p.k_splits, a.Tk, a.Hkv, a.cu_k, a.dk, a.dk_stride, a.scale, nullptr);
+        add(g.dv, p.k_splits, a.Tk, a.Hkv, a.cu_k, a.dv, a.dv_stride, 1.0f, nullptr);
     }
     return hipGetLastError();
 }

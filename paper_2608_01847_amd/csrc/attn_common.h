@@ -135,10 +135,12 @@ __device__ __forceinline__ constexpr int acc_row(int r) { return (r & 3) + 8 * (
 struct AttnParts {
     float *m, *l, *o;
 };
-// Gradients of a backward whose sums are split, fp32: dq [splits][Tq][Hq][D], dk and dv [splits][Tk][Hkv][D]
+// Gradients of a backward whose sums are split, fp32: dq [splits][Tq][Hq][D], dk and dv [splits][Tk][Hkv][D]; with dq the rows'
+// sums of dS [splits][Hq][Tq]
 struct AttnGradParts {
-    float *dq, *dk, *dv;
+    float *rest, *dq, *dk, *dv;
 };
+inline int64_t attn_rest_floats(int q_splits, int64_t rows) { return q_splits > 1 ? (q_splits * rows + 63) / 64 * 64 : 0; }
 struct AttnBwdPlan {
     int q_splits, k_splits;
 };

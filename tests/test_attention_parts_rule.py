@@ -46,9 +46,10 @@ def key_parts(L, Hq, Hkv, Tq, Tk, n, D=128):
     """(parts of dq, parts of dk and dv; 0: whole) that add up to the workspace, which holds a whole fp32 tensor for each."""
     cfg = focus.AttentionConfig(Hq, Hkv, D, 1, 0.1, 0, *(0,) * 6)
     size = L.focus_attention_workspace_size(focus.CALL_ATTENTION_BWD, ctypes.byref(cfg), Tq, Tk, n) - 256
-    rest = size - -(-Tq * Hq * 4 // 256) * 256
+    whole = lambda n: -(-n * Tq * Hq * 4 // 256) * 256  # numbers of the rows: delta, and with dq's parts the sums of theirs
     dq, dkv = Tq * Hq * D * 4, 2 * Tk * Hkv * D * 4
-    return [(q, k) for q in range(17) for k in range(17) if q * dq + k * dkv == rest and q != 1 and k != 1]
+    return [(q, k) for q in range(17) for k in range(17)
+            if q != 1 and k != 1 and whole(1) + whole(q) + q * dq + k * dkv == size]
 
 
 @pytest.mark.parametrize("Hq,Hkv,Tq,Tk,n,q", [(32, 8, 64, 2048, 1, 8), (4, 4, 512, 4096, 1, 16), (4, 4, 2028, 2028, 4, 0), (8, 8, 256, 256, 1, 0)])
