@@ -406,12 +406,13 @@ __global__ void __launch_bounds__(kBwdThreads) logprobs_bwd_kernel(LogprobBwdArg
 }
 
 // Parts of a row: up to two workgroups per CU, and no more than the row has steps (so that a part is a step or little less at
-// least), where that takes off enough of a row's steps to pay for the join. With 5 alternatives, one row of 151,936 (10 steps) takes 15.9 us in parts and 19.9 us in one, of 65,536 (4
-// steps) 15.6 and 12.3; 32 rows of 151,936 19.6 and 20.4, 64 rows 22.8 and 20.2;
-// 64 rows of 300,000 (19 steps) 25.7 and 32.7, 256 rows 42.2 and 34.9.
+// least), where that takes off enough of a row's steps to pay for the join and the rows do not keep the memory busy as they are. In
+// parts and in one, us, 5 alternatives: one row of 100,000 (7 steps) 17.7 and 15.3, of 151,936 (10) 17.4 and 18.2, 16 rows of these
+// 17.8 and 18.4, 32 rows 19.4 and 18.5, 63 rows 21.2 and 18.5; 64 rows of 300,000 (19) 24 and 31, 128 rows 29 and 31, 255 rows 40
+// and 33.
 int plan_splits(int64_t T, int64_t V) {
     const int64_t steps = (V + kStep - 1) / kStep;
-    if (T >= 256 || steps <= (T < 64 ? 4 : 16)) return 1;
+    if (T > 128 || steps <= (T < 32 ? 7 : 16)) return 1;
     return (int)std::min<int64_t>({kMaxParts / T, steps, kMaxSplits});
 }
 

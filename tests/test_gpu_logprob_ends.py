@@ -59,3 +59,35 @@ def test_masked_logits_at_the_end(F, n, mask, dt):
         some = torch.isfinite(lp[:, 0])
         assert ((logp.double().cpu() - lp[:, 0]).abs()[some] <= 2e-5 + 2.0 ** -22 * lp[some, 0].abs()).all()
         assert torch.equal(torch.isneginf(logp.cpu()), ~some)
+
+
+@pytest.mark.parametrize("top", [1, 5, 64])
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("T,V", [(1, 131073), (9, 151935), (31, 140001), (40, 300001), (128, 280003)])
+def test_rows_in_parts_with_ragged_ends(F, T, V, dt, top):
+    """Parts that end inside a vector; the largest in one part or spread, equal over the parts; parts without a token."""
+    from test_gpu_token_logprobs import check
+    g = torch.Generator().manual_seed(V)
+    i = torch.arange(V)
+    kinds = [torch.randn(V, generator=g), torch.zeros(V), i.float() / 64, torch.where(i > V - 70, 3.0, -1.0),
+             torch.where(i % 15000 == 0, 4.0, torch.randn(V, generator=g)), torch.where(i < V // 2, -math.inf, 1.0),
+             torch.where(i == V - 1, 0.0, -math.inf), torch.full((V,), torch.finfo(DT[dt]).min)]
+    announce(f"ragged parts {dt} {T}x{V} top={top}")
+    Z = torch.stack([kinds[t % len(kinds)] for t in range(T)]).to(DT[dt]).cuda()
+    t = torch.randint(-1, V, (T,), generator=g).cuda()
+    check(F, Z, t, top)
+
+
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+def test_domain_errors_in_parts(F, bad):
+    T, V = 5, 140001
+    Z = (torch.randn(T, V, generator=torch.Generator().manual_seed(1)) * 2.5).bfloat16().cuda()
+    Z[1, V - 2] = bad
+    ws = F.workspace(F.token_logprobs_workspace_size(T, V, 3))
+    logp, _, lse, _, _ = F.token_logprobs(Z, torch.zeros(T, dtype=torch.int64).cuda(), 3, ws=ws)
+    assert F.check_flags(ws) == F.ERR_DOMAIN
+    keep = [0, 2, 3, 4]
+    assert torch.isfinite(logp[keep]).all() and torch.isfinite(lse[keep]).all()
+    Z[1, V - 2] = 0.0
+    logp = F.token_logprobs(Z, torch.tensor([3, V, -5, 0, 1]).cuda(), ws=ws)[0]
+    assert F.check_flags(ws) == F.ERR_DOMAIN and logp[1] == 0 and logp[2] == 0
