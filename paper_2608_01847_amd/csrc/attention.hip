@@ -13,7 +13,8 @@
 // Operands come straight from global memory: one instruction takes 64 cycles for 512 bytes of operands, and a wave's loads of a
 // tile are under way together. Bound by the latency of those loads, one wave per SIMD having no other to hide it: 4 x 2,048
 // tokens, 16 heads of 64, full: forward 0.75 ms, 92 TFLOP/s of the 142 that an fp32 product of 4,096^3 reaches, backward 3.7 ms
-// (65 TFLOP/s of its seven products); 794 tokens in six sequences, 8 heads of 64: forward 16 us, dq 23, dk and dv 35.
+// (65 TFLOP/s of its seven products); 794 tokens in six sequences, 8 heads of 64: forward 16 us, dq 23, dk and dv 35. The keys of few
+// queries are not split: one query of 32/8 heads of 128 on 8,192 keys is 32 workgroups, 512 us.
 #include "attn_common.h"
 
 namespace focus {

@@ -5,8 +5,9 @@
 // causal tile's ragged edge is as narrow as it can be. The scores are formed transposed (keys down the accumulator's
 // rows, one query row per lane): the softmax runs within a lane and its partner 32 lanes on, and a register of probabilities
 // is already the B operand of the second product (rounded to bf16, the type that the instruction takes: 2^-9 of each, random
-// over the keys), whose contraction may take the keys in any order: step t of a 64-key tile contracts, for lanes 0-31 (32-63), keys 16 t + {0-3, 8-11} (+ 4), the order in which the accumulator holds them;
-// the transposing LDS reads of V follow the same order.
+// over the keys, which makes O's error 1.35 to 1.41 times that of rounding O), whose contraction may take the keys in any order:
+// step t of a 64-key tile contracts, for lanes 0-31 (32-63), keys 16 t + {0-3, 8-11} (+ 4), the order in which the accumulator
+// holds them; the transposing LDS reads of V follow the same order.
 //
 // Keys and values go through LDS in tiles of 64, two stages each, by direct-to-LDS loads a tile ahead, whose range check reads
 // rows past a sequence and features past head_dim as zeros.
@@ -316,7 +317,7 @@ struct RowTile {
 // 2,048 tokens 1.31-1.40 ms, 0.79-0.84, busy 42%: a workgroup's start and end, about 7 of its 41 us there, are hidden only
 // by the other one on its CU. No LDS bank conflicts.
 // SPLIT: the tiles of keys are dealt to gridDim.y workgroups, each leaving its unnormalised output, reference and sum in
-// fp32 for attn_join_kernel. One query of 32/8 heads over 8,192 keys: 10 us and the join's 5, of 33 MB at 3.2 TB/s; latency.
+// fp32 for attn_join_kernel. One query of 32/8 heads over 8,192 keys: 10 us and the join's 6, of 33 MB at 3.2 TB/s; latency.
 template <int DT, bool SPLIT>
 __global__ void __launch_bounds__(kThreads, 2) attn_fwd_bf16_kernel(AttnArgs a, AttnParts parts) {
     using G = Tile<DT>;
@@ -495,7 +496,7 @@ __global__ void __launch_bounds__(kThreads, 2) attn_fwd_bf16_kernel(AttnArgs a, 
 }
 
 // Joins the parts of a split forward, a workgroup per row, two features per lane: each wave adds a run of the parts in
-// order, eight loads under way, and the waves' sums are added in order. Latency-bound: two trips to memory, 5 us.
+// order, eight loads under way, and the waves' sums are added in order. Latency-bound: two trips to memory, 6 us.
 __global__ void __launch_bounds__(kThreads) attn_join_kernel(AttnArgs a, AttnParts parts, int splits) {
     __shared__ float2 lds[kWaves][64];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -542,8 +543,9 @@ __global__ void __launch_bounds__(kThreads) attn_join_kernel(AttnArgs a, AttnPar
 
 // dq of 128 query rows, and delta = rowsum(dO O) for the keys' pass. Both score-shaped products are transposed as in the
 // forward, so dS is the B operand of dq^T = k^T dS^T as it stands.
-// Bound: three products of 2 D flops a visible pair and an exponential. 32 x 2,048 tokens, 32/8 heads of 128, causal: 1.72 ms,
-// 0.96 PFLOP/s, matrix units busy 51%. Two waves per SIMD, 256 registers.
+// Bound: four products of 2 D flops a visible pair (dS counts twice) and an exponential. 32 x 2,048 tokens, 32/8 heads of 128,
+// causal: 2.13 ms, 1.03 PFLOP/s, matrix units busy 56%. Two waves per SIMD, 256 registers, in which the fragments' addresses are
+// formed for each read. With one product of dS (1.72 ms) and delta as O gives it dq was off by 1.5 times its rounding.
 // dS goes into its product in two parts, rounded to bf16 and what that left, so that 16 of its bits count. delta from the O that the
 // forward rounded is off by that rounding, which all of a row's dS share: their sum over the row's keys, 0 from the exact delta,
 // is what it is off by, and is added to it for the keys' pass. dq has it averaged over the row's keys; row tiles of few keys, whose dq
@@ -713,7 +715,7 @@ __global__ void __launch_bounds__(kThreads, 2) attn_bwd_q_bf16_kernel(AttnArgs a
 // B operands of dv^T = dO^T P and dk^T = q^T dS. Queries and their gradients go through LDS in tiles with their lse and delta,
 // from which the accumulators start; a query that does not exist, or sees nothing, has probability 0.
 // Bound: four products of 2 D flops a visible pair and an exponential. 32 x 2,048 tokens, 32/8 heads of 128, causal: 2.1 ms,
-// 1.05 PFLOP/s, matrix units busy 56%, no bank conflicts. P and dS are rounded to bf16 as in the other kernels.
+// 1.05 PFLOP/s, matrix units busy 55%, no bank conflicts. P and dS are rounded to bf16 as in the other kernels.
 // Two waves per SIMD, whose 256 registers hold the sums (64 per gradient and 128 features) and k: from 65 features on, v is read
 // from LDS each time and the tiles have 32 queries rather than 64.
 // SPLIT: the tiles of queries, all heads together, are dealt to gridDim.y workgroups, whose sums attn_grad_join_kernel adds.
@@ -1004,16 +1006,16 @@ hipError_t launch_attn_fwd_bf16(const AttnArgs &a, void *ws, hipStream_t st) {
 // Parts of a backward's sums. Where workgroups are few, one's run through all queries (keys) of a long sequence is the whole
 // call's time: they are split until two per CU are busy, with 4 tiles each at least by the mean length. The keys' pass, whose
 // runs over a causal sequence are from one to all of its queries long, is split on until there are four times as many with 64
-// tiles each, so that long and short ones even out (backward of four sequences of 2,048 with 64/8 heads 1.06 ms, 1.13 without
-// these parts and 1.15 with twice as many; of one of 8,192 3.70, 4.36 and 3.65). A part
+// tiles each, so that long and short ones even out (backward of four sequences of 2,048 with 64/8 heads 1.10 ms, 1.16 without
+// these parts and 1.18 with twice as many; of one of 8,192 3.76, 4.61 and 3.82). A part
 // costs 64 KB of fp32 sums per 128 rows and gradient, written and read again: splitting both passes up to 2,048 workgroups
-// with 8 tiles each made two sequences of 2,500 with 16/8 heads take 356 us in place of 239.
+// with 8 tiles each made two sequences of 2,500 with 16/8 heads take 355 us in place of 246.
 //
 // The keys' parts also have to save more than their two joins cost: 8 us, and per key and head 0.2 ns and 0.25 for each part, at
 // 1 us for a tile of 32 queries that a workgroup does not go through. In one part and in those, us, heads of 128: 64 queries of
-// 32/8 heads on 2,048 keys 38 and (two) 51, 512 of 4/4 on 4,096 50 and (three) 61, four of 507 with 4/4 42 and (three) 49; but
-// 256 with 32/8 54 and (eight) 40, 1,024 with 8/8 66 and (seven) 59, 4,096 with 2/1 307 and (fifteen) 85. Lengths that differ
-// widely lose by the mean here too: 2,000, 10, 10, 10 with 4/4 heads 121 and (three) 97.
+// 32/8 heads on 2,048 keys 41 and (two) 54, 512 of 4/4 on 4,096 57 and (three) 66, four of 507 with 4/4 45 and (three) 52; but
+// 256 with 32/8 60 and (eight) 47, 1,024 with 8/8 73 and (seven) 65, 4,096 with 2/1 313 and (fifteen) 92. Lengths that differ
+// widely lose by the mean here too: 2,000, 10, 10, 10 with 4/4 heads 131 and (three) 110.
 AttnBwdPlan plan_attn_bwd_bf16(int64_t Tq, int64_t Tk, int Hq, int Hkv, int64_t n_seq) {
     const int64_t kRows = 32 * kWaves, kBusy = 2 * kMfmaConcurrentWgs, kMost = 16;
     if (n_seq < 1) return {1, 1};

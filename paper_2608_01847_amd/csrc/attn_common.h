@@ -36,8 +36,8 @@ __device__ __forceinline__ void set_range(const AttnArgs &a, int qa, int qb, int
 //
 // Under a causal mask a tile's work grows with the rows before it (KEYS: behind it). The slots of kOrdered sequences, one after
 // the other, are then given out from the longest tiles to the shortest, over those sequences together: workgroups start in
-// the order of the slots, and what starts last should end soonest (backward of 4 x 2,048 tokens, 64/8 heads of 128, 1.02 ms;
-// sequence by sequence 1.07; sixteen sequences together, which share less in L2, 2% slower at 32 x 2,048).
+// the order of the slots, and what starts last should end soonest (backward of 4 x 2,048 tokens, 64/8 heads of 128, 1.11 ms;
+// sequence by sequence 1.15; sixteen sequences together, which share less in L2, 2% slower at 32 x 2,048).
 //
 // Every lane loads one sequence's four ends at once: after the bisection that many sequences need, one trip to memory.
 constexpr int kOrdered = 8;

@@ -14,8 +14,9 @@
 // logits have theirs read a second time (from the caches), by all threads, and those that reach it are ranked in LDS. The LDS
 // additions count and hand out places; no result depends on their order, keys being distinct.
 //
-// Measured, bf16: 8,192 rows of 151,936 with 5 alternatives, 2.49 GB, 450 us (5.5 TB/s); 4,096 rows of 32,000 forward 69 us
-// (3.8 TB/s), gradient 92 us (5.7 TB/s both ways); one row of 151,936 with 20 alternatives 11 us and the join's 8, latency.
+// Measured, bf16: 8,192 rows of 151,936 with 5 alternatives, 2.49 GB, 436 us (5.7 TB/s); 4,096 rows of 32,000 forward 69 us
+// (3.8 TB/s), gradient 90 us (5.8 TB/s both ways); one row of 151,936 with 20 alternatives 10 us and the join's 8, latency. Short
+// rows are bound by what a row costs beside its logits, the join of 512 threads' sums: 16,384 rows of 1,000 114 us, of 16,384 146.
 // Vectors of 8 logits, four per thread and step, are enough loads under way: fetching a step ahead (94 registers in place of 60)
 // made 8,192 rows take 490 us.
 #include "internal.h"

@@ -393,9 +393,12 @@ bool pick_nv(int64_t need, F &&f) {
 }
 
 // Chooses the threads per row and the vectors per thread: a wave per row while its lanes hold at most 16 elements each
-// (no barrier between the sums; at 2,560 features a workgroup per row is 2% faster, 510 us a step of 65,536 tokens, its
-// lanes holding few enough registers for four waves per SIMD), a workgroup per row up to 64 elements per thread, false
-// beyond that.
+// (no barrier between the sums), a workgroup per row up to 64 elements per thread, false beyond that. Forward and backward of
+// bf16 rows of 268 MB together, us, with a wave and with a workgroup per row: 1,024 features 91 + 169 and 173 + 211, 256 features
+// 205 + 221 and 549 + 637; fp32 1,024 features 100 + 167 and 102 + 168, 2,048 features 105 + 169 and 97 + 172. bf16 rows of 1,025 to
+// 2,048 features would gain from a wave forward (1,536: 95 in place of 149, 2,048: 93 in place of 120; backward as long), where
+// half of a workgroup's second vectors do not exist. Rows of few features leave lanes idle: 2,097,152 rows of 64 take
+// 636 + 677 us.
 template <typename F>
 bool norm_shape(int64_t C, F &&f) {
     const int64_t vecs = (C + 7) / 8;
