@@ -119,7 +119,12 @@ typedef enum {
     FOCUS_CALL_TOKEN_LOGPROBS = 15, /* M = tokens, N = vocabulary, K = alternatives (`top`) */
     FOCUS_CALL_TOKEN_LOGPROBS_BWD = 16,
     FOCUS_CALL_ATTENTION_FWD_F32 = 17,  /* sized by focus_attention_workspace_size: fp32, no more than bf16 */
-    FOCUS_CALL_ATTENTION_BWD_F32 = 18
+    FOCUS_CALL_ATTENTION_BWD_F32 = 18,
+    FOCUS_CALL_SANDWICH_NORM_FWD = 19,  /* M = tokens, K = features */
+    FOCUS_CALL_SANDWICH_NORM_BWD = 20,
+    FOCUS_CALL_LINEAR_CE_FWD = 21,      /* M = tokens, N = vocabulary, K = features */
+    FOCUS_CALL_LINEAR_CE_BWD = 22,
+    FOCUS_CALL_CLIP_GRAD_NORM = 23      /* M = tensors */
 } focus_call;
 
 /* Workspace bytes a call needs for the given sizes (M = tokens, N = rows / out features,
@@ -500,12 +505,108 @@ focus_status focus_token_logprobs_bwd(const void *Z, int dtype, int64_t T, int64
                                       const float *lse, const float *entropy_opt, const float *d_logp_opt,
                                       const float *d_entropy_opt, void *dZ, void *ws, size_t ws_bytes, focus_stream stream);
 
+/* ---- the rest of a training step ----------------------------------------------------------------- */
+
+/* How a block's normalised output is gated in focus_sandwich_norm_*. */
+typedef enum { FOCUS_GATE_NONE = 0, FOCUS_GATE_FEATURE = 1, FOCUS_GATE_TOKEN = 2 } focus_gate;
+
+/*   kind           : focus_norm_kind of both norms.
+ *   gate           : focus_gate; FOCUS_GATE_FEATURE: one number per feature, FOCUS_GATE_TOKEN: one per token and feature.
+ *   eps            : of both norms, >= 0 and finite.
+ *   residual_scale : factor of the residual stream, finite. */
+typedef struct {
+    int32_t kind;
+    int32_t gate;
+    float eps;
+    float residual_scale;
+} focus_sandwich_config;
+
+/* The norms after and before a block in one pass: the block's output B is normalised, gated and added to the scaled residual
+ * stream X, and the sum is normalised for the next block (statistics as in focus_norm_fwd):
+ *   U = norm(B) w_post + b_post,  Y = residual_scale X + gate U,  N = norm(Y) w_pre + b_pre
+ * N is the norm of Y before Y is rounded to dtype.
+ *   X, B, Y, N [T][C] (dtype); w_post, w_pre, b_post_opt, b_pre_opt [C] (w_dtype, either type); gate: NULL with FOCUS_GATE_NONE,
+ *   [C] (w_dtype) with FOCUS_GATE_FEATURE, [T][C] (dtype) with FOCUS_GATE_TOKEN. Sums in fp32.
+ *   stats_opt fp32, what the backward needs: [2][T] rstd of B, rstd of Y; a layer norm's [4][T], the means of B and Y behind them.
+ *   Y and N may each be X, B or a token's gate (of the same place), but not one another; apart from that they share no memory with the inputs.
+ * 0 <= T < 2^31, 0 <= C <= 2^24 (FOCUS_ERR_SHAPE). ws: focus_workspace_size(FOCUS_CALL_SANDWICH_NORM_FWD, NULL, T, 0, C). */
+focus_status focus_sandwich_norm_fwd(const focus_sandwich_config *cfg, const void *X, const void *B, int dtype, int64_t T,
+                                     int64_t C, const void *w_post, const void *b_post_opt, const void *gate,
+                                     const void *w_pre, const void *b_pre_opt, int w_dtype, void *Y, void *N,
+                                     float *stats_opt, void *ws, size_t ws_bytes, focus_stream stream);
+
+/* Its backward pass, from the inputs of the forward (U and Y are formed again) and its stats. With xb = norm(B), xy = norm(Y):
+ *   G = dN w_pre,  D = dY_opt + rstd_y (G - mean_c(G) - xy mean_c(G xy))      (the gradient of Y; RMS: without mean_c(G))
+ *   dX = residual_scale D,  dgate = D U,  P = D gate w_post,  dB = rstd_b (P - mean_c(P) - xb mean_c(P xb))
+ *   dw_pre = sum over tokens of dN xy, db_pre = of dN, dw_post = of D gate xb, db_post = of D gate
+ *   dY_opt: the gradient that reaches Y past the second norm, or NULL. dN, dY_opt, dX, dB [T][C] in dtype.
+ *   dgate_opt: FOCUS_GATE_FEATURE: [C] fp32, summed over the tokens; FOCUS_GATE_TOKEN: [T][C] in dtype; NULL where it is not
+ *   wanted (and with FOCUS_GATE_NONE). dw_* and db_*_opt [C] fp32, overwritten; with T == 0 they and a feature's dgate are zeros.
+ *   dX, dB and a token's dgate may each be any one of X, B, gate, dN and dY (of the same place), but not one another.
+ * The sums over tokens have a fixed order. ws: focus_workspace_size(FOCUS_CALL_SANDWICH_NORM_BWD, NULL, T, 0, C) bytes. */
+focus_status focus_sandwich_norm_bwd(const focus_sandwich_config *cfg, const void *dN, const void *dY_opt, const void *X,
+                                     const void *B, int dtype, int64_t T, int64_t C, const void *w_post,
+                                     const void *b_post_opt, const void *gate, const void *w_pre, int w_dtype,
+                                     const float *stats, void *dX, void *dB, void *dgate_opt, float *dw_post,
+                                     float *db_post_opt, float *dw_pre, float *db_pre_opt, void *ws, size_t ws_bytes,
+                                     focus_stream stream);
+
+/* Softmax cross entropy of an output layer over its vocabulary without the logits: the log probabilities of given tokens under
+ * Z = X W^T, as focus_token_logprobs gives them from logits in memory.
+ *   lse[t] = log sum_v exp Z[t][v]                                         (fp32 [T])
+ *   logp_opt[t] = Z[t][target[t]] - lse[t]; 0 where target[t] < 0 (a token left out)
+ *   X [T][K] hidden states, W [V][K] weights (dtype: FOCUS_BF16, FOCUS_F32); products exact or in fp32, sums in fp32.
+ *   target_opt [T] int64 (NULL: none, logp_opt must be NULL too).
+ * The mean cross entropy of n tokens is -sum(logp) / n. X and W have to be finite: a token with a logit that is not raises the
+ * domain flag, as a target >= V does (which is taken as left out); the token's results are then unspecified.
+ * 0 <= T <= 2^24, 1 <= V <= 2^24, 1 <= K <= 2^20 (FOCUS_ERR_SHAPE); T == 0 is a no-op. bf16 with K % 16 == 0 runs on the matrix
+ * instructions. ws: focus_workspace_size(FOCUS_CALL_LINEAR_CE_FWD, NULL, T, V, K) bytes; it serves fewer tokens too. */
+focus_status focus_linear_ce_fwd(const void *X, const void *W, int dtype, int64_t T, int64_t V, int64_t K,
+                                 const int64_t *target_opt, float *logp_opt, float *lse, void *ws, size_t ws_bytes,
+                                 focus_stream stream);
+
+/* Its gradients, from lse as the forward wrote it. With g = d_logp[t] (0 where target[t] < 0), h = d_lse[t]:
+ *   D[t][v] = g ([v == target[t]] - p) + h p,  p = exp(Z[t][v] - lse[t]);  dX = D W,  dW = D^T X
+ * (the mean cross entropy of n tokens: d_logp = -1/n; a penalty on lse: d_lse). The vocabulary goes in pieces, of each of
+ * which the logits are formed again: D of one piece is what lies in memory, 1 GiB at most up to 2^20 tokens.
+ *   d_logp_opt [T] fp32 needs target_opt; one of d_logp_opt, d_lse_opt is given at least (FOCUS_ERR_NULL).
+ *   dX_opt [T][K] (dtype), dW_opt [V][K] (dw_dtype: FOCUS_F32, or FOCUS_BF16 with bf16 operands): overwritten, one of them is
+ *   wanted at least. dW in fp32 is the G of focus_fakequant_bwd. With T == 0 dW is zeros.
+ * p carries the rounding of lse, 2^-24 |lse| of it; a token with |lse| above 65,536 (or NaN) and a gradient other than 0 raises
+ * the domain flag. They share no memory with an input or one another.
+ * ws: focus_workspace_size(FOCUS_CALL_LINEAR_CE_BWD, NULL, T, V, K) bytes; it serves fewer tokens too. */
+focus_status focus_linear_ce_bwd(const void *X, const void *W, int dtype, int64_t T, int64_t V, int64_t K,
+                                 const int64_t *target_opt, const float *lse, const float *d_logp_opt,
+                                 const float *d_lse_opt, void *dX_opt, void *dW_opt, int dw_dtype, void *ws,
+                                 size_t ws_bytes, focus_stream stream);
+
+/* One gradient of focus_clip_grad_norm. */
+typedef struct {
+    const void *grad;  /* n elements (dtype), 16-byte aligned */
+    void *out;         /* the scaled gradient: grad itself, a tensor of its own, or NULL (counted in the norm only) */
+    int64_t n;         /* 0 <= n <= 2^36 */
+    int32_t dtype;     /* FOCUS_F32 or FOCUS_BF16, of grad and out */
+    int32_t reserved;  /* 0 */
+} focus_grad_tensor;
+
+/* The norm over all gradients of a step, and the gradients scaled so that it is at most max_norm (in front of
+ * focus_adamw_step):
+ *   norm = sqrt(sum over all elements of grad^2)  -> *norm_out (device fp64)
+ *   out = grad * max_norm / norm where norm > max_norm, else grad               (rounded to the tensor's dtype)
+ *   tensors: HOST array of n_tensors entries (0 .. 2^20), read during the call. max_norm > 0 (may be infinite; else FOCUS_ERR_CONFIG).
+ *   An out shares no memory with any other tensor's grad or out, nor with a part of its own grad (FOCUS_ERR_SHAPE).
+ * Squares are formed and summed in fp64, in a fixed order: no size of a gradient overflows. A norm that is not finite raises the
+ * domain flag and scales by 1. ws: focus_workspace_size(FOCUS_CALL_CLIP_GRAD_NORM, NULL, n_tensors, 0, 0) bytes. */
+focus_status focus_clip_grad_norm(const focus_grad_tensor *tensors, int64_t n_tensors, double max_norm, double *norm_out,
+                                  void *ws, size_t ws_bytes, focus_stream stream);
+
 /* Synchronises `stream`, reads and clears the workspace's sticky domain flag. Returns
  * FOCUS_ERR_DOMAIN if any call on this workspace met a NaN scale or a coefficient c that is
  * <= 0 or not finite, a log2-domain AdamW step met a parameter that is not positive and
  * finite, focus_kl_top met a logit that is not finite, focus_attention_* met sequence ends that do not rise, or
  * focus_token_logprobs met a NaN or +inf logit or a target past the vocabulary, or focus_token_logprobs_bwd an lse without digits
- * for its probabilities, since the last check (outputs of such
+ * for its probabilities, focus_linear_ce_* a logit that is not finite, a target past the vocabulary or an lse without digits, or
+ * focus_clip_grad_norm a norm that is not finite, since the last check (outputs of such
  * blocks are unspecified), FOCUS_OK otherwise, FOCUS_ERR_HIP on a runtime error. */
 focus_status focus_check_flags(void *ws, focus_stream stream);
 

@@ -8,6 +8,7 @@
 #include <cmath>
 #include <initializer_list>
 #include <mutex>
+#include <new>
 
 using namespace focus;
 
@@ -205,6 +206,79 @@ struct AttnRows {
     }
 };
 
+// ---- the rest of a training step ----------------------------------------------------------------
+struct Span {
+    const void *p;
+    int64_t bytes;
+};
+
+bool meet(Span a, Span b) {
+    if (!a.p || !b.p || a.bytes <= 0 || b.bytes <= 0) return false;
+    const uintptr_t x = reinterpret_cast<uintptr_t>(a.p), y = reinterpret_cast<uintptr_t>(b.p);
+    return x < y + (uintptr_t)b.bytes && y < x + (uintptr_t)a.bytes;
+}
+
+// Whether an output shares memory with another output or an input; `in_place`: an output may stand in an input's place
+bool clash(std::initializer_list<Span> outs, std::initializer_list<Span> ins, bool in_place) {
+    for (const Span *o = outs.begin(); o != outs.end(); o++) {
+        for (const Span *q = o + 1; q != outs.end(); q++)
+            if (meet(*o, *q)) return true;
+        for (const Span &i : ins)
+            if (meet(*o, i) && !(in_place && o->p == i.p && o->bytes == i.bytes)) return true;
+    }
+    return false;
+}
+
+focus_status check_sandwich(const focus_sandwich_config *cfg, int dtype, int w_dtype, int64_t T, int64_t C, const void *gate) {
+    if (!cfg) return FOCUS_ERR_NULL;
+    if (cfg->kind != FOCUS_NORM_LAYER && cfg->kind != FOCUS_NORM_RMS) return FOCUS_ERR_CONFIG;
+    if (cfg->gate != FOCUS_GATE_NONE && cfg->gate != FOCUS_GATE_FEATURE && cfg->gate != FOCUS_GATE_TOKEN) return FOCUS_ERR_CONFIG;
+    if (!std::isfinite(cfg->eps) || cfg->eps < 0.f || !std::isfinite(cfg->residual_scale)) return FOCUS_ERR_CONFIG;
+    if (cfg->gate == FOCUS_GATE_NONE && gate) return FOCUS_ERR_CONFIG;
+    if (!dtype_ok(dtype) || !dtype_ok(w_dtype)) return FOCUS_ERR_DTYPE;
+    FOCUS_TRY(check_norm_shape(T, C));
+    if (T > 0 && C > kMaxElems / T) return FOCUS_ERR_SHAPE;
+    return FOCUS_OK;
+}
+
+constexpr int64_t kCeMaxRows = int64_t(1) << 24, kCeMaxK = int64_t(1) << 20;
+focus_status check_linear_ce(int64_t T, int64_t V, int64_t K) {
+    return T < 0 || V < 1 || K < 1 || T > kCeMaxRows || V > kCeMaxRows || K > kCeMaxK ? FOCUS_ERR_SHAPE : FOCUS_OK;
+}
+
+constexpr int64_t kMaxGradTensors = int64_t(1) << 20;
+static_assert(sizeof(focus_grad_tensor) == sizeof(GradTensor), "the ABI's struct is the launcher's");
+
+Span grad_span(const focus_grad_tensor &t, const void *p) { return Span{p, t.n * (t.dtype == FOCUS_BF16 ? 2 : 4)}; }
+
+// An output in a place of its own or its gradient's. Tensors that lie in rising order, as a rule, need one pass; for others
+// their outputs are sorted by address (`order`: scratch of n indices).
+focus_status check_grad_places(const focus_grad_tensor *t, int64_t n, int32_t *order) {
+    int64_t k = 0;
+    for (int64_t i = 0; i < n; i++) {
+        if (t[i].n == 0 || !t[i].out) continue;
+        const Span o = grad_span(t[i], t[i].out), g = grad_span(t[i], t[i].grad);
+        if (o.p != g.p && meet(o, g)) return FOCUS_ERR_SHAPE;
+        order[k++] = (int32_t)i;
+    }
+    auto less = [&](int32_t a, int32_t b) { return (uintptr_t)t[a].out < (uintptr_t)t[b].out; };
+    if (!std::is_sorted(order, order + k, less)) std::sort(order, order + k, less);
+    for (int64_t i = 1; i < k; i++)
+        if (meet(grad_span(t[order[i - 1]], t[order[i - 1]].out), grad_span(t[order[i]], t[order[i]].out))) return FOCUS_ERR_SHAPE;
+    for (int64_t i = 0; i < n; i++) {
+        if (t[i].n == 0) continue;
+        const Span g = grad_span(t[i], t[i].grad);
+        // the outputs are disjoint: the first one that ends behind the gradient's start is the only one to look at, as far as
+        // it is not its own
+        const int32_t *at = std::partition_point(order, order + k, [&](int32_t j) {
+            return (uintptr_t)t[j].out + (uintptr_t)grad_span(t[j], t[j].out).bytes <= (uintptr_t)g.p;
+        });
+        for (; at != order + k && meet(grad_span(t[*at], t[*at].out), g); at++)
+            if (*at != i) return FOCUS_ERR_SHAPE;
+    }
+    return FOCUS_OK;
+}
+
 focus_status check_ends(const int32_t *cu_q, const int32_t *cu_k, int64_t n_seq) {
     if (!cu_q != !cu_k || (!cu_q && n_seq != 1)) return FOCUS_ERR_NULL;
     return aligned_to({cu_q, cu_k}, 4) ? FOCUS_OK : FOCUS_ERR_SHAPE;
@@ -264,6 +338,15 @@ size_t focus_workspace_size(int call, const focus_qconfig *q, int64_t M, int64_t
         return logprobs_ws(M, N, (int)K);
     }
     if (call == FOCUS_CALL_TOKEN_LOGPROBS_BWD) return check_logits(M, N) == FOCUS_OK ? kWsHeader : 0;
+    if (call == FOCUS_CALL_SANDWICH_NORM_FWD || call == FOCUS_CALL_SANDWICH_NORM_BWD) {
+        if (check_norm_shape(M, K) != FOCUS_OK || (M > 0 && K > kMaxElems / M)) return 0;
+        return call == FOCUS_CALL_SANDWICH_NORM_FWD ? kWsHeader : sandwich_bwd_ws(M, K);
+    }
+    if (call == FOCUS_CALL_LINEAR_CE_FWD || call == FOCUS_CALL_LINEAR_CE_BWD) {
+        if (check_linear_ce(M, N, K) != FOCUS_OK) return 0;
+        return call == FOCUS_CALL_LINEAR_CE_FWD ? linear_ce_fwd_ws(M, N) : linear_ce_bwd_ws(M, N, K);
+    }
+    if (call == FOCUS_CALL_CLIP_GRAD_NORM) return M < 0 || M > kMaxGradTensors ? 0 : clip_grad_norm_ws(M);
     if (check_q(q) != FOCUS_OK) return 0;
     const int B = block_of(q->format);
     switch (call) {
@@ -665,6 +748,135 @@ focus_status focus_token_logprobs_bwd(const void *Z, int dtype, int64_t T, int64
     if (T == 0) return FOCUS_OK;
     return hip_status(launch_logprobs_bwd(dtype, Z, T, V, target_opt, lse, entropy_opt, d_logp_opt, d_entropy_opt, dZ,
                                           flag_of(ws), (hipStream_t)stream));
+}
+
+focus_status focus_sandwich_norm_fwd(const focus_sandwich_config *cfg, const void *X, const void *B, int dtype, int64_t T,
+                                     int64_t C, const void *w_post, const void *b_post_opt, const void *gate,
+                                     const void *w_pre, const void *b_pre_opt, int w_dtype, void *Y, void *N,
+                                     float *stats_opt, void *ws, size_t ws_bytes, focus_stream stream) {
+    FOCUS_TRY(check_sandwich(cfg, dtype, w_dtype, T, C, gate));
+    if (T > 0 && C > 0 && (!X || !B || !w_post || !w_pre || !Y || !N || (cfg->gate != FOCUS_GATE_NONE && !gate)))
+        return FOCUS_ERR_NULL;
+    if (!all_aligned({X, B, w_post, b_post_opt, gate, w_pre, b_pre_opt, Y, N, stats_opt})) return FOCUS_ERR_SHAPE;
+    FOCUS_TRY(check_ws(ws, ws_bytes, kWsHeader));
+    if (T == 0 || C == 0) return FOCUS_OK;
+    const bool token = cfg->gate == FOCUS_GATE_TOKEN;
+    const int64_t rows = T * C * (dtype == FOCUS_BF16 ? 2 : 4), row = C * (w_dtype == FOCUS_BF16 ? 2 : 4);
+    const Span stats{stats_opt, T * (cfg->kind == FOCUS_NORM_LAYER ? 4 : 2) * (int64_t)sizeof(float)};
+    if (clash({{Y, rows}, {N, rows}, stats}, {{X, rows}, {B, rows}, {token ? gate : nullptr, rows}}, true) ||
+        clash({{Y, rows}, {N, rows}, stats},
+              {{w_post, row}, {b_post_opt, row}, {token ? nullptr : gate, row}, {w_pre, row}, {b_pre_opt, row}}, false) ||
+        clash({stats}, {{X, rows}, {B, rows}, {gate, token ? rows : row}}, false))
+        return FOCUS_ERR_SHAPE;
+    SandwichArgs a{};
+    a.X = X, a.B = B, a.gate = gate, a.w1 = w_post, a.b1 = b_post_opt, a.w2 = w_pre, a.b2 = b_pre_opt, a.Y = Y, a.N = N;
+    a.stats = stats_opt, a.T = T, a.C = (int)C, a.w_dtype = w_dtype, a.layer = cfg->kind == FOCUS_NORM_LAYER;
+    a.gate_kind = cfg->gate, a.eps = cfg->eps, a.scale = cfg->residual_scale;
+    return hip_status(launch_sandwich_fwd(dtype, a, (hipStream_t)stream));
+}
+
+focus_status focus_sandwich_norm_bwd(const focus_sandwich_config *cfg, const void *dN, const void *dY_opt, const void *X,
+                                     const void *B, int dtype, int64_t T, int64_t C, const void *w_post,
+                                     const void *b_post_opt, const void *gate, const void *w_pre, int w_dtype,
+                                     const float *stats, void *dX, void *dB, void *dgate_opt, float *dw_post,
+                                     float *db_post_opt, float *dw_pre, float *db_pre_opt, void *ws, size_t ws_bytes,
+                                     focus_stream stream) {
+    FOCUS_TRY(check_sandwich(cfg, dtype, w_dtype, T, C, gate));
+    if (cfg->gate == FOCUS_GATE_NONE && dgate_opt) return FOCUS_ERR_CONFIG;
+    if (C > 0 && (!dw_post || !dw_pre)) return FOCUS_ERR_NULL;
+    if (T > 0 && C > 0 &&
+        (!dN || !X || !B || !w_post || !w_pre || !stats || !dX || !dB || (cfg->gate != FOCUS_GATE_NONE && !gate)))
+        return FOCUS_ERR_NULL;
+    if (!all_aligned({dN, dY_opt, X, B, w_post, b_post_opt, gate, w_pre, stats, dX, dB, dgate_opt, dw_post, db_post_opt, dw_pre,
+                      db_pre_opt}))
+        return FOCUS_ERR_SHAPE;
+    FOCUS_TRY(check_ws(ws, ws_bytes, sandwich_bwd_ws(T, C)));
+    if (C == 0) return FOCUS_OK;
+    const hipStream_t st = (hipStream_t)stream;
+    const bool token = cfg->gate == FOCUS_GATE_TOKEN;
+    const int64_t rows = T * C * (dtype == FOCUS_BF16 ? 2 : 4), row = C * (w_dtype == FOCUS_BF16 ? 2 : 4), sums = C * 4;
+    const Span dgate_t{token ? dgate_opt : nullptr, rows}, dgate_f{token ? nullptr : dgate_opt, sums};
+    const Span given{stats, T * (cfg->kind == FOCUS_NORM_LAYER ? 4 : 2) * (int64_t)sizeof(float)};
+    if (clash({{dX, rows}, {dB, rows}, dgate_t, dgate_f, {dw_post, sums}, {db_post_opt, sums}, {dw_pre, sums}, {db_pre_opt, sums}},
+              {{w_post, row}, {b_post_opt, row}, {token ? nullptr : gate, row}, {w_pre, row}, given}, false) ||
+        clash({{dX, rows}, {dB, rows}, dgate_t},
+              {{dN, rows}, {dY_opt, rows}, {X, rows}, {B, rows}, {token ? gate : nullptr, rows}}, true) ||
+        clash({dgate_f, {dw_post, sums}, {db_post_opt, sums}, {dw_pre, sums}, {db_pre_opt, sums}},
+              {{dN, rows}, {dY_opt, rows}, {X, rows}, {B, rows}, {token ? gate : nullptr, rows}}, false))
+        return FOCUS_ERR_SHAPE;
+    if (T == 0) {  // empty sums
+        for (void *p : {(void *)dw_post, (void *)db_post_opt, (void *)dw_pre, (void *)db_pre_opt, token ? nullptr : dgate_opt}) {
+            if (!p) continue;
+            const hipError_t e = launch_zero_fill(p, (size_t)sums, st);
+            if (e != hipSuccess) return hip_status(e);
+        }
+        return FOCUS_OK;
+    }
+    SandwichArgs a{};
+    a.X = X, a.B = B, a.gate = gate, a.w1 = w_post, a.b1 = b_post_opt, a.w2 = w_pre, a.stats = const_cast<float *>(stats);
+    a.dN = dN, a.dY = dY_opt, a.dX = dX, a.dB = dB, a.dgate = dgate_opt;
+    a.dw1 = dw_post, a.db1 = db_post_opt, a.dw2 = dw_pre, a.db2 = db_pre_opt;
+    a.T = T, a.C = (int)C, a.w_dtype = w_dtype, a.layer = cfg->kind == FOCUS_NORM_LAYER;
+    a.gate_kind = cfg->gate, a.eps = cfg->eps, a.scale = cfg->residual_scale;
+    return hip_status(launch_sandwich_bwd(dtype, a, ws, st));
+}
+
+focus_status focus_linear_ce_fwd(const void *X, const void *W, int dtype, int64_t T, int64_t V, int64_t K,
+                                 const int64_t *target_opt, float *logp_opt, float *lse, void *ws, size_t ws_bytes,
+                                 focus_stream stream) {
+    if (!dtype_ok(dtype)) return FOCUS_ERR_DTYPE;
+    FOCUS_TRY(check_linear_ce(T, V, K));
+    if (T > 0 && (!X || !W || !lse || (logp_opt && !target_opt))) return FOCUS_ERR_NULL;
+    if (!all_aligned({X, W}) || !aligned_to({logp_opt, lse}, 4) || !aligned_to({target_opt}, 8)) return FOCUS_ERR_SHAPE;
+    FOCUS_TRY(check_ws(ws, ws_bytes, linear_ce_fwd_ws(T, V)));
+    if (T == 0) return FOCUS_OK;
+    return hip_status(launch_linear_ce_fwd(dtype, X, W, T, V, K, target_opt, logp_opt, lse, flag_of(ws), ws, (hipStream_t)stream));
+}
+
+focus_status focus_linear_ce_bwd(const void *X, const void *W, int dtype, int64_t T, int64_t V, int64_t K,
+                                 const int64_t *target_opt, const float *lse, const float *d_logp_opt,
+                                 const float *d_lse_opt, void *dX_opt, void *dW_opt, int dw_dtype, void *ws,
+                                 size_t ws_bytes, focus_stream stream) {
+    if (!dtype_ok(dtype) || !dtype_ok(dw_dtype) || (dtype == FOCUS_F32 && dw_dtype != FOCUS_F32)) return FOCUS_ERR_DTYPE;
+    FOCUS_TRY(check_linear_ce(T, V, K));
+    if (T > 0 && (!X || !W || !lse || (!dX_opt && !dW_opt) || (!d_logp_opt && !d_lse_opt) || (d_logp_opt && !target_opt)))
+        return FOCUS_ERR_NULL;
+    if (!all_aligned({X, W, dX_opt, dW_opt}) || !aligned_to({lse, d_logp_opt, d_lse_opt}, 4) || !aligned_to({target_opt}, 8))
+        return FOCUS_ERR_SHAPE;
+    const int64_t e = dtype == FOCUS_BF16 ? 2 : 4, de = dw_dtype == FOCUS_BF16 ? 2 : 4;
+    if (clash({{dX_opt, T * K * e}, {dW_opt, V * K * de}},
+              {{X, T * K * e}, {W, V * K * e}, {target_opt, T * 8}, {lse, T * 4}, {d_logp_opt, T * 4}, {d_lse_opt, T * 4}}, false))
+        return FOCUS_ERR_SHAPE;
+    FOCUS_TRY(check_ws(ws, ws_bytes, linear_ce_bwd_ws(T, V, K)));
+    const hipStream_t st = (hipStream_t)stream;
+    if (T == 0) return dW_opt ? hip_status(launch_zero_fill(dW_opt, (size_t)(V * K * de), st)) : FOCUS_OK;  // an empty sum
+    return hip_status(launch_linear_ce_bwd(dtype, X, W, T, V, K, target_opt, lse, d_logp_opt, d_lse_opt, dX_opt, dW_opt, dw_dtype,
+                                           flag_of(ws), ws, st));
+}
+
+focus_status focus_clip_grad_norm(const focus_grad_tensor *tensors, int64_t n_tensors, double max_norm, double *norm_out,
+                                  void *ws, size_t ws_bytes, focus_stream stream) {
+    if (!(max_norm > 0.0)) return FOCUS_ERR_CONFIG;
+    if (n_tensors < 0 || n_tensors > kMaxGradTensors) return FOCUS_ERR_SHAPE;
+    if (!norm_out || (n_tensors > 0 && !tensors)) return FOCUS_ERR_NULL;
+    if (!aligned_to({norm_out}, 8)) return FOCUS_ERR_SHAPE;
+    for (int64_t i = 0; i < n_tensors; i++) {
+        const focus_grad_tensor &t = tensors[i];
+        if (!dtype_ok(t.dtype)) return FOCUS_ERR_DTYPE;
+        if (t.reserved != 0) return FOCUS_ERR_CONFIG;
+        if (t.n < 0 || t.n > kMaxGradElems || !all_aligned({t.grad, t.out})) return FOCUS_ERR_SHAPE;
+        if (t.n > 0 && !t.grad) return FOCUS_ERR_NULL;
+    }
+    constexpr int kOnStack = 1024;
+    int32_t few[kOnStack];
+    int32_t *const order = n_tensors <= kOnStack ? few : new (std::nothrow) int32_t[n_tensors];
+    if (!order) return FOCUS_ERR_HIP;
+    const focus_status places = check_grad_places(tensors, n_tensors, order);
+    if (order != few) delete[] order;
+    FOCUS_TRY(places);
+    FOCUS_TRY(check_ws(ws, ws_bytes, clip_grad_norm_ws(n_tensors)));
+    return hip_status(launch_clip_grad_norm(reinterpret_cast<const GradTensor *>(tensors), n_tensors, max_norm, norm_out,
+                                            flag_of(ws), ws, (hipStream_t)stream));
 }
 
 focus_status focus_check_flags(void *ws, focus_stream stream) {

@@ -1,0 +1,177 @@
+// The norm over all gradients of a step and the gradients scaled by it: norm = sqrt(sum g^2) over every element of every tensor,
+// out = g min(1, max_norm / norm).
+//
+// HBM-bound: every gradient is read once for the norm and once more to be scaled. Squares are summed in fp64, so that neither
+// the size of a gradient (1e-30 or 1e30) nor their number costs digits. Up to kGroup tensors travel in the arguments of a launch; a
+// group's elements are numbered in chunks of one tensor each, which the workgroups take in turn.
+#include "internal.h"
+#include "ops_device.h"
+
+namespace focus {
+
+namespace {
+
+constexpr int kGroup = 112;             // tensors of a launch: 28 bytes each of the 4 KB that a kernel's arguments have
+constexpr int kChunk = 8192;            // elements
+constexpr int kNormParts = 2048;        // workgroups of a launch at most, each with one partial sum
+
+struct GradGroup {
+    const void *g[kGroup];
+    void *out[kGroup];
+    int64_t n[kGroup];
+    uint32_t first[kGroup];             // first chunk of each tensor
+    uint32_t bf16[(kGroup + 31) / 32];  // a bit per tensor
+    uint32_t chunks;
+    int count;
+};
+static_assert(sizeof(GradGroup) <= 3968, "the group and a kernel's other arguments fit 4 KB");
+
+// The tensor of a chunk: the last one whose first chunk is not behind it
+__device__ __forceinline__ int tensor_of(const GradGroup &a, uint32_t chunk) {
+    int lo = 0, hi = a.count;
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) / 2;
+        if (a.first[mid] <= chunk) lo = mid;
+        else hi = mid;
+    }
+    return lo;
+}
+
+// f(piece start, elements of it) for the 8-element pieces of a chunk that this thread takes
+template <typename F>
+__device__ __forceinline__ void pieces(int64_t start, int64_t n, F &&f) {
+#pragma unroll
+    for (int j = 0; j < kChunk / 2048; j++) {
+        const int64_t c = start + (j * 256 + (int)threadIdx.x) * 8;
+        f(c, (int)(n - c < 8 ? n - c : 8));
+    }
+}
+
+template <typename T>
+__device__ __forceinline__ double chunk_squares(const T *g, int64_t start, int64_t n) {
+    Raw8<T> v[kChunk / 2048];
+    int j = 0;
+    pieces(start, n, [&](int64_t c, int m) { v[j++].load(g + c, m); });
+    double s = 0.0;
+#pragma unroll
+    for (int i = 0; i < kChunk / 2048; i++)
+#pragma unroll
+        for (int e = 0; e < 8; e++) {
+            const double x = (double)v[i][e];
+            s = __builtin_fma(x, x, s);
+        }
+    return s;
+}
+
+__global__ void __launch_bounds__(256) grad_norm_kernel(GradGroup a, double *__restrict__ part) {
+    __shared__ double lds[4];
+    double s = 0.0;
+    for (uint32_t c = blockIdx.x; c < a.chunks; c += gridDim.x) {
+        const int i = tensor_of(a, c);
+        const int64_t start = (int64_t)(c - a.first[i]) * kChunk;
+        if (a.bf16[i / 32] >> (i % 32) & 1u) s += chunk_squares(static_cast<const uint16_t *>(a.g[i]), start, a.n[i]);
+        else s += chunk_squares(static_cast<const float *>(a.g[i]), start, a.n[i]);
+    }
+    for (int m = 32; m >= 1; m >>= 1) s += __shfl_xor(s, m, 64);
+    if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = s;
+    __syncthreads();
+    if (threadIdx.x == 0) part[blockIdx.x] = lds[0] + lds[1] + lds[2] + lds[3];
+}
+
+// norm and factor from the partial sums, in a fixed order
+__global__ void __launch_bounds__(1024) grad_finish_kernel(const double *__restrict__ part, int64_t parts, double max_norm,
+                                                           double *__restrict__ norm, float *__restrict__ factor, uint32_t *flag) {
+    __shared__ double lds[1024];
+    double s = 0.0;
+    for (int64_t i = threadIdx.x; i < parts; i += 1024) s += part[i];
+    lds[threadIdx.x] = s;
+    __syncthreads();
+    for (int w = 512; w >= 1; w >>= 1) {
+        if ((int)threadIdx.x < w) lds[threadIdx.x] += lds[threadIdx.x + w];
+        __syncthreads();
+    }
+    if (threadIdx.x) return;
+    const double x = sqrt(lds[0]);
+    *norm = x;
+    const bool fine = x < (double)__builtin_inff();  // false for a NaN
+    *factor = fine && x > max_norm ? (float)(max_norm / x) : 1.0f;
+    if (!fine) raise_domain_flag(flag);
+}
+
+template <typename T>
+__device__ __forceinline__ void chunk_scale(const T *g, T *out, int64_t start, int64_t n, float f) {
+    Raw8<T> v[kChunk / 2048];
+    int j = 0;
+    pieces(start, n, [&](int64_t c, int m) { v[j++].load(g + c, m); });
+    j = 0;
+    pieces(start, n, [&](int64_t c, int m) {
+        float x[8];
+#pragma unroll
+        for (int e = 0; e < 8; e++) x[e] = v[j][e] * f;
+        j++;
+        store8_n(out + c, m, x);
+    });
+}
+
+__global__ void __launch_bounds__(256) grad_scale_kernel(GradGroup a, const float *__restrict__ factor) {
+    const float f = *factor;
+    for (uint32_t c = blockIdx.x; c < a.chunks; c += gridDim.x) {
+        const int i = tensor_of(a, c);
+        if (!a.out[i] || (f == 1.0f && a.out[i] == a.g[i])) continue;  // nothing to write
+        const int64_t start = (int64_t)(c - a.first[i]) * kChunk;
+        if (a.bf16[i / 32] >> (i % 32) & 1u)
+            chunk_scale(static_cast<const uint16_t *>(a.g[i]), static_cast<uint16_t *>(a.out[i]), start, a.n[i], f);
+        else
+            chunk_scale(static_cast<const float *>(a.g[i]), static_cast<float *>(a.out[i]), start, a.n[i], f);
+    }
+}
+
+// The group of the tensors from `first` on (empty ones are left out); the index behind its last
+int64_t next_group(const GradTensor *t, int64_t first, int64_t count, GradGroup &a) {
+    a.count = 0, a.chunks = 0;
+    for (uint32_t &b : a.bf16) b = 0;
+    int64_t i = first;
+    for (; i < count && a.count < kGroup; i++) {
+        if (t[i].n == 0) continue;
+        const int k = a.count++;
+        a.g[k] = t[i].grad, a.out[k] = t[i].out, a.n[k] = t[i].n, a.first[k] = a.chunks;
+        if (t[i].dtype == kBF16) a.bf16[k / 32] |= 1u << (k % 32);
+        a.chunks += (uint32_t)((t[i].n + kChunk - 1) / kChunk);
+    }
+    return i;
+}
+
+}  // namespace
+
+static_assert(kMaxGradElems / kChunk * kGroup < (int64_t(1) << 32), "chunk numbers of a group are 32-bit");
+
+size_t clip_grad_norm_ws(int64_t tensors) {
+    return 2 * kWsHeader + (size_t)((tensors + kGroup - 1) / kGroup) * kNormParts * sizeof(double);
+}
+
+hipError_t launch_clip_grad_norm(const GradTensor *t, int64_t count, double max_norm, double *norm, uint32_t *flag, void *ws,
+                                 hipStream_t st) {
+    float *const factor = reinterpret_cast<float *>(static_cast<char *>(ws) + kWsHeader);
+    double *const part = reinterpret_cast<double *>(static_cast<char *>(ws) + 2 * kWsHeader);
+    int64_t parts = 0;
+    bool scales = false;
+    GradGroup a;
+    for (int64_t i = 0; i < count;) {
+        i = next_group(t, i, count, a);
+        if (!a.count) continue;
+        for (int k = 0; k < a.count; k++) scales = scales || a.out[k];
+        const unsigned grid = std::min<uint32_t>(a.chunks, kNormParts);
+        grad_norm_kernel<<<grid, 256, 0, st>>>(a, part + parts);
+        parts += grid;
+    }
+    grad_finish_kernel<<<1, 1024, 0, st>>>(part, parts, max_norm, norm, factor, flag);
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess || !scales) return e;
+    for (int64_t i = 0; i < count;) {
+        i = next_group(t, i, count, a);
+        if (a.count) grad_scale_kernel<<<std::min<uint32_t>(a.chunks, kNormParts), 256, 0, st>>>(a, factor);
+    }
+    return hipGetLastError();
+}
+
+}  // namespace focus

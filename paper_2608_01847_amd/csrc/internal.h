@@ -145,4 +145,43 @@ hipError_t launch_logprobs_bwd(int dtype, const void *Z, int64_t T, int64_t V, c
                                const float *entropy, const float *d_logp, const float *d_entropy, void *dZ, uint32_t *flag,
                                hipStream_t st);
 
+// A call of the norms after and before a block (tensors [T][C], parameters [C])
+constexpr int kGateNone = 0, kGateFeature = 1, kGateToken = 2;
+struct SandwichArgs {
+    const void *X, *B, *gate;               // gate: none, [C] (the parameters' type) or [T][C]
+    const void *w1, *b1, *w2, *b2;          // gain and shift (NULL: none) after (1) and before (2) a block
+    void *Y, *N;
+    float *stats;                           // rstd1, rstd2, mean1, mean2 [T] each, the means for layer norms only
+    const void *dN, *dY;                    // dY may be NULL
+    void *dX, *dB, *dgate;                  // dgate: [C] fp32 or [T][C]
+    float *dw1, *db1, *dw2, *db2;
+    float *part;                            // [sums][workgroups][C]
+    int64_t T, rows, first;                 // rows of a workgroup; first row of a launch
+    int C, w_dtype, layer, gate_kind, sums;
+    float eps, scale;
+};
+size_t sandwich_bwd_ws(int64_t T, int64_t C);
+hipError_t launch_sandwich_fwd(int dtype, SandwichArgs a, hipStream_t st);
+hipError_t launch_sandwich_bwd(int dtype, SandwichArgs a, void *ws, hipStream_t st);
+
+size_t linear_ce_fwd_ws(int64_t T, int64_t V);
+size_t linear_ce_bwd_ws(int64_t T, int64_t V, int64_t K);
+hipError_t launch_linear_ce_fwd(int dtype, const void *X, const void *W, int64_t T, int64_t V, int64_t K, const int64_t *target,
+                                float *logp, float *lse, uint32_t *flag, void *ws, hipStream_t st);
+hipError_t launch_linear_ce_bwd(int dtype, const void *X, const void *W, int64_t T, int64_t V, int64_t K, const int64_t *target,
+                                const float *lse, const float *g, const float *h, void *dX, void *dW, int dw_dtype,
+                                uint32_t *flag, void *ws, hipStream_t st);
+
+struct GradTensor {
+    const void *grad;
+    void *out;  // NULL: counted in the norm only
+    int64_t n;
+    int32_t dtype;
+    int32_t reserved;
+};
+constexpr int64_t kMaxGradElems = int64_t(1) << 36;  // of one tensor
+size_t clip_grad_norm_ws(int64_t tensors);
+hipError_t launch_clip_grad_norm(const GradTensor *t, int64_t count, double max_norm, double *norm, uint32_t *flag, void *ws,
+                                 hipStream_t st);
+
 }  // namespace focus

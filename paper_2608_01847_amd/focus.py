@@ -20,8 +20,10 @@ CALL_RECON_GEMM_FWD, CALL_RECON_GEMM_BWD, CALL_EXPORT_PACKED, CALL_ADAMW = 3, 4,
 CALL_RECON_GEMM_DX, CALL_FAKEQUANT_ACT_BWD, CALL_KL_TOP, CALL_FAKEQUANT_WEIGHTS = 7, 8, 9, 10
 CALL_NORM_FWD, CALL_NORM_BWD, CALL_ATTENTION_FWD, CALL_ATTENTION_BWD = 11, 12, 13, 14
 CALL_TOKEN_LOGPROBS, CALL_TOKEN_LOGPROBS_BWD, CALL_ATTENTION_FWD_F32, CALL_ATTENTION_BWD_F32 = 15, 16, 17, 18
+CALL_SANDWICH_NORM_FWD, CALL_SANDWICH_NORM_BWD, CALL_LINEAR_CE_FWD, CALL_LINEAR_CE_BWD, CALL_CLIP_GRAD_NORM = 19, 20, 21, 22, 23
 MAX_WEIGHT_LAYERS = 16
 NORM_LAYER, NORM_RMS = 0, 1
+GATE_NONE, GATE_FEATURE, GATE_TOKEN = 0, 1, 2
 MAX_TOP = 64
 
 OK, ERR_NULL, ERR_SHAPE, ERR_DTYPE, ERR_CONFIG, ERR_WORKSPACE, ERR_DOMAIN, ERR_HIP, ERR_SCRATCH = range(9)
@@ -32,7 +34,8 @@ EXPORTED = ("focus_workspace_size", "focus_scales_init", "focus_fakequant_fwd", 
             "focus_recon_gemm_bwd_mxfp4", "focus_export_packed", "focus_fakequant_weights", "focus_recon_gemm_dx",
             "focus_fakequant_act_bwd", "focus_kl_top", "focus_adamw_step", "focus_norm_fwd", "focus_norm_bwd",
             "focus_attention_workspace_size", "focus_attention_fwd", "focus_attention_bwd", "focus_token_logprobs",
-            "focus_token_logprobs_bwd", "focus_check_flags", "focus_status_string")
+            "focus_token_logprobs_bwd", "focus_sandwich_norm_fwd", "focus_sandwich_norm_bwd", "focus_linear_ce_fwd",
+            "focus_linear_ce_bwd", "focus_clip_grad_norm", "focus_check_flags", "focus_status_string")
 
 
 class QConfig(ctypes.Structure):
@@ -57,6 +60,15 @@ class AttentionConfig(ctypes.Structure):
                 ("causal", ctypes.c_int32), ("scale", ctypes.c_float), ("reserved", ctypes.c_int32),
                 ("q_stride", ctypes.c_int64), ("k_stride", ctypes.c_int64), ("v_stride", ctypes.c_int64),
                 ("dq_stride", ctypes.c_int64), ("dk_stride", ctypes.c_int64), ("dv_stride", ctypes.c_int64)]
+
+
+class SandwichConfig(ctypes.Structure):
+    _fields_ = [("kind", ctypes.c_int32), ("gate", ctypes.c_int32), ("eps", ctypes.c_float), ("residual_scale", ctypes.c_float)]
+
+
+class GradTensor(ctypes.Structure):
+    _fields_ = [("grad", ctypes.c_void_p), ("out", ctypes.c_void_p), ("n", ctypes.c_int64), ("dtype", ctypes.c_int32),
+                ("reserved", ctypes.c_int32)]
 
 
 class FocusError(RuntimeError):
@@ -102,6 +114,12 @@ def lib() -> ctypes.CDLL:
         L.focus_attention_bwd.argtypes = [attn, p, p, p, p, p, p, i32, i64, i64, p, p, i64, p, p, p, p, sz, p]
         L.focus_token_logprobs.argtypes = [p, i32, i64, i64, p, i32, p, p, p, p, p, p, sz, p]
         L.focus_token_logprobs_bwd.argtypes = [p, i32, i64, i64, p, p, p, p, p, p, p, sz, p]
+        sandwich, f64 = ctypes.POINTER(SandwichConfig), ctypes.c_double
+        L.focus_sandwich_norm_fwd.argtypes = [sandwich, p, p, i32, i64, i64, p, p, p, p, p, i32, p, p, p, p, sz, p]
+        L.focus_sandwich_norm_bwd.argtypes = [sandwich, p, p, p, p, i32, i64, i64, p, p, p, p, i32, p, p, p, p, p, p, p, p, p, sz, p]
+        L.focus_linear_ce_fwd.argtypes = [p, p, i32, i64, i64, i64, p, p, p, p, sz, p]
+        L.focus_linear_ce_bwd.argtypes = [p, p, i32, i64, i64, i64, p, p, p, p, p, p, i32, p, sz, p]
+        L.focus_clip_grad_norm.argtypes = [ctypes.POINTER(GradTensor), i64, f64, p, p, sz, p]
         L.focus_check_flags.argtypes = [p, p]
         L.focus_status_string.argtypes = [i32]
         L.focus_status_string.restype = ctypes.c_char_p
@@ -110,7 +128,8 @@ def lib() -> ctypes.CDLL:
                      "focus_recon_gemm_bwd_mxfp4",
                      "focus_export_packed", "focus_fakequant_weights", "focus_adamw_step", "focus_check_flags", "focus_recon_gemm_dx", "focus_fakequant_act_bwd",
                      "focus_kl_top", "focus_norm_fwd", "focus_norm_bwd", "focus_attention_fwd", "focus_attention_bwd",
-                     "focus_token_logprobs", "focus_token_logprobs_bwd"):
+                     "focus_token_logprobs", "focus_token_logprobs_bwd", "focus_sandwich_norm_fwd", "focus_sandwich_norm_bwd",
+                     "focus_linear_ce_fwd", "focus_linear_ce_bwd", "focus_clip_grad_norm"):
             getattr(L, name).restype = ctypes.c_int
         _LIB = L
     return _LIB
@@ -669,6 +688,172 @@ def token_logprobs_bwd(Z: torch.Tensor, target, lse: torch.Tensor, entropy=None,
                                           _ptr(d_entropy), _ptr(dZ), _ptr(ws), ws.numel(), _stream()),
            "focus_token_logprobs_bwd")
     return dZ
+
+
+def sandwich_norm_workspace_size(T: int, C: int) -> int:
+    """Workspace bytes of sandwich_norm_fwd and sandwich_norm_bwd on T tokens of C features."""
+    return int(lib().focus_workspace_size(CALL_SANDWICH_NORM_BWD, None, T, 0, C))
+
+
+def _sandwich_config(where: str, X, w_post, w_pre, b_post, b_pre, gate, residual_scale, kind, eps) -> SandwichConfig:
+    T, C = X.shape
+    for t in (w_post, w_pre, b_post, b_pre):
+        if t is not None and (t.shape != (C,) or t.dtype != w_post.dtype):
+            raise ValueError(f"{where}: gains and shifts are [C] of one dtype")
+    g = GATE_NONE
+    if gate is not None:
+        g = GATE_FEATURE if gate.dim() == 1 else GATE_TOKEN
+        if gate.shape != ((C,) if g == GATE_FEATURE else X.shape) or gate.dtype != (w_post if g == GATE_FEATURE else X).dtype:
+            raise ValueError(f"{where}: the gate is [C] in the gains' dtype or [T][C] in X's")
+    return SandwichConfig(kind, g, eps, residual_scale)
+
+
+def sandwich_norm_fwd(X: torch.Tensor, B: torch.Tensor, w_post: torch.Tensor, w_pre: torch.Tensor, b_post=None, b_pre=None,
+                      gate=None, residual_scale: float = 1.0, kind: int = NORM_LAYER, eps: float = 1e-5,
+                      want_stats: bool = True, ws=None, out=None, n_out=None):
+    """Norms after and before a block: Y = residual_scale X + gate (norm(B) w_post + b_post), N = norm(Y) w_pre + b_pre over the
+    last dimension of X, B [T][C] -> (Y, N, stats or None). gate: None, [C] or [T][C]. `out` / `n_out`: preallocated Y / N, which
+    may be X, B or a gate [T][C]. stats (fp32, [2][T], layer norms [4][T]) is what the backward needs."""
+    T, C = X.shape
+    for t in (B, out, n_out):
+        if t is not None and (t.shape != X.shape or t.dtype != X.dtype):
+            raise ValueError("sandwich_norm_fwd: B, out and n_out have X's shape and dtype")
+    cfg = _sandwich_config("sandwich_norm_fwd", X, w_post, w_pre, b_post, b_pre, gate, residual_scale, kind, eps)
+    _one_gpu("sandwich_norm_fwd", X, B, w_post, w_pre, b_post, b_pre, gate, ws, out, n_out)
+    Y = out if out is not None else torch.empty_like(X)
+    N = n_out if n_out is not None else torch.empty_like(X)
+    stats = torch.empty(4 if kind == NORM_LAYER else 2, T, dtype=torch.float32, device=X.device) if want_stats else None
+    ws = _sized(ws, 256, X.device)
+    _check(lib().focus_sandwich_norm_fwd(ctypes.byref(cfg), _ptr(X), _ptr(B), _dt(X), T, C, _ptr(w_post), _ptr(b_post), _ptr(gate),
+                                         _ptr(w_pre), _ptr(b_pre), _dt(w_post), _ptr(Y), _ptr(N), _ptr(stats), _ptr(ws),
+                                         ws.numel(), _stream()), "focus_sandwich_norm_fwd")
+    return Y, N, stats
+
+
+def sandwich_norm_bwd(dN: torch.Tensor, dY, X: torch.Tensor, B: torch.Tensor, w_post: torch.Tensor, w_pre: torch.Tensor,
+                      stats: torch.Tensor, b_post=None, b_pre=None, gate=None, residual_scale: float = 1.0,
+                      kind: int = NORM_LAYER, eps: float = 1e-5, ws=None, out=None, b_out=None, gate_out=None):
+    """Backward of sandwich_norm_fwd on its inputs; dY (or None) is the gradient that reaches Y past the second norm
+    -> (dX, dB, {"w_post", "w_pre", "b_post", "b_pre", "gate": their gradients}): fp32 [C], None where there is no such
+    parameter, a gate [T][C]'s in X's dtype. `out` / `b_out` / `gate_out`: preallocated dX / dB / a gate [T][C]'s gradient, each of
+    which may be any one of the tensors [T][C] that the call reads."""
+    T, C = X.shape
+    for t in (dN, dY, B, out, b_out, gate_out):
+        if t is not None and (t.shape != X.shape or t.dtype != X.dtype):
+            raise ValueError("sandwich_norm_bwd: dN, dY, B, out, b_out and gate_out have X's shape and dtype")
+    cfg = _sandwich_config("sandwich_norm_bwd", X, w_post, w_pre, b_post, b_pre, gate, residual_scale, kind, eps)
+    if stats.shape != (4 if kind == NORM_LAYER else 2, T) or stats.dtype != torch.float32:
+        raise ValueError("sandwich_norm_bwd: stats are the forward's")
+    if gate_out is not None and cfg.gate != GATE_TOKEN:
+        raise ValueError("sandwich_norm_bwd: gate_out without a gate [T][C]")
+    _one_gpu("sandwich_norm_bwd", X, dN, dY, B, w_post, w_pre, stats, b_post, b_pre, gate, ws, out, b_out, gate_out)
+    dX = out if out is not None else torch.empty_like(X)
+    dB = b_out if b_out is not None else torch.empty_like(X)
+    per_feature = lambda t: torch.empty(C, dtype=torch.float32, device=X.device) if t is not None else None
+    grads = {"w_post": per_feature(w_post), "w_pre": per_feature(w_pre), "b_post": per_feature(b_post), "b_pre": per_feature(b_pre),
+             "gate": per_feature(gate) if cfg.gate != GATE_TOKEN else gate_out if gate_out is not None else torch.empty_like(X)}
+    ws = _sized(ws, sandwich_norm_workspace_size(T, C), X.device)
+    _check(lib().focus_sandwich_norm_bwd(ctypes.byref(cfg), _ptr(dN), _ptr(dY), _ptr(X), _ptr(B), _dt(X), T, C, _ptr(w_post),
+                                         _ptr(b_post), _ptr(gate), _ptr(w_pre), _dt(w_post), _ptr(stats), _ptr(dX), _ptr(dB),
+                                         _ptr(grads["gate"]), _ptr(grads["w_post"]), _ptr(grads["b_post"]),
+                                         _ptr(grads["w_pre"]), _ptr(grads["b_pre"]), _ptr(ws), ws.numel(), _stream()),
+           "focus_sandwich_norm_bwd")
+    return dX, dB, grads
+
+
+def linear_ce_workspace_size(T: int, V: int, K: int, backward: bool = True) -> int:
+    """Workspace bytes of linear_ce_fwd (and with `backward` of linear_ce_bwd too) on T or fewer tokens."""
+    calls = (CALL_LINEAR_CE_FWD, CALL_LINEAR_CE_BWD) if backward else (CALL_LINEAR_CE_FWD,)
+    return max(int(lib().focus_workspace_size(c, None, T, V, K)) for c in calls)
+
+
+def _linear_ce_inputs(where: str, X, W, target):
+    if X.dim() != 2 or W.dim() != 2 or X.shape[1] != W.shape[1] or X.dtype != W.dtype:
+        raise ValueError(f"{where}: X [T][K] and W [V][K] of one dtype expected")
+    return X.shape[0], W.shape[0], X.shape[1], _targets(target, X.shape[0])
+
+
+def linear_ce_fwd(X: torch.Tensor, W: torch.Tensor, target=None, ws=None):
+    """Log probabilities of the tokens `target` (int64 [T]; below zero: left out, 0) under the logits X W^T of hidden states
+    X [T][K] and an output layer W [V][K], without the logits -> (logp [T] or None, lse [T]), fp32. The mean cross entropy of n
+    tokens is -logp.sum() / n."""
+    T, V, K, pt = _linear_ce_inputs("linear_ce_fwd", X, W, target)
+    _one_gpu("linear_ce_fwd", X, W, target, ws)
+    logp = torch.empty(T, dtype=torch.float32, device=X.device) if target is not None else None
+    lse = torch.empty(T, dtype=torch.float32, device=X.device)
+    ws = _sized(ws, linear_ce_workspace_size(T, V, K, backward=False), X.device)
+    _check(lib().focus_linear_ce_fwd(_ptr(X), _ptr(W), _dt(X), T, V, K, pt, _ptr(logp), _ptr(lse), _ptr(ws), ws.numel(),
+                                     _stream()), "focus_linear_ce_fwd")
+    return logp, lse
+
+
+def linear_ce_bwd(X: torch.Tensor, W: torch.Tensor, target, lse: torch.Tensor, d_logp=None, d_lse=None, want_dx: bool = True,
+                  want_dw: bool = True, dw_dtype=None, ws=None, out=None, dw_out=None):
+    """Gradients of linear_ce_fwd's logp and lse (fp32 [T] each; the mean cross entropy of n tokens: d_logp = -1 / n)
+    -> (dX in X's dtype or None, dW in dw_dtype or None). dw_dtype defaults to W's; bf16 operands may have a float32 dW, the G
+    of fakequant_bwd. `out` / `dw_out`: preallocated dX / dW."""
+    T, V, K, pt = _linear_ce_inputs("linear_ce_bwd", X, W, target)
+    for t in (lse, d_logp, d_lse):
+        if t is not None and (t.shape != (T,) or t.dtype != torch.float32):
+            raise ValueError("linear_ce_bwd: lse, d_logp and d_lse are float32 [T]")
+    if out is not None and (out.shape != X.shape or out.dtype != X.dtype):
+        raise ValueError("linear_ce_bwd: out has X's shape and dtype")
+    if dw_out is not None and (dw_out.shape != W.shape or dw_out.dtype != (dw_dtype or dw_out.dtype)):
+        raise ValueError("linear_ce_bwd: dw_out has W's shape, and dw_dtype")
+    _one_gpu("linear_ce_bwd", X, W, target, lse, d_logp, d_lse, ws, out, dw_out)
+    dX = out if out is not None else torch.empty_like(X) if want_dx else None
+    dW = dw_out
+    if dW is None and want_dw:
+        dW = torch.empty(V, K, dtype=dw_dtype or W.dtype, device=X.device)
+    ws = _sized(ws, linear_ce_workspace_size(T, V, K), X.device)
+    _check(lib().focus_linear_ce_bwd(_ptr(X), _ptr(W), _dt(X), T, V, K, pt, _ptr(lse), _ptr(d_logp), _ptr(d_lse), _ptr(dX),
+                                     _ptr(dW), _dt(dW) if dW is not None else F32, _ptr(ws), ws.numel(), _stream()),
+           "focus_linear_ce_bwd")
+    return dX, dW
+
+
+class GradTensors:
+    """The gradients of a step for clip_grad_norm, set up once for tensors that stay where they are: `grads` are float32 or
+    bfloat16 tensors, `out` their scaled gradients (None: in place; a list may hold None for those that are only counted)."""
+
+    def __init__(self, grads, out=None):
+        self.grads = list(grads)
+        self.out = self.grads if out is None else list(out)
+        if len(self.out) != len(self.grads):
+            raise ValueError("clip_grad_norm: an output, or None, for every gradient")
+        self.array = (GradTensor * max(1, len(self.grads)))()
+        for i, (g, o) in enumerate(zip(self.grads, self.out)):
+            if o is not None and (o.shape != g.shape or o.dtype != g.dtype):
+                raise ValueError("clip_grad_norm: an output has its gradient's shape and dtype")
+            self.array[i] = GradTensor(_ptr(g), _ptr(o), g.numel(), _dt(g), 0)
+        if self.grads:
+            _one_gpu("clip_grad_norm", *self.grads, *self.out)
+
+
+def clip_grad_norm_workspace_size(n_tensors: int) -> int:
+    """Workspace bytes of clip_grad_norm on this many tensors."""
+    return int(lib().focus_workspace_size(CALL_CLIP_GRAD_NORM, None, n_tensors, 0, 0))
+
+
+def clip_grad_norm(grads, max_norm: float, out=None, ws=None, norm=None) -> torch.Tensor:
+    """The norm over all elements of `grads` (a list of float32 and bfloat16 tensors, or GradTensors) -> norm [1] float64; the
+    gradients are scaled by max_norm / norm where the norm is larger than max_norm, in place or into `out`."""
+    if isinstance(grads, GradTensors):
+        if out is not None:
+            raise ValueError("clip_grad_norm: the outputs are those of GradTensors")
+        plan = grads
+    else:
+        plan = GradTensors(grads, out)
+    device = plan.grads[0].device if plan.grads else torch.device("cuda", torch.cuda.current_device())
+    if norm is None:
+        norm = torch.empty(1, dtype=torch.float64, device=device)
+    elif norm.shape != (1,) or norm.dtype != torch.float64:
+        raise ValueError("clip_grad_norm: norm is float64 [1]")
+    ws = _sized(ws, clip_grad_norm_workspace_size(len(plan.grads)), device)
+    _one_gpu("clip_grad_norm", norm, ws, *plan.grads[:1])
+    _check(lib().focus_clip_grad_norm(plan.array, len(plan.grads), max_norm, _ptr(norm), _ptr(ws), ws.numel(), _stream()),
+           "focus_clip_grad_norm")
+    return norm
 
 
 def check_flags(ws: torch.Tensor) -> int:
