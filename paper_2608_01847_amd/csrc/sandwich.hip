@@ -16,36 +16,38 @@ namespace focus {
 
 namespace {
 
-constexpr int kThreads = 256;
+constexpr int kThreads = 256;  // of a workgroup whose waves take rows by themselves, and of the kernels for long rows
+constexpr int kMostThreads = 1024;
 constexpr int kStrips = 1024;  // workgroups of a backward launch at most, each with a row of partial sums per parameter
 
-// Sums of two values over the THREADS threads that share a row (a wave, or the workgroup), in every one of them; `lds` of 8 floats
-// is free again after the next barrier of the caller's (buffers in turn).
-template <int THREADS = kThreads>
+// Sums of two values over the threads that share a row, in every one of them: a wave (WAVE), or the workgroup of up to 16 waves.
+// `lds` of 32 floats is free again after the next barrier of the caller's (buffers in turn).
+template <bool WAVE = false>
 __device__ __forceinline__ void group_sum2(float &a, float &b, float *lds) {
     a = wave_sum(a);
     b = wave_sum(b);
-    if constexpr (THREADS == 64) return;
+    if constexpr (WAVE) return;
     if ((threadIdx.x & 63) == 0) {
         lds[threadIdx.x >> 6] = a;
-        lds[4 + (threadIdx.x >> 6)] = b;
+        lds[16 + (threadIdx.x >> 6)] = b;
     }
     __syncthreads();
     a = b = 0.0f;
-#pragma unroll
-    for (int i = 0; i < 4; i++) {
+    for (unsigned i = 0; i < blockDim.x / 64; i++) {
         a += lds[i];
-        b += lds[4 + i];
+        b += lds[16 + i];
     }
 }
 
-template <int THREADS = kThreads>
+template <bool WAVE = false>
 __device__ __forceinline__ float group_sum(float a, float *lds) {
     a = wave_sum(a);
-    if constexpr (THREADS == 64) return a;
+    if constexpr (WAVE) return a;
     if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = a;
     __syncthreads();
-    return lds[0] + lds[1] + lds[2] + lds[3];
+    a = 0.0f;
+    for (unsigned i = 0; i < blockDim.x / 64; i++) a += lds[i];
+    return a;
 }
 
 // Piece c .. c + 7 of a row of C elements (zeros past its end); rows of whole eights by a buffer load, whose range check takes
@@ -62,129 +64,186 @@ __device__ __forceinline__ void load_piece(Raw8<T> &v, const void *base, int64_t
     }
 }
 
-// A row is shared by THREADS threads (64: four rows per workgroup), NV vectors of 8 elements each: vector j of thread t starts at
-// column (j THREADS + t) 8. The row is read once; U and Y stay in registers in fp32.
-template <typename T, typename WT, int THREADS, int NV, bool TAIL>
-__global__ void __launch_bounds__(kThreads) sandwich_fwd_kernel(SandwichArgs a) {
-    __shared__ float lds[4][8];
-    constexpr int kRows = kThreads / THREADS;
-    const int t = threadIdx.x % THREADS, C = a.C;
-    const int64_t row = a.first + (int64_t)blockIdx.x * kRows + threadIdx.x / THREADS, at = row * C;
-    if (row >= a.T) return;  // whole waves where rows share a workgroup; no barrier is used there
-    Raw8<T> xr[NV], br[NV], gr[NV];
-    Raw8<WT> w1[NV], b1[NV], gf[NV], w2[NV], b2[NV];
-    const bool token = a.gate_kind == kGateToken, feature = a.gate_kind == kGateFeature;
-#pragma unroll
-    for (int j = 0; j < NV; j++) {
-        const int c = (j * THREADS + t) * 8;
-        load_piece<TAIL>(br[j], a.B, at, C, c);
-        load_piece<TAIL>(xr[j], a.X, at, C, c);
-        if (token) load_piece<TAIL>(gr[j], a.gate, at, C, c);
+// The parameters as the kernels use them, 8 at a time in fp32, 0 past the last feature: the gain and the shift after the block
+// (times the gate, where a feature has one) and those before the next. `Params` keeps them in LDS, over the columns that a row's
+// threads cover.
+template <bool BIAS, bool TOKEN>
+__device__ __forceinline__ void load_params(const SandwichArgs &a, int c, float (&w1)[8], float (&b1)[8], float (&w2)[8], float (&b2)[8]) {
+    const int n = a.C - c;
+    load8_param(a.w1, a.w_dtype, c, n, w1);
+    load8_param(a.w2, a.w_dtype, c, n, w2);
+    if constexpr (BIAS) {
+        load8_param(a.b1, a.w_dtype, c, a.b1 ? n : 0, b1);
+        load8_param(a.b2, a.w_dtype, c, a.b2 ? n : 0, b2);
     }
-    // the parameters are under way together with the row: a token alone waits for memory once
-#pragma unroll
-    for (int j = 0; j < NV; j++) {
-        const int c = (j * THREADS + t) * 8;
-        load_piece<TAIL>(w1[j], a.w1, 0, C, c);
-        load_piece<TAIL>(w2[j], a.w2, 0, C, c);
-        if (feature) load_piece<TAIL>(gf[j], a.gate, 0, C, c);
-        if (a.b1) load_piece<TAIL>(b1[j], a.b1, 0, C, c);
-        if (a.b2) load_piece<TAIL>(b2[j], a.b2, 0, C, c);
-    }
-    const float inv_n = 1.0f / (float)C;
-    float mean1 = 0.0f, mean2 = 0.0f, q = 0.0f;
-    if (a.layer) {
-        float s = 0.0f;
-#pragma unroll
-        for (int j = 0; j < NV; j++)
-#pragma unroll
-            for (int e = 0; e < 8; e++) s += br[j][e];
-        mean1 = group_sum<THREADS>(s, lds[0]) * inv_n;
-    }
-#pragma unroll
-    for (int j = 0; j < NV; j++) {
-        const int n = C - (j * THREADS + t) * 8;  // elements of this vector that exist
+    if (!TOKEN && a.gate_kind == kGateFeature) {
+        float g[8];
+        load8_param(a.gate, a.w_dtype, c, n, g);
 #pragma unroll
         for (int e = 0; e < 8; e++) {
-            const float d = e < n ? br[j][e] - mean1 : 0.0f;
-            q = __builtin_fmaf(d, d, q);
-        }
-    }
-    const float rstd1 = 1.0f / sqrtf(group_sum<THREADS>(q, lds[1]) * inv_n + a.eps);
-    float y[NV][8], s = 0.0f;
-#pragma unroll
-    for (int j = 0; j < NV; j++) {
-#pragma unroll
-        for (int e = 0; e < 8; e++) {  // columns past C have X, w1, b1 of 0
-            const float u = __builtin_fmaf((br[j][e] - mean1) * rstd1, w1[j][e], a.b1 ? b1[j][e] : 0.0f);
-            const float gate = token ? gr[j][e] : feature ? gf[j][e] : 1.0f;
-            y[j][e] = __builtin_fmaf(a.scale, xr[j][e], gate * u);
-            s += y[j][e];
-        }
-    }
-    if (a.layer) mean2 = group_sum<THREADS>(s, lds[2]) * inv_n;
-    q = 0.0f;
-#pragma unroll
-    for (int j = 0; j < NV; j++) {
-        const int n = C - (j * THREADS + t) * 8;
-#pragma unroll
-        for (int e = 0; e < 8; e++) {
-            const float d = e < n ? y[j][e] - mean2 : 0.0f;
-            q = __builtin_fmaf(d, d, q);
-        }
-    }
-    const float rstd2 = 1.0f / sqrtf(group_sum<THREADS>(q, lds[3]) * inv_n + a.eps);
-    T *const Y = static_cast<T *>(a.Y) + at, *const N = static_cast<T *>(a.N) + at;
-#pragma unroll
-    for (int j = 0; j < NV; j++) {
-        const int c = (j * THREADS + t) * 8;
-        if (c < C) {
-            store8_n<TAIL>(Y + c, C - c, y[j]);
-#pragma unroll
-            for (int e = 0; e < 8; e++) y[j][e] = __builtin_fmaf((y[j][e] - mean2) * rstd2, w2[j][e], a.b2 ? b2[j][e] : 0.0f);
-            store8_n<TAIL>(N + c, C - c, y[j]);
-        }
-    }
-    if (t == 0 && a.stats) {
-        a.stats[row] = rstd1;
-        a.stats[a.T + row] = rstd2;
-        if (a.layer) {
-            a.stats[2 * a.T + row] = mean1;
-            a.stats[3 * a.T + row] = mean2;
+            w1[e] *= g[e];
+            if constexpr (BIAS) b1[e] *= g[e];
         }
     }
 }
 
-// A workgroup takes `rows` consecutive rows. The parameters lie in LDS in their own type (a row's worth of registers less; without
-// a gate, a feature's gates of 1), the sums over the rows stay in registers and leave as one row of partial sums per
-// workgroup (waves that take rows by themselves are added in order through LDS first). BIAS: the sums without xh too; TOKEN: gates
-// of the tokens' own.
-template <typename T, typename WT, int THREADS, int NV, bool BIAS, bool TOKEN, bool TAIL>
-__global__ void __launch_bounds__(kThreads) sandwich_bwd_kernel(SandwichArgs a) {
-    constexpr int kRows = kThreads / THREADS, kWidth = NV * THREADS * 8;  // rows under way in a workgroup; columns it covers
-    extern __shared__ __attribute__((aligned(16))) char smem[];
-    __shared__ float lds[2][8];
-    const int t = threadIdx.x % THREADS, sub = threadIdx.x / THREADS, C = a.C;
-    WT *const lw1 = reinterpret_cast<WT *>(smem), *const lw2 = lw1 + kWidth, *const lgate = lw2 + kWidth,
-             *const lb1 = lgate + (TOKEN ? 0 : kWidth);
-    {
-        auto fill = [&](WT *to, const void *from, float missing) {
-            for (int c = threadIdx.x; c < kWidth; c += kThreads)
-                store_one(to + c, from && c < C ? load_one(static_cast<const WT *>(from) + c) : missing);
-        };
-        fill(lw1, a.w1, 0.0f);
-        fill(lw2, a.w2, 0.0f);
-        if constexpr (!TOKEN) fill(lgate, a.gate, 1.0f);
-        if constexpr (BIAS) fill(lb1, a.b1, 0.0f);
+template <bool BIAS, bool TOKEN>
+struct Params {
+    float *w1, *w2, *b1, *b2;
+    __device__ __forceinline__ Params(const SandwichArgs &a, float *lds, int width) {
+        w1 = lds, w2 = lds + width, b1 = lds + 2 * width, b2 = lds + 3 * width;
+        const int c = threadIdx.x * 8;  // at least as many threads as vectors
+        if (c >= width) return;
+        float v[4][8];
+        load_params<BIAS, TOKEN>(a, c, v[0], v[2], v[1], v[3]);
+#pragma unroll
+        for (int i = 0; i < (BIAS ? 4 : 2); i++)
+#pragma unroll
+            for (int h = 0; h < 2; h++)
+                reinterpret_cast<float4 *>(lds + i * width + c)[h] = make_float4(v[i][4 * h], v[i][4 * h + 1], v[i][4 * h + 2], v[i][4 * h + 3]);
     }
-    __syncthreads();
-    auto param = [&](const WT *p, int j) {
-        Raw8<WT> v;
-        v.load(p + (j * THREADS + t) * 8, 8);
-        return v;
+    static size_t bytes(size_t width) { return (BIAS ? 4 : 2) * width * sizeof(float); }
+};
+
+__device__ __forceinline__ void lds8(const float *p, float (&v)[8]) {
+    const float4 x = reinterpret_cast<const float4 *>(p)[0], y = reinterpret_cast<const float4 *>(p)[1];
+    v[0] = x.x, v[1] = x.y, v[2] = x.z, v[3] = x.w, v[4] = y.x, v[5] = y.y, v[6] = y.z, v[7] = y.w;
+}
+
+// A row is shared by a wave (WAVE: four rows in a workgroup) or by the workgroup, NV vectors of 8 elements per thread: with n threads
+// vector j of thread t starts at column (j n + t) 8. A row is read once, and U and Y stay in registers in fp32. Waves take one row each,
+// with the parameters from the caches; a workgroup takes `rows` consecutive rows, with the parameters in LDS, and asks for the next
+// row's pieces as soon as their registers are free. BIAS: with shifts; TOKEN: with gates of the tokens' own.
+template <typename T, bool WAVE, int NV, bool BIAS, bool TOKEN, bool TAIL>
+__global__ void __launch_bounds__(WAVE ? kThreads : kMostThreads) sandwich_fwd_kernel(SandwichArgs a) {
+    extern __shared__ __attribute__((aligned(16))) float smem[];
+    __shared__ float lds[4][32];
+    const int n_row = WAVE ? 64 : (int)blockDim.x;  // threads of a row
+    const int t = WAVE ? threadIdx.x % 64 : threadIdx.x, sub = WAVE ? threadIdx.x / 64 : 0, C = a.C;
+    const int64_t first = a.first + (int64_t)blockIdx.x * a.rows, last = first + a.rows < a.T ? first + a.rows : a.T;
+    Raw8<T> xr[NV], br[NV], gr[TOKEN ? NV : 1];
+    auto fetch = [&](Raw8<T> *to, const void *from, int64_t row) {
+        const int n = row < last ? C : 0;
+#pragma unroll
+        for (int j = 0; j < NV; j++) load_piece<TAIL>(to[j], from, row * C, n, (j * n_row + t) * 8);
     };
-    const int64_t first = (int64_t)blockIdx.x * a.rows;
-    const int64_t last = first + a.rows < a.T ? first + a.rows : a.T;
+    fetch(br, a.B, first + sub);
+    fetch(xr, a.X, first + sub);
+    if constexpr (TOKEN) fetch(gr, a.gate, first + sub);
+    float *const p[4] = {smem, smem + NV * n_row * 8, smem + 2 * NV * n_row * 8, smem + 3 * NV * n_row * 8};
+    if constexpr (!WAVE) {
+        Params<BIAS, TOKEN>(a, smem, NV * n_row * 8);
+        __syncthreads();
+    }
+    const float inv_n = 1.0f / (float)C;
+    for (int64_t row = first + sub; row < last; row += WAVE ? 4 : 1) {
+        const int64_t at = row * C;
+        float mean1 = 0.0f, mean2 = 0.0f, q = 0.0f, y[NV][8], s = 0.0f;
+#pragma unroll
+        for (int j = 0; j < NV; j++)
+#pragma unroll
+            for (int e = 0; e < 8; e++) y[j][e] = br[j][e];
+        if (a.layer) {
+#pragma unroll
+            for (int j = 0; j < NV; j++)
+#pragma unroll
+                for (int e = 0; e < 8; e++) s += y[j][e];
+            mean1 = group_sum<WAVE>(s, lds[0]) * inv_n;
+#pragma unroll
+            for (int j = 0; j < NV; j++) {
+                const int n = C - (j * n_row + t) * 8;  // elements of this vector that exist
+#pragma unroll
+                for (int e = 0; e < 8; e++) y[j][e] = e < n ? y[j][e] - mean1 : 0.0f;
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < NV; j++)
+#pragma unroll
+            for (int e = 0; e < 8; e++) q = __builtin_fmaf(y[j][e], y[j][e], q);
+        if constexpr (!WAVE) fetch(br, a.B, row + 1);
+        const float rstd1 = 1.0f / sqrtf(group_sum<WAVE>(q, lds[1]) * inv_n + a.eps);
+        s = 0.0f;
+        float w2[WAVE ? NV : 1][8], b2[WAVE ? NV : 1][8];
+#pragma unroll
+        for (int j = 0; j < NV; j++) {
+            const int c = (j * n_row + t) * 8;
+            float w[8], b[8];
+            if constexpr (WAVE) {
+                load_params<BIAS, TOKEN>(a, c, w, b, w2[j], b2[j]);
+            } else {
+                lds8(p[0] + c, w);
+                if constexpr (BIAS) lds8(p[2] + c, b);
+            }
+#pragma unroll
+            for (int e = 0; e < 8; e++) {  // columns past C are 0
+                const float xh = y[j][e] * rstd1;
+                float u = BIAS ? __builtin_fmaf(xh, w[e], b[e]) : xh * w[e];
+                if constexpr (TOKEN) u *= gr[TOKEN ? j : 0][e];
+                y[j][e] = __builtin_fmaf(a.scale, xr[j][e], u);
+                s += y[j][e];
+            }
+        }
+        if constexpr (!WAVE) {
+            fetch(xr, a.X, row + 1);
+            if constexpr (TOKEN) fetch(gr, a.gate, row + 1);
+        }
+        if (a.layer) mean2 = group_sum<WAVE>(s, lds[2]) * inv_n;
+        q = 0.0f;
+#pragma unroll
+        for (int j = 0; j < NV; j++) {
+            const int n = C - (j * n_row + t) * 8;
+#pragma unroll
+            for (int e = 0; e < 8; e++) {
+                const float d = !a.layer ? y[j][e] : e < n ? y[j][e] - mean2 : 0.0f;
+                q = __builtin_fmaf(d, d, q);
+            }
+        }
+        const float rstd2 = 1.0f / sqrtf(group_sum<WAVE>(q, lds[3]) * inv_n + a.eps);
+#pragma unroll
+        for (int j = 0; j < NV; j++) {
+            const int c = (j * n_row + t) * 8;
+            if (c < C) {
+                float w[8], b[8];
+                if constexpr (WAVE) {
+#pragma unroll
+                    for (int e = 0; e < 8; e++) {
+                        w[e] = w2[j][e];
+                        if constexpr (BIAS) b[e] = b2[j][e];
+                    }
+                } else {
+                    lds8(p[1] + c, w);
+                    if constexpr (BIAS) lds8(p[3] + c, b);
+                }
+                store8_n<TAIL>(static_cast<T *>(a.Y) + at + c, C - c, y[j]);
+#pragma unroll
+                for (int e = 0; e < 8; e++) {
+                    const float xh = (y[j][e] - mean2) * rstd2;
+                    y[j][e] = BIAS ? __builtin_fmaf(xh, w[e], b[e]) : xh * w[e];
+                }
+                store8_n<TAIL>(static_cast<T *>(a.N) + at + c, C - c, y[j]);
+            }
+        }
+        if (t == 0 && a.stats) {
+            a.stats[row] = rstd1;
+            a.stats[a.T + row] = rstd2;
+            if (a.layer) {
+                a.stats[2 * a.T + row] = mean1;
+                a.stats[3 * a.T + row] = mean2;
+            }
+        }
+    }
+}
+
+// Rows, threads and the next row's pieces as in the forward; the sums over the rows stay in registers and leave as one row of
+// partial sums per workgroup (waves that take rows by themselves are added in order through LDS first). BIAS: the sums without xh too.
+template <typename T, bool WAVE, int NV, bool BIAS, bool TOKEN, bool TAIL>
+__global__ void __launch_bounds__(WAVE ? kThreads : kMostThreads) sandwich_bwd_kernel(SandwichArgs a) {
+    constexpr int kRows = WAVE ? 4 : 1;
+    extern __shared__ __attribute__((aligned(16))) float smem[];
+    __shared__ float lds[2][32];
+    const int n_row = WAVE ? 64 : (int)blockDim.x;
+    const int t = WAVE ? threadIdx.x % 64 : threadIdx.x, sub = WAVE ? threadIdx.x / 64 : 0, C = a.C;
+    const int64_t first = (int64_t)blockIdx.x * a.rows, last = first + a.rows < a.T ? first + a.rows : a.T;
     constexpr int kSums = BIAS ? 4 : 2;
     float sums[kSums][NV][8];
 #pragma unroll
@@ -192,26 +251,42 @@ __global__ void __launch_bounds__(kThreads) sandwich_bwd_kernel(SandwichArgs a) 
 #pragma unroll
         for (int j = 0; j < NV; j++) zero8(sums[i][j]);
     const float inv_n = 1.0f / (float)C;
+    Raw8<T> xr[NV], br[NV], nr[NV], yr[NV], gr[TOKEN ? NV : 1];
+    auto fetch = [&](Raw8<T> *to, const void *from, int64_t row) {
+        const int n = row < last ? C : 0;
+#pragma unroll
+        for (int j = 0; j < NV; j++) load_piece<TAIL>(to[j], from, row * C, n, (j * n_row + t) * 8);
+    };
+    float stat[4];
+    auto fetch_stats = [&](int64_t row) {
+        row = row < last ? row : first;
+#pragma unroll
+        for (int i = 0; i < 4; i++) stat[i] = i < 2 || a.layer ? a.stats[i * a.T + row] : 0.0f;
+    };
+    auto fetch_all = [&](int64_t row) {
+        fetch(br, a.B, row);
+        fetch(xr, a.X, row);
+        if constexpr (TOKEN) fetch(gr, a.gate, row);
+        fetch(nr, a.dN, row);
+        fetch(yr, a.dY, row);
+        fetch_stats(row);
+    };
+    if constexpr (!WAVE) fetch_all(first);
+    const Params<BIAS, TOKEN> p(a, smem, NV * n_row * 8);
+    __syncthreads();
     for (int64_t row = first + sub; row < last; row += kRows) {
         const int64_t at = row * C;
-        const float rstd1 = a.stats[row], rstd2 = a.stats[a.T + row];
-        const float mean1 = a.layer ? a.stats[2 * a.T + row] : 0.0f, mean2 = a.layer ? a.stats[3 * a.T + row] : 0.0f;
-        Raw8<T> xr[NV], br[NV], nr[NV], yr[NV], gr[TOKEN ? NV : 1];
-#pragma unroll
-        for (int j = 0; j < NV; j++) {
-            const int c = (j * THREADS + t) * 8;
-            load_piece<TAIL>(br[j], a.B, at, C, c);
-            load_piece<TAIL>(xr[j], a.X, at, C, c);
-            if constexpr (TOKEN) load_piece<TAIL>(gr[j], a.gate, at, C, c);
-            load_piece<TAIL>(nr[j], a.dN, at, C, c);
-            load_piece<TAIL>(yr[j], a.dY, at, C, c);
-        }
+        if constexpr (WAVE) fetch_all(row);
+        // xh = h rstd - mean rstd in one operation: what the product is off by is as little as the mean itself may be
+        const float rstd1 = stat[0], rstd2 = stat[1], off1 = -stat[2] * rstd1, off2 = -stat[3] * rstd2;
+        if constexpr (!WAVE) fetch_stats(row + 1);
         // keeps the compiler from holding over the next sum what the packed rows and the LDS give again
         auto again = [&]() {
             asm volatile("" ::: "memory");
 #pragma unroll
             for (int j = 0; j < NV; j++) {
-                br[j].keep_packed(), nr[j].keep_packed(), yr[j].keep_packed();
+                br[j].keep_packed();
+                if constexpr (WAVE) nr[j].keep_packed(), yr[j].keep_packed();
                 if constexpr (TOKEN) gr[j].keep_packed();
             }
         };
@@ -220,12 +295,17 @@ __global__ void __launch_bounds__(kThreads) sandwich_bwd_kernel(SandwichArgs a) 
 #pragma unroll
         for (int j = 0; j < NV; j++) {
             __builtin_amdgcn_sched_barrier(0);  // one vector's values in fp32 at a time
-            const Raw8<WT> w1 = param(lw1, j), w2 = param(lw2, j), gf = TOKEN ? w1 : param(lgate, j), b1 = BIAS ? param(lb1, j) : w1;
+            const int c = (j * n_row + t) * 8;
+            float w1[8], w2[8], b1[8];
+            lds8(p.w1 + c, w1);
+            lds8(p.w2 + c, w2);
+            if constexpr (BIAS) lds8(p.b1 + c, b1);
 #pragma unroll
             for (int e = 0; e < 8; e++) {  // columns past C have dN = 0
-                const float u = __builtin_fmaf((br[j][e] - mean1) * rstd1, w1[e], BIAS ? b1[e] : 0.0f);
-                const float gate = TOKEN ? gr[TOKEN ? j : 0][e] : gf[e];
-                const float xh2 = (__builtin_fmaf(a.scale, xr[j][e], gate * u) - mean2) * rstd2;
+                const float xh1 = __builtin_fmaf(br[j][e], rstd1, off1);
+                float u = BIAS ? __builtin_fmaf(xh1, w1[e], b1[e]) : xh1 * w1[e];
+                if constexpr (TOKEN) u *= gr[TOKEN ? j : 0][e];
+                const float xh2 = __builtin_fmaf(__builtin_fmaf(a.scale, xr[j][e], u), rstd2, off2);
                 const float n = nr[j][e], g = n * w2[e];
                 sums[0][j][e] = __builtin_fmaf(n, xh2, sums[0][j][e]);
                 if constexpr (BIAS) sums[2][j][e] += n;
@@ -234,59 +314,75 @@ __global__ void __launch_bounds__(kThreads) sandwich_bwd_kernel(SandwichArgs a) 
                 d[j][e] = xh2;
             }
         }
-        group_sum2<THREADS>(sg, sgx, lds[0]);
+        if constexpr (!WAVE) fetch(xr, a.X, row + 1);
+        group_sum2<WAVE>(sg, sgx, lds[0]);
         const float mg2 = a.layer ? sg * inv_n : 0.0f, mgx2 = sgx * inv_n;
         sg = sgx = 0.0f;
         again();
 #pragma unroll
         for (int j = 0; j < NV; j++) {
-            __builtin_amdgcn_sched_barrier(0);  // one vector's values in fp32 at a time
-            const Raw8<WT> w1 = param(lw1, j), w2 = param(lw2, j), gf = TOKEN ? w1 : param(lgate, j);
+            __builtin_amdgcn_sched_barrier(0);
+            const int c = (j * n_row + t) * 8;
+            float w1[8], w2[8];
+            lds8(p.w1 + c, w1);
+            lds8(p.w2 + c, w2);
 #pragma unroll
             for (int e = 0; e < 8; e++) {  // columns past C have w1 = 0
-                d[j][e] = __builtin_fmaf(rstd2, nr[j][e] * w2[e] - mg2 - d[j][e] * mgx2, yr[j][e]);
-                const float xh1 = (br[j][e] - mean1) * rstd1;
+                const float g2 = __builtin_fmaf(-d[j][e], mgx2, __builtin_fmaf(nr[j][e], w2[e], -mg2));
+                d[j][e] = __builtin_fmaf(rstd2, g2, yr[j][e]);
+                const float xh1 = __builtin_fmaf(br[j][e], rstd1, off1);
                 const float through = TOKEN ? d[j][e] * gr[TOKEN ? j : 0][e] : d[j][e];  // a feature's gate is applied to the sum
                 sums[1][j][e] = __builtin_fmaf(through, xh1, sums[1][j][e]);
                 if constexpr (BIAS) sums[3][j][e] += through;
-                const float g = (TOKEN ? through : through * gf[e]) * w1[e];
+                const float g = through * w1[e];
                 sg += g;
                 sgx = __builtin_fmaf(g, xh1, sgx);
             }
         }
-        group_sum2<THREADS>(sg, sgx, lds[1]);
+        if constexpr (!WAVE) {
+            fetch(nr, a.dN, row + 1);
+            fetch(yr, a.dY, row + 1);
+        }
+        group_sum2<WAVE>(sg, sgx, lds[1]);
         const float mg1 = a.layer ? sg * inv_n : 0.0f, mgx1 = sgx * inv_n;
         again();
 #pragma unroll
         for (int j = 0; j < NV; j++) {
-            const int c = (j * THREADS + t) * 8;
+            const int c = (j * n_row + t) * 8;
             __builtin_amdgcn_sched_barrier(0);
             if (c < C) {
-                const Raw8<WT> w1 = param(lw1, j), gf = TOKEN ? w1 : param(lgate, j), b1 = BIAS ? param(lb1, j) : w1;
-                float v[8];
+                float v[8], w1[8], b1[8];
+                lds8(p.w1 + c, w1);
+                if constexpr (BIAS) lds8(p.b1 + c, b1);
 #pragma unroll
                 for (int e = 0; e < 8; e++) v[e] = a.scale * d[j][e];
                 store8_n<TAIL>(static_cast<T *>(a.dX) + at + c, C - c, v);
 #pragma unroll
                 for (int e = 0; e < 8; e++) {
-                    const float xh1 = (br[j][e] - mean1) * rstd1;
-                    const float g = d[j][e] * (TOKEN ? gr[TOKEN ? j : 0][e] : gf[e]) * w1[e];
-                    v[e] = rstd1 * (g - mg1 - xh1 * mgx1);
+                    const float xh1 = __builtin_fmaf(br[j][e], rstd1, off1);
+                    const float g = (TOKEN ? d[j][e] * gr[TOKEN ? j : 0][e] : d[j][e]) * w1[e];
+                    v[e] = rstd1 * __builtin_fmaf(-xh1, mgx1, g - mg1);
                 }
                 store8_n<TAIL>(static_cast<T *>(a.dB) + at + c, C - c, v);
                 if (TOKEN && a.dgate) {
 #pragma unroll
-                    for (int e = 0; e < 8; e++)
-                        v[e] = d[j][e] * __builtin_fmaf((br[j][e] - mean1) * rstd1, w1[e], BIAS ? b1[e] : 0.0f);
+                    for (int e = 0; e < 8; e++) {
+                        const float xh1 = __builtin_fmaf(br[j][e], rstd1, off1);
+                        v[e] = d[j][e] * (BIAS ? __builtin_fmaf(xh1, w1[e], b1[e]) : xh1 * w1[e]);
+                    }
                     store8_n<TAIL>(static_cast<T *>(a.dgate) + at + c, C - c, v);
                 }
             }
         }
+        if constexpr (!WAVE) {
+            fetch(br, a.B, row + 1);
+            if constexpr (TOKEN) fetch(gr, a.gate, row + 1);
+        }
     }
-    float *const join = reinterpret_cast<float *>(smem);  // kWidth floats, over the parameters
+    float *const join = smem;  // a row's width, over the parameters
 #pragma unroll
     for (int i = 0; i < kSums; i++) {
-        if constexpr (THREADS == 64) {
+        if constexpr (WAVE) {
             for (int s = 1; s < kRows; s++) {
                 __syncthreads();
                 if (sub == s)
@@ -306,7 +402,7 @@ __global__ void __launch_bounds__(kThreads) sandwich_bwd_kernel(SandwichArgs a) 
             float *const part = a.part + ((int64_t)i * gridDim.x + blockIdx.x) * C;
 #pragma unroll
             for (int j = 0; j < NV; j++) {
-                const int c = (j * THREADS + t) * 8;
+                const int c = (j * n_row + t) * 8;
                 if (c < C) store8_n<TAIL>(part + c, C - c, sums[i][j]);
             }
         }
@@ -331,7 +427,7 @@ struct Element {
 // A workgroup per row, which it reads once for each sum and once for the outputs, element by element.
 template <typename T>
 __global__ void __launch_bounds__(kThreads) sandwich_fwd_long_kernel(SandwichArgs a) {
-    __shared__ float lds[2][8];
+    __shared__ float lds[2][32];
     const int64_t row = a.first + blockIdx.x;
     const int C = a.C;
     const float n = (float)C;
@@ -378,7 +474,7 @@ __global__ void __launch_bounds__(kThreads) sandwich_fwd_long_kernel(SandwichArg
 // A workgroup takes `rows` rows one after the other; the sums over them are added up in its row of the partial sums.
 template <typename T>
 __global__ void __launch_bounds__(kThreads) sandwich_bwd_long_kernel(SandwichArgs a) {
-    __shared__ float lds[2][8];
+    __shared__ float lds[2][32];
     const int C = a.C;
     const int64_t first = (int64_t)blockIdx.x * a.rows;
     const int64_t last = first + a.rows < a.T ? first + a.rows : a.T;
@@ -465,61 +561,77 @@ __global__ void __launch_bounds__(1024) sandwich_finish_kernel(SandwichArgs a, i
     }
 }
 
-int64_t bwd_parts(int64_t T) {
-    const int64_t rows = std::max<int64_t>(4, (T + kStrips - 1) / kStrips);
-    return (T + rows - 1) / rows;
-}
-
-template <int... Vs, typename F>
-bool pick_nv(int64_t need, F &&f) {
-    bool done = false;
-    ((!done && need <= Vs ? (f(std::integral_constant<int, Vs>{}), done = true) : false), ...);
-    return done;
-}
-
-// Threads per row and vectors per thread: a wave per row up to 1,024 features, a workgroup up to 8,192 (32 elements per
-// thread), false beyond that. f(threads, vectors, whether a row has a piece of fewer than 8)
+// Who shares a row: a wave up to 1,024 features, beyond that a workgroup of as many waves as its vectors of 8 take; false past
+// 8,192. f(wave, vectors per thread, whether a row has a piece of fewer than 8, threads)
 template <typename F>
 bool sandwich_shape(int64_t C, F &&f) {
     const int64_t vecs = (C + 7) / 8;
-    auto tail = [&](auto threads, auto nv) { C % 8 ? f(threads, nv, std::true_type{}) : f(threads, nv, std::false_type{}); };
-    if (vecs <= 64 * 2) return pick_nv<1, 2>((vecs + 63) / 64, [&](auto nv) { tail(std::integral_constant<int, 64>{}, nv); });
-    return pick_nv<2, 4>((vecs + 255) / 256, [&](auto nv) { tail(std::integral_constant<int, 256>{}, nv); });
+    auto tail = [&](auto wave, auto nv, int64_t n) {
+        C % 8 ? f(wave, nv, std::true_type{}, (unsigned)n) : f(wave, nv, std::false_type{}, (unsigned)n);
+    };
+    if (vecs > kMostThreads) return false;
+    constexpr std::integral_constant<int, 1> one{};
+    constexpr std::integral_constant<int, 2> two{};
+    if (vecs <= 64) tail(std::true_type{}, one, kThreads);
+    else if (vecs <= 128) tail(std::true_type{}, two, kThreads);
+    else tail(std::false_type{}, one, (vecs + 63) / 64 * 64);
+    return true;
 }
 
-template <typename T, typename WT>
+// Workgroups of a launch that keeps the parameters in LDS: as many as are resident at once with four waves per SIMD (a second round
+// of workgroups would take as long as the first), each with `least` rows at least.
+int64_t sandwich_parts(int64_t T, int64_t C, int64_t least) {
+    const int64_t waves = C <= 1024 ? 4 : std::min<int64_t>(16, (C + 511) / 512);
+    const int64_t strips = std::min<int64_t>(kStrips, 256 * (16 / waves)), rows = std::max<int64_t>(least, (T + strips - 1) / strips);
+    return (T + rows - 1) / rows;
+}
+
+// Launches kernel(bias, token) with the parameters' LDS
+template <typename F>
+void sandwich_go(const SandwichArgs &a, bool bias, bool wave, int nv, unsigned threads, unsigned parts, hipStream_t st, F &&kernel) {
+    const size_t width = (size_t)nv * (wave ? 64 : threads) * 8;
+    auto go = [&](auto with_bias, auto of_token) {
+        auto *const k = kernel(with_bias, of_token);
+        const size_t lds = Params<decltype(with_bias)::value, decltype(of_token)::value>::bytes(width);  // 128 KB at most
+        if (lds > 64 * 1024)
+            (void)hipFuncSetAttribute(reinterpret_cast<const void *>(k), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+        k<<<parts, threads, lds, st>>>(a);
+    };
+    const bool token = a.gate_kind == kGateToken;
+    if (bias) token ? go(std::true_type{}, std::true_type{}) : go(std::true_type{}, std::false_type{});
+    else token ? go(std::false_type{}, std::true_type{}) : go(std::false_type{}, std::false_type{});
+}
+
+template <typename T>
 hipError_t sandwich_fwd(SandwichArgs a, hipStream_t st) {
-    constexpr int64_t kRows = (int64_t(1) << 24) - 4;  // a launch's work-items (256 per row at most) stay below 2^32; whole workgroups
-    for (a.first = 0; a.first < a.T; a.first += kRows) {
-        const int64_t rows = std::min(kRows, a.T - a.first);
-        const bool done = sandwich_shape(a.C, [&](auto threads, auto nv, auto tail) {
-            constexpr int TH = decltype(threads)::value, per = kThreads / TH;
-            sandwich_fwd_kernel<T, WT, TH, decltype(nv)::value, decltype(tail)::value>
-                <<<(unsigned)((rows + per - 1) / per), kThreads, 0, st>>>(a);
+    // A launch's work-items stay below 2^32. Up to 1,024 features a workgroup is four rows; up to 8,192 there are as many as are
+    // resident; beyond that one per row.
+    const int64_t most = a.C <= 1024 ? int64_t(1) << 25 : a.C <= 8 * kMostThreads ? a.T : (int64_t(1) << 24) - 1;
+    for (a.first = 0; a.first < a.T; a.first += most) {
+        const int64_t rows = std::min(most, a.T - a.first);
+        const int64_t parts = a.C <= 1024 ? (rows + 3) / 4 : a.C <= 8 * kMostThreads ? sandwich_parts(rows, a.C, 1) : rows;
+        a.rows = (rows + parts - 1) / parts;
+        if (a.C <= 1024) a.rows = 4;
+        const bool done = sandwich_shape(a.C, [&](auto wave, auto nv, auto tail, unsigned threads) {
+            sandwich_go(a, a.b1 || a.b2, wave.value, nv.value, threads, (unsigned)parts, st, [](auto bias, auto token) {
+                return &sandwich_fwd_kernel<T, decltype(wave)::value, decltype(nv)::value, decltype(bias)::value,
+                                            decltype(token)::value, decltype(tail)::value>;
+            });
         });
-        if (!done) sandwich_fwd_long_kernel<T><<<(unsigned)rows, kThreads, 0, st>>>(a);
+        if (!done) sandwich_fwd_long_kernel<T><<<(unsigned)parts, kThreads, 0, st>>>(a);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
     return hipSuccess;
 }
 
-template <typename T, typename WT>
+template <typename T>
 hipError_t sandwich_bwd(const SandwichArgs &a, unsigned parts, hipStream_t st) {
-    const bool done = sandwich_shape(a.C, [&](auto threads, auto nv, auto tail) {
-        constexpr int TH = decltype(threads)::value, NV = decltype(nv)::value;
-        constexpr size_t width = (size_t)NV * TH * 8;
-        const bool token = a.gate_kind == kGateToken;
-        const size_t params = (2 + !token + (a.sums == 4)) * width * sizeof(WT);
-        const size_t lds = TH == 64 ? std::max(params, width * sizeof(float)) : params;
-        auto go = [&](auto bias, auto of_token) {
-            auto *const kernel = sandwich_bwd_kernel<T, WT, TH, NV, decltype(bias)::value, decltype(of_token)::value, decltype(tail)::value>;
-            if (lds > 64 * 1024)
-                (void)hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
-            kernel<<<parts, kThreads, lds, st>>>(a);
-        };
-        if (a.sums == 4) token ? go(std::true_type{}, std::true_type{}) : go(std::true_type{}, std::false_type{});
-        else token ? go(std::false_type{}, std::true_type{}) : go(std::false_type{}, std::false_type{});
+    const bool done = sandwich_shape(a.C, [&](auto wave, auto nv, auto tail, unsigned threads) {
+        sandwich_go(a, a.sums == 4, wave.value, nv.value, threads, parts, st, [](auto bias, auto token) {
+            return &sandwich_bwd_kernel<T, decltype(wave)::value, decltype(nv)::value, decltype(bias)::value, decltype(token)::value,
+                                        decltype(tail)::value>;
+        });
     });
     if (!done) sandwich_bwd_long_kernel<T><<<parts, kThreads, 0, st>>>(a);
     return hipGetLastError();
@@ -533,18 +645,15 @@ size_t sandwich_bwd_ws(int64_t T, int64_t C) {
 }
 
 hipError_t launch_sandwich_fwd(int dtype, SandwichArgs a, hipStream_t st) {
-    if (dtype == kBF16) return a.w_dtype == kBF16 ? sandwich_fwd<uint16_t, uint16_t>(a, st) : sandwich_fwd<uint16_t, float>(a, st);
-    return a.w_dtype == kBF16 ? sandwich_fwd<float, uint16_t>(a, st) : sandwich_fwd<float, float>(a, st);
+    return dtype == kBF16 ? sandwich_fwd<uint16_t>(a, st) : sandwich_fwd<float>(a, st);
 }
 
 hipError_t launch_sandwich_bwd(int dtype, SandwichArgs a, void *ws, hipStream_t st) {
-    const int64_t parts = bwd_parts(a.T);
+    const int64_t parts = sandwich_parts(a.T, a.C, 4);
     a.part = reinterpret_cast<float *>(static_cast<char *>(ws) + kWsHeader);
     a.rows = (a.T + parts - 1) / parts;
     a.sums = a.b1 || a.db1 || a.db2 ? 4 : 2;
-    hipError_t e;
-    if (dtype == kBF16) e = a.w_dtype == kBF16 ? sandwich_bwd<uint16_t, uint16_t>(a, (unsigned)parts, st) : sandwich_bwd<uint16_t, float>(a, (unsigned)parts, st);
-    else e = a.w_dtype == kBF16 ? sandwich_bwd<float, uint16_t>(a, (unsigned)parts, st) : sandwich_bwd<float, float>(a, (unsigned)parts, st);
+    const hipError_t e = dtype == kBF16 ? sandwich_bwd<uint16_t>(a, (unsigned)parts, st) : sandwich_bwd<float>(a, (unsigned)parts, st);
     if (e != hipSuccess) return e;
     sandwich_finish_kernel<<<(unsigned)((a.C + 15) / 16), 256 * a.sums, 0, st>>>(a, (int)parts);
     return hipGetLastError();
