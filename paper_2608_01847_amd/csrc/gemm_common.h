@@ -169,6 +169,13 @@ hipError_t launch_bwd_small(int fmt, int w_dt, const void *dY, const void *X, co
 bool mfma_dx_supported(int64_t M, int64_t N, int64_t K);
 hipError_t launch_dx_mfma(const void *dY, const void *W, int64_t M, int64_t N, int64_t K, int64_t chunk, int64_t splits,
                           void *dX, float *part, hipStream_t st);
+// dY W as fp32 sums of its splits in part [splits][M][K], dY [M][ldy] with zeros behind its N columns to the next multiple of 32
+hipError_t launch_dx_sums(const void *dY, const void *W, int64_t M, int64_t N, int64_t ldy, int64_t K, int64_t chunk,
+                          int64_t splits, float *part, hipStream_t st);
+// out [N][K] = factor dY^T X (bf16 operands, dY [M][ldy] with ldy a multiple of 256); with splits > 1 the token ranges' fp32 sums
+// without the factor in part [splits][N][K] in place of out
+hipError_t launch_dw_mfma(const void *dY, const void *X, int64_t M, int64_t N, int64_t ldy, int64_t K, int64_t chunk,
+                          int64_t splits, const float *factor, void *out, int out_dtype, float *part, hipStream_t st);
 // the same product from packed MXFP4 operands (X codes [M][K/2], W codes in K-slabs [K/128][N][64],
 // block-major E8M0 bytes [K/32][rows]; K % 128 == 0)
 bool mfma_fwd_mx_supported(int64_t M, int64_t N, int64_t K);

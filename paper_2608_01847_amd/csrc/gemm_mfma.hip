@@ -528,25 +528,12 @@ fwd_mfma_kernel(const void *__restrict__ X, const void *__restrict__ W, const ui
 }
 
 // ------------------------------------------------------------------------------------------------
-template <int FMT, int WDT>
-__global__ void __launch_bounds__(kThreads, 1)
-bwd_mfma_kernel(const uint16_t *__restrict__ dY, const uint16_t *__restrict__ X, int64_t M, int64_t N, int64_t K,
-                int64_t chunk, const void *__restrict__ W, const float *__restrict__ s_fp,
-                const float *__restrict__ c, int sb_log2, const float *__restrict__ alpha_ptr, int ste_clip,
-                int e8m0_floor, float *__restrict__ part_s, float *__restrict__ part_c, int direct, uint32_t *flag,
-                int tiles_n) {
-    __shared__ __attribute__((aligned(16))) char smem[kBwdStages * kBwdStageBytes];
+// Main loop of the backward on bf16 operands: acc = the tile of X^T dY (rows = columns k0 .. of X, columns = columns n0 .. of dY) over
+// the tokens t_begin .. t_end - 1, X of K columns, dY of N.
+__device__ __forceinline__ void bwd_products(const uint16_t *__restrict__ dY, const uint16_t *__restrict__ X, int64_t N, int64_t K,
+                                             int64_t n0, int64_t k0, int64_t t_begin, int64_t t_end, char *smem,
+                                             f32x16_t (&acc)[4][4]) {
     const int t = threadIdx.x, lane = t & 63, wave = t >> 6, wm = wave >> 1, wn = wave & 1;
-    // linear id -> (split, tile): splits outermost, tiles of one split in grouped order, so that an
-    // XCD's concurrent workgroups share the operand panels of one token range
-    const uint32_t id = xcd_tile(blockIdx.y * gridDim.x + blockIdx.x, gridDim.x * gridDim.y);
-    uint32_t tk, tn;
-    grouped_tile(id % gridDim.x, gridDim.x / tiles_n, tiles_n, tk, tn);
-    const int64_t k0 = (int64_t)tk * kTile, n0 = (int64_t)tn * kTile;
-    const int64_t split = id / gridDim.x;
-    const int64_t t_begin = split * chunk, t_end = std::min<int64_t>(M, t_begin + chunk);
-
-    f32x16_t acc[4][4];
     const f32x16_t zero = {};
 #pragma unroll
     for (int i = 0; i < 4; i++)
@@ -625,9 +612,61 @@ bwd_mfma_kernel(const uint16_t *__restrict__ dY, const uint16_t *__restrict__ X,
     tr_wait(f);  // no read may still be in flight when the workgroup ends
     // the empty slots' zero writes must land before the workgroup's LDS is handed on
     FOCUS_WAIT_VMCNT(0);
+}
+
+template <int FMT, int WDT>
+__global__ void __launch_bounds__(kThreads, 1)
+bwd_mfma_kernel(const uint16_t *__restrict__ dY, const uint16_t *__restrict__ X, int64_t M, int64_t N, int64_t K,
+                int64_t chunk, const void *__restrict__ W, const float *__restrict__ s_fp,
+                const float *__restrict__ c, int sb_log2, const float *__restrict__ alpha_ptr, int ste_clip,
+                int e8m0_floor, float *__restrict__ part_s, float *__restrict__ part_c, int direct, uint32_t *flag,
+                int tiles_n) {
+    __shared__ __attribute__((aligned(16))) char smem[kBwdStages * kBwdStageBytes];
+    // linear id -> (split, tile): splits outermost, tiles of one split in grouped order, so that an
+    // XCD's concurrent workgroups share the operand panels of one token range
+    const uint32_t id = xcd_tile(blockIdx.y * gridDim.x + blockIdx.x, gridDim.x * gridDim.y);
+    uint32_t tk, tn;
+    grouped_tile(id % gridDim.x, gridDim.x / tiles_n, tiles_n, tk, tn);
+    const int64_t k0 = (int64_t)tk * kTile, n0 = (int64_t)tn * kTile;
+    const int64_t split = id / gridDim.x;
+    const int64_t t_begin = split * chunk, t_end = std::min<int64_t>(M, t_begin + chunk);
+
+    f32x16_t acc[4][4];
+    bwd_products(dY, X, N, K, n0, k0, t_begin, t_end, smem, acc);
     static_assert(sizeof(smem) >= 128 * 1024, "the epilogue's two quarters fit");
     ste_epilogue<FMT, WDT, kTile>(acc, k0, n0, split, N, K, W, s_fp, c, sb_log2, alpha_ptr, ste_clip, e8m0_floor, part_s,
                            part_c, direct, flag, smem);
+}
+
+// The plain product dW [N][K] = dY^T X, times *factor: dY [M][ldy] with N real columns (the others up to the tile's end exist and
+// are not stored). With `part` a token range of `chunk` per split, whose fp32 sums go to part [split][N][K].
+__global__ void __launch_bounds__(kThreads, 1)
+dw_mfma_kernel(const uint16_t *__restrict__ dY, const uint16_t *__restrict__ X, int64_t M, int64_t N, int64_t ldy, int64_t K,
+               int64_t chunk, const float *__restrict__ factor, void *__restrict__ out, int out_dtype, float *__restrict__ part,
+               int tiles_n) {
+    __shared__ __attribute__((aligned(16))) char smem[kBwdStages * kBwdStageBytes];
+    const uint32_t id = xcd_tile(blockIdx.y * gridDim.x + blockIdx.x, gridDim.x * gridDim.y);
+    uint32_t tk, tn;
+    grouped_tile(id % gridDim.x, gridDim.x / tiles_n, tiles_n, tk, tn);
+    const int64_t k0 = (int64_t)tk * kTile, n0 = (int64_t)tn * kTile;
+    const int64_t split = id / gridDim.x;
+    const int64_t t_begin = split * chunk, t_end = std::min<int64_t>(M, t_begin + chunk);
+    f32x16_t acc[4][4];
+    bwd_products(dY, X, ldy, K, n0, k0, t_begin, t_end, smem, acc);
+    __syncthreads();  // every wave is done with the operand stages
+    if (part) {
+        store_tile_f32(acc, smem, part + (split * N + n0) * K, N - n0, K, (uint32_t)k0, K);
+        return;
+    }
+    const float f = *factor;
+#pragma unroll
+    for (int i = 0; i < 4; i++)
+#pragma unroll
+        for (int j = 0; j < 4; j++)
+#pragma unroll
+            for (int r = 0; r < 16; r++) acc[i][j][r] *= f;
+    if (out_dtype == kBF16) store_tile_bf16(acc, smem, static_cast<uint16_t *>(out) + n0 * K, N - n0, K, (uint32_t)k0, K);
+    else store_tile_f32(acc, smem, static_cast<float *>(out) + n0 * K, N - n0, K, (uint32_t)k0, K);
 }
 
 // ------------------------------------------------------------------------------------------------
@@ -908,7 +947,7 @@ bwd_mfma_mx_kernel(const uint16_t *__restrict__ dY, const uint8_t *__restrict__ 
 
 // ------------------------------------------------------------------------------------------------
 // Input gradient dX_hat = dY W_hat: rows = tokens, columns = in features k, the reduction over the out
-// features n. dY [M][N] is contiguous along the reduction and staged and read as the forward's operands;
+// features n. dY [M][ldy] (ldy >= N, what lies between them in the last step of 32 being zeros) is contiguous along the reduction and staged and read as the forward's operands;
 // W_hat [N][K] is reduction-major and staged and read (transposing) as the backward's, so no transposed copy of
 // it is made. Pipeline and fragment sets of the backward, 32 n per step. With splits > 1 each workgroup covers
 // `chunk` of the n range and writes fp32 sums to part [split][M][K], which dx_finish_kernel adds up.
@@ -916,7 +955,7 @@ bwd_mfma_mx_kernel(const uint16_t *__restrict__ dY, const uint8_t *__restrict__ 
 // number: 4,096 x 32,000 x 2,560 (160 tiles, 3 splits) 587 us for 895, 640 x 31,808 x 1,184 65 for 590,
 // 65,536 x 9,728 x 2,560 (no splits) 2.63 ms for 2.71.
 __global__ void __launch_bounds__(kThreads, 1)
-dx_mfma_kernel(const uint16_t *__restrict__ dY, const uint16_t *__restrict__ W, int64_t M, int64_t N, int64_t K,
+dx_mfma_kernel(const uint16_t *__restrict__ dY, const uint16_t *__restrict__ W, int64_t M, int64_t N, int64_t ldy, int64_t K,
                int64_t chunk, uint16_t *__restrict__ dX, float *__restrict__ part, int tiles_k) {
     constexpr int S = kBwdStages;
     __shared__ __attribute__((aligned(16))) char smem[S * kBwdStageBytes];
@@ -939,12 +978,12 @@ dx_mfma_kernel(const uint16_t *__restrict__ dY, const uint16_t *__restrict__ W, 
 
     lds_char *const lsm = (lds_char *)smem;
     const int wave_u = __builtin_amdgcn_readfirstlane(wave);
-    const int64_t pitch = N * 2;
+    const int64_t pitch = ldy * 2;
     FwdDma<> pa;
     pa.init(pitch, wave_u, lane);
     BwdDma pb;
     pb.init(K, k0, wave_u, lane);
-    const __amdgpu_buffer_rsrc_t ra = make_rsrc(dY + m0 * N, (M - m0) * pitch);
+    const __amdgpu_buffer_rsrc_t ra = make_rsrc(dY + m0 * ldy, (M - m0) * pitch);
     const int64_t nk = n_end > n_begin ? (n_end - n_begin + kBwdStep - 1) / kBwdStep : 0;
     // offset bits of step j's dY loads: bytes past the row's end and steps past the range read as zeros
     auto a_bad = [&](int64_t j) { return j < nk ? pa.step_bad(pitch, n_begin * 2 + j * 64) : 0x80000000u; };
@@ -1113,9 +1152,27 @@ hipError_t launch_dx_mfma(const void *dY, const void *W, int64_t M, int64_t N, i
     const int tiles_m = (int)((M + kTile - 1) / kTile), tiles_k = (int)((K + kTile - 1) / kTile);
     const dim3 grid((unsigned)tiles_m * tiles_k, (unsigned)splits);
     uint16_t *d = static_cast<uint16_t *>(dX);
-    dx_mfma_kernel<<<grid, kThreads, 0, st>>>(static_cast<const uint16_t *>(dY), static_cast<const uint16_t *>(W), M, N, K,
+    dx_mfma_kernel<<<grid, kThreads, 0, st>>>(static_cast<const uint16_t *>(dY), static_cast<const uint16_t *>(W), M, N, N, K,
                                               chunk, d, splits > 1 ? part : nullptr, tiles_k);
     if (splits > 1) dx_finish_kernel<<<(unsigned)((M * K / 8 + 255) / 256), 256, 0, st>>>(part, splits, M * K, d);
+    return hipGetLastError();
+}
+
+hipError_t launch_dx_sums(const void *dY, const void *W, int64_t M, int64_t N, int64_t ldy, int64_t K, int64_t chunk,
+                          int64_t splits, float *part, hipStream_t st) {
+    const int tiles_m = (int)((M + kTile - 1) / kTile), tiles_k = (int)((K + kTile - 1) / kTile);
+    const dim3 grid((unsigned)tiles_m * tiles_k, (unsigned)splits);
+    dx_mfma_kernel<<<grid, kThreads, 0, st>>>(static_cast<const uint16_t *>(dY), static_cast<const uint16_t *>(W), M, N, ldy, K,
+                                              chunk, nullptr, part, tiles_k);
+    return hipGetLastError();
+}
+
+hipError_t launch_dw_mfma(const void *dY, const void *X, int64_t M, int64_t N, int64_t ldy, int64_t K, int64_t chunk,
+                          int64_t splits, const float *factor, void *out, int out_dtype, float *part, hipStream_t st) {
+    const int tiles_k = (int)((K + kTile - 1) / kTile), tiles_n = (int)((N + kTile - 1) / kTile);
+    dw_mfma_kernel<<<dim3((unsigned)tiles_k * tiles_n, (unsigned)splits), kThreads, 0, st>>>(
+        static_cast<const uint16_t *>(dY), static_cast<const uint16_t *>(X), M, N, ldy, K, chunk, factor, out, out_dtype,
+        splits > 1 ? part : nullptr, tiles_n);
     return hipGetLastError();
 }
 

@@ -1,0 +1,30 @@
+// What the kernels of the linear cross entropy share (not part of the public ABI).
+#pragma once
+
+#include "internal.h"
+
+namespace focus {
+
+constexpr int kCeTile = 256;  // edge of a logit tile on the matrix instructions
+constexpr int kCeFew = 32;    // tokens up to which the forward reads the weights straight into registers
+constexpr int kCeFewV = 128;  // vocabulary entries of its workgroups
+
+struct CeArgs {
+    const void *X, *W;
+    const int64_t *target;
+    float *lse, *logp;    // [T]; logp NULL where no targets are given
+    const float *g, *h;   // gradients of logp and lse, NULL: 0
+    float2 *part;         // [tiles][T] maximum and sum of a tile's exponentials
+    float *zt;            // [T] logit of the target
+    void *D;              // [T][pitch] of the piece: fp32, or bf16 relative to the token's scale
+    const float *scale;   // [T] larger of |g| and |h|, what D is relative to
+    int64_t T, V, K, pitch, v0, t0;  // first vocabulary entry of the piece, first token of the launch
+    int tiles_v;
+};
+
+// Logit tiles on the matrix instructions (bf16, K a multiple of 16): the tiles of `tokens` tokens from a.t0 on
+void launch_ce_stats_mfma(const CeArgs &a, int64_t tokens, hipStream_t st);
+void launch_ce_stats_few(const CeArgs &a, hipStream_t st);  // T <= kCeFew
+void launch_ce_grad_mfma(const CeArgs &a, int64_t tokens, uint32_t *flag, hipStream_t st);
+
+}  // namespace focus

@@ -8,7 +8,13 @@
 // Forward: a tile of logits is reduced at once to each token's maximum and sum of exponentials over the tile's part of the
 // vocabulary; a second kernel joins the parts. Backward: the vocabulary goes in pieces; of each the logits are formed again
 // and D, which both products read, is what lies in memory.
-#include "internal.h"
+//
+// bf16 operands with K a multiple of 16 go to the matrix instructions (linear_ce_mfma.hip), D in bf16 relative to a token's scale
+// r = max(|g|, |h|):
+//   D = r D',  dX[t] = r[t] (D' W)[t],  dW = G D'^T X',  X'[t] = X[t] r[t] / G  (rounded),  G = max r
+// so that the tokens' weights are rounded into X' where they differ, and nowhere where they are those of a mean (X' is X then).
+// Other shapes and fp32 take the kernels below.
+#include "linear_ce.h"
 #include "ops_device.h"
 
 namespace focus {
@@ -19,18 +25,6 @@ constexpr int kTileV = 64, kTileT = 64;  // logits of a tile
 constexpr int64_t kMaxGrid = (int64_t(1) << 24) - 1;  // a launch's work-items (256 per workgroup) stay below 2^32
 
 int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }
-
-struct CeArgs {
-    const void *X, *W;
-    const int64_t *target;
-    float *lse, *logp;       // [T]; logp NULL where no targets are given
-    const float *g, *h;      // gradients of logp and lse, NULL: 0
-    float2 *part;            // [tiles][T] maximum and sum of a tile's exponentials
-    float *zt;               // [T] logit of the target
-    float *D;                // [T][pitch] of the piece
-    int64_t T, V, K, pitch, v0, t0;  // first token and first vocabulary entry of the launch
-    int tiles_v;
-};
 
 // 64 tokens x 64 vocabulary entries of the logits in fp32, 4 x 4 per thread: acc[i][j] is that of token t0 + 4 (thread / 16)
 // + i and entry v0 + 4 (thread % 16) + j. For rows of K that the matrix-instruction kernels do not take; bound by LDS reads
@@ -148,7 +142,7 @@ __global__ void __launch_bounds__(256) ce_grad_kernel(CeArgs a, uint32_t *flag) 
             const int64_t v = v0 + tx * 4 + j;
             if (v - a.v0 >= a.pitch) continue;
             const float p = expf(acc[i][j] - lse);
-            a.D[t * a.pitch + (v - a.v0)] = v < a.V ? (v == want ? g : 0.0f) + (h - g) * p : 0.0f;
+            static_cast<float *>(a.D)[t * a.pitch + (v - a.v0)] = v < a.V ? (v == want ? g : 0.0f) + (h - g) * p : 0.0f;
         }
     }
     if (bad) raise_domain_flag(flag);
@@ -229,11 +223,194 @@ hipError_t product(CeProduct p, hipStream_t st) {
 
 size_t round256(size_t b) { return (b + 255) / 256 * 256; }
 
-// Vocabulary entries of a piece: D of a piece takes 1 GiB at most, as far as 256 entries allow
-constexpr int64_t kPieceBytes = int64_t(1) << 30;
-int64_t piece(int64_t T, int64_t V) {
-    const int64_t fit = kPieceBytes / (T * (int64_t)sizeof(float)) / 256 * 256;
-    return std::min(std::max<int64_t>(fit, 256), cdiv(V, 256) * 256);
+// ---- around the matrix-instruction kernels ------------------------------------------------------
+// r[t] = max(|g|, |h|) of the tokens (g: 0 where left out) and G, their maximum, by one workgroup
+__global__ void __launch_bounds__(1024) ce_scales_kernel(const int64_t *__restrict__ target, const float *__restrict__ g,
+                                                         const float *__restrict__ h, int64_t T, int64_t V, float *__restrict__ r,
+                                                         float *__restrict__ most) {
+    __shared__ float lds[16];
+    float m = 0.0f;
+    for (int64_t t = threadIdx.x; t < T; t += 1024) {
+        const bool kept = g && target[t] >= 0 && target[t] < V;
+        const float a = kept ? __builtin_fabsf(g[t]) : 0.0f, b = h ? __builtin_fabsf(h[t]) : 0.0f;
+        const float v = a > b || a != a ? a : b;  // a NaN stays one
+        r[t] = v;
+        m = v > m || v != v ? v : m;
+    }
+    for (int d = 32; d >= 1; d >>= 1) {
+        const float o = __shfl_xor(m, d, 64);
+        m = o > m || o != o ? o : m;
+    }
+    if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = m;
+    __syncthreads();
+    if (threadIdx.x) return;
+    for (int i = 0; i < 16; i++) m = lds[i] > m || lds[i] != lds[i] ? lds[i] : m;
+    *most = m;
+}
+
+// X' = X r / G, rounded to bf16; 8 elements per thread (K is a multiple of 16). A token whose gradient is 0 has a row of zeros.
+__global__ void __launch_bounds__(256) ce_scale_x_kernel(const uint16_t *__restrict__ X, const float *__restrict__ r,
+                                                         const float *__restrict__ most, int64_t first, int64_t n, int64_t K,
+                                                         uint16_t *__restrict__ out) {
+    const int64_t i = first + ((int64_t)blockIdx.x * 256 + threadIdx.x) * 8;
+    if (i >= n) return;
+    const float s = r[i / K], f = s == 0.0f ? 0.0f : s / *most;
+    float v[8];
+    load8_n(X + i, 8, v);
+#pragma unroll
+    for (int e = 0; e < 8; e++) v[e] = f == 0.0f ? 0.0f : v[e] * f;
+    store8_n(out + i, 8, v);
+}
+
+// total = before + the splits' sums in order; to `sums` in fp32, or times the row's (or everything's) factor to `out`
+__global__ void __launch_bounds__(256) ce_sums_kernel(const float *__restrict__ part, int64_t splits, const float *__restrict__ before,
+                                                      const float *__restrict__ factor, int per_row, int64_t first, int64_t n, int64_t K,
+                                                      float *__restrict__ sums, void *__restrict__ out, int out_dtype) {
+    const int64_t i = first + ((int64_t)blockIdx.x * 256 + threadIdx.x) * 8;
+    if (i >= n) return;
+    float s[8], v[8];
+    load8_n(part + i, 8, s);
+    for (int64_t z = 1; z < splits; z++) {
+        load8_n(part + z * n + i, 8, v);
+#pragma unroll
+        for (int e = 0; e < 8; e++) s[e] += v[e];
+    }
+    if (before) {
+        load8_n(before + i, 8, v);
+#pragma unroll
+        for (int e = 0; e < 8; e++) s[e] += v[e];
+    }
+    if (sums) {
+        store8_n(sums + i, 8, s);
+        return;
+    }
+    const float f = per_row ? factor[i / K] : *factor;
+#pragma unroll
+    for (int e = 0; e < 8; e++) s[e] *= f;
+    if (out_dtype == kBF16) store8_n(static_cast<uint16_t *>(out) + i, 8, s);
+    else store8_n(static_cast<float *>(out) + i, 8, s);
+}
+
+// f(first element, workgroups) in launches whose work-items stay below 2^32, 2,048 elements per workgroup
+template <typename F>
+hipError_t in_elements(int64_t n, F &&f) {
+    for (int64_t i = 0; i < n; i += kMaxGrid * 2048) {
+        f(i, (unsigned)cdiv(std::min(n - i, kMaxGrid * 2048), 2048));
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
+}
+
+bool on_mfma(int dtype, int64_t K) { return dtype == kBF16 && K % 16 == 0; }
+
+// Pieces of the vocabulary: as few as D takes 1 GiB each at most (a tile's 256 entries each at least), of one width but for the last
+constexpr int64_t kPieceBytes = int64_t(1) << 30, kMostWidth = int64_t(1) << 20;
+int64_t piece_width(int64_t T, int64_t V, int64_t esz) {
+    const int64_t fit = std::max<int64_t>(1, std::min(kPieceBytes / (T * esz), kMostWidth) / 256);
+    const int64_t tiles = cdiv(V, 256), pieces = cdiv(tiles, fit);
+    return cdiv(tiles, pieces) * 256;
+}
+// bytes of D for T tokens or fewer
+size_t piece_bytes(int64_t T, int64_t V, int64_t esz) {
+    return std::max<size_t>((size_t)(T * 256 * esz), (size_t)std::min(T * cdiv(V, 256) * 256 * esz, kPieceBytes));
+}
+
+constexpr int64_t kMostSplits = 64;
+
+// Splits of dW's token range: as plan_dx has them for the vocabulary's, in units of a 32-token step (0.9 us)
+struct Splits {
+    int64_t count, chunk;
+};
+Splits dw_splits(int64_t T, int64_t N, int64_t K) {
+    const int64_t tiles = cdiv(N, kCeTile) * cdiv(K, kCeTile), steps = cdiv(T, 32);
+    const int64_t most = tiles >= 4 * 256 ? 1 : std::min<int64_t>(std::min<int64_t>(kMostSplits, steps / 8), kDxSums / (N * K));
+    int64_t best = -1, count = 1;
+    for (int64_t s = 1; s <= std::max<int64_t>(1, most); s++) {
+        const int64_t cost = cdiv(tiles * s, 256) * (cdiv(steps, s) + 8) + (s > 1 ? s * N * K * 8 / 4000000 + 4 : 0);
+        if (best < 0 || cost < best) best = cost, count = s;
+    }
+    const int64_t chunk = cdiv(steps, count) * 32;
+    return {cdiv(T, chunk), chunk};
+}
+
+// fp32 sums of the splits: one of dX, or as many of dX or dW as kDxSums holds
+size_t sums_bytes(int64_t T, int64_t V, int64_t K) {
+    const int64_t rows = std::max(T, std::min(cdiv(V, 256) * 256, kMostWidth));
+    const int64_t many = rows > kDxSums / K / kMostSplits ? kDxSums : kMostSplits * rows * K;
+    return round256((size_t)std::max(T * K, many) * sizeof(float));
+}
+
+struct MfmaSpace {
+    float *r, *most, *sums, *part;
+    uint16_t *x, *D;
+};
+size_t mfma_space(int64_t T, int64_t V, int64_t K, char *base, MfmaSpace *s) {
+    size_t at = kWsHeader;
+    auto take = [&](size_t bytes) {
+        char *p = base + at;
+        at += round256(bytes);
+        return p;
+    };
+    char *const most = take(sizeof(float)), *const r = take((size_t)T * sizeof(float)), *const x = take((size_t)T * (size_t)K * 2);
+    char *const sums = take((size_t)T * (size_t)K * sizeof(float)), *const part = take(sums_bytes(T, V, K));
+    char *const D = take(piece_bytes(T, V, 2));
+    if (s)
+        *s = MfmaSpace{reinterpret_cast<float *>(r), reinterpret_cast<float *>(most), reinterpret_cast<float *>(sums),
+                       reinterpret_cast<float *>(part), reinterpret_cast<uint16_t *>(x), reinterpret_cast<uint16_t *>(D)};
+    return at;
+}
+
+hipError_t bwd_mfma(CeArgs a, void *dX, void *dW, int dw_dtype, uint32_t *flag, char *ws, hipStream_t st) {
+    MfmaSpace s;
+    mfma_space(a.T, a.V, a.K, ws, &s);
+    const int64_t T = a.T, V = a.V, K = a.K;
+    ce_scales_kernel<<<1, 1024, 0, st>>>(a.target, a.g, a.h, T, V, s.r, s.most);
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    a.scale = s.r, a.D = s.D;
+    if (dW) {
+        e = in_elements(T * K, [&](int64_t first, unsigned grid) {
+            ce_scale_x_kernel<<<grid, 256, 0, st>>>(static_cast<const uint16_t *>(a.X), s.r, s.most, first, T * K, K, s.x);
+        });
+        if (e != hipSuccess) return e;
+    }
+    const int64_t width = piece_width(T, V, 2);
+    a.pitch = width;
+    for (int64_t v0 = 0; v0 < V; v0 += width) {
+        const int64_t n = std::min(width, V - v0);
+        a.v0 = v0;
+        a.tiles_v = (int)cdiv(n, kCeTile);
+        e = in_runs(cdiv(T, kCeTile), a.tiles_v, [&](int64_t first, int64_t count) {
+            a.t0 = first * kCeTile;
+            launch_ce_grad_mfma(a, count * kCeTile, flag, st);
+        });
+        if (e != hipSuccess) return e;
+        const char *const W = static_cast<const char *>(a.W) + (size_t)v0 * (size_t)K * 2;
+        if (dX) {
+            const DxPlan p = plan_dx(kBF16, T, (n + 15) / 16 * 16, K);
+            e = launch_dx_sums(s.D, W, T, n, width, K, p.chunk, p.splits, s.part, st);
+            if (e != hipSuccess) return e;
+            const bool last = v0 + n == V;
+            e = in_elements(T * K, [&](int64_t first, unsigned grid) {
+                ce_sums_kernel<<<grid, 256, 0, st>>>(s.part, p.splits, v0 ? s.sums : nullptr, s.r, 1, first, T * K, K,
+                                                     last ? nullptr : s.sums, dX, kBF16);
+            });
+            if (e != hipSuccess) return e;
+        }
+        if (dW) {
+            char *const out = static_cast<char *>(dW) + (size_t)v0 * (size_t)K * (dw_dtype == kBF16 ? 2 : 4);
+            const Splits p = dw_splits(T, n, K);
+            e = launch_dw_mfma(s.D, s.x, T, n, width, K, p.chunk, p.count, s.most, out, dw_dtype, s.part, st);
+            if (e != hipSuccess) return e;
+            if (p.count > 1)
+                e = in_elements(n * K, [&](int64_t first, unsigned grid) {
+                    ce_sums_kernel<<<grid, 256, 0, st>>>(s.part, p.count, nullptr, s.most, 0, first, n * K, K, nullptr, out, dw_dtype);
+                });
+            if (e != hipSuccess) return e;
+        }
+    }
+    return hipSuccess;
 }
 
 }  // namespace
@@ -244,9 +421,8 @@ size_t linear_ce_fwd_ws(int64_t T, int64_t V) {
 
 size_t linear_ce_bwd_ws(int64_t T, int64_t V, int64_t K) {
     if (T == 0) return kWsHeader;
-    // D's piece for T tokens, or for fewer, whose pieces may be up to the limit
-    const size_t most = std::max<size_t>((size_t)T * 256 * sizeof(float), std::min<size_t>((size_t)T * (size_t)(cdiv(V, 256) * 256) * sizeof(float), kPieceBytes));
-    return kWsHeader + round256((size_t)T * (size_t)K * sizeof(float)) + most;
+    const size_t simple = kWsHeader + round256((size_t)T * (size_t)K * sizeof(float)) + piece_bytes(T, V, sizeof(float));
+    return std::max(simple, mfma_space(T, V, K, nullptr, nullptr));
 }
 
 hipError_t launch_linear_ce_fwd(int dtype, const void *X, const void *W, int64_t T, int64_t V, int64_t K, const int64_t *target,
@@ -256,12 +432,21 @@ hipError_t launch_linear_ce_fwd(int dtype, const void *X, const void *W, int64_t
     a.X = X, a.W = W, a.target = target, a.lse = lse, a.logp = logp, a.T = T, a.V = V, a.K = K;
     a.zt = reinterpret_cast<float *>(base);
     a.part = reinterpret_cast<float2 *>(base + round256((size_t)T * sizeof(float)));
-    a.tiles_v = (int)cdiv(V, kTileV);
-    hipError_t e = in_runs(cdiv(T, kTileT), a.tiles_v, [&](int64_t first, int64_t count) {
-        a.t0 = first * kTileT;
-        if (dtype == kBF16) ce_stats_kernel<kBF16><<<(unsigned)(count * a.tiles_v), 256, 0, st>>>(a);
-        else ce_stats_kernel<kF32><<<(unsigned)(count * a.tiles_v), 256, 0, st>>>(a);
-    });
+    const bool mfma = on_mfma(dtype, K), few = mfma && T <= kCeFew;
+    const int64_t rows = mfma ? kCeTile : kTileT;
+    a.tiles_v = (int)cdiv(V, few ? kCeFewV : mfma ? kCeTile : kTileV);
+    hipError_t e = hipSuccess;
+    if (few) {
+        launch_ce_stats_few(a, st);
+        e = hipGetLastError();
+    } else {
+        e = in_runs(cdiv(T, rows), a.tiles_v, [&](int64_t first, int64_t count) {
+            a.t0 = first * rows;
+            if (mfma) launch_ce_stats_mfma(a, count * rows, st);
+            else if (dtype == kBF16) ce_stats_kernel<kBF16><<<(unsigned)(count * a.tiles_v), 256, 0, st>>>(a);
+            else ce_stats_kernel<kF32><<<(unsigned)(count * a.tiles_v), 256, 0, st>>>(a);
+        });
+    }
     if (e != hipSuccess) return e;
     const int per = T >= 4096 ? 8 : 64;
     ce_join_kernel<<<(unsigned)cdiv(T * per, 256), 256, 0, st>>>(a, a.tiles_v, per, flag);
@@ -275,8 +460,9 @@ hipError_t launch_linear_ce_bwd(int dtype, const void *X, const void *W, int64_t
     float *const sums = reinterpret_cast<float *>(base);
     CeArgs a{};
     a.X = X, a.W = W, a.target = target, a.lse = const_cast<float *>(lse), a.g = g, a.h = h, a.T = T, a.V = V, a.K = K;
-    a.D = reinterpret_cast<float *>(base + round256((size_t)T * (size_t)K * sizeof(float)));
-    const int64_t width = piece(T, V);
+    if (on_mfma(dtype, K)) return bwd_mfma(a, dX, dW, dw_dtype, flag, static_cast<char *>(ws), st);
+    a.D = base + round256((size_t)T * (size_t)K * sizeof(float));
+    const int64_t width = piece_width(T, V, sizeof(float));
     const size_t esz = dtype == kBF16 ? 2 : 4, dsz = dw_dtype == kBF16 ? 2 : 4;
     for (int64_t v0 = 0; v0 < V; v0 += width) {
         const int64_t n = std::min(width, V - v0);
@@ -291,7 +477,7 @@ hipError_t launch_linear_ce_bwd(int dtype, const void *X, const void *W, int64_t
         const bool last = v0 + n == V;
         if (dX) {
             CeProduct p{};
-            p.A = a.D, p.am = n, p.ar = 1, p.M = T, p.N = K, p.R = n, p.b_dtype = dtype, p.out_dtype = dtype;
+            p.A = static_cast<const float *>(a.D), p.am = n, p.ar = 1, p.M = T, p.N = K, p.R = n, p.b_dtype = dtype, p.out_dtype = dtype;
             p.B = static_cast<const char *>(W) + (size_t)v0 * (size_t)K * esz;
             p.before = v0 ? sums : nullptr;
             p.sums = last ? nullptr : sums;
@@ -301,7 +487,7 @@ hipError_t launch_linear_ce_bwd(int dtype, const void *X, const void *W, int64_t
         }
         if (dW) {
             CeProduct p{};
-            p.A = a.D, p.am = 1, p.ar = n, p.M = n, p.N = K, p.R = T, p.b_dtype = dtype, p.out_dtype = dw_dtype;
+            p.A = static_cast<const float *>(a.D), p.am = 1, p.ar = n, p.M = n, p.N = K, p.R = T, p.b_dtype = dtype, p.out_dtype = dw_dtype;
             p.B = X;
             p.out = static_cast<char *>(dW) + (size_t)v0 * (size_t)K * dsz;
             e = product(p, st);

@@ -1,0 +1,294 @@
+// Logit tiles of the linear cross entropy on the bf16 matrix instructions (v_mfma_f32_32x32x16_bf16, fp32 sums).
+//
+// A workgroup of four waves forms 256 vocabulary entries x 256 tokens of W X^T, so that a lane holds one token's logits: rows =
+// vocabulary, columns = tokens. The maximum and the sum of exponentials over the tile's vocabulary are then sums over a lane's
+// registers, its partner's and another wave's, and no logit leaves the chip (forward); or the tile turns into that of D (backward),
+// which goes to memory in bf16, through LDS. Operands are K-contiguous and go straight into a ring of LDS stages, several steps ahead
+// of the matrix instructions, as in the reconstruction GEMM's forward.
+//
+// Up to 32 tokens the products are too few to hide the weights' way from memory, 2 K bytes per logit row: waves read 32 vocabulary
+// rows each straight into the matrix instructions' registers.
+#include "linear_ce.h"
+#include "mfma_common.h"
+#include "ops_device.h"
+
+namespace focus {
+
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kStages = 5;
+constexpr int kStep = 32;              // k per step
+constexpr int kOpBytes = kCeTile * 64; // 256 rows x 32 bf16
+constexpr int kStageBytes = 2 * kOpBytes;
+constexpr int kLoads = 8;              // loads per thread and stage
+constexpr float kLog2e = 1.44269504088896341f;
+
+// e^(z - m) = 2^(z log2e - c) 2^-r with c = fl(m log2e) and r what that rounding lost: one operation per exponent, and no digit lost
+// to the size of m
+struct Exponent {
+    float c, factor;
+    __device__ __forceinline__ explicit Exponent(float m) {
+        c = m * kLog2e;
+        factor = exp2_raw(-__builtin_fmaf(m, kLog2e, -c));
+    }
+    __device__ __forceinline__ float operator()(float z) const { return exp2_raw(__builtin_fmaf(z, kLog2e, -c)); }
+};
+
+struct TileFrags {
+    bf16x8_t a[4], b[4];
+};
+
+// acc[i][j][r] = logit of vocabulary entry v0 + 128 wm + 32 i + 8 (r / 4) + 4 (lane / 32) + r % 4 and token t0 + 128 wn + 32 j +
+// lane % 32; entries past V and tokens past T have rows of zeros. All LDS may be used again afterwards.
+__device__ __forceinline__ void logits_tile(const CeArgs &a, int64_t v0, int64_t t0, char *smem, f32x16_t (&acc)[4][4]) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wm = wave >> 1, wn = wave & 1;
+    const int lr = lane & 31, lh = lane >> 5;
+    const f32x16_t zero = {};
+#pragma unroll
+    for (int i = 0; i < 4; i++)
+#pragma unroll
+        for (int j = 0; j < 4; j++) acc[i][j] = zero;
+    lds_char *const lsm = (lds_char *)smem;
+    const int wave_u = __builtin_amdgcn_readfirstlane(wave);
+    const int64_t pitch = a.K * 2;
+    FwdDma<> dma;
+    dma.init(pitch, wave_u, lane);
+    const __amdgpu_buffer_rsrc_t ra = make_rsrc(static_cast<const char *>(a.W) + v0 * pitch, (a.V - v0) * pitch);
+    const __amdgpu_buffer_rsrc_t rb = make_rsrc(static_cast<const char *>(a.X) + t0 * pitch, (a.T - t0) * pitch);
+    const int64_t nk = (a.K + kStep - 1) / kStep;
+    // Load i of step j into its stage: 0-3 rows of W, 4-7 rows of X. Past the rows' end a load brings zeros without going to
+    // memory, so that every step is the same number of loads, which is what the waits count.
+    auto issue = [&](int64_t j, int stage, int i) {
+        const uint32_t base = (uint32_t)j * 64u, bad = dma.step_bad(pitch, base);
+        lds_char *const st = lsm + stage * kStageBytes;
+        if (i < 4) dma.issue_one(ra, base, bad, st, wave_u, i);
+        else dma.issue_one(rb, base, bad, st + kOpBytes, wave_u, i - 4);
+    };
+#pragma unroll
+    for (int s = 0; s < kStages - 1; s++)
+#pragma unroll
+        for (int i = 0; i < kLoads; i++) issue(s, s, i);
+    auto frags = [&](TileFrags &f, const char *st, int ks) {
+#pragma unroll
+        for (int i = 0; i < 4; i++) {
+            f.a[i] = *reinterpret_cast<const bf16x8_t *>(st + fwd_off(wm * 128 + i * 32 + lr, ks * 2 + lh));
+            f.b[i] = *reinterpret_cast<const bf16x8_t *>(st + kOpBytes + fwd_off(wn * 128 + i * 32 + lr, ks * 2 + lh));
+        }
+    };
+    // Before the barrier of step kt this thread's loads of steps up to kt + 1 have landed, after it everyone's have: the fragments
+    // of step kt + 1 are read while step kt is multiplied, in three sets that rotate, and stage (kt - 1) % 5, last read in step
+    // kt - 2, takes step kt + 4.
+    FOCUS_WAIT_VMCNT(kLoads * (kStages - 3));
+    asm volatile("s_barrier" ::: "memory");
+    TileFrags f, g, h;
+    frags(f, smem, 0);
+    frags(g, smem, 1);
+    int sc = 0;  // kt % kStages
+    auto step = [&](int64_t kt, TileFrags &P, TileFrags &Q, TileFrags &R) {
+        FOCUS_WAIT_VMCNT(kLoads * (kStages - 3));
+        asm volatile("s_barrier" ::: "memory");
+        const int next = sc == kStages - 1 ? 0 : sc + 1, free = sc == 0 ? kStages - 1 : sc - 1;
+        const char *const st = smem + next * kStageBytes;
+        // one load after every fourth matrix instruction: closer together they fill the load queue, on which a wave then waits
+        auto issue_at = [&](int i) {
+            __builtin_amdgcn_sched_barrier(0);
+            issue(kt + kStages - 1, free, i);
+            __builtin_amdgcn_sched_barrier(0);
+        };
+        frags(R, st, 0);
+        static_for<16>([&](auto idx) {
+            constexpr int i = idx / 4, jj = idx % 4;
+            acc[i][jj] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(P.a[i], P.b[jj], acc[i][jj], 0, 0, 0);
+            if constexpr (idx % 4 == 1) issue_at(idx / 4);
+        });
+        frags(P, st, 1);
+        static_for<16>([&](auto idx) {
+            constexpr int i = idx / 4, jj = idx % 4;
+            acc[i][jj] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(Q.a[i], Q.b[jj], acc[i][jj], 0, 0, 0);
+            if constexpr (idx % 4 == 1) issue_at(4 + idx / 4);
+        });
+        sc = next;
+    };
+    int64_t kt = 0;
+    for (; kt + 3 <= nk; kt += 3) {
+        step(kt, f, g, h);
+        step(kt + 1, h, f, g);
+        step(kt + 2, g, h, f);
+    }
+    if (kt < nk) step(kt, f, g, h);
+    if (kt + 1 < nk) step(kt + 1, h, f, g);
+    FOCUS_WAIT_VMCNT(0);  // the loads past the end write zeros
+    __syncthreads();
+}
+
+// Whether any lane's target lies in the 128 entries from v0 on, and its place there
+__device__ __forceinline__ bool target_near(int64_t want, int64_t v0, int &at) {
+    const int64_t d = want - v0;
+    const bool here = d >= 0 && d < 128;
+    at = here ? (int)d : -1;
+    return __any(here);
+}
+
+}  // namespace
+
+// Maximum and sum of exponentials of every token of the tile over its 256 vocabulary entries, and the logit of a target there.
+__global__ void __launch_bounds__(kThreads, 1) ce_stats_mfma_kernel(CeArgs a) {
+    __shared__ __attribute__((aligned(16))) char smem[kStages * kStageBytes];
+    uint32_t tv, tt;
+    grouped_tile(xcd_tile(blockIdx.x, gridDim.x), (uint32_t)a.tiles_v, gridDim.x / (uint32_t)a.tiles_v, tv, tt);
+    const int64_t v0 = (int64_t)tv * kCeTile, t0 = a.t0 + (int64_t)tt * kCeTile;
+    f32x16_t acc[4][4];
+    logits_tile(a, v0, t0, smem, acc);
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wm = wave >> 1, wn = wave & 1, lr = lane & 31, lh = lane >> 5;
+    if (v0 + kCeTile > a.V) {  // entries that do not exist
+        static_for<16>([&](auto ij) {
+            static_for<16>([&](auto r) {
+                const int64_t v = v0 + 128 * wm + 32 * (ij / 4) + 8 * (r / 4) + 4 * lh + r % 4;
+                if (v >= a.V) acc[ij / 4][ij % 4][(int)r] = -__builtin_inff();
+            });
+        });
+    }
+    float2 *const red = reinterpret_cast<float2 *>(smem);  // [2 waves along the vocabulary][256 tokens]
+    static_for<4>([&](auto j) {
+        const int64_t t = t0 + 128 * wn + 32 * j + lr;
+        int at;
+        if (target_near(a.target && t < a.T ? a.target[t] : -1, v0 + 128 * wm, at)) {
+            static_for<4>([&](auto i) {
+                static_for<16>([&](auto r) {
+                    if (at == 32 * i + 8 * (r / 4) + 4 * lh + r % 4) a.zt[t] = acc[i][j][(int)r];
+                });
+            });
+        }
+        float m = -__builtin_inff();
+        static_for<4>([&](auto i) { static_for<16>([&](auto r) { m = fmaxf(m, acc[i][j][(int)r]); }); });
+        m = fmaxf(m, __shfl_xor(m, 32, 64));
+        const Exponent e(m);
+        float s[4] = {0.0f, 0.0f, 0.0f, 0.0f};  // a NaN stays one
+        static_for<4>([&](auto i) { static_for<16>([&](auto r) { s[r % 4] += e(acc[i][j][(int)r]); }); });
+        float sum = ((s[0] + s[1]) + (s[2] + s[3])) * e.factor;
+        if (m == -__builtin_inff()) {  // no entry here exists, or none is a number
+            sum = 0.0f;
+            static_for<4>([&](auto i) {
+                static_for<16>([&](auto r) { sum += acc[i][j][(int)r] == m ? 0.0f : __builtin_nanf(""); });
+            });
+        }
+        sum += __shfl_xor(sum, 32, 64);
+        if (lh == 0) red[wm * kCeTile + 128 * wn + 32 * j + lr] = make_float2(m, sum);
+    });
+    __syncthreads();
+    const int64_t t = t0 + threadIdx.x;
+    if (t >= a.T) return;
+    const float2 x = red[threadIdx.x], y = red[kCeTile + threadIdx.x];
+    const float m = fmaxf(x.x, y.x);
+    a.part[(int64_t)tv * a.T + t] = make_float2(m, (x.x == m ? x.y : x.y * expf(x.x - m)) + (y.x == m ? y.y : y.y * expf(y.x - m)));
+}
+
+// The tile of D: D[t][v] = (h - g) p + g [v == target] relative to the token's scale, p = exp(z - lse), rounded to bf16. Relative to
+// the scale, a target's entry is 1 - p, whose rounding does not depend on g: the weights of a mean, 1 / n, would otherwise round
+// every token's largest term alike, by up to 2^-8 of the whole gradient. Entries past V are zeros.
+__global__ void __launch_bounds__(kThreads, 1) ce_grad_mfma_kernel(CeArgs a, uint32_t *flag) {
+    __shared__ __attribute__((aligned(16))) char smem[kStages * kStageBytes];
+    uint32_t tv, tt;
+    grouped_tile(xcd_tile(blockIdx.x, gridDim.x), (uint32_t)a.tiles_v, gridDim.x / (uint32_t)a.tiles_v, tv, tt);
+    const int64_t c0 = (int64_t)tv * kCeTile, v0 = a.v0 + c0, t0 = a.t0 + (int64_t)tt * kCeTile;
+    f32x16_t acc[4][4];
+    logits_tile(a, v0, t0, smem, acc);
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wm = wave >> 1, wn = wave & 1, lr = lane & 31, lh = lane >> 5;
+    bool bad = false;
+    static_for<4>([&](auto j) {
+        const int64_t t = t0 + 128 * wn + 32 * j + lr;
+        const bool real = t < a.T;
+        const int64_t want = a.target && real ? a.target[t] : -1;
+        const float g = a.g && want >= 0 && want < a.V ? a.g[t] : 0.0f, h = a.h && real ? a.h[t] : 0.0f;
+        const float lse = real ? a.lse[t] : 0.0f, scale = real ? a.scale[t] : 0.0f;
+        bad = bad || want >= a.V || ((g != 0.0f || h != 0.0f) && !(__builtin_fabsf(lse) <= 65536.0f));
+        const float inv = scale > 0.0f ? 1.0f / scale : 0.0f;
+        const Exponent e(lse);
+        const float by = (h - g) * inv * e.factor, hit = g * inv;
+        static_for<4>([&](auto i) { static_for<16>([&](auto r) { acc[i][j][(int)r] = by * e(acc[i][j][(int)r]); }); });
+        int at;
+        if (target_near(want, v0 + 128 * wm, at)) {
+            static_for<4>([&](auto i) {
+                static_for<16>([&](auto r) {
+                    if (at == 32 * i + 8 * (r / 4) + 4 * lh + r % 4) acc[i][j][(int)r] += hit;
+                });
+            });
+        }
+    });
+    if (v0 + kCeTile > a.V) {
+        static_for<16>([&](auto ij) {
+            static_for<16>([&](auto r) {
+                const int64_t v = v0 + 128 * wm + 32 * (ij / 4) + 8 * (r / 4) + 4 * lh + r % 4;
+                if (v >= a.V) acc[ij / 4][ij % 4][(int)r] = 0.0f;
+            });
+        });
+    }
+    // (a scale of infinity or NaN, as a NaN logit, goes through to the gradients)
+    store_tile_bf16(acc, smem, static_cast<uint16_t *>(a.D) + t0 * a.pitch, a.T - t0, a.pitch, (uint32_t)c0);
+    if (bad) raise_domain_flag(flag);
+}
+
+// Up to 32 tokens: a wave takes 32 vocabulary entries, whose rows it reads straight into the operand registers, 16 bytes of each row
+// per lane pair and load, kAhead of them under way; the tokens' rows come from the caches. Bound by the weights' way from memory.
+// The reduction index is the same in both operands, in their order.
+constexpr int kAhead = 8;
+__global__ void __launch_bounds__(kThreads) ce_stats_few_kernel(CeArgs a) {
+    __shared__ float2 red[4][kCeFew];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, lr = lane & 31, lh = lane >> 5;
+    const int64_t v0 = (int64_t)blockIdx.x * kCeFewV + wave * 32;
+    const uint32_t pitch = (uint32_t)a.K * 2u;
+    const __amdgpu_buffer_rsrc_t rw = make_rsrc(static_cast<const char *>(a.W) + v0 * pitch, (a.V - v0) * (int64_t)pitch);
+    const __amdgpu_buffer_rsrc_t rx = make_rsrc(a.X, a.T * (int64_t)pitch);
+    const uint32_t off = (uint32_t)lr * pitch + (uint32_t)lh * 16u;
+    auto load = [&](__amdgpu_buffer_rsrc_t rs, uint32_t k) {  // k: bytes; past the row's end zeros
+        const uint32_t past = (uint32_t)(k + lh * 16u >= pitch) << 31;
+        return __builtin_bit_cast(bf16x8_t, __builtin_amdgcn_raw_buffer_load_b128(rs, (int)((off + k) | past), 0, 0));
+    };
+    f32x16_t acc = {};
+    bf16x8_t w[kAhead], x[kAhead];
+#pragma unroll
+    for (int i = 0; i < kAhead; i++) w[i] = load(rw, 32u * i), x[i] = load(rx, 32u * i);
+    for (uint32_t k = 0; k < pitch; k += 32u * kAhead) {
+#pragma unroll
+        for (int i = 0; i < kAhead; i++) {
+            acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(w[i], x[i], acc, 0, 0, 0);
+            w[i] = load(rw, k + 32u * (kAhead + i)), x[i] = load(rx, k + 32u * (kAhead + i));
+        }
+    }
+    // lane: token lr, entries v0 + 8 (r / 4) + 4 lh + r % 4
+    const int64_t want = a.target && lr < a.T ? a.target[lr] : -1;
+    float m = -__builtin_inff(), sum = 0.0f;
+    static_for<16>([&](auto r) {
+        const int64_t v = v0 + 8 * (r / 4) + 4 * lh + r % 4;
+        if (v >= a.V) acc[(int)r] = -__builtin_inff();
+        else if (v == want) a.zt[lr] = acc[(int)r];
+        m = fmaxf(m, acc[(int)r]);
+    });
+    m = fmaxf(m, __shfl_xor(m, 32, 64));
+    static_for<16>([&](auto r) { sum += acc[(int)r] == -__builtin_inff() ? 0.0f : expf(acc[(int)r] - m); });
+    sum += __shfl_xor(sum, 32, 64);
+    if (lh == 0) red[wave][lr] = make_float2(m, sum);
+    __syncthreads();
+    const int t = threadIdx.x;
+    if (t >= kCeFew || t >= a.T) return;
+    m = fmaxf(fmaxf(red[0][t].x, red[1][t].x), fmaxf(red[2][t].x, red[3][t].x));
+    sum = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 4; i++) sum += red[i][t].x == m ? red[i][t].y : red[i][t].y * expf(red[i][t].x - m);
+    a.part[(int64_t)blockIdx.x * a.T + t] = make_float2(m, sum);
+}
+
+void launch_ce_stats_mfma(const CeArgs &a, int64_t tokens, hipStream_t st) {
+    const unsigned tiles_t = (unsigned)((tokens + kCeTile - 1) / kCeTile);
+    ce_stats_mfma_kernel<<<tiles_t * (unsigned)a.tiles_v, kThreads, 0, st>>>(a);
+}
+
+void launch_ce_grad_mfma(const CeArgs &a, int64_t tokens, uint32_t *flag, hipStream_t st) {
+    const unsigned tiles_t = (unsigned)((tokens + kCeTile - 1) / kCeTile);
+    ce_grad_mfma_kernel<<<tiles_t * (unsigned)a.tiles_v, kThreads, 0, st>>>(a, flag);
+}
+
+void launch_ce_stats_few(const CeArgs &a, hipStream_t st) { ce_stats_few_kernel<<<(unsigned)a.tiles_v, kThreads, 0, st>>>(a); }
+
+}  // namespace focus
