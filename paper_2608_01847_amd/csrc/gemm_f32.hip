@@ -16,6 +16,7 @@
 #include <type_traits>
 
 #include "gemm_common.h"
+#include "linear_ce.h"
 
 namespace focus {
 
@@ -70,24 +71,32 @@ __device__ __forceinline__ F32Cols read_cols_f32(uint32_t a, uint32_t b) {
 //            gradient's largest error comes from the outputs with one very large term, at whose size every
 //            later addition rounds: with one accumulator and fp32 sums 1.4e-5 of the gradients' root mean
 //            square (128 x 256 x 256, NVFP4, Student-t activations), 2.4e-6 so (5.9 us for 5.4).
-template <bool MSE, int T>
-__global__ void __launch_bounds__(256)
-fwd_f32_kernel(const float *__restrict__ X, const float *__restrict__ W, int64_t M, int64_t N, int64_t K,
-               const float *__restrict__ Yref, float *__restrict__ dY, float dscale, double *__restrict__ colpart,
-               int tiles_n) {
+constexpr int f32_fwd_lds(int T) { return T == 32 ? 4 * 4 * 2 * T * 64 : 3 * 4 * T * 64; }  // bytes
+template <int T>
+struct F32Tile {
+    static constexpr int R = T == 32 ? 4 : 16;  // registers of the tile that a wave's lanes hold after the products
+    typename std::conditional<T == 32, double, float>::type o[R];
+    // row (of the tile) of register r, and column, of this lane
+    __device__ __forceinline__ static int row(int r) {
+        const int wave = threadIdx.x >> 6, lh = (threadIdx.x & 63) >> 5;
+        return T == 32 ? 8 * wave + r + 4 * lh : (wave >> 1) * 32 + 8 * (r / 4) + r % 4 + 4 * lh;
+    }
+    __device__ __forceinline__ static int col() { return (T == 32 ? 0 : (threadIdx.x >> 6 & 1) * 32) + (threadIdx.x & 31); }
+};
+
+template <int T>
+__device__ __forceinline__ void f32_products(const float *__restrict__ X, const float *__restrict__ W, int64_t M, int64_t N, int64_t K,
+                                             int64_t m0, int64_t n0, char *smem, F32Tile<T> &tile) {
+    auto &o = tile.o;
     constexpr bool kSplit = T == 32;
     constexpr int S = kSplit ? 4 : 3;                     // stages
     constexpr int kSub = T * 64;                          // bytes of one 16-k tile of an operand
     constexpr int kStage = kSplit ? 2 * kSub : 4 * kSub;  // X then W, 16 k or 2 x 16 k each
     constexpr int kLoads = 4;                             // loads per stage per thread
-    __shared__ __attribute__((aligned(16))) char smem[kSplit ? 4 * S * kStage : S * kStage];
-    __shared__ double red[4][32];
+    static_assert((kSplit ? 4 : 1) * S * kStage == f32_fwd_lds(T), "the workgroup's LDS");
     const int t = threadIdx.x, lane = t & 63, wave = t >> 6, wm = kSplit ? 0 : wave >> 1, wn = kSplit ? 0 : wave & 1;
     const int lr = lane & 31, lh = lane >> 5;
     const int wave_u = __builtin_amdgcn_readfirstlane(wave);
-    const uint32_t tile = xcd_tile(blockIdx.x, gridDim.x);
-    const int64_t tm = tile / (uint32_t)tiles_n, tn = tile % (uint32_t)tiles_n;
-    const int64_t m0 = tm * T, n0 = tn * T;
     const int64_t pitch = K * 4;
     const __amdgpu_buffer_rsrc_t rx = make_rsrc(X + m0 * K, (M - m0) * pitch);
     const __amdgpu_buffer_rsrc_t rw = make_rsrc(W + n0 * K, (N - n0) * pitch);
@@ -149,8 +158,6 @@ fwd_f32_kernel(const float *__restrict__ X, const float *__restrict__ W, int64_t
     FOCUS_WAIT_VMCNT(0);
     __syncthreads();
     // ---- epilogue: this wave's registers r0 .. r0 + R - 1 of the tile's accumulator ----
-    constexpr int R = kSplit ? 4 : 16;
-    typename std::conditional<kSplit, double, float>::type o[R];
     if constexpr (kSplit) {
         double *part = reinterpret_cast<double *>(smem);  // [wave][register][lane]
 #pragma unroll
@@ -168,6 +175,25 @@ fwd_f32_kernel(const float *__restrict__ X, const float *__restrict__ W, int64_t
 #pragma unroll
         for (int r = 0; r < 16; r++) o[r] = acc[0][r];
     }
+}
+
+template <bool MSE, int T>
+__global__ void __launch_bounds__(256)
+fwd_f32_kernel(const float *__restrict__ X, const float *__restrict__ W, int64_t M, int64_t N, int64_t K,
+               const float *__restrict__ Yref, float *__restrict__ dY, float dscale, double *__restrict__ colpart,
+               int tiles_n) {
+    constexpr bool kSplit = T == 32;
+    constexpr int R = F32Tile<T>::R;
+    __shared__ __attribute__((aligned(16))) char smem[f32_fwd_lds(T)];
+    __shared__ double red[4][32];
+    const int t = threadIdx.x, lane = t & 63, wave = t >> 6, wm = kSplit ? 0 : wave >> 1, wn = kSplit ? 0 : wave & 1;
+    const int lr = lane & 31, lh = lane >> 5;
+    const uint32_t id = xcd_tile(blockIdx.x, gridDim.x);
+    const int64_t tm = id / (uint32_t)tiles_n, tn = id % (uint32_t)tiles_n;
+    const int64_t m0 = tm * T, n0 = tn * T;
+    F32Tile<T> tile;
+    f32_products<T>(X, W, M, N, K, m0, n0, smem, tile);
+    auto &o = tile.o;
     const int64_t n = n0 + wn * 32 + lr;
     const bool n_ok = n < N;
     double csum = 0.0;
@@ -214,6 +240,7 @@ fwd_f32_kernel(const float *__restrict__ X, const float *__restrict__ W, int64_t
 // error against 64 bits was up to 4.4 times that of many short splits (3,507 x 1,758 x 160: 3.1e-7 for 7.0e-8; now
 // 6.4e-8). The additions run beside the next chain's matrix instructions (3,507 x 1,758 x 160 36.9 us for 37.5,
 // 4,096 x 2,048 x 2,048 316 for 306); chains of 32 tokens took 41 and 347, of 128 left some errors above.
+constexpr int kPlain = 2;  // in place of the format: dY^T X, split by split to G_out
 template <int FMT, int WDT, bool W16>
 __global__ void __launch_bounds__(256)
 bwd_f32_kernel(const float *__restrict__ dY, const float *__restrict__ X, int64_t M, int64_t N, int64_t K, int64_t chunk,
@@ -315,6 +342,14 @@ bwd_f32_kernel(const float *__restrict__ dY, const float *__restrict__ X, int64_
     }
     FOCUS_WAIT_VMCNT(0);  // the empty slots' zero writes
     __syncthreads();
+    if constexpr (FMT == kPlain) {  // the sums themselves
+#pragma unroll
+        for (int r = 0; r < 16; r++) {
+            const int64_t n = n0 + wm * 32 + 8 * (r / 4) + 4 * lh + r % 4, k = k0 + wn * 32 + lr;
+            if (n < N && k < K) G_out[(split * N + n) * K + k] = (float)gsum[r];
+        }
+        return;
+    }
     // ---- G to LDS, then pieces of 8 consecutive k of one row per thread (see ste_piece) ----
     constexpr int kPitch = T + 4;
     float *const Gs = reinterpret_cast<float *>(smem);  // [64][68]
@@ -322,7 +357,7 @@ bwd_f32_kernel(const float *__restrict__ dY, const float *__restrict__ X, int64_
     for (int r = 0; r < 16; r++)
         Gs[(wm * 32 + 8 * (r / 4) + 4 * lh + r % 4) * kPitch + wn * 32 + lr] = (float)gsum[r];
     __syncthreads();
-    constexpr int B = block_of(FMT);
+    constexpr int B = FMT == kPlain ? 32 : block_of(FMT);
     const float alpha = FMT == kFmtNV ? *alpha_ptr : 1.0f;
     const int64_t nb = K / B, ns = K >> sb_log2;
     bool bad = false;
@@ -425,6 +460,109 @@ hipError_t launch_bwd_f32(int fmt, int w_dt, const float *dY, const float *X, in
     else { if (w_dt == kBF16) { BF_V(kFmtNV, kBF16); } else { BF_V(kFmtNV, kF32); } }
 #undef BF_V
 #undef BF
+    return hipGetLastError();
+}
+
+// ---- logit tiles of the linear cross entropy: rows = vocabulary, columns = tokens, so that a lane holds one token's logits ----
+namespace {
+
+// Maximum and sum of exponentials of each token over the tile's vocabulary, and the logit of a target there
+template <int T>
+__global__ void __launch_bounds__(256) ce_stats_f32_kernel(CeArgs a) {
+    __shared__ __attribute__((aligned(16))) char smem[f32_fwd_lds(T)];
+    constexpr int kWaves = T == 32 ? 4 : 2;  // that share a token
+    __shared__ float2 red[kWaves][T];
+    const uint32_t id = xcd_tile(blockIdx.x, gridDim.x), tiles_t = gridDim.x / (uint32_t)a.tiles_v;
+    const int64_t tv = id / tiles_t, v0 = tv * T, t0 = a.t0 + (int64_t)(id % tiles_t) * T;
+    F32Tile<T> tile;
+    f32_products<T>(static_cast<const float *>(a.W), static_cast<const float *>(a.X), a.V, a.T, a.K, v0, t0, smem, tile);
+    const int64_t t = t0 + tile.col();
+    const int64_t want = a.target && t < a.T ? a.target[t] : -1;
+    const float kNone = -__builtin_inff();
+    float z[F32Tile<T>::R], m = kNone, s = 0.0f;
+#pragma unroll
+    for (int r = 0; r < F32Tile<T>::R; r++) {
+        const int64_t v = v0 + tile.row(r);
+        z[r] = v < a.V ? (float)tile.o[r] : kNone;
+        if (v == want && v < a.V) a.zt[t] = z[r];
+        m = fmaxf(m, z[r]);
+    }
+    m = fmaxf(m, __shfl_xor(m, 32, 64));
+#pragma unroll
+    for (int r = 0; r < F32Tile<T>::R; r++) s += z[r] == kNone ? 0.0f : expf(z[r] - m);  // a NaN stays one
+    s += __shfl_xor(s, 32, 64);
+    const int wave = threadIdx.x >> 6;
+    if ((threadIdx.x & 32) == 0) red[T == 32 ? wave : wave >> 1][tile.col()] = make_float2(m, s);
+    __syncthreads();
+    if (threadIdx.x >= T || t0 + threadIdx.x >= a.T) return;
+    m = kNone, s = 0.0f;
+#pragma unroll
+    for (int w = 0; w < kWaves; w++) m = fmaxf(m, red[w][threadIdx.x].x);
+#pragma unroll
+    for (int w = 0; w < kWaves; w++) {
+        const float2 p = red[w][threadIdx.x];
+        s += p.x == m ? p.y : p.y * expf(p.x - m);
+    }
+    a.part[tv * a.T + t0 + threadIdx.x] = make_float2(m, s);
+}
+
+// D of the piece, [T][pitch] for dW and transposed, [pitch][T], for dX: each product reads its operand along the reduction
+template <int T>
+__global__ void __launch_bounds__(256) ce_grad_f32_kernel(CeArgs a, float *__restrict__ Dt, uint32_t *flag) {
+    __shared__ __attribute__((aligned(16))) char smem[f32_fwd_lds(T)];
+    const uint32_t id = xcd_tile(blockIdx.x, gridDim.x), tiles_t = gridDim.x / (uint32_t)a.tiles_v;
+    const int64_t c0 = (int64_t)(id / tiles_t) * T, v0 = a.v0 + c0, t0 = a.t0 + (int64_t)(id % tiles_t) * T;
+    F32Tile<T> tile;
+    f32_products<T>(static_cast<const float *>(a.W), static_cast<const float *>(a.X), a.V, a.T, a.K, v0, t0, smem, tile);
+    const int64_t t = t0 + tile.col();
+    if (t >= a.T) return;
+    const int64_t want = a.target ? a.target[t] : -1;
+    const float g = a.g && want >= 0 && want < a.V ? a.g[t] : 0.0f, h = a.h ? a.h[t] : 0.0f, lse = a.lse[t];
+    if (want >= a.V || ((g != 0.0f || h != 0.0f) && !(__builtin_fabsf(lse) <= 65536.0f))) raise_domain_flag(flag);
+    float *const D = static_cast<float *>(a.D);
+#pragma unroll
+    for (int r = 0; r < F32Tile<T>::R; r++) {
+        const int64_t c = c0 + tile.row(r), v = a.v0 + c;
+        if (c >= a.pitch) continue;
+        const float d = (v == want ? g : 0.0f) + (h - g) * expf((float)tile.o[r] - lse);
+        D[t * a.pitch + c] = d;
+        Dt[c * a.T + t] = d;
+    }
+}
+
+}  // namespace
+
+bool ce_f32_supported(int64_t T, int64_t V, int64_t K) {
+    return f32_fwd_supported(V, T, K) && f32_bwd_supported(T, std::min(V, kCeMostWidth), K) && f32_bwd_supported(V, T, K);
+}
+
+// Edge of a logit tile, as the forward chooses it: 64 x 64 where they give every CU one
+int64_t ce_f32_tile(int64_t T, int64_t n) {
+    return ((n + 63) / 64) * ((T + 63) / 64) < kMfmaConcurrentWgs ? 32 : 64;
+}
+
+void launch_ce_stats_f32(const CeArgs &a, int64_t edge, int64_t tokens, hipStream_t st) {
+    const unsigned grid = (unsigned)((tokens + edge - 1) / edge) * (unsigned)a.tiles_v;
+    if (edge == 64) ce_stats_f32_kernel<64><<<grid, 256, 0, st>>>(a);
+    else ce_stats_f32_kernel<32><<<grid, 256, 0, st>>>(a);
+}
+
+void launch_ce_grad_f32(const CeArgs &a, int64_t edge, int64_t tokens, float *Dt, uint32_t *flag, hipStream_t st) {
+    const unsigned grid = (unsigned)((tokens + edge - 1) / edge) * (unsigned)a.tiles_v;
+    if (edge == 64) ce_grad_f32_kernel<64><<<grid, 256, 0, st>>>(a, Dt, flag);
+    else ce_grad_f32_kernel<32><<<grid, 256, 0, st>>>(a, Dt, flag);
+}
+
+hipError_t launch_dw_f32(const float *dY, const float *X, int64_t M, int64_t N, int64_t K, int64_t chunk, int64_t splits, float *out,
+                         hipStream_t st) {
+    const int tiles_n = (int)((N + kF32Tile - 1) / kF32Tile), tiles_k = (int)((K + kF32Tile - 1) / kF32Tile);
+    const dim3 grid((unsigned)tiles_n * tiles_k, (unsigned)splits);
+    auto go = [&](auto w16) {
+        bwd_f32_kernel<kPlain, kF32, decltype(w16)::value><<<grid, 256, 0, st>>>(
+            dY, X, M, N, K, chunk, nullptr, nullptr, nullptr, 5, nullptr, 0, 0, nullptr, nullptr, 0, out, nullptr, tiles_k);
+    };
+    if (N % 4 == 0) go(std::true_type{});
+    else go(std::false_type{});
     return hipGetLastError();
 }
 

@@ -13,7 +13,7 @@
 // r = max(|g|, |h|):
 //   D = r D',  dX[t] = r[t] (D' W)[t],  dW = G D'^T X',  X'[t] = X[t] r[t] / G  (rounded),  G = max r
 // so that the tokens' weights are rounded into X' where they differ, and nowhere where they are those of a mean (X' is X then).
-// Other shapes and fp32 take the kernels below.
+// fp32 with K a multiple of 16 goes to the fp32 matrix instructions (gemm_f32.hip); other shapes take the kernels below.
 #include "linear_ce.h"
 #include "ops_device.h"
 
@@ -92,20 +92,37 @@ __global__ void __launch_bounds__(256) ce_stats_kernel(CeArgs a) {
     }
 }
 
-// Joins the parts of a token: m = max m_i, s = sum s_i exp(m_i - m), in a fixed order. `per` lanes (a power of two up to 64)
-// share a token, each taking every per-th part.
-__global__ void __launch_bounds__(256) ce_join_kernel(CeArgs a, int tiles, int per, uint32_t *flag) {
-    const int64_t t = ((int64_t)blockIdx.x * 256 + threadIdx.x) / per;
-    const int lane = threadIdx.x % per;
-    float m = -__builtin_inff(), s = 0.0f;
+// Joins the parts of a token: m = max m_i, s = sum s_i exp(m_i - m), in a fixed order. A workgroup takes `tokens` (a power of two)
+// neighbours, so that its loads run along part's rows; the 256 / tokens threads of one take every so many-th part, eight at a time
+// under way, each with a running maximum.
+__global__ void __launch_bounds__(256) ce_join_kernel(CeArgs a, int tiles, int tokens, uint32_t *flag) {
+    __shared__ float2 lds[256];
+    const float kNone = -__builtin_inff();
+    const int per = 256 / tokens, lane = threadIdx.x / tokens;
+    const int64_t t = (int64_t)blockIdx.x * tokens + threadIdx.x % tokens;
+    auto join = [&](float &m, float &s, float2 p) {  // an empty part is (-inf, 0)
+        const float top = fmaxf(m, p.x);
+        s = (m == top ? s : s * expf(m - top)) + (p.x == top ? p.y : p.y * expf(p.x - top));
+        m = top;
+    };
+    float m = kNone, s = 0.0f;
     if (t < a.T) {
-        for (int i = lane; i < tiles; i += per) m = fmaxf(m, a.part[(int64_t)i * a.T + t].x);
-        for (int d = per / 2; d >= 1; d >>= 1) m = fmaxf(m, __shfl_xor(m, d, 64));
-        for (int i = lane; i < tiles; i += per) {
-            const float2 p = a.part[(int64_t)i * a.T + t];
-            s += p.y * expf(p.x - m);
+        for (int i = lane; i < tiles; i += 8 * per) {
+            float2 p[8];
+#pragma unroll
+            for (int u = 0; u < 8; u++) p[u] = i + u * per < tiles ? a.part[(int64_t)(i + u * per) * a.T + t] : make_float2(kNone, 0.0f);
+#pragma unroll
+            for (int u = 0; u < 8; u++) join(m, s, p[u]);
         }
-        for (int d = per / 2; d >= 1; d >>= 1) s += __shfl_xor(s, d, 64);
+    }
+    lds[threadIdx.x] = make_float2(m, s);
+    __syncthreads();
+    for (int w = per / 2; w >= 1; w >>= 1) {
+        if (lane < w) {
+            join(m, s, lds[threadIdx.x + w * tokens]);
+            lds[threadIdx.x] = make_float2(m, s);
+        }
+        __syncthreads();
     }
     if (t >= a.T || lane != 0) return;
     const float ls = logf(s);
@@ -262,7 +279,7 @@ __global__ void __launch_bounds__(256) ce_scale_x_kernel(const uint16_t *__restr
     store8_n(out + i, 8, v);
 }
 
-// total = before + the splits' sums in order; to `sums` in fp32, or times the row's (or everything's) factor to `out`
+// total = before + the splits' sums in order; to `sums` in fp32, or times the row's (or everything's, or no) factor to `out`
 __global__ void __launch_bounds__(256) ce_sums_kernel(const float *__restrict__ part, int64_t splits, const float *__restrict__ before,
                                                       const float *__restrict__ factor, int per_row, int64_t first, int64_t n, int64_t K,
                                                       float *__restrict__ sums, void *__restrict__ out, int out_dtype) {
@@ -284,9 +301,11 @@ __global__ void __launch_bounds__(256) ce_sums_kernel(const float *__restrict__ 
         store8_n(sums + i, 8, s);
         return;
     }
-    const float f = per_row ? factor[i / K] : *factor;
+    if (factor) {
+        const float f = per_row ? factor[i / K] : *factor;
 #pragma unroll
-    for (int e = 0; e < 8; e++) s[e] *= f;
+        for (int e = 0; e < 8; e++) s[e] *= f;
+    }
     if (out_dtype == kBF16) store8_n(static_cast<uint16_t *>(out) + i, 8, s);
     else store8_n(static_cast<float *>(out) + i, 8, s);
 }
@@ -305,9 +324,9 @@ hipError_t in_elements(int64_t n, F &&f) {
 bool on_mfma(int dtype, int64_t K) { return dtype == kBF16 && K % 16 == 0; }
 
 // Pieces of the vocabulary: as few as D takes 1 GiB each at most (a tile's 256 entries each at least), of one width but for the last
-constexpr int64_t kPieceBytes = int64_t(1) << 30, kMostWidth = int64_t(1) << 20;
+constexpr int64_t kPieceBytes = int64_t(1) << 30;
 int64_t piece_width(int64_t T, int64_t V, int64_t esz) {
-    const int64_t fit = std::max<int64_t>(1, std::min(kPieceBytes / (T * esz), kMostWidth) / 256);
+    const int64_t fit = std::max<int64_t>(1, std::min(kPieceBytes / (T * esz), kCeMostWidth) / 256);
     const int64_t tiles = cdiv(V, 256), pieces = cdiv(tiles, fit);
     return cdiv(tiles, pieces) * 256;
 }
@@ -336,7 +355,7 @@ Splits dw_splits(int64_t T, int64_t N, int64_t K) {
 
 // fp32 sums of the splits: one of dX, or as many of dX or dW as kDxSums holds
 size_t sums_bytes(int64_t T, int64_t V, int64_t K) {
-    const int64_t rows = std::max(T, std::min(cdiv(V, 256) * 256, kMostWidth));
+    const int64_t rows = std::max(T, std::min(cdiv(V, 256) * 256, kCeMostWidth));
     const int64_t many = rows > kDxSums / K / kMostSplits ? kDxSums : kMostSplits * rows * K;
     return round256((size_t)std::max(T * K, many) * sizeof(float));
 }
@@ -359,6 +378,68 @@ size_t mfma_space(int64_t T, int64_t V, int64_t K, char *base, MfmaSpace *s) {
         *s = MfmaSpace{reinterpret_cast<float *>(r), reinterpret_cast<float *>(most), reinterpret_cast<float *>(sums),
                        reinterpret_cast<float *>(part), reinterpret_cast<uint16_t *>(x), reinterpret_cast<uint16_t *>(D)};
     return at;
+}
+
+// ---- fp32 ---------------------------------------------------------------------------------------
+// Splits of a product's reduction over R: whole rounds of 64 x 64 tiles, three per CU at once, in units of a 32-row step
+Splits f32_splits(int64_t R, int64_t N, int64_t K) {
+    const int64_t tiles = cdiv(N, 64) * cdiv(K, 64), steps = cdiv(R, 32), slots = 256;
+    const int64_t most = tiles >= 16 * slots ? 1 : std::min<int64_t>(std::min<int64_t>(kMostSplits, steps), kDxSums / (N * K));
+    int64_t best = -1, count = 1;
+    for (int64_t s = 1; s <= std::max<int64_t>(1, most); s++) {
+        const int64_t cost = cdiv(tiles * s, slots) * (cdiv(steps, s) + 3) + (s > 1 ? 4 + s * N * K / 281250 : 0);
+        if (best < 0 || cost < best) best = cost, count = s;
+    }
+    const int64_t chunk = cdiv(steps, count) * 32;
+    return {cdiv(R, chunk), chunk};
+}
+
+struct F32Space {
+    float *sums, *part, *D, *Dt;
+};
+size_t f32_space(int64_t T, int64_t V, int64_t K, char *base, F32Space *s) {
+    const size_t sums = round256((size_t)T * (size_t)K * sizeof(float)), D = round256(piece_bytes(T, V, sizeof(float)));
+    char *const at = base + kWsHeader;
+    if (s)
+        *s = F32Space{reinterpret_cast<float *>(at), reinterpret_cast<float *>(at + sums), reinterpret_cast<float *>(at + sums + sums_bytes(T, V, K)),
+                      reinterpret_cast<float *>(at + sums + sums_bytes(T, V, K) + D)};
+    return kWsHeader + sums + sums_bytes(T, V, K) + 2 * D;
+}
+
+hipError_t bwd_f32(CeArgs a, float *dX, float *dW, uint32_t *flag, char *ws, hipStream_t st) {
+    F32Space s;
+    f32_space(a.T, a.V, a.K, ws, &s);
+    const int64_t T = a.T, V = a.V, K = a.K, width = piece_width(T, V, sizeof(float));
+    a.D = s.D;
+    auto finish = [&](int64_t splits, const float *before, int64_t n, float *sums, float *out) {
+        return in_elements(n, [&](int64_t first, unsigned grid) {
+            ce_sums_kernel<<<grid, 256, 0, st>>>(s.part, splits, before, nullptr, 0, first, n, K, sums, out, kF32);
+        });
+    };
+    for (int64_t v0 = 0; v0 < V; v0 += width) {
+        const int64_t n = std::min(width, V - v0), edge = ce_f32_tile(T, n);
+        a.v0 = v0, a.pitch = n, a.tiles_v = (int)cdiv(n, edge);
+        hipError_t e = in_runs(cdiv(T, edge), a.tiles_v, [&](int64_t first, int64_t count) {
+            a.t0 = first * edge;
+            launch_ce_grad_f32(a, edge, count * edge, s.Dt, flag, st);
+        });
+        if (e != hipSuccess) return e;
+        if (dX) {
+            const Splits p = f32_splits(n, T, K);
+            const bool alone = p.count == 1 && n == V;
+            e = launch_dw_f32(s.Dt, static_cast<const float *>(a.W) + v0 * K, n, T, K, p.chunk, p.count, alone ? dX : s.part, st);
+            if (e == hipSuccess && !alone) e = finish(p.count, v0 ? s.sums : nullptr, T * K, v0 + n == V ? nullptr : s.sums, dX);
+            if (e != hipSuccess) return e;
+        }
+        if (dW) {
+            const Splits p = f32_splits(T, n, K);
+            float *const out = dW + v0 * K;
+            e = launch_dw_f32(s.D, static_cast<const float *>(a.X), T, n, K, p.chunk, p.count, p.count == 1 ? out : s.part, st);
+            if (e == hipSuccess && p.count > 1) e = finish(p.count, nullptr, n * K, nullptr, out);
+            if (e != hipSuccess) return e;
+        }
+    }
+    return hipSuccess;
 }
 
 hipError_t bwd_mfma(CeArgs a, void *dX, void *dW, int dw_dtype, uint32_t *flag, char *ws, hipStream_t st) {
@@ -416,13 +497,15 @@ hipError_t bwd_mfma(CeArgs a, void *dX, void *dW, int dw_dtype, uint32_t *flag, 
 }  // namespace
 
 size_t linear_ce_fwd_ws(int64_t T, int64_t V) {
-    return kWsHeader + round256((size_t)T * sizeof(float)) + (size_t)cdiv(V, kTileV) * (size_t)T * sizeof(float2);
+    // parts of 64 vocabulary entries, or of 32 in fp32 where there are fewer than 256 tiles of 64 x 64
+    const int64_t parts = std::max(cdiv(V, kTileV) * T, std::min(cdiv(V, 32) * T, int64_t(2) * 256 * 64));
+    return kWsHeader + round256((size_t)T * sizeof(float)) + (size_t)parts * sizeof(float2);
 }
 
 size_t linear_ce_bwd_ws(int64_t T, int64_t V, int64_t K) {
     if (T == 0) return kWsHeader;
     const size_t simple = kWsHeader + round256((size_t)T * (size_t)K * sizeof(float)) + piece_bytes(T, V, sizeof(float));
-    return std::max(simple, mfma_space(T, V, K, nullptr, nullptr));
+    return std::max(simple, std::max(mfma_space(T, V, K, nullptr, nullptr), f32_space(T, V, K, nullptr, nullptr)));
 }
 
 hipError_t launch_linear_ce_fwd(int dtype, const void *X, const void *W, int64_t T, int64_t V, int64_t K, const int64_t *target,
@@ -432,9 +515,9 @@ hipError_t launch_linear_ce_fwd(int dtype, const void *X, const void *W, int64_t
     a.X = X, a.W = W, a.target = target, a.lse = lse, a.logp = logp, a.T = T, a.V = V, a.K = K;
     a.zt = reinterpret_cast<float *>(base);
     a.part = reinterpret_cast<float2 *>(base + round256((size_t)T * sizeof(float)));
-    const bool mfma = on_mfma(dtype, K), few = mfma && T <= kCeFew;
-    const int64_t rows = mfma ? kCeTile : kTileT;
-    a.tiles_v = (int)cdiv(V, few ? kCeFewV : mfma ? kCeTile : kTileV);
+    const bool mfma = on_mfma(dtype, K), few = mfma && T <= kCeFew, f32 = dtype == kF32 && ce_f32_supported(T, V, K);
+    const int64_t rows = mfma ? kCeTile : f32 ? ce_f32_tile(T, V) : kTileT;
+    a.tiles_v = (int)cdiv(V, few ? kCeFewV : rows);
     hipError_t e = hipSuccess;
     if (few) {
         launch_ce_stats_few(a, st);
@@ -443,13 +526,14 @@ hipError_t launch_linear_ce_fwd(int dtype, const void *X, const void *W, int64_t
         e = in_runs(cdiv(T, rows), a.tiles_v, [&](int64_t first, int64_t count) {
             a.t0 = first * rows;
             if (mfma) launch_ce_stats_mfma(a, count * rows, st);
+            else if (f32) launch_ce_stats_f32(a, rows, count * rows, st);
             else if (dtype == kBF16) ce_stats_kernel<kBF16><<<(unsigned)(count * a.tiles_v), 256, 0, st>>>(a);
             else ce_stats_kernel<kF32><<<(unsigned)(count * a.tiles_v), 256, 0, st>>>(a);
         });
     }
     if (e != hipSuccess) return e;
-    const int per = T >= 4096 ? 8 : 64;
-    ce_join_kernel<<<(unsigned)cdiv(T * per, 256), 256, 0, st>>>(a, a.tiles_v, per, flag);
+    const int tokens = T >= 1024 ? 32 : T >= 32 ? 8 : 1;
+    ce_join_kernel<<<(unsigned)cdiv(T, tokens), 256, 0, st>>>(a, a.tiles_v, tokens, flag);
     return hipGetLastError();
 }
 
@@ -460,6 +544,8 @@ hipError_t launch_linear_ce_bwd(int dtype, const void *X, const void *W, int64_t
     float *const sums = reinterpret_cast<float *>(base);
     CeArgs a{};
     a.X = X, a.W = W, a.target = target, a.lse = const_cast<float *>(lse), a.g = g, a.h = h, a.T = T, a.V = V, a.K = K;
+    if (dtype == kF32 && ce_f32_supported(T, V, K))
+        return bwd_f32(a, static_cast<float *>(dX), static_cast<float *>(dW), flag, static_cast<char *>(ws), st);
     if (on_mfma(dtype, K)) return bwd_mfma(a, dX, dW, dw_dtype, flag, static_cast<char *>(ws), st);
     a.D = base + round256((size_t)T * (size_t)K * sizeof(float));
     const int64_t width = piece_width(T, V, sizeof(float));
