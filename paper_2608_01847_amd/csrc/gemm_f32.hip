@@ -235,7 +235,7 @@ fwd_f32_kernel(const float *__restrict__ X, const float *__restrict__ W, int64_t
 // Backward, G = dY^T X_hat over the tokens of one split (both token-major), 64 n x 64 k per workgroup, the
 // waves 2 x 2, with the fused straight-through epilogue. A step is 32 tokens ([32][64] floats per operand,
 // three stages of 16 KB); fragments are 4-byte LDS reads of 32 consecutive columns. dY rows start on 4-byte
-// boundaries only unless N % 4 == 0: they are then staged with 4-byte loads (W16 == false).
+// boundaries only unless ldy % 4 == 0: they are then staged with 4-byte loads (W16 == false).
 // A chain of roundings is 64 tokens long, the chains are added in fp64: with one chain per split the gradients'
 // error against 64 bits was up to 4.4 times that of many short splits (3,507 x 1,758 x 160: 3.1e-7 for 7.0e-8; now
 // 6.4e-8). The additions run beside the next chain's matrix instructions (3,507 x 1,758 x 160 36.9 us for 37.5,
@@ -243,7 +243,7 @@ fwd_f32_kernel(const float *__restrict__ X, const float *__restrict__ W, int64_t
 constexpr int kPlain = 2;  // in place of the format: dY^T X, split by split to G_out
 template <int FMT, int WDT, bool W16>
 __global__ void __launch_bounds__(256)
-bwd_f32_kernel(const float *__restrict__ dY, const float *__restrict__ X, int64_t M, int64_t N, int64_t K, int64_t chunk,
+bwd_f32_kernel(const float *__restrict__ dY, const float *__restrict__ X, int64_t M, int64_t N, int64_t ldy, int64_t K, int64_t chunk,
                const void *__restrict__ W, const float *__restrict__ s_fp, const float *__restrict__ c, int sb_log2,
                const float *__restrict__ alpha_ptr, int ste_clip, int e8m0_floor, float *__restrict__ part_s,
                float *__restrict__ part_c, int direct, float *__restrict__ G_out, uint32_t *flag, int tiles_k) {
@@ -270,18 +270,18 @@ bwd_f32_kernel(const float *__restrict__ dY, const float *__restrict__ X, int64_
     auto issue = [&](int64_t j, int s) {
         const int64_t t0 = t_begin + j * kStep, rem = t_end - t0;
         const int64_t rows = rem <= 0 ? 0 : (rem < kStep ? rem : kStep);
-        const __amdgpu_buffer_rsrc_t ry = make_rsrc(dY + (rows ? t0 * N : 0), rows * N * 4);
+        const __amdgpu_buffer_rsrc_t ry = make_rsrc(dY + (rows ? t0 * ldy : 0), rows * ldy * 4);
         const __amdgpu_buffer_rsrc_t rx = make_rsrc(X + (rows ? t0 * K : 0), rows * K * 4);
         lds_char *const st = lsm + s * kStage;
 #pragma unroll
         for (int i = 0; i < kLoadsY; i++) {
             if constexpr (W16) {
                 const uint32_t blk = (uint32_t)wave_u * 2u + i, row = 4u * blk + row16;
-                const uint32_t off = ((row * (uint32_t)N + (uint32_t)n0 + col16) * 4u) | y_bad;
+                const uint32_t off = ((row * (uint32_t)ldy + (uint32_t)n0 + col16) * 4u) | y_bad;
                 __builtin_amdgcn_raw_ptr_buffer_load_lds(ry, st + blk * 1024, 16, (int)off, 0, 0, 0);
             } else {
                 const uint32_t row = (uint32_t)wave_u * 8u + i;
-                const uint32_t off = ((row * (uint32_t)N + (uint32_t)n0 + (uint32_t)lane) * 4u) | y_bad;
+                const uint32_t off = ((row * (uint32_t)ldy + (uint32_t)n0 + (uint32_t)lane) * 4u) | y_bad;
                 __builtin_amdgcn_raw_ptr_buffer_load_lds(ry, st + row * 256, 4, (int)off, 0, 0, 0);
             }
         }
@@ -454,7 +454,7 @@ hipError_t launch_bwd_f32(int fmt, int w_dt, const float *dY, const float *X, in
     int sbl = 0;
     while ((1 << sbl) < sb) sbl++;
     const dim3 grid((unsigned)tiles_n * tiles_k, (unsigned)splits);
-#define BF(F, WD, V) bwd_f32_kernel<F, WD, V><<<grid, 256, 0, st>>>(dY, X, M, N, K, chunk, W, s_fp, c, sbl, alpha, ste_clip, e8m0_floor, part_s, part_c, direct, G_out, flag, tiles_k)
+#define BF(F, WD, V) bwd_f32_kernel<F, WD, V><<<grid, 256, 0, st>>>(dY, X, M, N, N, K, chunk, W, s_fp, c, sbl, alpha, ste_clip, e8m0_floor, part_s, part_c, direct, G_out, flag, tiles_k)
 #define BF_V(F, WD) if (N % 4 == 0) BF(F, WD, true); else BF(F, WD, false)
     if (fmt == kFmtMX) { if (w_dt == kBF16) { BF_V(kFmtMX, kBF16); } else { BF_V(kFmtMX, kF32); } }
     else { if (w_dt == kBF16) { BF_V(kFmtNV, kBF16); } else { BF_V(kFmtNV, kF32); } }
@@ -506,9 +506,10 @@ __global__ void __launch_bounds__(256) ce_stats_f32_kernel(CeArgs a) {
     a.part[tv * a.T + t0 + threadIdx.x] = make_float2(m, s);
 }
 
-// D of the piece, [T][pitch] for dW and transposed, [pitch][T], for dX: each product reads its operand along the reduction
+// D of the piece, [T][pitch] for dW and transposed, [entries][pitch_t], for dX: each product reads its operand along the reduction.
+// The pitches are multiples of 4; what lies between a row's end and its pitch is not read into a result.
 template <int T>
-__global__ void __launch_bounds__(256) ce_grad_f32_kernel(CeArgs a, float *__restrict__ Dt, uint32_t *flag) {
+__global__ void __launch_bounds__(256) ce_grad_f32_kernel(CeArgs a, float *__restrict__ Dt, int64_t pitch_t, uint32_t *flag) {
     __shared__ __attribute__((aligned(16))) char smem[f32_fwd_lds(T)];
     const uint32_t id = xcd_tile(blockIdx.x, gridDim.x), tiles_t = gridDim.x / (uint32_t)a.tiles_v;
     const int64_t c0 = (int64_t)(id / tiles_t) * T, v0 = a.v0 + c0, t0 = a.t0 + (int64_t)(id % tiles_t) * T;
@@ -523,17 +524,17 @@ __global__ void __launch_bounds__(256) ce_grad_f32_kernel(CeArgs a, float *__res
 #pragma unroll
     for (int r = 0; r < F32Tile<T>::R; r++) {
         const int64_t c = c0 + tile.row(r), v = a.v0 + c;
-        if (c >= a.pitch) continue;
+        if (v >= a.V || c >= a.pitch) continue;
         const float d = (v == want ? g : 0.0f) + (h - g) * expf((float)tile.o[r] - lse);
         D[t * a.pitch + c] = d;
-        Dt[c * a.T + t] = d;
+        Dt[c * pitch_t + t] = d;
     }
 }
 
 }  // namespace
 
 bool ce_f32_supported(int64_t T, int64_t V, int64_t K) {
-    return f32_fwd_supported(V, T, K) && f32_bwd_supported(T, std::min(V, kCeMostWidth), K) && f32_bwd_supported(V, T, K);
+    return f32_fwd_supported(V, T, K) && f32_bwd_supported(T, kCeMostWidth, K) && f32_bwd_supported(V, T + 3, K);
 }
 
 // Edge of a logit tile, as the forward chooses it: 64 x 64 where they give every CU one
@@ -547,22 +548,19 @@ void launch_ce_stats_f32(const CeArgs &a, int64_t edge, int64_t tokens, hipStrea
     else ce_stats_f32_kernel<32><<<grid, 256, 0, st>>>(a);
 }
 
-void launch_ce_grad_f32(const CeArgs &a, int64_t edge, int64_t tokens, float *Dt, uint32_t *flag, hipStream_t st) {
+void launch_ce_grad_f32(const CeArgs &a, int64_t edge, int64_t tokens, float *Dt, int64_t pitch_t, uint32_t *flag,
+                        hipStream_t st) {
     const unsigned grid = (unsigned)((tokens + edge - 1) / edge) * (unsigned)a.tiles_v;
-    if (edge == 64) ce_grad_f32_kernel<64><<<grid, 256, 0, st>>>(a, Dt, flag);
-    else ce_grad_f32_kernel<32><<<grid, 256, 0, st>>>(a, Dt, flag);
+    if (edge == 64) ce_grad_f32_kernel<64><<<grid, 256, 0, st>>>(a, Dt, pitch_t, flag);
+    else ce_grad_f32_kernel<32><<<grid, 256, 0, st>>>(a, Dt, pitch_t, flag);
 }
 
-hipError_t launch_dw_f32(const float *dY, const float *X, int64_t M, int64_t N, int64_t K, int64_t chunk, int64_t splits, float *out,
-                         hipStream_t st) {
+hipError_t launch_dw_f32(const float *dY, const float *X, int64_t M, int64_t N, int64_t ldy, int64_t K, int64_t chunk,
+                         int64_t splits, float *out, hipStream_t st) {
     const int tiles_n = (int)((N + kF32Tile - 1) / kF32Tile), tiles_k = (int)((K + kF32Tile - 1) / kF32Tile);
     const dim3 grid((unsigned)tiles_n * tiles_k, (unsigned)splits);
-    auto go = [&](auto w16) {
-        bwd_f32_kernel<kPlain, kF32, decltype(w16)::value><<<grid, 256, 0, st>>>(
-            dY, X, M, N, K, chunk, nullptr, nullptr, nullptr, 5, nullptr, 0, 0, nullptr, nullptr, 0, out, nullptr, tiles_k);
-    };
-    if (N % 4 == 0) go(std::true_type{});
-    else go(std::false_type{});
+    bwd_f32_kernel<kPlain, kF32, true><<<grid, 256, 0, st>>>(dY, X, M, N, ldy, K, chunk, nullptr, nullptr, nullptr, 5, nullptr, 0, 0,
+                                                             nullptr, nullptr, 0, out, nullptr, tiles_k);
     return hipGetLastError();
 }
 

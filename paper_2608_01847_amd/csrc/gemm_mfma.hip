@@ -665,7 +665,7 @@ dw_mfma_kernel(const uint16_t *__restrict__ dY, const uint16_t *__restrict__ X, 
         for (int j = 0; j < 4; j++)
 #pragma unroll
             for (int r = 0; r < 16; r++) acc[i][j][r] *= f;
-    if (out_dtype == kBF16) store_tile_bf16(acc, smem, static_cast<uint16_t *>(out) + n0 * K, N - n0, K, (uint32_t)k0, K);
+    if (out_dtype == kBF16) store_tile_bf16<kTile>(acc, smem, static_cast<uint16_t *>(out) + n0 * K, N - n0, K, (uint32_t)k0, K);
     else store_tile_f32(acc, smem, static_cast<float *>(out) + n0 * K, N - n0, K, (uint32_t)k0, K);
 }
 

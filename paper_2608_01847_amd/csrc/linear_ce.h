@@ -5,8 +5,8 @@
 
 namespace focus {
 
-constexpr int kCeTile = 256;  // edge of a logit tile on the matrix instructions
-constexpr int kCeFew = 32;    // tokens up to which the forward reads the weights straight into registers
+constexpr int kCeTile = 256;  // edge of a tile on the matrix instructions (of a logit tile: or half of it)
+constexpr int kCeFew = 16;    // tokens up to which the forward reads the weights straight into registers
 constexpr int kCeFewV = 128;  // vocabulary entries of its workgroups
 constexpr int64_t kCeMostWidth = int64_t(1) << 20;  // of a piece of the vocabulary
 
@@ -23,18 +23,20 @@ struct CeArgs {
     int tiles_v;
 };
 
-// Logit tiles on the matrix instructions (bf16, K a multiple of 16): the tiles of `tokens` tokens from a.t0 on
-void launch_ce_stats_mfma(const CeArgs &a, int64_t tokens, hipStream_t st);
+// Logit tiles on the matrix instructions (bf16, K a multiple of 16), of edge x edge: those of `tokens` tokens from a.t0 on
+int64_t ce_mfma_tile(int64_t T, int64_t n);
+void launch_ce_stats_mfma(const CeArgs &a, int64_t edge, int64_t tokens, hipStream_t st);
 void launch_ce_stats_few(const CeArgs &a, hipStream_t st);  // T <= kCeFew
-void launch_ce_grad_mfma(const CeArgs &a, int64_t tokens, uint32_t *flag, hipStream_t st);
+void launch_ce_grad_mfma(const CeArgs &a, int64_t edge, int64_t tokens, uint32_t *flag, hipStream_t st);
 
-// The same on the fp32 matrix instructions (K a multiple of 16), tiles of edge x edge; D's transpose, [pitch][T], goes to Dt
+// The same on the fp32 matrix instructions (K a multiple of 16), tiles of edge x edge; D's transpose, [entries][pitch_t], goes to Dt
 bool ce_f32_supported(int64_t T, int64_t V, int64_t K);
 int64_t ce_f32_tile(int64_t T, int64_t n);
 void launch_ce_stats_f32(const CeArgs &a, int64_t edge, int64_t tokens, hipStream_t st);
-void launch_ce_grad_f32(const CeArgs &a, int64_t edge, int64_t tokens, float *Dt, uint32_t *flag, hipStream_t st);
-// out [splits][N][K] = dY^T X over `chunk` rows (a multiple of 32) of dY [M][N] and X [M][K] each
-hipError_t launch_dw_f32(const float *dY, const float *X, int64_t M, int64_t N, int64_t K, int64_t chunk, int64_t splits, float *out,
-                         hipStream_t st);
+void launch_ce_grad_f32(const CeArgs &a, int64_t edge, int64_t tokens, float *Dt, int64_t pitch_t, uint32_t *flag,
+                        hipStream_t st);
+// out [splits][N][K] = dY^T X over `chunk` rows (a multiple of 32) of dY [M][ldy] (ldy a multiple of 4) and X [M][K] each
+hipError_t launch_dw_f32(const float *dY, const float *X, int64_t M, int64_t N, int64_t ldy, int64_t K, int64_t chunk,
+                         int64_t splits, float *out, hipStream_t st);
 
 }  // namespace focus

@@ -323,34 +323,36 @@ hipError_t in_elements(int64_t n, F &&f) {
 
 bool on_mfma(int dtype, int64_t K) { return dtype == kBF16 && K % 16 == 0; }
 
-// Pieces of the vocabulary: as few as D takes 1 GiB each at most (a tile's 256 entries each at least), of one width but for the last
-constexpr int64_t kPieceBytes = int64_t(1) << 30;
+// Pieces of the vocabulary: as few as D takes 1 GiB each at most (in fp32, whose products are slower against what a piece costs, 128 MiB;
+// a tile's 256 entries each at least), of one width but for the last
+constexpr int64_t piece_most(int64_t esz) { return int64_t(1) << (esz == 2 ? 30 : 27); }
 int64_t piece_width(int64_t T, int64_t V, int64_t esz) {
-    const int64_t fit = std::max<int64_t>(1, std::min(kPieceBytes / (T * esz), kCeMostWidth) / 256);
+    const int64_t fit = std::max<int64_t>(1, std::min(piece_most(esz) / (T * esz), kCeMostWidth) / 256);
     const int64_t tiles = cdiv(V, 256), pieces = cdiv(tiles, fit);
     return cdiv(tiles, pieces) * 256;
 }
 // bytes of D for T tokens or fewer
 size_t piece_bytes(int64_t T, int64_t V, int64_t esz) {
-    return std::max<size_t>((size_t)(T * 256 * esz), (size_t)std::min(T * cdiv(V, 256) * 256 * esz, kPieceBytes));
+    return std::max<size_t>((size_t)(T * 256 * esz), (size_t)std::min(T * cdiv(V, 256) * 256 * esz, piece_most(esz)));
 }
 
 constexpr int64_t kMostSplits = 64;
 
-// Splits of dW's token range: as plan_dx has them for the vocabulary's, in units of a 32-token step (0.9 us)
+// Splits of a product [M][N] over its reduction R, as the input gradient of a linear has them: whole rounds of 256 x 256 tiles, one
+// per CU, in units of a step of 32 (0.9 us), 8 of them for a tile's end; the fp32 sums written and read (about 4 MB in a unit)
 struct Splits {
     int64_t count, chunk;
 };
-Splits dw_splits(int64_t T, int64_t N, int64_t K) {
-    const int64_t tiles = cdiv(N, kCeTile) * cdiv(K, kCeTile), steps = cdiv(T, 32);
-    const int64_t most = tiles >= 4 * 256 ? 1 : std::min<int64_t>(std::min<int64_t>(kMostSplits, steps / 8), kDxSums / (N * K));
+Splits mfma_splits(int64_t R, int64_t M, int64_t N) {
+    const int64_t tiles = cdiv(M, kCeTile) * cdiv(N, kCeTile), steps = cdiv(R, 32);
+    const int64_t most = tiles >= 4 * 256 ? 1 : std::min<int64_t>(std::min<int64_t>(kMostSplits, steps / 8), kDxSums / (M * N));
     int64_t best = -1, count = 1;
     for (int64_t s = 1; s <= std::max<int64_t>(1, most); s++) {
-        const int64_t cost = cdiv(tiles * s, 256) * (cdiv(steps, s) + 8) + (s > 1 ? s * N * K * 8 / 4000000 + 4 : 0);
+        const int64_t cost = cdiv(tiles * s, 256) * (cdiv(steps, s) + 8) + (s > 1 ? s * M * N * 8 / 4000000 + 4 : 0);
         if (best < 0 || cost < best) best = cost, count = s;
     }
     const int64_t chunk = cdiv(steps, count) * 32;
-    return {cdiv(T, chunk), chunk};
+    return {cdiv(R, chunk), chunk};
 }
 
 // fp32 sums of the splits: one of dX, or as many of dX or dW as kDxSums holds
@@ -398,7 +400,8 @@ struct F32Space {
     float *sums, *part, *D, *Dt;
 };
 size_t f32_space(int64_t T, int64_t V, int64_t K, char *base, F32Space *s) {
-    const size_t sums = round256((size_t)T * (size_t)K * sizeof(float)), D = round256(piece_bytes(T, V, sizeof(float)));
+    const size_t sums = round256((size_t)T * (size_t)K * sizeof(float));
+    const size_t D = round256(piece_bytes((T + 3) / 4 * 4, V, sizeof(float)));  // transposed too, its rows of whole fours
     char *const at = base + kWsHeader;
     if (s)
         *s = F32Space{reinterpret_cast<float *>(at), reinterpret_cast<float *>(at + sums), reinterpret_cast<float *>(at + sums + sums_bytes(T, V, K)),
@@ -409,7 +412,7 @@ size_t f32_space(int64_t T, int64_t V, int64_t K, char *base, F32Space *s) {
 hipError_t bwd_f32(CeArgs a, float *dX, float *dW, uint32_t *flag, char *ws, hipStream_t st) {
     F32Space s;
     f32_space(a.T, a.V, a.K, ws, &s);
-    const int64_t T = a.T, V = a.V, K = a.K, width = piece_width(T, V, sizeof(float));
+    const int64_t T = a.T, V = a.V, K = a.K, width = piece_width((T + 3) / 4 * 4, V, sizeof(float)), pitch_t = (T + 3) / 4 * 4;
     a.D = s.D;
     auto finish = [&](int64_t splits, const float *before, int64_t n, float *sums, float *out) {
         return in_elements(n, [&](int64_t first, unsigned grid) {
@@ -418,23 +421,23 @@ hipError_t bwd_f32(CeArgs a, float *dX, float *dW, uint32_t *flag, char *ws, hip
     };
     for (int64_t v0 = 0; v0 < V; v0 += width) {
         const int64_t n = std::min(width, V - v0), edge = ce_f32_tile(T, n);
-        a.v0 = v0, a.pitch = n, a.tiles_v = (int)cdiv(n, edge);
+        a.v0 = v0, a.pitch = (n + 3) / 4 * 4, a.tiles_v = (int)cdiv(n, edge);
         hipError_t e = in_runs(cdiv(T, edge), a.tiles_v, [&](int64_t first, int64_t count) {
             a.t0 = first * edge;
-            launch_ce_grad_f32(a, edge, count * edge, s.Dt, flag, st);
+            launch_ce_grad_f32(a, edge, count * edge, s.Dt, pitch_t, flag, st);
         });
         if (e != hipSuccess) return e;
         if (dX) {
             const Splits p = f32_splits(n, T, K);
             const bool alone = p.count == 1 && n == V;
-            e = launch_dw_f32(s.Dt, static_cast<const float *>(a.W) + v0 * K, n, T, K, p.chunk, p.count, alone ? dX : s.part, st);
+            e = launch_dw_f32(s.Dt, static_cast<const float *>(a.W) + v0 * K, n, T, pitch_t, K, p.chunk, p.count, alone ? dX : s.part, st);
             if (e == hipSuccess && !alone) e = finish(p.count, v0 ? s.sums : nullptr, T * K, v0 + n == V ? nullptr : s.sums, dX);
             if (e != hipSuccess) return e;
         }
         if (dW) {
             const Splits p = f32_splits(T, n, K);
             float *const out = dW + v0 * K;
-            e = launch_dw_f32(s.D, static_cast<const float *>(a.X), T, n, K, p.chunk, p.count, p.count == 1 ? out : s.part, st);
+            e = launch_dw_f32(s.D, static_cast<const float *>(a.X), T, n, a.pitch, K, p.chunk, p.count, p.count == 1 ? out : s.part, st);
             if (e == hipSuccess && p.count > 1) e = finish(p.count, nullptr, n * K, nullptr, out);
             if (e != hipSuccess) return e;
         }
@@ -459,29 +462,29 @@ hipError_t bwd_mfma(CeArgs a, void *dX, void *dW, int dw_dtype, uint32_t *flag, 
     const int64_t width = piece_width(T, V, 2);
     a.pitch = width;
     for (int64_t v0 = 0; v0 < V; v0 += width) {
-        const int64_t n = std::min(width, V - v0);
+        const int64_t n = std::min(width, V - v0), edge = ce_mfma_tile(T, n);
         a.v0 = v0;
-        a.tiles_v = (int)cdiv(n, kCeTile);
-        e = in_runs(cdiv(T, kCeTile), a.tiles_v, [&](int64_t first, int64_t count) {
-            a.t0 = first * kCeTile;
-            launch_ce_grad_mfma(a, count * kCeTile, flag, st);
+        a.tiles_v = (int)(cdiv(n, kCeTile) * kCeTile / edge);  // whole tiles of the products that read D
+        e = in_runs(cdiv(T, edge), a.tiles_v, [&](int64_t first, int64_t count) {
+            a.t0 = first * edge;
+            launch_ce_grad_mfma(a, edge, count * edge, flag, st);
         });
         if (e != hipSuccess) return e;
         const char *const W = static_cast<const char *>(a.W) + (size_t)v0 * (size_t)K * 2;
         if (dX) {
-            const DxPlan p = plan_dx(kBF16, T, (n + 15) / 16 * 16, K);
-            e = launch_dx_sums(s.D, W, T, n, width, K, p.chunk, p.splits, s.part, st);
+            const Splits p = mfma_splits(n, T, K);
+            e = launch_dx_sums(s.D, W, T, n, width, K, p.chunk, p.count, s.part, st);
             if (e != hipSuccess) return e;
             const bool last = v0 + n == V;
             e = in_elements(T * K, [&](int64_t first, unsigned grid) {
-                ce_sums_kernel<<<grid, 256, 0, st>>>(s.part, p.splits, v0 ? s.sums : nullptr, s.r, 1, first, T * K, K,
+                ce_sums_kernel<<<grid, 256, 0, st>>>(s.part, p.count, v0 ? s.sums : nullptr, s.r, 1, first, T * K, K,
                                                      last ? nullptr : s.sums, dX, kBF16);
             });
             if (e != hipSuccess) return e;
         }
         if (dW) {
             char *const out = static_cast<char *>(dW) + (size_t)v0 * (size_t)K * (dw_dtype == kBF16 ? 2 : 4);
-            const Splits p = dw_splits(T, n, K);
+            const Splits p = mfma_splits(T, n, K);
             e = launch_dw_mfma(s.D, s.x, T, n, width, K, p.chunk, p.count, s.most, out, dw_dtype, s.part, st);
             if (e != hipSuccess) return e;
             if (p.count > 1)
@@ -516,7 +519,7 @@ hipError_t launch_linear_ce_fwd(int dtype, const void *X, const void *W, int64_t
     a.zt = reinterpret_cast<float *>(base);
     a.part = reinterpret_cast<float2 *>(base + round256((size_t)T * sizeof(float)));
     const bool mfma = on_mfma(dtype, K), few = mfma && T <= kCeFew, f32 = dtype == kF32 && ce_f32_supported(T, V, K);
-    const int64_t rows = mfma ? kCeTile : f32 ? ce_f32_tile(T, V) : kTileT;
+    const int64_t rows = mfma ? ce_mfma_tile(T, V) : f32 ? ce_f32_tile(T, V) : kTileT;
     a.tiles_v = (int)cdiv(V, few ? kCeFewV : rows);
     hipError_t e = hipSuccess;
     if (few) {
@@ -525,7 +528,7 @@ hipError_t launch_linear_ce_fwd(int dtype, const void *X, const void *W, int64_t
     } else {
         e = in_runs(cdiv(T, rows), a.tiles_v, [&](int64_t first, int64_t count) {
             a.t0 = first * rows;
-            if (mfma) launch_ce_stats_mfma(a, count * rows, st);
+            if (mfma) launch_ce_stats_mfma(a, rows, count * rows, st);
             else if (f32) launch_ce_stats_f32(a, rows, count * rows, st);
             else if (dtype == kBF16) ce_stats_kernel<kBF16><<<(unsigned)(count * a.tiles_v), 256, 0, st>>>(a);
             else ce_stats_kernel<kF32><<<(unsigned)(count * a.tiles_v), 256, 0, st>>>(a);

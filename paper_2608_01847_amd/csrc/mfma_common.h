@@ -286,28 +286,31 @@ __device__ __forceinline__ void ste_epilogue(const f32x16_t (&acc)[TT / 64][TT /
     else go(std::integral_constant<int, 4>{});
 }
 
-// Stores of a 256 x 256 tile acc whose lanes hold columns: acc[i][j][r] is row 128 wm + 32 i + 8 (r / 4) + 4 (lane / 32) + r % 4 of
-// column 128 wn + 32 j + lane % 32, written as out[column][row0 + row], `cols` columns of `ld` elements. Through LDS (128 KB), which the
-// operands are done with: a lane writes four rows at a time, and the 16-byte chunk index, xor-ed with the column, spreads them over the
-// banks; then 16-byte pieces leave along the rows. Rows at or past `rows` are not stored (rows: a multiple of 8, or of 4 in fp32).
-__device__ __forceinline__ void store_tile_bf16(const f32x16_t (&acc)[4][4], char *smem, uint16_t *out, int64_t cols, int64_t ld,
-                                                uint32_t row0, int64_t rows = int64_t(1) << 30) {
+// Stores of an E x E tile acc whose lanes hold columns: acc[i][j][r] is row E / 2 wm + 32 i + 8 (r / 4) + 4 (lane / 32) + r % 4 of
+// column E / 2 wn + 32 j + lane % 32, written as out[column][row0 + row], `cols` columns of `ld` elements. Through LDS (2 E^2 bytes, in
+// fp32 128 KB), which the operands are done with: a lane writes four rows at a time, and the 16-byte chunk index, xor-ed with the
+// column, spreads them over the banks; then 16-byte pieces leave along the rows. Rows at or past `rows` are not stored (rows: a
+// multiple of 8, or of 4 in fp32).
+template <int E>
+__device__ __forceinline__ void store_tile_bf16(const f32x16_t (&acc)[E / 64][E / 64], char *smem, uint16_t *out, int64_t cols,
+                                                int64_t ld, uint32_t row0, int64_t rows = int64_t(1) << 30) {
+    constexpr uint32_t kChunks = E / 8, kPitch = E * 2, kPer = 256 / kChunks;  // per column; columns of a pass
     const int t = threadIdx.x, lane = t & 63, wave = t >> 6, wm = wave >> 1, wn = wave & 1, lr = lane & 31, lh = lane >> 5;
-    static_for<4>([&](auto j) {
-        char *const col = smem + (uint32_t)(128 * wn + 32 * j + lr) * 512u + lh * 8u;
-        static_for<16>([&](auto iq) {
+    static_for<E / 64>([&](auto j) {
+        char *const col = smem + (uint32_t)(E / 2 * wn + 32 * j + lr) * kPitch + lh * 8u;
+        static_for<E / 16>([&](auto iq) {
             constexpr int i = iq / 4, q = iq % 4;
             const uint2 v = make_uint2(cvt_pk_bf16(acc[i][j][4 * q], acc[i][j][4 * q + 1]), cvt_pk_bf16(acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]));
-            *reinterpret_cast<uint2 *>(col + (((uint32_t)(16 * wm + 4 * i + q) ^ (uint32_t)lr) << 4)) = v;
+            *reinterpret_cast<uint2 *>(col + (((uint32_t)(E / 16 * wm + 4 * i + q) ^ ((uint32_t)lr % kChunks)) << 4)) = v;
         });
     });
     __syncthreads();
     const __amdgpu_buffer_rsrc_t rs = make_rsrc(out, cols * ld * 2);
-    const uint32_t ch = (uint32_t)t & 31u, row = row0 + ch * 8u, past = (uint32_t)((int64_t)row >= rows) << 31;
+    const uint32_t ch = (uint32_t)t % kChunks, row = row0 + ch * 8u, past = (uint32_t)((int64_t)row >= rows) << 31;
 #pragma unroll
-    for (uint32_t i = 0; i < 32; i++) {
-        const uint32_t c = (uint32_t)t / 32u + 8u * i;
-        const u32x4_t v = *reinterpret_cast<const u32x4_t *>(smem + c * 512u + ((ch ^ (c & 31u)) << 4));
+    for (uint32_t i = 0; i < E / kPer; i++) {
+        const uint32_t c = (uint32_t)t / kChunks + kPer * i;
+        const u32x4_t v = *reinterpret_cast<const u32x4_t *>(smem + c * kPitch + ((ch ^ (c % 32u % kChunks)) << 4));
         __builtin_amdgcn_raw_buffer_store_b128(v, rs, (int)(((c * (uint32_t)ld + row) * 2u) | past), 0, 0);
     }
 }
