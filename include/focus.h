@@ -555,10 +555,10 @@ focus_status focus_sandwich_norm_bwd(const focus_sandwich_config *cfg, const voi
  * Z = X W^T, as focus_token_logprobs gives them from logits in memory.
  *   lse[t] = log sum_v exp Z[t][v]                                         (fp32 [T])
  *   logp_opt[t] = Z[t][target[t]] - lse[t]; 0 where target[t] < 0 (a token left out)
- *   X [T][K] hidden states, W [V][K] weights (dtype: FOCUS_BF16, FOCUS_F32); products exact or in fp32, sums in fp32.
+ *   X [T][K] hidden states, W [V][K] weights (dtype: FOCUS_BF16, FOCUS_F32); products and sums in fp32.
  *   target_opt [T] int64 (NULL: none, logp_opt must be NULL too).
- * The mean cross entropy of n tokens is -sum(logp) / n. X and W have to be finite: a token with a logit that is not raises the
- * domain flag, as a target >= V does (which is taken as left out); the token's results are then unspecified.
+ * The mean cross entropy of n tokens is -sum(logp) / n. X and W have to be finite: a NaN or +inf logit raises the domain
+ * flag, as a target >= V does (which is taken as left out); the token's results are then unspecified.
  * 0 <= T <= 2^24, 1 <= V <= 2^24, 1 <= K <= 2^20 (FOCUS_ERR_SHAPE); T == 0 is a no-op. bf16 with K % 16 == 0 runs on the matrix
  * instructions. ws: focus_workspace_size(FOCUS_CALL_LINEAR_CE_FWD, NULL, T, V, K) bytes; it serves fewer tokens too. */
 focus_status focus_linear_ce_fwd(const void *X, const void *W, int dtype, int64_t T, int64_t V, int64_t K,
@@ -568,7 +568,9 @@ focus_status focus_linear_ce_fwd(const void *X, const void *W, int dtype, int64_
 /* Its gradients, from lse as the forward wrote it. With g = d_logp[t] (0 where target[t] < 0), h = d_lse[t]:
  *   D[t][v] = g ([v == target[t]] - p) + h p,  p = exp(Z[t][v] - lse[t]);  dX = D W,  dW = D^T X
  * (the mean cross entropy of n tokens: d_logp = -1/n; a penalty on lse: d_lse). The vocabulary goes in pieces, of each of
- * which the logits are formed again: D of one piece is what lies in memory, 1 GiB at most up to 2^20 tokens.
+ * which the logits are formed again: D of one piece is what lies in memory, 512 MiB at most up to 2^20 tokens (fp32: twice 128 MiB,
+ * up to 2^17 tokens). bf16 operands: D is rounded to bf16 relative to the larger of |d_logp| and |d_lse| of its token, and X times the
+ * token's share of the largest of these to bf16 for dW (nothing is rounded there where all are the same, as in a mean).
  *   d_logp_opt [T] fp32 needs target_opt; one of d_logp_opt, d_lse_opt is given at least (FOCUS_ERR_NULL).
  *   dX_opt [T][K] (dtype), dW_opt [V][K] (dw_dtype: FOCUS_F32, or FOCUS_BF16 with bf16 operands): overwritten, one of them is
  *   wanted at least. dW in fp32 is the G of focus_fakequant_bwd. With T == 0 dW is zeros.

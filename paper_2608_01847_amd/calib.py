@@ -44,6 +44,7 @@ from . import synth
 
 LEARNING_RATES = {F.MXFP4: (2e-2, 5e-2), F.NVFP4: (5e-3, 1e-3)}  # (scales, coefficients)
 VARIANTS = ("rtn", "scale", "crs", "crs_dgs")
+LOSSES = ("kl_top", "ce")  # of the decoder stack
 EPOCH_STEPS = 39  # 1,248 samples / batch 32
 EVAL_STEP = 1_000_000  # batch index of the held-out evaluation batch
 
@@ -282,6 +283,11 @@ class DecoderStack:
                   dq, dk, dv = attention'(STE_act(O, dH W_o_hat)), written as the slices of one [dq dk dv]; qkv: from that
         update:   AdamW on the three layers' S_fp and c (log2 domain)
 
+    With loss="ce" the student is trained on labels, the teacher's most likely tokens: the loss is their mean cross entropy, whose
+    gradients come from the output layer's operands without its logits, head: grad_s, grad_c from dL/dW_head_hat. With post_norm
+    the attention's output is normalised and gated before it joins the residual stream, H = X + gate norm(Y) and B = norm(H) in one
+    pass. With max_grad_norm the gradients of all scales and coefficients are scaled together before the update.
+
     Held-out batches are scored by the log probability that the student gives the teacher's most likely token, its entropy
     and how often its own most likely token is the same. Every arithmetic step runs in libfocus."""
 
@@ -291,8 +297,12 @@ class DecoderStack:
 
     def __init__(self, fmt: int, variant: str, hidden: int = 2560, heads: tuple = (32, 8), head_dim: int = 128,
                  vocab: int = 32000, lengths: tuple = (2048, 1024, 700, 324), k: int = 1000, x_kind: str = "lowrank",
-                 hyper: Hyper | None = None, device="cuda"):
+                 hyper: Hyper | None = None, device="cuda", loss: str = "kl_top", post_norm: bool = False,
+                 max_grad_norm: float | None = None):
         from .synth import Linear, Workload
+        if loss not in LOSSES:
+            raise ValueError(f"unknown loss {loss!r}")
+        self.loss, self.post_norm, self.max_grad_norm = loss, post_norm, max_grad_norm
         hq, hkv = heads
         self.heads, self.D, self.T = heads, head_dim, sum(lengths)
         rows = (hq + 2 * hkv) * head_dim
@@ -306,11 +316,16 @@ class DecoderStack:
         self.cu = torch.tensor([sum(lengths[:i]) for i in range(len(lengths) + 1)], dtype=torch.int32, device=device)
         g = torch.Generator(device="cpu").manual_seed(17)
         self.gain = {n: (1.0 + 0.1 * torch.randn(hidden, generator=g)).to(torch.bfloat16).to(device) for n in ("in", "out")}
+        self.gain["post"] = (1.0 + 0.1 * torch.randn(hidden, generator=g)).to(torch.bfloat16).to(device)
+        self.gate = (0.5 + 0.1 * torch.randn(hidden, generator=g)).to(torch.bfloat16).to(device)
         q = F.qconfig(fmt, self.sb)
         like = lambda h: torch.empty(self.T, h, head_dim, dtype=torch.bfloat16, device="meta")
         sizes = [F.workspace_size(F.CALL_FAKEQUANT_FWD, q), F.workspace_size(F.CALL_KL_TOP, q, self.T, vocab, 0),
                  F.norm_workspace_size(self.T, hidden), F.attention_workspace_size(like(hq), like(hkv), len(lengths)),
-                 F.token_logprobs_workspace_size(self.T, vocab, 1)]
+                 F.token_logprobs_workspace_size(self.T, vocab, 1), F.sandwich_norm_workspace_size(self.T, hidden),
+                 F.clip_grad_norm_workspace_size(2 * len(self.w.linears))]
+        if loss == "ce":
+            sizes.append(F.linear_ce_workspace_size(self.T, vocab, hidden))
         for l in self.w.linears:
             sizes += [F.workspace_size(c, q, self.T, l.N, l.K)
                       for c in (F.CALL_RECON_GEMM_FWD, F.CALL_RECON_GEMM_BWD, F.CALL_RECON_GEMM_DX)]
@@ -336,29 +351,49 @@ class DecoderStack:
         gemm = lambda x, n: F.recon_gemm_fwd(x, L[n].W, None, ws=ws)[0]
         A = F.norm_fwd(X, self.gain["in"], kind=F.NORM_RMS, want_stats=False, ws=ws)[0]
         O, _ = self._attend(gemm(A, "qkv"))
-        B = F.norm_fwd(gemm(O.flatten(1), "o"), self.gain["out"], residual=X, kind=F.NORM_RMS, want_stats=False, ws=ws)[0]
+        B = self._join(X, gemm(O.flatten(1), "o"))[1]
         return gemm(B, "head")
 
-    def _quantised(self, x: torch.Tensor, name: str):
-        """(x_hat, W_hat, x_hat W_hat^T) of one linear."""
+    def _join(self, X: torch.Tensor, Y: torch.Tensor):
+        """(H, B, statistics for the backward) of the residual stream X and the block's output Y."""
+        if self.post_norm:
+            return F.sandwich_norm_fwd(X, Y, self.gain["post"], self.gain["out"], gate=self.gate, kind=F.NORM_RMS, ws=self.ws)
+        B, H, _, rstd = F.norm_fwd(Y, self.gain["out"], residual=X, kind=F.NORM_RMS, ws=self.ws)
+        return H, B, rstd
+
+    def _join_backward(self, s: dict, dB: torch.Tensor) -> torch.Tensor:
+        """Gradient of the block's output from that of B."""
+        if self.post_norm:
+            return F.sandwich_norm_bwd(dB, None, s["X"], s["Y"], self.gain["post"], self.gain["out"], s["rstd"], gate=self.gate,
+                                       kind=F.NORM_RMS, ws=self.ws, out=dB)[1]
+        return F.norm_bwd(dB, s["H"], self.gain["out"], None, s["rstd"], kind=F.NORM_RMS, ws=self.ws, out=dB)[0]
+
+    def _quantised(self, x: torch.Tensor, name: str, product: bool = True):
+        """(x_hat, W_hat, x_hat W_hat^T or None) of one linear."""
         fmt, sb, ws, L = self.w.fmt, self.sb, self.ws, self.layers[name]
         x_hat = F.fakequant_fwd(x, fmt, sb, ws=ws)[0]
         w_hat = F.fakequant_fwd(L.W, fmt, sb, L.s, L.c if self.use_c else None, L.alpha, ws=ws)[0]
-        return x_hat, w_hat, F.recon_gemm_fwd(x_hat, w_hat, None, ws=ws)[0]
+        return x_hat, w_hat, F.recon_gemm_fwd(x_hat, w_hat, None, ws=ws)[0] if product else None
 
-    def student(self, X: torch.Tensor) -> dict:
-        """The quantised stack's forward: every tensor that the backward reads."""
+    def student(self, X: torch.Tensor, logits: bool = True) -> dict:
+        """The quantised stack's forward: every tensor that the backward reads, and the logits Z where they are wanted."""
         s = {"X": X}
         s["A"] = F.norm_fwd(X, self.gain["in"], kind=F.NORM_RMS, want_stats=False, ws=self.ws)[0]
         s["A_hat"], _, s["qkv"] = self._quantised(s["A"], "qkv")
         s["O"], s["lse"] = self._attend(s["qkv"])
-        s["O_hat"], s["Wo_hat"], Y = self._quantised(s["O"].flatten(1), "o")
-        s["B"], s["H"], _, s["rstd"] = F.norm_fwd(Y, self.gain["out"], residual=X, kind=F.NORM_RMS, ws=self.ws)
-        s["B_hat"], s["Wh_hat"], s["Z"] = self._quantised(s["B"], "head")
+        s["O_hat"], s["Wo_hat"], s["Y"] = self._quantised(s["O"].flatten(1), "o")
+        s["H"], s["B"], s["rstd"] = self._join(X, s["Y"])
+        s["B_hat"], s["Wh_hat"], s["Z"] = self._quantised(s["B"], "head", logits)
         return s
 
-    def backward(self, s: dict, dZ: torch.Tensor) -> dict:
-        """Gradients of the scales and coefficients of every linear (and of the fused q-k-v product) from dL/dZ."""
+    def label_loss(self, s: dict, target: torch.Tensor):
+        """(mean cross entropy of the tokens `target`, what its backward needs)."""
+        logp, lse = F.linear_ce_fwd(s["B_hat"], s["Wh_hat"], target, ws=self.ws)
+        return -logp.mean(), (target, lse, torch.full_like(lse, -1.0 / self.T))
+
+    def backward(self, s: dict, dZ: torch.Tensor | None = None, labels: tuple | None = None) -> dict:
+        """Gradients of the scales and coefficients of every linear (and of the fused q-k-v product) from dL/dZ, or from what
+        label_loss gave."""
         fmt, sb, ws = self.w.fmt, self.sb, self.ws
         grads = {}
 
@@ -366,46 +401,65 @@ class DecoderStack:
             L = self.layers[name]
             grads[name] = F.recon_gemm_bwd(dY, x_hat, L.W, fmt, sb, L.s, L.c if self.use_c else None, L.alpha, ws=ws)[:2]
 
-        linear("head", dZ, s["B_hat"])
-        dB = F.fakequant_act_bwd(s["B"], F.recon_gemm_dx(dZ, s["Wh_hat"], ws=ws), fmt, ws=ws)
-        dH, _, _ = F.norm_bwd(dB, s["H"], self.gain["out"], None, s["rstd"], kind=F.NORM_RMS, ws=ws, out=dB)
-        linear("o", dH, s["O_hat"])
-        dO = F.fakequant_act_bwd(s["O"].flatten(1), F.recon_gemm_dx(dH, s["Wo_hat"], ws=ws), fmt, ws=ws)
+        if labels is None:
+            linear("head", dZ, s["B_hat"])
+            dB_hat = F.recon_gemm_dx(dZ, s["Wh_hat"], ws=ws)
+        else:
+            dB_hat, G = F.linear_ce_bwd(s["B_hat"], s["Wh_hat"], *labels, dw_dtype=torch.float32, ws=ws)
+            L = self.layers["head"]
+            grads["head"] = F.fakequant_bwd(G, L.W, fmt, sb, L.s, L.c if self.use_c else None, L.alpha, ws=ws)
+        dB = F.fakequant_act_bwd(s["B"], dB_hat, fmt, ws=ws)
+        dY = self._join_backward(s, dB)
+        linear("o", dY, s["O_hat"])
+        dO = F.fakequant_act_bwd(s["O"].flatten(1), F.recon_gemm_dx(dY, s["Wo_hat"], ws=ws), fmt, ws=ws)
         dqkv = torch.empty_like(s["qkv"])
         F.attention_bwd(dO.view_as(s["O"]), *self._slices(s["qkv"]), s["O"], s["lse"], self.cu, ws=ws, out=self._slices(dqkv))
         linear("qkv", dqkv, s["A_hat"])
         grads["dqkv"] = dqkv
         return grads
 
+    def update(self, grads: dict) -> None:
+        """One AdamW step on the learned scales and coefficients, their gradients scaled to max_grad_norm before."""
+        self.t += 1
+        h, steps = self.hyper, []
+        for name, L in self.layers.items():
+            gs, gc = grads[name]
+            if self.learn_s:
+                steps.append((L.s, gs, L.ms, L.vs, self.t, h.lr_s, h.betas, h.eps, h.weight_decay, h.log2_scales, self.ws))
+            if self.learn_c:
+                steps.append((L.c, gc, L.mc, L.vc, self.t, h.lr_c, h.betas, h.eps, h.weight_decay, h.log2_coeffs, self.ws))
+        if self.max_grad_norm is not None:
+            F.clip_grad_norm([g for _, g, *_ in steps], self.max_grad_norm, ws=self.ws)
+        for step in steps:
+            F.adamw_step(*step)
+
     def run_batch(self, batch: int, learn: bool) -> dict:
-        """One batch: KL-Top, and the scores of the student's logits (one training step when `learn`)."""
+        """One batch: KL-Top, and the scores of the student's logits (one training step when `learn`; on labels that forms no
+        logits of the student, and the cross entropy is all it gives)."""
         X = synth.activation_batch(self.w, "x", batch, self.T, device=self.device)
         Zt = self.teacher(X)
+        target = F.token_logprobs(Zt, None, 1, ws=self.ws)[4][:, 0]
+        if learn and self.loss == "ce":
+            s = self.student(X, logits=False)
+            loss, labels = self.label_loss(s, target.long())
+            self.update(self.backward(s, labels=labels))
+            return {"ce": float(loss)}
         s = self.student(X)
         dZ, loss = F.kl_top(s["Z"], Zt, self.k, ws=self.ws)
-        target = F.token_logprobs(Zt, None, 1, ws=self.ws)[4][:, 0]
         logp, entropy, _, _, first = F.token_logprobs(s["Z"], target.long(), 1, ws=self.ws)
         if learn:
-            self.t += 1
-            h = self.hyper
-            grads = self.backward(s, dZ)
-            for name, L in self.layers.items():
-                gs, gc = grads[name]
-                if self.learn_s:
-                    F.adamw_step(L.s, gs, L.ms, L.vs, self.t, h.lr_s, h.betas, h.eps, h.weight_decay, h.log2_scales, self.ws)
-                if self.learn_c:
-                    F.adamw_step(L.c, gc, L.mc, L.vc, self.t, h.lr_c, h.betas, h.eps, h.weight_decay, h.log2_coeffs, self.ws)
+            self.update(self.backward(s, dZ))
         return {"kl_top": float(loss.item()), "nll": -float(logp.mean()), "entropy": float(entropy.mean()),
                 "agreement": float((first[:, 0] == target).float().mean())}
 
 
 def decoder_epoch(fmt: int, variant: str, steps: int = EPOCH_STEPS, **kw) -> dict:
-    """One epoch of the decoder stack -> held-out scores before and after, and the KL-Top curve."""
+    """One epoch of the decoder stack -> held-out scores before and after, and the curve of its loss."""
     stack = DecoderStack(fmt, variant, **kw)
     before = stack.run_batch(EVAL_STEP, learn=False)
     torch.cuda.synchronize()
     t0 = time.perf_counter()
-    curve = [stack.run_batch(b, learn=True)["kl_top"] for b in range(steps if variant != "rtn" else 0)]
+    curve = [stack.run_batch(b, learn=True)[stack.loss] for b in range(steps if variant != "rtn" else 0)]
     torch.cuda.synchronize()
     seconds = time.perf_counter() - t0
     after = stack.run_batch(EVAL_STEP, learn=False)
@@ -429,7 +483,16 @@ def main() -> None:
     ap.add_argument("--decoder-stack", action="store_true",
                     help="train one attention layer and the output layer of a decoder end to end on KL-Top instead")
     ap.add_argument("--vocab", type=int, default=32000)
+    ap.add_argument("--loss", default=None, choices=LOSSES, help="--decoder-stack: trained on KL-Top (default) or on labels")
+    ap.add_argument("--post-norm", action="store_true",
+                    help="--decoder-stack: the attention's output is normalised and gated before it joins the residual stream")
+    ap.add_argument("--max-grad-norm", type=float, default=None,
+                    help="--decoder-stack: the gradients of a step are scaled together to at most this norm")
     a = ap.parse_args()
+    if not a.decoder_stack and (a.loss is not None or a.post_norm or a.max_grad_norm is not None):
+        ap.error("--loss, --post-norm and --max-grad-norm belong to --decoder-stack")
+    if a.max_grad_norm is not None and not a.max_grad_norm > 0:
+        ap.error("--max-grad-norm is a positive number")
     if a.decoder_stack and (a.kl_top_stack or a.tokens is not None or a.eval_tokens is not None):
         ap.error("--decoder-stack is a loop of its own, on sequences of its own lengths")
     if a.decoder_stack and len(synth.WORKLOADS[a.workload].linears) < 7:
@@ -441,9 +504,11 @@ def main() -> None:
         hidden = w.inputs[w.linears[0].source]
         heads = (w.linears[0].N // 128, w.linears[1].N // 128)
         out = {"stack": f"hidden {hidden}, {heads[0]}/{heads[1]} heads of 128 -> vocab {a.vocab}",
-               "x_kind": a.x_kind or "lowrank", "steps": a.steps, "results": {}}
+               "x_kind": a.x_kind or "lowrank", "steps": a.steps, "loss": a.loss or "kl_top", "post_norm": a.post_norm,
+               "max_grad_norm": a.max_grad_norm, "results": {}}
         for v in a.variants.split(","):
-            r = decoder_epoch(w.fmt, v, a.steps, hidden=hidden, heads=heads, vocab=a.vocab, x_kind=a.x_kind or "lowrank")
+            r = decoder_epoch(w.fmt, v, a.steps, hidden=hidden, heads=heads, vocab=a.vocab, x_kind=a.x_kind or "lowrank",
+                              loss=a.loss or "kl_top", post_norm=a.post_norm, max_grad_norm=a.max_grad_norm)
             out["results"][v] = {"eval_before": r["eval_before"], "eval_after": r["eval_after"], "seconds": round(r["seconds"], 3),
                                  "train_first_last": r["train_curve"][:1] + r["train_curve"][-1:]}
         print(json.dumps(out))

@@ -24,7 +24,7 @@ struct GradGroup {
     uint32_t chunks;
     int count;
 };
-static_assert(sizeof(GradGroup) <= 3968, "the group and a kernel's other arguments fit 4 KB");
+static_assert(sizeof(GradGroup) <= 4032, "the group and a kernel's other arguments fit 4 KB");
 
 // The tensor of a chunk: the last one whose first chunk is not behind it
 __device__ __forceinline__ int tensor_of(const GradGroup &a, uint32_t chunk) {
@@ -78,24 +78,39 @@ __global__ void __launch_bounds__(256) grad_norm_kernel(GradGroup a, double *__r
     if (threadIdx.x == 0) part[blockIdx.x] = lds[0] + lds[1] + lds[2] + lds[3];
 }
 
-// norm and factor from the partial sums, in a fixed order
-__global__ void __launch_bounds__(1024) grad_finish_kernel(const double *__restrict__ part, int64_t parts, double max_norm,
-                                                           double *__restrict__ norm, float *__restrict__ factor, uint32_t *flag) {
-    __shared__ double lds[1024];
+// The norm from the partial sums, in a fixed order, in every thread of a workgroup of 256
+__device__ __forceinline__ double norm_of(const double *__restrict__ part, int64_t parts) {
+    __shared__ double lds[4];
     double s = 0.0;
-    for (int64_t i = threadIdx.x; i < parts; i += 1024) s += part[i];
-    lds[threadIdx.x] = s;
-    __syncthreads();
-    for (int w = 512; w >= 1; w >>= 1) {
-        if ((int)threadIdx.x < w) lds[threadIdx.x] += lds[threadIdx.x + w];
-        __syncthreads();
+    for (int64_t i = threadIdx.x; i < parts; i += 256 * 8) {
+        double v[8];
+#pragma unroll
+        for (int u = 0; u < 8; u++) v[u] = i + 256 * u < parts ? part[i + 256 * u] : 0.0;
+#pragma unroll
+        for (int u = 0; u < 8; u++) s += v[u];
     }
+    for (int m = 32; m >= 1; m >>= 1) s += __shfl_xor(s, m, 64);
+    if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = s;
+    __syncthreads();
+    return sqrt(lds[0] + lds[1] + lds[2] + lds[3]);
+}
+
+__device__ __forceinline__ float factor_of(double norm, double max_norm) {
+    return norm < (double)__builtin_inff() && norm > max_norm ? (float)(max_norm / norm) : 1.0f;
+}
+
+// Writes the norm (one workgroup), and the factor for scaling launches that do not form it themselves
+__device__ __forceinline__ void put_norm(double norm, double *out, uint32_t *flag) {
+    *out = norm;
+    if (!(norm < (double)__builtin_inff())) raise_domain_flag(flag);
+}
+
+__global__ void __launch_bounds__(256) grad_finish_kernel(const double *__restrict__ part, int64_t parts, double max_norm,
+                                                          double *__restrict__ norm, float *__restrict__ factor, uint32_t *flag) {
+    const double x = norm_of(part, parts);
     if (threadIdx.x) return;
-    const double x = sqrt(lds[0]);
-    *norm = x;
-    const bool fine = x < (double)__builtin_inff();  // false for a NaN
-    *factor = fine && x > max_norm ? (float)(max_norm / x) : 1.0f;
-    if (!fine) raise_domain_flag(flag);
+    put_norm(x, norm, flag);
+    *factor = factor_of(x, max_norm);
 }
 
 template <typename T>
@@ -113,8 +128,18 @@ __device__ __forceinline__ void chunk_scale(const T *g, T *out, int64_t start, i
     });
 }
 
-__global__ void __launch_bounds__(256) grad_scale_kernel(GradGroup a, const float *__restrict__ factor) {
-    const float f = *factor;
+// `parts`: the partial sums, of which every workgroup forms the factor itself and the first one writes the norm (a launch less);
+// 0: the factor is there
+__global__ void __launch_bounds__(256) grad_scale_kernel(GradGroup a, const double *__restrict__ part, int64_t parts, double max_norm,
+                                                         double *__restrict__ norm, const float *__restrict__ factor, uint32_t *flag) {
+    float f;
+    if (parts) {
+        const double x = norm_of(part, parts);
+        if (blockIdx.x == 0 && threadIdx.x == 0) put_norm(x, norm, flag);
+        f = factor_of(x, max_norm);
+    } else {
+        f = *factor;
+    }
     for (uint32_t c = blockIdx.x; c < a.chunks; c += gridDim.x) {
         const int i = tensor_of(a, c);
         if (!a.out[i] || (f == 1.0f && a.out[i] == a.g[i])) continue;  // nothing to write
@@ -154,6 +179,7 @@ hipError_t launch_clip_grad_norm(const GradTensor *t, int64_t count, double max_
     float *const factor = reinterpret_cast<float *>(static_cast<char *>(ws) + kWsHeader);
     double *const part = reinterpret_cast<double *>(static_cast<char *>(ws) + 2 * kWsHeader);
     int64_t parts = 0;
+    int groups = 0;
     bool scales = false;
     GradGroup a;
     for (int64_t i = 0; i < count;) {
@@ -162,16 +188,23 @@ hipError_t launch_clip_grad_norm(const GradTensor *t, int64_t count, double max_
         for (int k = 0; k < a.count; k++) scales = scales || a.out[k];
         const unsigned grid = std::min<uint32_t>(a.chunks, kNormParts);
         grad_norm_kernel<<<grid, 256, 0, st>>>(a, part + parts);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
         parts += grid;
+        groups++;
     }
-    grad_finish_kernel<<<1, 1024, 0, st>>>(part, parts, max_norm, norm, factor, flag);
+    const bool alone = scales && groups == 1;  // the one scaling launch finishes the norm as well
+    if (!alone) grad_finish_kernel<<<1, 256, 0, st>>>(part, parts, max_norm, norm, factor, flag);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || !scales) return e;
     for (int64_t i = 0; i < count;) {
         i = next_group(t, i, count, a);
-        if (a.count) grad_scale_kernel<<<std::min<uint32_t>(a.chunks, kNormParts), 256, 0, st>>>(a, factor);
+        if (!a.count) continue;
+        grad_scale_kernel<<<std::min<uint32_t>(a.chunks, kNormParts), 256, 0, st>>>(a, part, alone ? parts : 0, max_norm, norm, factor, flag);
+        e = hipGetLastError();
+        if (e != hipSuccess) return e;
     }
-    return hipGetLastError();
+    return hipSuccess;
 }
 
 }  // namespace focus
