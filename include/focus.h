@@ -557,8 +557,10 @@ focus_status focus_sandwich_norm_bwd(const focus_sandwich_config *cfg, const voi
  *   logp_opt[t] = Z[t][target[t]] - lse[t]; 0 where target[t] < 0 (a token left out)
  *   X [T][K] hidden states, W [V][K] weights (dtype: FOCUS_BF16, FOCUS_F32); products and sums in fp32.
  *   target_opt [T] int64 (NULL: none, logp_opt must be NULL too).
- * The mean cross entropy of n tokens is -sum(logp) / n. X and W have to be finite: a NaN or +inf logit raises the domain
- * flag, as a target >= V does (which is taken as left out); the token's results are then unspecified.
+ * The mean cross entropy of n tokens is -sum(logp) / n. W has to be finite, and X in every token that is not left out: a NaN, or a
+ * largest logit of 2^30 and more in size, raises the domain flag, as a target >= V does (which is taken as left out); the token's
+ * results are then unspecified, as the lse of a token left out is if its X is not finite. lse and logp share no memory with an
+ * input or one another.
  * 0 <= T <= 2^24, 1 <= V <= 2^24, 1 <= K <= 2^20 (FOCUS_ERR_SHAPE); T == 0 is a no-op. bf16 with K % 16 == 0 runs on the matrix
  * instructions. ws: focus_workspace_size(FOCUS_CALL_LINEAR_CE_FWD, NULL, T, V, K) bytes; it serves fewer tokens too. */
 focus_status focus_linear_ce_fwd(const void *X, const void *W, int dtype, int64_t T, int64_t V, int64_t K,
@@ -575,7 +577,8 @@ focus_status focus_linear_ce_fwd(const void *X, const void *W, int dtype, int64_
  *   dX_opt [T][K] (dtype), dW_opt [V][K] (dw_dtype: FOCUS_F32, or FOCUS_BF16 with bf16 operands): overwritten, one of them is
  *   wanted at least. dW in fp32 is the G of focus_fakequant_bwd. With T == 0 dW is zeros.
  * p carries the rounding of lse, 2^-24 |lse| of it; a token with |lse| above 65,536 (or NaN) and a gradient other than 0 raises
- * the domain flag. They share no memory with an input or one another.
+ * the domain flag. A token without a gradient (left out or d_logp 0, and no d_lse or that 0) adds nothing, whatever its X and lse
+ * hold, NaN too; its row of dX is zeros. dX and dW share no memory with an input or one another.
  * ws: focus_workspace_size(FOCUS_CALL_LINEAR_CE_BWD, NULL, T, V, K) bytes; it serves fewer tokens too. */
 focus_status focus_linear_ce_bwd(const void *X, const void *W, int dtype, int64_t T, int64_t V, int64_t K,
                                  const int64_t *target_opt, const float *lse, const float *d_logp_opt,
@@ -596,7 +599,8 @@ typedef struct {
  *   norm = sqrt(sum over all elements of grad^2)  -> *norm_out (device fp64)
  *   out = grad * max_norm / norm where norm > max_norm, else grad               (rounded to the tensor's dtype)
  *   tensors: HOST array of n_tensors entries (0 .. 2^20), read during the call. max_norm > 0 (may be infinite; else FOCUS_ERR_CONFIG).
- *   An out shares no memory with any other tensor's grad or out, nor with a part of its own grad (FOCUS_ERR_SHAPE).
+ *   An out shares no memory with any other tensor's grad or out, nor with a part of its own grad, norm_out with none of them
+ *   (FOCUS_ERR_SHAPE).
  * Squares are formed and summed in fp64, in a fixed order: no size of a gradient overflows. A norm that is not finite raises the
  * domain flag and scales by 1. ws: focus_workspace_size(FOCUS_CALL_CLIP_GRAD_NORM, NULL, n_tensors, 0, 0) bytes. */
 focus_status focus_clip_grad_norm(const focus_grad_tensor *tensors, int64_t n_tensors, double max_norm, double *norm_out,

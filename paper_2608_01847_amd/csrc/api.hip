@@ -828,6 +828,8 @@ focus_status focus_linear_ce_fwd(const void *X, const void *W, int dtype, int64_
     FOCUS_TRY(check_linear_ce(T, V, K));
     if (T > 0 && (!X || !W || !lse || (logp_opt && !target_opt))) return FOCUS_ERR_NULL;
     if (!all_aligned({X, W}) || !aligned_to({logp_opt, lse}, 4) || !aligned_to({target_opt}, 8)) return FOCUS_ERR_SHAPE;
+    const int64_t e = dtype == FOCUS_BF16 ? 2 : 4;
+    if (clash({{logp_opt, T * 4}, {lse, T * 4}}, {{X, T * K * e}, {W, V * K * e}, {target_opt, T * 8}}, false)) return FOCUS_ERR_SHAPE;
     FOCUS_TRY(check_ws(ws, ws_bytes, linear_ce_fwd_ws(T, V)));
     if (T == 0) return FOCUS_OK;
     return hip_status(launch_linear_ce_fwd(dtype, X, W, T, V, K, target_opt, logp_opt, lse, flag_of(ws), ws, (hipStream_t)stream));
@@ -866,6 +868,7 @@ focus_status focus_clip_grad_norm(const focus_grad_tensor *tensors, int64_t n_te
         if (t.reserved != 0) return FOCUS_ERR_CONFIG;
         if (t.n < 0 || t.n > kMaxGradElems || !all_aligned({t.grad, t.out})) return FOCUS_ERR_SHAPE;
         if (t.n > 0 && !t.grad) return FOCUS_ERR_NULL;
+        if (meet({norm_out, sizeof(double)}, grad_span(t, t.grad)) || meet({norm_out, sizeof(double)}, grad_span(t, t.out))) return FOCUS_ERR_SHAPE;
     }
     constexpr int kOnStack = 1024;
     int32_t few[kOnStack];

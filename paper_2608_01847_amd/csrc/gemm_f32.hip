@@ -507,25 +507,35 @@ __global__ void __launch_bounds__(256) ce_stats_f32_kernel(CeArgs a) {
 }
 
 // D of the piece, [T][pitch] for dW and transposed, [entries][pitch_t], for dX: each product reads its operand along the reduction.
-// The pitches are multiples of 4; what lies between a row's end and its pitch is not read into a result.
+// The pitches are multiples of 4; what lies between a row's end and its pitch is not read into a result. The workgroups of a token
+// tile share the copy of X (for dW; a launch of its own would cost 4 us).
 template <int T>
-__global__ void __launch_bounds__(256) ce_grad_f32_kernel(CeArgs a, float *__restrict__ Dt, int64_t pitch_t, uint32_t *flag) {
+__global__ void __launch_bounds__(256) ce_grad_f32_kernel(CeArgs a, float *__restrict__ Dt, int64_t pitch_t, float *__restrict__ x,
+                                                          uint32_t *flag) {
     __shared__ __attribute__((aligned(16))) char smem[f32_fwd_lds(T)];
     const uint32_t id = xcd_tile(blockIdx.x, gridDim.x), tiles_t = gridDim.x / (uint32_t)a.tiles_v;
     const int64_t c0 = (int64_t)(id / tiles_t) * T, v0 = a.v0 + c0, t0 = a.t0 + (int64_t)(id % tiles_t) * T;
     F32Tile<T> tile;
     f32_products<T>(static_cast<const float *>(a.W), static_cast<const float *>(a.X), a.V, a.T, a.K, v0, t0, smem, tile);
+    if (x) {
+        const int64_t fours = a.K / 4, n = std::min<int64_t>(T, a.T - t0) * fours;
+        const float4 *const from = reinterpret_cast<const float4 *>(static_cast<const float *>(a.X) + t0 * a.K);
+        for (int64_t i = (int64_t)(id / tiles_t) * 256 + threadIdx.x; i < n; i += (int64_t)a.tiles_v * 256)
+            reinterpret_cast<float4 *>(x + t0 * a.K)[i] =
+                ce_takes_part(a.target, a.g, a.h, a.V, t0 + i / fours) ? from[i] : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    }
     const int64_t t = t0 + tile.col();
     if (t >= a.T) return;
     const int64_t want = a.target ? a.target[t] : -1;
     const float g = a.g && want >= 0 && want < a.V ? a.g[t] : 0.0f, h = a.h ? a.h[t] : 0.0f, lse = a.lse[t];
+    const bool none = g == 0.0f && h == 0.0f;
     if (want >= a.V || ((g != 0.0f || h != 0.0f) && !(__builtin_fabsf(lse) <= 65536.0f))) raise_domain_flag(flag);
     float *const D = static_cast<float *>(a.D);
 #pragma unroll
     for (int r = 0; r < F32Tile<T>::R; r++) {
         const int64_t c = c0 + tile.row(r), v = a.v0 + c;
         if (v >= a.V || c >= a.pitch) continue;
-        const float d = (v == want ? g : 0.0f) + (h - g) * expf((float)tile.o[r] - lse);
+        const float d = none ? 0.0f : (v == want ? g : 0.0f) + (h - g) * expf((float)tile.o[r] - lse);
         D[t * a.pitch + c] = d;
         Dt[c * pitch_t + t] = d;
     }
@@ -548,11 +558,11 @@ void launch_ce_stats_f32(const CeArgs &a, int64_t edge, int64_t tokens, hipStrea
     else ce_stats_f32_kernel<32><<<grid, 256, 0, st>>>(a);
 }
 
-void launch_ce_grad_f32(const CeArgs &a, int64_t edge, int64_t tokens, float *Dt, int64_t pitch_t, uint32_t *flag,
-                        hipStream_t st) {
+void launch_ce_grad_f32(const CeArgs &a, int64_t edge, int64_t tokens, float *Dt, int64_t pitch_t, float *x,
+                        uint32_t *flag, hipStream_t st) {
     const unsigned grid = (unsigned)((tokens + edge - 1) / edge) * (unsigned)a.tiles_v;
-    if (edge == 64) ce_grad_f32_kernel<64><<<grid, 256, 0, st>>>(a, Dt, pitch_t, flag);
-    else ce_grad_f32_kernel<32><<<grid, 256, 0, st>>>(a, Dt, pitch_t, flag);
+    if (edge == 64) ce_grad_f32_kernel<64><<<grid, 256, 0, st>>>(a, Dt, pitch_t, x, flag);
+    else ce_grad_f32_kernel<32><<<grid, 256, 0, st>>>(a, Dt, pitch_t, x, flag);
 }
 
 hipError_t launch_dw_f32(const float *dY, const float *X, int64_t M, int64_t N, int64_t ldy, int64_t K, int64_t chunk,

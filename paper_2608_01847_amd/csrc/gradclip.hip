@@ -95,8 +95,11 @@ __device__ __forceinline__ double norm_of(const double *__restrict__ part, int64
     return sqrt(lds[0] + lds[1] + lds[2] + lds[3]);
 }
 
-__device__ __forceinline__ float factor_of(double norm, double max_norm) {
-    return norm < (double)__builtin_inff() && norm > max_norm ? (float)(max_norm / norm) : 1.0f;
+// The factor as a product x y of two: y = 2^-100 where it is so small that fp32 would lose its digits
+__device__ __forceinline__ float2 factor_of(double norm, double max_norm) {
+    if (!(norm < (double)__builtin_inff() && norm > max_norm)) return make_float2(1.0f, 1.0f);
+    const double f = max_norm / norm;
+    return f < 0x1p-100 ? make_float2((float)(f * 0x1p100), 0x1p-100f) : make_float2((float)f, 1.0f);
 }
 
 // Writes the norm (one workgroup), and the factor for scaling launches that do not form it themselves
@@ -106,7 +109,7 @@ __device__ __forceinline__ void put_norm(double norm, double *out, uint32_t *fla
 }
 
 __global__ void __launch_bounds__(256) grad_finish_kernel(const double *__restrict__ part, int64_t parts, double max_norm,
-                                                          double *__restrict__ norm, float *__restrict__ factor, uint32_t *flag) {
+                                                          double *__restrict__ norm, float2 *__restrict__ factor, uint32_t *flag) {
     const double x = norm_of(part, parts);
     if (threadIdx.x) return;
     put_norm(x, norm, flag);
@@ -114,7 +117,7 @@ __global__ void __launch_bounds__(256) grad_finish_kernel(const double *__restri
 }
 
 template <typename T>
-__device__ __forceinline__ void chunk_scale(const T *g, T *out, int64_t start, int64_t n, float f) {
+__device__ __forceinline__ void chunk_scale(const T *g, T *out, int64_t start, int64_t n, float2 f) {
     Raw8<T> v[kChunk / 2048];
     int j = 0;
     pieces(start, n, [&](int64_t c, int m) { v[j++].load(g + c, m); });
@@ -122,7 +125,7 @@ __device__ __forceinline__ void chunk_scale(const T *g, T *out, int64_t start, i
     pieces(start, n, [&](int64_t c, int m) {
         float x[8];
 #pragma unroll
-        for (int e = 0; e < 8; e++) x[e] = v[j][e] * f;
+        for (int e = 0; e < 8; e++) x[e] = v[j][e] * f.x * f.y;
         j++;
         store8_n(out + c, m, x);
     });
@@ -131,8 +134,8 @@ __device__ __forceinline__ void chunk_scale(const T *g, T *out, int64_t start, i
 // `parts`: the partial sums, of which every workgroup forms the factor itself and the first one writes the norm (a launch less);
 // 0: the factor is there
 __global__ void __launch_bounds__(256) grad_scale_kernel(GradGroup a, const double *__restrict__ part, int64_t parts, double max_norm,
-                                                         double *__restrict__ norm, const float *__restrict__ factor, uint32_t *flag) {
-    float f;
+                                                         double *__restrict__ norm, const float2 *__restrict__ factor, uint32_t *flag) {
+    float2 f;
     if (parts) {
         const double x = norm_of(part, parts);
         if (blockIdx.x == 0 && threadIdx.x == 0) put_norm(x, norm, flag);
@@ -142,7 +145,7 @@ __global__ void __launch_bounds__(256) grad_scale_kernel(GradGroup a, const doub
     }
     for (uint32_t c = blockIdx.x; c < a.chunks; c += gridDim.x) {
         const int i = tensor_of(a, c);
-        if (!a.out[i] || (f == 1.0f && a.out[i] == a.g[i])) continue;  // nothing to write
+        if (!a.out[i] || (f.x == 1.0f && a.out[i] == a.g[i])) continue;  // nothing to write
         const int64_t start = (int64_t)(c - a.first[i]) * kChunk;
         if (a.bf16[i / 32] >> (i % 32) & 1u)
             chunk_scale(static_cast<const uint16_t *>(a.g[i]), static_cast<uint16_t *>(a.out[i]), start, a.n[i], f);
@@ -176,7 +179,7 @@ size_t clip_grad_norm_ws(int64_t tensors) {
 
 hipError_t launch_clip_grad_norm(const GradTensor *t, int64_t count, double max_norm, double *norm, uint32_t *flag, void *ws,
                                  hipStream_t st) {
-    float *const factor = reinterpret_cast<float *>(static_cast<char *>(ws) + kWsHeader);
+    float2 *const factor = reinterpret_cast<float2 *>(static_cast<char *>(ws) + kWsHeader);
     double *const part = reinterpret_cast<double *>(static_cast<char *>(ws) + 2 * kWsHeader);
     int64_t parts = 0;
     int groups = 0;

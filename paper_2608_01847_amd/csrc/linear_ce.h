@@ -10,6 +10,8 @@ constexpr int kCeFew = 16;    // tokens up to which the forward reads the weight
 constexpr int kCeFewV = 128;  // vocabulary entries of its workgroups
 constexpr int64_t kCeMostWidth = int64_t(1) << 20;  // of a piece of the vocabulary
 
+constexpr float kCeMostLogit = 1073741824.0f;       // 2^30: a token whose largest logit reaches that in size raises the domain flag
+
 struct CeArgs {
     const void *X, *W;
     const int64_t *target;
@@ -23,17 +25,23 @@ struct CeArgs {
     int tiles_v;
 };
 
+// Whether token t has a gradient. One without it takes no part in the sums whatever its row of X and its lse hold, NaN too.
+__device__ __forceinline__ bool ce_takes_part(const int64_t *target, const float *g, const float *h, int64_t V, int64_t t) {
+    return (g && target[t] >= 0 && target[t] < V && g[t] != 0.0f) || (h && h[t] != 0.0f);
+}
+
 // Logit tiles on the matrix instructions (bf16, K a multiple of 16), of edge x edge: those of `tokens` tokens from a.t0 on
 int64_t ce_mfma_tile(int64_t T, int64_t n);
 void launch_ce_stats_mfma(const CeArgs &a, int64_t edge, int64_t tokens, hipStream_t st);
 void launch_ce_stats_few(const CeArgs &a, hipStream_t st);  // T <= kCeFew
 void launch_ce_grad_mfma(const CeArgs &a, int64_t edge, int64_t tokens, uint32_t *flag, hipStream_t st);
 
-// The same on the fp32 matrix instructions (K a multiple of 16), tiles of edge x edge; D's transpose, [entries][pitch_t], goes to Dt
+// The same on the fp32 matrix instructions (K a multiple of 16), tiles of edge x edge; D's transpose, [entries][pitch_t], goes to Dt;
+// with x, the rows of X that have a gradient go there, zeros in place of the others
 bool ce_f32_supported(int64_t T, int64_t V, int64_t K);
 int64_t ce_f32_tile(int64_t T, int64_t n);
 void launch_ce_stats_f32(const CeArgs &a, int64_t edge, int64_t tokens, hipStream_t st);
-void launch_ce_grad_f32(const CeArgs &a, int64_t edge, int64_t tokens, float *Dt, int64_t pitch_t, uint32_t *flag,
+void launch_ce_grad_f32(const CeArgs &a, int64_t edge, int64_t tokens, float *Dt, int64_t pitch_t, float *x, uint32_t *flag,
                         hipStream_t st);
 // out [splits][N][K] = dY^T X over `chunk` rows (a multiple of 32) of dY [M][ldy] (ldy a multiple of 4) and X [M][K] each
 hipError_t launch_dw_f32(const float *dY, const float *X, int64_t M, int64_t N, int64_t ldy, int64_t K, int64_t chunk,

@@ -127,9 +127,9 @@ __global__ void __launch_bounds__(256) ce_join_kernel(CeArgs a, int tiles, int t
     if (t >= a.T || lane != 0) return;
     const float ls = logf(s);
     a.lse[t] = m + ls;
-    bool bad = !(s < __builtin_inff()) || !(__builtin_fabsf(m) < __builtin_inff());
+    const int64_t want = a.target ? a.target[t] : 0;  // a token left out raises nothing
+    bool bad = want >= 0 && (!(s < __builtin_inff()) || !(__builtin_fabsf(m) < kCeMostLogit));
     if (a.logp) {
-        const int64_t want = a.target[t];
         const bool there = want >= 0 && want < a.V;
         bad = bad || want >= a.V;
         a.logp[t] = there ? (a.zt[t] - m) - ls : 0.0f;
@@ -153,27 +153,29 @@ __global__ void __launch_bounds__(256) ce_grad_kernel(CeArgs a, uint32_t *flag) 
         const int64_t want = a.target ? a.target[t] : -1;
         const bool there = want >= 0 && want < a.V;
         const float g = a.g && there ? a.g[t] : 0.0f, h = a.h ? a.h[t] : 0.0f, lse = a.lse[t];
+        const bool none = g == 0.0f && h == 0.0f;
         bad = bad || want >= a.V || ((g != 0.0f || h != 0.0f) && !(__builtin_fabsf(lse) <= 65536.0f));
 #pragma unroll
         for (int j = 0; j < 4; j++) {
             const int64_t v = v0 + tx * 4 + j;
             if (v - a.v0 >= a.pitch) continue;
             const float p = expf(acc[i][j] - lse);
-            static_cast<float *>(a.D)[t * a.pitch + (v - a.v0)] = v < a.V ? (v == want ? g : 0.0f) + (h - g) * p : 0.0f;
+            static_cast<float *>(a.D)[t * a.pitch + (v - a.v0)] = v < a.V && !none ? (v == want ? g : 0.0f) + (h - g) * p : 0.0f;
         }
     }
     if (bad) raise_domain_flag(flag);
 }
 
 // C[m][n] = before[m][n] + sum_r A(m, r) B[r][n] in fp32, 64 x 64 per workgroup, A(m, r) at A[m am + r ar]; written to
-// `sums` in fp32, or to `out` in its type.
+// `sums` in fp32, or to `out` in its type. rows: row r of B is token r's, zeros where that has no gradient.
 struct CeProduct {
-    const float *A, *before;
+    const float *A, *before, *g, *h;
+    const int64_t *target;
     const void *B;
     float *sums;
     void *out;
-    int64_t am, ar, M, N, R, m0;
-    int b_dtype, out_dtype, tiles_n;
+    int64_t am, ar, M, N, R, m0, V;
+    int b_dtype, out_dtype, tiles_n, rows;
 };
 __global__ void __launch_bounds__(256) ce_product_kernel(CeProduct a) {
     __shared__ float As[16][68];
@@ -186,7 +188,8 @@ __global__ void __launch_bounds__(256) ce_product_kernel(CeProduct a) {
             const bool along_m = a.am == 1;
             const int m = along_m ? i % 64 : i / 16, ra = along_m ? i / 64 : i % 16, n = i % 64, rb = i / 64;
             As[ra][m] = m0 + m < a.M && r0 + ra < a.R ? a.A[(m0 + m) * a.am + (r0 + ra) * a.ar] : 0.0f;
-            Bs[rb][n] = n0 + n < a.N && r0 + rb < a.R ? load1(a.B, a.b_dtype, (r0 + rb) * a.N + n0 + n) : 0.0f;
+            const bool real = n0 + n < a.N && r0 + rb < a.R && (!a.rows || ce_takes_part(a.target, a.g, a.h, a.V, r0 + rb));
+            Bs[rb][n] = real ? load1(a.B, a.b_dtype, (r0 + rb) * a.N + n0 + n) : 0.0f;
         }
         __syncthreads();
 #pragma unroll
@@ -397,16 +400,20 @@ Splits f32_splits(int64_t R, int64_t N, int64_t K) {
 }
 
 struct F32Space {
-    float *sums, *part, *D, *Dt;
+    float *sums, *part, *x, *D, *Dt;
 };
 size_t f32_space(int64_t T, int64_t V, int64_t K, char *base, F32Space *s) {
-    const size_t sums = round256((size_t)T * (size_t)K * sizeof(float));
+    const size_t x = round256((size_t)T * (size_t)K * sizeof(float)), part = sums_bytes(T, V, K);
     const size_t D = round256(piece_bytes((T + 3) / 4 * 4, V, sizeof(float)));  // transposed too, its rows of whole fours
-    char *const at = base + kWsHeader;
-    if (s)
-        *s = F32Space{reinterpret_cast<float *>(at), reinterpret_cast<float *>(at + sums), reinterpret_cast<float *>(at + sums + sums_bytes(T, V, K)),
-                      reinterpret_cast<float *>(at + sums + sums_bytes(T, V, K) + D)};
-    return kWsHeader + sums + sums_bytes(T, V, K) + 2 * D;
+    size_t at = kWsHeader;
+    auto take = [&](size_t bytes) {
+        float *p = reinterpret_cast<float *>(base + at);
+        at += bytes;
+        return p;
+    };
+    float *const sums = take(x), *const parts = take(part), *const rows = take(x), *const d = take(D), *const dt = take(D);
+    if (s) *s = F32Space{sums, parts, rows, d, dt};
+    return at;
 }
 
 hipError_t bwd_f32(CeArgs a, float *dX, float *dW, uint32_t *flag, char *ws, hipStream_t st) {
@@ -424,7 +431,7 @@ hipError_t bwd_f32(CeArgs a, float *dX, float *dW, uint32_t *flag, char *ws, hip
         a.v0 = v0, a.pitch = (n + 3) / 4 * 4, a.tiles_v = (int)cdiv(n, edge);
         hipError_t e = in_runs(cdiv(T, edge), a.tiles_v, [&](int64_t first, int64_t count) {
             a.t0 = first * edge;
-            launch_ce_grad_f32(a, edge, count * edge, s.Dt, pitch_t, flag, st);
+            launch_ce_grad_f32(a, edge, count * edge, s.Dt, pitch_t, dW && v0 == 0 ? s.x : nullptr, flag, st);
         });
         if (e != hipSuccess) return e;
         if (dX) {
@@ -437,7 +444,7 @@ hipError_t bwd_f32(CeArgs a, float *dX, float *dW, uint32_t *flag, char *ws, hip
         if (dW) {
             const Splits p = f32_splits(T, n, K);
             float *const out = dW + v0 * K;
-            e = launch_dw_f32(s.D, static_cast<const float *>(a.X), T, n, a.pitch, K, p.chunk, p.count, p.count == 1 ? out : s.part, st);
+            e = launch_dw_f32(s.D, s.x, T, n, a.pitch, K, p.chunk, p.count, p.count == 1 ? out : s.part, st);
             if (e == hipSuccess && p.count > 1) e = finish(p.count, nullptr, n * K, nullptr, out);
             if (e != hipSuccess) return e;
         }
@@ -577,7 +584,7 @@ hipError_t launch_linear_ce_bwd(int dtype, const void *X, const void *W, int64_t
         if (dW) {
             CeProduct p{};
             p.A = static_cast<const float *>(a.D), p.am = 1, p.ar = n, p.M = n, p.N = K, p.R = T, p.b_dtype = dtype, p.out_dtype = dw_dtype;
-            p.B = X;
+            p.B = X, p.rows = 1, p.target = target, p.g = g, p.h = h, p.V = V;
             p.out = static_cast<char *>(dW) + (size_t)v0 * (size_t)K * dsz;
             e = product(p, st);
             if (e != hipSuccess) return e;

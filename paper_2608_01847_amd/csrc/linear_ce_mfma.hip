@@ -223,9 +223,8 @@ __global__ void __launch_bounds__(kThreads, E == 256 ? 1 : 2) ce_grad_mfma_kerne
         const float g = a.g && want >= 0 && want < a.V ? a.g[t] : 0.0f, h = a.h && real ? a.h[t] : 0.0f;
         const float lse = real ? a.lse[t] : 0.0f, scale = real ? a.scale[t] : 0.0f;
         bad = bad || want >= a.V || ((g != 0.0f || h != 0.0f) && !(__builtin_fabsf(lse) <= 65536.0f));
-        const float inv = scale > 0.0f ? 1.0f / scale : 0.0f;
-        const Exponent e(lse);
-        const float by = (h - g) * inv * e.factor, hit = g * inv;
+        const Exponent e(lse);  // quotients: the inverse of a tiny scale would overflow
+        const float by = (h - g) / scale * e.factor, hit = g / scale;
         static_for<N>([&](auto i) { static_for<16>([&](auto r) { acc[i][j][(int)r] = by * e(acc[i][j][(int)r]); }); });
         int at;
         if (target_near<E>(want, v0, at)) {
@@ -233,6 +232,12 @@ __global__ void __launch_bounds__(kThreads, E == 256 ? 1 : 2) ce_grad_mfma_kerne
                 static_for<16>([&](auto r) {
                     if (at == entry_of<E>(i, r)) acc[i][j][(int)r] += hit;
                 });
+            });
+        }
+        const bool none = scale == 0.0f;  // no gradient (or no token), whatever X and lse hold
+        if (__any(none)) {
+            static_for<N>([&](auto i) {
+                static_for<16>([&](auto r) { acc[i][j][(int)r] = none ? 0.0f : acc[i][j][(int)r]; });
             });
         }
     });

@@ -78,6 +78,12 @@ def test_sizes_whose_squares_fp32_does_not_hold(F, scale):
     check(F, make([(5000, F32), (4097, BF)], 4, scale), 0.5 * scale)
 
 
+def test_factors_smaller_than_the_normal_numbers(F):
+    grads = make([(1000, F32), (5000, BF)], 5, 1e36)
+    check(F, grads, 1e-4)
+    check(F, make([(1000, F32), (5000, BF)], 5, 1e36), 1e-4, out=[torch.empty_like(g) for g in grads])
+
+
 def test_counted_only(F):
     announce("clip counted only")
     grads = make([(1000, F32), (1000, BF), (1000, F32)], 5)

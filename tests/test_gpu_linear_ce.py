@@ -204,6 +204,68 @@ def test_bad_targets_and_logits_raise_the_flag(F):
     assert F.check_flags(ws) == F.ERR_DOMAIN
 
 
+@pytest.mark.parametrize("dt,K", [("bf16", 64), ("bf16", 24), ("f32", 64), ("f32", 24)])
+def test_tokens_without_a_gradient_may_hold_anything(F, dt, K):
+    announce(f"linear ce padding {dt} K={K}")
+    X, W, target, g, _ = make(300, 700, K, DT[dt], 29)
+    ws = F.workspace(F.linear_ce_workspace_size(300, 700, K))
+    logp, lse = F.linear_ce_fwd(X, W, target, ws=ws)
+    g[10:14] = 0.0
+    out = target < 0
+    out[10:14] = True
+    want = F.linear_ce_bwd(X, W, target, lse, g, ws=ws)
+    bad = torch.tensor([math.nan, math.inf, -math.inf], device="cuda", dtype=X.dtype)
+    Y, at = X.clone(), torch.nonzero(out)[:, 0]
+    Y[at] = bad[at % 3][:, None]
+    Z = torch.where((target < 0)[:, None], Y, X)
+    a, rest = F.linear_ce_fwd(Z, W, target, ws=ws)
+    assert F.check_flags(ws) == F.OK and torch.equal(a, logp) and torch.equal(rest[target >= 0], lse[target >= 0])
+    lse[out] = math.nan
+    got = F.linear_ce_bwd(Y, W, target, lse, g, ws=ws)
+    assert F.check_flags(ws) == F.OK and all(torch.equal(x, y) for x, y in zip(got, want))
+    assert not got[0][out].any()
+    F.linear_ce_fwd(Z, W, None, ws=ws)  # every token counts
+    assert F.check_flags(ws) == F.ERR_DOMAIN
+
+
+def test_gradients_smaller_than_the_normal_numbers(F):
+    # fp32 results below 2^-126 have steps of 2^-149, bf16 ones of 2^-133; apart from that the bounds are those of any size
+    announce("linear ce tiny")
+    X, W, target, _, _ = make(200, 300, 64, torch.bfloat16, 30)
+    g = -(1.0 + torch.rand(200, generator=torch.Generator().manual_seed(31)).cuda()) * 2.0 ** -127
+    _, lse = F.linear_ce_fwd(X, W, target)
+    dX, dW = F.linear_ce_bwd(X, W, target, lse, g, dw_dtype=torch.float32)
+    _, rlse, D, rdX, rdW, S = reference(X, W, target, g, None)
+    terms = 2 * 2.0 ** -8 + 2 * (z_error(64, S) + 2.0 ** -20 + 2.0 ** -23 * float(rlse.abs().max())) + 1e-5
+    for got, ref, mags, step in ((dX, rdX, D.abs() @ W.double().abs(), 2.0 ** -133), (dW, rdW, D.abs().t() @ X.double().abs(), 2.0 ** -149)):
+        err = (got.double() - ref).abs()
+        assert (err <= terms * mags + 2.0 ** -8 * ref.abs() + step).all(), float(err.max())
+
+
+@pytest.mark.parametrize("dt,T,K", [("bf16", 4, 32), ("bf16", 20, 32), ("bf16", 600, 32), ("bf16", 20, 24), ("f32", 20, 32), ("f32", 20, 24)])
+def test_the_largest_logits(F, dt, T, K):
+    # one product each, so that logits are exact; neighbours differ by 2^15 and more, so that lse is the largest
+    announce(f"linear ce largest {dt} T={T} K={K}")
+    g = torch.Generator().manual_seed(32)
+    X = torch.zeros(T, K)
+    X[:, 0] = 2.0 ** 15
+    W = torch.zeros(500, K)
+    W[:, 0] = torch.randint(-127, 128, (500,), generator=g) * 2.0 ** 7
+    W[77, 0] = 2.0 ** 14
+    target = torch.randint(0, 500, (T,), generator=g)
+    ws = F.workspace(F.linear_ce_workspace_size(T, 500, K))
+    for sign in (1.0, -1.0):  # the other sign: the least logit in size is the largest
+        x, w = (sign * X).to(DT[dt]).cuda(), W.to(DT[dt]).cuda()
+        z = (x.double() @ w.double().t())
+        logp, lse = F.linear_ce_fwd(x, w, target.cuda(), ws=ws)
+        m = z.max(1).values
+        assert F.check_flags(ws) == F.OK
+        assert ((lse.double() - m).abs() <= 2.0 + 2.0 ** -24 * m.abs()).all()
+        assert ((logp.double() - (z.gather(1, target.cuda()[:, None])[:, 0] - m)).abs() <= 2.0 + 2.0 ** -22 * m.abs()).all()
+    F.linear_ce_fwd(2.0 * X.to(DT[dt]).cuda(), w, target.cuda(), ws=ws)
+    assert F.check_flags(ws) == F.ERR_DOMAIN
+
+
 def test_pieces_of_the_vocabulary(F):
     # tokens enough that the vocabulary takes several pieces, the last one odd
     T, V, K = 40000, 21013, 32

@@ -89,6 +89,8 @@ def test_linear_ce_checks(L, cpu_only):
                            (F.ERR_WORKSPACE, {"size": 256})):
             assert call(L, **kw) == status, (call, kw)
     assert ce_fwd(L, T=0, X=None, lse=None) == F.OK
+    for kw in ({"lse": at(3)}, {"lse": at(0)}, {"lse": at(1)}, {"logp": at(2)}, {"logp": ctypes.c_void_p(at(4).value + 8)}):
+        assert ce_fwd(L, **kw) == F.ERR_SHAPE, kw
     for status, kw in ((F.ERR_NULL, {"g": None}), (F.ERR_NULL, {"dX": None, "dW": None}), (F.ERR_DTYPE, {"wdt": 7}),
                        (F.ERR_DTYPE, {"dt": 0, "wdt": 1}), (F.ERR_SHAPE, {"dX": at(0)}), (F.ERR_SHAPE, {"dW": at(1)}),
                        (F.ERR_SHAPE, {"dW": at(6)}), (F.ERR_SHAPE, {"dX": ctypes.c_void_p(at(4).value)}), (F.OK, {"T": 0, "dW": None})):
@@ -133,6 +135,8 @@ def test_clip_checks(L, cpu_only):
                              (F.ERR_SHAPE, [ok, ok], {}), (F.ERR_SHAPE, [(at(0), at(2), 100, 0, 0), (at(1), within(2, 384), 100, 0, 0)], {}),
                              (F.ERR_SHAPE, [(at(0), within(1, 16), 100, 0, 0), (at(1), None, 100, 0, 0)], {}),
                              (F.ERR_SHAPE, [(at(1), at(1), 100, 0, 0), (at(0), at(1), 1, 0, 0)], {}),
+                             (F.ERR_SHAPE, [(at(8), None, 2, 0, 0)], {}), (F.ERR_SHAPE, [ok], {"norm": within(0, 392)}),
+                             (F.ERR_SHAPE, [(at(0), at(8), 1, 1, 0)], {}),
                              (F.ERR_SHAPE, [(at(0), within(0, 16), 100, 0, 0)], {}), (F.ERR_WORKSPACE, [ok], {"ws": None}),
                              (F.ERR_WORKSPACE, [ok], {"size": 512})):
         assert clip(L, args, **kw) == status, (args, kw)
