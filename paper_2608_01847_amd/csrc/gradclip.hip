@@ -2,8 +2,8 @@
 // out = g min(1, max_norm / norm).
 //
 // HBM-bound: every gradient is read once for the norm and once more to be scaled. Squares are summed in fp64, so that neither
-// the size of a gradient (1e-30 or 1e30) nor their number costs digits. Up to kGroup tensors travel in the arguments of a launch; a
-// group's elements are numbered in chunks of one tensor each, which the workgroups take in turn.
+// the size of a gradient (1e-30 or 1e30) nor their number costs digits. The tensors travel in the arguments of a launch, as many as
+// these hold; a group's elements are numbered in chunks of one tensor each, which the workgroups take in turn.
 #include "internal.h"
 #include "ops_device.h"
 
@@ -11,23 +11,28 @@ namespace focus {
 
 namespace {
 
-constexpr int kGroup = 112;             // tensors of a launch: 28 bytes each of the 4 KB that a kernel's arguments have
 constexpr int kChunk = 8192;            // elements
 constexpr int kNormParts = 2048;        // workgroups of a launch at most, each with one partial sum
 
+// Tensors of a launch, as many as fit the 4 KB that a kernel's arguments have: 14 bytes each, or 22 with outputs of their own. 252
+// tensors of 169 MB in 3 launches 122 us a pass; with 28 bytes each, in 7, 136.
+template <bool OUT>
 struct GradGroup {
-    const void *g[kGroup];
-    void *out[kGroup];
-    int64_t n[kGroup];
-    uint32_t first[kGroup];             // first chunk of each tensor
-    uint32_t bf16[(kGroup + 31) / 32];  // a bit per tensor
-    uint32_t chunks;
+    static constexpr int kMost = OUT ? 180 : 280;
+    const void *g[kMost];
+    void *out[OUT ? kMost : 1];
+    uint32_t first[kMost + 1];          // first chunk of each tensor, and the number of chunks
+    uint16_t tail[kMost];               // elements of its last chunk
+    uint32_t bf16[(kMost + 31) / 32];   // a bit per tensor
     int count;
+    __host__ __device__ uint32_t chunks() const { return first[count]; }
+    __host__ __device__ int64_t n(int i) const { return (int64_t)(first[i + 1] - first[i] - 1) * kChunk + tail[i]; }
 };
-static_assert(sizeof(GradGroup) <= 4032, "the group and a kernel's other arguments fit 4 KB");
+static_assert(sizeof(GradGroup<false>) <= 4032 && sizeof(GradGroup<true>) <= 4032, "the group and a kernel's other arguments fit 4 KB");
 
 // The tensor of a chunk: the last one whose first chunk is not behind it
-__device__ __forceinline__ int tensor_of(const GradGroup &a, uint32_t chunk) {
+template <bool OUT>
+__device__ __forceinline__ int tensor_of(const GradGroup<OUT> &a, uint32_t chunk) {
     int lo = 0, hi = a.count;
     while (hi - lo > 1) {
         const int mid = (lo + hi) / 2;
@@ -63,14 +68,14 @@ __device__ __forceinline__ double chunk_squares(const T *g, int64_t start, int64
     return s;
 }
 
-__global__ void __launch_bounds__(256) grad_norm_kernel(GradGroup a, double *__restrict__ part) {
+__global__ void __launch_bounds__(256) grad_norm_kernel(GradGroup<false> a, double *__restrict__ part) {
     __shared__ double lds[4];
     double s = 0.0;
-    for (uint32_t c = blockIdx.x; c < a.chunks; c += gridDim.x) {
+    for (uint32_t c = blockIdx.x; c < a.chunks(); c += gridDim.x) {
         const int i = tensor_of(a, c);
         const int64_t start = (int64_t)(c - a.first[i]) * kChunk;
-        if (a.bf16[i / 32] >> (i % 32) & 1u) s += chunk_squares(static_cast<const uint16_t *>(a.g[i]), start, a.n[i]);
-        else s += chunk_squares(static_cast<const float *>(a.g[i]), start, a.n[i]);
+        if (a.bf16[i / 32] >> (i % 32) & 1u) s += chunk_squares(static_cast<const uint16_t *>(a.g[i]), start, a.n(i));
+        else s += chunk_squares(static_cast<const float *>(a.g[i]), start, a.n(i));
     }
     for (int m = 32; m >= 1; m >>= 1) s += __shfl_xor(s, m, 64);
     if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = s;
@@ -131,83 +136,108 @@ __device__ __forceinline__ void chunk_scale(const T *g, T *out, int64_t start, i
     });
 }
 
-// `parts`: the partial sums, of which every workgroup forms the factor itself and the first one writes the norm (a launch less);
-// 0: the factor is there
-__global__ void __launch_bounds__(256) grad_scale_kernel(GradGroup a, const double *__restrict__ part, int64_t parts, double max_norm,
+// `parts`: the partial sums, of which every workgroup forms the factor itself and the first one writes the norm (where `norm` is
+// given); 0: the factor is there
+template <bool OUT>
+__global__ void __launch_bounds__(256) grad_scale_kernel(GradGroup<OUT> a, const double *__restrict__ part, int64_t parts, double max_norm,
                                                          double *__restrict__ norm, const float2 *__restrict__ factor, uint32_t *flag) {
     float2 f;
     if (parts) {
         const double x = norm_of(part, parts);
-        if (blockIdx.x == 0 && threadIdx.x == 0) put_norm(x, norm, flag);
+        if (norm && blockIdx.x == 0 && threadIdx.x == 0) put_norm(x, norm, flag);
         f = factor_of(x, max_norm);
     } else {
         f = *factor;
     }
-    for (uint32_t c = blockIdx.x; c < a.chunks; c += gridDim.x) {
+    for (uint32_t c = blockIdx.x; c < a.chunks(); c += gridDim.x) {
         const int i = tensor_of(a, c);
-        if (!a.out[i] || (f.x == 1.0f && a.out[i] == a.g[i])) continue;  // nothing to write
+        void *const out = OUT ? a.out[OUT ? i : 0] : const_cast<void *>(a.g[i]);
+        if (f.x == 1.0f && out == a.g[i]) continue;  // nothing to write
         const int64_t start = (int64_t)(c - a.first[i]) * kChunk;
         if (a.bf16[i / 32] >> (i % 32) & 1u)
-            chunk_scale(static_cast<const uint16_t *>(a.g[i]), static_cast<uint16_t *>(a.out[i]), start, a.n[i], f);
+            chunk_scale(static_cast<const uint16_t *>(a.g[i]), static_cast<uint16_t *>(out), start, a.n(i), f);
         else
-            chunk_scale(static_cast<const float *>(a.g[i]), static_cast<float *>(a.out[i]), start, a.n[i], f);
+            chunk_scale(static_cast<const float *>(a.g[i]), static_cast<float *>(out), start, a.n(i), f);
     }
 }
 
-// The group of the tensors from `first` on (empty ones are left out); the index behind its last
-int64_t next_group(const GradTensor *t, int64_t first, int64_t count, GradGroup &a) {
-    a.count = 0, a.chunks = 0;
+// The group of the tensors from `first` on (without empty ones and, where `scaled`, those that are only counted); the index behind
+// its last
+template <bool OUT>
+int64_t next_group(const GradTensor *t, int64_t first, int64_t count, bool scaled, GradGroup<OUT> &a) {
+    a.count = 0, a.first[0] = 0;
     for (uint32_t &b : a.bf16) b = 0;
     int64_t i = first;
-    for (; i < count && a.count < kGroup; i++) {
-        if (t[i].n == 0) continue;
+    for (; i < count && a.count < GradGroup<OUT>::kMost; i++) {
+        if (t[i].n == 0 || (scaled && !t[i].out)) continue;
         const int k = a.count++;
-        a.g[k] = t[i].grad, a.out[k] = t[i].out, a.n[k] = t[i].n, a.first[k] = a.chunks;
+        const int64_t chunks = (t[i].n + kChunk - 1) / kChunk;
+        a.g[k] = t[i].grad, a.first[k + 1] = a.first[k] + (uint32_t)chunks, a.tail[k] = (uint16_t)(t[i].n - (chunks - 1) * kChunk);
+        if constexpr (OUT) a.out[k] = t[i].out;
         if (t[i].dtype == kBF16) a.bf16[k / 32] |= 1u << (k % 32);
-        a.chunks += (uint32_t)((t[i].n + kChunk - 1) / kChunk);
     }
     return i;
 }
 
+struct Norm {
+    const double *part;
+    int64_t parts;  // 0: the factor is there
+    double max_norm, *out;
+    const float2 *factor;
+};
+template <bool OUT>
+hipError_t scale_all(const GradTensor *t, int64_t count, Norm x, uint32_t *flag, hipStream_t st) {
+    GradGroup<OUT> a;
+    for (int64_t i = 0; i < count;) {
+        i = next_group(t, i, count, true, a);
+        if (!a.count) continue;
+        grad_scale_kernel<OUT><<<std::min<uint32_t>(a.chunks(), kNormParts), 256, 0, st>>>(a, x.part, x.parts, x.max_norm, x.out, x.factor, flag);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+        x.out = nullptr;
+    }
+    return hipSuccess;
+}
+
 }  // namespace
 
-static_assert(kMaxGradElems / kChunk * kGroup < (int64_t(1) << 32), "chunk numbers of a group are 32-bit");
+static_assert(kMaxGradElems / kChunk * GradGroup<false>::kMost < (int64_t(1) << 32), "chunk numbers of a group are 32-bit");
 
 size_t clip_grad_norm_ws(int64_t tensors) {
-    return 2 * kWsHeader + (size_t)((tensors + kGroup - 1) / kGroup) * kNormParts * sizeof(double);
+    return 2 * kWsHeader + (size_t)((tensors + GradGroup<false>::kMost - 1) / GradGroup<false>::kMost) * kNormParts * sizeof(double);
 }
 
 hipError_t launch_clip_grad_norm(const GradTensor *t, int64_t count, double max_norm, double *norm, uint32_t *flag, void *ws,
                                  hipStream_t st) {
     float2 *const factor = reinterpret_cast<float2 *>(static_cast<char *>(ws) + kWsHeader);
     double *const part = reinterpret_cast<double *>(static_cast<char *>(ws) + 2 * kWsHeader);
-    int64_t parts = 0;
-    int groups = 0;
-    bool scales = false;
-    GradGroup a;
+    int64_t parts = 0, scaled = 0;
+    bool in_place = true;
+    for (int64_t i = 0; i < count; i++) {
+        if (t[i].n == 0 || !t[i].out) continue;
+        scaled++;
+        in_place = in_place && t[i].out == t[i].grad;
+    }
+    GradGroup<false> a;
     for (int64_t i = 0; i < count;) {
-        i = next_group(t, i, count, a);
+        i = next_group(t, i, count, false, a);
         if (!a.count) continue;
-        for (int k = 0; k < a.count; k++) scales = scales || a.out[k];
-        const unsigned grid = std::min<uint32_t>(a.chunks, kNormParts);
+        const unsigned grid = std::min<uint32_t>(a.chunks(), kNormParts);
         grad_norm_kernel<<<grid, 256, 0, st>>>(a, part + parts);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
         parts += grid;
-        groups++;
     }
-    const bool alone = scales && groups == 1;  // the one scaling launch finishes the norm as well
-    if (!alone) grad_finish_kernel<<<1, 256, 0, st>>>(part, parts, max_norm, norm, factor, flag);
-    hipError_t e = hipGetLastError();
-    if (e != hipSuccess || !scales) return e;
-    for (int64_t i = 0; i < count;) {
-        i = next_group(t, i, count, a);
-        if (!a.count) continue;
-        grad_scale_kernel<<<std::min<uint32_t>(a.chunks, kNormParts), 256, 0, st>>>(a, part, alone ? parts : 0, max_norm, norm, factor, flag);
-        e = hipGetLastError();
+    // one or two scaling launches form the norm themselves: 1 us each, where a launch for it takes 4.6 and the way to the next
+    const bool alone = scaled > 0 && scaled <= 2 * (in_place ? GradGroup<false>::kMost : GradGroup<true>::kMost);
+    if (!alone) {
+        grad_finish_kernel<<<1, 256, 0, st>>>(part, parts, max_norm, norm, factor, flag);
+        const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
-    return hipSuccess;
+    if (scaled == 0) return hipSuccess;
+    const Norm x{part, alone ? parts : 0, max_norm, norm, factor};
+    return in_place ? scale_all<false>(t, count, x, flag, st) : scale_all<true>(t, count, x, flag, st);
 }
 
 }  // namespace focus
