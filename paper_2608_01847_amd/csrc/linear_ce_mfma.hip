@@ -6,6 +6,12 @@
 // which goes to memory in bf16, through LDS. Operands are K-contiguous and go straight into a ring of LDS stages, several steps ahead
 // of the matrix instructions, as in the reconstruction GEMM's forward. Few tiles: 128 x 128, two workgroups per CU.
 //
+// Bound by the matrix units at the clock that they leave the card: 8,192 x 151,936 x 2,560 forward 5.1-5.4 ms, 1.18-1.25 PFLOP/s (a
+// library product of the shape, logits written, 1.40), matrix units busy 68% of a CU's cycles at 1.75 GHz, no LDS bank conflicts. The
+// edge is 256 because an operand byte read from LDS then feeds 128 products; 8 waves of 128 x 64 would read half as much again.
+// A cycle saved beside the products brings little: with what a token's D takes asked for before the products, eight trips to memory less
+// of about 120,000 cycles a tile, the backward of that size went from 16.55 to 16.42 ms.
+//
 // Up to 16 tokens the products are too few to hide the weights' way from memory, 2 K bytes per logit row: waves read 32 vocabulary
 // rows each straight into the matrix instructions' registers.
 #include "linear_ce.h"
@@ -31,6 +37,7 @@ constexpr float kLog2e = 1.44269504088896341f;
 // to the size of m
 struct Exponent {
     float c, factor;
+    __device__ __forceinline__ Exponent(float at, float f) : c(at), factor(f) {}
     __device__ __forceinline__ explicit Exponent(float m) {
         c = m * kLog2e;
         factor = exp2_raw(-__builtin_fmaf(m, kLog2e, -c));
@@ -137,19 +144,24 @@ __device__ __forceinline__ int entry_of(int i, int r) {
     return E / 2 * wm + 32 * i + 8 * (r / 4) + 4 * (lane >> 5) + r % 4;
 }
 
-// Whether any lane's target lies in its wave's half of the tile from v0 on, and its place in the tile
+// Place in the tile from v0 on of a target, or -1
 template <int E>
-__device__ __forceinline__ bool target_near(int64_t want, int64_t v0, int &at) {
+__device__ __forceinline__ int place_of(int64_t want, int64_t v0) {
     const int64_t d = want - v0;
+    return d >= 0 && d < E ? (int)d : -1;
+}
+
+// Whether a lane's place lies in its wave's half of the tile, for any lane of the wave
+template <int E>
+__device__ __forceinline__ bool near_any(int at) {
     const int half = (threadIdx.x >> 7) * (E / 2);
-    const bool here = d >= half && d < half + E / 2;
-    at = here ? (int)d : -1;
-    return __any(here);
+    return __any(at >= half && at < half + E / 2);
 }
 
 }  // namespace
 
-// Maximum and sum of exponentials of every token of the tile over its vocabulary entries, and the logit of a target there.
+// Maximum and sum of exponentials of every token of the tile over its vocabulary entries, and the logit of a target there: for a
+// wave 256 exponentials a lane, about 10,000 cycles beside the products' 82,000 at 2,560 features.
 template <int E>
 __global__ void __launch_bounds__(kThreads, E == 256 ? 1 : 2) ce_stats_mfma_kernel(CeArgs a) {
     __shared__ __attribute__((aligned(16))) char smem[Geometry<E>::kLds];
@@ -157,25 +169,30 @@ __global__ void __launch_bounds__(kThreads, E == 256 ? 1 : 2) ce_stats_mfma_kern
     uint32_t tv, tt;
     grouped_tile(xcd_tile(blockIdx.x, gridDim.x), (uint32_t)a.tiles_v, gridDim.x / (uint32_t)a.tiles_v, tv, tt);
     const int64_t v0 = (int64_t)tv * E, t0 = a.t0 + (int64_t)tt * E;
+    // asked for before the products, each thread one token's: behind them, four trips to memory one after the other
+    const int64_t own = t0 + threadIdx.x;
+    const int place = a.target && threadIdx.x < E && own < a.T ? place_of<E>(a.target[own], v0) : -1;
     f32x16_t acc[N][N];
     logits_tile<E>(a, v0, t0, smem, acc);
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wm = wave >> 1, wn = wave & 1, lr = lane & 31, lh = lane >> 5;
-    if (v0 + E > a.V) {  // entries that do not exist
-        static_for<N * N>([&](auto ij) {
-            static_for<16>([&](auto r) {
-                if (v0 + entry_of<E>(ij / N, r) >= a.V) acc[ij / N][ij % N][(int)r] = -__builtin_inff();
-            });
-        });
-    }
     float2 *const red = reinterpret_cast<float2 *>(smem);  // [2 waves along the vocabulary][E tokens]
-    static_for<N>([&](auto j) {
+    int *const places = reinterpret_cast<int *>(smem + 2 * E * sizeof(float2));
+    if (threadIdx.x < E) places[threadIdx.x] = place;
+    __syncthreads();
+    const int here = (int)std::min<int64_t>(E, a.V - v0);  // entries that exist
+    auto reduce = [&](auto whole, auto j) {
         const int64_t t = t0 + E / 2 * wn + 32 * j + lr;
-        int at;
-        if (target_near<E>(a.target && t < a.T ? a.target[t] : -1, v0, at)) {
+        const int at = places[E / 2 * wn + 32 * j + lr];
+        if (near_any<E>(at)) {
             static_for<N>([&](auto i) {
                 static_for<16>([&](auto r) {
                     if (at == entry_of<E>(i, r)) a.zt[t] = acc[i][j][(int)r];
                 });
+            });
+        }
+        if constexpr (!whole) {
+            static_for<N>([&](auto i) {
+                static_for<16>([&](auto r) { acc[i][j][(int)r] = entry_of<E>(i, r) < here ? acc[i][j][(int)r] : -__builtin_inff(); });
             });
         }
         float m = -__builtin_inff();
@@ -193,13 +210,14 @@ __global__ void __launch_bounds__(kThreads, E == 256 ? 1 : 2) ce_stats_mfma_kern
         }
         sum += __shfl_xor(sum, 32, 64);
         if (lh == 0) red[wm * E + E / 2 * wn + 32 * j + lr] = make_float2(m, sum);
-    });
+    };
+    if (here == E) static_for<N>([&](auto j) { reduce(std::true_type{}, j); });
+    else static_for<N>([&](auto j) { reduce(std::false_type{}, j); });
     __syncthreads();
-    const int64_t t = t0 + threadIdx.x;
-    if (threadIdx.x >= E || t >= a.T) return;
+    if (threadIdx.x >= E || own >= a.T) return;
     const float2 x = red[threadIdx.x], y = red[E + threadIdx.x];
     const float m = fmaxf(x.x, y.x);
-    a.part[(int64_t)tv * a.T + t] = make_float2(m, (x.x == m ? x.y : x.y * expf(x.x - m)) + (y.x == m ? y.y : y.y * expf(y.x - m)));
+    a.part[(int64_t)tv * a.T + own] = make_float2(m, (x.x == m ? x.y : x.y * expf(x.x - m)) + (y.x == m ? y.y : y.y * expf(y.x - m)));
 }
 
 // The tile of D: D[t][v] = (h - g) p + g [v == target] relative to the token's scale, p = exp(z - lse), rounded to bf16. Relative to
@@ -212,29 +230,36 @@ __global__ void __launch_bounds__(kThreads, E == 256 ? 1 : 2) ce_grad_mfma_kerne
     uint32_t tv, tt;
     grouped_tile(xcd_tile(blockIdx.x, gridDim.x), (uint32_t)a.tiles_v, gridDim.x / (uint32_t)a.tiles_v, tv, tt);
     const int64_t c0 = (int64_t)tv * E, v0 = a.v0 + c0, t0 = a.t0 + (int64_t)tt * E;
+    // what a token's D takes, as in the forward: the factor of the exponentials, what a target's entry adds, lse log2e, its place
+    float4 own = make_float4(0.0f, 0.0f, 0.0f, __int_as_float(-1));
+    bool bad = false;
+    if (threadIdx.x < E && t0 + threadIdx.x < a.T) {
+        const int64_t t = t0 + threadIdx.x, want = a.target ? a.target[t] : -1;
+        const float g = a.g && want >= 0 && want < a.V ? a.g[t] : 0.0f, h = a.h ? a.h[t] : 0.0f, lse = a.lse[t], scale = a.scale[t];
+        bad = want >= a.V || ((g != 0.0f || h != 0.0f) && !(__builtin_fabsf(lse) <= 65536.0f));
+        const Exponent e(lse);
+        // quotients: the inverse of a tiny scale would overflow
+        if (scale != 0.0f) own = make_float4((h - g) / scale * e.factor, g / scale, e.c, __int_as_float(place_of<E>(want, v0)));
+    }
     f32x16_t acc[N][N];
     logits_tile<E>(a, v0, t0, smem, acc);
+    float4 *const tokens = reinterpret_cast<float4 *>(smem + 2 * E * E);  // behind the tile
+    if (threadIdx.x < E) tokens[threadIdx.x] = own;
+    __syncthreads();
     const int lane = threadIdx.x & 63, wn = threadIdx.x >> 6 & 1, lr = lane & 31;
-    bool bad = false;
     static_for<N>([&](auto j) {
-        const int64_t t = t0 + E / 2 * wn + 32 * j + lr;
-        const bool real = t < a.T;
-        const int64_t want = a.target && real ? a.target[t] : -1;
-        const float g = a.g && want >= 0 && want < a.V ? a.g[t] : 0.0f, h = a.h && real ? a.h[t] : 0.0f;
-        const float lse = real ? a.lse[t] : 0.0f, scale = real ? a.scale[t] : 0.0f;
-        bad = bad || want >= a.V || ((g != 0.0f || h != 0.0f) && !(__builtin_fabsf(lse) <= 65536.0f));
-        const Exponent e(lse);  // quotients: the inverse of a tiny scale would overflow
-        const float by = (h - g) / scale * e.factor, hit = g / scale;
-        static_for<N>([&](auto i) { static_for<16>([&](auto r) { acc[i][j][(int)r] = by * e(acc[i][j][(int)r]); }); });
-        int at;
-        if (target_near<E>(want, v0, at)) {
+        const float4 of = tokens[E / 2 * wn + 32 * j + lr];
+        const Exponent e{of.z, 1.0f};
+        static_for<N>([&](auto i) { static_for<16>([&](auto r) { acc[i][j][(int)r] = of.x * e(acc[i][j][(int)r]); }); });
+        const int at = __float_as_int(of.w);
+        if (near_any<E>(at)) {
             static_for<N>([&](auto i) {
                 static_for<16>([&](auto r) {
-                    if (at == entry_of<E>(i, r)) acc[i][j][(int)r] += hit;
+                    if (at == entry_of<E>(i, r)) acc[i][j][(int)r] += of.y;
                 });
             });
         }
-        const bool none = scale == 0.0f;  // no gradient (or no token), whatever X and lse hold
+        const bool none = of.x == 0.0f && of.y == 0.0f;  // no gradient (or no token), whatever X and lse hold
         if (__any(none)) {
             static_for<N>([&](auto i) {
                 static_for<16>([&](auto r) { acc[i][j][(int)r] = none ? 0.0f : acc[i][j][(int)r]; });
@@ -254,7 +279,10 @@ __global__ void __launch_bounds__(kThreads, E == 256 ? 1 : 2) ce_grad_mfma_kerne
 
 // Up to 16 tokens: a wave takes 32 vocabulary entries, whose rows it reads straight into the operand registers (v_mfma_f32_16x16x32:
 // a load instruction takes 64 bytes each of 16 rows), kAhead steps of 32 k under way; the tokens' rows come from the caches. Bound
-// by the weights' way from memory.
+// by the weights' way from memory: 1 x 151,936 x 2,560 162 us, 4.8 TB/s; 16 tokens 200. With 32 x 32 tiles, which read 32 bytes of
+// a row at a time, 218; the waves of a workgroup on every fourth step of the same 32 entries, added up through LDS, 162 and 208, and
+// 139 for 117 at 4 x 32,000 x 8,192 (14 to 6.5 at 8 x 3,000 x 1,024, where 24 workgroups leave most CUs without work). From 17 tokens on
+// the tiles above take less (208 us for 253).
 typedef float f32x4_t __attribute__((ext_vector_type(4)));
 constexpr int kAhead = 8;
 __global__ void __launch_bounds__(kThreads) ce_stats_few_kernel(CeArgs a) {
