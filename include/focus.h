@@ -46,8 +46,9 @@ typedef enum {
     FOCUS_OK = 0,
     FOCUS_ERR_NULL = 1,      /* a required pointer is NULL */
     FOCUS_ERR_SHAPE = 2,     /* bad sizes (negative, too large, K not a multiple of the block size)
-                                or a tensor pointer that is not 16-byte aligned; focus_attention_*: an output
-                                that shares memory with an input */
+                                or a tensor pointer that is not 16-byte aligned; focus_attention_*, focus_linear_ce_*:
+                                an output that shares memory with an input; focus_sandwich_norm_*,
+                                focus_clip_grad_norm: one that does so beyond what the call allows */
     FOCUS_ERR_DTYPE = 3,     /* unknown dtype or unsupported dtype combination */
     FOCUS_ERR_CONFIG = 4,    /* bad focus_qconfig (format, sub_block, ste_clip, scale_layout, e8m0_rounding) */
     FOCUS_ERR_WORKSPACE = 5, /* workspace NULL, misaligned or smaller than focus_workspace_size() */

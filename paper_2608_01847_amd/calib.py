@@ -22,7 +22,8 @@ runs through zero within an epoch once its gradient keeps one sign (every elemen
 clamps, its straight-through gradient vanishes and momentum carries c on). Near c = 1 the log2 step
 changes c by about ln 2 times the learning rate, close to the linear step the rates were set for.
 Inputs are the seeded synthetic batches of `synth`. KLTopStack and DecoderStack train end to end on KL-Top instead of per layer;
-the second has the norms and the attention of a decoder between its linears.
+the second has the norms and the attention of a decoder between its linears, and trains on labels too, whose cross entropy and
+gradients come without the logits, with the norm of all its gradients bounded where that is asked for.
 
 With independent activation channels (X^T X nearly diagonal) the coefficients cannot lower the
 per-layer loss: c = 1 is round-to-nearest onto the dequantisation grid S_dq * E2M1, optimal for every

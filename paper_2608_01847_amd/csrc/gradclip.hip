@@ -68,6 +68,7 @@ __device__ __forceinline__ double chunk_squares(const T *g, int64_t start, int64
     return s;
 }
 
+// Bound by memory: 14 tensors of 490 MB 113 us, 4.3 TB/s; 169 MB, some of them still in the caches, 28 us, 6 TB/s
 __global__ void __launch_bounds__(256) grad_norm_kernel(GradGroup<false> a, double *__restrict__ part) {
     __shared__ double lds[4];
     double s = 0.0;
@@ -137,7 +138,7 @@ __device__ __forceinline__ void chunk_scale(const T *g, T *out, int64_t start, i
 }
 
 // `parts`: the partial sums, of which every workgroup forms the factor itself and the first one writes the norm (where `norm` is
-// given); 0: the factor is there
+// given); 0: the factor is there. Bound by memory: 490 MB read and written 176 us, 5.6 TB/s.
 template <bool OUT>
 __global__ void __launch_bounds__(256) grad_scale_kernel(GradGroup<OUT> a, const double *__restrict__ part, int64_t parts, double max_norm,
                                                          double *__restrict__ norm, const float2 *__restrict__ factor, uint32_t *flag) {

@@ -114,6 +114,9 @@ __device__ __forceinline__ void lds8(const float *p, float (&v)[8]) {
 // vector j of thread t starts at column (j n + t) 8. A row is read once, and U and Y stay in registers in fp32. Waves take one row each,
 // with the parameters from the caches; a workgroup takes `rows` consecutive rows, with the parameters in LDS, and asks for the next
 // row's pieces as soon as their registers are free. BIAS: with shifts; TOKEN: with gates of the tokens' own.
+// Bound by memory: 65,536 x 2,560 bf16 268 us, 5.0 TB/s, bytes 1.00 times the tensors' (with 256 threads of two vectors and no row asked
+// for ahead 313); 8,192 x 8,192 with token gates 129 us, 5.2 TB/s; a wave per row at 131,072 x 1,024 191 to 197 us, 5.5 TB/s. One row is four
+// dependent trips to memory and LDS: 1 x 8,192 5.3 us.
 template <typename T, bool WAVE, int NV, bool BIAS, bool TOKEN, bool TAIL>
 __global__ void __launch_bounds__(WAVE ? kThreads : kMostThreads) sandwich_fwd_kernel(SandwichArgs a) {
     extern __shared__ __attribute__((aligned(16))) float smem[];
@@ -236,6 +239,10 @@ __global__ void __launch_bounds__(WAVE ? kThreads : kMostThreads) sandwich_fwd_k
 
 // Rows, threads and the next row's pieces as in the forward; the sums over the rows stay in registers and leave as one row of
 // partial sums per workgroup (waves that take rows by themselves are added in order through LDS first). BIAS: the sums without xh too.
+// Memory and its latency bound it: 65,536 x 2,560 bf16 505 us, 4.0 TB/s, bytes 1.00 times the tensors'; 8,192 x 8,192 with token gates
+// 211 us, 5.1 TB/s. At 65,536 x 2,560 a workgroup of 256 threads with two vectors each took 522, one of five waves without the next row
+// under way 577 to 610, with it but the parameters converted anew for each row 534; 8,192 x 8,192 350 before, 211 after. A wave per
+// row: 131,072 x 1,024 295 us, 4.5 TB/s; 262,144 x 512 with token gates 444.
 template <typename T, bool WAVE, int NV, bool BIAS, bool TOKEN, bool TAIL>
 __global__ void __launch_bounds__(WAVE ? kThreads : kMostThreads) sandwich_bwd_kernel(SandwichArgs a) {
     constexpr int kRows = WAVE ? 4 : 1;
@@ -424,7 +431,8 @@ struct Element {
     }
 };
 
-// A workgroup per row, which it reads once for each sum and once for the outputs, element by element.
+// Rows of more than 8,192 features, which registers and LDS do not hold: a workgroup per row, which it reads once for each sum and once
+// for the outputs, element by element. Not tuned: 2,048 x 8,200 bf16 78 us, backward 646 (x 8,192 25 and 45).
 template <typename T>
 __global__ void __launch_bounds__(kThreads) sandwich_fwd_long_kernel(SandwichArgs a) {
     __shared__ float lds[2][32];
@@ -524,8 +532,9 @@ __global__ void __launch_bounds__(kThreads) sandwich_bwd_long_kernel(SandwichArg
     }
 }
 
-// Sums of the partial rows in order and in fp64: 16 columns x 16 row groups per sum of a workgroup, 8 loads in flight. A feature's
-// gate is applied here: with S = sum_t dYt xh1 and R = sum_t dYt, dw1 = gate S, db1 = gate R, dgate = w1 S + b1 R.
+// Sums of the partial rows in order and in fp64: 16 columns x 16 row groups per sum of a workgroup, 8 loads in flight. Bound by the
+// loads' latency, 8 rounds of them at 1,024 rows: 9 us for 1,001 features and 4 sums, 10.5 for 2,560 and 2. 64 row groups of 16 threads
+// for all sums took 15 (16 MB in 64-byte pieces, and twice the LDS steps). A feature's gate is applied here: with S = sum_t dYt xh1 and R = sum_t dYt, dw1 = gate S, db1 = gate R, dgate = w1 S + b1 R.
 __global__ void __launch_bounds__(1024) sandwich_finish_kernel(SandwichArgs a, int parts) {
     __shared__ double lds[4][16][17];
     const int col = threadIdx.x & 15, grp = (threadIdx.x >> 4) & 15, k = threadIdx.x >> 8, c = blockIdx.x * 16 + col, C = a.C;
