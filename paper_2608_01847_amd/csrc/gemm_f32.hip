@@ -465,8 +465,8 @@ hipError_t launch_bwd_f32(int fmt, int w_dt, const float *dY, const float *X, in
 
 // ---- logit tiles of the linear cross entropy: rows = vocabulary, columns = tokens, so that a lane holds one token's logits ----
 // Bound by the products, and for few tokens by whole rounds of tiles: 301 x 5,003 x 1,008 (395 tiles of 64 x 64 on 256 CUs) 43 us
-// forward, 47 for D, 47 for each gradient, 65 to 71 TFLOP/s; 1,024 x 10,000 x 1,024 207, 218 and 230 to 260 us, 102 TFLOP/s (a library
-// product of 8,192 in each dimension 154). Tiles of 32 x 32 for both: 49 and 50 us, and 279 and 287.
+// forward, 47 for D, 40 to 47 for each gradient, 65 to 75 TFLOP/s; 1,024 x 10,000 x 1,024 190 forward, 580 backward, 110 TFLOP/s (a
+// library product of 8,192 in each dimension 154). Tiles of 32 x 32 for both sizes' forward: 49 and 279.
 namespace {
 
 // Maximum and sum of exponentials of each token over the tile's vocabulary, and the logit of a target there

@@ -287,7 +287,8 @@ __global__ void __launch_bounds__(256) ce_scale_x_kernel(const uint16_t *__restr
 }
 
 // total = before + the splits' sums in order; to `sums` in fp32, or times the row's (or everything's, or no) factor to `out`. Bound by
-// memory: three splits of 8,192 x 2,560, the sum so far and the new one 63 us, 6.6 TB/s (the splits partly from the caches)
+// memory: three splits of 8,192 x 2,560, the sum so far and the new one 63 us, 6.6 TB/s (the splits partly from the caches); many splits
+// of little by their latency, hence eight under way (63 of 64 x 512: 9 us, one at a time 16)
 __global__ void __launch_bounds__(256) ce_sums_kernel(const float *__restrict__ part, int64_t splits, const float *__restrict__ before,
                                                       const float *__restrict__ factor, int per_row, int64_t first, int64_t n, int64_t K,
                                                       float *__restrict__ sums, void *__restrict__ out, int out_dtype) {
@@ -295,7 +296,17 @@ __global__ void __launch_bounds__(256) ce_sums_kernel(const float *__restrict__ 
     if (i >= n) return;
     float s[8], v[8];
     load8_n(part + i, 8, s);
-    for (int64_t z = 1; z < splits; z++) {
+    int64_t z = 1;
+    for (; z + 8 <= splits; z += 8) {  // eight under way
+        float u[8][8];
+#pragma unroll
+        for (int k = 0; k < 8; k++) load8_n(part + (z + k) * n + i, 8, u[k]);
+#pragma unroll
+        for (int k = 0; k < 8; k++)
+#pragma unroll
+            for (int e = 0; e < 8; e++) s[e] += u[k][e];
+    }
+    for (; z < splits; z++) {
         load8_n(part + z * n + i, 8, v);
 #pragma unroll
         for (int e = 0; e < 8; e++) s[e] += v[e];
@@ -391,13 +402,17 @@ size_t mfma_space(int64_t T, int64_t V, int64_t K, char *base, MfmaSpace *s) {
 }
 
 // ---- fp32 ---------------------------------------------------------------------------------------
-// Splits of a product's reduction over R: whole rounds of 64 x 64 tiles, three per CU at once, in units of a 32-row step
+// Splits of a product's reduction over R into tiles of 64 x 64, in ns: the tiles that a CU has take a step of 32 rows in turn, 0.69 us
+// where it has one, 0.56 of two and 0.51 of three, which is how many run at once, 1.5 us for their start and end; the sums' launch, and
+// what it and the tiles move. dX of 1,024 x 10,000 x 1,024 (256 tiles) 217 us unsplit, 175 in two and 162 in three, of 301 x 5,003 x 1,008
+// (80 tiles) 48 in three and 41 in six, of 100 x 8,000 x 2,048 (64) 48 in four and 40 in eight.
 Splits f32_splits(int64_t R, int64_t N, int64_t K) {
-    const int64_t tiles = cdiv(N, 64) * cdiv(K, 64), steps = cdiv(R, 32), slots = 256;
-    const int64_t most = tiles >= 16 * slots ? 1 : std::min<int64_t>(std::min<int64_t>(kMostSplits, steps), kDxSums / (N * K));
+    const int64_t tiles = cdiv(N, 64) * cdiv(K, 64), steps = cdiv(R, 32), cus = 256;
+    const int64_t most = tiles >= 16 * cus ? 1 : std::min<int64_t>(std::min<int64_t>(kMostSplits, steps), kDxSums / (N * K));
     int64_t best = -1, count = 1;
     for (int64_t s = 1; s <= std::max<int64_t>(1, most); s++) {
-        const int64_t cost = cdiv(tiles * s, slots) * (cdiv(steps, s) + 3) + (s > 1 ? 4 + s * N * K / 281250 : 0);
+        const int64_t on_cu = cdiv(tiles * s, cus), step = on_cu == 1 ? 690 : on_cu == 2 ? 560 : 510;
+        const int64_t cost = on_cu * cdiv(steps, s) * step + cdiv(on_cu, 3) * 1500 + (s > 1 ? 5000 + s * N * K / 560 : 0);
         if (best < 0 || cost < best) best = cost, count = s;
     }
     const int64_t chunk = cdiv(steps, count) * 32;
