@@ -562,8 +562,8 @@ focus_status focus_sandwich_norm_bwd(const focus_sandwich_config *cfg, const voi
  * largest logit of 2^30 and more in size, raises the domain flag, as a target >= V does (which is taken as left out); the token's
  * results are then unspecified, as the lse of a token left out is if its X is not finite. lse and logp share no memory with an
  * input or one another.
- * 0 <= T <= 2^24, 1 <= V <= 2^24, 1 <= K <= 2^20 (FOCUS_ERR_SHAPE); T == 0 is a no-op. bf16 with K % 16 == 0 runs on the matrix
- * instructions. ws: focus_workspace_size(FOCUS_CALL_LINEAR_CE_FWD, NULL, T, V, K) bytes; it serves fewer tokens too. */
+ * 0 <= T <= 2^24 (fp32: 2^23), 1 <= V <= 2^24, 1 <= K <= 2^20 (FOCUS_ERR_SHAPE); T == 0 is a no-op. Rows of another K than a multiple
+ * of 16 are copied into the workspace, padded. ws: focus_workspace_size(FOCUS_CALL_LINEAR_CE_FWD, NULL, T, V, K) bytes; it serves fewer tokens too. */
 focus_status focus_linear_ce_fwd(const void *X, const void *W, int dtype, int64_t T, int64_t V, int64_t K,
                                  const int64_t *target_opt, float *logp_opt, float *lse, void *ws, size_t ws_bytes,
                                  focus_stream stream);

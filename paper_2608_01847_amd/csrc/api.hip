@@ -242,8 +242,9 @@ focus_status check_sandwich(const focus_sandwich_config *cfg, int dtype, int w_d
 }
 
 constexpr int64_t kCeMaxRows = int64_t(1) << 24, kCeMaxK = int64_t(1) << 20;
-focus_status check_linear_ce(int64_t T, int64_t V, int64_t K) {
-    return T < 0 || V < 1 || K < 1 || T > kCeMaxRows || V > kCeMaxRows || K > kCeMaxK ? FOCUS_ERR_SHAPE : FOCUS_OK;
+focus_status check_linear_ce(int64_t T, int64_t V, int64_t K, int dtype = FOCUS_BF16) {
+    const int64_t most = dtype == FOCUS_BF16 ? kCeMaxRows : kCeMaxRows / 2;  // 32 rows of the fp32 D's transpose stay below 2 GB
+    return T < 0 || V < 1 || K < 1 || T > most || V > kCeMaxRows || K > kCeMaxK ? FOCUS_ERR_SHAPE : FOCUS_OK;
 }
 
 constexpr int64_t kMaxGradTensors = int64_t(1) << 20;
@@ -344,7 +345,7 @@ size_t focus_workspace_size(int call, const focus_qconfig *q, int64_t M, int64_t
     }
     if (call == FOCUS_CALL_LINEAR_CE_FWD || call == FOCUS_CALL_LINEAR_CE_BWD) {
         if (check_linear_ce(M, N, K) != FOCUS_OK) return 0;
-        return call == FOCUS_CALL_LINEAR_CE_FWD ? linear_ce_fwd_ws(M, N) : linear_ce_bwd_ws(M, N, K);
+        return call == FOCUS_CALL_LINEAR_CE_FWD ? linear_ce_fwd_ws(M, N, K) : linear_ce_bwd_ws(M, N, K);
     }
     if (call == FOCUS_CALL_CLIP_GRAD_NORM) return M < 0 || M > kMaxGradTensors ? 0 : clip_grad_norm_ws(M);
     if (check_q(q) != FOCUS_OK) return 0;
@@ -825,12 +826,12 @@ focus_status focus_linear_ce_fwd(const void *X, const void *W, int dtype, int64_
                                  const int64_t *target_opt, float *logp_opt, float *lse, void *ws, size_t ws_bytes,
                                  focus_stream stream) {
     if (!dtype_ok(dtype)) return FOCUS_ERR_DTYPE;
-    FOCUS_TRY(check_linear_ce(T, V, K));
+    FOCUS_TRY(check_linear_ce(T, V, K, dtype));
     if (T > 0 && (!X || !W || !lse || (logp_opt && !target_opt))) return FOCUS_ERR_NULL;
     if (!all_aligned({X, W}) || !aligned_to({logp_opt, lse}, 4) || !aligned_to({target_opt}, 8)) return FOCUS_ERR_SHAPE;
     const int64_t e = dtype == FOCUS_BF16 ? 2 : 4;
     if (clash({{logp_opt, T * 4}, {lse, T * 4}}, {{X, T * K * e}, {W, V * K * e}, {target_opt, T * 8}}, false)) return FOCUS_ERR_SHAPE;
-    FOCUS_TRY(check_ws(ws, ws_bytes, linear_ce_fwd_ws(T, V)));
+    FOCUS_TRY(check_ws(ws, ws_bytes, linear_ce_fwd_ws(T, V, K)));
     if (T == 0) return FOCUS_OK;
     return hip_status(launch_linear_ce_fwd(dtype, X, W, T, V, K, target_opt, logp_opt, lse, flag_of(ws), ws, (hipStream_t)stream));
 }
@@ -840,7 +841,7 @@ focus_status focus_linear_ce_bwd(const void *X, const void *W, int dtype, int64_
                                  const float *d_lse_opt, void *dX_opt, void *dW_opt, int dw_dtype, void *ws,
                                  size_t ws_bytes, focus_stream stream) {
     if (!dtype_ok(dtype) || !dtype_ok(dw_dtype) || (dtype == FOCUS_F32 && dw_dtype != FOCUS_F32)) return FOCUS_ERR_DTYPE;
-    FOCUS_TRY(check_linear_ce(T, V, K));
+    FOCUS_TRY(check_linear_ce(T, V, K, dtype));
     if (T > 0 && (!X || !W || !lse || (!dX_opt && !dW_opt) || (!d_logp_opt && !d_lse_opt) || (d_logp_opt && !target_opt)))
         return FOCUS_ERR_NULL;
     if (!all_aligned({X, W, dX_opt, dW_opt}) || !aligned_to({lse, d_logp_opt, d_lse_opt}, 4) || !aligned_to({target_opt}, 8))

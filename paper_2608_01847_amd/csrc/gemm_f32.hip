@@ -546,10 +546,6 @@ __global__ void __launch_bounds__(256) ce_grad_f32_kernel(CeArgs a, float *__res
 
 }  // namespace
 
-bool ce_f32_supported(int64_t T, int64_t V, int64_t K) {
-    return f32_fwd_supported(V, T, K) && f32_bwd_supported(T, kCeMostWidth, K) && f32_bwd_supported(V, T + 3, K);
-}
-
 // Edge of a logit tile, as the forward chooses it: 64 x 64 where they give every CU one
 int64_t ce_f32_tile(int64_t T, int64_t n) {
     return ((n + 63) / 64) * ((T + 63) / 64) < kMfmaConcurrentWgs ? 32 : 64;

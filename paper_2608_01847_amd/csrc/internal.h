@@ -164,7 +164,7 @@ size_t sandwich_bwd_ws(int64_t T, int64_t C);
 hipError_t launch_sandwich_fwd(int dtype, SandwichArgs a, hipStream_t st);
 hipError_t launch_sandwich_bwd(int dtype, SandwichArgs a, void *ws, hipStream_t st);
 
-size_t linear_ce_fwd_ws(int64_t T, int64_t V);
+size_t linear_ce_fwd_ws(int64_t T, int64_t V, int64_t K);
 size_t linear_ce_bwd_ws(int64_t T, int64_t V, int64_t K);
 hipError_t launch_linear_ce_fwd(int dtype, const void *X, const void *W, int64_t T, int64_t V, int64_t K, const int64_t *target,
                                 float *logp, float *lse, uint32_t *flag, void *ws, hipStream_t st);

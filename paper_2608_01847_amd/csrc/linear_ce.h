@@ -30,15 +30,14 @@ __device__ __forceinline__ bool ce_takes_part(const int64_t *target, const float
     return (g && target[t] >= 0 && target[t] < V && g[t] != 0.0f) || (h && h[t] != 0.0f);
 }
 
-// Logit tiles on the matrix instructions (bf16, K a multiple of 16), of edge x edge: those of `tokens` tokens from a.t0 on
+// Logit tiles on the matrix instructions (bf16; K a multiple of 16 throughout), of edge x edge: those of `tokens` tokens from a.t0 on
 int64_t ce_mfma_tile(int64_t T, int64_t n);
 void launch_ce_stats_mfma(const CeArgs &a, int64_t edge, int64_t tokens, hipStream_t st);
 void launch_ce_stats_few(const CeArgs &a, hipStream_t st);  // T <= kCeFew
 void launch_ce_grad_mfma(const CeArgs &a, int64_t edge, int64_t tokens, uint32_t *flag, hipStream_t st);
 
-// The same on the fp32 matrix instructions (K a multiple of 16), tiles of edge x edge; D's transpose, [entries][pitch_t], goes to Dt;
+// The same on the fp32 matrix instructions, tiles of edge x edge; D's transpose, [entries][pitch_t], goes to Dt;
 // with x, the rows of X that have a gradient go there, zeros in place of the others
-bool ce_f32_supported(int64_t T, int64_t V, int64_t K);
 int64_t ce_f32_tile(int64_t T, int64_t n);
 void launch_ce_stats_f32(const CeArgs &a, int64_t edge, int64_t tokens, hipStream_t st);
 void launch_ce_grad_f32(const CeArgs &a, int64_t edge, int64_t tokens, float *Dt, int64_t pitch_t, float *x, uint32_t *flag,

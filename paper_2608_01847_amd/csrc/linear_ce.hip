@@ -9,11 +9,11 @@
 // vocabulary; a second kernel joins the parts. Backward: the vocabulary goes in pieces; of each the logits are formed again
 // and D, which both products read, is what lies in memory.
 //
-// bf16 operands with K a multiple of 16 go to the matrix instructions (linear_ce_mfma.hip), D in bf16 relative to a token's scale
+// bf16 operands go to the matrix instructions (linear_ce_mfma.hip), D in bf16 relative to a token's scale
 // r = max(|g|, |h|):
 //   D = r D',  dX[t] = r[t] (D' W)[t],  dW = G D'^T X',  X'[t] = X[t] r[t] / G  (rounded),  G = max r
 // so that the tokens' weights are rounded into X' where they differ, and nowhere where they are those of a mean (X' is X then).
-// fp32 with K a multiple of 16 goes to the fp32 matrix instructions (gemm_f32.hip); other shapes take the kernels below.
+// fp32 goes to the fp32 matrix instructions (gemm_f32.hip). Rows of another K than a multiple of 16 are padded with zeros first.
 #include "linear_ce.h"
 #include "ops_device.h"
 
@@ -21,76 +21,9 @@ namespace focus {
 
 namespace {
 
-constexpr int kTileV = 64, kTileT = 64;  // logits of a tile
 constexpr int64_t kMaxGrid = (int64_t(1) << 24) - 1;  // a launch's work-items (256 per workgroup) stay below 2^32
 
 int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }
-
-// 64 tokens x 64 vocabulary entries of the logits in fp32, 4 x 4 per thread: acc[i][j] is that of token t0 + 4 (thread / 16)
-// + i and entry v0 + 4 (thread % 16) + j. For rows of K that the matrix-instruction kernels do not take; bound by LDS reads
-// (two of 16 bytes per 16 products).
-template <int DT>
-__device__ __forceinline__ void logits_tile(const CeArgs &a, int64_t t0, int64_t v0, float (&acc)[4][4]) {
-    __shared__ float As[16][68];
-    __shared__ float Bs[16][68];
-    const int tx = threadIdx.x % 16, ty = threadIdx.x / 16;
-#pragma unroll
-    for (int i = 0; i < 4; i++)
-#pragma unroll
-        for (int j = 0; j < 4; j++) acc[i][j] = 0.0f;
-    for (int64_t k0 = 0; k0 < a.K; k0 += 16) {
-        for (int i = threadIdx.x; i < 64 * 16; i += 256) {
-            const int r = i / 16, kk = i % 16;
-            const int64_t k = k0 + kk;
-            As[kk][r] = t0 + r < a.T && k < a.K ? load1(a.X, DT, (t0 + r) * a.K + k) : 0.0f;
-            Bs[kk][r] = v0 + r < a.V && k < a.K ? load1(a.W, DT, (v0 + r) * a.K + k) : 0.0f;
-        }
-        __syncthreads();
-#pragma unroll
-        for (int kk = 0; kk < 16; kk++) {
-            float x[4], w[4];
-#pragma unroll
-            for (int i = 0; i < 4; i++) {
-                x[i] = As[kk][ty * 4 + i];
-                w[i] = Bs[kk][tx * 4 + i];
-            }
-#pragma unroll
-            for (int i = 0; i < 4; i++)
-#pragma unroll
-                for (int j = 0; j < 4; j++) acc[i][j] = __builtin_fmaf(x[i], w[j], acc[i][j]);
-        }
-        __syncthreads();
-    }
-}
-
-template <int DT>
-__global__ void __launch_bounds__(256) ce_stats_kernel(CeArgs a) {
-    const int tile = (int)(blockIdx.x % (unsigned)a.tiles_v);
-    const int64_t t0 = a.t0 + (int64_t)(blockIdx.x / (unsigned)a.tiles_v) * kTileT, v0 = (int64_t)tile * kTileV;
-    float acc[4][4];
-    logits_tile<DT>(a, t0, v0, acc);
-    const int tx = threadIdx.x % 16, ty = threadIdx.x / 16;
-    const float kNone = -__builtin_inff();
-#pragma unroll
-    for (int i = 0; i < 4; i++) {
-        const int64_t t = t0 + ty * 4 + i;
-        const int64_t want = a.target && t < a.T ? a.target[t] : -1;
-        float m = kNone;
-#pragma unroll
-        for (int j = 0; j < 4; j++) {
-            const int64_t v = v0 + tx * 4 + j;
-            if (v >= a.V) acc[i][j] = kNone;
-            else if (v == want) a.zt[t] = acc[i][j];
-            m = fmaxf(m, acc[i][j]);
-        }
-        for (int s = 8; s >= 1; s >>= 1) m = fmaxf(m, __shfl_xor(m, s, 64));
-        float sum = 0.0f;
-#pragma unroll
-        for (int j = 0; j < 4; j++) sum += expf(acc[i][j] - m);  // a NaN stays one
-        for (int s = 8; s >= 1; s >>= 1) sum += __shfl_xor(sum, s, 64);
-        if (tx == 0 && t < a.T) a.part[(int64_t)tile * a.T + t] = make_float2(m, sum);
-    }
-}
 
 // Joins the parts of a token: m = max m_i, s = sum s_i exp(m_i - m), in a fixed order. A workgroup takes `tokens` (a power of two)
 // neighbours, so that its loads run along part's rows; the 256 / tokens threads of one take every so many-th part, eight at a time
@@ -138,91 +71,6 @@ __global__ void __launch_bounds__(256) ce_join_kernel(CeArgs a, int tiles, int t
     if (bad) raise_domain_flag(flag);
 }
 
-// D of the piece's tile, in fp32. This and the product below are for rows of K that no matrix-instruction kernel takes, and not tuned:
-// 301 x 5,003 x 1,001 195 us forward and 1.29 ms backward, with K = 1,008 47 and 139 in fp32, 17 and 60 in bf16.
-template <int DT>
-__global__ void __launch_bounds__(256) ce_grad_kernel(CeArgs a, uint32_t *flag) {
-    const int tile = (int)(blockIdx.x % (unsigned)a.tiles_v);
-    const int64_t t0 = a.t0 + (int64_t)(blockIdx.x / (unsigned)a.tiles_v) * kTileT, v0 = a.v0 + (int64_t)tile * kTileV;
-    float acc[4][4];
-    logits_tile<DT>(a, t0, v0, acc);
-    const int tx = threadIdx.x % 16, ty = threadIdx.x / 16;
-    bool bad = false;
-#pragma unroll
-    for (int i = 0; i < 4; i++) {
-        const int64_t t = t0 + ty * 4 + i;
-        if (t >= a.T) continue;
-        const int64_t want = a.target ? a.target[t] : -1;
-        const bool there = want >= 0 && want < a.V;
-        const float g = a.g && there ? a.g[t] : 0.0f, h = a.h ? a.h[t] : 0.0f, lse = a.lse[t];
-        const bool none = g == 0.0f && h == 0.0f;
-        bad = bad || want >= a.V || ((g != 0.0f || h != 0.0f) && !(__builtin_fabsf(lse) <= 65536.0f));
-#pragma unroll
-        for (int j = 0; j < 4; j++) {
-            const int64_t v = v0 + tx * 4 + j;
-            if (v - a.v0 >= a.pitch) continue;
-            const float p = expf(acc[i][j] - lse);
-            static_cast<float *>(a.D)[t * a.pitch + (v - a.v0)] = v < a.V && !none ? (v == want ? g : 0.0f) + (h - g) * p : 0.0f;
-        }
-    }
-    if (bad) raise_domain_flag(flag);
-}
-
-// C[m][n] = before[m][n] + sum_r A(m, r) B[r][n] in fp32, 64 x 64 per workgroup, A(m, r) at A[m am + r ar]; written to
-// `sums` in fp32, or to `out` in its type. rows: row r of B is token r's, zeros where that has no gradient.
-struct CeProduct {
-    const float *A, *before, *g, *h;
-    const int64_t *target;
-    const void *B;
-    float *sums;
-    void *out;
-    int64_t am, ar, M, N, R, m0, V;
-    int b_dtype, out_dtype, tiles_n, rows;
-};
-__global__ void __launch_bounds__(256) ce_product_kernel(CeProduct a) {
-    __shared__ float As[16][68];
-    __shared__ float Bs[16][68];
-    const int64_t m0 = a.m0 + (int64_t)(blockIdx.x / (unsigned)a.tiles_n) * 64, n0 = (int64_t)(blockIdx.x % (unsigned)a.tiles_n) * 64;
-    const int tx = threadIdx.x % 16, ty = threadIdx.x / 16;
-    float acc[4][4] = {};
-    for (int64_t r0 = 0; r0 < a.R; r0 += 16) {
-        for (int i = threadIdx.x; i < 64 * 16; i += 256) {
-            const bool along_m = a.am == 1;
-            const int m = along_m ? i % 64 : i / 16, ra = along_m ? i / 64 : i % 16, n = i % 64, rb = i / 64;
-            As[ra][m] = m0 + m < a.M && r0 + ra < a.R ? a.A[(m0 + m) * a.am + (r0 + ra) * a.ar] : 0.0f;
-            const bool real = n0 + n < a.N && r0 + rb < a.R && (!a.rows || ce_takes_part(a.target, a.g, a.h, a.V, r0 + rb));
-            Bs[rb][n] = real ? load1(a.B, a.b_dtype, (r0 + rb) * a.N + n0 + n) : 0.0f;
-        }
-        __syncthreads();
-#pragma unroll
-        for (int rr = 0; rr < 16; rr++) {
-            float x[4], y[4];
-#pragma unroll
-            for (int i = 0; i < 4; i++) {
-                x[i] = As[rr][ty * 4 + i];
-                y[i] = Bs[rr][tx * 4 + i];
-            }
-#pragma unroll
-            for (int i = 0; i < 4; i++)
-#pragma unroll
-                for (int j = 0; j < 4; j++) acc[i][j] = __builtin_fmaf(x[i], y[j], acc[i][j]);
-        }
-        __syncthreads();
-    }
-#pragma unroll
-    for (int i = 0; i < 4; i++) {
-        const int64_t m = m0 + ty * 4 + i;
-#pragma unroll
-        for (int j = 0; j < 4; j++) {
-            const int64_t n = n0 + tx * 4 + j;
-            if (m >= a.M || n >= a.N) continue;
-            const float v = acc[i][j] + (a.before ? a.before[m * a.N + n] : 0.0f);
-            if (a.sums) a.sums[m * a.N + n] = v;
-            else store1(a.out, a.out_dtype, m * a.N + n, v);
-        }
-    }
-}
-
 // Runs of row tiles whose launches stay within the grid's limit: f(first row tile, row tiles)
 template <typename F>
 hipError_t in_runs(int64_t tiles_m, int64_t tiles_n, F &&f) {
@@ -233,14 +81,6 @@ hipError_t in_runs(int64_t tiles_m, int64_t tiles_n, F &&f) {
         if (e != hipSuccess) return e;
     }
     return hipSuccess;
-}
-
-hipError_t product(CeProduct p, hipStream_t st) {
-    p.tiles_n = (int)cdiv(p.N, 64);
-    return in_runs(cdiv(p.M, 64), p.tiles_n, [&](int64_t first, int64_t count) {
-        p.m0 = first * 64;
-        ce_product_kernel<<<(unsigned)(count * p.tiles_n), 256, 0, st>>>(p);
-    });
 }
 
 size_t round256(size_t b) { return (b + 255) / 256 * 256; }
@@ -340,7 +180,39 @@ hipError_t in_elements(int64_t n, F &&f) {
     return hipSuccess;
 }
 
-bool on_mfma(int dtype, int64_t K) { return dtype == kBF16 && K % 16 == 0; }
+// ---- rows of another K than a multiple of 16 ------------------------------------------------------
+int64_t padded(int64_t K) { return (K + 15) / 16 * 16; }
+
+// out [rows][to] = in [rows][from] with zeros behind, or without what is behind; a wave per row, element by element (rows start
+// anywhere), eight under way. Bound by memory: 32,000 x 2,561 bf16 64 us, 5.1 TB/s. 4,096 tokens x 32,000 x 2,561 take 769 us forward and
+// 2.21 ms backward with it, with 2,560 features 640 and 1.77.
+template <typename T>
+__global__ void __launch_bounds__(256) ce_pad_kernel(const T *__restrict__ in, int64_t first, int64_t rows, int64_t from, int64_t to,
+                                                     T *__restrict__ out) {
+    const int64_t row = first + (int64_t)blockIdx.x * 4 + threadIdx.x / 64;
+    if (row >= rows) return;
+    in += row * from, out += row * to;
+    for (int64_t c0 = threadIdx.x % 64; c0 < to; c0 += 64 * 8) {
+        T v[8];
+#pragma unroll
+        for (int u = 0; u < 8; u++) v[u] = c0 + 64 * u < from && c0 + 64 * u < to ? in[c0 + 64 * u] : T(0);
+#pragma unroll
+        for (int u = 0; u < 8; u++)
+            if (c0 + 64 * u < to) out[c0 + 64 * u] = v[u];
+    }
+}
+hipError_t copy_rows(int dtype, const void *in, int64_t rows, int64_t from, int64_t to, void *out, hipStream_t st) {
+    for (int64_t i = 0; i < rows; i += kMaxGrid * 4) {
+        const unsigned grid = (unsigned)cdiv(std::min(rows - i, kMaxGrid * 4), 4);
+        if (dtype == kBF16) ce_pad_kernel<<<grid, 256, 0, st>>>(static_cast<const uint16_t *>(in), i, rows, from, to, static_cast<uint16_t *>(out));
+        else ce_pad_kernel<<<grid, 256, 0, st>>>(static_cast<const float *>(in), i, rows, from, to, static_cast<float *>(out));
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
+}
+// bytes of a padded copy, of fp32 elements
+size_t pad_bytes(int64_t rows, int64_t K) { return K % 16 ? round256((size_t)rows * (size_t)padded(K) * sizeof(float)) : 0; }
 
 // Pieces of the vocabulary, of D takes 512 MiB each at most (in fp32, whose products are slower against what a piece costs, 128 MiB; a
 // tile's 256 entries each at least); the last one is what is left. 8,192 tokens, vocabulary 151,936, both
@@ -524,41 +396,21 @@ hipError_t bwd_mfma(CeArgs a, void *dX, void *dW, int dw_dtype, uint32_t *flag, 
     return hipSuccess;
 }
 
-}  // namespace
-
-size_t linear_ce_fwd_ws(int64_t T, int64_t V) {
-    // parts of 64 vocabulary entries, or of 32 in fp32 where there are fewer than 256 tiles of 64 x 64
-    const int64_t parts = std::max(cdiv(V, kTileV) * T, std::min(cdiv(V, 32) * T, int64_t(2) * 256 * 64));
-    return kWsHeader + round256((size_t)T * sizeof(float)) + (size_t)parts * sizeof(float2);
-}
-
-size_t linear_ce_bwd_ws(int64_t T, int64_t V, int64_t K) {
-    if (T == 0) return kWsHeader;
-    const size_t simple = kWsHeader + round256((size_t)T * (size_t)K * sizeof(float)) + piece_bytes(T, V, sizeof(float));
-    return std::max(simple, std::max(mfma_space(T, V, K, nullptr, nullptr), f32_space(T, V, K, nullptr, nullptr)));
-}
-
-hipError_t launch_linear_ce_fwd(int dtype, const void *X, const void *W, int64_t T, int64_t V, int64_t K, const int64_t *target,
-                                float *logp, float *lse, uint32_t *flag, void *ws, hipStream_t st) {
-    char *const base = static_cast<char *>(ws) + kWsHeader;
-    CeArgs a{};
-    a.X = X, a.W = W, a.target = target, a.lse = lse, a.logp = logp, a.T = T, a.V = V, a.K = K;
+hipError_t fwd(int dtype, CeArgs a, uint32_t *flag, char *base, hipStream_t st) {
     a.zt = reinterpret_cast<float *>(base);
-    a.part = reinterpret_cast<float2 *>(base + round256((size_t)T * sizeof(float)));
-    const bool mfma = on_mfma(dtype, K), few = mfma && T <= kCeFew, f32 = dtype == kF32 && ce_f32_supported(T, V, K);
-    const int64_t rows = mfma ? ce_mfma_tile(T, V) : f32 ? ce_f32_tile(T, V) : kTileT;
-    a.tiles_v = (int)cdiv(V, few ? kCeFewV : rows);
+    a.part = reinterpret_cast<float2 *>(base + round256((size_t)a.T * sizeof(float)));
+    const bool mfma = dtype == kBF16, few = mfma && a.T <= kCeFew;
+    const int64_t T = a.T, edge = mfma ? ce_mfma_tile(T, a.V) : ce_f32_tile(T, a.V);
+    a.tiles_v = (int)cdiv(a.V, few ? kCeFewV : edge);
     hipError_t e = hipSuccess;
     if (few) {
         launch_ce_stats_few(a, st);
         e = hipGetLastError();
     } else {
-        e = in_runs(cdiv(T, rows), a.tiles_v, [&](int64_t first, int64_t count) {
-            a.t0 = first * rows;
-            if (mfma) launch_ce_stats_mfma(a, rows, count * rows, st);
-            else if (f32) launch_ce_stats_f32(a, rows, count * rows, st);
-            else if (dtype == kBF16) ce_stats_kernel<kBF16><<<(unsigned)(count * a.tiles_v), 256, 0, st>>>(a);
-            else ce_stats_kernel<kF32><<<(unsigned)(count * a.tiles_v), 256, 0, st>>>(a);
+        e = in_runs(cdiv(T, edge), a.tiles_v, [&](int64_t first, int64_t count) {
+            a.t0 = first * edge;
+            if (mfma) launch_ce_stats_mfma(a, edge, count * edge, st);
+            else launch_ce_stats_f32(a, edge, count * edge, st);
         });
     }
     if (e != hipSuccess) return e;
@@ -567,50 +419,60 @@ hipError_t launch_linear_ce_fwd(int dtype, const void *X, const void *W, int64_t
     return hipGetLastError();
 }
 
+hipError_t bwd(int dtype, const CeArgs &a, void *dX, void *dW, int dw_dtype, uint32_t *flag, char *ws, hipStream_t st) {
+    return dtype == kBF16 ? bwd_mfma(a, dX, dW, dw_dtype, flag, ws, st)
+                          : bwd_f32(a, static_cast<float *>(dX), static_cast<float *>(dW), flag, ws, st);
+}
+
+// The workspace of rows that are multiples of 16
+size_t fwd_space(int64_t T, int64_t V) {
+    // parts of 64 vocabulary entries, or of 32 in fp32 where there are fewer than 256 tiles of 64 x 64
+    const int64_t parts = std::max(cdiv(V, 64) * T, std::min(cdiv(V, 32) * T, int64_t(2) * 256 * 64));
+    return kWsHeader + round256(round256((size_t)T * sizeof(float)) + (size_t)parts * sizeof(float2));
+}
+size_t bwd_space(int64_t T, int64_t V, int64_t K) {
+    return round256(std::max(mfma_space(T, V, K, nullptr, nullptr), f32_space(T, V, K, nullptr, nullptr)));
+}
+
+}  // namespace
+
+size_t linear_ce_fwd_ws(int64_t T, int64_t V, int64_t K) { return fwd_space(T, V) + pad_bytes(T, K) + pad_bytes(V, K); }
+
+size_t linear_ce_bwd_ws(int64_t T, int64_t V, int64_t K) {
+    return T == 0 ? kWsHeader : bwd_space(T, V, padded(K)) + 2 * (pad_bytes(T, K) + pad_bytes(V, K));
+}
+
+hipError_t launch_linear_ce_fwd(int dtype, const void *X, const void *W, int64_t T, int64_t V, int64_t K, const int64_t *target,
+                                float *logp, float *lse, uint32_t *flag, void *ws, hipStream_t st) {
+    char *const base = static_cast<char *>(ws);
+    CeArgs a{};
+    a.X = X, a.W = W, a.target = target, a.lse = lse, a.logp = logp, a.T = T, a.V = V, a.K = padded(K);
+    if (K % 16) {
+        char *const x = base + fwd_space(T, V), *const w = x + pad_bytes(T, K);
+        hipError_t e = copy_rows(dtype, X, T, K, a.K, x, st);
+        if (e == hipSuccess) e = copy_rows(dtype, W, V, K, a.K, w, st);
+        if (e != hipSuccess) return e;
+        a.X = x, a.W = w;
+    }
+    return fwd(dtype, a, flag, base + kWsHeader, st);
+}
+
 hipError_t launch_linear_ce_bwd(int dtype, const void *X, const void *W, int64_t T, int64_t V, int64_t K, const int64_t *target,
                                 const float *lse, const float *g, const float *h, void *dX, void *dW, int dw_dtype,
                                 uint32_t *flag, void *ws, hipStream_t st) {
-    char *const base = static_cast<char *>(ws) + kWsHeader;
-    float *const sums = reinterpret_cast<float *>(base);
+    char *const base = static_cast<char *>(ws);
     CeArgs a{};
-    a.X = X, a.W = W, a.target = target, a.lse = const_cast<float *>(lse), a.g = g, a.h = h, a.T = T, a.V = V, a.K = K;
-    if (dtype == kF32 && ce_f32_supported(T, V, K))
-        return bwd_f32(a, static_cast<float *>(dX), static_cast<float *>(dW), flag, static_cast<char *>(ws), st);
-    if (on_mfma(dtype, K)) return bwd_mfma(a, dX, dW, dw_dtype, flag, static_cast<char *>(ws), st);
-    a.D = base + round256((size_t)T * (size_t)K * sizeof(float));
-    const int64_t width = piece_width(T, V, sizeof(float));
-    const size_t esz = dtype == kBF16 ? 2 : 4, dsz = dw_dtype == kBF16 ? 2 : 4;
-    for (int64_t v0 = 0; v0 < V; v0 += width) {
-        const int64_t n = std::min(width, V - v0);
-        a.v0 = v0, a.pitch = n;
-        a.tiles_v = (int)cdiv(n, kTileV);
-        hipError_t e = in_runs(cdiv(T, kTileT), a.tiles_v, [&](int64_t first, int64_t count) {
-            a.t0 = first * kTileT;
-            if (dtype == kBF16) ce_grad_kernel<kBF16><<<(unsigned)(count * a.tiles_v), 256, 0, st>>>(a, flag);
-            else ce_grad_kernel<kF32><<<(unsigned)(count * a.tiles_v), 256, 0, st>>>(a, flag);
-        });
-        if (e != hipSuccess) return e;
-        const bool last = v0 + n == V;
-        if (dX) {
-            CeProduct p{};
-            p.A = static_cast<const float *>(a.D), p.am = n, p.ar = 1, p.M = T, p.N = K, p.R = n, p.b_dtype = dtype, p.out_dtype = dtype;
-            p.B = static_cast<const char *>(W) + (size_t)v0 * (size_t)K * esz;
-            p.before = v0 ? sums : nullptr;
-            p.sums = last ? nullptr : sums;
-            p.out = dX;
-            e = product(p, st);
-            if (e != hipSuccess) return e;
-        }
-        if (dW) {
-            CeProduct p{};
-            p.A = static_cast<const float *>(a.D), p.am = 1, p.ar = n, p.M = n, p.N = K, p.R = T, p.b_dtype = dtype, p.out_dtype = dw_dtype;
-            p.B = X, p.rows = 1, p.target = target, p.g = g, p.h = h, p.V = V;
-            p.out = static_cast<char *>(dW) + (size_t)v0 * (size_t)K * dsz;
-            e = product(p, st);
-            if (e != hipSuccess) return e;
-        }
-    }
-    return hipSuccess;
+    a.X = X, a.W = W, a.target = target, a.lse = const_cast<float *>(lse), a.g = g, a.h = h, a.T = T, a.V = V, a.K = padded(K);
+    if (K % 16 == 0) return bwd(dtype, a, dX, dW, dw_dtype, flag, base, st);
+    char *const x = base + bwd_space(T, V, padded(K)), *const w = x + pad_bytes(T, K), *const dx = w + pad_bytes(V, K), *const dw = dx + pad_bytes(T, K);
+    hipError_t e = copy_rows(dtype, X, T, K, a.K, x, st);
+    if (e == hipSuccess) e = copy_rows(dtype, W, V, K, a.K, w, st);
+    if (e != hipSuccess) return e;
+    a.X = x, a.W = w;
+    e = bwd(dtype, a, dX ? dx : nullptr, dW ? dw : nullptr, dw_dtype, flag, base, st);
+    if (e == hipSuccess && dX) e = copy_rows(dtype, dx, T, a.K, K, dX, st);
+    if (e == hipSuccess && dW) e = copy_rows(dw_dtype, dw, V, a.K, K, dW, st);
+    return e;
 }
 
 }  // namespace focus
