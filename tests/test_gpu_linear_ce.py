@@ -117,6 +117,23 @@ def test_fp32_weight_gradient_of_bf16_operands(F):
     assert torch.equal(dW.bfloat16(), half)
 
 
+@pytest.mark.parametrize("T,K", [(5, 33), (300, 1), (300, 1001)])
+def test_padded_rows(F, T, K):
+    # the workspace holds NaN, and the bytes around the outputs stay as they are
+    announce(f"linear ce padded T={T} K={K}")
+    X, W, target, g, h = make(T, 901, K, torch.bfloat16, 33)
+    ws = F.workspace(F.linear_ce_workspace_size(T, 901, K))
+    ws[256:] = 255
+    _, lse, dX, dW = check(F, X, W, target, g, h, dw_dtype=torch.float32, ws=ws)
+    rows = lambda n, dt: torch.full((n * K + 64,), 7.0, dtype=dt, device="cuda")
+    x, w = rows(T, torch.bfloat16), rows(901, torch.bfloat16)
+    a, b = F.linear_ce_bwd(X, W, target, lse, g, h, ws=ws, out=x[:T * K].view(T, K), dw_out=w[:901 * K].view(901, K))
+    assert torch.equal(a, dX) and torch.equal(b, dW.bfloat16())
+    assert (x[T * K:] == 7).all() and (w[901 * K:] == 7).all()
+    assert torch.equal(F.linear_ce_bwd(X, W, target, lse, g, h, want_dw=False, ws=ws)[0], dX)
+    assert torch.equal(F.linear_ce_bwd(X, W, target, lse, g, h, want_dx=False, dw_dtype=torch.float32, ws=ws)[1], dW)
+
+
 @pytest.mark.parametrize("dt", ["f32", "bf16"])
 def test_one_gradient_at_a_time(F, dt):
     announce(f"linear ce parts {dt}")

@@ -89,6 +89,7 @@ def test_linear_ce_checks(L, cpu_only):
                            (F.ERR_WORKSPACE, {"size": 256})):
             assert call(L, **kw) == status, (call, kw)
     assert ce_fwd(L, T=0, X=None, lse=None) == F.OK
+    assert ce_fwd(L, dt=0, T=(1 << 23) + 1) == F.ERR_SHAPE and ce_bwd(L, dt=0, wdt=0, T=(1 << 23) + 1) == F.ERR_SHAPE
     for kw in ({"lse": at(3)}, {"lse": at(0)}, {"lse": at(1)}, {"logp": at(2)}, {"logp": ctypes.c_void_p(at(4).value + 8)}):
         assert ce_fwd(L, **kw) == F.ERR_SHAPE, kw
     for status, kw in ((F.ERR_NULL, {"g": None}), (F.ERR_NULL, {"dX": None, "dW": None}), (F.ERR_DTYPE, {"wdt": 7}),
