@@ -259,6 +259,9 @@ __global__ void __launch_bounds__(WAVE ? kThreads : kMostThreads) sandwich_bwd_k
         for (int j = 0; j < NV; j++) zero8(sums[i][j]);
     const float inv_n = 1.0f / (float)C;
     Raw8<T> xr[NV], br[NV], nr[NV], yr[NV], gr[TOKEN ? NV : 1];
+    // B and a token's gate are needed to the row's end: the next row's have registers of their own, where there are as many
+    constexpr bool kAhead = !WAVE && !TAIL && sizeof(T) == 2;
+    Raw8<T> bn[kAhead ? NV : 1], gn[kAhead && TOKEN ? NV : 1];
     auto fetch = [&](Raw8<T> *to, const void *from, int64_t row) {
         const int n = row < last ? C : 0;
 #pragma unroll
@@ -287,6 +290,10 @@ __global__ void __launch_bounds__(WAVE ? kThreads : kMostThreads) sandwich_bwd_k
         // xh = h rstd - mean rstd in one operation: what the product is off by is as little as the mean itself may be
         const float rstd1 = stat[0], rstd2 = stat[1], off1 = -stat[2] * rstd1, off2 = -stat[3] * rstd2;
         if constexpr (!WAVE) fetch_stats(row + 1);
+        if constexpr (kAhead) {
+            fetch(bn, a.B, row + 1);
+            if constexpr (TOKEN) fetch(gn, a.gate, row + 1);
+        }
         // keeps the compiler from holding over the next sum what the packed rows and the LDS give again
         auto again = [&]() {
             asm volatile("" ::: "memory");
@@ -381,7 +388,13 @@ __global__ void __launch_bounds__(WAVE ? kThreads : kMostThreads) sandwich_bwd_k
                 }
             }
         }
-        if constexpr (!WAVE) {
+        if constexpr (kAhead) {
+#pragma unroll
+            for (int j = 0; j < NV; j++) {
+                br[j] = bn[j];
+                if constexpr (TOKEN) gr[j] = gn[j];
+            }
+        } else if constexpr (!WAVE) {
             fetch(br, a.B, row + 1);
             if constexpr (TOKEN) fetch(gr, a.gate, row + 1);
         }
