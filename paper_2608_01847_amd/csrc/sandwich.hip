@@ -239,10 +239,12 @@ __global__ void __launch_bounds__(WAVE ? kThreads : kMostThreads) sandwich_fwd_k
 
 // Rows, threads and the next row's pieces as in the forward; the sums over the rows stay in registers and leave as one row of
 // partial sums per workgroup (waves that take rows by themselves are added in order through LDS first). BIAS: the sums without xh too.
-// Memory and its latency bound it: 65,536 x 2,560 bf16 505 us, 4.0 TB/s, bytes 1.00 times the tensors'; 8,192 x 8,192 with token gates
-// 211 us, 5.1 TB/s. At 65,536 x 2,560 a workgroup of 256 threads with two vectors each took 522, one of five waves without the next row
-// under way 577 to 610, with it but the parameters converted anew for each row 534; 8,192 x 8,192 350 before, 211 after. A wave per
-// row: 131,072 x 1,024 295 us, 4.5 TB/s; 262,144 x 512 with token gates 444.
+// Memory and its latency bound it: 65,536 x 2,560 bf16 459 us, 4.4 TB/s, bytes 1.00 times the tensors', without a gradient of Y 407;
+// 8,192 x 8,192 with token gates 192 us, 5.6 TB/s. The next row's B and gates have registers of their own where there are as many (bf16,
+// rows of whole eights), since the present ones are needed to the row's end: fetched there they took 485, 465 and 198 us; dN and dY the same
+// way 468 and 440. Before, at 65,536 x 2,560, a workgroup of 256 threads with two vectors each took 8% longer than one of five waves, that
+// without the next row under way 20% and with the parameters converted anew for each row 6%. A wave per row: 131,072 x 1,024 295 us,
+// 4.5 TB/s; 262,144 x 512 with token gates 444.
 template <typename T, bool WAVE, int NV, bool BIAS, bool TOKEN, bool TAIL>
 __global__ void __launch_bounds__(WAVE ? kThreads : kMostThreads) sandwich_bwd_kernel(SandwichArgs a) {
     constexpr int kRows = WAVE ? 4 : 1;
