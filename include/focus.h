@@ -572,8 +572,9 @@ focus_status focus_linear_ce_fwd(const void *X, const void *W, int dtype, int64_
  *   D[t][v] = g ([v == target[t]] - p) + h p,  p = exp(Z[t][v] - lse[t]);  dX = D W,  dW = D^T X
  * (the mean cross entropy of n tokens: d_logp = -1/n; a penalty on lse: d_lse). The vocabulary goes in pieces, of each of
  * which the logits are formed again: D of one piece is what lies in memory, 512 MiB at most up to 2^20 tokens (fp32: twice 128 MiB,
- * up to 2^17 tokens). bf16 operands: D is rounded to bf16 relative to the larger of |d_logp| and |d_lse| of its token, and X times the
- * token's share of the largest of these to bf16 for dW (nothing is rounded there where all are the same, as in a mean).
+ * up to 2^17 tokens). bf16 operands: D is rounded to bf16, independently entry by entry, and what that takes from a target's entry,
+ * most of a token's D as a rule, goes into both gradients by itself: they are off by their own rounding (none of a dW in fp32), and
+ * by what rounding the other entries costs, 2^-9 of these in the mean.
  *   d_logp_opt [T] fp32 needs target_opt; one of d_logp_opt, d_lse_opt is given at least (FOCUS_ERR_NULL).
  *   dX_opt [T][K] (dtype), dW_opt [V][K] (dw_dtype: FOCUS_F32, or FOCUS_BF16 with bf16 operands): overwritten, one of them is
  *   wanted at least. dW in fp32 is the G of focus_fakequant_bwd. With T == 0 dW is zeros.

@@ -172,10 +172,12 @@ hipError_t launch_dx_mfma(const void *dY, const void *W, int64_t M, int64_t N, i
 // dY W as fp32 sums of its splits in part [splits][M][K], dY [M][ldy] with zeros behind its N columns to the next multiple of 32
 hipError_t launch_dx_sums(const void *dY, const void *W, int64_t M, int64_t N, int64_t ldy, int64_t K, int64_t chunk,
                           int64_t splits, float *part, hipStream_t st);
-// out [N][K] = factor dY^T X (bf16 operands, dY [M][ldy] with ldy a multiple of 256); with splits > 1 the token ranges' fp32 sums
-// without the factor in part [splits][N][K] in place of out
+// out [N][K] = factor (dY + R)^T X (bf16 operands, dY [M][ldy] with ldy a multiple of 256); with splits > 1 the token ranges' fp32 sums
+// without the factor in part [splits][N][K] in place of out. R has one number per token, rest[m] in column place[m] - v0 if that is one
+// of the N (place NULL: none), which is rounded to bf16
 hipError_t launch_dw_mfma(const void *dY, const void *X, int64_t M, int64_t N, int64_t ldy, int64_t K, int64_t chunk,
-                          int64_t splits, const float *factor, void *out, int out_dtype, float *part, hipStream_t st);
+                          int64_t splits, const float *factor, const int32_t *place, const float *rest, int64_t v0, void *out,
+                          int out_dtype, float *part, hipStream_t st);
 // the same product from packed MXFP4 operands (X codes [M][K/2], W codes in K-slabs [K/128][N][64],
 // block-major E8M0 bytes [K/32][rows]; K % 128 == 0)
 bool mfma_fwd_mx_supported(int64_t M, int64_t N, int64_t K);

@@ -638,13 +638,120 @@ bwd_mfma_kernel(const uint16_t *__restrict__ dY, const uint16_t *__restrict__ X,
                            part_c, direct, flag, smem);
 }
 
-// The plain product dW [N][K] = dY^T X, times *factor: dY [M][ldy] with N real columns (the others up to the tile's end exist and
-// are not stored). With `part` a token range of `chunk` per split, whose fp32 sums go to part [split][N][K]. Bound as the backward
-// whose main loop it has: 8,192 tokens x 32,768 x 2,560 1.06 to 1.08 ms, 1.27 PFLOP/s; the tile leaves through LDS in 16-byte pieces.
+// acc += the tile of X^T R, where R [tokens][columns of the tile] holds one number per token at most: rest[t] in column place[t] - v0.
+// The tokens that have one are listed in order, 4,096 looked at together, and multiplied 32 at a time: their rows of X are staged as the
+// main loop's, R's fragments are made in registers. Bound by the latency of the look (0.7 us of a tile that has none) and of the first
+// rows (5 us), then 1.3 us per 32 tokens (0.9 in the main loop): 1,000 x 8,000 x 2,048, 33 of its tokens per tile, 42 -> 50 us, 8,192 x
+// 1,000 x 2,560, 350 of them, 52 -> 72.
+constexpr int kRestTokens = 4096, kRestList = kRestTokens + 4 * kBwdStep;  // behind the last, entries of no column: groups are read unasked
+__device__ __forceinline__ void rest_products(const int32_t *__restrict__ place, const float *__restrict__ rest,
+                                              const uint16_t *__restrict__ X, int64_t K, int32_t v0, int64_t k0, int64_t t_begin,
+                                              int64_t t_end, char *smem, f32x16_t (&acc)[4][4]) {
+    constexpr int kLook = kRestTokens / kThreads;
+    const int t = threadIdx.x, lane = t & 63, wave = t >> 6, wm = wave >> 1, wn = wave & 1, lr = lane & 31, lh = lane >> 5;
+    // two stages of 32 rows of X, then the list
+    uint32_t *const list = reinterpret_cast<uint32_t *>(smem + 2 * kBwdOpBytes);  // token (from the first looked at) and column
+    float *const value = reinterpret_cast<float *>(list + kRestList);
+    int *const counts = reinterpret_cast<int *>(value + kRestList);
+    uint32_t a_off[4];
+#pragma unroll
+    for (int i = 0; i < 4; i++) a_off[i] = tr_lane_off(wm * 128 + i * 32, lane);
+    for (int64_t c = t_begin; c < t_end; c += kRestTokens) {
+        const int first = wave * (kRestTokens / 4) + lane;  // this thread's are first + 64 u
+        int col[kLook], n = 0;
+        float v[kLook];
+#pragma unroll
+        for (int u = 0; u < kLook; u++) {
+            const bool there = c + first + 64 * u < t_end;
+            col[u] = there ? place[c + first + 64 * u] - v0 : -1;
+            v[u] = there ? rest[c + first + 64 * u] : 0.0f;
+        }
+#pragma unroll
+        for (int u = 0; u < kLook; u++) n += __popcll(__ballot((unsigned)col[u] < (unsigned)kTile));
+        __syncthreads();  // the operand stages, or the list, are done with
+        if (lane == 0) counts[wave] = n;
+        __syncthreads();
+        int at = 0, total = 0;
+#pragma unroll
+        for (int w = 0; w < 4; w++) {
+            at += w < wave ? counts[w] : 0;
+            total += counts[w];
+        }
+        if (total == 0) continue;  // of every thread
+#pragma unroll
+        for (int u = 0; u < kLook; u++) {
+            const bool here = (unsigned)col[u] < (unsigned)kTile;
+            const uint64_t mask = __ballot(here);
+            if (here) {
+                const int i = at + __popcll(mask & ((uint64_t(1) << lane) - 1));
+                list[i] = (uint32_t)(first + 64 * u) << 9 | (uint32_t)col[u];
+                value[i] = v[u];
+            }
+            at += __popcll(mask);
+        }
+        if (t < 4 * kBwdStep) list[total + t] = kTile, value[total + t] = 0.0f;
+        __syncthreads();
+        auto fetch = [&](u32x4_t (&x)[4], int group) {  // the pieces that BwdDma would bring
+#pragma unroll
+            for (int i = 0; i < 4; i++) {
+                const int row = 2 * (wave * 4 + i) + lh;
+                const int64_t k = k0 + ((lr ^ ((row & 3) << 2)) * 8);  // past K: rows of the tile that are not stored
+                x[i] = *reinterpret_cast<const u32x4_t *>(X + (c + (list[group * kBwdStep + row] >> 9)) * K + (k < K ? k : 0));
+            }
+        };
+        auto multiply = [&](u32x4_t (&x)[4], int group) {
+            char *const stage = smem + (group & 1) * kBwdOpBytes;  // last read before the previous group's barrier
+#pragma unroll
+            for (int i = 0; i < 4; i++) *reinterpret_cast<u32x4_t *>(stage + (wave * 4 + i) * 1024 + lane * 16) = x[i];
+            fetch(x, group + 2);
+            __syncthreads();
+            asm volatile("" ::: "memory");  // the reads below are asm
+            const uint32_t base = lds_addr(stage);
+            static_for<2>([&](auto ks) {
+                constexpr int kRow = decltype(ks)::value * 16 * kBwdRowBytes;
+                Frags f;
+                static_for<4>([&](auto i) {
+                    const i16x4_t va[2] = {ds_read_tr<kRow>(base + a_off[i]), ds_read_tr<kRow + 4 * kBwdRowBytes>(base + a_off[i])};
+                    f.a[i] = __builtin_bit_cast(bf16x8_t, va);
+                });
+                const int e0 = group * kBwdStep + 16 * ks + 8 * lh;
+                uint32_t of[8];
+                float w[8];
+#pragma unroll
+                for (int h = 0; h < 2; h++) {
+                    const u32x4_t l = reinterpret_cast<const u32x4_t *>(list + e0)[h], m = reinterpret_cast<const u32x4_t *>(value + e0)[h];
+#pragma unroll
+                    for (int e = 0; e < 4; e++) of[4 * h + e] = l[e] & 511u, w[4 * h + e] = __uint_as_float(m[e]);
+                }
+                static_for<4>([&](auto j) {
+                    const uint32_t own = wn * 128 + 32 * j + lr;
+                    u32x4_t b;
+#pragma unroll
+                    for (int e = 0; e < 4; e++)
+                        b[e] = cvt_pk_bf16(of[2 * e] == own ? w[2 * e] : 0.0f, of[2 * e + 1] == own ? w[2 * e + 1] : 0.0f);
+                    f.b[j] = __builtin_bit_cast(bf16x8_t, b);
+                });
+                tr_wait(f);
+                mma_frags(f, acc);
+            });
+        };
+        u32x4_t xa[4], xb[4];  // rows of two groups under way
+        fetch(xa, 0);
+        fetch(xb, 1);
+        for (int group = 0; group * kBwdStep < total; group += 2) {
+            multiply(xa, group);
+            if ((group + 1) * kBwdStep < total) multiply(xb, group + 1);
+        }
+    }
+}
+
+// The plain product dW [N][K] = (dY + R)^T X, times *factor: dY [M][ldy] with N real columns (the others up to the tile's end exist and
+// are not stored), R as above with `place`. With `part` a token range of `chunk` per split, whose fp32 sums go to part [split][N][K]. Bound
+// as the backward whose main loop it has: 8,192 tokens x 32,768 x 2,560 1.06 to 1.08 ms, 1.27 PFLOP/s; the tile leaves through LDS in 16-byte pieces.
 __global__ void __launch_bounds__(kThreads, 1)
 dw_mfma_kernel(const uint16_t *__restrict__ dY, const uint16_t *__restrict__ X, int64_t M, int64_t N, int64_t ldy, int64_t K,
-               int64_t chunk, const float *__restrict__ factor, void *__restrict__ out, int out_dtype, float *__restrict__ part,
-               int tiles_n) {
+               int64_t chunk, const float *__restrict__ factor, const int32_t *__restrict__ place, const float *__restrict__ rest,
+               int32_t v0, void *__restrict__ out, int out_dtype, float *__restrict__ part, int tiles_n) {
     __shared__ __attribute__((aligned(16))) char smem[kBwdStages * kBwdStageBytes];
     const uint32_t id = xcd_tile(blockIdx.y * gridDim.x + blockIdx.x, gridDim.x * gridDim.y);
     uint32_t tk, tn;
@@ -654,6 +761,8 @@ dw_mfma_kernel(const uint16_t *__restrict__ dY, const uint16_t *__restrict__ X, 
     const int64_t t_begin = split * chunk, t_end = std::min<int64_t>(M, t_begin + chunk);
     f32x16_t acc[4][4];
     bwd_products(dY, X, ldy, K, n0, k0, t_begin, t_end, smem, acc);
+    static_assert(sizeof(smem) >= 2 * kBwdOpBytes + 2 * kRestList * 4 + 16, "what the rests take fits");
+    if (place) rest_products(place, rest, X, K, v0 + (int32_t)n0, k0, t_begin, t_end, smem, acc);
     __syncthreads();  // every wave is done with the operand stages
     if (part) {
         store_tile_f32(acc, smem, part + (split * N + n0) * K, N - n0, K, (uint32_t)k0, K);
@@ -1170,11 +1279,12 @@ hipError_t launch_dx_sums(const void *dY, const void *W, int64_t M, int64_t N, i
 }
 
 hipError_t launch_dw_mfma(const void *dY, const void *X, int64_t M, int64_t N, int64_t ldy, int64_t K, int64_t chunk,
-                          int64_t splits, const float *factor, void *out, int out_dtype, float *part, hipStream_t st) {
+                          int64_t splits, const float *factor, const int32_t *place, const float *rest, int64_t v0, void *out,
+                          int out_dtype, float *part, hipStream_t st) {
     const int tiles_k = (int)((K + kTile - 1) / kTile), tiles_n = (int)((N + kTile - 1) / kTile);
     dw_mfma_kernel<<<dim3((unsigned)tiles_k * tiles_n, (unsigned)splits), kThreads, 0, st>>>(
-        static_cast<const uint16_t *>(dY), static_cast<const uint16_t *>(X), M, N, ldy, K, chunk, factor, out, out_dtype,
-        splits > 1 ? part : nullptr, tiles_n);
+        static_cast<const uint16_t *>(dY), static_cast<const uint16_t *>(X), M, N, ldy, K, chunk, factor, place, rest,
+        (int32_t)v0, out, out_dtype, splits > 1 ? part : nullptr, tiles_n);
     return hipGetLastError();
 }
 

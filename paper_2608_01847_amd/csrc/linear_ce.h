@@ -20,7 +20,8 @@ struct CeArgs {
     float2 *part;         // [tiles][T] maximum and sum of a tile's exponentials
     float *zt;            // [T] logit of the target
     void *D;              // [T][pitch] of the piece: fp32, or bf16 relative to the token's scale
-    const float *scale;   // [T] larger of |g| and |h|, what D is relative to
+    const float *scale;   // [T] the power of two at or below the larger of |g| and |h|, what D is relative to
+    float *rest;          // [T] what rounding the target's entry of D to bf16 left
     int64_t T, V, K, pitch, v0, t0;  // first vocabulary entry of the piece, first token of the launch
     int tiles_v;
 };

@@ -9,10 +9,13 @@
 // vocabulary; a second kernel joins the parts. Backward: the vocabulary goes in pieces; of each the logits are formed again
 // and D, which both products read, is what lies in memory.
 //
-// bf16 operands go to the matrix instructions (linear_ce_mfma.hip), D in bf16 relative to a token's scale
-// r = max(|g|, |h|):
-//   D = r D',  dX[t] = r[t] (D' W)[t],  dW = G D'^T X',  X'[t] = X[t] r[t] / G  (rounded),  G = max r
-// so that the tokens' weights are rounded into X' where they differ, and nowhere where they are those of a mean (X' is X then).
+// bf16 operands go to the matrix instructions (linear_ce_mfma.hip), D in bf16 relative to a token's scale r, the power of two at or
+// below max(|g|, |h|):
+//   D = r D',  dX[t] = r[t] (D' W)[t],  dW = G D'^T X',  X'[t] = X[t] r[t] / G,  G = max r
+// Scaling by powers of two rounds nothing. Rounding D' would cost the gradients as many digits as their own rounding does, nearly all of
+// them in one entry per token, the target's, which is most of a token's D and shared by all of its row: what that entry's rounding
+// leaves, e[t], goes into both gradients by itself,
+//   dX[t] += r[t] e[t] W[target[t]],  dW[target[t]] += G e[t] X'[t].
 // fp32 goes to the fp32 matrix instructions (gemm_f32.hip). Rows of another K than a multiple of 16 are padded with zeros first.
 #include "linear_ce.h"
 #include "ops_device.h"
@@ -86,18 +89,27 @@ hipError_t in_runs(int64_t tiles_m, int64_t tiles_n, F &&f) {
 size_t round256(size_t b) { return (b + 255) / 256 * 256; }
 
 // ---- around the matrix-instruction kernels ------------------------------------------------------
-// r[t] = max(|g|, |h|) of the tokens (g: 0 where left out) and G, their maximum, by one workgroup: 4,096 tokens 6 us, 8,192 9. (As
-// part of the next kernel, every workgroup of which forms G then, no faster: 1,500 x 3,001 x 512 backward 69 us, so 72.)
+// The power of two at or below a number that is not negative (0, infinity and NaN stay)
+__device__ __forceinline__ float power_below(float v) {
+    const uint32_t b = __float_as_uint(v);
+    if (b >= 0x7F800000u || b == 0) return v;
+    return __uint_as_float(b >= 0x00800000u ? b & 0x7F800000u : 0x80000000u >> __builtin_clz(b));
+}
+
+// r[t] of max(|g|, |h|) of the tokens (g: 0 where left out), their targets' places in the vocabulary (-1: none, or no gradient) and G, the
+// largest r, by one workgroup: 4,096 tokens 6 us, 8,192 9. (As part of the next kernel, every workgroup of which forms G then, no faster:
+// 1,500 x 3,001 x 512 backward 69 us, so 72.)
 __global__ void __launch_bounds__(1024) ce_scales_kernel(const int64_t *__restrict__ target, const float *__restrict__ g,
                                                          const float *__restrict__ h, int64_t T, int64_t V, float *__restrict__ r,
-                                                         float *__restrict__ most) {
+                                                         int32_t *__restrict__ place, float *__restrict__ most) {
     __shared__ float lds[16];
     float m = 0.0f;
     for (int64_t t = threadIdx.x; t < T; t += 1024) {
         const bool kept = g && target[t] >= 0 && target[t] < V;
         const float a = kept ? __builtin_fabsf(g[t]) : 0.0f, b = h ? __builtin_fabsf(h[t]) : 0.0f;
-        const float v = a > b || a != a ? a : b;  // a NaN stays one
+        const float v = power_below(a > b || a != a ? a : b);  // a NaN stays one
         r[t] = v;
+        place[t] = kept && v != 0.0f ? (int32_t)target[t] : -1;
         m = v > m || v != v ? v : m;
     }
     for (int d = 32; d >= 1; d >>= 1) {
@@ -111,7 +123,7 @@ __global__ void __launch_bounds__(1024) ce_scales_kernel(const int64_t *__restri
     *most = m;
 }
 
-// X' = X r / G, rounded to bf16; 8 elements per thread (K is a multiple of 16). A token whose gradient is 0 has a row of zeros. Bound
+// X' = X r / G, exact in bf16; 8 elements per thread (K is a multiple of 16). A token whose gradient is 0 has a row of zeros. Bound
 // by memory: 8,192 x 2,560 15 us, 5.6 TB/s.
 __global__ void __launch_bounds__(256) ce_scale_x_kernel(const uint16_t *__restrict__ X, const float *__restrict__ r,
                                                          const float *__restrict__ most, int64_t first, int64_t n, int64_t K,
@@ -126,12 +138,14 @@ __global__ void __launch_bounds__(256) ce_scale_x_kernel(const uint16_t *__restr
     store8_n(out + i, 8, v);
 }
 
-// total = before + the splits' sums in order; to `sums` in fp32, or times the row's (or everything's, or no) factor to `out`. Bound by
-// memory: three splits of 8,192 x 2,560, the sum so far and the new one 63 us, 6.6 TB/s (the splits partly from the caches); many splits
+// total = before + the splits' sums in order; to `sums` in fp32, or, with rest[t] W[place[t]] where `place` is given, times the row's (or
+// everything's, or no) factor to `out`. Bound by memory: three splits of 8,192 x 2,560, the sum so far and the new one 63 us, 6.6 TB/s (the splits partly from the caches); many splits
 // of little by their latency, hence eight under way (63 of 64 x 512: 9 us, one at a time 16)
 __global__ void __launch_bounds__(256) ce_sums_kernel(const float *__restrict__ part, int64_t splits, const float *__restrict__ before,
-                                                      const float *__restrict__ factor, int per_row, int64_t first, int64_t n, int64_t K,
-                                                      float *__restrict__ sums, void *__restrict__ out, int out_dtype) {
+                                                      const float *__restrict__ factor, int per_row, const int32_t *__restrict__ place,
+                                                      const float *__restrict__ rest, const uint16_t *__restrict__ W, int64_t first,
+                                                      int64_t n, int64_t K, float *__restrict__ sums, void *__restrict__ out,
+                                                      int out_dtype) {
     const int64_t i = first + ((int64_t)blockIdx.x * 256 + threadIdx.x) * 8;
     if (i >= n) return;
     float s[8], v[8];
@@ -160,8 +174,15 @@ __global__ void __launch_bounds__(256) ce_sums_kernel(const float *__restrict__ 
         store8_n(sums + i, 8, s);
         return;
     }
+    const int64_t row = per_row ? i / K : 0;
+    if (place && place[row] >= 0) {
+        const float e = rest[row];
+        load8_n(W + place[row] * K + (i - row * K), 8, v);
+#pragma unroll
+        for (int u = 0; u < 8; u++) s[u] = __builtin_fmaf(e, v[u], s[u]);
+    }
     if (factor) {
-        const float f = per_row ? factor[i / K] : *factor;
+        const float f = factor[row];
 #pragma unroll
         for (int e = 0; e < 8; e++) s[e] *= f;
     }
@@ -254,7 +275,8 @@ size_t sums_bytes(int64_t T, int64_t V, int64_t K) {
 }
 
 struct MfmaSpace {
-    float *r, *most, *sums, *part;
+    float *r, *rest, *most, *sums, *part;
+    int32_t *place;
     uint16_t *x, *D;
 };
 size_t mfma_space(int64_t T, int64_t V, int64_t K, char *base, MfmaSpace *s) {
@@ -264,12 +286,14 @@ size_t mfma_space(int64_t T, int64_t V, int64_t K, char *base, MfmaSpace *s) {
         at += round256(bytes);
         return p;
     };
-    char *const most = take(sizeof(float)), *const r = take((size_t)T * sizeof(float)), *const x = take((size_t)T * (size_t)K * 2);
+    char *const most = take(sizeof(float)), *const r = take((size_t)T * sizeof(float)), *const rest = take((size_t)T * sizeof(float));
+    char *const place = take((size_t)T * sizeof(int32_t)), *const x = take((size_t)T * (size_t)K * 2);
     char *const sums = take((size_t)T * (size_t)K * sizeof(float)), *const part = take(sums_bytes(T, V, K));
     char *const D = take(piece_bytes(T, V, 2));
     if (s)
-        *s = MfmaSpace{reinterpret_cast<float *>(r), reinterpret_cast<float *>(most), reinterpret_cast<float *>(sums),
-                       reinterpret_cast<float *>(part), reinterpret_cast<uint16_t *>(x), reinterpret_cast<uint16_t *>(D)};
+        *s = MfmaSpace{reinterpret_cast<float *>(r),    reinterpret_cast<float *>(rest), reinterpret_cast<float *>(most),
+                       reinterpret_cast<float *>(sums), reinterpret_cast<float *>(part), reinterpret_cast<int32_t *>(place),
+                       reinterpret_cast<uint16_t *>(x), reinterpret_cast<uint16_t *>(D)};
     return at;
 }
 
@@ -315,7 +339,7 @@ hipError_t bwd_f32(CeArgs a, float *dX, float *dW, uint32_t *flag, char *ws, hip
     a.D = s.D;
     auto finish = [&](int64_t splits, const float *before, int64_t n, float *sums, float *out) {
         return in_elements(n, [&](int64_t first, unsigned grid) {
-            ce_sums_kernel<<<grid, 256, 0, st>>>(s.part, splits, before, nullptr, 0, first, n, K, sums, out, kF32);
+            ce_sums_kernel<<<grid, 256, 0, st>>>(s.part, splits, before, nullptr, 0, nullptr, nullptr, nullptr, first, n, K, sums, out, kF32);
         });
     };
     for (int64_t v0 = 0; v0 < V; v0 += width) {
@@ -348,10 +372,11 @@ hipError_t bwd_mfma(CeArgs a, void *dX, void *dW, int dw_dtype, uint32_t *flag, 
     MfmaSpace s;
     mfma_space(a.T, a.V, a.K, ws, &s);
     const int64_t T = a.T, V = a.V, K = a.K;
-    ce_scales_kernel<<<1, 1024, 0, st>>>(a.target, a.g, a.h, T, V, s.r, s.most);
+    ce_scales_kernel<<<1, 1024, 0, st>>>(a.target, a.g, a.h, T, V, s.r, s.place, s.most);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    a.scale = s.r, a.D = s.D;
+    a.scale = s.r, a.rest = s.rest, a.D = s.D;
+    const int32_t *const place = a.g ? s.place : nullptr;  // nothing is at a target's place without its gradient
     if (dW) {
         e = in_elements(T * K, [&](int64_t first, unsigned grid) {
             ce_scale_x_kernel<<<grid, 256, 0, st>>>(static_cast<const uint16_t *>(a.X), s.r, s.most, first, T * K, K, s.x);
@@ -376,19 +401,20 @@ hipError_t bwd_mfma(CeArgs a, void *dX, void *dW, int dw_dtype, uint32_t *flag, 
             if (e != hipSuccess) return e;
             const bool last = v0 + n == V;
             e = in_elements(T * K, [&](int64_t first, unsigned grid) {
-                ce_sums_kernel<<<grid, 256, 0, st>>>(s.part, p.count, v0 ? s.sums : nullptr, s.r, 1, first, T * K, K,
-                                                     last ? nullptr : s.sums, dX, kBF16);
+                ce_sums_kernel<<<grid, 256, 0, st>>>(s.part, p.count, v0 ? s.sums : nullptr, s.r, 1, place, s.rest,
+                                                     static_cast<const uint16_t *>(a.W), first, T * K, K, last ? nullptr : s.sums, dX, kBF16);
             });
             if (e != hipSuccess) return e;
         }
         if (dW) {
             char *const out = static_cast<char *>(dW) + (size_t)v0 * (size_t)K * (dw_dtype == kBF16 ? 2 : 4);
             const Splits p = mfma_splits(T, n, K);
-            e = launch_dw_mfma(s.D, s.x, T, n, width, K, p.chunk, p.count, s.most, out, dw_dtype, s.part, st);
+            e = launch_dw_mfma(s.D, s.x, T, n, width, K, p.chunk, p.count, s.most, place, s.rest, v0, out, dw_dtype, s.part, st);
             if (e != hipSuccess) return e;
             if (p.count > 1)
                 e = in_elements(n * K, [&](int64_t first, unsigned grid) {
-                    ce_sums_kernel<<<grid, 256, 0, st>>>(s.part, p.count, nullptr, s.most, 0, first, n * K, K, nullptr, out, dw_dtype);
+                    ce_sums_kernel<<<grid, 256, 0, st>>>(s.part, p.count, nullptr, s.most, 0, nullptr, nullptr, nullptr, first, n * K, K,
+                                                         nullptr, out, dw_dtype);
                 });
             if (e != hipSuccess) return e;
         }

@@ -220,9 +220,8 @@ __global__ void __launch_bounds__(kThreads, E == 256 ? 1 : 2) ce_stats_mfma_kern
     a.part[(int64_t)tv * a.T + own] = make_float2(m, (x.x == m ? x.y : x.y * expf(x.x - m)) + (y.x == m ? y.y : y.y * expf(y.x - m)));
 }
 
-// The tile of D: D[t][v] = (h - g) p + g [v == target] relative to the token's scale, p = exp(z - lse), rounded to bf16. Relative to
-// the scale, a target's entry is 1 - p, whose rounding does not depend on g: the weights of a mean, 1 / n, would otherwise round
-// every token's largest term alike, by up to 2^-8 of the whole gradient. Entries past V are zeros.
+// The tile of D: D[t][v] = (h - g) p + g [v == target] relative to the token's scale, p = exp(z - lse), rounded to bf16; what that
+// leaves of a target's entry, the largest of most tokens, goes to `rest`. Entries past V are zeros.
 template <int E>
 __global__ void __launch_bounds__(kThreads, E == 256 ? 1 : 2) ce_grad_mfma_kernel(CeArgs a, uint32_t *flag) {
     __shared__ __attribute__((aligned(16))) char smem[Geometry<E>::kLds];
@@ -253,9 +252,13 @@ __global__ void __launch_bounds__(kThreads, E == 256 ? 1 : 2) ce_grad_mfma_kerne
         static_for<N>([&](auto i) { static_for<16>([&](auto r) { acc[i][j][(int)r] = of.x * e(acc[i][j][(int)r]); }); });
         const int at = __float_as_int(of.w);
         if (near_any<E>(at)) {
+            float *const rest = a.rest + t0 + E / 2 * wn + 32 * j + lr;
             static_for<N>([&](auto i) {
                 static_for<16>([&](auto r) {
-                    if (at == entry_of<E>(i, r)) acc[i][j][(int)r] += of.y;
+                    if (at == entry_of<E>(i, r)) {
+                        const float full = acc[i][j][(int)r] += of.y;
+                        *rest = full - __uint_as_float(cvt_pk_bf16(full, 0.0f) << 16);
+                    }
                 });
             });
         }
