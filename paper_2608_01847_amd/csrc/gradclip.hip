@@ -153,7 +153,7 @@ __global__ void __launch_bounds__(256) grad_scale_kernel(GradGroup<OUT> a, const
     for (uint32_t c = blockIdx.x; c < a.chunks(); c += gridDim.x) {
         const int i = tensor_of(a, c);
         void *const out = OUT ? a.out[OUT ? i : 0] : const_cast<void *>(a.g[i]);
-        if (f.x == 1.0f && out == a.g[i]) continue;  // nothing to write
+        if (f.x == 1.0f && f.y == 1.0f && out == a.g[i]) continue;  // nothing to write
         const int64_t start = (int64_t)(c - a.first[i]) * kChunk;
         if (a.bf16[i / 32] >> (i % 32) & 1u)
             chunk_scale(static_cast<const uint16_t *>(a.g[i]), static_cast<uint16_t *>(out), start, a.n(i), f);
