@@ -157,7 +157,7 @@ struct SandwichArgs {
     float *dw1, *db1, *dw2, *db2;
     float *part;                            // [sums][workgroups][C]
     int64_t T, rows, first;                 // rows of a workgroup; first row of a launch
-    int C, w_dtype, layer, gate_kind, sums;
+    int C, w_dtype, layer, gate_kind, sums, chunk;  // chunk: rows that the backward adds up before they go to part
     float eps, scale;
 };
 size_t sandwich_bwd_ws(int64_t T, int64_t C);

@@ -18,6 +18,7 @@ namespace {
 
 constexpr int kThreads = 256;  // of a workgroup whose waves take rows by themselves, and of the kernels for long rows
 constexpr int kMostThreads = 1024;
+constexpr int kChunk = 64;     // rows whose gradients of a parameter are added up one by one in fp32, as a rule
 constexpr int kStrips = 1024;  // workgroups of a backward launch at most, each with a row of partial sums per parameter
 
 // Sums of two values over the threads that share a row, in every one of them: a wave (WAVE), or the workgroup of up to 16 waves.
@@ -237,8 +238,9 @@ __global__ void __launch_bounds__(WAVE ? kThreads : kMostThreads) sandwich_fwd_k
     }
 }
 
-// Rows, threads and the next row's pieces as in the forward; the sums over the rows stay in registers and leave as one row of
-// partial sums per workgroup (waves that take rows by themselves are added in order through LDS first). BIAS: the sums without xh too.
+// Rows, threads and the next row's pieces as in the forward; the sums over the rows stay in registers, for `chunk` of them (64 as a
+// rule, so that no chain of fp32 additions is as long as a workgroup's rows), and are then added to its row of partial sums (waves
+// that take rows by themselves are added in order through LDS first). BIAS: the sums without xh too.
 // Memory and its latency bound it: 65,536 x 2,560 bf16 459 us, 4.4 TB/s, bytes 1.00 times the tensors', without a gradient of Y 407;
 // 8,192 x 8,192 with token gates 192 us, 5.6 TB/s. The next row's B and gates have registers of their own where there are as many (bf16,
 // rows of whole eights), since the present ones are needed to the row's end: fetched there they took 485, 465 and 198 us; dN and dY the same
@@ -265,13 +267,13 @@ __global__ void __launch_bounds__(WAVE ? kThreads : kMostThreads) sandwich_bwd_k
     constexpr bool kAhead = !WAVE && !TAIL && sizeof(T) == 2;
     Raw8<T> bn[kAhead ? NV : 1], gn[kAhead && TOKEN ? NV : 1];
     auto fetch = [&](Raw8<T> *to, const void *from, int64_t row) {
-        const int n = row < last ? C : 0;
+        const int n = WAVE || row < last ? C : 0;  // waves ask for the rows that they take alone
 #pragma unroll
         for (int j = 0; j < NV; j++) load_piece<TAIL>(to[j], from, row * C, n, (j * n_row + t) * 8);
     };
     float stat[4];
     auto fetch_stats = [&](int64_t row) {
-        row = row < last ? row : first;
+        row = WAVE || row < last ? row : first;
 #pragma unroll
         for (int i = 0; i < 4; i++) stat[i] = i < 2 || a.layer ? a.stats[i * a.T + row] : 0.0f;
     };
@@ -286,147 +288,163 @@ __global__ void __launch_bounds__(WAVE ? kThreads : kMostThreads) sandwich_bwd_k
     if constexpr (!WAVE) fetch_all(first);
     const Params<BIAS, TOKEN> p(a, smem, NV * n_row * 8);
     __syncthreads();
-    for (int64_t row = first + sub; row < last; row += kRows) {
-        const int64_t at = row * C;
-        if constexpr (WAVE) fetch_all(row);
-        // xh = h rstd - mean rstd in one operation: what the product is off by is as little as the mean itself may be
-        const float rstd1 = stat[0], rstd2 = stat[1], off1 = -stat[2] * rstd1, off2 = -stat[3] * rstd2;
-        if constexpr (!WAVE) fetch_stats(row + 1);
-        if constexpr (kAhead) {
-            fetch(bn, a.B, row + 1);
-            if constexpr (TOKEN) fetch(gn, a.gate, row + 1);
-        }
-        // keeps the compiler from holding over the next sum what the packed rows and the LDS give again
-        auto again = [&]() {
-            asm volatile("" ::: "memory");
+    const int rows = (int)(last - first);
+    for (int start = 0; start < rows; start += a.chunk * kRows) {
+        const int end = rows - start < a.chunk * kRows ? rows : start + a.chunk * kRows;
+        for (int i = start + sub; i < end; i += kRows) {
+            const int64_t row = first + i, at = row * C;
+            if constexpr (WAVE) fetch_all(row);
+            // xh = h rstd - mean rstd in one operation: what the product is off by is as little as the mean itself may be
+            const float rstd1 = stat[0], rstd2 = stat[1], off1 = -stat[2] * rstd1, off2 = -stat[3] * rstd2;
+            if constexpr (!WAVE) fetch_stats(row + 1);
+            if constexpr (kAhead) {
+                fetch(bn, a.B, row + 1);
+                if constexpr (TOKEN) fetch(gn, a.gate, row + 1);
+            }
+            // keeps the compiler from holding over the next sum what the packed rows and the LDS give again
+            auto again = [&]() {
+                asm volatile("" ::: "memory");
+#pragma unroll
+                for (int j = 0; j < NV; j++) {
+                    br[j].keep_packed();
+                    if constexpr (WAVE) nr[j].keep_packed(), yr[j].keep_packed();
+                    if constexpr (TOKEN) gr[j].keep_packed();
+                }
+            };
+            // xh2 of the row, and the two means that the second norm's gradient takes
+            float d[NV][8], sg = 0.0f, sgx = 0.0f;
 #pragma unroll
             for (int j = 0; j < NV; j++) {
-                br[j].keep_packed();
-                if constexpr (WAVE) nr[j].keep_packed(), yr[j].keep_packed();
-                if constexpr (TOKEN) gr[j].keep_packed();
-            }
-        };
-        // xh2 of the row, and the two means that the second norm's gradient takes
-        float d[NV][8], sg = 0.0f, sgx = 0.0f;
-#pragma unroll
-        for (int j = 0; j < NV; j++) {
-            __builtin_amdgcn_sched_barrier(0);  // one vector's values in fp32 at a time
-            const int c = (j * n_row + t) * 8;
-            float w1[8], w2[8], b1[8];
-            lds8(p.w1 + c, w1);
-            lds8(p.w2 + c, w2);
-            if constexpr (BIAS) lds8(p.b1 + c, b1);
-#pragma unroll
-            for (int e = 0; e < 8; e++) {  // columns past C have dN = 0
-                const float xh1 = __builtin_fmaf(br[j][e], rstd1, off1);
-                float u = BIAS ? __builtin_fmaf(xh1, w1[e], b1[e]) : xh1 * w1[e];
-                if constexpr (TOKEN) u *= gr[TOKEN ? j : 0][e];
-                const float xh2 = __builtin_fmaf(__builtin_fmaf(a.scale, xr[j][e], u), rstd2, off2);
-                const float n = nr[j][e], g = n * w2[e];
-                sums[0][j][e] = __builtin_fmaf(n, xh2, sums[0][j][e]);
-                if constexpr (BIAS) sums[2][j][e] += n;
-                sg += g;
-                sgx = __builtin_fmaf(g, xh2, sgx);
-                d[j][e] = xh2;
-            }
-        }
-        if constexpr (!WAVE) fetch(xr, a.X, row + 1);
-        group_sum2<WAVE>(sg, sgx, lds[0]);
-        const float mg2 = a.layer ? sg * inv_n : 0.0f, mgx2 = sgx * inv_n;
-        sg = sgx = 0.0f;
-        again();
-#pragma unroll
-        for (int j = 0; j < NV; j++) {
-            __builtin_amdgcn_sched_barrier(0);
-            const int c = (j * n_row + t) * 8;
-            float w1[8], w2[8];
-            lds8(p.w1 + c, w1);
-            lds8(p.w2 + c, w2);
-#pragma unroll
-            for (int e = 0; e < 8; e++) {  // columns past C have w1 = 0
-                const float g2 = __builtin_fmaf(-d[j][e], mgx2, __builtin_fmaf(nr[j][e], w2[e], -mg2));
-                d[j][e] = __builtin_fmaf(rstd2, g2, yr[j][e]);
-                const float xh1 = __builtin_fmaf(br[j][e], rstd1, off1);
-                const float through = TOKEN ? d[j][e] * gr[TOKEN ? j : 0][e] : d[j][e];  // a feature's gate is applied to the sum
-                sums[1][j][e] = __builtin_fmaf(through, xh1, sums[1][j][e]);
-                if constexpr (BIAS) sums[3][j][e] += through;
-                const float g = through * w1[e];
-                sg += g;
-                sgx = __builtin_fmaf(g, xh1, sgx);
-            }
-        }
-        if constexpr (!WAVE) {
-            fetch(nr, a.dN, row + 1);
-            fetch(yr, a.dY, row + 1);
-        }
-        group_sum2<WAVE>(sg, sgx, lds[1]);
-        const float mg1 = a.layer ? sg * inv_n : 0.0f, mgx1 = sgx * inv_n;
-        again();
-#pragma unroll
-        for (int j = 0; j < NV; j++) {
-            const int c = (j * n_row + t) * 8;
-            __builtin_amdgcn_sched_barrier(0);
-            if (c < C) {
-                float v[8], w1[8], b1[8];
+                __builtin_amdgcn_sched_barrier(0);  // one vector's values in fp32 at a time
+                const int c = (j * n_row + t) * 8;
+                float w1[8], w2[8], b1[8];
                 lds8(p.w1 + c, w1);
+                lds8(p.w2 + c, w2);
                 if constexpr (BIAS) lds8(p.b1 + c, b1);
 #pragma unroll
-                for (int e = 0; e < 8; e++) v[e] = a.scale * d[j][e];
-                store8_n<TAIL>(static_cast<T *>(a.dX) + at + c, C - c, v);
-#pragma unroll
-                for (int e = 0; e < 8; e++) {
+                for (int e = 0; e < 8; e++) {  // columns past C have dN = 0
                     const float xh1 = __builtin_fmaf(br[j][e], rstd1, off1);
-                    const float g = (TOKEN ? d[j][e] * gr[TOKEN ? j : 0][e] : d[j][e]) * w1[e];
-                    v[e] = rstd1 * __builtin_fmaf(-xh1, mgx1, g - mg1);
-                }
-                store8_n<TAIL>(static_cast<T *>(a.dB) + at + c, C - c, v);
-                if (TOKEN && a.dgate) {
-#pragma unroll
-                    for (int e = 0; e < 8; e++) {
-                        const float xh1 = __builtin_fmaf(br[j][e], rstd1, off1);
-                        v[e] = d[j][e] * (BIAS ? __builtin_fmaf(xh1, w1[e], b1[e]) : xh1 * w1[e]);
-                    }
-                    store8_n<TAIL>(static_cast<T *>(a.dgate) + at + c, C - c, v);
+                    float u = BIAS ? __builtin_fmaf(xh1, w1[e], b1[e]) : xh1 * w1[e];
+                    if constexpr (TOKEN) u *= gr[TOKEN ? j : 0][e];
+                    const float xh2 = __builtin_fmaf(__builtin_fmaf(a.scale, xr[j][e], u), rstd2, off2);
+                    const float n = nr[j][e], g = n * w2[e];
+                    sums[0][j][e] = __builtin_fmaf(n, xh2, sums[0][j][e]);
+                    if constexpr (BIAS) sums[2][j][e] += n;
+                    sg += g;
+                    sgx = __builtin_fmaf(g, xh2, sgx);
+                    d[j][e] = xh2;
                 }
             }
-        }
-        if constexpr (kAhead) {
+            if constexpr (!WAVE) fetch(xr, a.X, row + 1);
+            group_sum2<WAVE>(sg, sgx, lds[0]);
+            const float mg2 = a.layer ? sg * inv_n : 0.0f, mgx2 = sgx * inv_n;
+            sg = sgx = 0.0f;
+            again();
 #pragma unroll
             for (int j = 0; j < NV; j++) {
-                br[j] = bn[j];
-                if constexpr (TOKEN) gr[j] = gn[j];
+                __builtin_amdgcn_sched_barrier(0);
+                const int c = (j * n_row + t) * 8;
+                float w1[8], w2[8];
+                lds8(p.w1 + c, w1);
+                lds8(p.w2 + c, w2);
+#pragma unroll
+                for (int e = 0; e < 8; e++) {  // columns past C have w1 = 0
+                    const float g2 = __builtin_fmaf(-d[j][e], mgx2, __builtin_fmaf(nr[j][e], w2[e], -mg2));
+                    d[j][e] = __builtin_fmaf(rstd2, g2, yr[j][e]);
+                    const float xh1 = __builtin_fmaf(br[j][e], rstd1, off1);
+                    const float through = TOKEN ? d[j][e] * gr[TOKEN ? j : 0][e] : d[j][e];  // a feature's gate is applied to the sum
+                    sums[1][j][e] = __builtin_fmaf(through, xh1, sums[1][j][e]);
+                    if constexpr (BIAS) sums[3][j][e] += through;
+                    const float g = through * w1[e];
+                    sg += g;
+                    sgx = __builtin_fmaf(g, xh1, sgx);
+                }
             }
-        } else if constexpr (!WAVE) {
-            fetch(br, a.B, row + 1);
-            if constexpr (TOKEN) fetch(gr, a.gate, row + 1);
-        }
-    }
-    float *const join = smem;  // a row's width, over the parameters
-#pragma unroll
-    for (int i = 0; i < kSums; i++) {
-        if constexpr (WAVE) {
-            for (int s = 1; s < kRows; s++) {
-                __syncthreads();
-                if (sub == s)
-#pragma unroll
-                    for (int j = 0; j < NV; j++)
-#pragma unroll
-                        for (int e = 0; e < 8; e++) join[(j * 8 + e) * 64 + t] = sums[i][j][e];
-                __syncthreads();
-                if (sub == 0)
-#pragma unroll
-                    for (int j = 0; j < NV; j++)
-#pragma unroll
-                        for (int e = 0; e < 8; e++) sums[i][j][e] += join[(j * 8 + e) * 64 + t];
+            if constexpr (!WAVE) {
+                fetch(nr, a.dN, row + 1);
+                fetch(yr, a.dY, row + 1);
             }
-        }
-        if (sub == 0) {
-            float *const part = a.part + ((int64_t)i * gridDim.x + blockIdx.x) * C;
+            group_sum2<WAVE>(sg, sgx, lds[1]);
+            const float mg1 = a.layer ? sg * inv_n : 0.0f, mgx1 = sgx * inv_n;
+            again();
 #pragma unroll
             for (int j = 0; j < NV; j++) {
                 const int c = (j * n_row + t) * 8;
-                if (c < C) store8_n<TAIL>(part + c, C - c, sums[i][j]);
+                __builtin_amdgcn_sched_barrier(0);
+                if (c < C) {
+                    float v[8], w1[8], b1[8];
+                    lds8(p.w1 + c, w1);
+                    if constexpr (BIAS) lds8(p.b1 + c, b1);
+#pragma unroll
+                    for (int e = 0; e < 8; e++) v[e] = a.scale * d[j][e];
+                    store8_n<TAIL>(static_cast<T *>(a.dX) + at + c, C - c, v);
+#pragma unroll
+                    for (int e = 0; e < 8; e++) {
+                        const float xh1 = __builtin_fmaf(br[j][e], rstd1, off1);
+                        const float g = (TOKEN ? d[j][e] * gr[TOKEN ? j : 0][e] : d[j][e]) * w1[e];
+                        v[e] = rstd1 * __builtin_fmaf(-xh1, mgx1, g - mg1);
+                    }
+                    store8_n<TAIL>(static_cast<T *>(a.dB) + at + c, C - c, v);
+                    if (TOKEN && a.dgate) {
+#pragma unroll
+                        for (int e = 0; e < 8; e++) {
+                            const float xh1 = __builtin_fmaf(br[j][e], rstd1, off1);
+                            v[e] = d[j][e] * (BIAS ? __builtin_fmaf(xh1, w1[e], b1[e]) : xh1 * w1[e]);
+                        }
+                        store8_n<TAIL>(static_cast<T *>(a.dgate) + at + c, C - c, v);
+                    }
+                }
             }
+            if constexpr (kAhead) {
+#pragma unroll
+                for (int j = 0; j < NV; j++) {
+                    br[j] = bn[j];
+                    if constexpr (TOKEN) gr[j] = gn[j];
+                }
+            } else if constexpr (!WAVE) {
+                fetch(br, a.B, row + 1);
+                if constexpr (TOKEN) fetch(gr, a.gate, row + 1);
+            }
+        }
+        int lane = t;
+        asm volatile("" : "+v"(lane));  // addresses formed here: formed before the rows, they would hold registers over them
+        float *const join = smem + (BIAS ? 4 : 2) * NV * n_row * 8;  // of waves that take rows by themselves: a row's width behind the parameters
+#pragma unroll
+        for (int i = 0; i < kSums; i++) {
+            if constexpr (WAVE) {
+                for (int s = 1; s < kRows; s++) {
+                    __syncthreads();
+                    if (sub == s)
+#pragma unroll
+                        for (int j = 0; j < NV; j++)
+#pragma unroll
+                            for (int e = 0; e < 8; e++) join[(j * 8 + e) * 64 + lane] = sums[i][j][e];
+                    __syncthreads();
+                    if (sub == 0)
+#pragma unroll
+                        for (int j = 0; j < NV; j++)
+#pragma unroll
+                            for (int e = 0; e < 8; e++) sums[i][j][e] += join[(j * 8 + e) * 64 + lane];
+                }
+            }
+            if (sub == 0) {
+                float *const part = a.part + ((int64_t)i * gridDim.x + blockIdx.x) * C;
+#pragma unroll
+                for (int j = 0; j < NV; j++) {
+                    const int c = (j * n_row + lane) * 8;
+                    if (c < C) {
+                        if (start) {
+                            float v[8];
+                            load8_n(part + c, TAIL ? C - c : 8, v);
+#pragma unroll
+                            for (int e = 0; e < 8; e++) sums[i][j][e] += v[e];
+                        }
+                        store8_n<TAIL>(part + c, C - c, sums[i][j]);
+                    }
+                }
+            }
+#pragma unroll
+            for (int j = 0; j < NV; j++) zero8(sums[i][j]);
         }
     }
 }
@@ -494,56 +512,76 @@ __global__ void __launch_bounds__(kThreads) sandwich_fwd_long_kernel(SandwichArg
     }
 }
 
-// A workgroup takes `rows` rows one after the other; the sums over them are added up in its row of the partial sums.
+// A workgroup takes `rows` rows, kLongRows at a time: first their means, row by row, then their gradients and the sums over them, column
+// by column, which are added to its row of the partial sums, so that no chain of fp32 additions is as long as its rows.
+constexpr int kLongRows = kChunk;
 template <typename T>
 __global__ void __launch_bounds__(kThreads) sandwich_bwd_long_kernel(SandwichArgs a) {
     __shared__ float lds[2][32];
+    __shared__ float4 means[kLongRows];  // of g2, g2 xh2, g1 and g1 xh1
     const int C = a.C;
     const int64_t first = (int64_t)blockIdx.x * a.rows;
     const int64_t last = first + a.rows < a.T ? first + a.rows : a.T;
     const int64_t strip = (int64_t)gridDim.x * C;
     float *const part = a.part + (int64_t)blockIdx.x * C;
-    for (int64_t row = first; row < last; row++) {
-        const float rstd1 = a.stats[row], rstd2 = a.stats[a.T + row];
-        const float mean1 = a.layer ? a.stats[2 * a.T + row] : 0.0f, mean2 = a.layer ? a.stats[3 * a.T + row] : 0.0f;
-        const T *dn = static_cast<const T *>(a.dN) + row * C;
-        const T *dy = a.dY ? static_cast<const T *>(a.dY) + row * C : nullptr;
-        float sg = 0.0f, sgx = 0.0f;
-        for (int c = threadIdx.x; c < C; c += kThreads) {
-            const float g = load_one(dn + c) * load_param(a.w2, a.w_dtype, c);
-            sg += g;
-            sgx = __builtin_fmaf(g, (Element<T>(a, row, c, mean1, rstd1).y - mean2) * rstd2, sgx);
+    struct Row {
+        const T *dn, *dy;
+        float rstd1, rstd2, mean1, mean2;
+    };
+    auto row_of = [&](int64_t row) {
+        return Row{static_cast<const T *>(a.dN) + row * C, a.dY ? static_cast<const T *>(a.dY) + row * C : nullptr, a.stats[row],
+                   a.stats[a.T + row], a.layer ? a.stats[2 * a.T + row] : 0.0f, a.layer ? a.stats[3 * a.T + row] : 0.0f};
+    };
+    auto grad_y = [&](const Row &r, const Element<T> &e, int c, float mg2, float mgx2) {
+        const float g = load_one(r.dn + c) * load_param(a.w2, a.w_dtype, c), xh2 = (e.y - r.mean2) * r.rstd2;
+        return __builtin_fmaf(r.rstd2, g - mg2 - xh2 * mgx2, r.dy ? load_one(r.dy + c) : 0.0f);
+    };
+    for (int64_t start = first; start < last; start += kLongRows) {
+        const int n = (int)(last - start < kLongRows ? last - start : kLongRows);
+        for (int i = 0; i < n; i++) {
+            const Row r = row_of(start + i);
+            float sg = 0.0f, sgx = 0.0f;
+            for (int c = threadIdx.x; c < C; c += kThreads) {
+                const float g = load_one(r.dn + c) * load_param(a.w2, a.w_dtype, c);
+                sg += g;
+                sgx = __builtin_fmaf(g, (Element<T>(a, start + i, c, r.mean1, r.rstd1).y - r.mean2) * r.rstd2, sgx);
+            }
+            group_sum2(sg, sgx, lds[0]);
+            const float mg2 = a.layer ? sg / (float)C : 0.0f, mgx2 = sgx / (float)C;
+            sg = sgx = 0.0f;
+            for (int c = threadIdx.x; c < C; c += kThreads) {
+                const Element<T> e(a, start + i, c, r.mean1, r.rstd1);
+                const float g = grad_y(r, e, c, mg2, mgx2) * e.gate * load_param(a.w1, a.w_dtype, c);
+                sg += g;
+                sgx = __builtin_fmaf(g, e.xh1, sgx);
+            }
+            group_sum2(sg, sgx, lds[1]);
+            if (threadIdx.x == 0) means[i] = make_float4(mg2, mgx2, a.layer ? sg / (float)C : 0.0f, sgx / (float)C);
         }
-        group_sum2(sg, sgx, lds[0]);
-        const float mg2 = a.layer ? sg / (float)C : 0.0f, mgx2 = sgx / (float)C;
-        auto grad_y = [&](const Element<T> &e, int c) {
-            const float g = load_one(dn + c) * load_param(a.w2, a.w_dtype, c), xh2 = (e.y - mean2) * rstd2;
-            return __builtin_fmaf(rstd2, g - mg2 - xh2 * mgx2, dy ? load_one(dy + c) : 0.0f);
-        };
-        sg = sgx = 0.0f;
+        __syncthreads();
         for (int c = threadIdx.x; c < C; c += kThreads) {
-            const Element<T> e(a, row, c, mean1, rstd1);
-            const float d = grad_y(e, c), dn1 = load_one(dn + c);
-            const float g = d * e.gate * load_param(a.w1, a.w_dtype, c);
-            sg += g;
-            sgx = __builtin_fmaf(g, e.xh1, sgx);
-            const float through = a.gate_kind == kGateToken ? d * e.gate : d;  // a feature's gate is applied to the sum
-            float v[4] = {dn1 * ((e.y - mean2) * rstd2), through * e.xh1, dn1, through};
+            float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+            for (int i = 0; i < n; i++) {
+                const Row r = row_of(start + i);
+                const float4 m = means[i];
+                const Element<T> e(a, start + i, c, r.mean1, r.rstd1);
+                const float dn = load_one(r.dn + c), d = grad_y(r, e, c, m.x, m.y), g = d * e.gate * load_param(a.w1, a.w_dtype, c);
+                const float through = a.gate_kind == kGateToken ? d * e.gate : d;  // a feature's gate is applied to the sum
+                v[0] += dn * ((e.y - r.mean2) * r.rstd2);
+                v[1] += through * e.xh1;
+                v[2] += dn;
+                v[3] += through;
+                const int64_t at = (start + i) * C + c;
+                store_one(static_cast<T *>(a.dX) + at, a.scale * d);
+                store_one(static_cast<T *>(a.dB) + at, r.rstd1 * (g - m.z - e.xh1 * m.w));
+                if (a.gate_kind == kGateToken && a.dgate) store_one(static_cast<T *>(a.dgate) + at, d * e.u);
+            }
             for (int i = 0; i < a.sums; i++) {
                 float *const at = part + i * strip + c;
-                *at = row == first ? v[i] : *at + v[i];
+                *at = start == first ? v[i] : *at + v[i];
             }
         }
-        group_sum2(sg, sgx, lds[1]);
-        const float mg1 = a.layer ? sg / (float)C : 0.0f, mgx1 = sgx / (float)C;
-        for (int c = threadIdx.x; c < C; c += kThreads) {
-            const Element<T> e(a, row, c, mean1, rstd1);
-            const float d = grad_y(e, c), g = d * e.gate * load_param(a.w1, a.w_dtype, c);
-            const int64_t i = row * C + c;
-            store_one(static_cast<T *>(a.dX) + i, a.scale * d);
-            store_one(static_cast<T *>(a.dB) + i, rstd1 * (g - mg1 - e.xh1 * mgx1));
-            if (a.gate_kind == kGateToken && a.dgate) store_one(static_cast<T *>(a.dgate) + i, d * e.u);
-        }
+        __syncthreads();  // the means are read
     }
 }
 
@@ -616,7 +654,8 @@ void sandwich_go(const SandwichArgs &a, bool bias, bool wave, int nv, unsigned t
     const size_t width = (size_t)nv * (wave ? 64 : threads) * 8;
     auto go = [&](auto with_bias, auto of_token) {
         auto *const k = kernel(with_bias, of_token);
-        const size_t lds = Params<decltype(with_bias)::value, decltype(of_token)::value>::bytes(width);  // 128 KB at most
+        // the parameters, 128 KB at most, and where waves take rows by themselves what joins their sums
+        const size_t lds = Params<decltype(with_bias)::value, decltype(of_token)::value>::bytes(width) + (wave ? width * sizeof(float) : 0);
         if (lds > 64 * 1024)
             (void)hipFuncSetAttribute(reinterpret_cast<const void *>(k), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
         k<<<parts, threads, lds, st>>>(a);
@@ -676,6 +715,11 @@ hipError_t launch_sandwich_bwd(int dtype, SandwichArgs a, void *ws, hipStream_t 
     const int64_t parts = sandwich_parts(a.T, a.C, 4);
     a.part = reinterpret_cast<float *>(static_cast<char *>(ws) + kWsHeader);
     a.rows = (a.T + parts - 1) / parts;
+    // rows of a chain of fp32 additions: 64, and where there are more than 64 such chains (a wave has a quarter of the rows up to 1,024
+    // features) the root of their number
+    const int64_t of_one = a.C <= 1024 ? (a.rows + 3) / 4 : a.rows;
+    a.chunk = kChunk;
+    while ((int64_t)a.chunk * a.chunk < of_one) a.chunk++;
     a.sums = a.b1 || a.db1 || a.db2 ? 4 : 2;
     const hipError_t e = dtype == kBF16 ? sandwich_bwd<uint16_t>(a, (unsigned)parts, st) : sandwich_bwd<float>(a, (unsigned)parts, st);
     if (e != hipSuccess) return e;
