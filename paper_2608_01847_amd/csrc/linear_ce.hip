@@ -249,15 +249,19 @@ size_t piece_bytes(int64_t T, int64_t V, int64_t esz) {
 }
 
 constexpr int64_t kMostSplits = 64;
+// of a reduction over R: eight steps of 32 each at least, in fp32 one
+int64_t mfma_most_splits(int64_t R) { return std::min<int64_t>(kMostSplits, cdiv(R, 32) / 8); }
+int64_t f32_most_splits(int64_t R) { return std::min<int64_t>(kMostSplits, cdiv(R, 32)); }
 
-// Splits of a product [M][N] over its reduction R, as the input gradient of a linear has them: whole rounds of 256 x 256 tiles, one
-// per CU, in units of a step of 32 (0.9 us), 8 of them for a tile's end; the fp32 sums written and read (about 4 MB in a unit)
 struct Splits {
     int64_t count, chunk;
 };
-Splits mfma_splits(int64_t R, int64_t M, int64_t N) {
+// Splits of a product [M][N] over its reduction R, as the input gradient of a linear has them, whose sums have `room`: whole rounds of
+// 256 x 256 tiles, one per CU, in units of a step of 32 (0.9 us), 8 of them for a tile's end; the fp32 sums written and read (about 4 MB in
+// a unit)
+Splits mfma_splits(int64_t R, int64_t M, int64_t N, int64_t room) {
     const int64_t tiles = cdiv(M, kCeTile) * cdiv(N, kCeTile), steps = cdiv(R, 32);
-    const int64_t most = tiles >= 4 * 256 ? 1 : std::min<int64_t>(std::min<int64_t>(kMostSplits, steps / 8), kDxSums / (M * N));
+    const int64_t most = tiles >= 4 * 256 ? 1 : std::min(mfma_most_splits(R), std::min(room, kDxSums) / (M * N));
     int64_t best = -1, count = 1;
     for (int64_t s = 1; s <= std::max<int64_t>(1, most); s++) {
         const int64_t cost = cdiv(tiles * s, 256) * (cdiv(steps, s) + 8) + (s > 1 ? s * M * N * 8 / 4000000 + 4 : 0);
@@ -267,12 +271,19 @@ Splits mfma_splits(int64_t R, int64_t M, int64_t N) {
     return {cdiv(R, chunk), chunk};
 }
 
-// fp32 sums of the splits: one of dX, or as many of dX or dW as kDxSums holds
-size_t sums_bytes(int64_t T, int64_t V, int64_t K) {
-    const int64_t rows = std::max(T, std::min(cdiv(V, 256) * 256, kCeMostWidth));
-    const int64_t many = rows > kDxSums / K / kMostSplits ? kDxSums : kMostSplits * rows * K;
-    return round256((size_t)std::max(T * K, many) * sizeof(float));
+// Room for the fp32 sums of the splits, in elements: one of dX, or of dX and of the widest piece's dW as many as the rules below may take.
+// Splitting saves less than the time of a reduction's steps in one tile, which the sums' own must stay below: `worth` elements of them a
+// step. It grows with T: a workspace serves fewer tokens too.
+int64_t sums_room(int64_t T, int64_t V, int64_t K, int64_t (*splits)(int64_t), int64_t worth) {
+    const int64_t rows = std::min(cdiv(V, 256) * 256, kCeMostWidth);
+    auto many = [&](int64_t R, int64_t n) {
+        const int64_t count = splits(R), most = std::min(kDxSums, worth * (cdiv(R, 32) + 8));
+        return count <= 1 ? 0 : n > most / K / count ? most : count * n * K;
+    };
+    return std::max(T * K, std::max(many(V, T), many(T, rows)));
 }
+int64_t mfma_room(int64_t T, int64_t V, int64_t K) { return sums_room(T, V, K, mfma_most_splits, 500000); }
+int64_t f32_room(int64_t T, int64_t V, int64_t K) { return sums_room(T, V, K, f32_most_splits, 690 * 560); }
 
 struct MfmaSpace {
     float *r, *rest, *most, *sums, *part;
@@ -288,7 +299,7 @@ size_t mfma_space(int64_t T, int64_t V, int64_t K, char *base, MfmaSpace *s) {
     };
     char *const most = take(sizeof(float)), *const r = take((size_t)T * sizeof(float)), *const rest = take((size_t)T * sizeof(float));
     char *const place = take((size_t)T * sizeof(int32_t)), *const x = take((size_t)T * (size_t)K * 2);
-    char *const sums = take((size_t)T * (size_t)K * sizeof(float)), *const part = take(sums_bytes(T, V, K));
+    char *const sums = take((size_t)T * (size_t)K * sizeof(float)), *const part = take((size_t)mfma_room(T, V, K) * sizeof(float));
     char *const D = take(piece_bytes(T, V, 2));
     if (s)
         *s = MfmaSpace{reinterpret_cast<float *>(r),    reinterpret_cast<float *>(rest), reinterpret_cast<float *>(most),
@@ -302,9 +313,9 @@ size_t mfma_space(int64_t T, int64_t V, int64_t K, char *base, MfmaSpace *s) {
 // where it has one, 0.56 of two and 0.51 of three, which is how many run at once, 1.5 us for their start and end; the sums' launch, and
 // what it and the tiles move. dX of 1,024 x 10,000 x 1,024 (256 tiles) 217 us unsplit, 175 in two and 162 in three, of 301 x 5,003 x 1,008
 // (80 tiles) 48 in three and 41 in six, of 100 x 8,000 x 2,048 (64) 48 in four and 40 in eight.
-Splits f32_splits(int64_t R, int64_t N, int64_t K) {
+Splits f32_splits(int64_t R, int64_t N, int64_t K, int64_t room) {
     const int64_t tiles = cdiv(N, 64) * cdiv(K, 64), steps = cdiv(R, 32), cus = 256;
-    const int64_t most = tiles >= 16 * cus ? 1 : std::min<int64_t>(std::min<int64_t>(kMostSplits, steps), kDxSums / (N * K));
+    const int64_t most = tiles >= 16 * cus ? 1 : std::min(f32_most_splits(R), std::min(room, kDxSums) / (N * K));
     int64_t best = -1, count = 1;
     for (int64_t s = 1; s <= std::max<int64_t>(1, most); s++) {
         const int64_t on_cu = cdiv(tiles * s, cus), step = on_cu == 1 ? 690 : on_cu == 2 ? 560 : 510;
@@ -319,7 +330,7 @@ struct F32Space {
     float *sums, *part, *x, *D, *Dt;
 };
 size_t f32_space(int64_t T, int64_t V, int64_t K, char *base, F32Space *s) {
-    const size_t x = round256((size_t)T * (size_t)K * sizeof(float)), part = sums_bytes(T, V, K);
+    const size_t x = round256((size_t)T * (size_t)K * sizeof(float)), part = round256((size_t)f32_room(T, V, K) * sizeof(float));
     const size_t D = round256(piece_bytes((T + 3) / 4 * 4, V, sizeof(float)));  // transposed too, its rows of whole fours
     size_t at = kWsHeader;
     auto take = [&](size_t bytes) {
@@ -336,6 +347,7 @@ hipError_t bwd_f32(CeArgs a, float *dX, float *dW, uint32_t *flag, char *ws, hip
     F32Space s;
     f32_space(a.T, a.V, a.K, ws, &s);
     const int64_t T = a.T, V = a.V, K = a.K, width = piece_width((T + 3) / 4 * 4, V, sizeof(float)), pitch_t = (T + 3) / 4 * 4;
+    const int64_t room = f32_room(T, V, K);
     a.D = s.D;
     auto finish = [&](int64_t splits, const float *before, int64_t n, float *sums, float *out) {
         return in_elements(n, [&](int64_t first, unsigned grid) {
@@ -351,14 +363,14 @@ hipError_t bwd_f32(CeArgs a, float *dX, float *dW, uint32_t *flag, char *ws, hip
         });
         if (e != hipSuccess) return e;
         if (dX) {
-            const Splits p = f32_splits(n, T, K);
+            const Splits p = f32_splits(n, T, K, room);
             const bool alone = p.count == 1 && n == V;
             e = launch_dw_f32(s.Dt, static_cast<const float *>(a.W) + v0 * K, n, T, pitch_t, K, p.chunk, p.count, alone ? dX : s.part, st);
             if (e == hipSuccess && !alone) e = finish(p.count, v0 ? s.sums : nullptr, T * K, v0 + n == V ? nullptr : s.sums, dX);
             if (e != hipSuccess) return e;
         }
         if (dW) {
-            const Splits p = f32_splits(T, n, K);
+            const Splits p = f32_splits(T, n, K, room);
             float *const out = dW + v0 * K;
             e = launch_dw_f32(s.D, s.x, T, n, a.pitch, K, p.chunk, p.count, p.count == 1 ? out : s.part, st);
             if (e == hipSuccess && p.count > 1) e = finish(p.count, nullptr, n * K, nullptr, out);
@@ -371,7 +383,7 @@ hipError_t bwd_f32(CeArgs a, float *dX, float *dW, uint32_t *flag, char *ws, hip
 hipError_t bwd_mfma(CeArgs a, void *dX, void *dW, int dw_dtype, uint32_t *flag, char *ws, hipStream_t st) {
     MfmaSpace s;
     mfma_space(a.T, a.V, a.K, ws, &s);
-    const int64_t T = a.T, V = a.V, K = a.K;
+    const int64_t T = a.T, V = a.V, K = a.K, room = mfma_room(T, V, K);
     ce_scales_kernel<<<1, 1024, 0, st>>>(a.target, a.g, a.h, T, V, s.r, s.place, s.most);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
@@ -396,7 +408,7 @@ hipError_t bwd_mfma(CeArgs a, void *dX, void *dW, int dw_dtype, uint32_t *flag, 
         if (e != hipSuccess) return e;
         const char *const W = static_cast<const char *>(a.W) + (size_t)v0 * (size_t)K * 2;
         if (dX) {
-            const Splits p = mfma_splits(n, T, K);
+            const Splits p = mfma_splits(n, T, K, room);
             e = launch_dx_sums(s.D, W, T, n, width, K, p.chunk, p.count, s.part, st);
             if (e != hipSuccess) return e;
             const bool last = v0 + n == V;
@@ -408,7 +420,7 @@ hipError_t bwd_mfma(CeArgs a, void *dX, void *dW, int dw_dtype, uint32_t *flag, 
         }
         if (dW) {
             char *const out = static_cast<char *>(dW) + (size_t)v0 * (size_t)K * (dw_dtype == kBF16 ? 2 : 4);
-            const Splits p = mfma_splits(T, n, K);
+            const Splits p = mfma_splits(T, n, K, room);
             e = launch_dw_mfma(s.D, s.x, T, n, width, K, p.chunk, p.count, s.most, place, s.rest, v0, out, dw_dtype, s.part, st);
             if (e != hipSuccess) return e;
             if (p.count > 1)
