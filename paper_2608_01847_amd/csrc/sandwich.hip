@@ -34,6 +34,7 @@ __device__ __forceinline__ void group_sum2(float &a, float &b, float *lds) {
     }
     __syncthreads();
     a = b = 0.0f;
+#pragma unroll 4  // four reads under way: one by one, 16 waves take 0.7 us a row
     for (unsigned i = 0; i < blockDim.x / 64; i++) {
         a += lds[i];
         b += lds[16 + i];
@@ -241,12 +242,16 @@ __global__ void __launch_bounds__(WAVE ? kThreads : kMostThreads) sandwich_fwd_k
 // Rows, threads and the next row's pieces as in the forward; the sums over the rows stay in registers, for `chunk` of them (64 as a
 // rule, so that no chain of fp32 additions is as long as a workgroup's rows), and are then added to its row of partial sums (waves
 // that take rows by themselves are added in order through LDS first). BIAS: the sums without xh too.
-// Memory and its latency bound it: 65,536 x 2,560 bf16 459 us, 4.4 TB/s, bytes 1.00 times the tensors', without a gradient of Y 407;
-// 8,192 x 8,192 with token gates 192 us, 5.6 TB/s. The next row's B and gates have registers of their own where there are as many (bf16,
-// rows of whole eights), since the present ones are needed to the row's end: fetched there they took 485, 465 and 198 us; dN and dY the same
-// way 468 and 440. Before, at 65,536 x 2,560, a workgroup of 256 threads with two vectors each took 8% longer than one of five waves, that
-// without the next row under way 20% and with the parameters converted anew for each row 6%. A wave per row: 131,072 x 1,024 295 us,
-// 4.5 TB/s; 262,144 x 512 with token gates 444.
+// Memory and its latency bound rows of whole eights: 65,536 x 2,560 bf16 458 us, 4.4 TB/s, bytes 1.00 times the tensors', without a
+// gradient of Y 408; 8,192 x 8,192 with token gates 213 us, 5.0 TB/s; 16,384 x 8,192 fp32 632 us, 5.1 TB/s. The next row's B and gates have
+// registers of their own where there are as many (bf16, whole eights), since the present ones are needed to the row's end: fetched there
+// 65,536 x 2,560 took 6% longer; dN and dY the same way 2 and 8%. Before, a workgroup of 256 threads with two vectors each took 8% longer
+// than one of five waves, that without the next row under way 20% and with the parameters converted anew for each row 6%. A wave per row:
+// 131,072 x 1,024 339 us, 4.8 TB/s; 262,144 x 512 with token gates 458.
+// Rows that are no whole eights take more registers (addresses, the last piece's branches) than the 128 that 1,024 threads leave each: in
+// fp32 33 of them go to memory with shifts and token gates, 17 with shifts, 12 with token gates, 1 otherwise, in bf16 8 with both (2 in
+// fp32 rows of whole eights with both, none elsewhere). Layer norm, token gates and shifts, 32,768 x 2,561 fp32 896 us, 3.0 TB/s, x 2,560
+// 564, 4.8; bf16 444 and 325; 8,192 x 5,001 fp32 487, 2.7 TB/s.
 template <typename T, bool WAVE, int NV, bool BIAS, bool TOKEN, bool TAIL>
 __global__ void __launch_bounds__(WAVE ? kThreads : kMostThreads) sandwich_bwd_kernel(SandwichArgs a) {
     constexpr int kRows = WAVE ? 4 : 1;
@@ -465,7 +470,7 @@ struct Element {
 };
 
 // Rows of more than 8,192 features, which registers and LDS do not hold: a workgroup per row, which it reads once for each sum and once
-// for the outputs, element by element. Not tuned: 2,048 x 8,200 bf16 78 us, backward 646 (x 8,192 25 and 45).
+// for the outputs, element by element. Not tuned: 2,048 x 8,200 bf16 79 us, backward 517 (x 8,192 25 and 44).
 template <typename T>
 __global__ void __launch_bounds__(kThreads) sandwich_fwd_long_kernel(SandwichArgs a) {
     __shared__ float lds[2][32];
