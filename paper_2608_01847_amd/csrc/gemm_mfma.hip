@@ -747,7 +747,8 @@ __device__ __forceinline__ void rest_products(const int32_t *__restrict__ place,
 
 // The plain product dW [N][K] = (dY + R)^T X, times *factor: dY [M][ldy] with N real columns (the others up to the tile's end exist and
 // are not stored), R as above with `place`. With `part` a token range of `chunk` per split, whose fp32 sums go to part [split][N][K]. Bound
-// as the backward whose main loop it has: 8,192 tokens x 32,768 x 2,560 1.06 to 1.08 ms, 1.27 PFLOP/s; the tile leaves through LDS in 16-byte pieces.
+// as the backward whose main loop it has: 8,192 tokens x 32,768 x 2,560 1.14 to 1.17 ms, 1.18 to 1.2 PFLOP/s (without R 1.06 to 1.08); the tile
+// leaves through LDS in 16-byte pieces.
 __global__ void __launch_bounds__(kThreads, 1)
 dw_mfma_kernel(const uint16_t *__restrict__ dY, const uint16_t *__restrict__ X, int64_t M, int64_t N, int64_t ldy, int64_t K,
                int64_t chunk, const float *__restrict__ factor, const int32_t *__restrict__ place, const float *__restrict__ rest,

@@ -97,8 +97,8 @@ __device__ __forceinline__ float power_below(float v) {
 }
 
 // r[t] of max(|g|, |h|) of the tokens (g: 0 where left out), their targets' places in the vocabulary (-1: none, or no gradient) and G, the
-// largest r, by one workgroup: 4,096 tokens 6 us, 8,192 9. (As part of the next kernel, every workgroup of which forms G then, no faster:
-// 1,500 x 3,001 x 512 backward 69 us, so 72.)
+// largest r, by one workgroup: 4,096 tokens 7 us, 8,192 12. (As part of the next kernel, every workgroup of which forms G then, no faster:
+// 1,500 x 3,001 x 512 backward 3 us longer.)
 __global__ void __launch_bounds__(1024) ce_scales_kernel(const int64_t *__restrict__ target, const float *__restrict__ g,
                                                          const float *__restrict__ h, int64_t T, int64_t V, float *__restrict__ r,
                                                          int32_t *__restrict__ place, float *__restrict__ most) {
@@ -139,8 +139,9 @@ __global__ void __launch_bounds__(256) ce_scale_x_kernel(const uint16_t *__restr
 }
 
 // total = before + the splits' sums in order; to `sums` in fp32, or, with rest[t] W[place[t]] where `place` is given, times the row's (or
-// everything's, or no) factor to `out`. Bound by memory: three splits of 8,192 x 2,560, the sum so far and the new one 63 us, 6.6 TB/s (the splits partly from the caches); many splits
-// of little by their latency, hence eight under way (63 of 64 x 512: 9 us, one at a time 16)
+// everything's, or no) factor to `out`. Bound by memory: three splits of 8,192 x 2,560, the sum so far and the new one 63 us, 6.6 TB/s (the
+// splits partly from the caches), of 4,096 x 2,560 with `rest` 27 us, without 23; many splits of little by their latency, hence eight under
+// way (63 of 64 x 512: 9 us, one at a time 16)
 __global__ void __launch_bounds__(256) ce_sums_kernel(const float *__restrict__ part, int64_t splits, const float *__restrict__ before,
                                                       const float *__restrict__ factor, int per_row, const int32_t *__restrict__ place,
                                                       const float *__restrict__ rest, const uint16_t *__restrict__ W, int64_t first,
@@ -205,8 +206,8 @@ hipError_t in_elements(int64_t n, F &&f) {
 int64_t padded(int64_t K) { return (K + 15) / 16 * 16; }
 
 // out [rows][to] = in [rows][from] with zeros behind, or without what is behind; a wave per row, element by element (rows start
-// anywhere), eight under way. Bound by memory: 32,000 x 2,561 bf16 64 us, 5.1 TB/s. 4,096 tokens x 32,000 x 2,561 take 769 us forward and
-// 2.21 ms backward with it, with 2,560 features 640 and 1.77.
+// anywhere), eight under way. Bound by memory: 32,000 x 2,561 bf16 64 us, 5.1 TB/s. 4,096 tokens x 32,000 x 2,561 take 745 us forward and
+// 2.24 ms backward with it, with 2,560 features 650 and 1.85.
 template <typename T>
 __global__ void __launch_bounds__(256) ce_pad_kernel(const T *__restrict__ in, int64_t first, int64_t rows, int64_t from, int64_t to,
                                                      T *__restrict__ out) {
@@ -235,9 +236,8 @@ hipError_t copy_rows(int dtype, const void *in, int64_t rows, int64_t from, int6
 // bytes of a padded copy, of fp32 elements
 size_t pad_bytes(int64_t rows, int64_t K) { return K % 16 ? round256((size_t)rows * (size_t)padded(K) * sizeof(float)) : 0; }
 
-// Pieces of the vocabulary, of D takes 512 MiB each at most (in fp32, whose products are slower against what a piece costs, 128 MiB; a
-// tile's 256 entries each at least); the last one is what is left. 8,192 tokens, vocabulary 151,936, both
-// ways: 22.0 ms, with 1 GiB 22.1.
+// Pieces of the vocabulary, of which D takes 512 MiB each at most (in fp32, whose products are slower against what a piece costs, 128 MiB; a
+// tile's 256 entries each at least); the last one is what is left. With 1 GiB 8,192 tokens, vocabulary 151,936, both ways, take 0.5% longer.
 constexpr int64_t piece_most(int64_t esz) { return int64_t(1) << (esz == 2 ? 29 : 27); }
 int64_t piece_width(int64_t T, int64_t V, int64_t esz) {
     const int64_t fit = std::max<int64_t>(1, std::min(piece_most(esz) / (T * esz), kCeMostWidth) / 256);
